@@ -522,6 +522,73 @@ size_t puro_muonh_grouped_workspace_size(const puro_muonh_matrix_t *mats, int32_
 puro_status_t puro_muonh_step_grouped(const puro_muonh_matrix_t *mats, int32_t count, double eta, double *sums,
                                       void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * RMSNorm of each query and key head with the position rotation in the same
+ * pass, and its backward.
+ *
+ * The model normalises queries and keys head by head and rotates them by their
+ * positions ahead of the attention (section "Model architecture and
+ * pretraining system": the Qwen3 architecture).  Per token t and head, with
+ * D = head_dim:
+ *     rstd = 1 / sqrt(mean_c x[c]^2 + eps)
+ *     n[c] = (x[c] * rstd) * gain[c]
+ *     y    = R(pos[t]) n
+ * in FP32, y rounded to BF16 once.  R turns the first rot_dim channels in
+ * pairs by the angles whose cosines and sines the tables hold:
+ *     (a, b) -> (a cos - b sin, b cos + a sin),   a = n[i], b = n[i + rot_dim/2]
+ * (interleaved: a = n[2i], b = n[2i + 1]), i < rot_dim/2; the other channels
+ * pass unturned.  Backward, with xh = x * rstd and dn = R^T dy:
+ *     dgain[c] = sum over tokens and heads of dn[c] * xh[c]
+ *     dx = rstd * (dn * gain - xh * mean(dn * gain * xh))
+ *
+ *   q, k, ...: the heads as strided views (puro_heads_t), for instance of one
+ *     qkv output, of [tokens, heads, D] or of [heads, tokens, D].  Data 16-byte
+ *     aligned; strides >= 0, multiples of 8 elements, outputs' of at least D
+ *     where there is more than one token or head (heads of one output must not
+ *     overlap).  A view without heads may be NULL.
+ *   head_dim: a multiple of 16 up to 256.  rot_dim: a multiple of 16 up to
+ *     head_dim; 0 for the norm alone (the tables may then be NULL).
+ *   q_gain, k_gain: bf16 [D], 16-byte aligned, or NULL for no gain.
+ *   cos, sin: fp32 [max_positions, rot_dim/2], 16-byte aligned.
+ *   positions: int32 [tokens], or NULL: token t is at position t (then tokens
+ *     <= max_positions).  A negative position marks a padding row: its y is
+ *     zero and its rstd 0 (backward: dx is zero and the row adds nothing to the
+ *     gains' gradients), whatever the row holds.  A position past the tables
+ *     gives NaN in the row (y, rstd; dx and the gains' gradients) and stores
+ *     PURO_ERR_INVALID_ARG in *dev_status when dev_status is non-NULL; the
+ *     tables are not read there.
+ *   q_out, k_out: y.  They may be q and k themselves (same strides).
+ *   rstd: fp32 [tokens, q heads + k heads], the query heads first; written by
+ *     the forward pass (optional, NULL: not), read by the backward pass.
+ *   dq_out, dk_out: dy.  dq, dk: dx, which may be dq_out and dk_out themselves.
+ *   dq_gain, dk_gain: fp32 [D], written, or NULL.  They are sums in a fixed
+ *     order, through the workspace: 4-byte aligned scratch of
+ *     puro_qk_norm_rope_workspace_size bytes (only with a gain's gradient).
+ * One kernel; the backward with a gain's gradient two.
+ */
+typedef struct {
+    void *data;            /* device, bf16: channel c of head h of token t at      */
+    int64_t token_stride;  /*   data[t * token_stride + h * head_stride + c]       */
+    int64_t head_stride;
+    int32_t heads;
+    int32_t reserved;      /* must be 0                                            */
+} puro_heads_t;
+
+puro_status_t puro_qk_norm_rope(const puro_heads_t *q, const puro_heads_t *k, int64_t tokens, int32_t head_dim,
+                                const void *q_gain, const void *k_gain, float eps, const float *cos,
+                                const float *sin, int64_t max_positions, int32_t rot_dim, int32_t interleaved,
+                                const int32_t *positions, const puro_heads_t *q_out, const puro_heads_t *k_out,
+                                float *rstd, int32_t *dev_status, void *stream);
+puro_status_t puro_qk_norm_rope_backward(const puro_heads_t *dq_out, const puro_heads_t *dk_out,
+                                         const puro_heads_t *q, const puro_heads_t *k, const float *rstd,
+                                         int64_t tokens, int32_t head_dim, const void *q_gain, const void *k_gain,
+                                         const float *cos, const float *sin, int64_t max_positions, int32_t rot_dim,
+                                         int32_t interleaved, const int32_t *positions, const puro_heads_t *dq,
+                                         const puro_heads_t *dk, float *dq_gain, float *dk_gain, void *workspace,
+                                         size_t workspace_bytes, int32_t *dev_status, void *stream);
+/* Bytes of scratch for the gains' gradients.  Host-only, no CUDA call. */
+size_t puro_qk_norm_rope_workspace_size(int64_t tokens, int32_t q_heads, int32_t k_heads, int32_t head_dim);
+
 /* Human-readable name of a status code (static string). */
 const char *puro_status_string(puro_status_t s);
 

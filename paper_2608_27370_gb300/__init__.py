@@ -98,6 +98,11 @@ _SIGNATURES = {
     "puro_bf16_linear_fprop": (_I32, [_P, _P, _P, _I64, _I64, _I64, _P, _P]),
     "puro_bf16_linear_dgrad": (_I32, [_P, _P, _P, _I64, _I64, _I64, _P, _P]),
     "puro_bf16_linear_wgrad": (_I32, [_P, _P, _P, _I64, _I64, _I64, _P, _P]),
+    "puro_qk_norm_rope": (_I32, [_P, _P, _I64, _I32, _P, _P, ctypes.c_float, _P, _P, _I64, _I32, _I32, _P, _P, _P, _P, _P,
+                                 _P]),
+    "puro_qk_norm_rope_backward": (_I32, [_P, _P, _P, _P, _P, _I64, _I32, _P, _P, _P, _P, _I64, _I32, _I32, _P, _P, _P, _P,
+                                          _P, _P, ctypes.c_size_t, _P, _P]),
+    "puro_qk_norm_rope_workspace_size": (ctypes.c_size_t, [_I64, _I32, _I32, _I32]),
     "puro_set_wait_timeout_ns": (None, [ctypes.c_uint64]),
     "puro_set_gemm_tile_n": (ctypes.c_int, [ctypes.c_int32]),
     "puro_status_string": (ctypes.c_char_p, [_I32]),
@@ -558,6 +563,127 @@ def puro_bf16_linear_dgrad(dy, w_t, dx, M, N, K, dev_status=None, stream=None) -
 
 def puro_bf16_linear_wgrad(dy_t, x_t, dw, M, N, K, dev_status=None, stream=None) -> None:
     _bf16("puro_bf16_linear_wgrad", dy_t, x_t, dw, M, N, K, dev_status, stream)
+
+
+# --------------------------------------------------------------------------
+# Query and key norms with the position rotation
+# --------------------------------------------------------------------------
+def _current_device() -> int:
+    return torch.cuda.current_device()
+
+
+def _on_current_device(*tensors) -> None:
+    """Kernels are launched on the current device: every tensor has to be there."""
+    here = _current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != here:
+            raise ValueError(f"a tensor is on cuda:{t.get_device()}, the current device is cuda:{here}")
+
+
+class puro_heads_t(ctypes.Structure):
+    """Mirror of the C struct puro_heads_t."""
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("heads", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+def _heads(t: Optional[torch.Tensor], name: str, tokens: int, channels: int):
+    """The C view of a bf16 [tokens, heads, channels] tensor with unit channel stride."""
+    if t is None:
+        return puro_heads_t()
+    if not t.is_cuda or t.dtype != torch.bfloat16 or t.dim() != 3:
+        raise ValueError(f"{name} must be a bf16 CUDA tensor [tokens, heads, head_dim]")
+    if t.shape[0] != tokens or t.shape[2] != channels:
+        raise ValueError(f"{name} is {tuple(t.shape)}, expected {tokens} tokens of {channels} channels")
+    if t.numel() and t.stride(2) != 1:
+        raise ValueError(f"{name} must have unit channel stride")
+    return puro_heads_t(t.data_ptr() or None, t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0,
+                        t.shape[1], 0)
+
+
+def _sized(t: Optional[torch.Tensor], dtype, n: int, name: str) -> Optional[int]:
+    if t is not None and t.numel() != n:
+        raise ValueError(f"{name} has {t.numel()} values, expected {n}")
+    return _ptr(t, dtype, name)
+
+
+def _tables(cos, sin):
+    if cos is None and sin is None:
+        return None, None, 0, 0
+    if cos is None or sin is None or cos.dim() != 2 or cos.shape != sin.shape:
+        raise ValueError("cos and sin must be two tables [positions, rot_dim / 2] of one shape")
+    return (_ptr(cos, torch.float32, "cos"), _ptr(sin, torch.float32, "sin"), cos.shape[0], 2 * cos.shape[1])
+
+
+def puro_qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], q_gain: Optional[torch.Tensor],
+                      k_gain: Optional[torch.Tensor], eps: float, cos: Optional[torch.Tensor],
+                      sin: Optional[torch.Tensor], positions: Optional[torch.Tensor], interleaved: bool,
+                      q_out: Optional[torch.Tensor], k_out: Optional[torch.Tensor], rstd: Optional[torch.Tensor] = None,
+                      dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """RMSNorm of each query and key head (bf16 [tokens, heads, head_dim]
+    views, for instance of one qkv output; optional bf16 gains) and the
+    rotation by the tokens' positions (fp32 tables cos and sin [positions,
+    rot_dim / 2], None for the norm alone) in one pass: q_out, k_out (which may
+    be q and k) and rstd (fp32 [tokens, q heads + k heads]) for the backward.
+    positions: int32 [tokens], None for 0, 1, ...; a negative one marks a
+    padding row, whose output is zero."""
+    _on_current_device(q, k, q_gain, k_gain, cos, sin, positions, q_out, k_out, rstd, dev_status)
+    st = (_native or _load_native()).puro_qk_norm_rope(q, k, q_gain, k_gain, eps, cos, sin, positions, interleaved, q_out,
+                                                       k_out, rstd, dev_status, stream)
+    if st is not None:
+        return _check("puro_qk_norm_rope", st)
+    some = q if q is not None else k
+    if some is None or some.dim() != 3:
+        raise ValueError("q or k must be a bf16 CUDA tensor [tokens, heads, head_dim]")
+    tokens, _, d = some.shape
+    h = [_heads(t, n, tokens, d) for t, n in ((q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out"))]
+    cp, sp, npos, rot = _tables(cos, sin)
+    st = load_library().puro_qk_norm_rope(
+        ctypes.byref(h[0]), ctypes.byref(h[1]), tokens, d, _sized(q_gain, torch.bfloat16, d, "q_gain"),
+        _sized(k_gain, torch.bfloat16, d, "k_gain"), float(eps), cp, sp, npos, rot, int(bool(interleaved)),
+        _sized(positions, torch.int32, tokens, "positions"), ctypes.byref(h[2]), ctypes.byref(h[3]),
+        _sized(rstd, torch.float32, tokens * (h[0].heads + h[1].heads), "rstd"),
+        _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
+    _check("puro_qk_norm_rope", st)
+
+
+def puro_qk_norm_rope_backward(dq_out: Optional[torch.Tensor], dk_out: Optional[torch.Tensor],
+                               q: Optional[torch.Tensor], k: Optional[torch.Tensor], rstd: torch.Tensor,
+                               q_gain: Optional[torch.Tensor], k_gain: Optional[torch.Tensor],
+                               cos: Optional[torch.Tensor], sin: Optional[torch.Tensor],
+                               positions: Optional[torch.Tensor], interleaved: bool, dq: Optional[torch.Tensor],
+                               dk: Optional[torch.Tensor], dq_gain: Optional[torch.Tensor] = None,
+                               dk_gain: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                               dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Backward of puro_qk_norm_rope from the gradients of its outputs, its
+    inputs and rstd: dq, dk (bf16 views, which may be dq_out and dk_out) and the
+    gains' gradients (fp32 [head_dim], through a workspace of
+    puro_qk_norm_rope_workspace_size bytes)."""
+    _on_current_device(dq_out, dk_out, q, k, rstd, q_gain, k_gain, cos, sin, positions, dq, dk, dq_gain, dk_gain, workspace,
+                       dev_status)
+    st = (_native or _load_native()).puro_qk_norm_rope_backward(dq_out, dk_out, q, k, rstd, q_gain, k_gain, cos, sin,
+                                                                positions, interleaved, dq, dk, dq_gain, dk_gain, workspace,
+                                                                dev_status, stream)
+    if st is not None:
+        return _check("puro_qk_norm_rope_backward", st)
+    some = q if q is not None else k
+    if some is None or some.dim() != 3:
+        raise ValueError("q or k must be a bf16 CUDA tensor [tokens, heads, head_dim]")
+    tokens, _, d = some.shape
+    h = [_heads(t, n, tokens, d) for t, n in ((dq_out, "dq_out"), (dk_out, "dk_out"), (q, "q"), (k, "k"), (dq, "dq"),
+                                              (dk, "dk"))]
+    cp, sp, npos, rot = _tables(cos, sin)
+    st = load_library().puro_qk_norm_rope_backward(
+        *[ctypes.byref(x) for x in h[:4]], _sized(rstd, torch.float32, tokens * (h[2].heads + h[3].heads), "rstd"), tokens, d,
+        _sized(q_gain, torch.bfloat16, d, "q_gain"), _sized(k_gain, torch.bfloat16, d, "k_gain"), cp, sp, npos, rot,
+        int(bool(interleaved)), _sized(positions, torch.int32, tokens, "positions"), ctypes.byref(h[4]), ctypes.byref(h[5]),
+        _sized(dq_gain, torch.float32, d, "dq_gain"), _sized(dk_gain, torch.float32, d, "dk_gain"),
+        _ptr(workspace, None, "workspace"), workspace.numel() * workspace.element_size() if workspace is not None else 0,
+        _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
+    _check("puro_qk_norm_rope_backward", st)
+
+
+def puro_qk_norm_rope_workspace_size(tokens: int, q_heads: int, k_heads: int, head_dim: int) -> int:
+    return int(load_library().puro_qk_norm_rope_workspace_size(tokens, q_heads, k_heads, head_dim))
 
 
 def puro_set_wait_timeout_ns(ns: int) -> None:

@@ -721,6 +721,127 @@ PURO_API puro_status_t puro_bf16_linear_wgrad(const void *dy_t, const void *x_t,
     return bf16_gemm(dy_t, x_t, dw, N, K, M, dev_status, stream);
 }
 
+// ------------------------------------------------------ query and key norms
+namespace puro {
+namespace {
+
+// The view h as kernels take it; false for one that the header does not allow.
+bool take_heads(const puro_heads_t *h, int64_t tokens, int32_t D, bool written, QkHeads *out) {
+    *out = QkHeads{};
+    if (!h) return true;
+    if (h->heads < 0 || h->reserved != 0 || h->token_stride < 0 || h->head_stride < 0 || h->token_stride % 8 ||
+        h->head_stride % 8)
+        return false;
+    if (h->heads == 0) return true;
+    if (tokens > 0 && (!h->data || !aligned16(h->data))) return false;
+    if (written && ((tokens > 1 && h->token_stride < D) || (h->heads > 1 && h->head_stride < D))) return false;
+    *out = QkHeads{static_cast<uint16_t *>(h->data), h->token_stride, h->head_stride, h->heads};
+    return true;
+}
+
+// The checks both directions share.
+puro_status_t check_qk(const QkArgs &p) {
+    if (p.tokens < 0 || p.D < 16 || p.D > 256 || p.D % 16 || p.rot < 0 || p.rot > p.D || p.rot % 16 || p.max_positions < 0)
+        return PURO_ERR_INVALID_ARG;
+    if (!aligned16(p.q_gain) || !aligned16(p.k_gain)) return PURO_ERR_INVALID_ARG;
+    if (p.rot > 0) {
+        if (p.max_positions > 0 && (!p.cos || !p.sin)) return PURO_ERR_INVALID_ARG;
+        if (!aligned16(p.cos) || !aligned16(p.sin)) return PURO_ERR_INVALID_ARG;
+        if (!p.positions && p.tokens > p.max_positions) return PURO_ERR_INVALID_ARG;
+    }
+    if ((reinterpret_cast<uintptr_t>(p.positions) & 3u) || (reinterpret_cast<uintptr_t>(p.rstd) & 3u) ||
+        (reinterpret_cast<uintptr_t>(p.status) & 3u))
+        return PURO_ERR_INVALID_ARG;
+    if (p.q.heads != p.q_out.heads || p.k.heads != p.k_out.heads) return PURO_ERR_INVALID_ARG;
+    if (p.tokens > INT32_MAX || p.q.heads > 65535 || p.k.heads > 65535) return PURO_ERR_UNSUPPORTED;
+    return PURO_OK;
+}
+
+}  // namespace
+}  // namespace puro
+
+PURO_API puro_status_t puro_qk_norm_rope(const puro_heads_t *q, const puro_heads_t *k, int64_t tokens, int32_t head_dim,
+                                         const void *q_gain, const void *k_gain, float eps, const float *cos,
+                                         const float *sin, int64_t max_positions, int32_t rot_dim, int32_t interleaved,
+                                         const int32_t *positions, const puro_heads_t *q_out, const puro_heads_t *k_out,
+                                         float *rstd, int32_t *dev_status, void *stream) {
+    QkArgs p{};
+    p.tokens = tokens;
+    p.D = head_dim;
+    p.rot = rot_dim;
+    p.inter = interleaved != 0;
+    p.q_gain = static_cast<const uint16_t *>(q_gain);
+    p.k_gain = static_cast<const uint16_t *>(k_gain);
+    p.eps = eps;
+    p.cos = cos;
+    p.sin = sin;
+    p.max_positions = max_positions;
+    p.positions = positions;
+    p.rstd = rstd;
+    p.status = dev_status;
+    if (!(eps >= 0.0f)) return PURO_ERR_INVALID_ARG;
+    if (!take_heads(q, tokens, head_dim, false, &p.q) || !take_heads(k, tokens, head_dim, false, &p.k) ||
+        !take_heads(q_out, tokens, head_dim, true, &p.q_out) || !take_heads(k_out, tokens, head_dim, true, &p.k_out))
+        return PURO_ERR_INVALID_ARG;
+    const puro_status_t st = check_qk(p);
+    if (st != PURO_OK) return st;
+    if (tokens == 0 || p.q.heads + p.k.heads == 0) return PURO_OK;
+    return cuda_status(launch_qk_norm_rope(p, static_cast<cudaStream_t>(stream)));
+}
+
+PURO_API size_t puro_qk_norm_rope_workspace_size(int64_t tokens, int32_t q_heads, int32_t k_heads, int32_t head_dim) {
+    if (tokens <= 0 || q_heads < 0 || k_heads < 0 || head_dim <= 0 || head_dim > 256) return 0;
+    int q_blocks = 0, blocks = 0;
+    qk_backward_blocks(tokens, q_heads, k_heads, head_dim, &q_blocks, &blocks);
+    return static_cast<size_t>(blocks) * static_cast<size_t>(head_dim) * sizeof(float);
+}
+
+PURO_API puro_status_t puro_qk_norm_rope_backward(const puro_heads_t *dq_out, const puro_heads_t *dk_out,
+                                                  const puro_heads_t *q, const puro_heads_t *k, const float *rstd,
+                                                  int64_t tokens, int32_t head_dim, const void *q_gain,
+                                                  const void *k_gain, const float *cos, const float *sin,
+                                                  int64_t max_positions, int32_t rot_dim, int32_t interleaved,
+                                                  const int32_t *positions, const puro_heads_t *dq,
+                                                  const puro_heads_t *dk, float *dq_gain, float *dk_gain,
+                                                  void *workspace, size_t workspace_bytes, int32_t *dev_status,
+                                                  void *stream) {
+    QkArgs p{};
+    p.tokens = tokens;
+    p.D = head_dim;
+    p.rot = rot_dim;
+    p.inter = interleaved != 0;
+    p.q_gain = static_cast<const uint16_t *>(q_gain);
+    p.k_gain = static_cast<const uint16_t *>(k_gain);
+    p.cos = cos;
+    p.sin = sin;
+    p.max_positions = max_positions;
+    p.positions = positions;
+    p.rstd = const_cast<float *>(rstd);
+    p.status = dev_status;
+    if (!take_heads(q, tokens, head_dim, false, &p.q) || !take_heads(k, tokens, head_dim, false, &p.k) ||
+        !take_heads(dq_out, tokens, head_dim, false, &p.q_out) || !take_heads(dk_out, tokens, head_dim, false, &p.k_out) ||
+        !take_heads(dq, tokens, head_dim, true, &p.dq) || !take_heads(dk, tokens, head_dim, true, &p.dk))
+        return PURO_ERR_INVALID_ARG;
+    const puro_status_t st = check_qk(p);
+    if (st != PURO_OK) return st;
+    if (p.q.heads != p.dq.heads || p.k.heads != p.dk.heads) return PURO_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(dq_gain) & 3u) || (reinterpret_cast<uintptr_t>(dk_gain) & 3u)) return PURO_ERR_INVALID_ARG;
+    const bool empty = tokens == 0 || p.q.heads + p.k.heads == 0;
+    if (!empty && !rstd) return PURO_ERR_INVALID_ARG;
+    if (!empty && (dq_gain || dk_gain)) {
+        if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 3u) ||
+            workspace_bytes < puro_qk_norm_rope_workspace_size(tokens, p.q.heads, p.k.heads, head_dim))
+            return PURO_ERR_INVALID_ARG;
+        p.partial = static_cast<float *>(workspace);
+    }
+    if (empty) {  // sums of nothing
+        p.q.heads = p.k.heads = 0;
+        p.tokens = 0;
+        if (!dq_gain && !dk_gain) return PURO_OK;
+    }
+    return cuda_status(launch_qk_norm_rope_backward(p, dq_gain, dk_gain, static_cast<cudaStream_t>(stream)));
+}
+
 PURO_API void puro_set_wait_timeout_ns(uint64_t ns) { g_wait_timeout_ns.store(ns); }
 
 PURO_API puro_status_t puro_set_gemm_tile_n(int32_t tile_n) {

@@ -41,7 +41,9 @@ PyObject *operand_type = nullptr;  // the binding's FP8Operand class
     X(puro_fp8_linear_dgrad_quantize)  \
     X(puro_bf16_linear_fprop)          \
     X(puro_bf16_linear_dgrad)          \
-    X(puro_bf16_linear_wgrad)
+    X(puro_bf16_linear_wgrad)          \
+    X(puro_qk_norm_rope)               \
+    X(puro_qk_norm_rope_backward)
 struct Library {
 #define PURO_FIELD(name) decltype(&::name) name;
     PURO_ENTRIES(PURO_FIELD)
@@ -106,6 +108,10 @@ struct Args {
         if (x < INT32_MIN || x > INT32_MAX) return fail(), 0;
         return static_cast<int32_t>(x);
     }
+    bool flag(int i) {
+        if (v[i] != Py_True && v[i] != Py_False) return fail(), false;
+        return v[i] == Py_True;
+    }
     float f32(int i) {
         if (!PyFloat_CheckExact(v[i])) return fail(), 0.0f;
         return static_cast<float>(PyFloat_AS_DOUBLE(v[i]));
@@ -152,6 +158,37 @@ struct Args {
             t->role = static_cast<int32_t>(e[2]);
         }
         for (PyObject *o : f) Py_XDECREF(o);  // the operand keeps its tensors
+    }
+    // Heads of tokens: a bf16 view [tokens, heads, channels] with unit channel stride.
+    void heads(int i, puro_heads_t *h, int64_t *tokens, int64_t *channels) {
+        *h = puro_heads_t{};
+        *tokens = *channels = 0;
+        const at::Tensor *t = plain(v[i]);
+        if (!t || t->scalar_type() != at::kBFloat16 || t->dim() != 3 || t->stride(2) != 1 || t->size(1) > INT32_MAX) {
+            ok = false;
+            return;
+        }
+        h->data = t->data_ptr();
+        h->token_stride = t->size(0) > 1 ? t->stride(0) : 0;
+        h->head_stride = t->size(1) > 1 ? t->stride(1) : 0;
+        h->heads = static_cast<int32_t>(t->size(1));
+        *tokens = t->size(0);
+        *channels = t->size(2);
+    }
+    // Two tables [positions, pairs] of one shape.
+    void tables(int i, const float **co, const float **si, int64_t *positions, int32_t *rot) {
+        *co = static_cast<const float *>(ptr_of(v[i], at::kFloat, at::kFloat));
+        *si = static_cast<const float *>(ptr_of(v[i + 1], at::kFloat, at::kFloat));
+        int64_t r[2] = {}, c[2] = {};
+        shape(i, &r[0], &c[0]);
+        shape(i + 1, &r[1], &c[1]);
+        if (r[0] != r[1] || c[0] != c[1] || c[0] > 1024) ok = false;
+        *positions = r[0];
+        *rot = static_cast<int32_t>(2 * c[0]);
+    }
+    // A tensor's number of values has to be n.
+    void numel(int i, int64_t n) {
+        if (ok && v[i] != Py_None && THPVariable_Unpack(v[i]).numel() != n) ok = false;
     }
     std::nullptr_t fail() {
         ok = false;
@@ -337,6 +374,71 @@ PURO_NATIVE(bf16_fprop, 8)
 PURO_NATIVE(bf16_dgrad, 8)
 PURO_NATIVE(bf16_wgrad, 8)
 
+// (q, k, q_gain, k_gain, eps, cos, sin, positions, interleaved, q_out, k_out,
+// rstd, dev_status, stream)
+PyObject *qk_norm_rope_call(Args &a) {
+    puro_heads_t q, k, qo, ko;
+    int64_t t[4], d[4], positions;
+    a.heads(0, &q, &t[0], &d[0]);
+    a.heads(1, &k, &t[1], &d[1]);
+    const void *gq = a.opt(2, kBF16), *gk = a.opt(3, kBF16);
+    const float eps = a.f32(4);
+    const float *co, *si;
+    int32_t rot;
+    a.tables(5, &co, &si, &positions, &rot);
+    const int32_t *pos = static_cast<const int32_t *>(a.opt(7, at::kInt));
+    const bool inter = a.flag(8);
+    a.heads(9, &qo, &t[2], &d[2]);
+    a.heads(10, &ko, &t[3], &d[3]);
+    float *rstd = static_cast<float *>(a.opt(11, kF32));
+    int32_t *st = a.status(12);
+    void *s = a.stream(13);
+    for (int i = 1; i < 4; ++i)
+        if (t[i] != t[0] || d[i] != d[0]) a.ok = false;
+    a.numel(2, d[0]);
+    a.numel(3, d[0]);
+    a.numel(7, t[0]);
+    a.numel(11, t[0] * (q.heads + k.heads));
+    if (d[0] > 1024) a.ok = false;
+    return finish(a, [&] {
+        return lib.puro_qk_norm_rope(&q, &k, t[0], static_cast<int32_t>(d[0]), gq, gk, eps, co, si, positions, rot, inter, pos,
+                                     &qo, &ko, rstd, st, s);
+    });
+}
+PURO_NATIVE(qk_norm_rope, 14)
+
+// (dq_out, dk_out, q, k, rstd, q_gain, k_gain, cos, sin, positions, interleaved,
+// dq, dk, dq_gain, dk_gain, workspace, dev_status, stream)
+PyObject *qk_norm_rope_backward_call(Args &a) {
+    puro_heads_t h[6];
+    int64_t t[6], d[6], positions;
+    const int at_arg[6] = {0, 1, 2, 3, 11, 12};
+    for (int i = 0; i < 6; ++i) a.heads(at_arg[i], &h[i], &t[i], &d[i]);
+    const float *rstd = static_cast<const float *>(a.ptr(4, kF32));
+    const void *gq = a.opt(5, kBF16), *gk = a.opt(6, kBF16);
+    const float *co, *si;
+    int32_t rot;
+    a.tables(7, &co, &si, &positions, &rot);
+    const int32_t *pos = static_cast<const int32_t *>(a.opt(9, at::kInt));
+    const bool inter = a.flag(10);
+    float *dgq = static_cast<float *>(a.opt(13, kF32)), *dgk = static_cast<float *>(a.opt(14, kF32));
+    size_t bytes;
+    void *ws = a.scratch(15, &bytes);
+    int32_t *st = a.status(16);
+    void *s = a.stream(17);
+    for (int i = 1; i < 6; ++i)
+        if (t[i] != t[0] || d[i] != d[0]) a.ok = false;
+    a.numel(4, t[0] * (h[2].heads + h[3].heads));
+    for (int i : {5, 6, 13, 14}) a.numel(i, d[0]);
+    a.numel(9, t[0]);
+    if (d[0] > 1024) a.ok = false;
+    return finish(a, [&] {
+        return lib.puro_qk_norm_rope_backward(&h[0], &h[1], &h[2], &h[3], rstd, t[0], static_cast<int32_t>(d[0]), gq, gk, co,
+                                              si, positions, rot, inter, pos, &h[4], &h[5], dgq, dgk, ws, bytes, st, s);
+    });
+}
+PURO_NATIVE(qk_norm_rope_backward, 18)
+
 // (the FP8Operand class)
 PyObject *set_operand_type(PyObject *, PyObject *const *argv, Py_ssize_t n) {
     if (n != 1) {
@@ -390,6 +492,8 @@ PyMethodDef methods[] = {PURO_METHOD("set_operand_type", set_operand_type),
                          PURO_METHOD("puro_bf16_linear_fprop", bf16_fprop),
                          PURO_METHOD("puro_bf16_linear_dgrad", bf16_dgrad),
                          PURO_METHOD("puro_bf16_linear_wgrad", bf16_wgrad),
+                         PURO_METHOD("puro_qk_norm_rope", qk_norm_rope),
+                         PURO_METHOD("puro_qk_norm_rope_backward", qk_norm_rope_backward),
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Native argument marshalling of the Python binding.", -1, methods};

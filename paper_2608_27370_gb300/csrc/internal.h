@@ -214,6 +214,36 @@ bool wgrad_keeps_split(int64_t M, int64_t N, int64_t K);
 int choose_tile_n(int64_t M, int64_t N, int64_t K);
 int choose_grouped_tile_n(int64_t M, int64_t N, int64_t K);
 
+// Heads of a token, as views: channel c of head h of token t is
+// data[t * token_stride + h * head_stride + c].
+struct QkHeads {
+    uint16_t *data;  // bf16
+    int64_t token_stride, head_stride;
+    int heads;
+};
+// Per-head RMSNorm and position rotation of queries and keys (see qknorm.cu).
+struct QkArgs {
+    QkHeads q, k;          // x
+    QkHeads q_out, k_out;  // y; backward: dy
+    QkHeads dq, dk;        // backward: dx
+    int64_t tokens;
+    int D, rot, inter;
+    const uint16_t *q_gain, *k_gain;  // bf16 [D], or null
+    float eps;
+    const float *cos, *sin;  // [max_positions, rot / 2]
+    int64_t max_positions;
+    const int32_t *positions;  // [tokens], or null: token t is at position t
+    float *rstd;               // [tokens, q.heads + k.heads]; forward: or null
+    float *partial;            // backward: [blocks, D] partial sums of the gains' gradients, or null
+    int q_blocks;              // backward: blocks that take query heads
+    int32_t *status;
+};
+cudaError_t launch_qk_norm_rope(const QkArgs &p, cudaStream_t s);
+cudaError_t launch_qk_norm_rope_backward(QkArgs p, float *dq_gain, float *dk_gain, cudaStream_t s);
+// Blocks of the backward pass (one partial sum each), those of the query heads
+// first.  Host-only, shape-only.
+void qk_backward_blocks(int64_t tokens, int q_heads, int k_heads, int D, int *q_blocks, int *blocks);
+
 // Tile shape of the GEMM kernel: rows of A per CTA (a CTA pair computes
 // 2 * kGemmBM rows), columns of a tile (rows of B per pair), and the bytes
 // of K per pipeline stage (one 128-byte swizzle row).
