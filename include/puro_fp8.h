@@ -79,6 +79,15 @@ typedef enum {
 typedef enum { PURO_E4M3 = 0, PURO_E5M2 = 1 } puro_fp8_format_t;
 typedef enum { PURO_SCALE_TENSOR = 0, PURO_SCALE_BLOCK = 1 } puro_scaling_t;
 typedef enum { PURO_ROLE_ACT = 0, PURO_ROLE_WEIGHT = 1 } puro_role_t;
+/* Activations: max(z, 0); z / (1 + e^-z); z Phi(z), Phi the normal
+ * distribution function; z / (1 + e^-2u), u = sqrt(2/pi) (z + 0.044715 z^3). */
+typedef enum {
+    PURO_ACT_NONE = 0,
+    PURO_ACT_RELU = 1,
+    PURO_ACT_SILU = 2,
+    PURO_ACT_GELU = 3,
+    PURO_ACT_GELU_TANH = 4
+} puro_act_t;
 
 /* One quantised GEMM operand, as produced by puro_fp8_quantize. */
 typedef struct {
@@ -243,6 +252,54 @@ puro_status_t puro_fp8_quantize_swiglu(const void *gate, const void *up, int64_t
  */
 puro_status_t puro_swiglu_bf16(const void *gate, const void *up, int64_t rows, int64_t cols, int64_t ld, void *y,
                                void *stream);
+
+/*
+ * Backward of a linear's bias and activation, y = act(z) (+ residual),
+ * z = x W^T + bias:
+ *     dz = dy * act'(z),   dbias[c] = sum over the rows of dz[:, c]
+ * in FP32 (the sum takes dz before its rounding), dz rounded to BF16.  The
+ * residual's gradient is dy itself.
+ *   dy: bf16 [rows, cols].  z: bf16 [rows, cols], or NULL with PURO_ACT_NONE.
+ *   dz: bf16 [rows, cols], or NULL: not written.
+ *   dbias: fp32 [cols], written, or NULL.  The sums are in a fixed order,
+ *     through the workspace: 16-byte aligned scratch of
+ *     puro_act_backward_workspace_size(rows, cols) bytes (only with dbias).
+ * puro_fp8_quantize_act_backward also quantises the BF16 dz exactly as
+ * puro_fp8_quantize does with PURO_SCALE_BLOCK / PURO_ROLE_ACT: q, scale, q_t,
+ * scale_t, dev_status, and rows and cols multiples of 128, as there.
+ * puro_act_backward_bf16 takes any rows, cols a multiple of 8; dz may be dy
+ * itself, and with PURO_ACT_NONE and no dz only the sums are made.
+ * One kernel, and one for dbias.
+ */
+puro_status_t puro_fp8_quantize_act_backward(const void *dy, const void *z, int64_t rows, int64_t cols, int32_t act,
+                                             int32_t fmt, void *dz, float *dbias, void *workspace,
+                                             size_t workspace_bytes, uint8_t *q, void *scale, uint8_t *q_t,
+                                             void *scale_t, int32_t *dev_status, void *stream);
+puro_status_t puro_act_backward_bf16(const void *dy, const void *z, int64_t rows, int64_t cols, int32_t act, void *dz,
+                                     float *dbias, void *workspace, size_t workspace_bytes, void *stream);
+/* Host-only, no CUDA call. */
+size_t puro_act_backward_workspace_size(int64_t rows, int64_t cols);
+
+/*
+ * Backward of the gated MLP's gate, h = act(gate) * up (PURO_ACT_SILU: SwiGLU):
+ *     dgate = dh * up * act'(gate),   dup = dh * act(gate)
+ * in FP32, rounded to BF16 as the row [dgate, dup] of 2*cols values, the
+ * output gradient of the fused gate/up linear.
+ *   dh: bf16 [rows, cols].  gate, up: bf16 [rows, cols] with rows ld elements
+ *     apart, as in puro_fp8_quantize_swiglu.
+ *   dgate_up: bf16 [rows, 2*cols] (the quantising form: or NULL, not written).
+ * puro_fp8_quantize_gated_backward also quantises the BF16 rows exactly as
+ * puro_fp8_quantize does with PURO_SCALE_BLOCK / PURO_ROLE_ACT: q [rows,
+ * 2*cols], q_t [2*cols, rows] and their scales; rows and cols multiples of 128.
+ * puro_gated_backward_bf16 takes any rows, cols a multiple of 8.
+ * One kernel.
+ */
+puro_status_t puro_fp8_quantize_gated_backward(const void *dh, const void *gate, const void *up, int64_t rows,
+                                               int64_t cols, int64_t ld, int32_t act, int32_t fmt, void *dgate_up,
+                                               uint8_t *q, void *scale, uint8_t *q_t, void *scale_t,
+                                               int32_t *dev_status, void *stream);
+puro_status_t puro_gated_backward_bf16(const void *dh, const void *gate, const void *up, int64_t rows, int64_t cols,
+                                       int64_t ld, int32_t act, void *dgate_up, void *stream);
 
 /*
  * The three FP8 GEMMs of a linear layer with weight W [N, K], input X [M, K]

@@ -35,6 +35,7 @@ from . import _build
 E4M3, E5M2 = 0, 1
 SCALE_TENSOR, SCALE_BLOCK = 0, 1
 ROLE_ACT, ROLE_WEIGHT = 0, 1
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = range(5)
 
 PURO_OK = 0
 PURO_ERR_INVALID_ARG = 1
@@ -98,6 +99,12 @@ _SIGNATURES = {
     "puro_bf16_linear_fprop": (_I32, [_P, _P, _P, _I64, _I64, _I64, _P, _P]),
     "puro_bf16_linear_dgrad": (_I32, [_P, _P, _P, _I64, _I64, _I64, _P, _P]),
     "puro_bf16_linear_wgrad": (_I32, [_P, _P, _P, _I64, _I64, _I64, _P, _P]),
+    "puro_fp8_quantize_act_backward": (_I32, [_P, _P, _I64, _I64, _I32, _I32, _P, _P, _P, ctypes.c_size_t, _P, _P, _P, _P, _P,
+                                              _P]),
+    "puro_act_backward_bf16": (_I32, [_P, _P, _I64, _I64, _I32, _P, _P, _P, ctypes.c_size_t, _P]),
+    "puro_act_backward_workspace_size": (ctypes.c_size_t, [_I64, _I64]),
+    "puro_fp8_quantize_gated_backward": (_I32, [_P, _P, _P, _I64, _I64, _I64, _I32, _I32, _P, _P, _P, _P, _P, _P, _P]),
+    "puro_gated_backward_bf16": (_I32, [_P, _P, _P, _I64, _I64, _I64, _I32, _P, _P]),
     "puro_qk_norm_rope": (_I32, [_P, _P, _I64, _I32, _P, _P, ctypes.c_float, _P, _P, _I64, _I32, _I32, _P, _P, _P, _P, _P,
                                  _P]),
     "puro_qk_norm_rope_backward": (_I32, [_P, _P, _P, _P, _P, _I64, _I32, _P, _P, _P, _P, _I64, _I32, _I32, _P, _P, _P, _P,
@@ -566,6 +573,98 @@ def puro_bf16_linear_wgrad(dy_t, x_t, dw, M, N, K, dev_status=None, stream=None)
 
 
 # --------------------------------------------------------------------------
+# Backward of activations and gates
+# --------------------------------------------------------------------------
+def puro_act_backward_workspace_size(rows: int, cols: int) -> int:
+    return int(load_library().puro_act_backward_workspace_size(rows, cols))
+
+
+def _ws(workspace: Optional[torch.Tensor]):
+    return _ptr(workspace, None, "workspace"), workspace.numel() * workspace.element_size() if workspace is not None else 0
+
+
+def puro_fp8_quantize_act_backward(dy: torch.Tensor, z: Optional[torch.Tensor], act: int, fmt: int,
+                                   dz: Optional[torch.Tensor], dbias: Optional[torch.Tensor],
+                                   workspace: Optional[torch.Tensor], q: torch.Tensor, scale: torch.Tensor,
+                                   q_t: Optional[torch.Tensor] = None, scale_t: Optional[torch.Tensor] = None,
+                                   dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dz = dy * act'(z) (bf16, z None without an activation) as the FP8 copies
+    that puro_fp8_quantize makes of it, dbias (fp32 [cols]) its sum over the
+    rows, through a workspace of puro_act_backward_workspace_size bytes; dz
+    (bf16) is written only when given."""
+    _on_current_device(dy, z, dz, dbias, workspace, q, scale, q_t, scale_t, dev_status)
+    st = (_native or _load_native()).puro_fp8_quantize_act_backward(dy, z, act, fmt, dz, dbias, workspace, q, scale, q_t,
+                                                                    scale_t, dev_status, stream)
+    if st is not None:
+        return _check("puro_fp8_quantize_act_backward", st)
+    rows, cols = dy.shape
+    n, u8, bf16 = rows * cols, torch.uint8, torch.bfloat16
+    st = load_library().puro_fp8_quantize_act_backward(
+        _ptr(dy, bf16, "dy"), _sized(z, bf16, n, "z"), rows, cols, act, fmt, _sized(dz, bf16, n, "dz"),
+        _sized(dbias, torch.float32, cols, "dbias"), *_ws(workspace), _sized(q, u8, n, "q"), _ptr(scale, u8, "scale"),
+        _sized(q_t, u8, n, "q_t"), _ptr(scale_t, u8, "scale_t"), _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
+    _check("puro_fp8_quantize_act_backward", st)
+
+
+def puro_act_backward_bf16(dy: torch.Tensor, z: Optional[torch.Tensor], act: int, dz: Optional[torch.Tensor],
+                           dbias: Optional[torch.Tensor], workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The same without the quantiser: dz (bf16, may be dy) and dbias, each only when given."""
+    _on_current_device(dy, z, dz, dbias, workspace)
+    st = (_native or _load_native()).puro_act_backward_bf16(dy, z, act, dz, dbias, workspace, stream)
+    if st is not None:
+        return _check("puro_act_backward_bf16", st)
+    rows, cols = dy.shape
+    n, bf16 = rows * cols, torch.bfloat16
+    st = load_library().puro_act_backward_bf16(
+        _ptr(dy, bf16, "dy"), _sized(z, bf16, n, "z"), rows, cols, act, _sized(dz, bf16, n, "dz"),
+        _sized(dbias, torch.float32, cols, "dbias"), *_ws(workspace), _stream(stream))
+    _check("puro_act_backward_bf16", st)
+
+
+def puro_fp8_quantize_gated_backward(dh: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, act: int, fmt: int,
+                                     dgate_up: Optional[torch.Tensor], q: torch.Tensor, scale: torch.Tensor,
+                                     q_t: Optional[torch.Tensor] = None, scale_t: Optional[torch.Tensor] = None,
+                                     dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """[dgate, dup] = [dh * up * act'(gate), dh * act(gate)] (bf16 [rows, 2
+    cols]) as the FP8 copies that puro_fp8_quantize makes of it: the output
+    gradient of the fused gate/up linear, whose output gate and up are views
+    of.  dgate_up (bf16) is written only when given."""
+    _on_current_device(dh, gate, up, dgate_up, q, scale, q_t, scale_t, dev_status)
+    st = (_native or _load_native()).puro_fp8_quantize_gated_backward(dh, gate, up, act, fmt, dgate_up, q, scale, q_t, scale_t,
+                                                                      dev_status, stream)
+    if st is not None:
+        return _check("puro_fp8_quantize_gated_backward", st)
+    g, u, rows, cols, ld = _gate_up(gate, up)
+    n, u8, bf16 = 2 * rows * cols, torch.uint8, torch.bfloat16
+    _same_shape(dh, gate, "dh")
+    st = load_library().puro_fp8_quantize_gated_backward(
+        _ptr(dh, bf16, "dh"), g, u, rows, cols, ld, act, fmt, _sized(dgate_up, bf16, n, "dgate_up"), _sized(q, u8, n, "q"),
+        _ptr(scale, u8, "scale"), _sized(q_t, u8, n, "q_t"), _ptr(scale_t, u8, "scale_t"),
+        _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
+    _check("puro_fp8_quantize_gated_backward", st)
+
+
+def _same_shape(t: torch.Tensor, like: torch.Tensor, name: str) -> None:
+    if t.shape != like.shape:
+        raise ValueError(f"{name} is {tuple(t.shape)}, expected {tuple(like.shape)}")
+
+
+def puro_gated_backward_bf16(dh: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, act: int, dgate_up: torch.Tensor,
+                             stream=None) -> None:
+    """The same without the quantiser."""
+    _on_current_device(dh, gate, up, dgate_up)
+    st = (_native or _load_native()).puro_gated_backward_bf16(dh, gate, up, act, dgate_up, stream)
+    if st is not None:
+        return _check("puro_gated_backward_bf16", st)
+    g, u, rows, cols, ld = _gate_up(gate, up)
+    _same_shape(dh, gate, "dh")
+    st = load_library().puro_gated_backward_bf16(_ptr(dh, torch.bfloat16, "dh"), g, u, rows, cols, ld, act,
+                                                 _sized(dgate_up, torch.bfloat16, 2 * rows * cols, "dgate_up"),
+                                                 _stream(stream))
+    _check("puro_gated_backward_bf16", st)
+
+
+# --------------------------------------------------------------------------
 # Query and key norms with the position rotation
 # --------------------------------------------------------------------------
 def _current_device() -> int:
@@ -748,6 +847,7 @@ def quantize(x: torch.Tensor, fmt: int = E4M3, scaling: int = SCALE_BLOCK, role:
 
 
 __all__ = [n for n in dir() if n.startswith("puro_")] + [
-    "E4M3", "E5M2", "SCALE_TENSOR", "SCALE_BLOCK", "ROLE_ACT", "ROLE_WEIGHT", "PuroError", "FP8Operand",
+    "E4M3", "E5M2", "SCALE_TENSOR", "SCALE_BLOCK", "ROLE_ACT", "ROLE_WEIGHT", "ACT_NONE", "ACT_RELU", "ACT_SILU",
+    "ACT_GELU", "ACT_GELU_TANH", "PuroError", "FP8Operand",
     "Quantized", "quantize", "load_library", "empty_scales", "scale_vec_shape", "LIB_PATH", "HEADER_PATH",
 ]

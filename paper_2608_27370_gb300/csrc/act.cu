@@ -1,0 +1,166 @@
+// act.cu -- backward of a linear's bias and activation, and of the gate of the
+// gated MLP (Puro-2B, section "Model architecture and pretraining system"), in
+// BF16; quantize.cu has the forms that emit FP8 copies.
+//   dz = dy * act'(z),                 dbias[c] = sum over rows of dz[:, c]
+//   dgate = dh * up * act'(gate),      dup = dh * act(gate)
+// Bound by memory: every input read once, every output written once; a thread
+// takes eight columns (16 bytes) of a row.  The bias's gradient sums FP32
+// values that are not rounded: a thread over the rows of its slab, a block over
+// its eight rows of threads, then the slabs in order, so always in one order.
+#include <cuda_bf16.h>
+
+#include <algorithm>
+
+#include "act_math.cuh"
+#include "internal.h"
+#include "ptx.cuh"
+#include "quant_math.cuh"
+
+namespace puro {
+
+constexpr int kActCols = 256;                // columns of a block: 32 threads of eight
+constexpr int kActRows = 8;                  // rows of threads
+constexpr int64_t kActBlocks = 152 * 4;      // blocks to aim for
+
+PURO_DEV void widen8(const uint4 &w, float (&v)[8]) {
+    const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = bf16_lo(ws[i]);
+        v[2 * i + 1] = bf16_hi(ws[i]);
+    }
+}
+PURO_DEV uint4 narrow8(const float (&v)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<uint32_t *>(&b);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+ActBackwardPlan plan_act_backward(int64_t rows, int64_t cols) {
+    const int64_t strips = (cols + kActCols - 1) / kActCols;
+    int64_t slabs = std::max<int64_t>(1, std::min((rows + 31) / 32, (kActBlocks + strips - 1) / strips));
+    const int64_t slab_rows = ((rows + slabs - 1) / slabs + kActRows - 1) / kActRows * kActRows;
+    slabs = (rows + slab_rows - 1) / slab_rows;
+    return ActBackwardPlan{static_cast<int>(slabs), slab_rows};
+}
+
+template <int ACT>
+__global__ void __launch_bounds__(256) act_backward_kernel(const uint16_t *dy, const uint16_t *__restrict__ z,
+                                                           int64_t rows, int64_t cols, int64_t slab_rows, uint16_t *dz,
+                                                           float *__restrict__ partial) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * kActCols + 8 * tx;
+    const int64_t r1 = min(rows, (static_cast<int64_t>(blockIdx.y) + 1) * slab_rows);
+    float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    if (c < cols) {
+#pragma unroll 4
+        for (int64_t r = blockIdx.y * slab_rows + ty; r < r1; r += kActRows) {
+            const int64_t at = r * cols + c;
+            const uint4 dw = *reinterpret_cast<const uint4 *>(dy + at);  // (dz may be dy)
+            float d[8];
+            widen8(dw, d);
+            if constexpr (ACT != PURO_ACT_NONE) {
+                float zf[8];
+                widen8(__ldg(reinterpret_cast<const uint4 *>(z + at)), zf);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] *= act_slope_f32<ACT>(zf[i]).d;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += d[i];
+            if (dz) *reinterpret_cast<uint4 *>(dz + at) = ACT == PURO_ACT_NONE ? dw : narrow8(d);
+        }
+    }
+    if (!partial) return;
+    __shared__ float part[kActRows][kActCols];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[ty][8 * tx + i] = sum[i];
+    __syncthreads();
+    const int64_t oc = static_cast<int64_t>(blockIdx.x) * kActCols + threadIdx.x;
+    if (oc >= cols) return;
+    float a = part[0][threadIdx.x];
+#pragma unroll
+    for (int k = 1; k < kActRows; ++k) a += part[k][threadIdx.x];
+    partial[blockIdx.y * cols + oc] = a;
+}
+
+cudaError_t launch_act_backward(const uint16_t *dy, const uint16_t *z, int64_t rows, int64_t cols, int act, uint16_t *dz,
+                                float *partial, cudaStream_t s) {
+    const ActBackwardPlan plan = plan_act_backward(rows, cols);
+    auto kern = act == PURO_ACT_RELU        ? act_backward_kernel<PURO_ACT_RELU>
+                : act == PURO_ACT_SILU      ? act_backward_kernel<PURO_ACT_SILU>
+                : act == PURO_ACT_GELU      ? act_backward_kernel<PURO_ACT_GELU>
+                : act == PURO_ACT_GELU_TANH ? act_backward_kernel<PURO_ACT_GELU_TANH>
+                                            : act_backward_kernel<PURO_ACT_NONE>;
+    return launch_pdl(kern, dim3(static_cast<unsigned>((cols + kActCols - 1) / kActCols), plan.slabs), dim3(256), 0, s, dy, z,
+                      rows, cols, plan.slab_rows, dz, partial);
+}
+
+// 32 columns a block, eight interleaved shares of the partial sums each.
+__global__ void __launch_bounds__(256) column_sums_kernel(const float *__restrict__ partial, int64_t n, int64_t cols,
+                                                          float *__restrict__ out) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + tx;
+    float a = 0.0f;
+    if (c < cols)
+        for (int64_t k = ty; k < n; k += 8) a += partial[k * cols + c];
+    __shared__ float part[8][32];
+    part[ty][tx] = a;
+    __syncthreads();
+    if (ty == 0 && c < cols) {
+#pragma unroll
+        for (int k = 1; k < 8; ++k) a += part[k][tx];
+        out[c] = a;
+    }
+}
+
+cudaError_t launch_column_sums(const float *partial, int64_t n, int64_t cols, float *dbias, cudaStream_t s) {
+    return launch_pdl(column_sums_kernel, dim3(static_cast<unsigned>((cols + 31) / 32)), dim3(256), 0, s, partial, n, cols, dbias);
+}
+
+// [dgate, dup] of eight columns of one row a thread and step.
+template <int ACT>
+__global__ void __launch_bounds__(256) gated_backward_kernel(const uint16_t *__restrict__ dh, const uint16_t *__restrict__ gate,
+                                                             const uint16_t *__restrict__ up, int64_t rows, int64_t cols,
+                                                             int64_t ld, uint16_t *__restrict__ dgate_up) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int64_t per_row = cols / 8, chunks = rows * per_row, stride = static_cast<int64_t>(gridDim.x) * blockDim.x;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < chunks; i += stride) {
+        const int64_t r = i / per_row, c = (i - r * per_row) * 8;
+        float d[8], g[8], u[8], dg[8];
+        widen8(__ldg(reinterpret_cast<const uint4 *>(dh) + i), d);
+        widen8(__ldg(reinterpret_cast<const uint4 *>(gate + r * ld + c)), g);
+        widen8(__ldg(reinterpret_cast<const uint4 *>(up + r * ld + c)), u);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const ActSlope s = act_slope_f32<ACT>(g[k]);
+            dg[k] = d[k] * (u[k] * s.d);
+            d[k] *= s.a;
+        }
+        uint16_t *out = dgate_up + r * 2 * cols + c;
+        *reinterpret_cast<uint4 *>(out) = narrow8(dg);
+        *reinterpret_cast<uint4 *>(out + cols) = narrow8(d);
+    }
+}
+
+cudaError_t launch_gated_backward(const uint16_t *dh, const uint16_t *gate, const uint16_t *up, int64_t rows, int64_t cols,
+                                  int64_t ld, int act, uint16_t *dgate_up, cudaStream_t s) {
+    auto kern = act == PURO_ACT_RELU        ? gated_backward_kernel<PURO_ACT_RELU>
+                : act == PURO_ACT_SILU      ? gated_backward_kernel<PURO_ACT_SILU>
+                : act == PURO_ACT_GELU      ? gated_backward_kernel<PURO_ACT_GELU>
+                : act == PURO_ACT_GELU_TANH ? gated_backward_kernel<PURO_ACT_GELU_TANH>
+                                            : gated_backward_kernel<PURO_ACT_NONE>;
+    const int64_t want = (rows * (cols / 8) + 255) / 256, cap = 152 * 8;
+    return launch_pdl(kern, dim3(static_cast<unsigned>(want < cap ? want : cap)), dim3(256), 0, s, dh, gate, up, rows, cols, ld,
+                      dgate_up);
+}
+
+}  // namespace puro

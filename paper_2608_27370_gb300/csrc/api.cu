@@ -2,6 +2,7 @@
 // (entirely on the host, before anything is enqueued), TMA descriptor
 // encoding and kernel launch.  See the header for the contract of every
 // entry point.
+#include <algorithm>
 #include <atomic>
 #include <mutex>
 
@@ -641,6 +642,144 @@ PURO_API puro_status_t puro_rmsnorm_bf16(const void *h, int64_t rows, int64_t co
     if (e != cudaSuccess) return cuda_status(e);
     return cuda_status(launch_rmsnorm_apply(static_cast<const uint16_t *>(h), rows, cols, rstd,
                                             static_cast<const uint16_t *>(gamma), static_cast<uint16_t *>(y), s));
+}
+
+// ------------------------------------------------------ activation backward
+namespace puro {
+namespace {
+
+bool valid_act(int32_t a) { return a >= PURO_ACT_NONE && a <= PURO_ACT_GELU_TANH; }
+
+// Quantiser arguments and maps of a producer that reads x (rows x_ld elements
+// apart, x_cols columns) and quantises [rows, cols], with an optional BF16 output y.
+bool producer_maps(const void *x, int64_t x_cols, int64_t x_ld, int64_t rows, int64_t cols, int32_t fmt, void *y,
+                   uint8_t *q, void *scale, uint8_t *q_t, void *scale_t, int32_t *dev_status, QuantArgs *a,
+                   CUtensorMap (&m)[4]) {
+    *a = QuantArgs{};
+    a->fmt = fmt;
+    a->rows = rows;
+    a->cols = cols;
+    a->has_t = q_t != nullptr;
+    a->kind = kQuantBlockAct;
+    a->scale_u8 = static_cast<uint8_t *>(scale);
+    a->scale_t_u8 = static_cast<uint8_t *>(scale_t);
+    a->status = dev_status;
+    a->wait_ns = g_wait_timeout_ns.load();
+    a->x = static_cast<const uint16_t *>(x);
+    if (!make_map(&m[0], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, x_cols, rows, x_ld * 2, 128, 128, CU_TENSOR_MAP_SWIZZLE_NONE) ||
+        !make_map(&m[1], CU_TENSOR_MAP_DATA_TYPE_UINT8, q, cols, rows, cols, 128, 128, CU_TENSOR_MAP_SWIZZLE_NONE))
+        return false;
+    m[2] = m[1];
+    if (q_t && !make_map(&m[2], CU_TENSOR_MAP_DATA_TYPE_UINT8, q_t, rows, cols, rows, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B))
+        return false;
+    m[3] = m[0];
+    return !y || make_map(&m[3], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, y, cols, rows, cols * 2, 128, 128, CU_TENSOR_MAP_SWIZZLE_NONE);
+}
+
+bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// The arguments both forms of the bias and activation backward share; zeroed
+// sums of no rows are left to the caller.
+puro_status_t check_act_backward(const void *dy, const void *z, int64_t rows, int64_t cols, int32_t act, const void *dz,
+                                 const float *dbias, const void *workspace, size_t workspace_bytes) {
+    if (!valid_act(act) || rows < 0 || cols < 0) return PURO_ERR_INVALID_ARG;
+    if (rows > INT32_MAX || cols > INT32_MAX) return PURO_ERR_UNSUPPORTED;
+    if (!aligned4(dbias) || !aligned16(dy) || !aligned16(z) || !aligned16(dz)) return PURO_ERR_INVALID_ARG;
+    if (rows == 0 || cols == 0) return PURO_OK;
+    if (!dy || (act != PURO_ACT_NONE && !z)) return PURO_ERR_INVALID_ARG;
+    if (dbias && (!workspace || !aligned16(workspace) || workspace_bytes < puro_act_backward_workspace_size(rows, cols)))
+        return PURO_ERR_INVALID_ARG;
+    return PURO_OK;
+}
+
+}  // namespace
+}  // namespace puro
+
+PURO_API size_t puro_act_backward_workspace_size(int64_t rows, int64_t cols) {
+    if (rows <= 0 || cols <= 0 || rows > INT32_MAX || cols > INT32_MAX) return 0;
+    const int64_t sums = std::max<int64_t>((rows + 127) / 128, plan_act_backward(rows, cols).slabs);
+    return static_cast<size_t>(sums) * static_cast<size_t>(cols) * sizeof(float);
+}
+
+PURO_API puro_status_t puro_fp8_quantize_act_backward(const void *dy, const void *z, int64_t rows, int64_t cols,
+                                                      int32_t act, int32_t fmt, void *dz, float *dbias, void *workspace,
+                                                      size_t workspace_bytes, uint8_t *q, void *scale, uint8_t *q_t,
+                                                      void *scale_t, int32_t *dev_status, void *stream) {
+    if (!valid_fmt(fmt) || rows % 128 || cols % 128) return PURO_ERR_INVALID_ARG;
+    if ((q_t == nullptr) != (scale_t == nullptr)) return PURO_ERR_INVALID_ARG;
+    const puro_status_t st = check_act_backward(dy, z, rows, cols, act, dz, dbias, workspace, workspace_bytes);
+    if (st != PURO_OK) return st;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (rows == 0 || cols == 0)
+        return cuda_status(dbias && cols > 0 ? cudaMemsetAsync(dbias, 0, static_cast<size_t>(cols) * 4, s) : cudaSuccess);
+    if (!q || !scale || !aligned16(q) || !aligned16(scale) || !aligned16(q_t) || !aligned16(scale_t)) return PURO_ERR_INVALID_ARG;
+    QuantArgs a;
+    CUtensorMap m[4];
+    if (!producer_maps(dy, cols, cols, rows, cols, fmt, dz, q, scale, q_t, scale_t, dev_status, &a, m)) return PURO_ERR_CUDA;
+    ProdArgs prod{};
+    prod.write_y = dz != nullptr;
+    prod.up = act == PURO_ACT_NONE ? nullptr : static_cast<const uint16_t *>(z);
+    prod.ld = cols;
+    prod.act = act;
+    prod.col_sum = dbias ? static_cast<float *>(workspace) : nullptr;
+    const cudaError_t e = launch_quantize_act_backward(a, m[0], m[1], m[2], m[3], prod, s);
+    if (e != cudaSuccess || !dbias) return cuda_status(e);
+    return cuda_status(launch_column_sums(prod.col_sum, rows / 128, cols, dbias, s));
+}
+
+PURO_API puro_status_t puro_act_backward_bf16(const void *dy, const void *z, int64_t rows, int64_t cols, int32_t act,
+                                              void *dz, float *dbias, void *workspace, size_t workspace_bytes,
+                                              void *stream) {
+    if (cols % 8) return PURO_ERR_INVALID_ARG;
+    const puro_status_t st = check_act_backward(dy, z, rows, cols, act, dz, dbias, workspace, workspace_bytes);
+    if (st != PURO_OK) return st;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (rows == 0 || cols == 0)
+        return cuda_status(dbias && cols > 0 ? cudaMemsetAsync(dbias, 0, static_cast<size_t>(cols) * 4, s) : cudaSuccess);
+    if (!dz && !dbias) return PURO_OK;
+    float *partial = dbias ? static_cast<float *>(workspace) : nullptr;
+    const cudaError_t e = launch_act_backward(static_cast<const uint16_t *>(dy), static_cast<const uint16_t *>(z), rows, cols, act,
+                                              static_cast<uint16_t *>(dz), partial, s);
+    if (e != cudaSuccess || !dbias) return cuda_status(e);
+    return cuda_status(launch_column_sums(partial, plan_act_backward(rows, cols).slabs, cols, dbias, s));
+}
+
+PURO_API puro_status_t puro_fp8_quantize_gated_backward(const void *dh, const void *gate, const void *up, int64_t rows,
+                                                        int64_t cols, int64_t ld, int32_t act, int32_t fmt,
+                                                        void *dgate_up, uint8_t *q, void *scale, uint8_t *q_t,
+                                                        void *scale_t, int32_t *dev_status, void *stream) {
+    if (!valid_fmt(fmt) || !valid_act(act) || rows < 0 || cols < 0 || ld < cols || ld % 8) return PURO_ERR_INVALID_ARG;
+    if (rows % 128 || cols % 128) return PURO_ERR_INVALID_ARG;
+    if ((q_t == nullptr) != (scale_t == nullptr)) return PURO_ERR_INVALID_ARG;
+    if (rows > INT32_MAX || 2 * cols > INT32_MAX || ld > INT32_MAX) return PURO_ERR_UNSUPPORTED;
+    if (rows == 0 || cols == 0) return PURO_OK;
+    if (!dh || !gate || !up || !q || !scale) return PURO_ERR_INVALID_ARG;
+    if (!aligned16(dh) || !aligned16(gate) || !aligned16(up) || !aligned16(dgate_up) || !aligned16(q) || !aligned16(scale) ||
+        !aligned16(q_t) || !aligned16(scale_t))
+        return PURO_ERR_INVALID_ARG;
+    QuantArgs a;
+    CUtensorMap m[4];
+    if (!producer_maps(dh, cols, cols, rows, 2 * cols, fmt, dgate_up, q, scale, q_t, scale_t, dev_status, &a, m))
+        return PURO_ERR_CUDA;
+    ProdArgs prod{};
+    prod.write_y = dgate_up != nullptr;
+    prod.gate = static_cast<const uint16_t *>(gate);
+    prod.up = static_cast<const uint16_t *>(up);
+    prod.ld = ld;
+    prod.act = act;
+    return cuda_status(launch_quantize_gated_backward(a, m[0], m[1], m[2], m[3], prod, static_cast<cudaStream_t>(stream)));
+}
+
+PURO_API puro_status_t puro_gated_backward_bf16(const void *dh, const void *gate, const void *up, int64_t rows,
+                                                int64_t cols, int64_t ld, int32_t act, void *dgate_up, void *stream) {
+    if (!valid_act(act) || rows < 0 || cols < 0 || cols % 8 || ld < cols || ld % 8) return PURO_ERR_INVALID_ARG;
+    if (rows > INT32_MAX || cols > INT32_MAX || ld > INT32_MAX) return PURO_ERR_UNSUPPORTED;
+    if (rows == 0 || cols == 0) return PURO_OK;
+    if (!dh || !gate || !up || !dgate_up || !aligned16(dh) || !aligned16(gate) || !aligned16(up) || !aligned16(dgate_up))
+        return PURO_ERR_INVALID_ARG;
+    return cuda_status(launch_gated_backward(static_cast<const uint16_t *>(dh), static_cast<const uint16_t *>(gate),
+                                             static_cast<const uint16_t *>(up), rows, cols, ld, act,
+                                             static_cast<uint16_t *>(dgate_up), static_cast<cudaStream_t>(stream)));
 }
 
 PURO_API puro_status_t puro_fp8_linear_fprop(const puro_fp8_tensor_t *x, const puro_fp8_tensor_t *w, void *y,

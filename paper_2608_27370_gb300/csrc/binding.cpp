@@ -42,6 +42,10 @@ PyObject *operand_type = nullptr;  // the binding's FP8Operand class
     X(puro_bf16_linear_fprop)          \
     X(puro_bf16_linear_dgrad)          \
     X(puro_bf16_linear_wgrad)          \
+    X(puro_fp8_quantize_act_backward)  \
+    X(puro_act_backward_bf16)          \
+    X(puro_fp8_quantize_gated_backward) \
+    X(puro_gated_backward_bf16)        \
     X(puro_qk_norm_rope)               \
     X(puro_qk_norm_rope_backward)
 struct Library {
@@ -185,6 +189,23 @@ struct Args {
         if (r[0] != r[1] || c[0] != c[1] || c[0] > 1024) ok = false;
         *positions = r[0];
         *rot = static_cast<int32_t>(2 * c[0]);
+    }
+    // Two bf16 views of one shape and row stride, with unit column stride.
+    void gate_up(int i, const void **gate, const void **up, int64_t *rows, int64_t *cols, int64_t *ld) {
+        *gate = *up = nullptr;
+        *rows = *cols = *ld = 0;
+        const at::Tensor *g = plain(v[i]), *u = plain(v[i + 1]);
+        if (!g || !u || g->scalar_type() != at::kBFloat16 || u->scalar_type() != at::kBFloat16 || g->dim() != 2 ||
+            u->dim() != 2 || g->sizes() != u->sizes() || g->size(0) < 2 || g->stride(1) != 1 || u->stride(1) != 1 ||
+            g->stride(0) != u->stride(0)) {
+            ok = false;
+            return;
+        }
+        *gate = g->data_ptr();
+        *up = u->data_ptr();
+        *rows = g->size(0);
+        *cols = g->size(1);
+        *ld = g->stride(0);
     }
     // A tensor's number of values has to be n.
     void numel(int i, int64_t n) {
@@ -374,6 +395,79 @@ PURO_NATIVE(bf16_fprop, 8)
 PURO_NATIVE(bf16_dgrad, 8)
 PURO_NATIVE(bf16_wgrad, 8)
 
+// (dy, z, act, fmt, dz, dbias, workspace, q, scale, q_t, scale_t, dev_status, stream)
+PyObject *quantize_act_backward_call(Args &a) {
+    const void *dy = a.ptr(0, kBF16), *z = a.opt(1, kBF16);
+    int64_t r, c;
+    a.shape(0, &r, &c);
+    const int32_t act = a.i32(2), fmt = a.i32(3);
+    void *dz = a.opt(4, kBF16);
+    float *db = static_cast<float *>(a.opt(5, kF32));
+    size_t bytes;
+    void *ws = a.scratch(6, &bytes);
+    uint8_t *q = u8(a.opt(7, kU8)), *qt = u8(a.opt(9, kU8));
+    void *sc = a.opt(8, kU8), *sct = a.opt(10, kU8);
+    int32_t *st = a.status(11);
+    void *s = a.stream(12);
+    for (int i : {1, 4, 7, 9}) a.numel(i, r * c);
+    a.numel(5, c);
+    return finish(a, [&] {
+        return lib.puro_fp8_quantize_act_backward(dy, z, r, c, act, fmt, dz, db, ws, bytes, q, sc, qt, sct, st, s);
+    });
+}
+PURO_NATIVE(quantize_act_backward, 13)
+
+// (dy, z, act, dz, dbias, workspace, stream)
+PyObject *act_backward_bf16_call(Args &a) {
+    const void *dy = a.ptr(0, kBF16), *z = a.opt(1, kBF16);
+    int64_t r, c;
+    a.shape(0, &r, &c);
+    const int32_t act = a.i32(2);
+    void *dz = a.opt(3, kBF16);
+    float *db = static_cast<float *>(a.opt(4, kF32));
+    size_t bytes;
+    void *ws = a.scratch(5, &bytes);
+    void *s = a.stream(6);
+    for (int i : {1, 3}) a.numel(i, r * c);
+    a.numel(4, c);
+    return finish(a, [&] { return lib.puro_act_backward_bf16(dy, z, r, c, act, dz, db, ws, bytes, s); });
+}
+PURO_NATIVE(act_backward_bf16, 7)
+
+// (dh, gate, up, act, fmt, dgate_up, q, scale, q_t, scale_t, dev_status, stream)
+PyObject *quantize_gated_backward_call(Args &a) {
+    const void *dh = a.ptr(0, kBF16), *g, *u;
+    int64_t r, c, ld, dr, dc;
+    a.gate_up(1, &g, &u, &r, &c, &ld);
+    a.shape(0, &dr, &dc);
+    if (dr != r || dc != c) a.ok = false;
+    const int32_t act = a.i32(3), fmt = a.i32(4);
+    void *dgu = a.opt(5, kBF16), *sc = a.opt(7, kU8), *sct = a.opt(9, kU8);
+    uint8_t *q = u8(a.opt(6, kU8)), *qt = u8(a.opt(8, kU8));
+    int32_t *st = a.status(10);
+    void *s = a.stream(11);
+    for (int i : {5, 6, 8}) a.numel(i, 2 * r * c);
+    return finish(a, [&] {
+        return lib.puro_fp8_quantize_gated_backward(dh, g, u, r, c, ld, act, fmt, dgu, q, sc, qt, sct, st, s);
+    });
+}
+PURO_NATIVE(quantize_gated_backward, 12)
+
+// (dh, gate, up, act, dgate_up, stream)
+PyObject *gated_backward_bf16_call(Args &a) {
+    const void *dh = a.ptr(0, kBF16), *g, *u;
+    int64_t r, c, ld, dr, dc;
+    a.gate_up(1, &g, &u, &r, &c, &ld);
+    a.shape(0, &dr, &dc);
+    if (dr != r || dc != c) a.ok = false;
+    const int32_t act = a.i32(3);
+    void *dgu = a.ptr(4, kBF16);
+    void *s = a.stream(5);
+    a.numel(4, 2 * r * c);
+    return finish(a, [&] { return lib.puro_gated_backward_bf16(dh, g, u, r, c, ld, act, dgu, s); });
+}
+PURO_NATIVE(gated_backward_bf16, 6)
+
 // (q, k, q_gain, k_gain, eps, cos, sin, positions, interleaved, q_out, k_out,
 // rstd, dev_status, stream)
 PyObject *qk_norm_rope_call(Args &a) {
@@ -492,6 +586,10 @@ PyMethodDef methods[] = {PURO_METHOD("set_operand_type", set_operand_type),
                          PURO_METHOD("puro_bf16_linear_fprop", bf16_fprop),
                          PURO_METHOD("puro_bf16_linear_dgrad", bf16_dgrad),
                          PURO_METHOD("puro_bf16_linear_wgrad", bf16_wgrad),
+                         PURO_METHOD("puro_fp8_quantize_act_backward", quantize_act_backward),
+                         PURO_METHOD("puro_act_backward_bf16", act_backward_bf16),
+                         PURO_METHOD("puro_fp8_quantize_gated_backward", quantize_gated_backward),
+                         PURO_METHOD("puro_gated_backward_bf16", gated_backward_bf16),
                          PURO_METHOD("puro_qk_norm_rope", qk_norm_rope),
                          PURO_METHOD("puro_qk_norm_rope_backward", qk_norm_rope_backward),
                          {nullptr, nullptr, 0, nullptr}};

@@ -76,13 +76,19 @@ enum QuantProd : int {
     kProdNone = 0,
     kProdRmsNorm = 1,  // y = bf16((h * rstd[row]) * gamma[col])
     kProdSwiGlu = 2,   // y = bf16(silu(gate) * up)
+    kProdActBackward = 3,    // y = bf16(dy * act'(z))
+    kProdGatedBackward = 4,  // y = bf16([dh * up * act'(gate), dh * act(gate)])
 };
 struct ProdArgs {
     const float *rstd;      // kProdRmsNorm: [rows]
     const uint16_t *gamma;  // kProdRmsNorm: bf16 [cols], or null (no gain)
     bool write_y;           // also store y (through tm_y)
-    const uint16_t *up;     // kProdSwiGlu: bf16 [rows, cols], rows ld elements apart
-    int64_t ld;             // kProdSwiGlu: row stride of up (and of the gate tm_x maps)
+    const uint16_t *up;     // kProdSwiGlu, kProdGatedBackward: bf16 [rows, cols], rows ld elements apart;
+                            // kProdActBackward: z, or null (no activation)
+    int64_t ld;             // row stride of up (and of the gate)
+    int act;                // kProdActBackward, kProdGatedBackward: puro_act_t
+    const uint16_t *gate;   // kProdGatedBackward
+    float *col_sum;         // kProdActBackward: sums of dz over each 128 rows, [rows / 128, cols], or null
 };
 
 // rstd[r] = 1 / sqrt(mean(h[r,:]^2) + eps) (cols a multiple of 8).
@@ -110,6 +116,28 @@ cudaError_t launch_quantize_rmsnorm(const QuantArgs &a, const CUtensorMap &tm_x,
 cudaError_t launch_quantize_swiglu(const QuantArgs &a, const CUtensorMap &tm_x, const CUtensorMap &tm_q,
                                    const CUtensorMap &tm_qt, const CUtensorMap &tm_y, const ProdArgs &prod,
                                    cudaStream_t s);
+// The activation quantiser fed by dz = dy * act'(z): tm_x maps dy, prod.up is z.
+cudaError_t launch_quantize_act_backward(const QuantArgs &a, const CUtensorMap &tm_x, const CUtensorMap &tm_q,
+                                         const CUtensorMap &tm_qt, const CUtensorMap &tm_y, const ProdArgs &prod,
+                                         cudaStream_t s);
+// The activation quantiser fed by [dgate, dup] = [dh * up * act'(gate), dh * act(gate)]
+// (a.cols = 2 * cols of dh): tm_x maps dh.
+cudaError_t launch_quantize_gated_backward(const QuantArgs &a, const CUtensorMap &tm_x, const CUtensorMap &tm_q,
+                                           const CUtensorMap &tm_qt, const CUtensorMap &tm_y, const ProdArgs &prod,
+                                           cudaStream_t s);
+// The same without the quantiser (cols a multiple of 8); see act.cu.
+struct ActBackwardPlan {
+    int slabs;          // row slabs of the sums of dz
+    int64_t slab_rows;  // rows of each
+};
+ActBackwardPlan plan_act_backward(int64_t rows, int64_t cols);  // host-only, shape-only
+cudaError_t launch_act_backward(const uint16_t *dy, const uint16_t *z, int64_t rows, int64_t cols, int act, uint16_t *dz,
+                                float *partial, cudaStream_t s);
+cudaError_t launch_gated_backward(const uint16_t *dh, const uint16_t *gate, const uint16_t *up, int64_t rows, int64_t cols,
+                                  int64_t ld, int act, uint16_t *dgate_up, cudaStream_t s);
+// dbias[c] = the n partial sums of column c, in order.
+cudaError_t launch_column_sums(const float *partial, int64_t n, int64_t cols, float *dbias, cudaStream_t s);
+
 // y = bf16(silu(gate) * up), the unfused application (cols a multiple of 8;
 // gate and up rows ld elements apart, y contiguous).
 cudaError_t launch_swiglu_apply(const uint16_t *gate, const uint16_t *up, int64_t rows, int64_t cols, int64_t ld,

@@ -17,7 +17,9 @@
 // kernels are otherwise instruction bound.
 #include <cfloat>
 #include <cuda_bf16.h>
+#include <type_traits>
 
+#include "act_math.cuh"
 #include "internal.h"
 #include "ptx.cuh"
 #include "quant_math.cuh"
@@ -225,19 +227,6 @@ cudaError_t launch_rmsnorm_apply(const uint16_t *h, int64_t rows, int64_t cols, 
 }
 
 // ------------------------------------------------------ SwiGLU producer
-// 2^x and 1/x by the special-function unit (PTX ex2.approx / rcp.approx:
-// relative error around 2^-22; subnormal results flush to zero).
-PURO_DEV float ex2_approx(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-PURO_DEV float rcp_approx(float x) {
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 // silu(g) = g * sigmoid(g) in fp32, with sigmoid from t = e^-|g| (in (0, 1],
 // so nothing overflows): sigmoid(g) = r = 1 / (1 + t) for g >= 0, t * r
 // otherwise.  t = 2^(64 - |g| log2 e) * 2^-64: the special-function
@@ -595,6 +584,12 @@ struct QuantActSmem {
     alignas(16) uint16_t gamma[2][kQT];          // kProdRmsNorm: of the tile's columns
     uint64_t full[2];
 };
+// kProdActBackward: the rows' sums of the tile's columns, [row block][column].
+struct QuantActSumSmem : QuantActSmem {
+    alignas(16) float col_sum[16][kQT];
+};
+template <int PROD>
+using QuantActSmemOf = std::conditional_t<PROD == kProdActBackward, QuantActSumSmem, QuantActSmem>;
 
 // y = bf16((h * rstd) * gamma) for a 4-value chunk, two products an instruction
 // (rs: rstd twice; gm: the gains in pairs).
@@ -626,6 +621,43 @@ PURO_DEV uint2 swiglu_chunk4(uint2 g, uint2 u) {
     return make_uint2(out[0], out[1]);
 }
 
+PURO_DEV uint2 pack4(const float (&f)[4]) {
+    __nv_bfloat162 lo = __floats2bfloat162_rn(f[0], f[1]), hi = __floats2bfloat162_rn(f[2], f[3]);
+    return make_uint2(*reinterpret_cast<uint32_t *>(&lo), *reinterpret_cast<uint32_t *>(&hi));
+}
+PURO_DEV void unpack4(uint2 w, float (&f)[4]) {
+    f[0] = bf16_lo(w.x), f[1] = bf16_hi(w.x), f[2] = bf16_lo(w.y), f[3] = bf16_hi(w.y);
+}
+
+// dz = dy * act'(z) of a 4-value chunk, rounded to BF16; sum += dz unrounded.
+template <int ACT>
+PURO_DEV uint2 act_backward_chunk4(uint2 dy, uint2 z, float (&sum)[4]) {
+    float d[4], zf[4];
+    unpack4(dy, d);
+    unpack4(z, zf);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        d[j] *= act_slope_f32<ACT>(zf[j]).d;
+        sum[j] += d[j];
+    }
+    return ACT == PURO_ACT_NONE ? dy : pack4(d);
+}
+
+// dgate = dh * up * act'(gate) (half 0) or dup = dh * act(gate) (half 1).
+template <int ACT>
+PURO_DEV uint2 gated_backward_chunk4(uint2 dh, uint2 gate, uint2 up, int half) {
+    float d[4], g[4], u[4];
+    unpack4(dh, d);
+    unpack4(gate, g);
+    unpack4(up, u);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const ActSlope s = act_slope_f32<ACT>(g[j]);
+        d[j] *= half ? s.a : u[j] * s.d;
+    }
+    return pack4(d);
+}
+
 // Behind a producer the kernel is bound by its instructions between the tile's
 // three barriers, not by HBM, so the produced block stays in registers (it is
 // written back to shared memory only for a y output), RMSNorm's products are
@@ -643,8 +675,8 @@ __global__ void __launch_bounds__(kQAThreads, 2)
                      int64_t rows, int64_t cols, uint8_t *__restrict__ scale_u8, uint8_t *__restrict__ scale_t_u8,
                      ProdArgs prod, int tiles_n, int ntiles, int32_t *status, uint64_t wait_ns) {
     extern __shared__ uint8_t smem_raw[];
-    QuantActSmem &sm = *reinterpret_cast<QuantActSmem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
-                                                         ~static_cast<uintptr_t>(1023));
+    using Smem = QuantActSmemOf<PROD>;
+    Smem &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const int tid = threadIdx.x, lane = tid & 31;
     const int br = tid >> 5;  // block row: tile rows 8br .. 8br+7 (the warp)
     const int bc = lane;      // block column: tile columns 4bc .. 4bc+3
@@ -663,7 +695,7 @@ __global__ void __launch_bounds__(kQAThreads, 2)
     const uint32_t tile_bytes = kQT * kQT * 2 + (rstd16 ? kQT * 4 : 0) + (prod.gamma ? kQT * 2 : 0);
     auto issue_tile = [&](const TileWalk &t, int b) {
         mbar_arrive_expect_tx(&sm.full[b], PROD == kProdRmsNorm ? tile_bytes : kQT * kQT * 2);
-        tma_load_2d(sm.in[b], &tm_x, &sm.full[b], t.c * kQT, t.r * kQT);
+        tma_load_2d(sm.in[b], &tm_x, &sm.full[b], (PROD == kProdGatedBackward ? t.c >> 1 : t.c) * kQT, t.r * kQT);
     };
     auto issue_vectors = [&](const TileWalk &t, int b) {
         if constexpr (PROD == kProdRmsNorm) {
@@ -688,7 +720,7 @@ __global__ void __launch_bounds__(kQAThreads, 2)
         if (PROD != kProdRmsNorm) issue_tile(cur, 0);
         issue_vectors(cur, 0);
     }
-    uint2 un[8];  // kProdSwiGlu: this thread's block of u for the current tile
+    uint2 un[8] = {};  // this thread's block of u (kProdSwiGlu) or z (kProdActBackward) for the current tile
     auto load_up = [&](const TileWalk &t) {
         const int64_t row0 = static_cast<int64_t>(t.r) * kQT + 8 * br;
         const int64_t col0 = static_cast<int64_t>(t.c) * kQT + 4 * bc;
@@ -696,13 +728,13 @@ __global__ void __launch_bounds__(kQAThreads, 2)
 #pragma unroll
         for (int i = 0; i < 8; ++i) un[i] = __ldg(reinterpret_cast<const uint2 *>(p + i * prod.ld));
     };
-    if constexpr (PROD == kProdSwiGlu) {
-        if (tile < ntiles) load_up(cur);
-    }
+    constexpr bool kLoadsUp = PROD == kProdSwiGlu || PROD == kProdActBackward;
+    if (kLoadsUp && prod.up && tile < ntiles) load_up(cur);
     for (int it = 0; tile < ntiles; ++it, tile += step, cur = nxt, nxt.advance()) {
         const int buf = it & 1;
         const int64_t r0 = static_cast<int64_t>(cur.r) * kQT;
-        const int64_t c0 = static_cast<int64_t>(cur.c) * kQT;
+        // (kProdGatedBackward: the tiles of dgate and dup over the same gates follow one another)
+        const int64_t c0 = static_cast<int64_t>(PROD == kProdGatedBackward ? (cur.c & 1) * (tiles_n >> 1) + (cur.c >> 1) : cur.c) * kQT;
         if (tid == 0) {
             const int next = tile + step;
             // with a y output, the buffer's last reader was the y store of
@@ -753,6 +785,35 @@ __global__ void __launch_bounds__(kQAThreads, 2)
             }
             if (prod.write_y) fence_proxy_async_smem();
             if (tile + step < ntiles) load_up(nxt);
+        } else if constexpr (PROD == kProdActBackward) {
+            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            act_dispatch(prod.act, [&](auto act) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = act_backward_chunk4<decltype(act)::value>(v[i], un[i], sum);
+            });
+            if (prod.col_sum) *reinterpret_cast<float4 *>(&sm.col_sum[br][4 * bc]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+            if (prod.write_y) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) *reinterpret_cast<uint2 *>(in + (8 * br + i) * kQT + 4 * bc) = v[i];
+                fence_proxy_async_smem();
+            }
+            if (prod.up && tile + step < ntiles) load_up(nxt);
+        } else if constexpr (PROD == kProdGatedBackward) {
+            const int64_t at = (r0 + 8 * br) * prod.ld + static_cast<int64_t>(cur.c >> 1) * kQT + 4 * bc;
+            const int half = cur.c & 1;
+            act_dispatch(prod.act, [&](auto act) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint2 g = __ldg(reinterpret_cast<const uint2 *>(prod.gate + at + i * prod.ld));
+                    const uint2 u = half ? make_uint2(0u, 0u) : __ldg(reinterpret_cast<const uint2 *>(prod.up + at + i * prod.ld));
+                    v[i] = gated_backward_chunk4<decltype(act)::value>(v[i], g, u, half);
+                }
+            });
+            if (prod.write_y) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) *reinterpret_cast<uint2 *>(in + (8 * br + i) * kQT + 4 * bc) = v[i];
+                fence_proxy_async_smem();
+            }
         }
 
         // ---- A: row groups (a warp holds its eight rows whole) and column partials
@@ -810,6 +871,16 @@ __global__ void __launch_bounds__(kQAThreads, 2)
             if (prod.write_y && tid == 0) {  // every block's y is in shared memory
                 tma_store_2d(&tm_y, sm.in[buf], static_cast<int32_t>(c0), static_cast<int32_t>(r0));
                 bulk_commit_group();
+            }
+        }
+
+        if constexpr (PROD == kProdActBackward) {  // the tile's 128 rows, their blocks in order
+            if (prod.col_sum && tid >= kQAThreads - kQT) {
+                const int c = tid - (kQAThreads - kQT);
+                float a = sm.col_sum[0][c];
+#pragma unroll
+                for (int b = 1; b < 16; ++b) a += sm.col_sum[b][c];
+                prod.col_sum[static_cast<int64_t>(cur.r) * cols + c0 + c] = a;
             }
         }
 
@@ -1085,7 +1156,7 @@ static cudaError_t launch_quant_t(const QuantArgs &a, const CUtensorMap &tm_x, c
                                   ProdArgs prod = ProdArgs{}) {
     if constexpr (KIND == kQuantBlockAct) {  // the 512-thread activation kernel (whole tiles)
         auto kern = quant_act_kernel<FMT, HAS_T, PROD>;
-        const size_t smem = sizeof(QuantActSmem) + 1024;
+        const size_t smem = sizeof(QuantActSmemOf<PROD>) + 1024;
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
         if (e != cudaSuccess) return e;
         const int tiles_n = static_cast<int>(a.cols / kQT);
@@ -1160,6 +1231,28 @@ static cudaError_t launch_swiglu_f(const QuantArgs &a, const CUtensorMap &tm_x, 
                                    cudaStream_t s) {
     return a.has_t ? launch_quant_t<FMT, kQuantBlockAct, true, kProdSwiGlu>(a, tm_x, tm_q, tm_qt, s, &tm_y, prod)
                    : launch_quant_t<FMT, kQuantBlockAct, false, kProdSwiGlu>(a, tm_x, tm_q, tm_qt, s, &tm_y, prod);
+}
+
+template <int FMT, int PROD>
+static cudaError_t launch_prod_f(const QuantArgs &a, const CUtensorMap &tm_x, const CUtensorMap &tm_q,
+                                 const CUtensorMap &tm_qt, const CUtensorMap &tm_y, const ProdArgs &prod,
+                                 cudaStream_t s) {
+    return a.has_t ? launch_quant_t<FMT, kQuantBlockAct, true, PROD>(a, tm_x, tm_q, tm_qt, s, &tm_y, prod)
+                   : launch_quant_t<FMT, kQuantBlockAct, false, PROD>(a, tm_x, tm_q, tm_qt, s, &tm_y, prod);
+}
+
+cudaError_t launch_quantize_act_backward(const QuantArgs &a, const CUtensorMap &tm_x, const CUtensorMap &tm_q,
+                                         const CUtensorMap &tm_qt, const CUtensorMap &tm_y, const ProdArgs &prod,
+                                         cudaStream_t s) {
+    return a.fmt == 0 ? launch_prod_f<0, kProdActBackward>(a, tm_x, tm_q, tm_qt, tm_y, prod, s)
+                      : launch_prod_f<1, kProdActBackward>(a, tm_x, tm_q, tm_qt, tm_y, prod, s);
+}
+
+cudaError_t launch_quantize_gated_backward(const QuantArgs &a, const CUtensorMap &tm_x, const CUtensorMap &tm_q,
+                                           const CUtensorMap &tm_qt, const CUtensorMap &tm_y, const ProdArgs &prod,
+                                           cudaStream_t s) {
+    return a.fmt == 0 ? launch_prod_f<0, kProdGatedBackward>(a, tm_x, tm_q, tm_qt, tm_y, prod, s)
+                      : launch_prod_f<1, kProdGatedBackward>(a, tm_x, tm_q, tm_qt, tm_y, prod, s);
 }
 
 cudaError_t launch_quantize_swiglu(const QuantArgs &a, const CUtensorMap &tm_x, const CUtensorMap &tm_q,
