@@ -340,6 +340,53 @@ puro_status_t puro_fp8_linear_wgrad(const puro_fp8_tensor_t *dy_t, const puro_fp
                                     int32_t *dev_status, void *stream);
 
 /*
+ * Fprop with bias, activation and residual in the GEMM's epilogue:
+ *     z = x w^T + bias,   y = act(z) + residual
+ * (the qkv projection's bias in the Qwen2 shape; the output and down
+ * projections, whose result joins the residual stream; an ungated MLP's
+ * activation).  The product is accumulated and everything after it computed in
+ * FP32; y, and z where it is kept for puro_*_act_backward, are each rounded to
+ * BF16 once.
+ *   x, w, workspace, dev_status, y: as in puro_fp8_linear_fprop /
+ *     puro_bf16_linear_fprop (y bf16 [M, N]; the BF16 form takes any M, N and K
+ *     multiples of 8).
+ *   bias: bf16 [N], or NULL.
+ *   residual: bf16 [M, N] with rows ld_residual elements apart (>= N, a multiple
+ *     of 8), or NULL.  y may be the residual itself (then ld_residual = N).
+ *   z: bf16 [M, N], or NULL: not written.
+ * All pointers 16-byte aligned.  An empty reduction gives z = bias.
+ */
+puro_status_t puro_fp8_linear_fprop_epilogue(const puro_fp8_tensor_t *x, const puro_fp8_tensor_t *w, const void *bias,
+                                             int32_t act, const void *residual, int64_t ld_residual, void *z, void *y,
+                                             void *workspace, size_t workspace_bytes, int32_t *dev_status,
+                                             void *stream);
+puro_status_t puro_bf16_linear_fprop_epilogue(const void *x, const void *w, int64_t M, int64_t N, int64_t K,
+                                              const void *bias, int32_t act, const void *residual,
+                                              int64_t ld_residual, void *z, void *y, int32_t *dev_status,
+                                              void *stream);
+
+/*
+ * The gated MLP's two projections, activation and product in one kernel:
+ *     gate = x wg^T,  up = x wu^T,  h = act(gate) * up
+ * (PURO_ACT_SILU: SwiGLU; section "Model architecture and pretraining system").
+ * w is the fused gate/up weight [2F, K]: the rows of wg, then those of wu.  The
+ * products are accumulated and h computed in FP32; h is rounded to BF16 once.
+ *   gate_up: bf16 [M, 2F], the rounded products, kept for
+ *     puro_*_gated_backward, or NULL: not written.
+ * puro_fp8_gated_fprop (BLOCK operands; F a multiple of 128) quantises the BF16
+ * h exactly as puro_fp8_quantize does with PURO_SCALE_BLOCK / PURO_ROLE_ACT:
+ * hq [M, F], and hq_t [F, M] where given, with their scales, in format fmt;
+ * h itself (bf16 [M, F]) is written only when given.
+ * puro_bf16_gated_fprop writes h; any M, F and K multiples of 8.
+ * One kernel; an empty reduction gives zeros (memsets).
+ */
+puro_status_t puro_fp8_gated_fprop(const puro_fp8_tensor_t *x, const puro_fp8_tensor_t *w, int32_t act, int32_t fmt,
+                                   void *gate_up, void *h, uint8_t *hq, void *hq_scale, uint8_t *hq_t,
+                                   void *hq_t_scale, int32_t *dev_status, void *stream);
+puro_status_t puro_bf16_gated_fprop(const void *x, const void *w, int64_t M, int64_t F, int64_t K, int32_t act,
+                                    void *gate_up, void *h, int32_t *dev_status, void *stream);
+
+/*
  * Dgrad and Wgrad of one linear in one call.
  *
  *   dx = dy * w_t^T     (as puro_fp8_linear_dgrad)

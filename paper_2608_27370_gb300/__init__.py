@@ -99,6 +99,10 @@ _SIGNATURES = {
     "puro_bf16_linear_fprop": (_I32, [_P, _P, _P, _I64, _I64, _I64, _P, _P]),
     "puro_bf16_linear_dgrad": (_I32, [_P, _P, _P, _I64, _I64, _I64, _P, _P]),
     "puro_bf16_linear_wgrad": (_I32, [_P, _P, _P, _I64, _I64, _I64, _P, _P]),
+    "puro_fp8_linear_fprop_epilogue": (_I32, [_P, _P, _P, _I32, _P, _I64, _P, _P, _P, ctypes.c_size_t, _P, _P]),
+    "puro_bf16_linear_fprop_epilogue": (_I32, [_P, _P, _I64, _I64, _I64, _P, _I32, _P, _I64, _P, _P, _P, _P]),
+    "puro_fp8_gated_fprop": (_I32, [_P, _P, _I32, _I32, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "puro_bf16_gated_fprop": (_I32, [_P, _P, _I64, _I64, _I64, _I32, _P, _P, _P, _P]),
     "puro_fp8_quantize_act_backward": (_I32, [_P, _P, _I64, _I64, _I32, _I32, _P, _P, _P, ctypes.c_size_t, _P, _P, _P, _P, _P,
                                               _P]),
     "puro_act_backward_bf16": (_I32, [_P, _P, _I64, _I64, _I32, _P, _P, _P, ctypes.c_size_t, _P]),
@@ -570,6 +574,99 @@ def puro_bf16_linear_dgrad(dy, w_t, dx, M, N, K, dev_status=None, stream=None) -
 
 def puro_bf16_linear_wgrad(dy_t, x_t, dw, M, N, K, dev_status=None, stream=None) -> None:
     _bf16("puro_bf16_linear_wgrad", dy_t, x_t, dw, M, N, K, dev_status, stream)
+
+
+# --------------------------------------------------------------------------
+# Linears with an epilogue, the gated MLP's projections
+# --------------------------------------------------------------------------
+def _rows_of(t: Optional[torch.Tensor], rows: int, cols: int, name: str):
+    """Pointer and row stride of an optional bf16 [rows, cols] view with unit column stride."""
+    if t is None:
+        return None, cols
+    if not t.is_cuda or t.dtype != torch.bfloat16 or tuple(t.shape) != (rows, cols):
+        raise ValueError(f"{name} must be a bf16 CUDA tensor [{rows}, {cols}]")
+    if t.numel() and t.stride(1) != 1:
+        raise ValueError(f"{name} must have unit column stride")
+    return t.data_ptr() or None, t.stride(0) if rows > 1 else cols
+
+
+def puro_fp8_linear_fprop_epilogue(x: FP8Operand, w: FP8Operand, y: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                                   act: int = ACT_NONE, residual: Optional[torch.Tensor] = None,
+                                   z: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                                   dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Y [M,N] = act(Z) + residual, Z = X [M,K] . W [N,K]^T + bias, all behind
+    the product in the GEMM's epilogue.  bias bf16 [N]; residual bf16 [M,N]
+    (rows may be strided; it may be y); z, when given, receives Z (bf16 [M,N])
+    for the backward."""
+    _on_current_device(x.data, w.data, y, bias, residual, z, workspace, dev_status)
+    st = (_native or _load_native()).puro_fp8_linear_fprop_epilogue(x, w, y, bias, act, residual, z, workspace, dev_status,
+                                                                    stream)
+    if st is not None:
+        return _check("puro_fp8_linear_fprop_epilogue", st)
+    cx, cw = x.as_c(), w.as_c()
+    m, n, bf16 = cx.rows, cw.rows, torch.bfloat16
+    res, ld = _rows_of(residual, m, n, "residual")
+    st = load_library().puro_fp8_linear_fprop_epilogue(
+        ctypes.byref(cx), ctypes.byref(cw), _sized(bias, bf16, n, "bias"), act, res, ld, _sized(z, bf16, m * n, "z"),
+        _sized(y, bf16, m * n, "y"), *_ws(workspace), _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
+    _check("puro_fp8_linear_fprop_epilogue", st)
+
+
+def puro_bf16_linear_fprop_epilogue(x: torch.Tensor, w: torch.Tensor, y: torch.Tensor,
+                                    bias: Optional[torch.Tensor] = None, act: int = ACT_NONE,
+                                    residual: Optional[torch.Tensor] = None, z: Optional[torch.Tensor] = None,
+                                    dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The same from BF16 x [M,K] and w [N,K]; any M, from a single token on."""
+    _on_current_device(x, w, y, bias, residual, z, dev_status)
+    st = (_native or _load_native()).puro_bf16_linear_fprop_epilogue(x, w, y, bias, act, residual, z, dev_status, stream)
+    if st is not None:
+        return _check("puro_bf16_linear_fprop_epilogue", st)
+    (m, k), n, bf16 = x.shape, w.shape[0], torch.bfloat16
+    res, ld = _rows_of(residual, m, n, "residual")
+    st = load_library().puro_bf16_linear_fprop_epilogue(
+        _ptr(x, bf16, "x"), _sized(w, bf16, n * k, "w"), m, n, k, _sized(bias, bf16, n, "bias"), act, res, ld,
+        _sized(z, bf16, m * n, "z"), _sized(y, bf16, m * n, "y"), _ptr(dev_status, torch.int32, "dev_status"),
+        _stream(stream))
+    _check("puro_bf16_linear_fprop_epilogue", st)
+
+
+def puro_fp8_gated_fprop(x: FP8Operand, w: FP8Operand, act: int, fmt: int, gate_up: Optional[torch.Tensor],
+                         h: Optional[torch.Tensor], hq: torch.Tensor, hq_scale: torch.Tensor,
+                         hq_t: Optional[torch.Tensor] = None, hq_t_scale: Optional[torch.Tensor] = None,
+                         dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The gated MLP's two projections, activation and product in one kernel:
+    h = act(X . Wg^T) * (X . Wu^T), w = [Wg; Wu] [2F,K] quantised as one
+    operand.  h is written as the FP8 copies that puro_fp8_quantize makes of
+    it; gate_up (bf16 [M,2F], for the backward) and h (bf16 [M,F]) only when
+    given."""
+    _on_current_device(x.data, w.data, gate_up, h, hq, hq_scale, hq_t, hq_t_scale, dev_status)
+    st = (_native or _load_native()).puro_fp8_gated_fprop(x, w, act, fmt, gate_up, h, hq, hq_scale, hq_t, hq_t_scale,
+                                                          dev_status, stream)
+    if st is not None:
+        return _check("puro_fp8_gated_fprop", st)
+    cx, cw = x.as_c(), w.as_c()
+    n, u8, bf16 = cx.rows * (cw.rows // 2), torch.uint8, torch.bfloat16
+    st = load_library().puro_fp8_gated_fprop(
+        ctypes.byref(cx), ctypes.byref(cw), act, fmt, _sized(gate_up, bf16, cx.rows * cw.rows, "gate_up"),
+        _sized(h, bf16, n, "h"), _sized(hq, u8, n, "hq"), _ptr(hq_scale, u8, "hq_scale"), _sized(hq_t, u8, n, "hq_t"),
+        _ptr(hq_t_scale, u8, "hq_t_scale"), _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
+    _check("puro_fp8_gated_fprop", st)
+
+
+def puro_bf16_gated_fprop(x: torch.Tensor, w: torch.Tensor, act: int, gate_up: Optional[torch.Tensor], h: torch.Tensor,
+                          dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The same from BF16 x [M,K] and w [2F,K], h in BF16; any M, from a single token on."""
+    _on_current_device(x, w, gate_up, h, dev_status)
+    st = (_native or _load_native()).puro_bf16_gated_fprop(x, w, act, gate_up, h, dev_status, stream)
+    if st is not None:
+        return _check("puro_bf16_gated_fprop", st)
+    (m, k), n, bf16 = x.shape, w.shape[0], torch.bfloat16
+    if n % 2:
+        raise ValueError("w must hold the gate's and up's rows, as many of each")
+    st = load_library().puro_bf16_gated_fprop(
+        _ptr(x, bf16, "x"), _sized(w, bf16, n * k, "w"), m, n // 2, k, act, _sized(gate_up, bf16, m * n, "gate_up"),
+        _sized(h, bf16, m * (n // 2), "h"), _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
+    _check("puro_bf16_gated_fprop", st)
 
 
 # --------------------------------------------------------------------------

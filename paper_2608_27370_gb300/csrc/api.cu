@@ -281,6 +281,29 @@ puro_status_t fp8_backward(const puro_fp8_tensor_t *dy, const puro_fp8_tensor_t 
     return run_fp8_gemm(aw, gw, mw, s);
 }
 
+// The BF16 GEMM's arguments and maps but for the output's (M, N, K > 0).
+puro_status_t prepare_bf16_gemm(const void *a, const void *b, int64_t M, int64_t N, int64_t K, int tile_n,
+                                int32_t *dev_status, GemmArgs *g, GemmMaps *m) {
+    *m = GemmMaps{};
+    if (!make_map(&m->a, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a, K, M, K * 2, kGemmBKBytes / 2, kGemmBM,
+                  CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !make_map(&m->b, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, b, K, N, K * 2, kGemmBKBytes / 2,
+                  static_cast<uint32_t>(tile_n / 2), CU_TENSOR_MAP_SWIZZLE_128B))
+        return PURO_ERR_CUDA;
+    m->d = m->ws = m->sfa = m->sfb = m->a;  // (the kernel prefetches every descriptor)
+    *g = GemmArgs{};
+    g->kind = kGemmBF16;
+    g->M = M;
+    g->N = N;
+    g->K = K;
+    g->tile_n = tile_n;
+    g->status = dev_status;
+    g->wait_timeout_ns = g_wait_timeout_ns.load();
+    g->num_sms = sm_count();
+    g->splits = 1;
+    return g->num_sms > 0 ? PURO_OK : PURO_ERR_CUDA;
+}
+
 puro_status_t bf16_gemm(const void *a, const void *b, void *d, int64_t M, int64_t N, int64_t K,
                         int32_t *dev_status, void *stream) {
     if (!a || !b || !d || !aligned16(a) || !aligned16(b) || !aligned16(d)) return PURO_ERR_INVALID_ARG;
@@ -289,29 +312,103 @@ puro_status_t bf16_gemm(const void *a, const void *b, void *d, int64_t M, int64_
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (M == 0 || N == 0) return PURO_OK;
     if (K == 0) return cuda_status(cudaMemsetAsync(d, 0, static_cast<size_t>(M * N) * 2, s));
-    const int tile_n = tile_width(kGemmBF16, false, M, N, K);
-    GemmMaps m{};
-    if (!make_map(&m.a, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a, K, M, K * 2, kGemmBKBytes / 2, kGemmBM,
-                  CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !make_map(&m.b, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, b, K, N, K * 2, kGemmBKBytes / 2,
-                  static_cast<uint32_t>(tile_n / 2), CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !make_map(&m.d, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, d, N, M, N * 2, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
+    GemmArgs g;
+    GemmMaps m;
+    const puro_status_t st =
+        prepare_bf16_gemm(a, b, M, N, K, tile_width(kGemmBF16, false, M, N, K), dev_status, &g, &m);
+    if (st != PURO_OK) return st;
+    if (!make_map(&m.d, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, d, N, M, N * 2, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
         return PURO_ERR_CUDA;
-    m.ws = m.d;
-    m.sfa = m.d;
-    m.sfb = m.d;
-    GemmArgs g{};
-    g.kind = kGemmBF16;
-    g.M = M;
-    g.N = N;
-    g.K = K;
-    g.tile_n = tile_n;
-    g.status = dev_status;
-    g.wait_timeout_ns = g_wait_timeout_ns.load();
-    g.num_sms = sm_count();
-    if (g.num_sms <= 0) return PURO_ERR_CUDA;
-    g.splits = 1;
     g.out = d;
+    return cuda_status(launch_gemm(g, m, s));
+}
+
+// ---- linears with an epilogue, and the gated MLP's two projections
+bool valid_act(int32_t a) { return a >= PURO_ACT_NONE && a <= PURO_ACT_GELU_TANH; }
+
+puro_status_t check_epilogue(const void *bias, int32_t act, const void *residual, int64_t ld_residual, const void *z,
+                             const void *y, int64_t M, int64_t N, GemmEpilogue *e) {
+    if (!valid_act(act) || !aligned16(bias) || !aligned16(residual) || !aligned16(z)) return PURO_ERR_INVALID_ARG;
+    if (residual && (ld_residual < N || ld_residual % 8)) return PURO_ERR_INVALID_ARG;
+    if (M > 0 && N > 0 && (!y || !aligned16(y))) return PURO_ERR_INVALID_ARG;
+    *e = GemmEpilogue{};
+    e->on = true;
+    e->act = act;
+    e->bias = static_cast<const uint16_t *>(bias);
+    e->residual = static_cast<const uint16_t *>(residual);
+    e->ld_residual = ld_residual;
+    e->z = static_cast<uint16_t *>(const_cast<void *>(z));
+    e->y = static_cast<uint16_t *>(const_cast<void *>(y));
+    return PURO_OK;
+}
+
+puro_status_t fp8_gemm_epilogue(const puro_fp8_tensor_t *x, const puro_fp8_tensor_t *w, const void *bias, int32_t act,
+                                const void *residual, int64_t ld_residual, void *z, void *y, void *workspace,
+                                size_t workspace_bytes, int32_t *dev_status, void *stream) {
+    puro_status_t st = validate_fp8_gemm(x, w, y);
+    if (st != PURO_OK) return st;
+    GemmEpilogue epi;
+    st = check_epilogue(bias, act, residual, ld_residual, z, y, x->rows, w->rows, &epi);
+    if (st != PURO_OK) return st;
+    GemmArgs g{};
+    GemmMaps m{};
+    GemmAction action;
+    const int width = g_tile_n.load() ? 256 : 0;
+    st = prepare_fp8_gemm(x, w, y, workspace, workspace_bytes, dev_status, false, width, &g, &m, &action);
+    if (st != PURO_OK) return st;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (action == kGemmZeroFill) {  // an empty reduction: the epilogue of zero
+        const int sms = sm_count();
+        return sms > 0 ? cuda_status(launch_epilogue(nullptr, 0, 0, g.M, g.N, epi, sms, s)) : PURO_ERR_CUDA;
+    }
+    g.epi = epi;
+    return run_fp8_gemm(action, g, m, s);
+}
+
+puro_status_t bf16_gemm_epilogue(const void *x, const void *w, int64_t M, int64_t N, int64_t K, const void *bias,
+                                 int32_t act, const void *residual, int64_t ld_residual, void *z, void *y,
+                                 int32_t *dev_status, void *stream) {
+    if (M < 0 || N < 0 || K < 0 || N % 8 || K % 8) return PURO_ERR_INVALID_ARG;
+    if (M > INT32_MAX || N > INT32_MAX || K > INT32_MAX) return PURO_ERR_UNSUPPORTED;
+    GemmEpilogue epi;
+    puro_status_t st = check_epilogue(bias, act, residual, ld_residual, z, y, M, N, &epi);
+    if (st != PURO_OK) return st;
+    if (M == 0 || N == 0) return PURO_OK;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (K == 0) {
+        const int sms = sm_count();
+        return sms > 0 ? cuda_status(launch_epilogue(nullptr, 0, 0, M, N, epi, sms, s)) : PURO_ERR_CUDA;
+    }
+    if (!x || !w || !aligned16(x) || !aligned16(w)) return PURO_ERR_INVALID_ARG;
+    GemmArgs g;
+    GemmMaps m;
+    st = prepare_bf16_gemm(x, w, M, N, K, tile_width(kGemmBF16, false, M, N, K), dev_status, &g, &m);
+    if (st != PURO_OK) return st;
+    g.epi = epi;
+    return cuda_status(launch_gemm(g, m, s));
+}
+
+puro_status_t bf16_gated(const void *x, const void *w, int64_t M, int64_t F, int64_t K, int32_t act, void *gate_up,
+                         void *h, int32_t *dev_status, void *stream) {
+    if (M < 0 || F < 0 || K < 0 || F % 8 || K % 8) return PURO_ERR_INVALID_ARG;
+    if (M > INT32_MAX || 2 * F > INT32_MAX || K > INT32_MAX) return PURO_ERR_UNSUPPORTED;
+    GemmEpilogue epi;
+    puro_status_t st = check_epilogue(nullptr, act, nullptr, 0, gate_up, h, M, F, &epi);
+    if (st != PURO_OK) return st;
+    if (M == 0 || F == 0) return PURO_OK;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (K == 0) {
+        cudaError_t e = cudaMemsetAsync(h, 0, static_cast<size_t>(M * F) * 2, s);
+        if (e == cudaSuccess && gate_up) e = cudaMemsetAsync(gate_up, 0, static_cast<size_t>(M * F) * 4, s);
+        return cuda_status(e);
+    }
+    if (!x || !w || !aligned16(x) || !aligned16(w)) return PURO_ERR_INVALID_ARG;
+    GemmArgs g;
+    GemmMaps m;
+    st = prepare_bf16_gemm(x, w, M, 2 * F, K, 256, dev_status, &g, &m);
+    if (st != PURO_OK) return st;
+    g.epi = epi;
+    g.gated = true;
     return cuda_status(launch_gemm(g, m, s));
 }
 
@@ -319,9 +416,12 @@ puro_status_t bf16_gemm(const void *a, const void *b, void *d, int64_t M, int64_
 // quantised in the epilogue into the blockwise activation copies of D: Dq
 // [M, N] with 1x128 groups along N and, when q_t is given, Dq^T [N, M] with
 // groups of 128 rows; D itself in BF16 only when d is given.
+// gate: the activation of the gated MLP, whose h = act(gate) * up takes D's
+// place (b's rows are the gate's, then up's; gate_up: both in BF16, optional),
+// or null.
 puro_status_t fp8_gemm_quant(const puro_fp8_tensor_t *a, const puro_fp8_tensor_t *b, int32_t fmt, void *d,
                              uint8_t *q, void *q_scale, uint8_t *q_t, void *q_t_scale, int32_t *dev_status,
-                             void *stream) {
+                             void *stream, const int32_t *gate = nullptr, void *gate_up = nullptr) {
     puro_status_t st = check_operand(a);
     if (st != PURO_OK) return st;
     st = check_operand(b);
@@ -333,7 +433,8 @@ puro_status_t fp8_gemm_quant(const puro_fp8_tensor_t *a, const puro_fp8_tensor_t
     if ((q_t == nullptr) != (q_t_scale == nullptr)) return PURO_ERR_INVALID_ARG;
     if (q_t && (!aligned16(q_t) || !aligned16(q_t_scale))) return PURO_ERR_INVALID_ARG;
     if (d && !aligned16(d)) return PURO_ERR_INVALID_ARG;
-    const int64_t M = a->rows, N = b->rows, K = a->red;  // multiples of 128 (check_operand)
+    if (gate && (!valid_act(*gate) || b->rows % 256 || !aligned16(gate_up))) return PURO_ERR_INVALID_ARG;
+    const int64_t M = a->rows, K = a->red, N = gate ? b->rows / 2 : b->rows;  // multiples of 128 (check_operand)
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (M == 0 || N == 0) return PURO_OK;
     if (K == 0) {  // a zero product: zero codes, scale exponent 127 (as the quantiser gives an all-zero tensor)
@@ -343,14 +444,15 @@ puro_status_t fp8_gemm_quant(const puro_fp8_tensor_t *a, const puro_fp8_tensor_t
         if (e == cudaSuccess && q_t)
             e = cudaMemsetAsync(q_t_scale, 127, static_cast<size_t>(N * ((M / 128 + 3) / 4) * 4), s);
         if (e == cudaSuccess && d) e = cudaMemsetAsync(d, 0, static_cast<size_t>(M * N) * 2, s);
+        if (e == cudaSuccess && gate_up) e = cudaMemsetAsync(gate_up, 0, static_cast<size_t>(M * N) * 4, s);
         return cuda_status(e);
     }
     GemmMaps m{};
     if (!make_map(&m.a, CU_TENSOR_MAP_DATA_TYPE_UINT8, a->data, K, M, K, kGemmBKBytes, kGemmBM,
                   CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !make_map(&m.b, CU_TENSOR_MAP_DATA_TYPE_UINT8, b->data, K, N, K, kGemmBKBytes, kGemmBN / 2,
+        !make_map(&m.b, CU_TENSOR_MAP_DATA_TYPE_UINT8, b->data, K, b->rows, K, kGemmBKBytes, kGemmBN / 2,
                   CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !make_scale_map(&m.sfa, a->scale, M, K) || !make_scale_map(&m.sfb, b->scale, N, K))
+        !make_scale_map(&m.sfa, a->scale, M, K) || !make_scale_map(&m.sfb, b->scale, b->rows, K))
         return PURO_ERR_CUDA;
     m.d = m.a;  // the quantising epilogue stores from registers: no output map (the kernel prefetches tm_d)
     m.ws = m.a;
@@ -359,7 +461,7 @@ puro_status_t fp8_gemm_quant(const puro_fp8_tensor_t *a, const puro_fp8_tensor_t
     g.a_fmt = a->fmt;
     g.b_fmt = b->fmt;
     g.M = M;
-    g.N = N;
+    g.N = b->rows;
     g.K = K;
     g.tile_n = 256;
     g.sfb = static_cast<const uint8_t *>(b->scale);
@@ -376,6 +478,12 @@ puro_status_t fp8_gemm_quant(const puro_fp8_tensor_t *a, const puro_fp8_tensor_t
     g.qt = q_t;
     g.qt_scale = static_cast<uint8_t *>(q_t_scale);
     g.d_bf16 = d;
+    if (gate) {
+        g.gated = true;
+        g.epi.act = *gate;
+        g.epi.z = static_cast<uint16_t *>(gate_up);
+        g.epi.y = static_cast<uint16_t *>(d);
+    }
     return cuda_status(launch_gemm(g, m, s));
 }
 
@@ -648,8 +756,6 @@ PURO_API puro_status_t puro_rmsnorm_bf16(const void *h, int64_t rows, int64_t co
 namespace puro {
 namespace {
 
-bool valid_act(int32_t a) { return a >= PURO_ACT_NONE && a <= PURO_ACT_GELU_TANH; }
-
 // Quantiser arguments and maps of a producer that reads x (rows x_ld elements
 // apart, x_cols columns) and quantises [rows, cols], with an optional BF16 output y.
 bool producer_maps(const void *x, int64_t x_cols, int64_t x_ld, int64_t rows, int64_t cols, int32_t fmt, void *y,
@@ -786,6 +892,31 @@ PURO_API puro_status_t puro_fp8_linear_fprop(const puro_fp8_tensor_t *x, const p
                                              void *workspace, size_t workspace_bytes, int32_t *dev_status,
                                              void *stream) {
     return fp8_gemm(x, w, y, workspace, workspace_bytes, dev_status, stream);
+}
+
+PURO_API puro_status_t puro_fp8_linear_fprop_epilogue(const puro_fp8_tensor_t *x, const puro_fp8_tensor_t *w,
+                                                      const void *bias, int32_t act, const void *residual,
+                                                      int64_t ld_residual, void *z, void *y, void *workspace,
+                                                      size_t workspace_bytes, int32_t *dev_status, void *stream) {
+    return fp8_gemm_epilogue(x, w, bias, act, residual, ld_residual, z, y, workspace, workspace_bytes, dev_status, stream);
+}
+
+PURO_API puro_status_t puro_bf16_linear_fprop_epilogue(const void *x, const void *w, int64_t M, int64_t N, int64_t K,
+                                                       const void *bias, int32_t act, const void *residual,
+                                                       int64_t ld_residual, void *z, void *y, int32_t *dev_status,
+                                                       void *stream) {
+    return bf16_gemm_epilogue(x, w, M, N, K, bias, act, residual, ld_residual, z, y, dev_status, stream);
+}
+
+PURO_API puro_status_t puro_fp8_gated_fprop(const puro_fp8_tensor_t *x, const puro_fp8_tensor_t *w, int32_t act,
+                                            int32_t fmt, void *gate_up, void *h, uint8_t *hq, void *hq_scale,
+                                            uint8_t *hq_t, void *hq_t_scale, int32_t *dev_status, void *stream) {
+    return fp8_gemm_quant(x, w, fmt, h, hq, hq_scale, hq_t, hq_t_scale, dev_status, stream, &act, gate_up);
+}
+
+PURO_API puro_status_t puro_bf16_gated_fprop(const void *x, const void *w, int64_t M, int64_t F, int64_t K, int32_t act,
+                                             void *gate_up, void *h, int32_t *dev_status, void *stream) {
+    return bf16_gated(x, w, M, F, K, act, gate_up, h, dev_status, stream);
 }
 
 PURO_API puro_status_t puro_fp8_linear_dgrad(const puro_fp8_tensor_t *dy, const puro_fp8_tensor_t *w_t, void *dx,

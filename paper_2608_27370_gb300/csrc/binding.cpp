@@ -42,6 +42,10 @@ PyObject *operand_type = nullptr;  // the binding's FP8Operand class
     X(puro_bf16_linear_fprop)          \
     X(puro_bf16_linear_dgrad)          \
     X(puro_bf16_linear_wgrad)          \
+    X(puro_fp8_linear_fprop_epilogue)  \
+    X(puro_bf16_linear_fprop_epilogue) \
+    X(puro_fp8_gated_fprop)            \
+    X(puro_bf16_gated_fprop)           \
     X(puro_fp8_quantize_act_backward)  \
     X(puro_act_backward_bf16)          \
     X(puro_fp8_quantize_gated_backward) \
@@ -206,6 +210,17 @@ struct Args {
         *rows = g->size(0);
         *cols = g->size(1);
         *ld = g->stride(0);
+    }
+    // An optional bf16 [rows, cols] view with unit column stride, and its row stride.
+    const void *rows_of(int i, int64_t rows, int64_t cols, int64_t *ld) {
+        *ld = cols;
+        if (v[i] == Py_None) return nullptr;
+        const at::Tensor *t = plain(v[i]);
+        if (!t || t->scalar_type() != at::kBFloat16 || t->dim() != 2 || t->size(0) != rows || t->size(1) != cols ||
+            t->stride(1) != 1)
+            return fail();
+        if (rows > 1) *ld = t->stride(0);
+        return t->data_ptr();
     }
     // A tensor's number of values has to be n.
     void numel(int i, int64_t n) {
@@ -394,6 +409,77 @@ PyObject *bf16_wgrad_call(Args &a) { return bf16(a, lib.puro_bf16_linear_wgrad);
 PURO_NATIVE(bf16_fprop, 8)
 PURO_NATIVE(bf16_dgrad, 8)
 PURO_NATIVE(bf16_wgrad, 8)
+
+// (x, w, y, bias, act, residual, z, workspace, dev_status, stream)
+PyObject *linear_fprop_epilogue_call(Args &a) {
+    puro_fp8_tensor_t x, w;
+    a.operand(0, &x);
+    a.operand(1, &w);
+    void *y = a.ptr(2, kBF16), *z = a.opt(6, kBF16);
+    const void *bias = a.opt(3, kBF16);
+    const int32_t act = a.i32(4);
+    int64_t ld;
+    const void *res = a.rows_of(5, x.rows, w.rows, &ld);
+    size_t bytes;
+    void *ws = a.scratch(7, &bytes);
+    int32_t *st = a.status(8);
+    void *s = a.stream(9);
+    for (int i : {2, 6}) a.numel(i, x.rows * w.rows);
+    a.numel(3, w.rows);
+    return finish(a, [&] { return lib.puro_fp8_linear_fprop_epilogue(&x, &w, bias, act, res, ld, z, y, ws, bytes, st, s); });
+}
+PURO_NATIVE(linear_fprop_epilogue, 10)
+
+// (x, w, y, bias, act, residual, z, dev_status, stream)
+PyObject *bf16_fprop_epilogue_call(Args &a) {
+    const void *x = a.ptr(0, kBF16), *w = a.ptr(1, kBF16), *bias = a.opt(3, kBF16);
+    void *y = a.ptr(2, kBF16), *z = a.opt(6, kBF16);
+    int64_t M, K, N, K2, ld;
+    a.shape(0, &M, &K);
+    a.shape(1, &N, &K2);
+    if (K != K2) a.ok = false;
+    const int32_t act = a.i32(4);
+    const void *res = a.rows_of(5, M, N, &ld);
+    int32_t *st = a.status(7);
+    void *s = a.stream(8);
+    for (int i : {2, 6}) a.numel(i, M * N);
+    a.numel(3, N);
+    return finish(a, [&] { return lib.puro_bf16_linear_fprop_epilogue(x, w, M, N, K, bias, act, res, ld, z, y, st, s); });
+}
+PURO_NATIVE(bf16_fprop_epilogue, 9)
+
+// (x, w, act, fmt, gate_up, h, hq, hq_scale, hq_t, hq_t_scale, dev_status, stream)
+PyObject *gated_fprop_call(Args &a) {
+    puro_fp8_tensor_t x, w;
+    a.operand(0, &x);
+    a.operand(1, &w);
+    const int32_t act = a.i32(2), fmt = a.i32(3);
+    void *gu = a.opt(4, kBF16), *h = a.opt(5, kBF16), *sc = a.opt(7, kU8), *sct = a.opt(9, kU8);
+    uint8_t *q = u8(a.opt(6, kU8)), *qt = u8(a.opt(8, kU8));
+    int32_t *st = a.status(10);
+    void *s = a.stream(11);
+    a.numel(4, x.rows * w.rows);
+    for (int i : {5, 6, 8}) a.numel(i, x.rows * (w.rows / 2));
+    return finish(a, [&] { return lib.puro_fp8_gated_fprop(&x, &w, act, fmt, gu, h, q, sc, qt, sct, st, s); });
+}
+PURO_NATIVE(gated_fprop, 12)
+
+// (x, w, act, gate_up, h, dev_status, stream)
+PyObject *bf16_gated_fprop_call(Args &a) {
+    const void *x = a.ptr(0, kBF16), *w = a.ptr(1, kBF16);
+    int64_t M, K, N, K2;
+    a.shape(0, &M, &K);
+    a.shape(1, &N, &K2);
+    if (K != K2 || N % 2) a.ok = false;
+    const int32_t act = a.i32(2);
+    void *gu = a.opt(3, kBF16), *h = a.ptr(4, kBF16);
+    int32_t *st = a.status(5);
+    void *s = a.stream(6);
+    a.numel(3, M * N);
+    a.numel(4, M * (N / 2));
+    return finish(a, [&] { return lib.puro_bf16_gated_fprop(x, w, M, N / 2, K, act, gu, h, st, s); });
+}
+PURO_NATIVE(bf16_gated_fprop, 7)
 
 // (dy, z, act, fmt, dz, dbias, workspace, q, scale, q_t, scale_t, dev_status, stream)
 PyObject *quantize_act_backward_call(Args &a) {
@@ -586,6 +672,10 @@ PyMethodDef methods[] = {PURO_METHOD("set_operand_type", set_operand_type),
                          PURO_METHOD("puro_bf16_linear_fprop", bf16_fprop),
                          PURO_METHOD("puro_bf16_linear_dgrad", bf16_dgrad),
                          PURO_METHOD("puro_bf16_linear_wgrad", bf16_wgrad),
+                         PURO_METHOD("puro_fp8_linear_fprop_epilogue", linear_fprop_epilogue),
+                         PURO_METHOD("puro_bf16_linear_fprop_epilogue", bf16_fprop_epilogue),
+                         PURO_METHOD("puro_fp8_gated_fprop", gated_fprop),
+                         PURO_METHOD("puro_bf16_gated_fprop", bf16_gated_fprop),
                          PURO_METHOD("puro_fp8_quantize_act_backward", quantize_act_backward),
                          PURO_METHOD("puro_act_backward_bf16", act_backward_bf16),
                          PURO_METHOD("puro_fp8_quantize_gated_backward", quantize_gated_backward),

@@ -60,6 +60,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "act_math.cuh"
 #include "internal.h"
 #include "ptx.cuh"
 #include "quant_math.cuh"
@@ -179,6 +180,7 @@ struct GemmParams {
     // unit fewer take first (see PairUnits); 0: plain round-robin.
     int lead;
     const uint8_t *b;  // B (rows of K bytes) where it is prefetched, or null
+    GemmEpilogue epi;  // the forms with an epilogue
 };
 
 // Instruction descriptors (tcgen05.mma), both operands K-major, M = 256
@@ -527,6 +529,279 @@ PURO_DEV void quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int w
     }
 }
 
+// ------------------------------------------------ epilogues that compute
+// Forms whose epilogue does more than round the accumulator have more epilogue
+// warps: warp 4 + 4j + q takes column quarter j of the tile and the rows of
+// tensor-memory lane quarter q, one per lane.  Four warps a scheduler keep the
+// special-function chains of the activations overlapped.  Everything they read
+// (bias, residual) comes straight from global memory; everything they
+// write leaves from registers as whole 64-byte row segments
+// (quad_transpose_chunks), so rows and columns may end anywhere (columns at a
+// multiple of eight).
+template <int OUT, int BN, int S>
+constexpr bool wide_epilogue_form() {
+    return S == 1 && (OUT == kGemmOutEpilogue || OUT == kGemmOutGated || OUT == kGemmOutGatedQuant);
+}
+
+// 32 values of each lane's row, rounded to BF16, to out[row, col0 .. col0 + 31]
+// (rows ld elements apart), rows below `rows` and columns below `cols` only.
+PURO_DEV void store_rows32(const float (&f)[32], uint16_t *out, int64_t ld, int row0, int col0, int rows, int cols,
+                           int lane) {
+    uint32_t x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+        x[i] = *reinterpret_cast<uint32_t *>(&b);
+    }
+    quad_transpose_chunks(x, lane);
+    const int row = row0 + (lane & ~3), col = col0 + 8 * (lane & 3);
+    if (col >= cols) return;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        if (row + r < rows)
+            *reinterpret_cast<uint4 *>(out + static_cast<int64_t>(row + r) * ld + col) =
+                make_uint4(x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]);
+}
+
+PURO_DEV void add8(float *f, const uint4 &w) {
+    const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] += bf16_lo(ws[i]);
+        f[2 * i + 1] += bf16_hi(ws[i]);
+    }
+}
+
+// z = f + bias in place for the 32 columns from col0 (columns past the last one unused).
+PURO_DEV void add_bias32(float (&f)[32], const GemmEpilogue &epi, int col0, int cols) {
+    if (!epi.bias) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (col0 + 8 * i < cols) add8(f + 8 * i, __ldg(reinterpret_cast<const uint4 *>(epi.bias + col0 + 8 * i)));
+}
+
+// y = act(f) + residual in place.
+PURO_DEV void finish32(float (&f)[32], const GemmEpilogue &epi, int row, int col0, int rows, int cols) {
+    if (epi.act != PURO_ACT_NONE)
+        act_dispatch(epi.act, [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) f[i] = act_f32<decltype(act)::value>(f[i]);
+        });
+    if (epi.residual && row < rows) {
+        const uint16_t *r = epi.residual + row * epi.ld_residual + col0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)  // (the output may be the residual itself)
+            if (col0 + 8 * i < cols) add8(f + 8 * i, *reinterpret_cast<const uint4 *>(r + 8 * i));
+    }
+}
+
+// kGemmOutEpilogue and kGemmOutGated.
+template <int KIND, int OUT, int BN, bool SHIFTED, class Smem>
+PURO_DEV void wide_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int warp, int lane, int pair, int num_pairs,
+                            int rank) {
+    constexpr int kAccBufs = SHIFTED ? 1 : 2, kAccShift = SHIFTED ? 128 : 256;
+    const int j = (warp - 4) >> 2, q = warp & 3;
+    const uint32_t tempty0 = mapa_shared(smem_u32(&sm.tempty[0]), 0);  // the even CTA's
+    float sab = 1.0f;
+    if constexpr (KIND == kGemmFP8Tensor) sab = __fmul_rn(*p.sia, *p.sib);
+    int local = 0;
+    PairUnits units(p, pair, num_pairs);
+    for (int u = units.next(); u >= 0; u = units.next(), ++local) {
+        const WorkUnit wu = work_unit<BN>(p, u);
+        const int row0 = wu.m0 + kBM * rank + 32 * q;
+        const int buf = local % kAccBufs;
+        bool ok = (sm.abort_flag == 0) &&
+                  mbar_wait_bounded(&sm.tfull[buf], static_cast<uint32_t>(local / kAccBufs) & 1u, p.wait_ns);
+        if (!__all_sync(0xFFFFFFFFu, ok)) {
+            if (lane == 0) record_timeout(sm, p.status);
+            break;
+        }
+        tc_fence_after_sync();
+        const uint32_t t_row =
+            tmem + (static_cast<uint32_t>(32 * q) << 16) + static_cast<uint32_t>((local & 1) * kAccShift);
+        // kGemmOutEpilogue: columns 64j .. 64j + 63; kGemmOutGated: 32j .. 32j + 31 of the gate, then of up
+        const uint32_t c0 = OUT == kGemmOutGated ? 32u * j : 64u * j, c1 = OUT == kGemmOutGated ? 128u + 32u * j : c0 + 32u;
+        float f[2][32];
+        tmem_ld_32x32b_x32(t_row + c0, reinterpret_cast<uint32_t(&)[32]>(f[0]));
+        tmem_ld_32x32b_x32(t_row + c1, reinterpret_cast<uint32_t(&)[32]>(f[1]));
+        tmem_ld_wait();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster_cta_scope(tempty0 + 8u * buf);  // in registers
+        if (row0 >= p.M) continue;
+        if constexpr (KIND == kGemmFP8Tensor) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                f[0][i] = __fmul_rn(f[0][i], sab);
+                f[1][i] = __fmul_rn(f[1][i], sab);
+            }
+        }
+        if constexpr (OUT == kGemmOutGated) {
+            const int F = p.N / 2, col0 = wu.n0 / 2 + 32 * j;
+            if (col0 >= F) continue;
+            if (p.epi.z) {
+                store_rows32(f[0], p.epi.z, p.N, row0, col0, p.M, F, lane);
+                store_rows32(f[1], p.epi.z + F, p.N, row0, col0, p.M, F, lane);
+            }
+            act_dispatch(p.epi.act, [&](auto act) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) f[0][i] = act_f32<decltype(act)::value>(f[0][i]) * f[1][i];
+            });
+            store_rows32(f[0], p.epi.y, F, row0, col0, p.M, F, lane);
+        } else {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int col0 = wu.n0 + 64 * j + 32 * c;
+                if (col0 >= p.N) break;
+                add_bias32(f[c], p.epi, col0, p.N);
+                if (p.epi.z) store_rows32(f[c], p.epi.z, p.N, row0, col0, p.M, p.N, lane);
+                finish32(f[c], p.epi, row0 + lane, col0, p.M, p.N);
+                store_rows32(f[c], p.epi.y, p.N, row0, col0, p.M, p.N, lane);
+            }
+        }
+    }
+}
+
+// kGemmOutGatedQuant (block kind, 256-wide): a tile's 128 columns of h and this
+// CTA's 128 rows are one block of groups both ways, as in quant_epilogue; warp
+// 4 + 4j + q holds 32 columns of each of its rows.  The four warps of one q
+// exchange row maxima (named barrier 1 + q), the four of one j column maxima
+// (9 + j), so all sixteen leave together (13).
+template <int FMT, class Smem>
+PURO_DEV void gated_quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int warp, int lane, int pair,
+                                   int num_pairs, int rank) {
+    const int j = (warp - 4) >> 2, q = warp & 3;
+    const uint32_t bar_row = 1u + static_cast<uint32_t>(q), bar_col = 9u + static_cast<uint32_t>(j);
+    const uint32_t tempty0 = mapa_shared(smem_u32(&sm.tempty[0]), 0);  // the even CTA's
+    QuantEpiSmem &qe = sm.qe;
+    const uint32_t sel1 = (lane & 1) ? 0x3715u : 0x6240u;  // quad byte transpose (see quant_epilogue)
+    const uint32_t sel2 = (lane & 2) ? 0x3276u : 0x5410u;
+    const int F = p.N / 2;
+    int local = 0;
+    PairUnits units(p, pair, num_pairs);
+    for (int u = units.next(); u >= 0; u = units.next(), ++local) {
+        const WorkUnit wu = work_unit<256>(p, u);
+        const int m0 = wu.m0 + kBM * rank, row0 = m0 + 32 * q;
+        const int c0 = wu.n0 / 2, col0 = c0 + 32 * j;  // the tile's and the warp's first column of h
+        bool ok = (sm.abort_flag == 0) && mbar_wait_bounded(&sm.tfull[0], static_cast<uint32_t>(local & 1), p.wait_ns);
+        ok = named_bar_and(13u, 512, __all_sync(0xFFFFFFFFu, ok));
+        if (!ok) {
+            if (lane == 0) record_timeout(sm, p.status);
+            break;
+        }
+        tc_fence_after_sync();
+        const uint32_t t_row =
+            tmem + (static_cast<uint32_t>(32 * q) << 16) + static_cast<uint32_t>((local & 1) * 128 + 32 * j);
+        float g[32], up[32];
+        tmem_ld_32x32b_x32(t_row, reinterpret_cast<uint32_t(&)[32]>(g));
+        tmem_ld_32x32b_x32(t_row + 128, reinterpret_cast<uint32_t(&)[32]>(up));
+        tmem_ld_wait();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster_cta_scope(tempty0);  // in registers
+        if (m0 >= p.M) continue;  // (whole 128-row blocks: uniform over the CTA)
+        if (p.epi.z) {
+            store_rows32(g, p.epi.z, p.N, row0, col0, p.M, F, lane);
+            store_rows32(up, p.epi.z + F, p.N, row0, col0, p.M, F, lane);
+        }
+        act_dispatch(p.epi.act, [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) g[i] = act_f32<decltype(act)::value>(g[i]) * up[i];
+        });
+        if (p.epi.y) store_rows32(g, p.epi.y, F, row0, col0, p.M, F, lane);
+        uint32_t v[16];  // h in BF16, columns 2k / 2k + 1 in the low / high half of v[k]
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            __nv_bfloat162 b2 = __floats2bfloat162_rn(g[2 * i], g[2 * i + 1]);
+            v[i] = *reinterpret_cast<uint32_t *>(&b2);
+        }
+
+        // ---- rowwise copy: the row's group is the four warps' 128 columns
+        {
+            uint32_t m2 = 0;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) m2 = __vmaxu2(m2, v[k] & 0x7FFF7FFFu);
+            qe.rowmax[q][j][lane] = max(m2 & 0xFFFFu, m2 >> 16);
+            named_bar_sync(bar_row, 128);
+            const uint32_t gr = e8m0_exponent<FMT>(max(max(qe.rowmax[q][0][lane], qe.rowmax[q][1][lane]),
+                                                       max(qe.rowmax[q][2][lane], qe.rowmax[q][3][lane])));
+            const float rmul = mul_of(gr);
+            const uint64_t rm2 = f32x2(rmul, rmul);
+            const bool rnan = isnan(rmul);
+            uint32_t x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                x[k] = quant4<FMT>(bf16_lo(v[2 * k]), bf16_hi(v[2 * k]), bf16_lo(v[2 * k + 1]), bf16_hi(v[2 * k + 1]), rm2, rnan);
+            // the two 16-byte halves swapped within lane pairs: a store writes 32-byte row pieces
+            const bool odd = (lane & 1) != 0;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, sel_u32(odd, x[w], x[4 + w]), 1);
+                if (odd)
+                    x[w] = got;
+                else
+                    x[4 + w] = got;
+            }
+            uint8_t *to = p.q + static_cast<int64_t>(row0 + (lane & ~1)) * F + col0 + 16 * (lane & 1);
+            *reinterpret_cast<uint4 *>(to) = make_uint4(x[0], x[1], x[2], x[3]);
+            *reinterpret_cast<uint4 *>(to + F) = make_uint4(x[4], x[5], x[6], x[7]);
+            if (j == 0) store_scale_vec(p.q_scale, row0 + lane, c0 / 128, F / 128, static_cast<uint8_t>(gr));
+        }
+        if (p.qt == nullptr) continue;  // uniform
+
+        // ---- transposed copy: column maxima over the warp's 32 rows by a
+        // reduce-scatter butterfly; lane l then holds word l / 2 (columns l & ~1, l | 1)
+        {
+            uint32_t a[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) a[k] = v[k] & 0x7FFF7FFFu;
+#pragma unroll
+            for (int st = 0; st < 4; ++st) {
+                const int half = 8 >> st, bit = 16 >> st;
+                const bool upper = (lane & bit) != 0;
+#pragma unroll
+                for (int i = 0; i < half; ++i) {
+                    const uint32_t keep = sel_u32(upper, a[i + half], a[i]);
+                    const uint32_t send = sel_u32(upper, a[i], a[i + half]);
+                    a[i] = __vmaxu2(keep, __shfl_xor_sync(0xFFFFFFFFu, send, bit));
+                }
+            }
+            a[0] = __vmaxu2(a[0], __shfl_xor_sync(0xFFFFFFFFu, a[0], 1));
+            if ((lane & 1) == 0) qe.colmax[j][q][lane >> 1] = a[0];
+        }
+        named_bar_sync(bar_col, 128);
+        bool col_ok = true;
+        if (q == 0) {
+            const uint32_t m2c = __vmaxu2(__vmaxu2(qe.colmax[j][0][lane >> 1], qe.colmax[j][1][lane >> 1]),
+                                          __vmaxu2(qe.colmax[j][2][lane >> 1], qe.colmax[j][3][lane >> 1]));
+            const uint32_t gc = e8m0_exponent<FMT>((lane & 1) ? (m2c >> 16) : (m2c & 0xFFFFu));
+            const float cmul = mul_of(gc);
+            qe.colmul[j][lane] = cmul;
+            col_ok = !isnan(cmul);
+            store_scale_vec(p.qt_scale, col0 + lane, m0 / 128, p.M / 128, static_cast<uint8_t>(gc));
+        }
+        const bool any_nan = !named_bar_and(bar_col, 128, col_ok);
+        uint8_t *qt_base = p.qt + static_cast<int64_t>(col0 + (lane & 3)) * p.M + row0 + 4 * (lane >> 2);
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {  // columns 4w .. 4w+3 of the warp's 32
+            const float4 cm = *reinterpret_cast<const float4 *>(&qe.colmul[j][4 * w]);
+            const uint32_t a = v[2 * w], b = v[2 * w + 1];
+            uint32_t lo, hi;
+            if (any_nan) {
+                lo = quant2_cols<FMT>(bf16_lo(a), bf16_hi(a), cm.x, cm.y);
+                hi = quant2_cols<FMT>(bf16_lo(b), bf16_hi(b), cm.z, cm.w);
+            } else {
+                lo = cvt_f32x2<FMT>(mul_f32x2(f32x2(bf16_lo(a), bf16_hi(a)), f32x2(cm.x, cm.y)));
+                hi = cvt_f32x2<FMT>(mul_f32x2(f32x2(bf16_lo(b), bf16_hi(b)), f32x2(cm.z, cm.w)));
+            }
+            uint32_t x = lo | (hi << 16);
+            x = __byte_perm(x, __shfl_xor_sync(0xFFFFFFFFu, x, 1), sel1);
+            x = __byte_perm(x, __shfl_xor_sync(0xFFFFFFFFu, x, 2), sel2);
+            *reinterpret_cast<uint32_t *>(qt_base + static_cast<int64_t>(4 * w) * p.M) = x;
+        }
+    }
+}
+
 // OUT: kGemmOutBF16 writes D in BF16; kGemmOutF32Partial writes FP32
 // partial tiles of a split reduction to the workspace [splits * Mp, N],
 // Mp = num_m * 256 (rows split * Mp + m), so that a ragged last pair tile
@@ -540,8 +815,13 @@ PURO_DEV void quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int w
 // not read with BN = 224.  kGemmOutQuant (block kind, BN = 256, 640
 // threads) quantises the BF16-rounded tile in the epilogue (quant_epilogue)
 // and does not use tm_d.
+template <int OUT, int BN, int S = 1>
+constexpr int gemm_threads() {
+    return OUT == kGemmOutQuant ? kThreads + 384 : wide_epilogue_form<OUT, BN, S>() ? 128 + BN / 64 * 128 : kThreads;
+}
+// Whether the form quantises, and so exchanges maxima through QuantEpiSmem.
 template <int OUT>
-constexpr int gemm_threads() { return OUT == kGemmOutQuant ? kThreads + 384 : kThreads; }
+constexpr bool quantises() { return OUT == kGemmOutQuant || OUT == kGemmOutGatedQuant; }
 
 // S > 1: S pairs of a cluster share one 128-wide tile, each a part of its
 // reduction.  Each CTA then hands the columns that another pair finishes to
@@ -549,14 +829,15 @@ constexpr int gemm_threads() { return OUT == kGemmOutQuant ? kThreads + 384 : kT
 // up its own 128 / S columns in pair order.  One launch and no scratch, for
 // outputs of few tiles: see cluster_split.
 template <int KIND, int OUT, int BN, int S = 1>
-__global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT>(), 1)
+__global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT, BN, S>(), 1)
     gemm_tn_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
                    const __grid_constant__ CUtensorMap tm_d, const __grid_constant__ CUtensorMap tm_sfa,
                    const __grid_constant__ CUtensorMap tm_sfb, const __grid_constant__ CUtensorMap tm_a1,
                    const __grid_constant__ CUtensorMap tm_b1, const __grid_constant__ CUtensorMap tm_d1,
                    const __grid_constant__ CUtensorMap tm_sfa1, const __grid_constant__ CUtensorMap tm_sfb1,
                    const GemmParams p) {
-    using Smem = GemmSmem<BN, OUT == kGemmOutQuant, S>;
+    using Smem = GemmSmem<BN, quantises<OUT>(), S>;
+    constexpr int kAllThreads = gemm_threads<OUT, BN, S>();
     constexpr int kBNHalf = Smem::kBNHalf;
     constexpr int kStages = Smem::kStages, kAtoms = Smem::kAtoms;
     constexpr int kBKBytes = GemmStage<BN>::kBKBytes, kStagesPerGroup = GemmStage<BN>::kPerGroup;
@@ -564,10 +845,12 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
     constexpr bool kHelper = kMX && Smem::kSfbByHelper;
     constexpr bool OUT_F32 = (OUT == kGemmOutF32Partial || OUT == kGemmOutF32Add);
     constexpr bool OUT_Q = (OUT == kGemmOutQuant);
+    constexpr bool kWide = wide_epilogue_form<OUT, BN, S>();
+    constexpr bool kGated = OUT == kGemmOutGated || OUT == kGemmOutGatedQuant;
     // The narrow forms run few tiles a launch: their epilogue arrives at the
     // closing cluster barrier ahead of its last stores (which costs the
     // 256-wide form 0.5%).
-    constexpr bool kEarlyLeave = BN < 256 && !OUT_Q;
+    constexpr bool kEarlyLeave = BN < 256 && !OUT_Q && !kWide;
     constexpr bool kShifted = kMX && BN == 256;         // shared-half accumulators
     constexpr int kAccBufs = kShifted ? 1 : 2;          // hand-off barrier pairs (tfull / tempty)
     constexpr int kAccShift = kShifted ? 128 : 256;     // column offset between consecutive tiles' accumulators
@@ -582,7 +865,8 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
                   "the 224-wide form is block-scaled, BF16 out");
     static_assert(OUT != kGemmOutF32Partial || BN == 256, "reductions split through memory run 256-wide");
     static_assert(S == 1 || (BN == 128 && KIND != kGemmBF16 && OUT != kGemmOutF32Partial), "128-wide FP8 tiles");
-    static_assert(!OUT_Q || (kMX && BN == 256), "the quantising epilogue is block-scaled and 256-wide");
+    static_assert(!quantises<OUT>() || (kMX && BN == 256), "the quantising epilogues are block-scaled and 256-wide");
+    static_assert(!kGated || (BN == 256 && S == 1), "128 columns of the gate and 128 of up, one from each CTA");
     static_assert(!kMX || kSfBase + kSfSets * kSfColsPerSet <= kTmemCols, "TMEM budget");
     static_assert(kAccShift + BN <= (kMX ? kSfBase : kTmemCols), "accumulators clear of the scale columns");
 
@@ -597,6 +881,10 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
     const uint16_t both = static_cast<uint16_t>(0x3u << even);
     const int pair = blockIdx.x / (2 * S);              // (S > 1: the cluster)
     const int num_pairs = gridDim.x / (2 * S);
+    // first row of B of this CTA's half of a tile
+    auto b_row_of = [&](const WorkUnit &w) {
+        return kGated ? w.n0 / 2 + (p.N / 2) * static_cast<int>(rank) : w.n0 + kBNHalf * static_cast<int>(rank);
+    };
     auto unit = [&](int u) {
         WorkUnit w = work_unit<BN>(p, u);
         if constexpr (S > 1) {
@@ -613,7 +901,7 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&sm.tfull[b], 1);
-            mbar_init(&sm.tempty[b], OUT_Q ? 32 : 8);  // the epilogue warps of both CTAs
+            mbar_init(&sm.tempty[b], 2 * (kAllThreads - 128) / 32);  // the epilogue warps of both CTAs
         }
         for (int s = 0; s < kSfbSlots; ++s) {
             mbar_init(&sm.sfb_full[s], 2);  // the helper warp of each CTA
@@ -647,7 +935,7 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
     // The producer does not use tensor memory: its first copies do not wait for the allocation.
     if (warp != 0) {
         tc_fence_before_sync();
-        named_bar_sync(kAllocBarrier, gemm_threads<OUT>() - 32);
+        named_bar_sync(kAllocBarrier, kAllThreads - 32);
         tc_fence_after_sync();
     }
     cluster_wait();
@@ -662,7 +950,7 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
     // 10.0; one weight that stays in L2 12.5, 12.5, 13.1 -> 13.0, 9.4 -> 9.5.
     if (p.b && warp >= 4 && p.num_units <= num_pairs) {
         const WorkUnit wu = unit(pair);
-        const int row = wu.n0 + kBNHalf * static_cast<int>(rank) + static_cast<int>(threadIdx.x) - 128;
+        const int row = b_row_of(wu) + static_cast<int>(threadIdx.x) - 128;
         if (wu.m0 == 0 && static_cast<int>(threadIdx.x) - 128 < kBNHalf && row < p.N) {
             const uint8_t *b = p.b + static_cast<int64_t>(row) * p.K;
             const int k1 = min(p.K, wu.kb1 * kBK);
@@ -691,7 +979,7 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
         tc_fence_before_sync();
         __syncwarp();
         cluster_arrive();
-        if (warp >= 4) named_bar_arrive(kLeaveBarrier, gemm_threads<OUT>() - 96);  // lets warp 1 go on
+        if (warp >= 4) named_bar_arrive(kLeaveBarrier, kAllThreads - 96);  // lets warp 1 go on
         left = true;
     };
 
@@ -707,7 +995,7 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
         for (int u = u0; u >= 0 && !aborted; u = units.next()) {
             const WorkUnit wu = u == u0 ? w0 : unit(u);
             const int a_row = wu.m0 + kBM * static_cast<int>(rank);
-            const int b_row = wu.n0 + kBNHalf * static_cast<int>(rank);
+            const int b_row = b_row_of(wu);
             const CUtensorMap *ma = wu.problem ? &tm_a1 : &tm_a;
             const CUtensorMap *mb = wu.problem ? &tm_b1 : &tm_b;
             const CUtensorMap *msfa = wu.problem ? &tm_sfa1 : &tm_sfa;
@@ -733,10 +1021,11 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
                     const int kg = kb / kStagesPerGroup;
                     tma_load_2d_pair_e(e, sm.sf_a[stage], msfa, full_bar, 0, (a_row / 128) * kgroups + kg);
                     if constexpr (!kHelper) {
-                        tma_load_2d_pair_e(e, sm.sf_b[stage], msfb, full_bar, 0, (wu.n0 / 128) * kgroups + kg);
+                        const int rb = kGated ? wu.n0 / 256 : wu.n0 / 128;  // 128-row blocks of B: this one and
+                        const int rb1 = kGated ? rb + p.N / 256 : rb + 1;   // the next, or up's
+                        tma_load_2d_pair_e(e, sm.sf_b[stage], msfb, full_bar, 0, rb * kgroups + kg);
                         if constexpr (Smem::kSfbChunks == 2)
-                            tma_load_2d_pair_e(e, sm.sf_b[stage] + 512, msfb, full_bar, 0,
-                                             (wu.n0 / 128 + 1) * kgroups + kg);
+                            tma_load_2d_pair_e(e, sm.sf_b[stage] + 512, msfb, full_bar, 0, rb1 * kgroups + kg);
                     }
                 }
                 ++issued;
@@ -907,6 +1196,16 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
             else
                 quant_epilogue<1>(sm, p, tmem, warp, lane, pair, num_pairs, static_cast<int>(rank));
         }
+    } else if constexpr (OUT == kGemmOutGatedQuant) {
+        if (warp >= 4) {
+            if (p.q_fmt == 0)
+                gated_quant_epilogue<0>(sm, p, tmem, warp, lane, pair, num_pairs, static_cast<int>(rank));
+            else
+                gated_quant_epilogue<1>(sm, p, tmem, warp, lane, pair, num_pairs, static_cast<int>(rank));
+        }
+    } else if constexpr (kWide) {
+        if (warp >= 4)
+            wide_epilogue<KIND, OUT, BN, kShifted>(sm, p, tmem, warp, lane, pair, num_pairs, static_cast<int>(rank));
     } else if (warp >= 4) {
         // ------------------------------------------------ epilogue (both CTAs)
         const int q = warp & 3;  // TMEM lane quarter of this warp
@@ -1002,6 +1301,17 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
                                 a[4 * i + k] = t == 0 ? b : a[4 * i + k] + b;
                             }
                         }
+                    }
+                    if constexpr (OUT == kGemmOutEpilogue) {
+                        if constexpr (KIND == kGemmFP8Tensor) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) a[i] = __fmul_rn(a[i], sab);
+                        }
+                        add_bias32(a, p.epi, col, n_out);
+                        if (p.epi.z) store_rows32(a, p.epi.z, n_out, m0 + 32 * q, col, p.M, n_out, lane);
+                        finish32(a, p.epi, m0 + lr, col, p.M, n_out);
+                        store_rows32(a, p.epi.y, n_out, m0 + 32 * q, col, p.M, n_out, lane);
+                        continue;
                     }
                     if (e) bulk_wait_group_read0();
                     __syncwarp();
@@ -1142,7 +1452,7 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
     // early wait at the CTA's barriers.
     if (!left) leave();
     if (warp == 1) {
-        named_bar_sync(kLeaveBarrier, gemm_threads<OUT>() - 96);  // this CTA's epilogue warps have arrived
+        named_bar_sync(kLeaveBarrier, kAllThreads - 96);  // this CTA's epilogue warps have arrived
         cluster_wait();
         tc_fence_after_sync();
         tmem_dealloc_pair(tmem, kTmemCols);
@@ -1196,6 +1506,50 @@ __global__ void __launch_bounds__(256) splitk_reduce_add_f32_kernel(const float4
         o.w += a.w;
         out[i] = o;
     }
+}
+
+// The epilogue behind a reduction split through memory: eight columns of a row
+// a thread and step, the partial products summed in chunk order.
+__global__ void __launch_bounds__(256) epilogue_kernel(const float *__restrict__ ws, int splits, int64_t stride, int64_t M,
+                                                       int64_t N, const GemmEpilogue epi) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int64_t per_row = N / 8, chunks = M * per_row, step = static_cast<int64_t>(gridDim.x) * blockDim.x;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < chunks; i += step) {
+        const int64_t row = i / per_row, col = (i - row * per_row) * 8;
+        float f[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        for (int sp = 0; sp < splits; ++sp) {
+            const float4 *from = reinterpret_cast<const float4 *>(ws + sp * stride + 8 * i);
+            const float4 a = from[0], b = from[1];
+            const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] = sp == 0 ? v[k] : f[k] + v[k];
+        }
+        auto out = [&](uint16_t *to) {
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * k], f[2 * k + 1]);
+                w[k] = *reinterpret_cast<uint32_t *>(&b);
+            }
+            *reinterpret_cast<uint4 *>(to + 8 * i) = make_uint4(w[0], w[1], w[2], w[3]);
+        };
+        if (epi.bias) add8(f, __ldg(reinterpret_cast<const uint4 *>(epi.bias + col)));
+        if (epi.z) out(epi.z);
+        act_dispatch(epi.act, [&](auto act) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] = act_f32<decltype(act)::value>(f[k]);
+        });
+        if (epi.residual) add8(f, *reinterpret_cast<const uint4 *>(epi.residual + row * epi.ld_residual + col));
+        out(epi.y);
+    }
+}
+
+cudaError_t launch_epilogue(const float *ws, int splits, int64_t stride, int64_t M, int64_t N, const GemmEpilogue &epi,
+                            int num_sms, cudaStream_t s) {
+    const int64_t want = (M * (N / 8) + 255) / 256, cap = static_cast<int64_t>(num_sms) * 8;
+    return launch_pdl(epilogue_kernel, dim3(static_cast<unsigned>(want < cap ? want : cap)), dim3(256), 0, s, ws, splits, stride,
+                      M, N, epi);
 }
 
 int choose_splits(int64_t M, int64_t N, int64_t K, bool bf16) {
@@ -1327,7 +1681,7 @@ static int max_resident_pairs(int num_sms, size_t smem) {
     if (dev >= 0 && dev < 64 && cache[dev] > 0) return cache[dev];
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(num_sms / 2 * 2), 1, 1);
-    cfg.blockDim = dim3(gemm_threads<OUT>(), 1, 1);
+    cfg.blockDim = dim3(gemm_threads<OUT, BN>(), 1, 1);
     cfg.dynamicSmemBytes = smem;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
@@ -1383,6 +1737,7 @@ static GemmParams make_params(const GemmArgs &g, int splits) {
     p.qt_scale = g.qt_scale;
     p.d_bf16 = static_cast<uint16_t *>(g.d_bf16);
     p.q_fmt = g.q_fmt;
+    p.epi = g.epi;
     p.units0 = p.num_units;  // one problem unless a grouped launch adds a second
     p.lead = 0;
     return p;
@@ -1394,12 +1749,12 @@ template <int KIND, int OUT, int BN>
 static cudaError_t launch_params(const GemmParams &p, const GemmArgs &g, const GemmMaps &m, const GemmMaps &m1,
                                  cudaStream_t s) {
     auto kern = gemm_tn_kernel<KIND, OUT, BN>;
-    const size_t smem = sizeof(GemmSmem<BN, OUT == kGemmOutQuant>) + 1024;
+    const size_t smem = sizeof(GemmSmem<BN, quantises<OUT>()>) + 1024;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
     const int pairs_max = max_resident_pairs<KIND, OUT, BN>(g.num_sms, smem);
     const int pairs = p.num_units < pairs_max ? p.num_units : pairs_max;
-    return launch_pdl(kern, dim3(2 * pairs), dim3(gemm_threads<OUT>()), smem, s, m.a, m.b,
+    return launch_pdl(kern, dim3(2 * pairs), dim3(gemm_threads<OUT, BN>()), smem, s, m.a, m.b,
                       OUT == kGemmOutF32Partial ? m.ws : m.d, m.sfa, m.sfb, m1.a, m1.b, m1.d, m1.sfa, m1.sfb, p);
 }
 
@@ -1432,8 +1787,19 @@ static cudaError_t launch_width(const GemmArgs &g, const GemmMaps &m, cudaStream
 
 template <int KIND>
 static cudaError_t launch_split_or_not(const GemmArgs &g, const GemmMaps &m, cudaStream_t s) {
-    if constexpr (KIND == kGemmFP8Block)
+    if constexpr (KIND == kGemmFP8Block) {
+        if (g.quant_out && g.gated) return launch_kind<KIND, kGemmOutGatedQuant, 256>(g, m, 1, s);
         if (g.quant_out) return launch_kind<KIND, kGemmOutQuant, 256>(g, m, 1, s);
+    }
+    if (g.epi.on) {
+        if (g.splits <= 1) return launch_width<KIND, kGemmOutEpilogue>(g, m, s);
+        if (g.cluster == 2) return launch_cluster<KIND, kGemmOutEpilogue, 2>(g, m, s);
+        if (g.cluster == 4) return launch_cluster<KIND, kGemmOutEpilogue, 4>(g, m, s);
+        const cudaError_t e = launch_kind<KIND, kGemmOutF32Partial, 256>(g, m, g.splits, s);
+        if (e != cudaSuccess) return e;
+        return launch_epilogue(static_cast<const float *>(g.workspace), g.splits, splitk_rows_per_chunk(g.M) * g.N, g.M, g.N,
+                               g.epi, g.num_sms, s);
+    }
     if (g.splits <= 1) {
         if (g.accumulate_f32) return launch_width<KIND, kGemmOutF32Add>(g, m, s);
         if constexpr (KIND == kGemmFP8Block)
@@ -1537,7 +1903,10 @@ bool wgrad_keeps_split(int64_t M, int64_t N, int64_t K) {
 
 cudaError_t launch_gemm(const GemmArgs &g, const GemmMaps &m, cudaStream_t s) {
     switch (g.kind) {
-        case kGemmBF16: return launch_width<kGemmBF16, kGemmOutBF16>(g, m, s);
+        case kGemmBF16:
+            if (g.gated) return launch_kind<kGemmBF16, kGemmOutGated, 256>(g, m, 1, s);
+            if (g.epi.on) return launch_width<kGemmBF16, kGemmOutEpilogue>(g, m, s);
+            return launch_width<kGemmBF16, kGemmOutBF16>(g, m, s);
         case kGemmFP8Tensor: return launch_split_or_not<kGemmFP8Tensor>(g, m, s);
         default: return launch_split_or_not<kGemmFP8Block>(g, m, s);
     }

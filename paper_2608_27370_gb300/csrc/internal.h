@@ -159,6 +159,24 @@ enum GemmOut : int {
     kGemmOutF32Partial = 1,  // FP32 partial tiles of a split reduction (workspace)
     kGemmOutF32Add = 2,      // D (FP32) += the product (main-grad accumulation)
     kGemmOutQuant = 3,       // D rounded to BF16, then its blockwise FP8 copies (block kind, 256-wide, unsplit)
+    kGemmOutEpilogue = 4,    // act(D + bias) + residual in BF16 (GemmEpilogue)
+    kGemmOutGated = 5,       // act(gate) * up in BF16, gate and up the halves of D (GemmEpilogue; 256-wide, unsplit)
+    kGemmOutGatedQuant = 6,  // its blockwise FP8 copies (block kind)
+};
+
+// What the forms with an epilogue read and write beside the operands.
+//   kGemmOutEpilogue: z = D + bias (bf16 [M, N] when z is set), y = act(z) +
+//     residual (bf16 [M, N]); bias bf16 [N], residual bf16 with rows ld_residual
+//     elements apart, each or null.
+//   kGemmOutGated, kGemmOutGatedQuant: B is [gate rows, up rows] of F = N / 2
+//     each; h = act(gate) * up, bf16 [M, F] in y when set; z, when set, is
+//     [gate, up] rounded to bf16 [M, N].
+struct GemmEpilogue {
+    bool on;
+    int act;
+    const uint16_t *bias, *residual;
+    int64_t ld_residual;
+    uint16_t *z, *y;
 };
 
 struct GemmArgs {
@@ -190,6 +208,8 @@ struct GemmArgs {
     // transposed copy qt [N, M] (scales qt_scale), in format q_fmt; D itself
     // is stored in BF16 only when d_bf16 is set.
     bool quant_out;
+    bool gated;                  // kGemmOutGated, or with quant_out kGemmOutGatedQuant
+    GemmEpilogue epi;            // .on without gated: kGemmOutEpilogue
     int q_fmt;
     uint8_t *q, *q_scale, *qt, *qt_scale;
     void *d_bf16;
@@ -210,6 +230,10 @@ struct GemmMaps {
 };
 
 cudaError_t launch_gemm(const GemmArgs &g, const GemmMaps &m, cudaStream_t s);
+// The epilogue alone, of the sum of `splits` FP32 partial products [M, N] in ws,
+// stride elements apart (0 partial products: of zero).
+cudaError_t launch_epilogue(const float *ws, int splits, int64_t stride, int64_t M, int64_t N, const GemmEpilogue &epi,
+                            int num_sms, cudaStream_t s);
 // Two block-scaled GEMMs with BF16 output in one launch (the Dgrad and Wgrad
 // of one linear): the same tile width (256, 192 or 128), neither reduction split.
 cudaError_t launch_gemm_grouped(const GemmArgs &g0, const GemmMaps &m0, const GemmArgs &g1, const GemmMaps &m1,
