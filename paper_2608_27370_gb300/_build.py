@@ -1,6 +1,6 @@
 """Build the CUDA library libpuro_fp8.so in-tree with nvcc for sm_103a.
 
-Seven translation units are compiled in parallel and linked into one shared
+Eight translation units are compiled in parallel and linked into one shared
 object with the CUDA runtime linked statically, so the library loads on a
 machine without a GPU driver (only the first CUDA call needs one).  Beside it
 the Python binding's native marshalling module _native.so is compiled and
@@ -24,7 +24,7 @@ LIB = os.path.join(PKG, "libpuro_fp8.so")
 NATIVE = os.path.join(PKG, "_native.so")
 BINDING = os.path.join(CSRC, "binding.cpp")
 NATIVE_FOR = os.path.join(BUILD, "native_for.txt")  # what _native.so was compiled for
-SOURCES = ["api.cu", "quantize.cu", "gemm.cu", "noalloc.cu", "muonh.cu", "qknorm.cu", "act.cu"]
+SOURCES = ["api.cu", "quantize.cu", "gemm.cu", "noalloc.cu", "muonh.cu", "qknorm.cu", "act.cu", "skinny.cu"]
 HEADERS = ["ptx.cuh", "internal.h", "quant_math.cuh", "act_math.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",

@@ -35,6 +35,24 @@ PURO_DEV Sigmoid sigmoid_both(float u) {
     return u >= 0.0f ? Sigmoid{r, tr} : Sigmoid{tr, r};
 }
 
+// The normal distribution function Phi(z) and e^(-z^2/2), by formula 7.1.26 of
+// Abramowitz and Stegun, Handbook of Mathematical Functions (erf to 1.5e-7 by a
+// polynomial in 1 / (1 + p x) times e^(-x^2), x = |z| / sqrt(2)); with the FP32
+// roundings Phi is within 2^-21.  Behind the GEMM's epilogue CUDA's normcdff
+// made it the bound: [8192, 2048] x 6144 84.9 us.
+struct Normal {
+    float cdf, bell;
+};
+PURO_DEV Normal normal_both(float z) {
+    const float t = rcp_approx(fmaf(fabsf(z), 0.3275911f * 0.70710678f, 1.0f));
+    const float e = ex2_approx(z * z * -0.72134752f);
+    float q = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+    q = fmaf(t, q, 0.5f * 1.421413741f);
+    q = fmaf(t, q, 0.5f * -0.284496736f);
+    q = fmaf(t, q, 0.5f * 0.254829592f) * (t * e);
+    return Normal{z >= 0.0f ? 1.0f - q : q, e};
+}
+
 constexpr float kGeluC = 1.5957691216f;              // 2 sqrt(2 / pi)
 constexpr float kGeluK = 0.044715f * 1.5957691216f;  // gelu_tanh(z) = z sigmoid(z (kGeluC + kGeluK z^2))
 
@@ -42,9 +60,11 @@ constexpr float kGeluK = 0.044715f * 1.5957691216f;  // gelu_tanh(z) = z sigmoid
 template <int ACT>
 PURO_DEV float act_f32(float z) {
     if constexpr (ACT == PURO_ACT_RELU) return z < 0.0f ? 0.0f : z;  // (NaN stays)
-    if constexpr (ACT == PURO_ACT_SILU) return z * sigmoid_both(z).s;
-    if constexpr (ACT == PURO_ACT_GELU) return z * normcdff(z);
-    if constexpr (ACT == PURO_ACT_GELU_TANH) return z * sigmoid_both(z * fmaf(kGeluK, z * z, kGeluC)).s;
+    // (e^-u may overflow: the reciprocal is then zero, and the activation below 1e-36)
+    if constexpr (ACT == PURO_ACT_SILU) return z * rcp_approx(1.0f + ex2_approx(z * -1.44269504f));
+    if constexpr (ACT == PURO_ACT_GELU) return z * normal_both(z).cdf;
+    if constexpr (ACT == PURO_ACT_GELU_TANH)
+        return z * rcp_approx(1.0f + ex2_approx(z * fmaf(-1.44269504f * kGeluK, z * z, -1.44269504f * kGeluC)));
     return z;
 }
 
@@ -62,8 +82,8 @@ PURO_DEV ActSlope act_slope_f32(float z) {
         return ActSlope{z * g.s, fmaf(zb * g.s, g.c, g.s)};
     }
     if constexpr (ACT == PURO_ACT_GELU) {
-        const float p = normcdff(z);  // d = p + z e^{-z^2/2} / sqrt(2 pi)
-        return ActSlope{z * p, fmaf(zb * 0.39894228f, ex2_approx(zb * zb * -0.72134752f), p)};
+        const Normal n = normal_both(z);  // d = Phi + z e^(-z^2/2) / sqrt(2 pi)
+        return ActSlope{z * n.cdf, fmaf(zb * 0.39894228f, n.bell, n.cdf)};
     }
     if constexpr (ACT == PURO_ACT_GELU_TANH) {
         const Sigmoid g = sigmoid_both(z * fmaf(kGeluK, z * z, kGeluC));

@@ -380,10 +380,15 @@ puro_status_t bf16_gemm_epilogue(const void *x, const void *w, int64_t M, int64_
         return sms > 0 ? cuda_status(launch_epilogue(nullptr, 0, 0, M, N, epi, sms, s)) : PURO_ERR_CUDA;
     }
     if (!x || !w || !aligned16(x) || !aligned16(w)) return PURO_ERR_INVALID_ARG;
+    if (is_skinny_linear(M, N, K, false))
+        return cuda_status(launch_skinny_linear(static_cast<const uint16_t *>(x), static_cast<const uint16_t *>(w), M, N, K, false,
+                                                epi, s));
     GemmArgs g;
     GemmMaps m;
-    st = prepare_bf16_gemm(x, w, M, N, K, tile_width(kGemmBF16, false, M, N, K), dev_status, &g, &m);
+    const int cluster = cluster_or_whole(M, N, 2 * K);
+    st = prepare_bf16_gemm(x, w, M, N, K, cluster > 1 ? 128 : tile_width(kGemmBF16, false, M, N, K), dev_status, &g, &m);
     if (st != PURO_OK) return st;
+    g.cluster = cluster;
     g.epi = epi;
     return cuda_status(launch_gemm(g, m, s));
 }
@@ -403,6 +408,9 @@ puro_status_t bf16_gated(const void *x, const void *w, int64_t M, int64_t F, int
         return cuda_status(e);
     }
     if (!x || !w || !aligned16(x) || !aligned16(w)) return PURO_ERR_INVALID_ARG;
+    if (is_skinny_linear(M, F, K, true))
+        return cuda_status(launch_skinny_linear(static_cast<const uint16_t *>(x), static_cast<const uint16_t *>(w), M, F, K, true,
+                                                epi, s));
     GemmArgs g;
     GemmMaps m;
     st = prepare_bf16_gemm(x, w, M, 2 * F, K, 256, dev_status, &g, &m);

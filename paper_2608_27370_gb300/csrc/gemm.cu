@@ -94,6 +94,18 @@ struct QuantEpiSmem {
     uint32_t colmax[4][4][32];        // [quarter][warp][column pair]: packed max |bf16| over the warp's rows
     alignas(16) float colmul[4][64];  // [quarter][column]: 2^(127 - g), NaN for a non-finite column
 };
+// The same of kGemmOutGatedQuant, whose warp 4 + 4j + q holds 32 columns (j) of 32
+// rows (q): the maxima of a tile and the next one's, so that a warp may be a
+// tile ahead of those it exchanged them with, and each warp's multipliers.
+struct GatedEpiSmem {
+    uint32_t rowmax[2][4][4][32];      // [tile's parity][q][j][lane]
+    uint32_t colmax[2][4][4][16];      // [tile's parity][j][q][column pair]
+    alignas(16) float colmul[16][32];  // [warp][column]
+};
+// kGemmOutEpilogue: the 64 columns of bias of each epilogue warp's quarter, in BF16.
+struct LinearEpiSmem {
+    alignas(16) uint32_t bias[16][32];
+};
 struct NoQuantEpiSmem {};
 
 // Pipeline stages.  A 256-wide tile's k-block keeps the tensor pipe busy for
@@ -121,7 +133,7 @@ struct SplitSmem {
 };
 struct NoSplitSmem {};
 
-template <int BN, bool QOUT = false, int S = 1>
+template <int BN, class EpiSmem = NoQuantEpiSmem, int S = 1>
 struct GemmSmem {
     static constexpr int kBNHalf = BN / 2;                 // rows of B per CTA
     static constexpr bool kSfbByHelper = (BN == 224);      // B scale images built by warps 2 and 3
@@ -145,7 +157,7 @@ struct GemmSmem {
     uint32_t tmem_base;
     volatile int abort_flag;
     volatile int started;  // the producer is past its wait for the kernel before
-    std::conditional_t<QOUT, QuantEpiSmem, NoQuantEpiSmem> qe;
+    EpiSmem qe;
     std::conditional_t<(S > 1), SplitSmem<S>, NoSplitSmem> split;
 };
 
@@ -534,10 +546,9 @@ PURO_DEV void quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int w
 // warps: warp 4 + 4j + q takes column quarter j of the tile and the rows of
 // tensor-memory lane quarter q, one per lane.  Four warps a scheduler keep the
 // special-function chains of the activations overlapped.  Everything they read
-// (bias, residual) comes straight from global memory; everything they
-// write leaves from registers as whole 64-byte row segments
-// (quad_transpose_chunks), so rows and columns may end anywhere (columns at a
-// multiple of eight).
+// (bias, residual) comes straight from global memory; what they write in BF16
+// leaves by plain stores of whole 64-byte row segments (store_rows32), so rows
+// and columns may end anywhere (columns at a multiple of eight).
 template <int OUT, int BN, int S>
 constexpr bool wide_epilogue_form() {
     return S == 1 && (OUT == kGemmOutEpilogue || OUT == kGemmOutGated || OUT == kGemmOutGatedQuant);
@@ -545,22 +556,39 @@ constexpr bool wide_epilogue_form() {
 
 // 32 values of each lane's row, rounded to BF16, to out[row, col0 .. col0 + 31]
 // (rows ld elements apart), rows below `rows` and columns below `cols` only.
-PURO_DEV void store_rows32(const float (&f)[32], uint16_t *out, int64_t ld, int row0, int col0, int rows, int cols,
-                           int lane) {
+// Sixteen rows at a time go through the warp's kilobyte of staging (64-byte rows,
+// 16-byte chunk c of row r at c ^ (r / 2) % 4), so that a store writes eight
+// whole 64-byte pieces.
+constexpr int kRowStage = 1024;
+PURO_DEV void store_rows32(const float (&f)[32], uint8_t *stage, uint16_t *out, int64_t ld, int row0, int col0,
+                           int rows, int cols, int lane) {
     uint32_t x[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
         x[i] = *reinterpret_cast<uint32_t *>(&b);
     }
-    quad_transpose_chunks(x, lane);
-    const int row = row0 + (lane & ~3), col = col0 + 8 * (lane & 3);
-    if (col >= cols) return;
+    const int col = col0 + 8 * (lane & 3);
+    uint8_t *mine = stage + 64 * (lane & 15);
+    const uint8_t *theirs = stage + 64 * (lane >> 2) + 16 * ((lane & 3) ^ ((lane >> 3) & 3));  // (and 8 rows on: the same chunk)
+    uint16_t *to = out + static_cast<int64_t>(row0 + (lane >> 2)) * ld + col;
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-        if (row + r < rows)
-            *reinterpret_cast<uint4 *>(out + static_cast<int64_t>(row + r) * ld + col) =
-                make_uint4(x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]);
+    for (int half = 0; half < 2; ++half) {
+        if ((lane >> 4) == half) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                *reinterpret_cast<uint4 *>(mine + 16 * (c ^ ((lane >> 1) & 3))) =
+                    make_uint4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(theirs + 512 * k);
+            const int r = 16 * half + 8 * k;
+            if (row0 + r + (lane >> 2) < rows && col < cols) *reinterpret_cast<uint4 *>(to + r * ld) = v;
+        }
+        __syncwarp();
+    }
 }
 
 PURO_DEV void add8(float *f, const uint4 &w) {
@@ -572,27 +600,69 @@ PURO_DEV void add8(float *f, const uint4 &w) {
     }
 }
 
-// z = f + bias in place for the 32 columns from col0 (columns past the last one unused).
-PURO_DEV void add_bias32(float (&f)[32], const GemmEpilogue &epi, int col0, int cols) {
-    if (!epi.bias) return;
+// z = f + bias in place (bias: 32 BF16 columns).
+PURO_DEV void add_bias32(float (&f)[32], const uint4 *bias) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (col0 + 8 * i < cols) add8(f + 8 * i, __ldg(reinterpret_cast<const uint4 *>(epi.bias + col0 + 8 * i)));
+    for (int i = 0; i < 4; ++i) add8(f + 8 * i, bias[i]);
 }
 
-// y = act(f) + residual in place.
-PURO_DEV void finish32(float (&f)[32], const GemmEpilogue &epi, int row, int col0, int rows, int cols) {
-    if (epi.act != PURO_ACT_NONE)
-        act_dispatch(epi.act, [&](auto act) {
+PURO_DEV void act32(float (&f)[32], int act) {
+    if (act == PURO_ACT_NONE) return;
+    act_dispatch(act, [&](auto a) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) f[i] = act_f32<decltype(act)::value>(f[i]);
-        });
-    if (epi.residual && row < rows) {
-        const uint16_t *r = epi.residual + row * epi.ld_residual + col0;
+        for (int i = 0; i < 32; ++i) f[i] = act_f32<decltype(a)::value>(f[i]);
+    });
+}
+
+// f += the lane's row of the residual at the 32 columns from col0, loaded as
+// store_rows32 stores and handed on through the same staging.  (The output may be
+// the residual itself.)
+PURO_DEV void add_residual32(float (&f)[32], uint8_t *stage, const GemmEpilogue &epi, int row0, int col0, int rows,
+                             int cols, int lane) {
+    if (!epi.residual) return;
+    const int col = col0 + 8 * (lane & 3), row = row0 + (lane >> 2);
+    const uint8_t *mine = stage + 64 * (lane & 15);
+    uint8_t *theirs = stage + 64 * (lane >> 2) + 16 * ((lane & 3) ^ ((lane >> 3) & 3));
+    const uint16_t *from = epi.residual + row * epi.ld_residual + col;
+    uint4 v[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)  // (the output may be the residual itself)
-            if (col0 + 8 * i < cols) add8(f + 8 * i, *reinterpret_cast<const uint4 *>(r + 8 * i));
+    for (int k = 0; k < 4; ++k)
+        v[k] = row + 8 * k < rows && col < cols ? *reinterpret_cast<const uint4 *>(from + 8 * k * epi.ld_residual)
+                                                : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) *reinterpret_cast<uint4 *>(theirs + 512 * k) = v[2 * half + k];
+        __syncwarp();
+        if ((lane >> 4) == half) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                add8(f + 8 * c, *reinterpret_cast<const uint4 *>(mine + 16 * (c ^ ((lane >> 1) & 3))));
+        }
+        __syncwarp();
     }
+}
+
+// g = act(g) * up.  SwiGLU's products and sums go in pairs.
+PURO_DEV void gate32(float (&g)[32], const float (&up)[32], int act) {
+    act_dispatch(act, [&](auto a) {
+        constexpr int ACT = decltype(a)::value;
+        if constexpr (ACT == PURO_ACT_SILU) {
+            const uint64_t m = f32x2(-1.44269504f, -1.44269504f), one = f32x2(1.0f, 1.0f);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const uint64_t z = f32x2(g[2 * i], g[2 * i + 1]);
+                float lo, hi;
+                split_f32x2(mul_f32x2(z, m), lo, hi);
+                split_f32x2(add_f32x2(f32x2(ex2_approx(lo), ex2_approx(hi)), one), lo, hi);
+                const uint64_t s = mul_f32x2(z, f32x2(rcp_approx(lo), rcp_approx(hi)));
+                split_f32x2(mul_f32x2(s, f32x2(up[2 * i], up[2 * i + 1])), g[2 * i], g[2 * i + 1]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) g[i] = act_f32<ACT>(g[i]) * up[i];
+        }
+    });
 }
 
 // kGemmOutEpilogue and kGemmOutGated.
@@ -601,15 +671,31 @@ PURO_DEV void wide_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int wa
                             int rank) {
     constexpr int kAccBufs = SHIFTED ? 1 : 2, kAccShift = SHIFTED ? 128 : 256;
     const int j = (warp - 4) >> 2, q = warp & 3;
+    uint8_t *stage = sm.epi[0] + kRowStage * (warp - 4);
     const uint32_t tempty0 = mapa_shared(smem_u32(&sm.tempty[0]), 0);  // the even CTA's
     float sab = 1.0f;
     if constexpr (KIND == kGemmFP8Tensor) sab = __fmul_rn(*p.sia, *p.sib);
     int local = 0;
-    PairUnits units(p, pair, num_pairs);
-    for (int u = units.next(); u >= 0; u = units.next(), ++local) {
+    for (int u = pair; u < p.num_units; u += num_pairs, ++local) {  // (as PairUnits without a second problem)
         const WorkUnit wu = work_unit<BN>(p, u);
         const int row0 = wu.m0 + kBM * rank + 32 * q;
         const int buf = local % kAccBufs;
+        if constexpr (OUT == kGemmOutEpilogue) {  // while the tile is computed
+            const int nq = wu.n0 + 64 * j;
+            if (p.epi.bias) {
+                __syncwarp();
+                sm.qe.bias[warp - 4][lane] =
+                    nq + 2 * lane < p.N ? __ldg(reinterpret_cast<const uint32_t *>(p.epi.bias + nq + 2 * lane)) : 0u;
+                __syncwarp();
+            }
+            // (the first unit's and the next one's: an epilogue as long as its tile's MMAs has no time to wait)
+            if (p.epi.residual)
+                for (int v = local == 0 ? u : u + num_pairs; v <= u + num_pairs && v < p.num_units; v += num_pairs) {
+                    const WorkUnit w = work_unit<BN>(p, v);
+                    const int row = w.m0 + kBM * rank + 32 * q + lane, col = w.n0 + 64 * j;
+                    if (row < p.M && col < p.N) prefetch_l2(p.epi.residual + row * p.epi.ld_residual + col);
+                }
+        }
         bool ok = (sm.abort_flag == 0) &&
                   mbar_wait_bounded(&sm.tfull[buf], static_cast<uint32_t>(local / kAccBufs) & 1u, p.wait_ns);
         if (!__all_sync(0xFFFFFFFFu, ok)) {
@@ -640,23 +726,22 @@ PURO_DEV void wide_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int wa
             const int F = p.N / 2, col0 = wu.n0 / 2 + 32 * j;
             if (col0 >= F) continue;
             if (p.epi.z) {
-                store_rows32(f[0], p.epi.z, p.N, row0, col0, p.M, F, lane);
-                store_rows32(f[1], p.epi.z + F, p.N, row0, col0, p.M, F, lane);
+                store_rows32(f[0], stage, p.epi.z, p.N, row0, col0, p.M, F, lane);
+                store_rows32(f[1], stage, p.epi.z + F, p.N, row0, col0, p.M, F, lane);
             }
-            act_dispatch(p.epi.act, [&](auto act) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) f[0][i] = act_f32<decltype(act)::value>(f[0][i]) * f[1][i];
-            });
-            store_rows32(f[0], p.epi.y, F, row0, col0, p.M, F, lane);
+            gate32(f[0], f[1], p.epi.act);
+            store_rows32(f[0], stage, p.epi.y, F, row0, col0, p.M, F, lane);
         } else {
+            const int nq = wu.n0 + 64 * j;
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const int col0 = wu.n0 + 64 * j + 32 * c;
+                const int col0 = nq + 32 * c;
                 if (col0 >= p.N) break;
-                add_bias32(f[c], p.epi, col0, p.N);
-                if (p.epi.z) store_rows32(f[c], p.epi.z, p.N, row0, col0, p.M, p.N, lane);
-                finish32(f[c], p.epi, row0 + lane, col0, p.M, p.N);
-                store_rows32(f[c], p.epi.y, p.N, row0, col0, p.M, p.N, lane);
+                if (p.epi.bias) add_bias32(f[c], reinterpret_cast<const uint4 *>(sm.qe.bias[warp - 4]) + 4 * c);
+                if (p.epi.z) store_rows32(f[c], stage, p.epi.z, p.N, row0, col0, p.M, p.N, lane);
+                act32(f[c], p.epi.act);
+                add_residual32(f[c], stage, p.epi, row0, col0, p.M, p.N, lane);
+                store_rows32(f[c], stage, p.epi.y, p.N, row0, col0, p.M, p.N, lane);
             }
         }
     }
@@ -666,32 +751,32 @@ PURO_DEV void wide_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int wa
 // CTA's 128 rows are one block of groups both ways, as in quant_epilogue; warp
 // 4 + 4j + q holds 32 columns of each of its rows.  The four warps of one q
 // exchange row maxima (named barrier 1 + q), the four of one j column maxima
-// (9 + j), so all sixteen leave together (13).
+// (9 + j).  A warp whose wait runs out goes on through the barriers of its tiles,
+// which the others still meet it at, and stores nothing more.
 template <int FMT, class Smem>
 PURO_DEV void gated_quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int warp, int lane, int pair,
                                    int num_pairs, int rank) {
     const int j = (warp - 4) >> 2, q = warp & 3;
     const uint32_t bar_row = 1u + static_cast<uint32_t>(q), bar_col = 9u + static_cast<uint32_t>(j);
     const uint32_t tempty0 = mapa_shared(smem_u32(&sm.tempty[0]), 0);  // the even CTA's
-    QuantEpiSmem &qe = sm.qe;
+    GatedEpiSmem &qe = sm.qe;
+    uint8_t *stage = sm.epi[0] + kRowStage * (warp - 4);
+    float *colmul = qe.colmul[warp - 4];
     const uint32_t sel1 = (lane & 1) ? 0x3715u : 0x6240u;  // quad byte transpose (see quant_epilogue)
     const uint32_t sel2 = (lane & 2) ? 0x3276u : 0x5410u;
     const int F = p.N / 2;
     int local = 0;
-    PairUnits units(p, pair, num_pairs);
-    for (int u = units.next(); u >= 0; u = units.next(), ++local) {
+    for (int u = pair; u < p.num_units; u += num_pairs, ++local) {  // (as PairUnits without a second problem)
         const WorkUnit wu = work_unit<256>(p, u);
         const int m0 = wu.m0 + kBM * rank, row0 = m0 + 32 * q;
         const int c0 = wu.n0 / 2, col0 = c0 + 32 * j;  // the tile's and the warp's first column of h
         bool ok = (sm.abort_flag == 0) && mbar_wait_bounded(&sm.tfull[0], static_cast<uint32_t>(local & 1), p.wait_ns);
-        ok = named_bar_and(13u, 512, __all_sync(0xFFFFFFFFu, ok));
-        if (!ok) {
-            if (lane == 0) record_timeout(sm, p.status);
-            break;
-        }
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        if (!ok && lane == 0) record_timeout(sm, p.status);
+        const int par = local & 1;
         tc_fence_after_sync();
         const uint32_t t_row =
-            tmem + (static_cast<uint32_t>(32 * q) << 16) + static_cast<uint32_t>((local & 1) * 128 + 32 * j);
+            tmem + (static_cast<uint32_t>(32 * q) << 16) + static_cast<uint32_t>(par * 128 + 32 * j);
         float g[32], up[32];
         tmem_ld_32x32b_x32(t_row, reinterpret_cast<uint32_t(&)[32]>(g));
         tmem_ld_32x32b_x32(t_row + 128, reinterpret_cast<uint32_t(&)[32]>(up));
@@ -700,15 +785,12 @@ PURO_DEV void gated_quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem,
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster_cta_scope(tempty0);  // in registers
         if (m0 >= p.M) continue;  // (whole 128-row blocks: uniform over the CTA)
-        if (p.epi.z) {
-            store_rows32(g, p.epi.z, p.N, row0, col0, p.M, F, lane);
-            store_rows32(up, p.epi.z + F, p.N, row0, col0, p.M, F, lane);
+        if (p.epi.z && ok) {
+            store_rows32(g, stage, p.epi.z, p.N, row0, col0, p.M, F, lane);
+            store_rows32(up, stage, p.epi.z + F, p.N, row0, col0, p.M, F, lane);
         }
-        act_dispatch(p.epi.act, [&](auto act) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) g[i] = act_f32<decltype(act)::value>(g[i]) * up[i];
-        });
-        if (p.epi.y) store_rows32(g, p.epi.y, F, row0, col0, p.M, F, lane);
+        gate32(g, up, p.epi.act);
+        if (p.epi.y && ok) store_rows32(g, stage, p.epi.y, F, row0, col0, p.M, F, lane);
         uint32_t v[16];  // h in BF16, columns 2k / 2k + 1 in the low / high half of v[k]
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -721,10 +803,10 @@ PURO_DEV void gated_quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem,
             uint32_t m2 = 0;
 #pragma unroll
             for (int k = 0; k < 16; ++k) m2 = __vmaxu2(m2, v[k] & 0x7FFF7FFFu);
-            qe.rowmax[q][j][lane] = max(m2 & 0xFFFFu, m2 >> 16);
+            qe.rowmax[par][q][j][lane] = max(m2 & 0xFFFFu, m2 >> 16);
             named_bar_sync(bar_row, 128);
-            const uint32_t gr = e8m0_exponent<FMT>(max(max(qe.rowmax[q][0][lane], qe.rowmax[q][1][lane]),
-                                                       max(qe.rowmax[q][2][lane], qe.rowmax[q][3][lane])));
+            const uint32_t gr = e8m0_exponent<FMT>(max(max(qe.rowmax[par][q][0][lane], qe.rowmax[par][q][1][lane]),
+                                                       max(qe.rowmax[par][q][2][lane], qe.rowmax[par][q][3][lane])));
             const float rmul = mul_of(gr);
             const uint64_t rm2 = f32x2(rmul, rmul);
             const bool rnan = isnan(rmul);
@@ -743,9 +825,11 @@ PURO_DEV void gated_quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem,
                     x[4 + w] = got;
             }
             uint8_t *to = p.q + static_cast<int64_t>(row0 + (lane & ~1)) * F + col0 + 16 * (lane & 1);
-            *reinterpret_cast<uint4 *>(to) = make_uint4(x[0], x[1], x[2], x[3]);
-            *reinterpret_cast<uint4 *>(to + F) = make_uint4(x[4], x[5], x[6], x[7]);
-            if (j == 0) store_scale_vec(p.q_scale, row0 + lane, c0 / 128, F / 128, static_cast<uint8_t>(gr));
+            if (ok) {
+                *reinterpret_cast<uint4 *>(to) = make_uint4(x[0], x[1], x[2], x[3]);
+                *reinterpret_cast<uint4 *>(to + F) = make_uint4(x[4], x[5], x[6], x[7]);
+            }
+            if (j == 0 && ok) store_scale_vec(p.q_scale, row0 + lane, c0 / 128, F / 128, static_cast<uint8_t>(gr));
         }
         if (p.qt == nullptr) continue;  // uniform
 
@@ -767,24 +851,24 @@ PURO_DEV void gated_quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem,
                 }
             }
             a[0] = __vmaxu2(a[0], __shfl_xor_sync(0xFFFFFFFFu, a[0], 1));
-            if ((lane & 1) == 0) qe.colmax[j][q][lane >> 1] = a[0];
+            if ((lane & 1) == 0) qe.colmax[par][j][q][lane >> 1] = a[0];
         }
         named_bar_sync(bar_col, 128);
-        bool col_ok = true;
-        if (q == 0) {
-            const uint32_t m2c = __vmaxu2(__vmaxu2(qe.colmax[j][0][lane >> 1], qe.colmax[j][1][lane >> 1]),
-                                          __vmaxu2(qe.colmax[j][2][lane >> 1], qe.colmax[j][3][lane >> 1]));
+        bool any_nan;
+        {  // lane l: the multiplier of the warp's column l
+            const uint32_t(*cm)[16] = qe.colmax[par][j];
+            const uint32_t m2c = __vmaxu2(__vmaxu2(cm[0][lane >> 1], cm[1][lane >> 1]), __vmaxu2(cm[2][lane >> 1], cm[3][lane >> 1]));
             const uint32_t gc = e8m0_exponent<FMT>((lane & 1) ? (m2c >> 16) : (m2c & 0xFFFFu));
             const float cmul = mul_of(gc);
-            qe.colmul[j][lane] = cmul;
-            col_ok = !isnan(cmul);
-            store_scale_vec(p.qt_scale, col0 + lane, m0 / 128, p.M / 128, static_cast<uint8_t>(gc));
+            colmul[lane] = cmul;
+            if (q == 0 && ok) store_scale_vec(p.qt_scale, col0 + lane, m0 / 128, p.M / 128, static_cast<uint8_t>(gc));
+            any_nan = __any_sync(0xFFFFFFFFu, isnan(cmul));  // (and the warp's multipliers are written)
+            __syncwarp();
         }
-        const bool any_nan = !named_bar_and(bar_col, 128, col_ok);
         uint8_t *qt_base = p.qt + static_cast<int64_t>(col0 + (lane & 3)) * p.M + row0 + 4 * (lane >> 2);
 #pragma unroll
         for (int w = 0; w < 8; ++w) {  // columns 4w .. 4w+3 of the warp's 32
-            const float4 cm = *reinterpret_cast<const float4 *>(&qe.colmul[j][4 * w]);
+            const float4 cm = *reinterpret_cast<const float4 *>(&colmul[4 * w]);
             const uint32_t a = v[2 * w], b = v[2 * w + 1];
             uint32_t lo, hi;
             if (any_nan) {
@@ -797,7 +881,7 @@ PURO_DEV void gated_quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem,
             uint32_t x = lo | (hi << 16);
             x = __byte_perm(x, __shfl_xor_sync(0xFFFFFFFFu, x, 1), sel1);
             x = __byte_perm(x, __shfl_xor_sync(0xFFFFFFFFu, x, 2), sel2);
-            *reinterpret_cast<uint32_t *>(qt_base + static_cast<int64_t>(4 * w) * p.M) = x;
+            if (ok) *reinterpret_cast<uint32_t *>(qt_base + static_cast<int64_t>(4 * w) * p.M) = x;
         }
     }
 }
@@ -819,9 +903,12 @@ template <int OUT, int BN, int S = 1>
 constexpr int gemm_threads() {
     return OUT == kGemmOutQuant ? kThreads + 384 : wide_epilogue_form<OUT, BN, S>() ? 128 + BN / 64 * 128 : kThreads;
 }
-// Whether the form quantises, and so exchanges maxima through QuantEpiSmem.
-template <int OUT>
-constexpr bool quantises() { return OUT == kGemmOutQuant || OUT == kGemmOutGatedQuant; }
+// Shared memory of the form's epilogue, beside the staging.
+template <int OUT, int S = 1>
+using EpiSmemOf = std::conditional_t<
+    OUT == kGemmOutQuant, QuantEpiSmem,
+    std::conditional_t<OUT == kGemmOutGatedQuant, GatedEpiSmem,
+                       std::conditional_t<OUT == kGemmOutEpilogue && S == 1, LinearEpiSmem, NoQuantEpiSmem>>>;
 
 // S > 1: S pairs of a cluster share one 128-wide tile, each a part of its
 // reduction.  Each CTA then hands the columns that another pair finishes to
@@ -836,7 +923,7 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
                    const __grid_constant__ CUtensorMap tm_b1, const __grid_constant__ CUtensorMap tm_d1,
                    const __grid_constant__ CUtensorMap tm_sfa1, const __grid_constant__ CUtensorMap tm_sfb1,
                    const GemmParams p) {
-    using Smem = GemmSmem<BN, quantises<OUT>(), S>;
+    using Smem = GemmSmem<BN, EpiSmemOf<OUT, S>, S>;
     constexpr int kAllThreads = gemm_threads<OUT, BN, S>();
     constexpr int kBNHalf = Smem::kBNHalf;
     constexpr int kStages = Smem::kStages, kAtoms = Smem::kAtoms;
@@ -864,8 +951,8 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
     static_assert(BN == 256 || BN == 192 || BN == 128 || (BN == 224 && kMX && OUT == kGemmOutBF16),
                   "the 224-wide form is block-scaled, BF16 out");
     static_assert(OUT != kGemmOutF32Partial || BN == 256, "reductions split through memory run 256-wide");
-    static_assert(S == 1 || (BN == 128 && KIND != kGemmBF16 && OUT != kGemmOutF32Partial), "128-wide FP8 tiles");
-    static_assert(!quantises<OUT>() || (kMX && BN == 256), "the quantising epilogues are block-scaled and 256-wide");
+    static_assert(S == 1 || (BN == 128 && OUT != kGemmOutF32Partial), "128-wide tiles");
+    static_assert(!(OUT_Q || OUT == kGemmOutGatedQuant) || (kMX && BN == 256), "the quantising epilogues are block-scaled and 256-wide");
     static_assert(!kGated || (BN == 256 && S == 1), "128 columns of the gate and 128 of up, one from each CTA");
     static_assert(!kMX || kSfBase + kSfSets * kSfColsPerSet <= kTmemCols, "TMEM budget");
     static_assert(kAccShift + BN <= (kMX ? kSfBase : kTmemCols), "accumulators clear of the scale columns");
@@ -1307,10 +1394,18 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
 #pragma unroll
                             for (int i = 0; i < 32; ++i) a[i] = __fmul_rn(a[i], sab);
                         }
-                        add_bias32(a, p.epi, col, n_out);
-                        if (p.epi.z) store_rows32(a, p.epi.z, n_out, m0 + 32 * q, col, p.M, n_out, lane);
-                        finish32(a, p.epi, m0 + lr, col, p.M, n_out);
-                        store_rows32(a, p.epi.y, n_out, m0 + 32 * q, col, p.M, n_out, lane);
+                        if (p.epi.bias) {
+                            uint4 b[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                b[i] = col + 8 * i < n_out ? __ldg(reinterpret_cast<const uint4 *>(p.epi.bias + col) + i)
+                                                           : make_uint4(0u, 0u, 0u, 0u);
+                            add_bias32(a, b);
+                        }
+                        if (p.epi.z) store_rows32(a, stage_buf, p.epi.z, n_out, m0 + 32 * q, col, p.M, n_out, lane);
+                        act32(a, p.epi.act);
+                        add_residual32(a, stage_buf, p.epi, m0 + 32 * q, col, p.M, n_out, lane);
+                        store_rows32(a, stage_buf, p.epi.y, n_out, m0 + 32 * q, col, p.M, n_out, lane);
                         continue;
                     }
                     if (e) bulk_wait_group_read0();
@@ -1662,6 +1757,24 @@ int cluster_split(int64_t M, int64_t N, int64_t K, int splits) {
     return 1;
 }
 
+// Pairs per cluster that share each 128-wide tile of a BF16 linear with an
+// epilogue (K reduction bytes), or 1: there is no workspace to split through, so
+// the choice is between clusters and whole tiles, by the modelled cycles of
+// cluster_split and choose_tile_n.  Eight calls with rotating weights in a graph,
+// us a call, whole tiles and in clusters: [256, 1536] x 1536 8.3 and 6.7, [256, 2048]
+// x 1536 8.4 and 7.5, [256, 1536] x 8960 28.4 and 14.7.
+int cluster_or_whole(int64_t M, int64_t N, int64_t K) {
+    const int64_t stages = (K + 255) / 256, tiles = pair_tiles(M, N, 128);
+    int64_t whole = INT64_MAX;
+    for (const TileCost &c : kTileCosts)
+        whole = std::min(whole, (pair_tiles(M, N, c.width) + kSplitRefPairs - 1) / kSplitRefPairs * tile_cycles(c, K));
+    for (const int s : {4, 2}) {
+        if (tiles > (s == 4 ? 15 : 36) || stages < 2 * s) continue;
+        return (stages + s - 1) / s * 8 * kTileCosts[2].per_mma + kTileCosts[2].per_tile + 2000 < whole ? s : 1;
+    }
+    return 1;
+}
+
 int64_t splitk_rows_per_chunk(int64_t M) { return (M + kPairM - 1) / kPairM * kPairM; }
 
 size_t splitk_workspace_bytes(int64_t M, int64_t N, int64_t K, bool bf16) {
@@ -1749,7 +1862,7 @@ template <int KIND, int OUT, int BN>
 static cudaError_t launch_params(const GemmParams &p, const GemmArgs &g, const GemmMaps &m, const GemmMaps &m1,
                                  cudaStream_t s) {
     auto kern = gemm_tn_kernel<KIND, OUT, BN>;
-    const size_t smem = sizeof(GemmSmem<BN, quantises<OUT>()>) + 1024;
+    const size_t smem = sizeof(GemmSmem<BN, EpiSmemOf<OUT>>) + 1024;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
     const int pairs_max = max_resident_pairs<KIND, OUT, BN>(g.num_sms, smem);
@@ -1762,7 +1875,7 @@ static cudaError_t launch_params(const GemmParams &p, const GemmArgs &g, const G
 template <int KIND, int OUT, int S>
 static cudaError_t launch_cluster(const GemmArgs &g, const GemmMaps &m, cudaStream_t s) {
     auto kern = gemm_tn_kernel<KIND, OUT, 128, S>;
-    const size_t smem = sizeof(GemmSmem<128, false, S>) + 1024;
+    const size_t smem = sizeof(GemmSmem<128, NoQuantEpiSmem, S>) + 1024;
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
     const GemmParams p = make_params<KIND, OUT, 128>(g, 1);
@@ -1905,6 +2018,8 @@ cudaError_t launch_gemm(const GemmArgs &g, const GemmMaps &m, cudaStream_t s) {
     switch (g.kind) {
         case kGemmBF16:
             if (g.gated) return launch_kind<kGemmBF16, kGemmOutGated, 256>(g, m, 1, s);
+            if (g.epi.on && g.cluster == 2) return launch_cluster<kGemmBF16, kGemmOutEpilogue, 2>(g, m, s);
+            if (g.epi.on && g.cluster == 4) return launch_cluster<kGemmBF16, kGemmOutEpilogue, 4>(g, m, s);
             if (g.epi.on) return launch_width<kGemmBF16, kGemmOutEpilogue>(g, m, s);
             return launch_width<kGemmBF16, kGemmOutBF16>(g, m, s);
         case kGemmFP8Tensor: return launch_split_or_not<kGemmFP8Tensor>(g, m, s);

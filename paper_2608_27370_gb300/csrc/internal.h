@@ -230,6 +230,11 @@ struct GemmMaps {
 };
 
 cudaError_t launch_gemm(const GemmArgs &g, const GemmMaps &m, cudaStream_t s);
+// BF16 linears of a few tokens with the epilogue, or gated (N = F, the columns of
+// h), and whether a shape is one of them; see skinny.cu.
+bool is_skinny_linear(int64_t M, int64_t N, int64_t K, bool gated);  // host-only, shape-only
+cudaError_t launch_skinny_linear(const uint16_t *x, const uint16_t *w, int64_t M, int64_t N, int64_t K, bool gated,
+                                 const GemmEpilogue &epi, cudaStream_t s);
 // The epilogue alone, of the sum of `splits` FP32 partial products [M, N] in ws,
 // stride elements apart (0 partial products: of zero).
 cudaError_t launch_epilogue(const float *ws, int splits, int64_t stride, int64_t M, int64_t N, const GemmEpilogue &epi,
@@ -252,6 +257,7 @@ puro_status_t fp8_gemm_validate(const puro_fp8_tensor_t *a, const puro_fp8_tenso
 int choose_splits(int64_t M, int64_t N, int64_t K, bool bf16);
 size_t splitk_workspace_bytes(int64_t M, int64_t N, int64_t K, bool bf16);
 int cluster_split(int64_t M, int64_t N, int64_t K, int splits);  // see GemmArgs::cluster
+int cluster_or_whole(int64_t M, int64_t N, int64_t K);  // of a BF16 linear with an epilogue, K in bytes
 int64_t splitk_rows_per_chunk(int64_t M);  // M rounded up to a whole 256-row pair tile
 // Whether a linear's Dgrad (dX [M, K], reduction N) and Wgrad (dW [N, K],
 // reduction M) are modelled faster as one grouped launch (balanced

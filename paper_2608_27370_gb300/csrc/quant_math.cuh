@@ -56,6 +56,13 @@ PURO_DEV uint64_t mul_f32x2(uint64_t a, uint64_t b) {
     return r;
 }
 
+PURO_DEV uint64_t add_f32x2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+PURO_DEV void split_f32x2(uint64_t v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+
 template <int FMT>
 PURO_DEV uint32_t cvt_f32x2(uint64_t v) {
     float lo, hi;
