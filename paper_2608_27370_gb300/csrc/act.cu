@@ -14,31 +14,12 @@
 #include "act_math.cuh"
 #include "internal.h"
 #include "ptx.cuh"
-#include "quant_math.cuh"
 
 namespace puro {
 
 constexpr int kActCols = 256;                // columns of a block: 32 threads of eight
 constexpr int kActRows = 8;                  // rows of threads
 constexpr int64_t kActBlocks = 152 * 4;      // blocks to aim for
-
-PURO_DEV void widen8(const uint4 &w, float (&v)[8]) {
-    const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = bf16_lo(ws[i]);
-        v[2 * i + 1] = bf16_hi(ws[i]);
-    }
-}
-PURO_DEV uint4 narrow8(const float (&v)[8]) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        w[i] = *reinterpret_cast<uint32_t *>(&b);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
 
 ActBackwardPlan plan_act_backward(int64_t rows, int64_t cols) {
     const int64_t strips = (cols + kActCols - 1) / kActCols;
@@ -62,18 +43,15 @@ __global__ void __launch_bounds__(256) act_backward_kernel(const uint16_t *dy, c
 #pragma unroll 4
         for (int64_t r = blockIdx.y * slab_rows + ty; r < r1; r += kActRows) {
             const int64_t at = r * cols + c;
-            const uint4 dw = *reinterpret_cast<const uint4 *>(dy + at);  // (dz may be dy)
-            float d[8];
-            widen8(dw, d);
-            if constexpr (ACT != PURO_ACT_NONE) {
-                float zf[8];
-                widen8(__ldg(reinterpret_cast<const uint4 *>(z + at)), zf);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) d[i] *= act_slope_f32<ACT>(zf[i]).d;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] += d[i];
-            if (dz) *reinterpret_cast<uint4 *>(dz + at) = ACT == PURO_ACT_NONE ? dw : narrow8(d);
+            const uint4 d = *reinterpret_cast<const uint4 *>(dy + at);  // (dz may be dy)
+            uint4 zw = d;
+            if constexpr (ACT != PURO_ACT_NONE) zw = __ldg(reinterpret_cast<const uint4 *>(z + at));
+            uint4 o;
+            o.x = act_backward2<ACT>(d.x, zw.x, sum[0], sum[1]);
+            o.y = act_backward2<ACT>(d.y, zw.y, sum[2], sum[3]);
+            o.z = act_backward2<ACT>(d.z, zw.z, sum[4], sum[5]);
+            o.w = act_backward2<ACT>(d.w, zw.w, sum[6], sum[7]);
+            if (dz) *reinterpret_cast<uint4 *>(dz + at) = ACT == PURO_ACT_NONE ? d : o;
         }
     }
     if (!partial) return;
@@ -135,19 +113,16 @@ __global__ void __launch_bounds__(256) gated_backward_kernel(const uint16_t *__r
     const int64_t per_row = cols / 8, chunks = rows * per_row, stride = static_cast<int64_t>(gridDim.x) * blockDim.x;
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < chunks; i += stride) {
         const int64_t r = i / per_row, c = (i - r * per_row) * 8;
-        float d[8], g[8], u[8], dg[8];
-        widen8(__ldg(reinterpret_cast<const uint4 *>(dh) + i), d);
-        widen8(__ldg(reinterpret_cast<const uint4 *>(gate + r * ld + c)), g);
-        widen8(__ldg(reinterpret_cast<const uint4 *>(up + r * ld + c)), u);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const ActSlope s = act_slope_f32<ACT>(g[k]);
-            dg[k] = d[k] * (u[k] * s.d);
-            d[k] *= s.a;
-        }
+        const uint4 d = __ldg(reinterpret_cast<const uint4 *>(dh) + i);
+        const uint4 g = __ldg(reinterpret_cast<const uint4 *>(gate + r * ld + c)), u = __ldg(reinterpret_cast<const uint4 *>(up + r * ld + c));
+        uint4 dg, du;
+        gated_backward2<ACT>(d.x, g.x, u.x, dg.x, du.x);
+        gated_backward2<ACT>(d.y, g.y, u.y, dg.y, du.y);
+        gated_backward2<ACT>(d.z, g.z, u.z, dg.z, du.z);
+        gated_backward2<ACT>(d.w, g.w, u.w, dg.w, du.w);
         uint16_t *out = dgate_up + r * 2 * cols + c;
-        *reinterpret_cast<uint4 *>(out) = narrow8(dg);
-        *reinterpret_cast<uint4 *>(out + cols) = narrow8(d);
+        *reinterpret_cast<uint4 *>(out) = dg;
+        *reinterpret_cast<uint4 *>(out + cols) = du;
     }
 }
 

@@ -764,30 +764,21 @@ PURO_API puro_status_t puro_rmsnorm_bf16(const void *h, int64_t rows, int64_t co
 namespace puro {
 namespace {
 
-// Quantiser arguments and maps of a producer that reads x (rows x_ld elements
-// apart, x_cols columns) and quantises [rows, cols], with an optional BF16 output y.
-bool producer_maps(const void *x, int64_t x_cols, int64_t x_ld, int64_t rows, int64_t cols, int32_t fmt, void *y,
-                   uint8_t *q, void *scale, uint8_t *q_t, void *scale_t, int32_t *dev_status, QuantArgs *a,
-                   CUtensorMap (&m)[4]) {
-    *a = QuantArgs{};
-    a->fmt = fmt;
-    a->rows = rows;
-    a->cols = cols;
-    a->has_t = q_t != nullptr;
-    a->kind = kQuantBlockAct;
-    a->scale_u8 = static_cast<uint8_t *>(scale);
-    a->scale_t_u8 = static_cast<uint8_t *>(scale_t);
-    a->status = dev_status;
-    a->wait_ns = g_wait_timeout_ns.load();
-    a->x = static_cast<const uint16_t *>(x);
-    if (!make_map(&m[0], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, x_cols, rows, x_ld * 2, 128, 128, CU_TENSOR_MAP_SWIZZLE_NONE) ||
-        !make_map(&m[1], CU_TENSOR_MAP_DATA_TYPE_UINT8, q, cols, rows, cols, 128, 128, CU_TENSOR_MAP_SWIZZLE_NONE))
+// The maps of a quantised backward: y [rows, cols] contiguous, z and up [rows,
+// cols] with rows ld elements apart (null: none), the output [rows, out_cols].
+bool backward_maps(const void *y, const void *z, const void *up, int64_t rows, int64_t cols, int64_t ld, int64_t out_cols,
+                   uint8_t *q, uint8_t *q_t, BackwardQuantMaps *m) {
+    auto tiles = [&](CUtensorMap *t, const void *x, int64_t row) {
+        return make_map(t, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, cols, rows, row * 2, 128, 128, CU_TENSOR_MAP_SWIZZLE_NONE);
+    };
+    if (!tiles(&m->y, y, cols) || (z && !tiles(&m->z, z, ld)) || (up && !tiles(&m->up, up, ld)) ||
+        !make_map(&m->q, CU_TENSOR_MAP_DATA_TYPE_UINT8, q, out_cols, rows, out_cols, 128, 128, CU_TENSOR_MAP_SWIZZLE_NONE) ||
+        (q_t && !make_map(&m->qt, CU_TENSOR_MAP_DATA_TYPE_UINT8, q_t, rows, out_cols, rows, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B)))
         return false;
-    m[2] = m[1];
-    if (q_t && !make_map(&m[2], CU_TENSOR_MAP_DATA_TYPE_UINT8, q_t, rows, cols, rows, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B))
-        return false;
-    m[3] = m[0];
-    return !y || make_map(&m[3], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, y, cols, rows, cols * 2, 128, 128, CU_TENSOR_MAP_SWIZZLE_NONE);
+    if (!z) m->z = m->y;  // (descriptors the kernel prefetches)
+    if (!up) m->up = m->y;
+    if (!q_t) m->qt = m->q;
+    return true;
 }
 
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -827,18 +818,22 @@ PURO_API puro_status_t puro_fp8_quantize_act_backward(const void *dy, const void
     if (rows == 0 || cols == 0)
         return cuda_status(dbias && cols > 0 ? cudaMemsetAsync(dbias, 0, static_cast<size_t>(cols) * 4, s) : cudaSuccess);
     if (!q || !scale || !aligned16(q) || !aligned16(scale) || !aligned16(q_t) || !aligned16(scale_t)) return PURO_ERR_INVALID_ARG;
-    QuantArgs a;
-    CUtensorMap m[4];
-    if (!producer_maps(dy, cols, cols, rows, cols, fmt, dz, q, scale, q_t, scale_t, dev_status, &a, m)) return PURO_ERR_CUDA;
-    ProdArgs prod{};
-    prod.write_y = dz != nullptr;
-    prod.up = act == PURO_ACT_NONE ? nullptr : static_cast<const uint16_t *>(z);
-    prod.ld = cols;
-    prod.act = act;
-    prod.col_sum = dbias ? static_cast<float *>(workspace) : nullptr;
-    const cudaError_t e = launch_quantize_act_backward(a, m[0], m[1], m[2], m[3], prod, s);
+    BackwardQuantMaps m;
+    if (!backward_maps(dy, act == PURO_ACT_NONE ? nullptr : z, nullptr, rows, cols, cols, cols, q, q_t, &m)) return PURO_ERR_CUDA;
+    BackwardQuantArgs a{};
+    a.rows = rows;
+    a.cols = cols;
+    a.fmt = fmt;
+    a.act = act;
+    a.scale = static_cast<uint8_t *>(scale);
+    a.scale_t = static_cast<uint8_t *>(scale_t);
+    a.out = static_cast<uint16_t *>(dz);
+    a.col_sum = dbias ? static_cast<float *>(workspace) : nullptr;
+    a.status = dev_status;
+    a.wait_ns = g_wait_timeout_ns.load();
+    const cudaError_t e = launch_quantize_backward(a, m, false, s);
     if (e != cudaSuccess || !dbias) return cuda_status(e);
-    return cuda_status(launch_column_sums(prod.col_sum, rows / 128, cols, dbias, s));
+    return cuda_status(launch_column_sums(a.col_sum, rows / 128, cols, dbias, s));
 }
 
 PURO_API puro_status_t puro_act_backward_bf16(const void *dy, const void *z, int64_t rows, int64_t cols, int32_t act,
@@ -871,17 +866,19 @@ PURO_API puro_status_t puro_fp8_quantize_gated_backward(const void *dh, const vo
     if (!aligned16(dh) || !aligned16(gate) || !aligned16(up) || !aligned16(dgate_up) || !aligned16(q) || !aligned16(scale) ||
         !aligned16(q_t) || !aligned16(scale_t))
         return PURO_ERR_INVALID_ARG;
-    QuantArgs a;
-    CUtensorMap m[4];
-    if (!producer_maps(dh, cols, cols, rows, 2 * cols, fmt, dgate_up, q, scale, q_t, scale_t, dev_status, &a, m))
-        return PURO_ERR_CUDA;
-    ProdArgs prod{};
-    prod.write_y = dgate_up != nullptr;
-    prod.gate = static_cast<const uint16_t *>(gate);
-    prod.up = static_cast<const uint16_t *>(up);
-    prod.ld = ld;
-    prod.act = act;
-    return cuda_status(launch_quantize_gated_backward(a, m[0], m[1], m[2], m[3], prod, static_cast<cudaStream_t>(stream)));
+    BackwardQuantMaps m;
+    if (!backward_maps(dh, gate, up, rows, cols, ld, 2 * cols, q, q_t, &m)) return PURO_ERR_CUDA;
+    BackwardQuantArgs a{};
+    a.rows = rows;
+    a.cols = cols;
+    a.fmt = fmt;
+    a.act = act;
+    a.scale = static_cast<uint8_t *>(scale);
+    a.scale_t = static_cast<uint8_t *>(scale_t);
+    a.out = static_cast<uint16_t *>(dgate_up);
+    a.status = dev_status;
+    a.wait_ns = g_wait_timeout_ns.load();
+    return cuda_status(launch_quantize_backward(a, m, true, static_cast<cudaStream_t>(stream)));
 }
 
 PURO_API puro_status_t puro_gated_backward_bf16(const void *dh, const void *gate, const void *up, int64_t rows,

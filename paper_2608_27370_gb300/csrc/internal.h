@@ -76,19 +76,13 @@ enum QuantProd : int {
     kProdNone = 0,
     kProdRmsNorm = 1,  // y = bf16((h * rstd[row]) * gamma[col])
     kProdSwiGlu = 2,   // y = bf16(silu(gate) * up)
-    kProdActBackward = 3,    // y = bf16(dy * act'(z))
-    kProdGatedBackward = 4,  // y = bf16([dh * up * act'(gate), dh * act(gate)])
 };
 struct ProdArgs {
     const float *rstd;      // kProdRmsNorm: [rows]
     const uint16_t *gamma;  // kProdRmsNorm: bf16 [cols], or null (no gain)
     bool write_y;           // also store y (through tm_y)
-    const uint16_t *up;     // kProdSwiGlu, kProdGatedBackward: bf16 [rows, cols], rows ld elements apart;
-                            // kProdActBackward: z, or null (no activation)
-    int64_t ld;             // row stride of up (and of the gate)
-    int act;                // kProdActBackward, kProdGatedBackward: puro_act_t
-    const uint16_t *gate;   // kProdGatedBackward
-    float *col_sum;         // kProdActBackward: sums of dz over each 128 rows, [rows / 128, cols], or null
+    const uint16_t *up;     // kProdSwiGlu: bf16 [rows, cols], rows ld elements apart
+    int64_t ld;             // kProdSwiGlu: row stride of up (and of the gate tm_x maps)
 };
 
 // rstd[r] = 1 / sqrt(mean(h[r,:]^2) + eps) (cols a multiple of 8).
@@ -116,15 +110,23 @@ cudaError_t launch_quantize_rmsnorm(const QuantArgs &a, const CUtensorMap &tm_x,
 cudaError_t launch_quantize_swiglu(const QuantArgs &a, const CUtensorMap &tm_x, const CUtensorMap &tm_q,
                                    const CUtensorMap &tm_qt, const CUtensorMap &tm_y, const ProdArgs &prod,
                                    cudaStream_t s);
-// The activation quantiser fed by dz = dy * act'(z): tm_x maps dy, prod.up is z.
-cudaError_t launch_quantize_act_backward(const QuantArgs &a, const CUtensorMap &tm_x, const CUtensorMap &tm_q,
-                                         const CUtensorMap &tm_qt, const CUtensorMap &tm_y, const ProdArgs &prod,
-                                         cudaStream_t s);
-// The activation quantiser fed by [dgate, dup] = [dh * up * act'(gate), dh * act(gate)]
-// (a.cols = 2 * cols of dh): tm_x maps dh.
-cudaError_t launch_quantize_gated_backward(const QuantArgs &a, const CUtensorMap &tm_x, const CUtensorMap &tm_q,
-                                           const CUtensorMap &tm_qt, const CUtensorMap &tm_y, const ProdArgs &prod,
-                                           cudaStream_t s);
+// Backward of an activation (dz = dy * act'(z)) or of a gate ([dgate, dup] = [dh
+// * up * act'(gate), dh * act(gate)]), quantised in blocks as activations are.
+struct BackwardQuantArgs {
+    int64_t rows, cols;        // of dy or dh: whole 128x128 tiles; the output of a gate has 2 * cols columns
+    int fmt, act;              // FP8 format; puro_act_t (z is not read for PURO_ACT_NONE)
+    uint8_t *scale, *scale_t;  // scale vectors of the rowwise and (or null: no such copy) the transposed copy
+    uint16_t *out;             // the BF16 output, or null
+    float *col_sum;            // no gate: sums of dz over each 128 rows, [rows / 128, cols], or null
+    int32_t *status;
+    uint64_t wait_ns;
+};
+// y: dy or dh; z: z or gate; up (gate only): bf16, box {128, 128}, no swizzle.
+// q: u8 output, box {128, 128}; qt: the transposed copy, with the 128-byte swizzle.
+struct BackwardQuantMaps {
+    CUtensorMap y, z, up, q, qt;
+};
+cudaError_t launch_quantize_backward(const BackwardQuantArgs &a, const BackwardQuantMaps &m, bool gated, cudaStream_t s);
 // The same without the quantiser (cols a multiple of 8); see act.cu.
 struct ActBackwardPlan {
     int slabs;          // row slabs of the sums of dz

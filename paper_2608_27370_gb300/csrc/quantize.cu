@@ -17,7 +17,6 @@
 // kernels are otherwise instruction bound.
 #include <cfloat>
 #include <cuda_bf16.h>
-#include <type_traits>
 
 #include "act_math.cuh"
 #include "internal.h"
@@ -584,13 +583,6 @@ struct QuantActSmem {
     alignas(16) uint16_t gamma[2][kQT];          // kProdRmsNorm: of the tile's columns
     uint64_t full[2];
 };
-// kProdActBackward: the rows' sums of the tile's columns, [row block][column].
-struct QuantActSumSmem : QuantActSmem {
-    alignas(16) float col_sum[16][kQT];
-};
-template <int PROD>
-using QuantActSmemOf = std::conditional_t<PROD == kProdActBackward, QuantActSumSmem, QuantActSmem>;
-
 // y = bf16((h * rstd) * gamma) for a 4-value chunk, two products an instruction
 // (rs: rstd twice; gm: the gains in pairs).
 PURO_DEV uint2 rmsnorm_chunk4(uint2 w, uint64_t rs, const uint64_t (&gm)[2], bool has_gamma) {
@@ -621,43 +613,6 @@ PURO_DEV uint2 swiglu_chunk4(uint2 g, uint2 u) {
     return make_uint2(out[0], out[1]);
 }
 
-PURO_DEV uint2 pack4(const float (&f)[4]) {
-    __nv_bfloat162 lo = __floats2bfloat162_rn(f[0], f[1]), hi = __floats2bfloat162_rn(f[2], f[3]);
-    return make_uint2(*reinterpret_cast<uint32_t *>(&lo), *reinterpret_cast<uint32_t *>(&hi));
-}
-PURO_DEV void unpack4(uint2 w, float (&f)[4]) {
-    f[0] = bf16_lo(w.x), f[1] = bf16_hi(w.x), f[2] = bf16_lo(w.y), f[3] = bf16_hi(w.y);
-}
-
-// dz = dy * act'(z) of a 4-value chunk, rounded to BF16; sum += dz unrounded.
-template <int ACT>
-PURO_DEV uint2 act_backward_chunk4(uint2 dy, uint2 z, float (&sum)[4]) {
-    float d[4], zf[4];
-    unpack4(dy, d);
-    unpack4(z, zf);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        d[j] *= act_slope_f32<ACT>(zf[j]).d;
-        sum[j] += d[j];
-    }
-    return ACT == PURO_ACT_NONE ? dy : pack4(d);
-}
-
-// dgate = dh * up * act'(gate) (half 0) or dup = dh * act(gate) (half 1).
-template <int ACT>
-PURO_DEV uint2 gated_backward_chunk4(uint2 dh, uint2 gate, uint2 up, int half) {
-    float d[4], g[4], u[4];
-    unpack4(dh, d);
-    unpack4(gate, g);
-    unpack4(up, u);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const ActSlope s = act_slope_f32<ACT>(g[j]);
-        d[j] *= half ? s.a : u[j] * s.d;
-    }
-    return pack4(d);
-}
-
 // Behind a producer the kernel is bound by its instructions between the tile's
 // three barriers, not by HBM, so the produced block stays in registers (it is
 // written back to shared memory only for a y output), RMSNorm's products are
@@ -675,8 +630,8 @@ __global__ void __launch_bounds__(kQAThreads, 2)
                      int64_t rows, int64_t cols, uint8_t *__restrict__ scale_u8, uint8_t *__restrict__ scale_t_u8,
                      ProdArgs prod, int tiles_n, int ntiles, int32_t *status, uint64_t wait_ns) {
     extern __shared__ uint8_t smem_raw[];
-    using Smem = QuantActSmemOf<PROD>;
-    Smem &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    QuantActSmem &sm = *reinterpret_cast<QuantActSmem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                                         ~static_cast<uintptr_t>(1023));
     const int tid = threadIdx.x, lane = tid & 31;
     const int br = tid >> 5;  // block row: tile rows 8br .. 8br+7 (the warp)
     const int bc = lane;      // block column: tile columns 4bc .. 4bc+3
@@ -695,7 +650,7 @@ __global__ void __launch_bounds__(kQAThreads, 2)
     const uint32_t tile_bytes = kQT * kQT * 2 + (rstd16 ? kQT * 4 : 0) + (prod.gamma ? kQT * 2 : 0);
     auto issue_tile = [&](const TileWalk &t, int b) {
         mbar_arrive_expect_tx(&sm.full[b], PROD == kProdRmsNorm ? tile_bytes : kQT * kQT * 2);
-        tma_load_2d(sm.in[b], &tm_x, &sm.full[b], (PROD == kProdGatedBackward ? t.c >> 1 : t.c) * kQT, t.r * kQT);
+        tma_load_2d(sm.in[b], &tm_x, &sm.full[b], t.c * kQT, t.r * kQT);
     };
     auto issue_vectors = [&](const TileWalk &t, int b) {
         if constexpr (PROD == kProdRmsNorm) {
@@ -720,7 +675,7 @@ __global__ void __launch_bounds__(kQAThreads, 2)
         if (PROD != kProdRmsNorm) issue_tile(cur, 0);
         issue_vectors(cur, 0);
     }
-    uint2 un[8] = {};  // this thread's block of u (kProdSwiGlu) or z (kProdActBackward) for the current tile
+    uint2 un[8];  // kProdSwiGlu: this thread's block of u for the current tile
     auto load_up = [&](const TileWalk &t) {
         const int64_t row0 = static_cast<int64_t>(t.r) * kQT + 8 * br;
         const int64_t col0 = static_cast<int64_t>(t.c) * kQT + 4 * bc;
@@ -728,13 +683,13 @@ __global__ void __launch_bounds__(kQAThreads, 2)
 #pragma unroll
         for (int i = 0; i < 8; ++i) un[i] = __ldg(reinterpret_cast<const uint2 *>(p + i * prod.ld));
     };
-    constexpr bool kLoadsUp = PROD == kProdSwiGlu || PROD == kProdActBackward;
-    if (kLoadsUp && prod.up && tile < ntiles) load_up(cur);
+    if constexpr (PROD == kProdSwiGlu) {
+        if (tile < ntiles) load_up(cur);
+    }
     for (int it = 0; tile < ntiles; ++it, tile += step, cur = nxt, nxt.advance()) {
         const int buf = it & 1;
         const int64_t r0 = static_cast<int64_t>(cur.r) * kQT;
-        // (kProdGatedBackward: the tiles of dgate and dup over the same gates follow one another)
-        const int64_t c0 = static_cast<int64_t>(PROD == kProdGatedBackward ? (cur.c & 1) * (tiles_n >> 1) + (cur.c >> 1) : cur.c) * kQT;
+        const int64_t c0 = static_cast<int64_t>(cur.c) * kQT;
         if (tid == 0) {
             const int next = tile + step;
             // with a y output, the buffer's last reader was the y store of
@@ -785,35 +740,6 @@ __global__ void __launch_bounds__(kQAThreads, 2)
             }
             if (prod.write_y) fence_proxy_async_smem();
             if (tile + step < ntiles) load_up(nxt);
-        } else if constexpr (PROD == kProdActBackward) {
-            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            act_dispatch(prod.act, [&](auto act) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = act_backward_chunk4<decltype(act)::value>(v[i], un[i], sum);
-            });
-            if (prod.col_sum) *reinterpret_cast<float4 *>(&sm.col_sum[br][4 * bc]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
-            if (prod.write_y) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) *reinterpret_cast<uint2 *>(in + (8 * br + i) * kQT + 4 * bc) = v[i];
-                fence_proxy_async_smem();
-            }
-            if (prod.up && tile + step < ntiles) load_up(nxt);
-        } else if constexpr (PROD == kProdGatedBackward) {
-            const int64_t at = (r0 + 8 * br) * prod.ld + static_cast<int64_t>(cur.c >> 1) * kQT + 4 * bc;
-            const int half = cur.c & 1;
-            act_dispatch(prod.act, [&](auto act) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint2 g = __ldg(reinterpret_cast<const uint2 *>(prod.gate + at + i * prod.ld));
-                    const uint2 u = half ? make_uint2(0u, 0u) : __ldg(reinterpret_cast<const uint2 *>(prod.up + at + i * prod.ld));
-                    v[i] = gated_backward_chunk4<decltype(act)::value>(v[i], g, u, half);
-                }
-            });
-            if (prod.write_y) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) *reinterpret_cast<uint2 *>(in + (8 * br + i) * kQT + 4 * bc) = v[i];
-                fence_proxy_async_smem();
-            }
         }
 
         // ---- A: row groups (a warp holds its eight rows whole) and column partials
@@ -871,16 +797,6 @@ __global__ void __launch_bounds__(kQAThreads, 2)
             if (prod.write_y && tid == 0) {  // every block's y is in shared memory
                 tma_store_2d(&tm_y, sm.in[buf], static_cast<int32_t>(c0), static_cast<int32_t>(r0));
                 bulk_commit_group();
-            }
-        }
-
-        if constexpr (PROD == kProdActBackward) {  // the tile's 128 rows, their blocks in order
-            if (prod.col_sum && tid >= kQAThreads - kQT) {
-                const int c = tid - (kQAThreads - kQT);
-                float a = sm.col_sum[0][c];
-#pragma unroll
-                for (int b = 1; b < 16; ++b) a += sm.col_sum[b][c];
-                prod.col_sum[static_cast<int64_t>(cur.r) * cols + c0 + c] = a;
             }
         }
 
@@ -1027,6 +943,237 @@ __global__ void __launch_bounds__(kQAThreads, 2)
     if (tid == 0) bulk_wait_group0();
 }
 
+// ------------------------------------------- backward of activations, quantised
+// dz = dy * act'(z) or, GATED, [dgate, dup] = [dh * up * act'(gate), dh *
+// act(gate)], rounded to BF16 and cast as quant_act_kernel casts: 512 threads on
+// a 128x128 tile, thread t on the 8x4 block of rows 8*br .. and columns 4*bc ..,
+// br = warp, bc = lane.  The inputs' tiles come by TMA into one buffer each.  Once
+// they are in registers the buffers are free: y's for the next tile's y, and the
+// others (GATED) for the staging of the codes, which leaves room for two CTAs an
+// SM with 96 KB of loads each; they alternate, one computing while the other
+// waits for its tiles.  Both outputs of a gate come from one evaluation of the
+// activation.
+// As a producer of quant_act_kernel (a tile of one output at a time, the gates
+// loaded into registers), us: [8192, 6144] gated 171 -> 108, [8192, 8960]
+// gelu_tanh with dbias 115 -> 90.
+template <bool GATED>
+struct QuantBackwardSmem {
+    static constexpr int kOut = GATED ? 2 : 1;
+    alignas(1024) uint16_t y[kQT * kQT];          // dy or dh
+    alignas(1024) uint16_t z[kOut][kQT * kQT];    // z, or gate and up; GATED: then the codes of each output
+    alignas(1024) uint8_t stage[GATED ? 16 : 2 * kQT * kQT];  // the codes, rowwise and transposed
+    alignas(16) uint32_t col_part[kOut][16][kQT / 2];
+    alignas(16) float col_mul[kOut][kQT];
+    alignas(16) float col_sum[GATED ? 1 : 16][kQT];  // sums of dz over each block of eight rows
+    alignas(16) uint8_t row_g[kOut][kQT];
+    alignas(16) uint8_t col_g[kOut][kQT];
+    uint64_t full;
+};
+
+template <int FMT, bool HAS_T, bool GATED>
+__global__ void __launch_bounds__(kQAThreads, 2)
+    quant_backward_kernel(const __grid_constant__ BackwardQuantMaps m, const BackwardQuantArgs a) {
+    constexpr int kOut = GATED ? 2 : 1;
+    using Smem = QuantBackwardSmem<GATED>;
+    extern __shared__ uint8_t smem_raw[];
+    Smem &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    const int tid = threadIdx.x, lane = tid & 31, br = tid >> 5, bc = lane;
+    const bool has_z = GATED || a.act != PURO_ACT_NONE;
+    auto q_stage = [&](int o) { return GATED ? reinterpret_cast<uint8_t *>(sm.z[o]) : sm.stage; };
+    auto qt_stage = [&](int o) { return q_stage(o) + kQT * kQT; };
+    if (tid == 0) {
+        mbar_init(&sm.full, 1);
+        fence_mbarrier_init();
+        tma_prefetch_desc(&m.y);
+        tma_prefetch_desc(&m.z);
+        if (GATED) tma_prefetch_desc(&m.up);
+        tma_prefetch_desc(&m.q);
+        if (HAS_T) tma_prefetch_desc(&m.qt);
+    }
+    __syncthreads();
+    const int tiles_n = static_cast<int>(a.cols / kQT);
+    const int ntiles = static_cast<int>(a.rows / kQT) * tiles_n;
+    const int step = gridDim.x;
+    int tile = blockIdx.x;
+    TileWalk cur(ntiles - 1 - tile, step, tiles_n), nxt = cur;
+    nxt.advance();
+    auto load_y = [&](const TileWalk &t) {  // opens the tile's phase of the barrier
+        mbar_arrive_expect_tx(&sm.full, (1 + (has_z ? kOut : 0)) * kQT * kQT * 2);
+        tma_load_2d(sm.y, &m.y, &sm.full, t.c * kQT, t.r * kQT);
+    };
+    auto load_z = [&](const TileWalk &t) {
+        if (has_z) tma_load_2d(sm.z[0], &m.z, &sm.full, t.c * kQT, t.r * kQT);
+        if constexpr (GATED) tma_load_2d(sm.z[kOut - 1], &m.up, &sm.full, t.c * kQT, t.r * kQT);
+    };
+    pdl_wait();
+    pdl_launch_dependents();
+    if (tid == 0) {  // (the grid has no more CTAs than tiles)
+        load_y(cur);
+        load_z(cur);
+    }
+    const int64_t out_cols = a.cols * kOut;
+    for (int it = 0; tile < ntiles; ++it, tile += step, cur = nxt, nxt.advance()) {
+        const int64_t r0 = static_cast<int64_t>(cur.r) * kQT, c0 = static_cast<int64_t>(cur.c) * kQT;
+        const bool landed = tile_landed(&sm.full, static_cast<uint32_t>(it) & 1u, a.wait_ns);
+
+        uint2 v[kOut][8];  // the outputs in BF16
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        act_dispatch(a.act, [&](auto act) {
+            constexpr int ACT = decltype(act)::value;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int at = (8 * br + i) * kQT + 4 * bc;
+                const uint2 y = *reinterpret_cast<const uint2 *>(sm.y + at);
+                if constexpr (GATED) {
+                    const uint2 g = *reinterpret_cast<const uint2 *>(sm.z[0] + at), u = *reinterpret_cast<const uint2 *>(sm.z[kOut - 1] + at);
+                    gated_backward2<ACT>(y.x, g.x, u.x, v[0][i].x, v[kOut - 1][i].x);
+                    gated_backward2<ACT>(y.y, g.y, u.y, v[0][i].y, v[kOut - 1][i].y);
+                } else if constexpr (ACT == PURO_ACT_NONE) {
+                    v[0][i] = y;
+                    sum[0] += bf16_lo(y.x), sum[1] += bf16_hi(y.x), sum[2] += bf16_lo(y.y), sum[3] += bf16_hi(y.y);
+                } else {
+                    const uint2 z = *reinterpret_cast<const uint2 *>(sm.z[0] + at);
+                    v[0][i] = make_uint2(act_backward2<ACT>(y.x, z.x, sum[0], sum[1]), act_backward2<ACT>(y.y, z.y, sum[2], sum[3]));
+                }
+            }
+        });
+
+        // ---- A: row groups (a warp holds its eight rows whole) and column partials
+        float mul[kOut];  // lane i % 8: of row i
+#pragma unroll
+        for (int o = 0; o < kOut; ++o) {
+            uint32_t rmax[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t w = __vmaxu2(v[o][i].x & 0x7FFF7FFFu, v[o][i].y & 0x7FFF7FFFu);
+                rmax[i] = __reduce_max_sync(0xFFFFFFFFu, __vmaxu2(w, __byte_perm(w, 0u, 0x1032)));
+            }
+            const bool b0 = lane & 1, b1 = lane & 2, b2 = lane & 4;
+            const uint32_t s01 = b0 ? rmax[1] : rmax[0], s23 = b0 ? rmax[3] : rmax[2];
+            const uint32_t s45 = b0 ? rmax[5] : rmax[4], s67 = b0 ? rmax[7] : rmax[6];
+            const uint32_t g = e8m0_exponent<FMT>((b2 ? (b1 ? s67 : s45) : (b1 ? s23 : s01)) & 0xFFFFu);
+            mul[o] = mul_of(g);
+            if (lane < 8) sm.row_g[o][8 * br + lane] = static_cast<uint8_t>(g);
+            if constexpr (HAS_T) {
+                uint2 cm = make_uint2(0u, 0u);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    cm.x = __vmaxu2(cm.x, v[o][i].x & 0x7FFF7FFFu);
+                    cm.y = __vmaxu2(cm.y, v[o][i].y & 0x7FFF7FFFu);
+                }
+                *reinterpret_cast<uint2 *>(&sm.col_part[o][br][2 * bc]) = cm;
+            }
+        }
+        if (!GATED && a.col_sum)
+            *reinterpret_cast<float4 *>(&sm.col_sum[br][4 * bc]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+        if (!GATED && tid == 0) bulk_wait_group_read0();  // the staging is free
+        if (__syncthreads_or(!landed)) {                  // (S2) partials written, every input in registers
+            if (tid == 0) {
+                if (a.status) atomicExch(a.status, kQuantStatusTimeout);
+                mbar_wait_bounded(&sm.full, static_cast<uint32_t>(it) & 1u, kQuantDrainNs);  // its loads land
+            }
+            break;
+        }
+        const bool more = tile + step < ntiles;
+        if (tid == 0 && more) {
+            load_y(nxt);
+            if (!GATED) load_z(nxt);
+        }
+
+        // ---- B: column scales, two threads per column (eight row blocks each)
+        if constexpr (HAS_T) {
+            const int o = tid / (2 * kQT), c = (tid >> 1) & (kQT - 1), h = tid & 1;
+            if (o < kOut) {
+                uint32_t w = 0;
+#pragma unroll
+                for (int b = 0; b < 8; ++b) w = __vmaxu2(w, sm.col_part[o][8 * h + b][c >> 1]);
+                w = __vmaxu2(w, __shfl_xor_sync(0xFFFFFFFFu, w, 1));
+                if (h == 0) {
+                    const uint32_t g = e8m0_exponent<FMT>((c & 1) ? (w >> 16) : (w & 0xFFFFu));
+                    sm.col_mul[o][c] = mul_of(g);
+                    sm.col_g[o][c] = static_cast<uint8_t>(g);
+                }
+            }
+        }
+        if (!GATED && a.col_sum && tid >= kQAThreads - kQT) {  // the tile's 128 rows, their blocks in order
+            const int c = tid - (kQAThreads - kQT);
+            float s = sm.col_sum[0][c];
+#pragma unroll
+            for (int b = 1; b < (GATED ? 1 : 16); ++b) s += sm.col_sum[b][c];
+            a.col_sum[static_cast<int64_t>(cur.r) * a.cols + c0 + c] = s;
+        }
+        if (a.out) {  // the BF16 rows: a warp stores 256 bytes of one
+#pragma unroll
+            for (int o = 0; o < kOut; ++o)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    *reinterpret_cast<uint2 *>(a.out + (r0 + 8 * br + i) * out_cols + o * a.cols + c0 + 4 * bc) = v[o][i];
+        }
+        if (HAS_T) __syncthreads();  // (S3) column scales ready
+
+        // ---- C: codes into the staging
+#pragma unroll
+        for (int o = 0; o < kOut; ++o) {
+            uint8_t *qs = q_stage(o);
+            float4 cmv = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+            float msum = mul[o];
+            if constexpr (HAS_T) {
+                cmv = *reinterpret_cast<const float4 *>(&sm.col_mul[o][4 * bc]);
+                msum += (cmv.x + cmv.y) + (cmv.z + cmv.w);
+            }
+            // a group that holds Inf or NaN has a NaN multiplier: its codes are NaN with each value's sign
+            const bool some_nan = __any_sync(0xFFFFFFFFu, isnan(msum));
+            const uint32_t col_nan = (isnan(cmv.x) ? 0xFFu : 0u) | (isnan(cmv.y) ? 0xFF00u : 0u) |
+                                     (isnan(cmv.z) ? 0xFF0000u : 0u) | (isnan(cmv.w) ? 0xFF000000u : 0u);
+            const uint64_t cm01 = f32x2(cmv.x, cmv.y), cm23 = f32x2(cmv.z, cmv.w);
+            uint32_t rw[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint2 w = v[o][i];
+                const float rm = __shfl_sync(0xFFFFFFFFu, mul[o], i);
+                const uint64_t p0 = f32x2(bf16_lo(w.x), bf16_hi(w.x)), p1 = f32x2(bf16_lo(w.y), bf16_hi(w.y)), rr = f32x2(rm, rm);
+                uint32_t q = cvt_f32x4<FMT>(mul_f32x2(p0, rr), mul_f32x2(p1, rr));
+                if constexpr (HAS_T) rw[i] = cvt_f32x4<FMT>(mul_f32x2(p0, cm01), mul_f32x2(p1, cm23));
+                if (__builtin_expect(some_nan, 0)) {
+                    const uint32_t nan = 0x7F7F7F7Fu | ((w.x >> 8) & 0x80u) | ((w.x >> 16) & 0x8000u) | ((w.y & 0x8000u) << 8) |
+                                         (w.y & 0x80000000u);
+                    if (isnan(rm)) q = nan;
+                    if constexpr (HAS_T) rw[i] = (rw[i] & ~col_nan) | (nan & col_nan);
+                }
+                *reinterpret_cast<uint32_t *>(qs + (8 * br + i) * kQT + 4 * bc) = q;
+            }
+            if constexpr (HAS_T) stage_transposed_8x4(qt_stage(o), rw, br, bc);
+        }
+        // scale vectors: of output tid / 256, the rowwise operand's rows, then the transposed one's
+        {
+            const int o = tid / (2 * kQT);
+            const bool col = (tid & kQT) != 0;
+            if (o < kOut && (!col || HAS_T)) {
+                const int i = tid & (kQT - 1);
+                const int64_t oc0 = o * a.cols + c0;
+                store_scale_vec(col ? a.scale_t : a.scale, (col ? oc0 : r0) + i, (col ? r0 : oc0) / kQT,
+                                (col ? a.rows : out_cols) / kQT, col ? sm.col_g[o][i] : sm.row_g[o][i]);
+            }
+        }
+        fence_proxy_async_smem();
+        __syncthreads();  // (S4) staging complete, exponents read
+        if (tid == 0) {
+#pragma unroll
+            for (int o = 0; o < kOut; ++o) {
+                const int oc0 = static_cast<int>(o * a.cols + c0);
+                tma_store_2d(&m.q, q_stage(o), oc0, static_cast<int32_t>(r0));
+                if (HAS_T) tma_store_2d(&m.qt, qt_stage(o), static_cast<int32_t>(r0), oc0);
+            }
+            bulk_commit_group();
+            if (GATED && more) {  // the gates' buffers hold the codes until they have left
+                bulk_wait_group_read0();
+                load_z(nxt);
+            }
+        }
+    }
+    if (tid == 0) bulk_wait_group0();
+}
+
 // ------------------------------------------------------ grouped weight cast
 // The weights of a model are quantised once per optimizer step (section "FP8
 // Mixed-Precision Training": 128x128 blocks), so all of them can go through
@@ -1156,7 +1303,7 @@ static cudaError_t launch_quant_t(const QuantArgs &a, const CUtensorMap &tm_x, c
                                   ProdArgs prod = ProdArgs{}) {
     if constexpr (KIND == kQuantBlockAct) {  // the 512-thread activation kernel (whole tiles)
         auto kern = quant_act_kernel<FMT, HAS_T, PROD>;
-        const size_t smem = sizeof(QuantActSmemOf<PROD>) + 1024;
+        const size_t smem = sizeof(QuantActSmem) + 1024;
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
         if (e != cudaSuccess) return e;
         const int tiles_n = static_cast<int>(a.cols / kQT);
@@ -1233,26 +1380,20 @@ static cudaError_t launch_swiglu_f(const QuantArgs &a, const CUtensorMap &tm_x, 
                    : launch_quant_t<FMT, kQuantBlockAct, false, kProdSwiGlu>(a, tm_x, tm_q, tm_qt, s, &tm_y, prod);
 }
 
-template <int FMT, int PROD>
-static cudaError_t launch_prod_f(const QuantArgs &a, const CUtensorMap &tm_x, const CUtensorMap &tm_q,
-                                 const CUtensorMap &tm_qt, const CUtensorMap &tm_y, const ProdArgs &prod,
-                                 cudaStream_t s) {
-    return a.has_t ? launch_quant_t<FMT, kQuantBlockAct, true, PROD>(a, tm_x, tm_q, tm_qt, s, &tm_y, prod)
-                   : launch_quant_t<FMT, kQuantBlockAct, false, PROD>(a, tm_x, tm_q, tm_qt, s, &tm_y, prod);
+template <int FMT, bool GATED>
+static cudaError_t launch_backward_f(const BackwardQuantArgs &a, const BackwardQuantMaps &m, cudaStream_t s) {
+    auto kern = a.scale_t ? quant_backward_kernel<FMT, true, GATED> : quant_backward_kernel<FMT, false, GATED>;
+    const size_t smem = sizeof(QuantBackwardSmem<GATED>) + 1024;
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e != cudaSuccess) return e;
+    const int64_t ntiles = a.rows / kQT * (a.cols / kQT);
+    const int cap = 2 * sm_count_here();  // persistent: two CTAs per SM
+    return launch_pdl(kern, dim3(static_cast<unsigned>(ntiles < cap ? ntiles : cap)), dim3(kQAThreads), smem, s, m, a);
 }
 
-cudaError_t launch_quantize_act_backward(const QuantArgs &a, const CUtensorMap &tm_x, const CUtensorMap &tm_q,
-                                         const CUtensorMap &tm_qt, const CUtensorMap &tm_y, const ProdArgs &prod,
-                                         cudaStream_t s) {
-    return a.fmt == 0 ? launch_prod_f<0, kProdActBackward>(a, tm_x, tm_q, tm_qt, tm_y, prod, s)
-                      : launch_prod_f<1, kProdActBackward>(a, tm_x, tm_q, tm_qt, tm_y, prod, s);
-}
-
-cudaError_t launch_quantize_gated_backward(const QuantArgs &a, const CUtensorMap &tm_x, const CUtensorMap &tm_q,
-                                           const CUtensorMap &tm_qt, const CUtensorMap &tm_y, const ProdArgs &prod,
-                                           cudaStream_t s) {
-    return a.fmt == 0 ? launch_prod_f<0, kProdGatedBackward>(a, tm_x, tm_q, tm_qt, tm_y, prod, s)
-                      : launch_prod_f<1, kProdGatedBackward>(a, tm_x, tm_q, tm_qt, tm_y, prod, s);
+cudaError_t launch_quantize_backward(const BackwardQuantArgs &a, const BackwardQuantMaps &m, bool gated, cudaStream_t s) {
+    if (gated) return a.fmt == 0 ? launch_backward_f<0, true>(a, m, s) : launch_backward_f<1, true>(a, m, s);
+    return a.fmt == 0 ? launch_backward_f<0, false>(a, m, s) : launch_backward_f<1, false>(a, m, s);
 }
 
 cudaError_t launch_quantize_swiglu(const QuantArgs &a, const CUtensorMap &tm_x, const CUtensorMap &tm_q,
