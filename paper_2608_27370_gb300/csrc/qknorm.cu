@@ -29,8 +29,7 @@
 namespace puro {
 
 constexpr int kQkThreads = 256;
-constexpr int kQkFwdBatch = 4;   // heads of a token a group loads at once
-constexpr int kQkBwdBatch = 2;
+constexpr int kQkFwdBatch = 3, kQkBwdBatch = 2;  // heads of a token a group loads at once
 constexpr int kQkBwdBlocks = 152 * 2;  // at most: two an SM are resident, each leaves a partial sum of a gain's gradient
 constexpr int32_t kQkStatusInvalid = 1;  // PURO_ERR_INVALID_ARG
 
@@ -50,45 +49,91 @@ PURO_DEV QkLane qk_lane(int c, int D, int rot, int inter) {
     return l;
 }
 
-PURO_DEV void load8(const float *p, float (&v)[8]) {
-    const float4 a = __ldg(reinterpret_cast<const float4 *>(p)), b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-}
-
-PURO_DEV void widen8(const uint4 &w, float *v) {
-    const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+// The lane's sixteen channels as eight pairs (a, b), two pairs to a packed value:
+// a[j] holds the first channels of pairs 2j and 2j + 1, b[j] the second.
+struct Pairs {
+    uint64_t a[4], b[4];
+};
+template <bool INTER>
+PURO_DEV Pairs unpack16(const uint4 &w0, const uint4 &w1) {
+    const uint32_t x[4] = {w0.x, w0.y, w0.z, w0.w}, y[4] = {w1.x, w1.y, w1.z, w1.w};
+    Pairs p;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = bf16_lo(ws[i]);
-        v[2 * i + 1] = bf16_hi(ws[i]);
-    }
-}
-
-PURO_DEV uint4 narrow8(const float *v) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        w[i] = *reinterpret_cast<uint32_t *>(&b);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-// R v (sign 1) or R^T v (sign -1) of the lane's sixteen channels.
-PURO_DEV void turn16(float (&v)[16], const float (&co)[8], const float (&si)[8], bool inter, float sign) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float s = sign * si[i];
-        const float a = inter ? v[2 * i] : v[i], b = inter ? v[2 * i + 1] : v[8 + i];
-        const float p = a * co[i] - b * s, q = b * co[i] + a * s;
-        if (inter) {
-            v[2 * i] = p;
-            v[2 * i + 1] = q;
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (INTER) {  // neighbours: pairs 0 .. 3 in w0, 4 .. 7 in w1
+            const uint32_t u = j < 2 ? x[2 * j] : y[2 * j - 4], v = j < 2 ? x[2 * j + 1] : y[2 * j - 3];
+            p.a[j] = f32x2(bf16_lo(u), bf16_lo(v));
+            p.b[j] = f32x2(bf16_hi(u), bf16_hi(v));
         } else {
-            v[i] = p;
-            v[8 + i] = q;
+            p.a[j] = f32x2(bf16_lo(x[j]), bf16_hi(x[j]));
+            p.b[j] = f32x2(bf16_lo(y[j]), bf16_hi(y[j]));
         }
     }
+    return p;
+}
+
+PURO_DEV uint32_t round2(float lo, float hi) {
+    __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t *>(&b);
+}
+template <bool INTER>
+PURO_DEV void pack16(const Pairs &p, uint4 &w0, uint4 &w1) {
+    uint32_t x[4], y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float a0, a1, b0, b1;
+        split_f32x2(p.a[j], a0, a1);
+        split_f32x2(p.b[j], b0, b1);
+        if constexpr (INTER) {
+            (j < 2 ? x : y)[2 * j & 3] = round2(a0, b0);
+            (j < 2 ? x : y)[(2 * j & 3) + 1] = round2(a1, b1);
+        } else {
+            x[j] = round2(a0, a1);
+            y[j] = round2(b0, b1);
+        }
+    }
+    w0 = make_uint4(x[0], x[1], x[2], x[3]);
+    w1 = make_uint4(y[0], y[1], y[2], y[3]);
+}
+
+// The angles of the lane's pairs: cosines, sines and negative sines.
+struct Angles {
+    uint64_t c[4], s[4], n[4];
+};
+// R p, or with s and n exchanged R^T p.
+PURO_DEV void turn(Pairs &p, const uint64_t (&c)[4], const uint64_t (&s)[4], const uint64_t (&n)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint64_t a = p.a[j], b = p.b[j];
+        p.a[j] = fma_f32x2(b, n[j], mul_f32x2(a, c[j]));
+        p.b[j] = fma_f32x2(a, s[j], mul_f32x2(b, c[j]));
+    }
+}
+PURO_DEV void scale(Pairs &p, uint64_t f) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        p.a[j] = mul_f32x2(p.a[j], f);
+        p.b[j] = mul_f32x2(p.b[j], f);
+    }
+}
+PURO_DEV void times(Pairs &p, const Pairs &q) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        p.a[j] = mul_f32x2(p.a[j], q.a[j]);
+        p.b[j] = mul_f32x2(p.b[j], q.b[j]);
+    }
+}
+// The sum of the products of the lane's channels.
+PURO_DEV float dot(const Pairs &p, const Pairs &q) {
+    uint64_t s = mul_f32x2(p.a[0], q.a[0]), t = mul_f32x2(p.b[0], q.b[0]);
+#pragma unroll
+    for (int j = 1; j < 4; ++j) {
+        s = fma_f32x2(p.a[j], q.a[j], s);
+        t = fma_f32x2(p.b[j], q.b[j], t);
+    }
+    float lo, hi;
+    split_f32x2(add_f32x2(s, t), lo, hi);
+    return lo + hi;
 }
 
 template <int G>
@@ -99,83 +144,103 @@ PURO_DEV float group_sum(float x) {
 }
 
 // The token's position and angles.  A negative position marks a padding row
-// (kPad); one past the tables cannot be rotated (kOut).
+// (kRowPad); one past the tables cannot be rotated (kRowOut).
 enum QkRow : int { kRowLive, kRowPad, kRowOut };
-PURO_DEV QkRow qk_angles(const QkArgs &p, int64_t t, const QkLane &l, float (&co)[8], float (&si)[8]) {
+PURO_DEV QkRow qk_angles(const QkArgs &p, int64_t t, const QkLane &l, Angles &g) {
     const int64_t pos = p.positions ? __ldg(p.positions + t) : t;
     if (pos < 0) return kRowPad;
     if (p.rot > 0 && pos >= p.max_positions) return kRowOut;
     if (l.in && l.turned) {
-        load8(p.cos + pos * (p.rot / 2) + l.pair, co);
-        load8(p.sin + pos * (p.rot / 2) + l.pair, si);
+        const float4 *c = reinterpret_cast<const float4 *>(p.cos + pos * (p.rot / 2) + l.pair);
+        const float4 *s = reinterpret_cast<const float4 *>(p.sin + pos * (p.rot / 2) + l.pair);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const float4 x = __ldg(c + k), y = __ldg(s + k);
+            g.c[2 * k] = f32x2(x.x, x.y);
+            g.c[2 * k + 1] = f32x2(x.z, x.w);
+            g.s[2 * k] = f32x2(y.x, y.y);
+            g.s[2 * k + 1] = f32x2(y.z, y.w);
+            g.n[2 * k] = f32x2(-y.x, -y.y);
+            g.n[2 * k + 1] = f32x2(-y.z, -y.w);
+        }
     }
     return kRowLive;
 }
 
-PURO_DEV float nan_f32() { return __uint_as_float(0x7FC00000u); }
+// 1 / sqrt(x) (about 2^-23 off).
+PURO_DEV float rsqrt_f32(float x) {
+    float y;
+    asm("rsqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 
+// What a row that is not live counts as: zeros for padding, whatever it holds,
+// and NaN past the tables.
+PURO_DEV void replace_row(QkRow row, uint4 (&w)[2]) {
+    const uint32_t v = row == kRowPad ? 0u : 0x7FC07FC0u;
+    w[0] = w[1] = make_uint4(v, v, v, v);
+}
+
+// A block: some tokens' batch of heads of one kind, the batches of the same tokens
+// next to one another (the queries' first).  On 8192 tokens of 16 + 8 heads of 128
+// 22 us (4.7 TB/s), on 32768 45 us (5.3 TB/s); the same loads and stores without the
+// arithmetic take 16.4.  Persistent blocks with the next items' loads in flight
+// (cp.async, two ahead) took 23 to 45 us: what that saves goes into addresses.
 template <int G, bool INTER>
-__global__ void __launch_bounds__(kQkThreads) qk_norm_rope_kernel(const QkArgs p) {
+__global__ void __launch_bounds__(kQkThreads, 3) qk_norm_rope_kernel(const QkArgs p) {
     constexpr int B = kQkFwdBatch;
     pdl_wait();
     pdl_launch_dependents();
     const QkLane l = qk_lane(threadIdx.x % G, p.D, p.rot, INTER);
-    const int64_t t = static_cast<int64_t>(blockIdx.x) * (kQkThreads / G) + threadIdx.x / G;
-    const int h0 = blockIdx.y * B, heads = p.q.heads + p.k.heads;
-    const bool live = t < p.tokens;
+    const unsigned q_batches = (p.q.heads + B - 1) / B, batches = q_batches + (p.k.heads + B - 1) / B;
+    const int64_t t = static_cast<int64_t>(blockIdx.x / batches) * (kQkThreads / G) + threadIdx.x / G;
+    const unsigned batch = blockIdx.x % batches;
+    const bool is_q = batch < q_batches, live = t < p.tokens && l.in;
+    const QkHeads &src = is_q ? p.q : p.k, &dst = is_q ? p.q_out : p.k_out;
+    const int h0 = static_cast<int>(is_q ? batch : batch - q_batches) * B, n = min(B, src.heads - h0);
+    const uint16_t *from = src.data + t * src.token_stride + h0 * src.head_stride;
     uint4 x[B][2];
 #pragma unroll
     for (int b = 0; b < B; ++b) {
-        const int h = h0 + b;
         x[b][0] = x[b][1] = make_uint4(0, 0, 0, 0);
-        if (live && l.in && h < heads) {
-            const QkHeads &src = h < p.q.heads ? p.q : p.k;
-            const uint16_t *r = src.data + t * src.token_stride + (h < p.q.heads ? h : h - p.q.heads) * src.head_stride;
-            x[b][0] = *reinterpret_cast<const uint4 *>(r + l.o0);
-            x[b][1] = *reinterpret_cast<const uint4 *>(r + l.o1);
+        if (live && b < n) {
+            x[b][0] = *reinterpret_cast<const uint4 *>(from + l.o0);
+            x[b][1] = *reinterpret_cast<const uint4 *>(from + l.o1);
         }
+        from += src.head_stride;
     }
-    float co[8], si[8];
-    const QkRow row = live ? qk_angles(p, t, l, co, si) : kRowPad;
-    if (row == kRowOut && p.status && l.pair == 0) *p.status = kQkStatusInvalid;
+    Angles ang;
+    const QkRow row = live ? qk_angles(p, t, l, ang) : kRowPad;
+    if (row != kRowLive) {
+#pragma unroll
+        for (int b = 0; b < B; ++b) replace_row(row, x[b]);
+        if (row == kRowOut && p.status && l.pair == 0) *p.status = kQkStatusInvalid;
+    }
+    const float inv = 1.0f / static_cast<float>(p.D);
+    const uint16_t *gains = is_q ? p.q_gain : p.k_gain;
+    Pairs gain;
+    if (gains && l.in)
+        gain = unpack16<INTER>(__ldg(reinterpret_cast<const uint4 *>(gains + l.o0)), __ldg(reinterpret_cast<const uint4 *>(gains + l.o1)));
+    uint16_t *to = dst.data + t * dst.token_stride + h0 * dst.head_stride;
+    float *rstds = p.rstd + t * (p.q.heads + p.k.heads) + (is_q ? 0 : p.q.heads) + h0;
+    const bool store_rstd = live && p.rstd && l.pair == 0, turned = row == kRowLive && l.turned;
 #pragma unroll
     for (int b = 0; b < B; ++b) {
-        const int h = h0 + b;
-        if (h >= heads) break;  // the same for the whole block
-        float v[16];
-        widen8(x[b][0], v);
-        widen8(x[b][1], v + 8);
-        float s0 = 0.0f, s1 = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            s0 = fmaf(v[i], v[i], s0);
-            s1 = fmaf(v[8 + i], v[8 + i], s1);
-        }
-        const float ss = group_sum<G>(s0 + s1);
-        float rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(ss, static_cast<float>(p.D)) + p.eps));
+        if (b >= n) break;  // the same for the whole block
+        Pairs v = unpack16<INTER>(x[b][0], x[b][1]);
+        float rstd = rsqrt_f32(fmaf(group_sum<G>(dot(v, v)), inv, p.eps));
         if (row == kRowPad) rstd = 0.0f;
-        if (row == kRowOut) rstd = nan_f32();
-        const bool is_q = h < p.q.heads;
-        if (live && p.rstd && l.pair == 0) p.rstd[t * heads + h] = rstd;
-        if (!live || !l.in) continue;
-        const uint16_t *gain = is_q ? p.q_gain : p.k_gain;
-        if (gain) {
-            float g[16];
-            widen8(__ldg(reinterpret_cast<const uint4 *>(gain + l.o0)), g);
-            widen8(__ldg(reinterpret_cast<const uint4 *>(gain + l.o1)), g + 8);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = v[i] * rstd * g[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] *= rstd;
+        if (store_rstd) rstds[b] = rstd;
+        if (gains) times(v, gain);
+        scale(v, f32x2(rstd, rstd));
+        if (turned) turn(v, ang.c, ang.s, ang.n);
+        uint4 y0, y1;
+        pack16<INTER>(v, y0, y1);
+        if (live) {
+            *reinterpret_cast<uint4 *>(to + l.o0) = y0;
+            *reinterpret_cast<uint4 *>(to + l.o1) = y1;
         }
-        if (row == kRowLive && l.turned) turn16(v, co, si, INTER, 1.0f);
-        uint4 y0 = narrow8(v), y1 = narrow8(v + 8);
-        if (row == kRowPad) y0 = y1 = make_uint4(0, 0, 0, 0);  // whatever the row holds
-        const QkHeads &dst = is_q ? p.q_out : p.k_out;
-        uint16_t *w = dst.data + t * dst.token_stride + (is_q ? h : h - p.q.heads) * dst.head_stride;
-        *reinterpret_cast<uint4 *>(w + l.o0) = y0;
-        *reinterpret_cast<uint4 *>(w + l.o1) = y1;
+        to += dst.head_stride;
     }
 }
 
@@ -193,29 +258,29 @@ __global__ void __launch_bounds__(kQkThreads, 2) qk_norm_rope_backward_kernel(co
     const int blocks = is_q ? p.q_blocks : gridDim.x - p.q_blocks;
     const QkHeads &X = is_q ? p.q : p.k, &DY = is_q ? p.q_out : p.k_out, &DX = is_q ? p.dq : p.dk;
     const int first = is_q ? 0 : p.q.heads, heads = p.q.heads + p.k.heads;
-    const int64_t batches = (X.heads + B - 1) / B;
+    const int batches = (X.heads + B - 1) / B;
     const uint16_t *gain = is_q ? p.q_gain : p.k_gain;
-    uint4 gw[2] = {};
-    if (gain && l.in) {
-        gw[0] = __ldg(reinterpret_cast<const uint4 *>(gain + l.o0));
-        gw[1] = __ldg(reinterpret_cast<const uint4 *>(gain + l.o1));
-    }
-    float acc[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[i] = 0.0f;
-    const int64_t items = p.tokens * batches, step = static_cast<int64_t>(blocks) * kGroups;
+    Pairs g = {};
+    if (gain && l.in)
+        g = unpack16<INTER>(__ldg(reinterpret_cast<const uint4 *>(gain + l.o0)), __ldg(reinterpret_cast<const uint4 *>(gain + l.o1)));
+    const float inv = 1.0f / static_cast<float>(p.D);
+    Pairs acc = {};  // (zero bits)
+    // item = token * batches + batch; the next one is a step on, taken without a division
+    const int64_t items = p.tokens * batches;
+    const int step = blocks * kGroups, dt = step / batches, db = step - dt * batches;
+    const int item0 = block * kGroups + threadIdx.x / G;
+    int64_t t = item0 / batches;
+    int batch = static_cast<int>(item0 - t * batches);
     for (int64_t i0 = static_cast<int64_t>(block) * kGroups; i0 < items; i0 += step) {
-        const int64_t item = i0 + threadIdx.x / G;
-        const int64_t t = item / batches;
-        const int h0 = static_cast<int>(item - t * batches) * B;
-        const bool live = item < items;
+        const int h0 = batch * B;
+        const bool live = t < p.tokens && l.in;
         uint4 x[B][2], dy[B][2];
         float rs[B];
 #pragma unroll
         for (int b = 0; b < B; ++b) {
             x[b][0] = x[b][1] = dy[b][0] = dy[b][1] = make_uint4(0, 0, 0, 0);
             rs[b] = 0.0f;
-            if (live && l.in && h0 + b < X.heads) {
+            if (live && h0 + b < X.heads) {
                 const uint16_t *px = X.data + t * X.token_stride + (h0 + b) * X.head_stride;
                 const uint16_t *py = DY.data + t * DY.token_stride + (h0 + b) * DY.head_stride;
                 x[b][0] = *reinterpret_cast<const uint4 *>(px + l.o0);
@@ -225,53 +290,74 @@ __global__ void __launch_bounds__(kQkThreads, 2) qk_norm_rope_backward_kernel(co
                 rs[b] = __ldg(p.rstd + t * heads + first + h0 + b);
             }
         }
-        float co[8], si[8];
-        const QkRow row = live ? qk_angles(p, t, l, co, si) : kRowPad;
-        if (row == kRowOut && p.status && l.pair == 0) *p.status = kQkStatusInvalid;
+        Angles ang;
+        const QkRow row = live ? qk_angles(p, t, l, ang) : kRowPad;
+        if (row != kRowLive) {
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                replace_row(row, x[b]);
+                replace_row(row, dy[b]);
+                if (row == kRowPad) rs[b] = 0.0f;
+            }
+            if (row == kRowOut && p.status && l.pair == 0) *p.status = kQkStatusInvalid;
+        }
+        const bool turned = row == kRowLive && l.turned;
 #pragma unroll
         for (int b = 0; b < B; ++b) {
-            float d[16], xh[16], g[16];
-            widen8(dy[b][0], d);
-            widen8(dy[b][1], d + 8);
-            widen8(x[b][0], xh);
-            widen8(x[b][1], xh + 8);
-            widen8(gw[0], g);
-            widen8(gw[1], g + 8);
-            if (row == kRowLive && l.turned) turn16(d, co, si, INTER, -1.0f);
-            const float r = row == kRowOut ? nan_f32() : rs[b];
-            float s0 = 0.0f, s1 = 0.0f;
+            Pairs d = unpack16<INTER>(dy[b][0], dy[b][1]), xh = unpack16<INTER>(x[b][0], x[b][1]);
+            if (turned) turn(d, ang.c, ang.n, ang.s);
+            scale(xh, f32x2(rs[b], rs[b]));
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                xh[i] *= r;
-                if (row != kRowPad) acc[i] = fmaf(d[i], xh[i], acc[i]);
-                if (gain) d[i] *= g[i];
-                if (i < 8)
-                    s0 = fmaf(d[i], xh[i], s0);
-                else
-                    s1 = fmaf(d[i], xh[i], s1);
+            for (int j = 0; j < 4; ++j) {
+                acc.a[j] = fma_f32x2(d.a[j], xh.a[j], acc.a[j]);
+                acc.b[j] = fma_f32x2(d.b[j], xh.b[j], acc.b[j]);
             }
-            const float m = group_sum<G>(s0 + s1) / static_cast<float>(p.D);
-            if (!live || !l.in || h0 + b >= X.heads) continue;
+            if (gain) times(d, g);
+            const float m = -inv * group_sum<G>(dot(d, xh));
+            const uint64_t mm = f32x2(m, m);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) d[i] = r * (d[i] - xh[i] * m);
-            uint4 y0 = narrow8(d), y1 = narrow8(d + 8);
-            if (row == kRowPad) y0 = y1 = make_uint4(0, 0, 0, 0);
-            uint16_t *w = DX.data + t * DX.token_stride + (h0 + b) * DX.head_stride;
-            *reinterpret_cast<uint4 *>(w + l.o0) = y0;
-            *reinterpret_cast<uint4 *>(w + l.o1) = y1;
+            for (int j = 0; j < 4; ++j) {
+                d.a[j] = fma_f32x2(xh.a[j], mm, d.a[j]);
+                d.b[j] = fma_f32x2(xh.b[j], mm, d.b[j]);
+            }
+            scale(d, f32x2(rs[b], rs[b]));
+            uint4 y0, y1;
+            pack16<INTER>(d, y0, y1);
+            if (live && h0 + b < X.heads) {
+                uint16_t *w = DX.data + t * DX.token_stride + (h0 + b) * DX.head_stride;
+                *reinterpret_cast<uint4 *>(w + l.o0) = y0;
+                *reinterpret_cast<uint4 *>(w + l.o1) = y1;
+            }
+        }
+        t += dt;
+        batch += db;
+        if (batch >= batches) {
+            batch -= batches;
+            ++t;
         }
     }
     if (!p.partial) return;
     // the block's partial sum: over the groups of a warp, then over the warps in order
     __shared__ float part[kQkThreads / 32][16 * G];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int j = 0; j < 4; ++j) {
+        float v[4];  // first and second channels of pairs 2j and 2j + 1
+        split_f32x2(acc.a[j], v[0], v[1]);
+        split_f32x2(acc.b[j], v[2], v[3]);
 #pragma unroll
-        for (int o = G; o < 32; o <<= 1) acc[i] += __shfl_xor_sync(0xFFFFFFFFu, acc[i], o);
-    }
-    if ((threadIdx.x & 31) < G && l.in) {
+        for (int i = 0; i < 4; ++i) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) part[threadIdx.x / 32][(i < 8 ? l.o0 : l.o1 - 8) + i] = acc[i];
+            for (int o = G; o < 32; o <<= 1) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], o);
+        }
+        if ((threadIdx.x & 31) < G && l.in) {
+            float *to = part[threadIdx.x / 32];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int pr = 2 * j + k;  // the lane's pair
+                to[INTER ? l.o0 + 2 * pr : l.o0 + pr] = v[k];
+                to[INTER ? l.o0 + 2 * pr + 1 : l.o1 + pr] = v[2 + k];
+            }
+        }
     }
     __syncthreads();
     for (int c = threadIdx.x; c < p.D; c += kQkThreads) {
@@ -282,26 +368,27 @@ __global__ void __launch_bounds__(kQkThreads, 2) qk_norm_rope_backward_kernel(co
     }
 }
 
-// dgain = the blocks' partial sums, eight slices of them in block order and the
-// slices in order.  One block each for the queries' and the keys' gain.
+// dgain = the blocks' partial sums: 32 columns a block, 32 interleaved shares of
+// the partial sums each, then the shares in order.
 __global__ void __launch_bounds__(1024) qk_gain_kernel(const float *__restrict__ partial, int D, int q_blocks, int blocks,
                                                        float *__restrict__ dq_gain, float *__restrict__ dk_gain) {
     pdl_wait();
     pdl_launch_dependents();
-    __shared__ float part[1024];
-    const int from = blockIdx.x ? q_blocks : 0, n = blockIdx.x ? blocks - q_blocks : q_blocks;
-    float *out = blockIdx.x ? dk_gain : dq_gain;
-    const int slices = 1024 / D;
-    const int c = threadIdx.x % D, s = threadIdx.x / D;
+    __shared__ float part[32][33];
+    const int from = blockIdx.y ? q_blocks : 0, n = blockIdx.y ? blocks - q_blocks : q_blocks;
+    float *out = blockIdx.y ? dk_gain : dq_gain;
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = 32 * blockIdx.x + tx;
     float a = 0.0f;
-    if (s < slices)
-        for (int b = s; b < n; b += slices) a += partial[static_cast<int64_t>(from + b) * D + c];
-    part[threadIdx.x] = a;
-    __syncthreads();
-    if (s == 0 && out) {
-        for (int k = 1; k < slices; ++k) a += part[k * D + c];
-        out[c] = a;
+    if (c < D) {
+#pragma unroll 4
+        for (int b = ty; b < n; b += 32) a += partial[static_cast<int64_t>(from + b) * D + c];
     }
+    part[ty][tx] = a;
+    __syncthreads();
+    if (ty != 0 || c >= D || !out) return;
+#pragma unroll
+    for (int k = 1; k < 32; ++k) a += part[k][tx];
+    out[c] = a;
 }
 
 static int group_lanes(int D) { return D <= 64 ? 4 : D <= 128 ? 8 : 16; }
@@ -309,52 +396,44 @@ static int group_lanes(int D) { return D <= 64 ? 4 : D <= 128 ? 8 : 16; }
 // Blocks for the query and key heads of the backward pass; host-only, by shape
 // alone (the partial sums' order is fixed by it).
 void qk_backward_blocks(int64_t tokens, int q_heads, int k_heads, int D, int *q_blocks, int *blocks) {
-    const int64_t groups = kQkThreads / group_lanes(D);
+    const int64_t groups = kQkThreads / group_lanes(D), most = kQkBwdBlocks;
     auto need = [&](int heads) { return (tokens * ((heads + kQkBwdBatch - 1) / kQkBwdBatch) + groups - 1) / groups; };
     const int64_t nq = need(q_heads), nk = need(k_heads);
-    if (nq + nk <= kQkBwdBlocks) {
+    if (nq + nk <= most) {
         *q_blocks = static_cast<int>(nq);
         *blocks = static_cast<int>(nq + nk);
         return;
     }
-    int64_t q = k_heads == 0 ? kQkBwdBlocks : q_heads == 0 ? 0 : std::max<int64_t>(1, std::min<int64_t>(kQkBwdBlocks - 1, (kQkBwdBlocks * nq + (nq + nk) / 2) / (nq + nk)));
-    *q_blocks = static_cast<int>(q);
-    *blocks = kQkBwdBlocks;
+    const int64_t q = (most * nq + (nq + nk) / 2) / (nq + nk);
+    *q_blocks = static_cast<int>(nk == 0 ? most : nq == 0 ? 0 : std::max<int64_t>(1, std::min<int64_t>(most - 1, q)));
+    *blocks = static_cast<int>(most);
 }
 
-template <int G>
-static cudaError_t launch_fwd(const QkArgs &p, cudaStream_t s) {
-    const int64_t per = kQkThreads / G;
-    const dim3 grid(static_cast<unsigned>((p.tokens + per - 1) / per), (p.q.heads + p.k.heads + kQkFwdBatch - 1) / kQkFwdBatch);
-    return launch_pdl(p.inter ? qk_norm_rope_kernel<G, true> : qk_norm_rope_kernel<G, false>, grid, dim3(kQkThreads), 0, s, p);
-}
-
-template <int G>
-static cudaError_t launch_bwd(const QkArgs &p, int blocks, cudaStream_t s) {
-    return launch_pdl(p.inter ? qk_norm_rope_backward_kernel<G, true> : qk_norm_rope_backward_kernel<G, false>, dim3(blocks),
-                      dim3(kQkThreads), 0, s, p);
-}
+// kern<G, INTER> for the group's lanes and the kind of pairs
+#define PURO_QK_KERNEL(kern, p)                                                                      \
+    (group_lanes((p).D) == 4   ? ((p).inter ? kern<4, true> : kern<4, false>)                         \
+     : group_lanes((p).D) == 8 ? ((p).inter ? kern<8, true> : kern<8, false>)                         \
+                               : ((p).inter ? kern<16, true> : kern<16, false>))
 
 cudaError_t launch_qk_norm_rope(const QkArgs &p, cudaStream_t s) {
-    switch (group_lanes(p.D)) {
-        case 4: return launch_fwd<4>(p, s);
-        case 8: return launch_fwd<8>(p, s);
-        default: return launch_fwd<16>(p, s);
-    }
+    const int64_t per = kQkThreads / group_lanes(p.D);
+    auto batches = [](int heads) { return (heads + kQkFwdBatch - 1) / kQkFwdBatch; };
+    const int64_t grid = (p.tokens + per - 1) / per * (batches(p.q.heads) + batches(p.k.heads));
+    if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
+    return launch_pdl(PURO_QK_KERNEL(qk_norm_rope_kernel, p), dim3(static_cast<unsigned>(grid)), dim3(kQkThreads), 0, s, p);
 }
 
 cudaError_t launch_qk_norm_rope_backward(QkArgs p, float *dq_gain, float *dk_gain, cudaStream_t s) {
     int blocks = 0;
     qk_backward_blocks(p.tokens, p.q.heads, p.k.heads, p.D, &p.q_blocks, &blocks);
-    cudaError_t e = cudaSuccess;
-    if (blocks > 0) switch (group_lanes(p.D)) {
-            case 4: e = launch_bwd<4>(p, blocks, s); break;
-            case 8: e = launch_bwd<8>(p, blocks, s); break;
-            default: e = launch_bwd<16>(p, blocks, s);
-        }
-    if (e != cudaSuccess || !(dq_gain || dk_gain)) return e;
-    return launch_pdl(qk_gain_kernel, dim3(2), dim3(1024), 0, s, static_cast<const float *>(p.partial), p.D, p.q_blocks, blocks,
-                      dq_gain, dk_gain);
+    if (blocks > 0) {
+        const cudaError_t e =
+            launch_pdl(PURO_QK_KERNEL(qk_norm_rope_backward_kernel, p), dim3(blocks), dim3(kQkThreads), 0, s, p);
+        if (e != cudaSuccess) return e;
+    }
+    if (!(dq_gain || dk_gain)) return cudaSuccess;
+    return launch_pdl(qk_gain_kernel, dim3((p.D + 31) / 32, 2), dim3(1024), 0, s, static_cast<const float *>(p.partial), p.D,
+                      p.q_blocks, blocks, dq_gain, dk_gain);
 }
 
 }  // namespace puro
