@@ -202,6 +202,56 @@ def _ptr(t: Optional[torch.Tensor], dtype=None, name: str = "tensor") -> Optiona
     return t.data_ptr()
 
 
+def _sized(t: Optional[torch.Tensor], dtype, n: int, name: str) -> Optional[int]:
+    if t is not None and t.numel() != n:
+        raise ValueError(f"{name} has {t.numel()} values, expected {n}")
+    return _ptr(t, dtype, name)
+
+
+def _copies(q, scale, q_t, scale_t, rows: int, cols: int):
+    """Pointers of an FP8 copy [rows, cols] and its transpose with their scale vectors."""
+    u8 = torch.uint8
+
+    def vectors(t, r, red, name):
+        return _sized(t, u8, r * ((red // 128 + 3) // 4) * 4, name)
+
+    return (_sized(q, u8, rows * cols, "q"), vectors(scale, rows, cols, "scale"), _sized(q_t, u8, rows * cols, "q_t"),
+            vectors(scale_t, cols, rows, "scale_t"))
+
+
+def _ws(workspace: Optional[torch.Tensor]):
+    return _ptr(workspace, None, "workspace"), workspace.numel() * workspace.element_size() if workspace is not None else 0
+
+
+def _same_shape(t: torch.Tensor, like: torch.Tensor, name: str) -> None:
+    if t.shape != like.shape:
+        raise ValueError(f"{name} is {tuple(t.shape)}, expected {tuple(like.shape)}")
+
+
+def _rows_of(t: Optional[torch.Tensor], rows: int, cols: int, name: str):
+    """Pointer and row stride of an optional bf16 [rows, cols] view with unit column stride."""
+    if t is None:
+        return None, cols
+    if not t.is_cuda or t.dtype != torch.bfloat16 or tuple(t.shape) != (rows, cols):
+        raise ValueError(f"{name} must be a bf16 CUDA tensor [{rows}, {cols}]")
+    if t.numel() and t.stride(1) != 1:
+        raise ValueError(f"{name} must have unit column stride")
+    return t.data_ptr() or None, t.stride(0) if rows > 1 else cols
+
+
+def _current_device() -> int:
+    return torch.cuda.current_device()
+
+
+def _on_current_device(*tensors) -> None:
+    """Kernels are launched on the current device: every tensor has to be there.  (The native
+    module looks only whether all are on one device, so one is looked at ahead of it.)"""
+    here = _current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != here:
+            raise ValueError(f"a tensor is on cuda:{t.get_device()}, the current device is cuda:{here}")
+
+
 # --------------------------------------------------------------------------
 # Entry points (same names as the C ABI)
 # --------------------------------------------------------------------------
@@ -579,17 +629,6 @@ def puro_bf16_linear_wgrad(dy_t, x_t, dw, M, N, K, dev_status=None, stream=None)
 # --------------------------------------------------------------------------
 # Linears with an epilogue, the gated MLP's projections
 # --------------------------------------------------------------------------
-def _rows_of(t: Optional[torch.Tensor], rows: int, cols: int, name: str):
-    """Pointer and row stride of an optional bf16 [rows, cols] view with unit column stride."""
-    if t is None:
-        return None, cols
-    if not t.is_cuda or t.dtype != torch.bfloat16 or tuple(t.shape) != (rows, cols):
-        raise ValueError(f"{name} must be a bf16 CUDA tensor [{rows}, {cols}]")
-    if t.numel() and t.stride(1) != 1:
-        raise ValueError(f"{name} must have unit column stride")
-    return t.data_ptr() or None, t.stride(0) if rows > 1 else cols
-
-
 def puro_fp8_linear_fprop_epilogue(x: FP8Operand, w: FP8Operand, y: torch.Tensor, bias: Optional[torch.Tensor] = None,
                                    act: int = ACT_NONE, residual: Optional[torch.Tensor] = None,
                                    z: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
@@ -598,11 +637,12 @@ def puro_fp8_linear_fprop_epilogue(x: FP8Operand, w: FP8Operand, y: torch.Tensor
     the product in the GEMM's epilogue.  bias bf16 [N]; residual bf16 [M,N]
     (rows may be strided; it may be y); z, when given, receives Z (bf16 [M,N])
     for the backward."""
-    _on_current_device(x.data, w.data, y, bias, residual, z, workspace, dev_status)
+    _on_current_device(x.data)
     st = (_native or _load_native()).puro_fp8_linear_fprop_epilogue(x, w, y, bias, act, residual, z, workspace, dev_status,
                                                                     stream)
     if st is not None:
         return _check("puro_fp8_linear_fprop_epilogue", st)
+    _on_current_device(x.data, w.data, y, bias, residual, z, workspace, dev_status)
     cx, cw = x.as_c(), w.as_c()
     m, n, bf16 = cx.rows, cw.rows, torch.bfloat16
     res, ld = _rows_of(residual, m, n, "residual")
@@ -617,10 +657,11 @@ def puro_bf16_linear_fprop_epilogue(x: torch.Tensor, w: torch.Tensor, y: torch.T
                                     residual: Optional[torch.Tensor] = None, z: Optional[torch.Tensor] = None,
                                     dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
     """The same from BF16 x [M,K] and w [N,K]; any M, from a single token on."""
-    _on_current_device(x, w, y, bias, residual, z, dev_status)
+    _on_current_device(x)
     st = (_native or _load_native()).puro_bf16_linear_fprop_epilogue(x, w, y, bias, act, residual, z, dev_status, stream)
     if st is not None:
         return _check("puro_bf16_linear_fprop_epilogue", st)
+    _on_current_device(x, w, y, bias, residual, z, dev_status)
     (m, k), n, bf16 = x.shape, w.shape[0], torch.bfloat16
     res, ld = _rows_of(residual, m, n, "residual")
     st = load_library().puro_bf16_linear_fprop_epilogue(
@@ -639,27 +680,28 @@ def puro_fp8_gated_fprop(x: FP8Operand, w: FP8Operand, act: int, fmt: int, gate_
     operand.  h is written as the FP8 copies that puro_fp8_quantize makes of
     it; gate_up (bf16 [M,2F], for the backward) and h (bf16 [M,F]) only when
     given."""
-    _on_current_device(x.data, w.data, gate_up, h, hq, hq_scale, hq_t, hq_t_scale, dev_status)
+    _on_current_device(x.data)
     st = (_native or _load_native()).puro_fp8_gated_fprop(x, w, act, fmt, gate_up, h, hq, hq_scale, hq_t, hq_t_scale,
                                                           dev_status, stream)
     if st is not None:
         return _check("puro_fp8_gated_fprop", st)
+    _on_current_device(x.data, w.data, gate_up, h, hq, hq_scale, hq_t, hq_t_scale, dev_status)
     cx, cw = x.as_c(), w.as_c()
-    n, u8, bf16 = cx.rows * (cw.rows // 2), torch.uint8, torch.bfloat16
+    n, bf16 = cx.rows * (cw.rows // 2), torch.bfloat16
     st = load_library().puro_fp8_gated_fprop(
         ctypes.byref(cx), ctypes.byref(cw), act, fmt, _sized(gate_up, bf16, cx.rows * cw.rows, "gate_up"),
-        _sized(h, bf16, n, "h"), _sized(hq, u8, n, "hq"), _ptr(hq_scale, u8, "hq_scale"), _sized(hq_t, u8, n, "hq_t"),
-        _ptr(hq_t_scale, u8, "hq_t_scale"), _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
+        _sized(h, bf16, n, "h"), *_copies(hq, hq_scale, hq_t, hq_t_scale, cx.rows, cw.rows // 2), _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
     _check("puro_fp8_gated_fprop", st)
 
 
 def puro_bf16_gated_fprop(x: torch.Tensor, w: torch.Tensor, act: int, gate_up: Optional[torch.Tensor], h: torch.Tensor,
                           dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
     """The same from BF16 x [M,K] and w [2F,K], h in BF16; any M, from a single token on."""
-    _on_current_device(x, w, gate_up, h, dev_status)
+    _on_current_device(x)
     st = (_native or _load_native()).puro_bf16_gated_fprop(x, w, act, gate_up, h, dev_status, stream)
     if st is not None:
         return _check("puro_bf16_gated_fprop", st)
+    _on_current_device(x, w, gate_up, h, dev_status)
     (m, k), n, bf16 = x.shape, w.shape[0], torch.bfloat16
     if n % 2:
         raise ValueError("w must hold the gate's and up's rows, as many of each")
@@ -676,10 +718,6 @@ def puro_act_backward_workspace_size(rows: int, cols: int) -> int:
     return int(load_library().puro_act_backward_workspace_size(rows, cols))
 
 
-def _ws(workspace: Optional[torch.Tensor]):
-    return _ptr(workspace, None, "workspace"), workspace.numel() * workspace.element_size() if workspace is not None else 0
-
-
 def puro_fp8_quantize_act_backward(dy: torch.Tensor, z: Optional[torch.Tensor], act: int, fmt: int,
                                    dz: Optional[torch.Tensor], dbias: Optional[torch.Tensor],
                                    workspace: Optional[torch.Tensor], q: torch.Tensor, scale: torch.Tensor,
@@ -689,27 +727,29 @@ def puro_fp8_quantize_act_backward(dy: torch.Tensor, z: Optional[torch.Tensor], 
     that puro_fp8_quantize makes of it, dbias (fp32 [cols]) its sum over the
     rows, through a workspace of puro_act_backward_workspace_size bytes; dz
     (bf16) is written only when given."""
-    _on_current_device(dy, z, dz, dbias, workspace, q, scale, q_t, scale_t, dev_status)
+    _on_current_device(dy)
     st = (_native or _load_native()).puro_fp8_quantize_act_backward(dy, z, act, fmt, dz, dbias, workspace, q, scale, q_t,
                                                                     scale_t, dev_status, stream)
     if st is not None:
         return _check("puro_fp8_quantize_act_backward", st)
+    _on_current_device(dy, z, dz, dbias, workspace, q, scale, q_t, scale_t, dev_status)
     rows, cols = dy.shape
-    n, u8, bf16 = rows * cols, torch.uint8, torch.bfloat16
+    n, bf16 = rows * cols, torch.bfloat16
     st = load_library().puro_fp8_quantize_act_backward(
         _ptr(dy, bf16, "dy"), _sized(z, bf16, n, "z"), rows, cols, act, fmt, _sized(dz, bf16, n, "dz"),
-        _sized(dbias, torch.float32, cols, "dbias"), *_ws(workspace), _sized(q, u8, n, "q"), _ptr(scale, u8, "scale"),
-        _sized(q_t, u8, n, "q_t"), _ptr(scale_t, u8, "scale_t"), _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
+        _sized(dbias, torch.float32, cols, "dbias"), *_ws(workspace), *_copies(q, scale, q_t, scale_t, rows, cols),
+        _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
     _check("puro_fp8_quantize_act_backward", st)
 
 
 def puro_act_backward_bf16(dy: torch.Tensor, z: Optional[torch.Tensor], act: int, dz: Optional[torch.Tensor],
                            dbias: Optional[torch.Tensor], workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """The same without the quantiser: dz (bf16, may be dy) and dbias, each only when given."""
-    _on_current_device(dy, z, dz, dbias, workspace)
+    _on_current_device(dy)
     st = (_native or _load_native()).puro_act_backward_bf16(dy, z, act, dz, dbias, workspace, stream)
     if st is not None:
         return _check("puro_act_backward_bf16", st)
+    _on_current_device(dy, z, dz, dbias, workspace)
     rows, cols = dy.shape
     n, bf16 = rows * cols, torch.bfloat16
     st = load_library().puro_act_backward_bf16(
@@ -726,33 +766,29 @@ def puro_fp8_quantize_gated_backward(dh: torch.Tensor, gate: torch.Tensor, up: t
     cols]) as the FP8 copies that puro_fp8_quantize makes of it: the output
     gradient of the fused gate/up linear, whose output gate and up are views
     of.  dgate_up (bf16) is written only when given."""
-    _on_current_device(dh, gate, up, dgate_up, q, scale, q_t, scale_t, dev_status)
+    _on_current_device(dh)
     st = (_native or _load_native()).puro_fp8_quantize_gated_backward(dh, gate, up, act, fmt, dgate_up, q, scale, q_t, scale_t,
                                                                       dev_status, stream)
     if st is not None:
         return _check("puro_fp8_quantize_gated_backward", st)
+    _on_current_device(dh, gate, up, dgate_up, q, scale, q_t, scale_t, dev_status)
     g, u, rows, cols, ld = _gate_up(gate, up)
-    n, u8, bf16 = 2 * rows * cols, torch.uint8, torch.bfloat16
+    n, bf16 = 2 * rows * cols, torch.bfloat16
     _same_shape(dh, gate, "dh")
     st = load_library().puro_fp8_quantize_gated_backward(
-        _ptr(dh, bf16, "dh"), g, u, rows, cols, ld, act, fmt, _sized(dgate_up, bf16, n, "dgate_up"), _sized(q, u8, n, "q"),
-        _ptr(scale, u8, "scale"), _sized(q_t, u8, n, "q_t"), _ptr(scale_t, u8, "scale_t"),
-        _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
+        _ptr(dh, bf16, "dh"), g, u, rows, cols, ld, act, fmt, _sized(dgate_up, bf16, n, "dgate_up"),
+        *_copies(q, scale, q_t, scale_t, rows, 2 * cols), _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
     _check("puro_fp8_quantize_gated_backward", st)
-
-
-def _same_shape(t: torch.Tensor, like: torch.Tensor, name: str) -> None:
-    if t.shape != like.shape:
-        raise ValueError(f"{name} is {tuple(t.shape)}, expected {tuple(like.shape)}")
 
 
 def puro_gated_backward_bf16(dh: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, act: int, dgate_up: torch.Tensor,
                              stream=None) -> None:
     """The same without the quantiser."""
-    _on_current_device(dh, gate, up, dgate_up)
+    _on_current_device(dh)
     st = (_native or _load_native()).puro_gated_backward_bf16(dh, gate, up, act, dgate_up, stream)
     if st is not None:
         return _check("puro_gated_backward_bf16", st)
+    _on_current_device(dh, gate, up, dgate_up)
     g, u, rows, cols, ld = _gate_up(gate, up)
     _same_shape(dh, gate, "dh")
     st = load_library().puro_gated_backward_bf16(_ptr(dh, torch.bfloat16, "dh"), g, u, rows, cols, ld, act,
@@ -764,18 +800,6 @@ def puro_gated_backward_bf16(dh: torch.Tensor, gate: torch.Tensor, up: torch.Ten
 # --------------------------------------------------------------------------
 # Query and key norms with the position rotation
 # --------------------------------------------------------------------------
-def _current_device() -> int:
-    return torch.cuda.current_device()
-
-
-def _on_current_device(*tensors) -> None:
-    """Kernels are launched on the current device: every tensor has to be there."""
-    here = _current_device()
-    for t in tensors:
-        if t is not None and t.is_cuda and t.get_device() != here:
-            raise ValueError(f"a tensor is on cuda:{t.get_device()}, the current device is cuda:{here}")
-
-
 class puro_heads_t(ctypes.Structure):
     """Mirror of the C struct puro_heads_t."""
     _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
@@ -794,12 +818,6 @@ def _heads(t: Optional[torch.Tensor], name: str, tokens: int, channels: int):
         raise ValueError(f"{name} must have unit channel stride")
     return puro_heads_t(t.data_ptr() or None, t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0,
                         t.shape[1], 0)
-
-
-def _sized(t: Optional[torch.Tensor], dtype, n: int, name: str) -> Optional[int]:
-    if t is not None and t.numel() != n:
-        raise ValueError(f"{name} has {t.numel()} values, expected {n}")
-    return _ptr(t, dtype, name)
 
 
 def _tables(cos, sin):
@@ -822,11 +840,12 @@ def puro_qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], q_ga
     be q and k) and rstd (fp32 [tokens, q heads + k heads]) for the backward.
     positions: int32 [tokens], None for 0, 1, ...; a negative one marks a
     padding row, whose output is zero."""
-    _on_current_device(q, k, q_gain, k_gain, cos, sin, positions, q_out, k_out, rstd, dev_status)
+    _on_current_device(q if q is not None else k)
     st = (_native or _load_native()).puro_qk_norm_rope(q, k, q_gain, k_gain, eps, cos, sin, positions, interleaved, q_out,
                                                        k_out, rstd, dev_status, stream)
     if st is not None:
         return _check("puro_qk_norm_rope", st)
+    _on_current_device(q, k, q_gain, k_gain, cos, sin, positions, q_out, k_out, rstd, dev_status)
     some = q if q is not None else k
     if some is None or some.dim() != 3:
         raise ValueError("q or k must be a bf16 CUDA tensor [tokens, heads, head_dim]")
@@ -854,13 +873,14 @@ def puro_qk_norm_rope_backward(dq_out: Optional[torch.Tensor], dk_out: Optional[
     inputs and rstd: dq, dk (bf16 views, which may be dq_out and dk_out) and the
     gains' gradients (fp32 [head_dim], through a workspace of
     puro_qk_norm_rope_workspace_size bytes)."""
-    _on_current_device(dq_out, dk_out, q, k, rstd, q_gain, k_gain, cos, sin, positions, dq, dk, dq_gain, dk_gain, workspace,
-                       dev_status)
+    _on_current_device(q if q is not None else k)
     st = (_native or _load_native()).puro_qk_norm_rope_backward(dq_out, dk_out, q, k, rstd, q_gain, k_gain, cos, sin,
                                                                 positions, interleaved, dq, dk, dq_gain, dk_gain, workspace,
                                                                 dev_status, stream)
     if st is not None:
         return _check("puro_qk_norm_rope_backward", st)
+    _on_current_device(dq_out, dk_out, q, k, rstd, q_gain, k_gain, cos, sin, positions, dq, dk, dq_gain, dk_gain,
+                       workspace, dev_status)
     some = q if q is not None else k
     if some is None or some.dim() != 3:
         raise ValueError("q or k must be a bf16 CUDA tensor [tokens, heads, head_dim]")

@@ -64,12 +64,20 @@ bool have_library = false;
 struct Args {
     PyObject *const *v;
     bool ok = true;
+    int device = -1;     // of the first tensor
+    bool mixed = false;  // another one's differs
 
     const at::Tensor *plain(PyObject *o) {
         if (!THPVariable_CheckExact(o)) return nullptr;
         const at::Tensor &t = THPVariable_Unpack(o);
         if (!t.defined() || !t.has_storage() || !t.is_cuda() || t.numel() == 0) return nullptr;
+        if (device < 0) device = t.get_device();
+        if (t.get_device() != device) mixed = true;
         return &t;
+    }
+    // Every tensor so far has to be on one device (the caller has compared the first with the current one).
+    void one_device() {
+        if (mixed) ok = false;
     }
     // Device pointer of a contiguous tensor of dtype dt or dt2.
     void *ptr_of(PyObject *o, at::ScalarType dt, at::ScalarType dt2) {
@@ -221,6 +229,11 @@ struct Args {
             return fail();
         if (rows > 1) *ld = t->stride(0);
         return t->data_ptr();
+    }
+    // The scale vectors of an FP8 copy [rows, red] and (optional) of its transpose.
+    void scales(int i, int it, int64_t rows, int64_t red) {
+        numel(i, rows * ((red / 128 + 3) / 4) * 4);
+        numel(it, red * ((rows / 128 + 3) / 4) * 4);
     }
     // A tensor's number of values has to be n.
     void numel(int i, int64_t n) {
@@ -426,6 +439,7 @@ PyObject *linear_fprop_epilogue_call(Args &a) {
     void *s = a.stream(9);
     for (int i : {2, 6}) a.numel(i, x.rows * w.rows);
     a.numel(3, w.rows);
+    a.one_device();
     return finish(a, [&] { return lib.puro_fp8_linear_fprop_epilogue(&x, &w, bias, act, res, ld, z, y, ws, bytes, st, s); });
 }
 PURO_NATIVE(linear_fprop_epilogue, 10)
@@ -444,6 +458,7 @@ PyObject *bf16_fprop_epilogue_call(Args &a) {
     void *s = a.stream(8);
     for (int i : {2, 6}) a.numel(i, M * N);
     a.numel(3, N);
+    a.one_device();
     return finish(a, [&] { return lib.puro_bf16_linear_fprop_epilogue(x, w, M, N, K, bias, act, res, ld, z, y, st, s); });
 }
 PURO_NATIVE(bf16_fprop_epilogue, 9)
@@ -460,6 +475,8 @@ PyObject *gated_fprop_call(Args &a) {
     void *s = a.stream(11);
     a.numel(4, x.rows * w.rows);
     for (int i : {5, 6, 8}) a.numel(i, x.rows * (w.rows / 2));
+    a.scales(7, 9, x.rows, w.rows / 2);
+    a.one_device();
     return finish(a, [&] { return lib.puro_fp8_gated_fprop(&x, &w, act, fmt, gu, h, q, sc, qt, sct, st, s); });
 }
 PURO_NATIVE(gated_fprop, 12)
@@ -477,6 +494,7 @@ PyObject *bf16_gated_fprop_call(Args &a) {
     void *s = a.stream(6);
     a.numel(3, M * N);
     a.numel(4, M * (N / 2));
+    a.one_device();
     return finish(a, [&] { return lib.puro_bf16_gated_fprop(x, w, M, N / 2, K, act, gu, h, st, s); });
 }
 PURO_NATIVE(bf16_gated_fprop, 7)
@@ -497,6 +515,8 @@ PyObject *quantize_act_backward_call(Args &a) {
     void *s = a.stream(12);
     for (int i : {1, 4, 7, 9}) a.numel(i, r * c);
     a.numel(5, c);
+    a.scales(8, 10, r, c);
+    a.one_device();
     return finish(a, [&] {
         return lib.puro_fp8_quantize_act_backward(dy, z, r, c, act, fmt, dz, db, ws, bytes, q, sc, qt, sct, st, s);
     });
@@ -516,6 +536,7 @@ PyObject *act_backward_bf16_call(Args &a) {
     void *s = a.stream(6);
     for (int i : {1, 3}) a.numel(i, r * c);
     a.numel(4, c);
+    a.one_device();
     return finish(a, [&] { return lib.puro_act_backward_bf16(dy, z, r, c, act, dz, db, ws, bytes, s); });
 }
 PURO_NATIVE(act_backward_bf16, 7)
@@ -533,6 +554,8 @@ PyObject *quantize_gated_backward_call(Args &a) {
     int32_t *st = a.status(10);
     void *s = a.stream(11);
     for (int i : {5, 6, 8}) a.numel(i, 2 * r * c);
+    a.scales(7, 9, r, 2 * c);
+    a.one_device();
     return finish(a, [&] {
         return lib.puro_fp8_quantize_gated_backward(dh, g, u, r, c, ld, act, fmt, dgu, q, sc, qt, sct, st, s);
     });
@@ -550,6 +573,7 @@ PyObject *gated_backward_bf16_call(Args &a) {
     void *dgu = a.ptr(4, kBF16);
     void *s = a.stream(5);
     a.numel(4, 2 * r * c);
+    a.one_device();
     return finish(a, [&] { return lib.puro_gated_backward_bf16(dh, g, u, r, c, ld, act, dgu, s); });
 }
 PURO_NATIVE(gated_backward_bf16, 6)
@@ -580,6 +604,7 @@ PyObject *qk_norm_rope_call(Args &a) {
     a.numel(7, t[0]);
     a.numel(11, t[0] * (q.heads + k.heads));
     if (d[0] > 1024) a.ok = false;
+    a.one_device();
     return finish(a, [&] {
         return lib.puro_qk_norm_rope(&q, &k, t[0], static_cast<int32_t>(d[0]), gq, gk, eps, co, si, positions, rot, inter, pos,
                                      &qo, &ko, rstd, st, s);
@@ -612,6 +637,7 @@ PyObject *qk_norm_rope_backward_call(Args &a) {
     for (int i : {5, 6, 13, 14}) a.numel(i, d[0]);
     a.numel(9, t[0]);
     if (d[0] > 1024) a.ok = false;
+    a.one_device();
     return finish(a, [&] {
         return lib.puro_qk_norm_rope_backward(&h[0], &h[1], &h[2], &h[3], rstd, t[0], static_cast<int32_t>(d[0]), gq, gk, co,
                                               si, positions, rot, inter, pos, &h[4], &h[5], dgq, dgk, ws, bytes, st, s);
