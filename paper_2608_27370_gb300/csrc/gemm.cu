@@ -614,21 +614,20 @@ PURO_DEV void act32(float (&f)[32], int act) {
     });
 }
 
-// f += the lane's row of the residual at the 32 columns from col0, loaded as
-// store_rows32 stores and handed on through the same staging.  (The output may be
-// the residual itself.)
-PURO_DEV void add_residual32(float (&f)[32], uint8_t *stage, const GemmEpilogue &epi, int row0, int col0, int rows,
-                             int cols, int lane) {
-    if (!epi.residual) return;
+// 32 columns of the warp's rows of the residual, as store_rows32 stores them;
+// zeros past the last row or column.  (The output may be the residual itself.)
+PURO_DEV void load_residual32(uint4 (&v)[4], const GemmEpilogue &epi, int row0, int col0, int rows, int cols, int lane) {
     const int col = col0 + 8 * (lane & 3), row = row0 + (lane >> 2);
-    const uint8_t *mine = stage + 64 * (lane & 15);
-    uint8_t *theirs = stage + 64 * (lane >> 2) + 16 * ((lane & 3) ^ ((lane >> 3) & 3));
     const uint16_t *from = epi.residual + row * epi.ld_residual + col;
-    uint4 v[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k)
         v[k] = row + 8 * k < rows && col < cols ? *reinterpret_cast<const uint4 *>(from + 8 * k * epi.ld_residual)
                                                 : make_uint4(0u, 0u, 0u, 0u);
+}
+// f += them, handed to the lanes that hold the rows through the staging.
+PURO_DEV void add_residual32(float (&f)[32], const uint4 (&v)[4], uint8_t *stage, int lane) {
+    const uint8_t *mine = stage + 64 * (lane & 15);
+    uint8_t *theirs = stage + 64 * (lane >> 2) + 16 * ((lane & 3) ^ ((lane >> 3) & 3));
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
 #pragma unroll
@@ -680,6 +679,7 @@ PURO_DEV void wide_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int wa
         const WorkUnit wu = work_unit<BN>(p, u);
         const int row0 = wu.m0 + kBM * rank + 32 * q;
         const int buf = local % kAccBufs;
+        uint4 res[4];  // the residual's next 32 columns
         if constexpr (OUT == kGemmOutEpilogue) {  // while the tile is computed
             const int nq = wu.n0 + 64 * j;
             if (p.epi.bias) {
@@ -695,6 +695,7 @@ PURO_DEV void wide_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int wa
                     const int row = w.m0 + kBM * rank + 32 * q + lane, col = w.n0 + 64 * j;
                     if (row < p.M && col < p.N) prefetch_l2(p.epi.residual + row * p.epi.ld_residual + col);
                 }
+            if (p.epi.residual) load_residual32(res, p.epi, row0, nq, p.M, p.N, lane);
         }
         bool ok = (sm.abort_flag == 0) &&
                   mbar_wait_bounded(&sm.tfull[buf], static_cast<uint32_t>(local / kAccBufs) & 1u, p.wait_ns);
@@ -740,7 +741,10 @@ PURO_DEV void wide_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int wa
                 if (p.epi.bias) add_bias32(f[c], reinterpret_cast<const uint4 *>(sm.qe.bias[warp - 4]) + 4 * c);
                 if (p.epi.z) store_rows32(f[c], stage, p.epi.z, p.N, row0, col0, p.M, p.N, lane);
                 act32(f[c], p.epi.act);
-                add_residual32(f[c], stage, p.epi, row0, col0, p.M, p.N, lane);
+                if (p.epi.residual) {
+                    add_residual32(f[c], res, stage, lane);
+                    if (c == 0) load_residual32(res, p.epi, row0, nq + 32, p.M, p.N, lane);
+                }
                 store_rows32(f[c], stage, p.epi.y, p.N, row0, col0, p.M, p.N, lane);
             }
         }
@@ -903,6 +907,15 @@ template <int OUT, int BN, int S = 1>
 constexpr int gemm_threads() {
     return OUT == kGemmOutQuant ? kThreads + 384 : wide_epilogue_form<OUT, BN, S>() ? 128 + BN / 64 * 128 : kThreads;
 }
+// Registers: sixteen epilogue warps of a 640-thread block get 96 each at launch,
+// some short of what they hold (64 accumulators, the residual, addresses).  The
+// four warps ahead of them need few and give theirs up: 4 * 56 + 16 * 104 = 1888
+// a lane, of the 20 * 96 = 1920 that the block was launched with (launch_params
+// looks that it was: an increase beyond them would wait for ever).
+constexpr int kFewRegs = 56, kManyRegs = 104;
+template <int OUT, int BN, int S = 1>
+constexpr bool register_split() { return wide_epilogue_form<OUT, BN, S>() && BN == 256; }
+
 // Shared memory of the form's epilogue, beside the staging.
 template <int OUT, int S = 1>
 using EpiSmemOf = std::conditional_t<
@@ -934,6 +947,7 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
     constexpr bool OUT_Q = (OUT == kGemmOutQuant);
     constexpr bool kWide = wide_epilogue_form<OUT, BN, S>();
     constexpr bool kGated = OUT == kGemmOutGated || OUT == kGemmOutGatedQuant;
+    constexpr bool kRegSplit = register_split<OUT, BN, S>();
     // The narrow forms run few tiles a launch: their epilogue arrives at the
     // closing cluster barrier ahead of its last stores (which costs the
     // 256-wide form 0.5%).
@@ -1070,6 +1084,19 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
         left = true;
     };
 
+    if (kWide && warp >= 4) {
+        // ------------------------------------------------ epilogue that computes (both CTAs)
+        if constexpr (kRegSplit) reg_inc<kManyRegs>();
+        if constexpr (OUT == kGemmOutGatedQuant) {
+            if (p.q_fmt == 0)
+                gated_quant_epilogue<0>(sm, p, tmem, warp, lane, pair, num_pairs, static_cast<int>(rank));
+            else
+                gated_quant_epilogue<1>(sm, p, tmem, warp, lane, pair, num_pairs, static_cast<int>(rank));
+        } else if constexpr (kWide) {
+            wide_epilogue<KIND, OUT, BN, kShifted>(sm, p, tmem, warp, lane, pair, num_pairs, static_cast<int>(rank));
+        }
+    } else {
+    if constexpr (kRegSplit) reg_dec<kFewRegs>();
     if (warp == 0) {
         // ------------------------------------------------ TMA producer
         // (the whole warp, as the MMA issuer: see there)
@@ -1283,16 +1310,6 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
             else
                 quant_epilogue<1>(sm, p, tmem, warp, lane, pair, num_pairs, static_cast<int>(rank));
         }
-    } else if constexpr (OUT == kGemmOutGatedQuant) {
-        if (warp >= 4) {
-            if (p.q_fmt == 0)
-                gated_quant_epilogue<0>(sm, p, tmem, warp, lane, pair, num_pairs, static_cast<int>(rank));
-            else
-                gated_quant_epilogue<1>(sm, p, tmem, warp, lane, pair, num_pairs, static_cast<int>(rank));
-        }
-    } else if constexpr (kWide) {
-        if (warp >= 4)
-            wide_epilogue<KIND, OUT, BN, kShifted>(sm, p, tmem, warp, lane, pair, num_pairs, static_cast<int>(rank));
     } else if (warp >= 4) {
         // ------------------------------------------------ epilogue (both CTAs)
         const int q = warp & 3;  // TMEM lane quarter of this warp
@@ -1404,7 +1421,11 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
                         }
                         if (p.epi.z) store_rows32(a, stage_buf, p.epi.z, n_out, m0 + 32 * q, col, p.M, n_out, lane);
                         act32(a, p.epi.act);
-                        add_residual32(a, stage_buf, p.epi, m0 + 32 * q, col, p.M, n_out, lane);
+                        if (p.epi.residual) {
+                            uint4 res[4];
+                            load_residual32(res, p.epi, m0 + 32 * q, col, p.M, n_out, lane);
+                            add_residual32(a, res, stage_buf, lane);
+                        }
                         store_rows32(a, stage_buf, p.epi.y, n_out, m0 + 32 * q, col, p.M, n_out, lane);
                         continue;
                     }
@@ -1537,6 +1558,7 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
         }
         if (e) bulk_wait_group0();
         __syncwarp();
+    }
     }
 
     // The pair's MMAs into both CTAs' tensor memory are complete and read
@@ -1865,6 +1887,13 @@ static cudaError_t launch_params(const GemmParams &p, const GemmArgs &g, const G
     const size_t smem = sizeof(GemmSmem<BN, EpiSmemOf<OUT>>) + 1024;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
+    if constexpr (register_split<OUT, BN>()) {
+        static const bool enough = [&] {
+            cudaFuncAttributes at{};
+            return cudaFuncGetAttributes(&at, kern) == cudaSuccess && at.numRegs * 20 >= 4 * kFewRegs + 16 * kManyRegs;
+        }();
+        if (!enough) return cudaErrorLaunchOutOfResources;
+    }
     const int pairs_max = max_resident_pairs<KIND, OUT, BN>(g.num_sms, smem);
     const int pairs = p.num_units < pairs_max ? p.num_units : pairs_max;
     return launch_pdl(kern, dim3(2 * pairs), dim3(gemm_threads<OUT, BN>()), smem, s, m.a, m.b,

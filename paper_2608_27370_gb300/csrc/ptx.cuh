@@ -66,6 +66,15 @@ PURO_DEV bool named_bar_and(uint32_t id, uint32_t threads, bool pred) {
     return r != 0;
 }
 
+// ------------------------------------------------ registers of a warpgroup
+// Every warp of a warpgroup (four warps) runs one of these: N registers a thread
+// from here on, the rest given back to the block, or taken from what others of
+// the block gave back (waiting until they have).
+template <int N>
+PURO_DEV void reg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+PURO_DEV void reg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+
 // ---------------------------------------------------------------- mbarrier
 PURO_DEV void mbar_init(uint64_t *bar, uint32_t count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count) : "memory");
