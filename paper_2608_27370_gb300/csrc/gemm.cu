@@ -98,8 +98,8 @@ struct QuantEpiSmem {
 // rows (q): the maxima of a tile and the next one's, so that a warp may be a
 // tile ahead of those it exchanged them with, and each warp's multipliers.
 struct GatedEpiSmem {
-    uint32_t rowmax[2][4][4][32];      // [tile's parity][q][j][lane]
-    uint32_t colmax[2][4][4][16];      // [tile's parity][j][q][column pair]
+    uint32_t rowmax[2][4][4][32];      // [quantised tile's parity][q][j][lane]
+    uint32_t colmax[2][4][4][16];      // [quantised tile's parity][j][q][column pair]
     alignas(16) float colmul[16][32];  // [warp][column]
 };
 // kGemmOutEpilogue: the 64 columns of bias of each epilogue warp's quarter, in BF16.
@@ -546,27 +546,54 @@ PURO_DEV void quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int w
 // warps: warp 4 + 4j + q takes column quarter j of the tile and the rows of
 // tensor-memory lane quarter q, one per lane.  Four warps a scheduler keep the
 // special-function chains of the activations overlapped.  Everything they read
-// (bias, residual) comes straight from global memory; what they write in BF16
-// leaves by plain stores of whole 64-byte row segments (store_rows32), so rows
-// and columns may end anywhere (columns at a multiple of eight).
+// (bias, residual) comes straight from global memory, what they write in BF16
+// leaves by plain stores (store_rows32), so rows and columns may end anywhere
+// (columns at a multiple of eight).  us, rotating operands, [8192, 2048] x 6144
+// block-scaled: the plain GEMM 61.7, this epilogue alone 63.5, with bias 64.0, SiLU
+// 64.6, GELU 68.2, a residual (33 MB more) 67.1; [32768, 2048] x 1536 77-79, 80, 82, 81,
+// 96, 103.
 template <int OUT, int BN, int S>
 constexpr bool wide_epilogue_form() {
     return S == 1 && (OUT == kGemmOutEpilogue || OUT == kGemmOutGated || OUT == kGemmOutGatedQuant);
 }
 
+// 32 bytes of one lane (PTX: 256-bit accesses of sm_100 on; 32-byte aligned).
+PURO_DEV void store_v8(void *p, const uint32_t *v) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+                 "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+
+PURO_DEV void load_v8(const void *p, uint4 &a, uint4 &b) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w)
+                 : "l"(p)
+                 : "memory");
+}
+
 // 32 values of each lane's row, rounded to BF16, to out[row, col0 .. col0 + 31]
-// (rows ld elements apart), rows below `rows` and columns below `cols` only.
-// Sixteen rows at a time go through the warp's kilobyte of staging (64-byte rows,
-// 16-byte chunk c of row r at c ^ (r / 2) % 4), so that a store writes eight
-// whole 64-byte pieces.
+// (rows ld elements apart), rows below `rows` and columns below `cols` only.  Two
+// 32-byte stores a lane, whole sectors, where the rows are aligned for them ([8192,
+// 8960] x 1536 with gelu and z 125 -> 99 us).  Otherwise sixteen rows at a time go
+// through the warp's kilobyte of staging (64-byte rows, 16-byte chunk c of row r at
+// c ^ (r / 2) % 4), so that a store writes eight 64-byte pieces.
 constexpr int kRowStage = 1024;
-PURO_DEV void store_rows32(const float (&f)[32], uint8_t *stage, uint16_t *out, int64_t ld, int row0, int col0,
-                           int rows, int cols, int lane) {
-    uint32_t x[16];
+PURO_DEV void round32(const float (&f)[32], uint32_t (&x)[16]) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
         x[i] = *reinterpret_cast<uint32_t *>(&b);
+    }
+}
+PURO_DEV void store_rows32(const uint32_t (&x)[16], uint8_t *stage, uint16_t *out, int64_t ld, int row0, int col0,
+                           int rows, int cols, int lane) {
+    if (((reinterpret_cast<uintptr_t>(out) | static_cast<uintptr_t>(2 * ld)) & 31u) == 0 && col0 + 32 <= cols) {
+        if (row0 + lane < rows) {
+            uint16_t *to = out + static_cast<int64_t>(row0 + lane) * ld + col0;
+            store_v8(to, &x[0]);
+            store_v8(to + 16, &x[8]);
+        }
+        return;
     }
     const int col = col0 + 8 * (lane & 3);
     uint8_t *mine = stage + 64 * (lane & 15);
@@ -589,6 +616,13 @@ PURO_DEV void store_rows32(const float (&f)[32], uint8_t *stage, uint16_t *out, 
         }
         __syncwarp();
     }
+}
+
+PURO_DEV void store_rows32(const float (&f)[32], uint8_t *stage, uint16_t *out, int64_t ld, int row0, int col0,
+                           int rows, int cols, int lane) {
+    uint32_t x[16];
+    round32(f, x);
+    store_rows32(x, stage, out, ld, row0, col0, rows, cols, lane);
 }
 
 PURO_DEV void add8(float *f, const uint4 &w) {
@@ -614,9 +648,24 @@ PURO_DEV void act32(float (&f)[32], int act) {
     });
 }
 
-// 32 columns of the warp's rows of the residual, as store_rows32 stores them;
-// zeros past the last row or column.  (The output may be the residual itself.)
+// 32 columns of the lane's row of the residual (direct: where 32-byte loads are
+// aligned), or of the warp's rows as store_rows32 stores them; zeros past the last
+// row or column.  (The output may be the residual itself.)
+PURO_DEV bool residual_direct(const GemmEpilogue &epi, int col0, int cols) {
+    return ((reinterpret_cast<uintptr_t>(epi.residual) | static_cast<uintptr_t>(2 * epi.ld_residual)) & 31u) == 0 &&
+           col0 + 32 <= cols;
+}
 PURO_DEV void load_residual32(uint4 (&v)[4], const GemmEpilogue &epi, int row0, int col0, int rows, int cols, int lane) {
+    if (residual_direct(epi, col0, cols)) {
+        const uint16_t *from = epi.residual + (row0 + lane) * epi.ld_residual + col0;
+        const bool in = row0 + lane < rows;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            v[2 * k] = v[2 * k + 1] = make_uint4(0u, 0u, 0u, 0u);
+            if (in) load_v8(from + 16 * k, v[2 * k], v[2 * k + 1]);
+        }
+        return;
+    }
     const int col = col0 + 8 * (lane & 3), row = row0 + (lane >> 2);
     const uint16_t *from = epi.residual + row * epi.ld_residual + col;
 #pragma unroll
@@ -625,7 +674,11 @@ PURO_DEV void load_residual32(uint4 (&v)[4], const GemmEpilogue &epi, int row0, 
                                                 : make_uint4(0u, 0u, 0u, 0u);
 }
 // f += them, handed to the lanes that hold the rows through the staging.
-PURO_DEV void add_residual32(float (&f)[32], const uint4 (&v)[4], uint8_t *stage, int lane) {
+PURO_DEV void add_residual32(float (&f)[32], const uint4 (&v)[4], bool direct, uint8_t *stage, int lane) {
+    if (direct) {
+        add_bias32(f, v);
+        return;
+    }
     const uint8_t *mine = stage + 64 * (lane & 15);
     uint8_t *theirs = stage + 64 * (lane >> 2) + 16 * ((lane & 3) ^ ((lane >> 3) & 3));
 #pragma unroll
@@ -742,7 +795,7 @@ PURO_DEV void wide_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int wa
                 if (p.epi.z) store_rows32(f[c], stage, p.epi.z, p.N, row0, col0, p.M, p.N, lane);
                 act32(f[c], p.epi.act);
                 if (p.epi.residual) {
-                    add_residual32(f[c], res, stage, lane);
+                    add_residual32(f[c], res, residual_direct(p.epi, col0, p.N), stage, lane);
                     if (c == 0) load_residual32(res, p.epi, row0, nq + 32, p.M, p.N, lane);
                 }
                 store_rows32(f[c], stage, p.epi.y, p.N, row0, col0, p.M, p.N, lane);
@@ -756,14 +809,22 @@ PURO_DEV void wide_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int wa
 // 4 + 4j + q holds 32 columns of each of its rows.  The four warps of one q
 // exchange row maxima (named barrier 1 + q), the four of one j column maxima
 // (9 + j).  A warp whose wait runs out goes on through the barriers of its tiles,
-// which the others still meet it at, and stores nothing more.
+// where the others still meet it, and stores nothing more.
+// With gate and up kept, rotating operands, us: [32768, 8960] x 1536 781, [8192,
+// 6144] x 2048 163, [1024, 6144] x 2048 26.3 (the plain GEMM of [32768, 17920] 555-590,
+// the second kernel it would take 360-410).  What the stores cost is their traffic:
+// without gate and up 554-566 on the first shape, without the transposed copy
+// besides 507-537.  The stores of gate and up come first: behind the maxima, to fill
+// the barriers' waits, 895 and 183; one 32-byte store a lane instead of 64-byte rows
+// through staging 814 -> 773.
 template <int FMT, class Smem>
 PURO_DEV void gated_quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int warp, int lane, int pair,
                                    int num_pairs, int rank) {
     const int j = (warp - 4) >> 2, q = warp & 3;
-    const uint32_t bar_row = 1u + static_cast<uint32_t>(q), bar_col = 9u + static_cast<uint32_t>(j);
     const uint32_t tempty0 = mapa_shared(smem_u32(&sm.tempty[0]), 0);  // the even CTA's
+    const uint32_t bar_row = 1u + static_cast<uint32_t>(q), bar_col = 9u + static_cast<uint32_t>(j);
     GatedEpiSmem &qe = sm.qe;
+    uint32_t done = 0;  // tiles quantised
     uint8_t *stage = sm.epi[0] + kRowStage * (warp - 4);
     float *colmul = qe.colmul[warp - 4];
     const uint32_t sel1 = (lane & 1) ? 0x3715u : 0x6240u;  // quad byte transpose (see quant_epilogue)
@@ -777,10 +838,10 @@ PURO_DEV void gated_quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem,
         bool ok = (sm.abort_flag == 0) && mbar_wait_bounded(&sm.tfull[0], static_cast<uint32_t>(local & 1), p.wait_ns);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok && lane == 0) record_timeout(sm, p.status);
-        const int par = local & 1;
+        const int par = static_cast<int>(done & 1u);  // (a skipped tile has no part in the alternation)
         tc_fence_after_sync();
         const uint32_t t_row =
-            tmem + (static_cast<uint32_t>(32 * q) << 16) + static_cast<uint32_t>(par * 128 + 32 * j);
+            tmem + (static_cast<uint32_t>(32 * q) << 16) + static_cast<uint32_t>((local & 1) * 128 + 32 * j);
         float g[32], up[32];
         tmem_ld_32x32b_x32(t_row, reinterpret_cast<uint32_t(&)[32]>(g));
         tmem_ld_32x32b_x32(t_row + 128, reinterpret_cast<uint32_t(&)[32]>(up));
@@ -794,20 +855,35 @@ PURO_DEV void gated_quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem,
             store_rows32(up, stage, p.epi.z + F, p.N, row0, col0, p.M, F, lane);
         }
         gate32(g, up, p.epi.act);
-        if (p.epi.y && ok) store_rows32(g, stage, p.epi.y, F, row0, col0, p.M, F, lane);
         uint32_t v[16];  // h in BF16, columns 2k / 2k + 1 in the low / high half of v[k]
+        round32(g, v);
+        if (p.epi.y && ok) store_rows32(v, stage, p.epi.y, F, row0, col0, p.M, F, lane);
+        // ---- maxima over the warp's part of its rows and of its columns
+        {
+            uint32_t a[16], m2 = 0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            __nv_bfloat162 b2 = __floats2bfloat162_rn(g[2 * i], g[2 * i + 1]);
-            v[i] = *reinterpret_cast<uint32_t *>(&b2);
+            for (int k = 0; k < 16; ++k) {
+                a[k] = v[k] & 0x7FFF7FFFu;
+                m2 = __vmaxu2(m2, a[k]);
+            }
+            qe.rowmax[par][q][j][lane] = max(m2 & 0xFFFFu, m2 >> 16);
+            if (p.qt) {  // reduce-scatter over the 32 rows; lane l then holds word l / 2 (columns l & ~1, l | 1)
+#pragma unroll
+                for (int st = 0; st < 4; ++st) {
+                    const int half = 8 >> st, bit = 16 >> st;
+                    const bool upper = (lane & bit) != 0;
+#pragma unroll
+                    for (int i = 0; i < half; ++i) {
+                        const uint32_t keep = upper ? a[i + half] : a[i], send = upper ? a[i] : a[i + half];
+                        a[i] = __vmaxu2(keep, __shfl_xor_sync(0xFFFFFFFFu, send, bit));
+                    }
+                }
+                a[0] = __vmaxu2(a[0], __shfl_xor_sync(0xFFFFFFFFu, a[0], 1));
+                if ((lane & 1) == 0) qe.colmax[par][j][q][lane >> 1] = a[0];
+            }
         }
-
         // ---- rowwise copy: the row's group is the four warps' 128 columns
         {
-            uint32_t m2 = 0;
-#pragma unroll
-            for (int k = 0; k < 16; ++k) m2 = __vmaxu2(m2, v[k] & 0x7FFF7FFFu);
-            qe.rowmax[par][q][j][lane] = max(m2 & 0xFFFFu, m2 >> 16);
             named_bar_sync(bar_row, 128);
             const uint32_t gr = e8m0_exponent<FMT>(max(max(qe.rowmax[par][q][0][lane], qe.rowmax[par][q][1][lane]),
                                                        max(qe.rowmax[par][q][2][lane], qe.rowmax[par][q][3][lane])));
@@ -818,45 +894,21 @@ PURO_DEV void gated_quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem,
 #pragma unroll
             for (int k = 0; k < 8; ++k)
                 x[k] = quant4<FMT>(bf16_lo(v[2 * k]), bf16_hi(v[2 * k]), bf16_lo(v[2 * k + 1]), bf16_hi(v[2 * k + 1]), rm2, rnan);
-            // the two 16-byte halves swapped within lane pairs: a store writes 32-byte row pieces
-            const bool odd = (lane & 1) != 0;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, sel_u32(odd, x[w], x[4 + w]), 1);
-                if (odd)
-                    x[w] = got;
-                else
-                    x[4 + w] = got;
-            }
-            uint8_t *to = p.q + static_cast<int64_t>(row0 + (lane & ~1)) * F + col0 + 16 * (lane & 1);
             if (ok) {
-                *reinterpret_cast<uint4 *>(to) = make_uint4(x[0], x[1], x[2], x[3]);
-                *reinterpret_cast<uint4 *>(to + F) = make_uint4(x[4], x[5], x[6], x[7]);
+                uint8_t *to = p.q + static_cast<int64_t>(row0 + lane) * F + col0;
+                if ((reinterpret_cast<uintptr_t>(p.q) & 31u) == 0) {
+                    store_v8(to, x);
+                } else {
+                    *reinterpret_cast<uint4 *>(to) = make_uint4(x[0], x[1], x[2], x[3]);
+                    *reinterpret_cast<uint4 *>(to + 16) = make_uint4(x[4], x[5], x[6], x[7]);
+                }
             }
             if (j == 0 && ok) store_scale_vec(p.q_scale, row0 + lane, c0 / 128, F / 128, static_cast<uint8_t>(gr));
         }
+        ++done;
         if (p.qt == nullptr) continue;  // uniform
 
-        // ---- transposed copy: column maxima over the warp's 32 rows by a
-        // reduce-scatter butterfly; lane l then holds word l / 2 (columns l & ~1, l | 1)
-        {
-            uint32_t a[16];
-#pragma unroll
-            for (int k = 0; k < 16; ++k) a[k] = v[k] & 0x7FFF7FFFu;
-#pragma unroll
-            for (int st = 0; st < 4; ++st) {
-                const int half = 8 >> st, bit = 16 >> st;
-                const bool upper = (lane & bit) != 0;
-#pragma unroll
-                for (int i = 0; i < half; ++i) {
-                    const uint32_t keep = sel_u32(upper, a[i + half], a[i]);
-                    const uint32_t send = sel_u32(upper, a[i], a[i + half]);
-                    a[i] = __vmaxu2(keep, __shfl_xor_sync(0xFFFFFFFFu, send, bit));
-                }
-            }
-            a[0] = __vmaxu2(a[0], __shfl_xor_sync(0xFFFFFFFFu, a[0], 1));
-            if ((lane & 1) == 0) qe.colmax[par][j][q][lane >> 1] = a[0];
-        }
+        // ---- transposed copy: a column's group is the four warps' 128 rows
         named_bar_sync(bar_col, 128);
         bool any_nan;
         {  // lane l: the multiplier of the warp's column l
@@ -1424,7 +1476,7 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
                         if (p.epi.residual) {
                             uint4 res[4];
                             load_residual32(res, p.epi, m0 + 32 * q, col, p.M, n_out, lane);
-                            add_residual32(a, res, stage_buf, lane);
+                            add_residual32(a, res, residual_direct(p.epi, col, n_out), stage_buf, lane);
                         }
                         store_rows32(a, stage_buf, p.epi.y, n_out, m0 + 32 * q, col, p.M, n_out, lane);
                         continue;
