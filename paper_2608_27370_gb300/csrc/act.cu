@@ -116,10 +116,10 @@ __global__ void __launch_bounds__(256) gated_backward_kernel(const uint16_t *__r
         const uint4 d = __ldg(reinterpret_cast<const uint4 *>(dh) + i);
         const uint4 g = __ldg(reinterpret_cast<const uint4 *>(gate + r * ld + c)), u = __ldg(reinterpret_cast<const uint4 *>(up + r * ld + c));
         uint4 dg, du;
-        gated_backward2<ACT>(d.x, g.x, u.x, dg.x, du.x);
-        gated_backward2<ACT>(d.y, g.y, u.y, dg.y, du.y);
-        gated_backward2<ACT>(d.z, g.z, u.z, dg.z, du.z);
-        gated_backward2<ACT>(d.w, g.w, u.w, dg.w, du.w);
+        dg.x = gate_backward2<ACT>(d.x, g.x, u.x), du.x = up_backward2<ACT>(d.x, g.x);
+        dg.y = gate_backward2<ACT>(d.y, g.y, u.y), du.y = up_backward2<ACT>(d.y, g.y);
+        dg.z = gate_backward2<ACT>(d.z, g.z, u.z), du.z = up_backward2<ACT>(d.z, g.z);
+        dg.w = gate_backward2<ACT>(d.w, g.w, u.w), du.w = up_backward2<ACT>(d.w, g.w);
         uint16_t *out = dgate_up + r * 2 * cols + c;
         *reinterpret_cast<uint4 *>(out) = dg;
         *reinterpret_cast<uint4 *>(out + cols) = du;

@@ -60,47 +60,61 @@ PURO_DEV float act_f32(float z) {
     return z;
 }
 
-PURO_DEV float bounded(float z) { return fminf(fmaxf(z, -128.0f), 128.0f); }
 PURO_DEV uint64_t splat(float x) { return f32x2(x, x); }
+PURO_DEV uint64_t widen2(uint32_t w) { return f32x2(bf16_lo(w), bf16_hi(w)); }
+// Both BF16 values kept within 128 of zero (NaN stays).
+PURO_DEV uint32_t bounded2(uint32_t w) {
+    uint32_t r;
+    asm("{\n\t.reg .b32 t;\n\tmin.NaN.bf16x2 t, %1, %2;\n\tmax.NaN.bf16x2 %0, t, %3;\n\t}" : "=r"(r) : "r"(w), "r"(0x43004300u), "r"(0xC300C300u));
+    return r;
+}
 
-// Two activations a and their slopes d, in packed arithmetic.  Where the slope has
-// a product z * (a bell around zero) it takes a bounded z, so that infinities have
-// the slopes 0 and 1 (NaN stays, through the sigmoid or Phi).  With s = sigmoid(u):
-//   SiLU (u = z):      a = z s,  d = s + z s (1 - s)
-//   tanh GELU:         a = z s,  d = s + z s (1 - s) u',  u = z (c + k z^2)
-//   GELU:              a = z Phi,  d = Phi + z e^(-z^2/2) / sqrt(2 pi)
-// 1 - s is taken as a difference: 6e-8 off where s is near 1, where d is too.
-struct ActSlope2 {
-    uint64_t a, d;
-};
+// sigmoid(u) from v = -u log2 e, two at a time.  (e^-u may overflow: the reciprocal
+// is then zero.)
+PURO_DEV uint64_t sigmoid2(uint64_t v) {
+    float lo, hi;
+    split_f32x2(v, lo, hi);
+    split_f32x2(add_f32x2(f32x2(ex2_approx(lo), ex2_approx(hi)), splat(1.0f)), lo, hi);
+    return f32x2(rcp_approx(lo), rcp_approx(hi));
+}
+PURO_DEV uint64_t tanh_gelu_exponent2(uint64_t z) {  // -u log2 e, u = z (kGeluC + kGeluK z^2)
+    return mul_f32x2(z, fma_f32x2(mul_f32x2(z, z), splat(-1.44269504f * kGeluK), splat(-1.44269504f * kGeluC)));
+}
+
+// Activations of a BF16 pair, and their slopes, in packed arithmetic.  With s =
+// sigmoid(u), Phi the normal distribution function:
+//   SiLU (u = z):  a = z s,    d = s + z s (1 - s)
+//   tanh GELU:     a = z s,    d = s + z s (1 - s) u'
+//   GELU:          a = z Phi,  d = Phi + z e^(-z^2/2) / sqrt(2 pi)
+// Slopes take z within 128 of zero, beyond which they are 0 and 1 to the last bit:
+// infinities then have those slopes too.  1 - s is taken as a difference: 6e-8 off
+// where s is near 1, where d is too.
 template <int ACT>
-PURO_DEV ActSlope2 act_slope2(float z0, float z1) {
-    const uint64_t z = f32x2(z0, z1);
+PURO_DEV uint64_t act2(uint32_t w) {
+    const uint64_t z = widen2(w);
+    if constexpr (ACT == PURO_ACT_SILU) return mul_f32x2(z, sigmoid2(mul_f32x2(z, splat(-1.44269504f))));
+    if constexpr (ACT == PURO_ACT_GELU_TANH) return mul_f32x2(z, sigmoid2(tanh_gelu_exponent2(z)));
+    if constexpr (ACT != PURO_ACT_NONE) return f32x2(act_f32<ACT>(bf16_lo(w)), act_f32<ACT>(bf16_hi(w)));
+    return z;
+}
+template <int ACT>
+PURO_DEV uint64_t slope2(uint32_t w) {
+    if constexpr (ACT == PURO_ACT_NONE) return splat(1.0f);
     if constexpr (ACT == PURO_ACT_RELU) {
-        auto relu = [](float x) { return x < 0.0f ? 0.0f : x; };
         auto step = [](float x) { return x > 0.0f ? 1.0f : (x <= 0.0f ? 0.0f : x); };
-        return ActSlope2{f32x2(relu(z0), relu(z1)), f32x2(step(z0), step(z1))};
+        return f32x2(step(bf16_lo(w)), step(bf16_hi(w)));
     }
-    if constexpr (ACT == PURO_ACT_SILU || ACT == PURO_ACT_GELU_TANH) {
-        constexpr bool kTanh = ACT == PURO_ACT_GELU_TANH;
-        uint64_t u = mul_f32x2(z, splat(-1.44269504f));  // -u log2 e
-        if constexpr (kTanh)
-            u = mul_f32x2(z, fma_f32x2(mul_f32x2(z, z), splat(-1.44269504f * kGeluK), splat(-1.44269504f * kGeluC)));
-        float lo, hi;
-        split_f32x2(u, lo, hi);
-        split_f32x2(add_f32x2(f32x2(ex2_approx(lo), ex2_approx(hi)), splat(1.0f)), lo, hi);
-        const uint64_t s = f32x2(rcp_approx(lo), rcp_approx(hi));
-        const uint64_t zb = f32x2(bounded(z0), bounded(z1));
-        uint64_t bell = mul_f32x2(mul_f32x2(zb, s), fma_f32x2(s, splat(-1.0f), splat(1.0f)));
-        if constexpr (kTanh) bell = mul_f32x2(bell, fma_f32x2(mul_f32x2(zb, zb), splat(3.0f * kGeluK), splat(kGeluC)));
-        return ActSlope2{mul_f32x2(z, s), add_f32x2(bell, s)};
-    }
+    const uint32_t wb = bounded2(w);
+    const uint64_t z = widen2(wb);
     if constexpr (ACT == PURO_ACT_GELU) {
-        const Normal n0 = normal_both(z0), n1 = normal_both(z1);
-        const uint64_t cdf = f32x2(n0.cdf, n1.cdf), zb = f32x2(bounded(z0), bounded(z1));
-        return ActSlope2{mul_f32x2(z, cdf), fma_f32x2(mul_f32x2(zb, splat(0.39894228f)), f32x2(n0.bell, n1.bell), cdf)};
+        const Normal n0 = normal_both(bf16_lo(wb)), n1 = normal_both(bf16_hi(wb));
+        return fma_f32x2(mul_f32x2(z, splat(0.39894228f)), f32x2(n0.bell, n1.bell), f32x2(n0.cdf, n1.cdf));
     }
-    return ActSlope2{z, splat(1.0f)};
+    constexpr bool kTanh = ACT == PURO_ACT_GELU_TANH;
+    const uint64_t s = sigmoid2(kTanh ? tanh_gelu_exponent2(z) : mul_f32x2(z, splat(-1.44269504f)));
+    uint64_t bell = mul_f32x2(mul_f32x2(z, s), fma_f32x2(s, splat(-1.0f), splat(1.0f)));
+    if constexpr (kTanh) bell = mul_f32x2(bell, fma_f32x2(mul_f32x2(z, z), splat(3.0f * kGeluK), splat(kGeluC)));
+    return add_f32x2(bell, s);
 }
 
 PURO_DEV uint32_t pack_bf16x2(uint64_t v) {
@@ -113,7 +127,7 @@ PURO_DEV uint32_t pack_bf16x2(uint64_t v) {
 // dz = dy * act'(z) of two BF16 pairs; the unrounded values are added to s0, s1.
 template <int ACT>
 PURO_DEV uint32_t act_backward2(uint32_t dy, uint32_t z, float &s0, float &s1) {
-    const uint64_t d = mul_f32x2(f32x2(bf16_lo(dy), bf16_hi(dy)), act_slope2<ACT>(bf16_lo(z), bf16_hi(z)).d);
+    const uint64_t d = ACT == PURO_ACT_NONE ? widen2(dy) : mul_f32x2(widen2(dy), slope2<ACT>(z));
     float lo, hi;
     split_f32x2(d, lo, hi);
     s0 += lo;
@@ -123,11 +137,12 @@ PURO_DEV uint32_t act_backward2(uint32_t dy, uint32_t z, float &s0, float &s1) {
 
 // dgate = dh * (up * act'(gate)) and dup = dh * act(gate) of two BF16 pairs.
 template <int ACT>
-PURO_DEV void gated_backward2(uint32_t dh, uint32_t gate, uint32_t up, uint32_t &dgate, uint32_t &dup) {
-    const ActSlope2 s = act_slope2<ACT>(bf16_lo(gate), bf16_hi(gate));
-    const uint64_t d = f32x2(bf16_lo(dh), bf16_hi(dh));
-    dgate = pack_bf16x2(mul_f32x2(d, mul_f32x2(f32x2(bf16_lo(up), bf16_hi(up)), s.d)));
-    dup = pack_bf16x2(mul_f32x2(d, s.a));
+PURO_DEV uint32_t gate_backward2(uint32_t dh, uint32_t gate, uint32_t up) {
+    return pack_bf16x2(mul_f32x2(widen2(dh), mul_f32x2(widen2(up), slope2<ACT>(gate))));
+}
+template <int ACT>
+PURO_DEV uint32_t up_backward2(uint32_t dh, uint32_t gate) {
+    return pack_bf16x2(mul_f32x2(widen2(dh), act2<ACT>(gate)));
 }
 
 // f(std::integral_constant<int, act>): one copy of the code for each activation.

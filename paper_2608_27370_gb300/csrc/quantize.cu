@@ -944,49 +944,140 @@ __global__ void __launch_bounds__(kQAThreads, 2)
 }
 
 // ------------------------------------------- backward of activations, quantised
-// dz = dy * act'(z) or, GATED, [dgate, dup] = [dh * up * act'(gate), dh *
-// act(gate)], rounded to BF16 and cast as quant_act_kernel casts: 512 threads on
-// a 128x128 tile, thread t on the 8x4 block of rows 8*br .. and columns 4*bc ..,
-// br = warp, bc = lane.  The inputs' tiles come by TMA into one buffer each.  Once
-// they are in registers the buffers are free: y's for the next tile's y, and the
-// others (GATED) for the staging of the codes, which leaves room for two CTAs an
-// SM with 96 KB of loads each; they alternate, one computing while the other
-// waits for its tiles.  Both outputs of a gate come from one evaluation of the
-// activation.
-// As a producer of quant_act_kernel (a tile of one output at a time, the gates
-// loaded into registers), us: [8192, 6144] gated 171 -> 108, [8192, 8960]
-// gelu_tanh with dbias 115 -> 90.
-template <bool GATED>
-struct QuantBackwardSmem {
-    static constexpr int kOut = GATED ? 2 : 1;
-    alignas(1024) uint16_t y[kQT * kQT];          // dy or dh
-    alignas(1024) uint16_t z[kOut][kQT * kQT];    // z, or gate and up; GATED: then the codes of each output
-    alignas(1024) uint8_t stage[GATED ? 16 : 2 * kQT * kQT];  // the codes, rowwise and transposed
-    alignas(16) uint32_t col_part[kOut][16][kQT / 2];
-    alignas(16) float col_mul[kOut][kQT];
-    alignas(16) float col_sum[GATED ? 1 : 16][kQT];  // sums of dz over each block of eight rows
-    alignas(16) uint8_t row_g[kOut][kQT];
-    alignas(16) uint8_t col_g[kOut][kQT];
+// dz = dy * act'(z) or [dgate, dup] = [dh * up * act'(gate), dh * act(gate)],
+// rounded to BF16 and cast as quant_act_kernel casts: 512 threads (a team) on a
+// 128x128 tile, thread t on the 8x4 block of rows 8*br .. and columns 4*bc .., br =
+// warp, bc = lane.  The inputs' tiles come by TMA.  Shared by both kernels, after
+// the outputs of the tile are in registers.
+
+// One output of a tile: v[i] is row 8br + i, columns 4bc .. 4bc + 3, in BF16.
+struct OutTile {
+    alignas(16) uint32_t col_part[16][kQT / 2];  // [row block][column pair]: maxima
+    alignas(16) float col_mul[kQT];
+    alignas(16) uint8_t row_g[kQT];
+    alignas(16) uint8_t col_g[kQT];
+};
+
+// Row groups (a warp holds its eight rows whole) and column partials.  Returns, in
+// lane i % 8, the multiplier of row i.
+template <int FMT, bool HAS_T>
+PURO_DEV float tile_maxima(OutTile &t, const uint2 (&v)[8], int br, int bc) {
+    // (absmax_bf16x2 and one mask rather than masks and integer maxima: the integer pipe is the busiest)
+    uint32_t rmax[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t w = absmax_bf16x2(v[i].x, v[i].y);
+        rmax[i] = __reduce_max_sync(0xFFFFFFFFu, absmax_bf16x2(w, __byte_perm(w, 0u, 0x1032)) & 0x7FFF7FFFu);
+    }
+    const bool b0 = bc & 1, b1 = bc & 2, b2 = bc & 4;
+    const uint32_t s01 = b0 ? rmax[1] : rmax[0], s23 = b0 ? rmax[3] : rmax[2];
+    const uint32_t s45 = b0 ? rmax[5] : rmax[4], s67 = b0 ? rmax[7] : rmax[6];
+    const uint32_t g = e8m0_exponent<FMT>((b2 ? (b1 ? s67 : s45) : (b1 ? s23 : s01)) & 0xFFFFu);
+    if (bc < 8) t.row_g[8 * br + bc] = static_cast<uint8_t>(g);
+    if constexpr (HAS_T) {
+        uint2 cm = v[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) {
+            cm.x = absmax_bf16x2(cm.x, v[i].x);
+            cm.y = absmax_bf16x2(cm.y, v[i].y);
+        }
+        *reinterpret_cast<uint2 *>(&t.col_part[br][2 * bc]) = make_uint2(cm.x & 0x7FFF7FFFu, cm.y & 0x7FFF7FFFu);
+    }
+    return mul_of(g);
+}
+
+// Column scales from the partials, two of the team's threads per column.
+template <int FMT>
+PURO_DEV void tile_column_scales(OutTile &t, int tid) {
+    if (tid >= 2 * kQT) return;
+    const int c = tid >> 1, h = tid & 1;
+    uint32_t w = 0;
+#pragma unroll
+    for (int b = 0; b < 8; ++b) w = __vmaxu2(w, t.col_part[8 * h + b][c >> 1]);
+    w = __vmaxu2(w, __shfl_xor_sync(0xFFFFFFFFu, w, 1));
+    if (h == 0) {
+        const uint32_t g = e8m0_exponent<FMT>((c & 1) ? (w >> 16) : (w & 0xFFFFu));
+        t.col_mul[c] = mul_of(g);
+        t.col_g[c] = static_cast<uint8_t>(g);
+    }
+}
+
+// Codes into the staging (rowwise; transposed with the 128-byte swizzle) and the
+// scale vectors.  Operand rows r0 .., columns oc0 .. of an output [rows, out_cols].
+template <int FMT, bool HAS_T>
+PURO_DEV void tile_codes(const OutTile &t, const uint2 (&v)[8], float mul, uint8_t *stage, int tid, int br, int bc, int64_t r0,
+                         int64_t oc0, int64_t rows, int64_t out_cols, uint8_t *scale, uint8_t *scale_t) {
+    float4 cmv = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+    float msum = mul;
+    if constexpr (HAS_T) {
+        cmv = *reinterpret_cast<const float4 *>(&t.col_mul[4 * bc]);
+        msum += (cmv.x + cmv.y) + (cmv.z + cmv.w);
+    }
+    const uint64_t cm01 = f32x2(cmv.x, cmv.y), cm23 = f32x2(cmv.z, cmv.w);
+    uint32_t rw[8];
+    auto code = [&](int i, float rm, uint32_t &q) {
+        const uint64_t p0 = f32x2(bf16_lo(v[i].x), bf16_hi(v[i].x)), p1 = f32x2(bf16_lo(v[i].y), bf16_hi(v[i].y)), rr = f32x2(rm, rm);
+        q = cvt_f32x4<FMT>(mul_f32x2(p0, rr), mul_f32x2(p1, rr));
+        if constexpr (HAS_T) rw[i] = cvt_f32x4<FMT>(mul_f32x2(p0, cm01), mul_f32x2(p1, cm23));
+    };
+    uint8_t *to = stage + 8 * br * kQT + 4 * bc;
+    if (!__any_sync(0xFFFFFFFFu, isnan(msum))) {  // every group of the warp's block finite
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t q;
+            code(i, __shfl_sync(0xFFFFFFFFu, mul, i), q);
+            *reinterpret_cast<uint32_t *>(to + i * kQT) = q;
+        }
+    } else {
+        // a group that holds Inf or NaN has a NaN multiplier: its codes are NaN with each value's sign
+        const uint32_t col_nan = (isnan(cmv.x) ? 0xFFu : 0u) | (isnan(cmv.y) ? 0xFF00u : 0u) | (isnan(cmv.z) ? 0xFF0000u : 0u) |
+                                 (isnan(cmv.w) ? 0xFF000000u : 0u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float rm = __shfl_sync(0xFFFFFFFFu, mul, i);
+            uint32_t q;
+            code(i, rm, q);
+            const uint32_t nan = 0x7F7F7F7Fu | ((v[i].x >> 8) & 0x80u) | ((v[i].x >> 16) & 0x8000u) | ((v[i].y & 0x8000u) << 8) |
+                                 (v[i].y & 0x80000000u);
+            *reinterpret_cast<uint32_t *>(to + i * kQT) = isnan(rm) ? nan : q;
+            if constexpr (HAS_T) rw[i] = (rw[i] & ~col_nan) | (nan & col_nan);
+        }
+    }
+    if constexpr (HAS_T) stage_transposed_8x4(stage + kQT * kQT, rw, br, bc);
+    if (tid < 2 * kQT) {  // the rowwise operand's rows, then the transposed one's
+        const bool col = tid >= kQT;
+        const int i = tid & (kQT - 1);
+        if (!col || HAS_T)
+            store_scale_vec(col ? scale_t : scale, (col ? oc0 : r0) + i, (col ? r0 : oc0) / kQT, (col ? rows : out_cols) / kQT,
+                            col ? t.col_g[i] : t.row_g[i]);
+    }
+}
+
+// ---- dz: two CTAs of one team an SM.  The buffers of dy and z are free for the next
+// tile once the outputs are in registers, so its loads run under the casting.  As a
+// producer of quant_act_kernel, with z loaded into registers, [8192, 8960] gelu_tanh
+// with dbias took 115 us, so 85 (5.2 TB/s).
+struct ActBackwardSmem {
+    alignas(1024) uint16_t y[kQT * kQT], z[kQT * kQT];
+    alignas(1024) uint8_t stage[2 * kQT * kQT];
+    OutTile out;
+    alignas(16) float col_sum[16][kQT];  // sums of dz over each block of eight rows
     uint64_t full;
 };
 
-template <int FMT, bool HAS_T, bool GATED>
+template <int FMT, bool HAS_T>
 __global__ void __launch_bounds__(kQAThreads, 2)
-    quant_backward_kernel(const __grid_constant__ BackwardQuantMaps m, const BackwardQuantArgs a) {
-    constexpr int kOut = GATED ? 2 : 1;
-    using Smem = QuantBackwardSmem<GATED>;
+    quant_act_backward_kernel(const __grid_constant__ BackwardQuantMaps m, const BackwardQuantArgs a) {
     extern __shared__ uint8_t smem_raw[];
-    Smem &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-    const int tid = threadIdx.x, lane = tid & 31, br = tid >> 5, bc = lane;
-    const bool has_z = GATED || a.act != PURO_ACT_NONE;
-    auto q_stage = [&](int o) { return GATED ? reinterpret_cast<uint8_t *>(sm.z[o]) : sm.stage; };
-    auto qt_stage = [&](int o) { return q_stage(o) + kQT * kQT; };
+    ActBackwardSmem &sm = *reinterpret_cast<ActBackwardSmem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                                               ~static_cast<uintptr_t>(1023));
+    const int tid = threadIdx.x, bc = tid & 31, br = tid >> 5;
+    const bool has_z = a.act != PURO_ACT_NONE;
     if (tid == 0) {
         mbar_init(&sm.full, 1);
         fence_mbarrier_init();
         tma_prefetch_desc(&m.y);
         tma_prefetch_desc(&m.z);
-        if (GATED) tma_prefetch_desc(&m.up);
         tma_prefetch_desc(&m.q);
         if (HAS_T) tma_prefetch_desc(&m.qt);
     }
@@ -997,26 +1088,18 @@ __global__ void __launch_bounds__(kQAThreads, 2)
     int tile = blockIdx.x;
     TileWalk cur(ntiles - 1 - tile, step, tiles_n), nxt = cur;
     nxt.advance();
-    auto load_y = [&](const TileWalk &t) {  // opens the tile's phase of the barrier
-        mbar_arrive_expect_tx(&sm.full, (1 + (has_z ? kOut : 0)) * kQT * kQT * 2);
+    auto load = [&](const TileWalk &t) {
+        mbar_arrive_expect_tx(&sm.full, (has_z ? 2 : 1) * kQT * kQT * 2);
         tma_load_2d(sm.y, &m.y, &sm.full, t.c * kQT, t.r * kQT);
-    };
-    auto load_z = [&](const TileWalk &t) {
-        if (has_z) tma_load_2d(sm.z[0], &m.z, &sm.full, t.c * kQT, t.r * kQT);
-        if constexpr (GATED) tma_load_2d(sm.z[kOut - 1], &m.up, &sm.full, t.c * kQT, t.r * kQT);
+        if (has_z) tma_load_2d(sm.z, &m.z, &sm.full, t.c * kQT, t.r * kQT);
     };
     pdl_wait();
     pdl_launch_dependents();
-    if (tid == 0) {  // (the grid has no more CTAs than tiles)
-        load_y(cur);
-        load_z(cur);
-    }
-    const int64_t out_cols = a.cols * kOut;
+    if (tid == 0) load(cur);  // (the grid has no more CTAs than tiles)
     for (int it = 0; tile < ntiles; ++it, tile += step, cur = nxt, nxt.advance()) {
         const int64_t r0 = static_cast<int64_t>(cur.r) * kQT, c0 = static_cast<int64_t>(cur.c) * kQT;
         const bool landed = tile_landed(&sm.full, static_cast<uint32_t>(it) & 1u, a.wait_ns);
-
-        uint2 v[kOut][8];  // the outputs in BF16
+        uint2 v[8];
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         act_dispatch(a.act, [&](auto act) {
             constexpr int ACT = decltype(act)::value;
@@ -1024,150 +1107,159 @@ __global__ void __launch_bounds__(kQAThreads, 2)
             for (int i = 0; i < 8; ++i) {
                 const int at = (8 * br + i) * kQT + 4 * bc;
                 const uint2 y = *reinterpret_cast<const uint2 *>(sm.y + at);
-                if constexpr (GATED) {
-                    const uint2 g = *reinterpret_cast<const uint2 *>(sm.z[0] + at), u = *reinterpret_cast<const uint2 *>(sm.z[kOut - 1] + at);
-                    gated_backward2<ACT>(y.x, g.x, u.x, v[0][i].x, v[kOut - 1][i].x);
-                    gated_backward2<ACT>(y.y, g.y, u.y, v[0][i].y, v[kOut - 1][i].y);
-                } else if constexpr (ACT == PURO_ACT_NONE) {
-                    v[0][i] = y;
+                if constexpr (ACT == PURO_ACT_NONE) {
+                    v[i] = y;
                     sum[0] += bf16_lo(y.x), sum[1] += bf16_hi(y.x), sum[2] += bf16_lo(y.y), sum[3] += bf16_hi(y.y);
                 } else {
-                    const uint2 z = *reinterpret_cast<const uint2 *>(sm.z[0] + at);
-                    v[0][i] = make_uint2(act_backward2<ACT>(y.x, z.x, sum[0], sum[1]), act_backward2<ACT>(y.y, z.y, sum[2], sum[3]));
+                    const uint2 z = *reinterpret_cast<const uint2 *>(sm.z + at);
+                    v[i] = make_uint2(act_backward2<ACT>(y.x, z.x, sum[0], sum[1]), act_backward2<ACT>(y.y, z.y, sum[2], sum[3]));
                 }
             }
         });
-
-        // ---- A: row groups (a warp holds its eight rows whole) and column partials
-        float mul[kOut];  // lane i % 8: of row i
-#pragma unroll
-        for (int o = 0; o < kOut; ++o) {
-            uint32_t rmax[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t w = __vmaxu2(v[o][i].x & 0x7FFF7FFFu, v[o][i].y & 0x7FFF7FFFu);
-                rmax[i] = __reduce_max_sync(0xFFFFFFFFu, __vmaxu2(w, __byte_perm(w, 0u, 0x1032)));
-            }
-            const bool b0 = lane & 1, b1 = lane & 2, b2 = lane & 4;
-            const uint32_t s01 = b0 ? rmax[1] : rmax[0], s23 = b0 ? rmax[3] : rmax[2];
-            const uint32_t s45 = b0 ? rmax[5] : rmax[4], s67 = b0 ? rmax[7] : rmax[6];
-            const uint32_t g = e8m0_exponent<FMT>((b2 ? (b1 ? s67 : s45) : (b1 ? s23 : s01)) & 0xFFFFu);
-            mul[o] = mul_of(g);
-            if (lane < 8) sm.row_g[o][8 * br + lane] = static_cast<uint8_t>(g);
-            if constexpr (HAS_T) {
-                uint2 cm = make_uint2(0u, 0u);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    cm.x = __vmaxu2(cm.x, v[o][i].x & 0x7FFF7FFFu);
-                    cm.y = __vmaxu2(cm.y, v[o][i].y & 0x7FFF7FFFu);
-                }
-                *reinterpret_cast<uint2 *>(&sm.col_part[o][br][2 * bc]) = cm;
-            }
-        }
-        if (!GATED && a.col_sum)
-            *reinterpret_cast<float4 *>(&sm.col_sum[br][4 * bc]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
-        if (!GATED && tid == 0) bulk_wait_group_read0();  // the staging is free
-        if (__syncthreads_or(!landed)) {                  // (S2) partials written, every input in registers
+        const float mul = tile_maxima<FMT, HAS_T>(sm.out, v, br, bc);
+        if (a.col_sum) *reinterpret_cast<float4 *>(&sm.col_sum[br][4 * bc]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+        if (tid == 0) bulk_wait_group_read0();  // the staging is free
+        if (__syncthreads_or(!landed)) {        // (S2) partials written, every input in registers
             if (tid == 0) {
                 if (a.status) atomicExch(a.status, kQuantStatusTimeout);
                 mbar_wait_bounded(&sm.full, static_cast<uint32_t>(it) & 1u, kQuantDrainNs);  // its loads land
             }
             break;
         }
-        const bool more = tile + step < ntiles;
-        if (tid == 0 && more) {
-            load_y(nxt);
-            if (!GATED) load_z(nxt);
-        }
-
-        // ---- B: column scales, two threads per column (eight row blocks each)
-        if constexpr (HAS_T) {
-            const int o = tid / (2 * kQT), c = (tid >> 1) & (kQT - 1), h = tid & 1;
-            if (o < kOut) {
-                uint32_t w = 0;
-#pragma unroll
-                for (int b = 0; b < 8; ++b) w = __vmaxu2(w, sm.col_part[o][8 * h + b][c >> 1]);
-                w = __vmaxu2(w, __shfl_xor_sync(0xFFFFFFFFu, w, 1));
-                if (h == 0) {
-                    const uint32_t g = e8m0_exponent<FMT>((c & 1) ? (w >> 16) : (w & 0xFFFFu));
-                    sm.col_mul[o][c] = mul_of(g);
-                    sm.col_g[o][c] = static_cast<uint8_t>(g);
-                }
-            }
-        }
-        if (!GATED && a.col_sum && tid >= kQAThreads - kQT) {  // the tile's 128 rows, their blocks in order
+        if (tid == 0 && tile + step < ntiles) load(nxt);
+        if constexpr (HAS_T) tile_column_scales<FMT>(sm.out, tid);
+        if (a.col_sum && tid >= kQAThreads - kQT) {  // the tile's 128 rows, their blocks in order
             const int c = tid - (kQAThreads - kQT);
             float s = sm.col_sum[0][c];
 #pragma unroll
-            for (int b = 1; b < (GATED ? 1 : 16); ++b) s += sm.col_sum[b][c];
+            for (int b = 1; b < 16; ++b) s += sm.col_sum[b][c];
             a.col_sum[static_cast<int64_t>(cur.r) * a.cols + c0 + c] = s;
         }
         if (a.out) {  // the BF16 rows: a warp stores 256 bytes of one
 #pragma unroll
-            for (int o = 0; o < kOut; ++o)
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    *reinterpret_cast<uint2 *>(a.out + (r0 + 8 * br + i) * out_cols + o * a.cols + c0 + 4 * bc) = v[o][i];
+            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint2 *>(a.out + (r0 + 8 * br + i) * a.cols + c0 + 4 * bc) = v[i];
         }
         if (HAS_T) __syncthreads();  // (S3) column scales ready
-
-        // ---- C: codes into the staging
-#pragma unroll
-        for (int o = 0; o < kOut; ++o) {
-            uint8_t *qs = q_stage(o);
-            float4 cmv = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
-            float msum = mul[o];
-            if constexpr (HAS_T) {
-                cmv = *reinterpret_cast<const float4 *>(&sm.col_mul[o][4 * bc]);
-                msum += (cmv.x + cmv.y) + (cmv.z + cmv.w);
-            }
-            // a group that holds Inf or NaN has a NaN multiplier: its codes are NaN with each value's sign
-            const bool some_nan = __any_sync(0xFFFFFFFFu, isnan(msum));
-            const uint32_t col_nan = (isnan(cmv.x) ? 0xFFu : 0u) | (isnan(cmv.y) ? 0xFF00u : 0u) |
-                                     (isnan(cmv.z) ? 0xFF0000u : 0u) | (isnan(cmv.w) ? 0xFF000000u : 0u);
-            const uint64_t cm01 = f32x2(cmv.x, cmv.y), cm23 = f32x2(cmv.z, cmv.w);
-            uint32_t rw[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint2 w = v[o][i];
-                const float rm = __shfl_sync(0xFFFFFFFFu, mul[o], i);
-                const uint64_t p0 = f32x2(bf16_lo(w.x), bf16_hi(w.x)), p1 = f32x2(bf16_lo(w.y), bf16_hi(w.y)), rr = f32x2(rm, rm);
-                uint32_t q = cvt_f32x4<FMT>(mul_f32x2(p0, rr), mul_f32x2(p1, rr));
-                if constexpr (HAS_T) rw[i] = cvt_f32x4<FMT>(mul_f32x2(p0, cm01), mul_f32x2(p1, cm23));
-                if (__builtin_expect(some_nan, 0)) {
-                    const uint32_t nan = 0x7F7F7F7Fu | ((w.x >> 8) & 0x80u) | ((w.x >> 16) & 0x8000u) | ((w.y & 0x8000u) << 8) |
-                                         (w.y & 0x80000000u);
-                    if (isnan(rm)) q = nan;
-                    if constexpr (HAS_T) rw[i] = (rw[i] & ~col_nan) | (nan & col_nan);
-                }
-                *reinterpret_cast<uint32_t *>(qs + (8 * br + i) * kQT + 4 * bc) = q;
-            }
-            if constexpr (HAS_T) stage_transposed_8x4(qt_stage(o), rw, br, bc);
-        }
-        // scale vectors: of output tid / 256, the rowwise operand's rows, then the transposed one's
-        {
-            const int o = tid / (2 * kQT);
-            const bool col = (tid & kQT) != 0;
-            if (o < kOut && (!col || HAS_T)) {
-                const int i = tid & (kQT - 1);
-                const int64_t oc0 = o * a.cols + c0;
-                store_scale_vec(col ? a.scale_t : a.scale, (col ? oc0 : r0) + i, (col ? r0 : oc0) / kQT,
-                                (col ? a.rows : out_cols) / kQT, col ? sm.col_g[o][i] : sm.row_g[o][i]);
-            }
-        }
+        tile_codes<FMT, HAS_T>(sm.out, v, mul, sm.stage, tid, br, bc, r0, c0, a.rows, a.cols, a.scale, a.scale_t);
         fence_proxy_async_smem();
         __syncthreads();  // (S4) staging complete, exponents read
         if (tid == 0) {
-#pragma unroll
-            for (int o = 0; o < kOut; ++o) {
-                const int oc0 = static_cast<int>(o * a.cols + c0);
-                tma_store_2d(&m.q, q_stage(o), oc0, static_cast<int32_t>(r0));
-                if (HAS_T) tma_store_2d(&m.qt, qt_stage(o), static_cast<int32_t>(r0), oc0);
-            }
+            tma_store_2d(&m.q, sm.stage, static_cast<int32_t>(c0), static_cast<int32_t>(r0));
+            if (HAS_T) tma_store_2d(&m.qt, sm.stage + kQT * kQT, static_cast<int32_t>(r0), static_cast<int32_t>(c0));
             bulk_commit_group();
-            if (GATED && more) {  // the gates' buffers hold the codes until they have left
+        }
+    }
+    if (tid == 0) bulk_wait_group0();
+}
+
+// ---- [dgate, dup]: one CTA of two teams an SM, team 0 on dgate and team 1 on dup of
+// the same tile.  Two stages of the three inputs: while a tile is computed the next
+// one's 96 KB are on their way, and a tile's own gate and up buffers, once read,
+// hold the codes until they have left.  Two CTAs an SM with single buffers, each
+// computing both outputs from one activation, waited for their loads: [8192, 6144] 108
+// us, so 102 (4.9 TB/s, bound by its instructions: 64% of the issue slots).  Both
+// outputs from one evaluation here too, handed to the teams through the buffers,
+// took 109, for the barrier.
+struct GatedBackwardSmem {
+    struct Stage {
+        alignas(1024) uint16_t h[kQT * kQT], z[2][kQT * kQT];  // dh; gate and up, then the codes of dgate and dup
+    } in[2];
+    OutTile out[2];
+    uint64_t full[2];
+};
+
+template <int FMT, bool HAS_T>
+__global__ void __launch_bounds__(2 * kQAThreads, 1)
+    quant_gated_backward_kernel(const __grid_constant__ BackwardQuantMaps m, const BackwardQuantArgs a) {
+    extern __shared__ uint8_t smem_raw[];
+    GatedBackwardSmem &sm = *reinterpret_cast<GatedBackwardSmem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                                                   ~static_cast<uintptr_t>(1023));
+    const int team = threadIdx.x / kQAThreads, tid = threadIdx.x % kQAThreads, bc = tid & 31, br = tid >> 5;
+    if (threadIdx.x == 0) {
+        mbar_init(&sm.full[0], 1);
+        mbar_init(&sm.full[1], 1);
+        fence_mbarrier_init();
+        tma_prefetch_desc(&m.y);
+        tma_prefetch_desc(&m.z);
+        tma_prefetch_desc(&m.up);
+        tma_prefetch_desc(&m.q);
+        if (HAS_T) tma_prefetch_desc(&m.qt);
+    }
+    __syncthreads();
+    const int tiles_n = static_cast<int>(a.cols / kQT);
+    const int ntiles = static_cast<int>(a.rows / kQT) * tiles_n;
+    const int step = gridDim.x;
+    int tile = blockIdx.x;
+    TileWalk cur(ntiles - 1 - tile, step, tiles_n), nxt2 = cur;  // this tile and the one after the next
+    nxt2.advance();
+    // dh's load opens a stage's phase; each team loads its own of gate and up
+    auto load_h = [&](const TileWalk &t, int s) {
+        mbar_arrive_expect_tx(&sm.full[s], 3 * kQT * kQT * 2);
+        tma_load_2d(sm.in[s].h, &m.y, &sm.full[s], t.c * kQT, t.r * kQT);
+    };
+    auto load_z = [&](const TileWalk &t, int s) {
+        tma_load_2d(sm.in[s].z[team], team ? &m.up : &m.z, &sm.full[s], t.c * kQT, t.r * kQT);
+    };
+    pdl_wait();
+    pdl_launch_dependents();
+    if (tid == 0) {
+        if (team == 0) load_h(cur, 0);
+        load_z(cur, 0);
+        if (tile + step < ntiles) {
+            if (team == 0) load_h(nxt2, 1);
+            load_z(nxt2, 1);
+        }
+    }
+    nxt2.advance();
+    const int64_t out_cols = 2 * a.cols;
+    for (int it = 0; tile < ntiles; ++it, tile += step, cur.advance(), nxt2.advance()) {
+        const int s = it & 1;
+        const int64_t r0 = static_cast<int64_t>(cur.r) * kQT, c0 = static_cast<int64_t>(cur.c) * kQT;
+        const int64_t oc0 = team * a.cols + c0;
+        const bool landed = tile_landed(&sm.full[s], static_cast<uint32_t>(it >> 1) & 1u, a.wait_ns);
+        uint2 v[8];
+        act_dispatch(a.act, [&](auto act) {
+            constexpr int ACT = decltype(act)::value;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int at = (8 * br + i) * kQT + 4 * bc;
+                const uint2 h = *reinterpret_cast<const uint2 *>(sm.in[s].h + at), g = *reinterpret_cast<const uint2 *>(sm.in[s].z[0] + at);
+                if (team == 0) {
+                    const uint2 u = *reinterpret_cast<const uint2 *>(sm.in[s].z[1] + at);
+                    v[i] = make_uint2(gate_backward2<ACT>(h.x, g.x, u.x), gate_backward2<ACT>(h.y, g.y, u.y));
+                } else {
+                    v[i] = make_uint2(up_backward2<ACT>(h.x, g.x), up_backward2<ACT>(h.y, g.y));
+                }
+            }
+        });
+        const float mul = tile_maxima<FMT, HAS_T>(sm.out[team], v, br, bc);
+        if (__syncthreads_or(!landed)) {  // (S2) partials written, every input in registers
+            if (threadIdx.x == 0) {
+                if (a.status) atomicExch(a.status, kQuantStatusTimeout);
+                mbar_wait_bounded(&sm.full[s], static_cast<uint32_t>(it >> 1) & 1u, kQuantDrainNs);  // the loads land
+                if (tile + step < ntiles) mbar_wait_bounded(&sm.full[s ^ 1], static_cast<uint32_t>((it + 1) >> 1) & 1u, kQuantDrainNs);
+            }
+            break;
+        }
+        const bool more = tile + 2 * step < ntiles;
+        if (threadIdx.x == 0 && more) load_h(nxt2, s);
+        if constexpr (HAS_T) tile_column_scales<FMT>(sm.out[team], tid);
+        if (a.out) {  // the BF16 rows: a warp stores 256 bytes of one
+#pragma unroll
+            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint2 *>(a.out + (r0 + 8 * br + i) * out_cols + oc0 + 4 * bc) = v[i];
+        }
+        if (HAS_T) named_bar_sync(1u + static_cast<uint32_t>(team), kQAThreads);  // (S3) column scales ready
+        uint8_t *stage = reinterpret_cast<uint8_t *>(sm.in[s].z[team]);
+        tile_codes<FMT, HAS_T>(sm.out[team], v, mul, stage, tid, br, bc, r0, oc0, a.rows, out_cols, a.scale, a.scale_t);
+        fence_proxy_async_smem();
+        named_bar_sync(1u + static_cast<uint32_t>(team), kQAThreads);  // (S4) staging complete, exponents read
+        if (tid == 0) {
+            tma_store_2d(&m.q, stage, static_cast<int32_t>(oc0), static_cast<int32_t>(r0));
+            if (HAS_T) tma_store_2d(&m.qt, stage + kQT * kQT, static_cast<int32_t>(r0), static_cast<int32_t>(oc0));
+            bulk_commit_group();
+            if (more) {  // the buffer holds the codes until they have left
                 bulk_wait_group_read0();
-                load_z(nxt);
+                load_z(nxt2, s);
             }
         }
     }
@@ -1380,20 +1472,21 @@ static cudaError_t launch_swiglu_f(const QuantArgs &a, const CUtensorMap &tm_x, 
                    : launch_quant_t<FMT, kQuantBlockAct, false, kProdSwiGlu>(a, tm_x, tm_q, tm_qt, s, &tm_y, prod);
 }
 
-template <int FMT, bool GATED>
-static cudaError_t launch_backward_f(const BackwardQuantArgs &a, const BackwardQuantMaps &m, cudaStream_t s) {
-    auto kern = a.scale_t ? quant_backward_kernel<FMT, true, GATED> : quant_backward_kernel<FMT, false, GATED>;
-    const size_t smem = sizeof(QuantBackwardSmem<GATED>) + 1024;
+template <int FMT, bool HAS_T>
+static cudaError_t launch_backward_f(const BackwardQuantArgs &a, const BackwardQuantMaps &m, bool gated, cudaStream_t s) {
+    auto kern = gated ? quant_gated_backward_kernel<FMT, HAS_T> : quant_act_backward_kernel<FMT, HAS_T>;
+    const size_t smem = (gated ? sizeof(GatedBackwardSmem) : sizeof(ActBackwardSmem)) + 1024;
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
     const int64_t ntiles = a.rows / kQT * (a.cols / kQT);
-    const int cap = 2 * sm_count_here();  // persistent: two CTAs per SM
-    return launch_pdl(kern, dim3(static_cast<unsigned>(ntiles < cap ? ntiles : cap)), dim3(kQAThreads), smem, s, m, a);
+    const int cap = (gated ? 1 : 2) * sm_count_here();  // persistent: as many as are resident
+    return launch_pdl(kern, dim3(static_cast<unsigned>(ntiles < cap ? ntiles : cap)), dim3((gated ? 2 : 1) * kQAThreads), smem, s,
+                      m, a);
 }
 
 cudaError_t launch_quantize_backward(const BackwardQuantArgs &a, const BackwardQuantMaps &m, bool gated, cudaStream_t s) {
-    if (gated) return a.fmt == 0 ? launch_backward_f<0, true>(a, m, s) : launch_backward_f<1, true>(a, m, s);
-    return a.fmt == 0 ? launch_backward_f<0, false>(a, m, s) : launch_backward_f<1, false>(a, m, s);
+    if (a.scale_t) return a.fmt == 0 ? launch_backward_f<0, true>(a, m, gated, s) : launch_backward_f<1, true>(a, m, gated, s);
+    return a.fmt == 0 ? launch_backward_f<0, false>(a, m, gated, s) : launch_backward_f<1, false>(a, m, gated, s);
 }
 
 cudaError_t launch_quantize_swiglu(const QuantArgs &a, const CUtensorMap &tm_x, const CUtensorMap &tm_q,
