@@ -28,8 +28,8 @@
 
 namespace puro {
 
-constexpr int kQkThreads = 256;
-constexpr int kQkFwdBatch = 3, kQkBwdBatch = 2;  // heads of a token a group loads at once
+constexpr int kQkFwdThreads = 128, kQkThreads = 256;  // (the backward's)
+constexpr int kQkFwdBatch = 4, kQkBwdBatch = 2;       // heads of a token a group loads at once
 constexpr int kQkBwdBlocks = 152 * 2;  // at most: two an SM are resident, each leaves a partial sum of a gain's gradient
 constexpr int32_t kQkStatusInvalid = 1;  // PURO_ERR_INVALID_ARG
 
@@ -183,17 +183,20 @@ PURO_DEV void replace_row(QkRow row, uint4 (&w)[2]) {
 
 // A block: some tokens' batch of heads of one kind, the batches of the same tokens
 // next to one another (the queries' first).  On 8192 tokens of 16 + 8 heads of 128
-// 22 us (4.7 TB/s), on 32768 45 us (5.3 TB/s); the same loads and stores without the
-// arithmetic take 16.4.  Persistent blocks with the next items' loads in flight
-// (cp.async, two ahead) took 23 to 45 us: what that saves goes into addresses.
+// 20.6 us (5.0 TB/s), on 32768 of 12 + 2 heads 42.0 us (5.7 TB/s); the same loads and
+// stores without the arithmetic take 16.4 and 35.3.  Blocks of 256 threads, three
+// an SM: 22.1 and 44.7; batches of two, three, five, six heads 22.7, 21.6, 20.4, 20.8 (and
+// more for one token, 2.3 us, or 1024).  Persistent blocks with the next items' loads
+// in flight (cp.async, two ahead) took 23 to 45 us: what that saves goes into
+// addresses.
 template <int G, bool INTER>
-__global__ void __launch_bounds__(kQkThreads, 3) qk_norm_rope_kernel(const QkArgs p) {
+__global__ void __launch_bounds__(kQkFwdThreads, 5) qk_norm_rope_kernel(const QkArgs p) {
     constexpr int B = kQkFwdBatch;
     pdl_wait();
     pdl_launch_dependents();
     const QkLane l = qk_lane(threadIdx.x % G, p.D, p.rot, INTER);
     const unsigned q_batches = (p.q.heads + B - 1) / B, batches = q_batches + (p.k.heads + B - 1) / B;
-    const int64_t t = static_cast<int64_t>(blockIdx.x / batches) * (kQkThreads / G) + threadIdx.x / G;
+    const int64_t t = static_cast<int64_t>(blockIdx.x / batches) * (kQkFwdThreads / G) + threadIdx.x / G;
     const unsigned batch = blockIdx.x % batches;
     const bool is_q = batch < q_batches, live = t < p.tokens && l.in;
     const QkHeads &src = is_q ? p.q : p.k, &dst = is_q ? p.q_out : p.k_out;
@@ -246,7 +249,9 @@ __global__ void __launch_bounds__(kQkThreads, 3) qk_norm_rope_kernel(const QkArg
 
 // Blocks [0, p.q_blocks) take the query heads, the others the key heads, each a
 // strided share of (token, batch of heads); so a thread sums one gain's
-// gradient, in a fixed order, and a block leaves one partial sum [D].
+// gradient, in a fixed order, and a block leaves one partial sum [D].  8192 tokens
+// of 16 + 8 heads of 128 31.5 us with the gains' sum (4.9 TB/s), 32768 of 12 + 2 heads
+// 65.8 (5.4 TB/s); one, three, four heads a batch 37, 33, 33 us on the first.
 template <int G, bool INTER>
 __global__ void __launch_bounds__(kQkThreads, 2) qk_norm_rope_backward_kernel(const QkArgs p) {
     constexpr int B = kQkBwdBatch, kGroups = kQkThreads / G;
@@ -416,11 +421,11 @@ void qk_backward_blocks(int64_t tokens, int q_heads, int k_heads, int D, int *q_
                                : ((p).inter ? kern<16, true> : kern<16, false>))
 
 cudaError_t launch_qk_norm_rope(const QkArgs &p, cudaStream_t s) {
-    const int64_t per = kQkThreads / group_lanes(p.D);
+    const int64_t per = kQkFwdThreads / group_lanes(p.D);
     auto batches = [](int heads) { return (heads + kQkFwdBatch - 1) / kQkFwdBatch; };
     const int64_t grid = (p.tokens + per - 1) / per * (batches(p.q.heads) + batches(p.k.heads));
     if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
-    return launch_pdl(PURO_QK_KERNEL(qk_norm_rope_kernel, p), dim3(static_cast<unsigned>(grid)), dim3(kQkThreads), 0, s, p);
+    return launch_pdl(PURO_QK_KERNEL(qk_norm_rope_kernel, p), dim3(static_cast<unsigned>(grid)), dim3(kQkFwdThreads), 0, s, p);
 }
 
 cudaError_t launch_qk_norm_rope_backward(QkArgs p, float *dq_gain, float *dk_gain, cudaStream_t s) {

@@ -167,6 +167,7 @@ static cudaError_t launch_skinny(const uint16_t *x, const uint16_t *w, int64_t M
 // 1024 2.7 / 8.3 and 2.9 / 8.3, [8960] x 1536 21.7 / 15.9 and 22.9 / 15.7 (at 16 tokens
 // 15.2 / 15.9).
 bool is_skinny_linear(int64_t M, int64_t N, int64_t K, bool gated) {
+    if (K > (1 << 30)) return false;  // (k is an int there)
     return M <= 16 || (M <= 32 && N * K * (gated ? 2 : 1) <= (4 << 20));
 }
 
