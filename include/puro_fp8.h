@@ -20,10 +20,13 @@
  *   - Ownership: the caller allocates and owns every buffer.  The library
  *     allocates no memory, never synchronises the stream (except
  *     puro_fp8_get_status, which says so) and keeps no state between calls.
+ *   - Overlap: an output may not overlap an input or another output, unless
+ *     the call says which may be the same.
  *   - Ordering: all work is enqueued on `stream` (a cudaStream_t passed as
  *     void*; NULL is the legacy default stream) in call order.
  *   - Pointers: device pointers unless marked "host".  Every tensor pointer
- *     must be 16-byte aligned.
+ *     must be 16-byte aligned.  (Linears with an epilogue are faster with
+ *     rows at 32 bytes.)
  *   - Errors: argument violations are detected on the host before anything
  *     is enqueued and return PURO_ERR_INVALID_ARG or PURO_ERR_UNSUPPORTED;
  *     a failed launch returns PURO_ERR_CUDA.  No entry point traps or

@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(256) act_backward_kernel(const uint16_t *dy, c
 #pragma unroll 4
         for (int64_t r = blockIdx.y * slab_rows + ty; r < r1; r += kActRows) {
             const int64_t at = r * cols + c;
-            const uint4 d = *reinterpret_cast<const uint4 *>(dy + at);  // (dz may be dy)
+            const uint4 d = __ldcg(reinterpret_cast<const uint4 *>(dy + at));  // (dz may be dy: past L1)
             uint4 zw = d;
             if constexpr (ACT != PURO_ACT_NONE) zw = __ldg(reinterpret_cast<const uint4 *>(z + at));
             uint4 o;

@@ -650,7 +650,9 @@ PURO_DEV void act32(float (&f)[32], int act) {
 
 // 32 columns of the lane's row of the residual (direct: where 32-byte loads are
 // aligned), or of the warp's rows as store_rows32 stores them; zeros past the last
-// row or column.  (The output may be the residual itself.)
+// row or column.  (The output may be the residual itself: pieces of less than a sector are
+// loaded past L1, where the part that another SM overwrites would stay as it was, for a
+// kernel that is already waiting there to read it.)
 PURO_DEV bool residual_direct(const GemmEpilogue &epi, int col0, int cols) {
     return ((reinterpret_cast<uintptr_t>(epi.residual) | static_cast<uintptr_t>(2 * epi.ld_residual)) & 31u) == 0 &&
            col0 + 32 <= cols;
@@ -670,7 +672,7 @@ PURO_DEV void load_residual32(uint4 (&v)[4], const GemmEpilogue &epi, int row0, 
     const uint16_t *from = epi.residual + row * epi.ld_residual + col;
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-        v[k] = row + 8 * k < rows && col < cols ? *reinterpret_cast<const uint4 *>(from + 8 * k * epi.ld_residual)
+        v[k] = row + 8 * k < rows && col < cols ? __ldcg(reinterpret_cast<const uint4 *>(from + 8 * k * epi.ld_residual))
                                                 : make_uint4(0u, 0u, 0u, 0u);
 }
 // f += them, handed to the lanes that hold the rows through the staging.
@@ -1709,7 +1711,7 @@ __global__ void __launch_bounds__(256) epilogue_kernel(const float *__restrict__
 #pragma unroll
             for (int k = 0; k < 8; ++k) f[k] = act_f32<decltype(act)::value>(f[k]);
         });
-        if (epi.residual) add8(f, *reinterpret_cast<const uint4 *>(epi.residual + row * epi.ld_residual + col));
+        if (epi.residual) add8(f, __ldcg(reinterpret_cast<const uint4 *>(epi.residual + row * epi.ld_residual + col)));
         out(epi.y);
     }
 }
@@ -1834,7 +1836,7 @@ int cluster_split(int64_t M, int64_t N, int64_t K, int splits) {
 // Pairs per cluster that share each 128-wide tile of a BF16 linear with an
 // epilogue (K reduction bytes), or 1: there is no workspace to split through, so
 // the choice is between clusters and whole tiles, by the modelled cycles of
-// cluster_split and choose_tile_n.  Eight calls with rotating weights in a graph,
+// cluster_split and choose_tile_n.  Sixteen calls of four weights in a graph,
 // us a call, whole tiles and in clusters: [256, 1536] x 1536 8.3 and 6.7, [256, 2048]
 // x 1536 8.4 and 7.5, [256, 1536] x 8960 28.4 and 14.7.
 int cluster_or_whole(int64_t M, int64_t N, int64_t K) {

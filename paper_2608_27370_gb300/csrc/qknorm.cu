@@ -202,13 +202,13 @@ __global__ void __launch_bounds__(kQkFwdThreads, 5) qk_norm_rope_kernel(const Qk
     const QkHeads &src = is_q ? p.q : p.k, &dst = is_q ? p.q_out : p.k_out;
     const int h0 = static_cast<int>(is_q ? batch : batch - q_batches) * B, n = min(B, src.heads - h0);
     const uint16_t *from = src.data + t * src.token_stride + h0 * src.head_stride;
-    uint4 x[B][2];
+    uint4 x[B][2];  // (y may be x: loaded past L1, where a neighbour's part of a sector would stay as it was)
 #pragma unroll
     for (int b = 0; b < B; ++b) {
         x[b][0] = x[b][1] = make_uint4(0, 0, 0, 0);
         if (live && b < n) {
-            x[b][0] = *reinterpret_cast<const uint4 *>(from + l.o0);
-            x[b][1] = *reinterpret_cast<const uint4 *>(from + l.o1);
+            x[b][0] = __ldcg(reinterpret_cast<const uint4 *>(from + l.o0));
+            x[b][1] = __ldcg(reinterpret_cast<const uint4 *>(from + l.o1));
         }
         from += src.head_stride;
     }
@@ -290,8 +290,8 @@ __global__ void __launch_bounds__(kQkThreads, 2) qk_norm_rope_backward_kernel(co
                 const uint16_t *py = DY.data + t * DY.token_stride + (h0 + b) * DY.head_stride;
                 x[b][0] = *reinterpret_cast<const uint4 *>(px + l.o0);
                 x[b][1] = *reinterpret_cast<const uint4 *>(px + l.o1);
-                dy[b][0] = *reinterpret_cast<const uint4 *>(py + l.o0);
-                dy[b][1] = *reinterpret_cast<const uint4 *>(py + l.o1);
+                dy[b][0] = __ldcg(reinterpret_cast<const uint4 *>(py + l.o0));  // (dx may be dy: as above)
+                dy[b][1] = __ldcg(reinterpret_cast<const uint4 *>(py + l.o1));
                 rs[b] = __ldg(p.rstd + t * heads + first + h0 + b);
             }
         }

@@ -583,6 +583,7 @@ struct QuantActSmem {
     alignas(16) uint16_t gamma[2][kQT];          // kProdRmsNorm: of the tile's columns
     uint64_t full[2];
 };
+
 // y = bf16((h * rstd) * gamma) for a 4-value chunk, two products an instruction
 // (rs: rstd twice; gm: the gains in pairs).
 PURO_DEV uint2 rmsnorm_chunk4(uint2 w, uint64_t rs, const uint64_t (&gm)[2], bool has_gamma) {

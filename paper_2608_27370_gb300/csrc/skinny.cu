@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(WARPS * 32) skinny_linear_kernel(const uint16_
         const __nv_bfloat16 b = __float2bfloat16_rn(v);
         to[at] = *reinterpret_cast<const uint16_t *>(&b);
     };
-    auto bf = [](const uint16_t *p, int64_t at) { return __uint_as_float(static_cast<uint32_t>(p[at]) << 16); };
+    auto bf = [](uint16_t b) { return __uint_as_float(static_cast<uint32_t>(b) << 16); };
     const int n = threadIdx.x & 7, col = n0 + n;
     for (int m = threadIdx.x >> 3; m < M; m += WARPS * 4) {
         float f[kTiles];
@@ -123,10 +123,11 @@ __global__ void __launch_bounds__(WARPS * 32) skinny_linear_kernel(const uint16_
             out(epi.y, static_cast<int64_t>(m) * N + col, f[0] * f[kTiles - 1]);
         } else {
             const int64_t at = static_cast<int64_t>(m) * N + col;
-            if (epi.bias) f[0] += bf(epi.bias, col);
+            if (epi.bias) f[0] += bf(epi.bias[col]);
             if (epi.z) out(epi.z, at, f[0]);
             act_dispatch(epi.act, [&](auto act) { f[0] = act_f32<decltype(act)::value>(f[0]); });
-            if (epi.residual) f[0] += bf(epi.residual, m * epi.ld_residual + col);
+            // (y may be the residual: past L1, where a neighbour's part of the sector would stay as it was)
+            if (epi.residual) f[0] += bf(__ldcg(epi.residual + m * epi.ld_residual + col));
             out(epi.y, at, f[0]);
         }
     }

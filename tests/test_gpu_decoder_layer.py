@@ -214,3 +214,33 @@ def test_one_token_at_a_time_in_bf16():
             # both round the same products once; the sums' orders differ: a BF16 step at most, or what cancelled
             d = (a[0].double() - b[i].double()).abs()
             assert bool((d <= 2.0 ** -7 * b[i].double().abs() + 2.0 ** -9 * b[i].double().pow(2).mean().sqrt()).all())
+
+
+@pytest.mark.gpu
+def test_a_residual_stream_updated_in_place():
+    """Each linear adds to the stream in place and the next kernel, already started, reads it: captured and replayed, the
+    bytes of calls that are waited for one by one.  (Rows end inside a 32-byte sector.)"""
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    width, inner, blocks, rows = 1032, 520, 12, 3
+    w_in = [_normal((inner, width), width ** -0.5, 40 + i) for i in range(blocks)]
+    w_out = [_normal((width, inner), inner ** -0.5, 60 + i) for i in range(blocks)]
+    h0, h, mid = _normal((rows, width), 1.0, 80), torch.empty((rows, width), dtype=BF, device=DEV), torch.empty(
+        (rows, inner), dtype=BF, device=DEV)
+
+    def run(wait):
+        h.copy_(h0)
+        for wi, wo in zip(w_in, w_out):
+            P.puro_bf16_linear_fprop_epilogue(h, wi, mid, act=P.ACT_GELU)
+            wait()
+            P.puro_bf16_linear_fprop_epilogue(mid, wo, h, residual=h)
+            wait()
+
+    run(torch.cuda.synchronize)
+    ref = h.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(lambda: None)
+    for _ in range(20):
+        graph.replay()
+        assert torch.equal(h, ref)
