@@ -574,7 +574,10 @@ PURO_DEV void load_v8(const void *p, uint4 &a, uint4 &b) {
 // 32 values of each lane's row, rounded to BF16, to out[row, col0 .. col0 + 31]
 // (rows ld elements apart), rows below `rows` and columns below `cols` only.  Two
 // 32-byte stores a lane, whole sectors, where the rows are aligned for them ([8192,
-// 8960] x 1536 with gelu and z 125 -> 99 us).  Otherwise sixteen rows at a time go
+// 8960] x 1536 with gelu and z 125 -> 99 us).  PAIRS: as 64-byte pieces of two lanes,
+// fewer requests for more instructions (worth it behind the gated form, but 77 -> 89
+// us on [8192, 2048] x 6144 with a residual, whose warps store before they release the
+// accumulator).  Otherwise sixteen rows at a time go
 // through the warp's kilobyte of staging (64-byte rows, 16-byte chunk c of row r at
 // c ^ (r / 2) % 4), so that a store writes eight 64-byte pieces.
 constexpr int kRowStage = 1024;
@@ -585,10 +588,24 @@ PURO_DEV void round32(const float (&f)[32], uint32_t (&x)[16]) {
         x[i] = *reinterpret_cast<uint32_t *>(&b);
     }
 }
+template <bool PAIRS = false>
 PURO_DEV void store_rows32(const uint32_t (&x)[16], uint8_t *stage, uint16_t *out, int64_t ld, int row0, int col0,
                            int rows, int cols, int lane) {
     if (((reinterpret_cast<uintptr_t>(out) | static_cast<uintptr_t>(2 * ld)) & 31u) == 0 && col0 + 32 <= cols) {
-        if (row0 + lane < rows) {
+        if constexpr (PAIRS) {  // the pair of lanes exchanges halves: 64 bytes of the even row, then of the odd one
+            const bool odd = lane & 1;
+            uint32_t even_row[8], odd_row[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, odd ? x[i] : x[8 + i], 1);
+                even_row[i] = odd ? got : x[i];
+                odd_row[i] = odd ? x[8 + i] : got;
+            }
+            const int row = row0 + (lane & ~1);
+            uint16_t *to = out + static_cast<int64_t>(row) * ld + col0 + 16 * (lane & 1);
+            if (row < rows) store_v8(to, even_row);
+            if (row + 1 < rows) store_v8(to + ld, odd_row);
+        } else if (row0 + lane < rows) {
             uint16_t *to = out + static_cast<int64_t>(row0 + lane) * ld + col0;
             store_v8(to, &x[0]);
             store_v8(to + 16, &x[8]);
@@ -618,11 +635,12 @@ PURO_DEV void store_rows32(const uint32_t (&x)[16], uint8_t *stage, uint16_t *ou
     }
 }
 
+template <bool PAIRS = false>
 PURO_DEV void store_rows32(const float (&f)[32], uint8_t *stage, uint16_t *out, int64_t ld, int row0, int col0,
                            int rows, int cols, int lane) {
     uint32_t x[16];
     round32(f, x);
-    store_rows32(x, stage, out, ld, row0, col0, rows, cols, lane);
+    store_rows32<PAIRS>(x, stage, out, ld, row0, col0, rows, cols, lane);
 }
 
 PURO_DEV void add8(float *f, const uint4 &w) {
@@ -806,19 +824,25 @@ PURO_DEV void wide_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int wa
     }
 }
 
+// NaN codes with the signs of four BF16 values.
+PURO_DEV uint32_t nan_codes4(uint32_t a, uint32_t b) { return 0x7F7F7F7Fu | (__byte_perm(a, b, 0x7531) & 0x80808080u); }
+
 // kGemmOutGatedQuant (block kind, 256-wide): a tile's 128 columns of h and this
 // CTA's 128 rows are one block of groups both ways, as in quant_epilogue; warp
 // 4 + 4j + q holds 32 columns of each of its rows.  The four warps of one q
 // exchange row maxima (named barrier 1 + q), the four of one j column maxima
 // (9 + j).  A warp whose wait runs out goes on through the barriers of its tiles,
 // where the others still meet it, and stores nothing more.
-// With gate and up kept, rotating operands, us: [32768, 8960] x 1536 781, [8192,
-// 6144] x 2048 163, [1024, 6144] x 2048 26.3 (the plain GEMM of [32768, 17920] 555-590,
-// the second kernel it would take 360-410).  What the stores cost is their traffic:
-// without gate and up 554-566 on the first shape, without the transposed copy
-// besides 507-537.  The stores of gate and up come first: behind the maxima, to fill
-// the barriers' waits, 895 and 183; one 32-byte store a lane instead of 64-byte rows
-// through staging 814 -> 773.
+// With gate and up kept, rotating operands, us: [32768, 8960] x 1536 725, [8192,
+// 6144] x 2048 154, [1024, 6144] x 2048 25.3 (the plain GEMM of [32768, 17920] 555-590,
+// the second kernel it would take 360-410).  A tile takes 9030 cycles on the first
+// shape, 7250 of them the epilogue's, and 7430 without stores: they compete with the
+// operands' loads for L2, by requests more than by bytes (confined to 1 MB they cost
+// the same), so gate and up leave in 64-byte pieces (in 32-byte ones 775, 166).
+// Codes gathered in shared memory and stored as 128-byte rows: 740, 162, for the
+// barriers.  The stores of gate and up come first: behind the maxima, to fill the
+// barriers' waits, 895 and 183.  The codes of a tile's copies are computed without a
+// branch for each four, which would end their overlap (826 -> 738 on the first).
 template <int FMT, class Smem>
 PURO_DEV void gated_quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int warp, int lane, int pair,
                                    int num_pairs, int rank) {
@@ -853,13 +877,13 @@ PURO_DEV void gated_quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem,
         if (lane == 0) mbar_arrive_cluster_cta_scope(tempty0);  // in registers
         if (m0 >= p.M) continue;  // (whole 128-row blocks: uniform over the CTA)
         if (p.epi.z && ok) {
-            store_rows32(g, stage, p.epi.z, p.N, row0, col0, p.M, F, lane);
-            store_rows32(up, stage, p.epi.z + F, p.N, row0, col0, p.M, F, lane);
+            store_rows32<true>(g, stage, p.epi.z, p.N, row0, col0, p.M, F, lane);
+            store_rows32<true>(up, stage, p.epi.z + F, p.N, row0, col0, p.M, F, lane);
         }
         gate32(g, up, p.epi.act);
         uint32_t v[16];  // h in BF16, columns 2k / 2k + 1 in the low / high half of v[k]
         round32(g, v);
-        if (p.epi.y && ok) store_rows32(v, stage, p.epi.y, F, row0, col0, p.M, F, lane);
+        if (p.epi.y && ok) store_rows32<true>(v, stage, p.epi.y, F, row0, col0, p.M, F, lane);
         // ---- maxima over the warp's part of its rows and of its columns
         {
             uint32_t a[16], m2 = 0;
@@ -891,11 +915,13 @@ PURO_DEV void gated_quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem,
                                                        max(qe.rowmax[par][q][2][lane], qe.rowmax[par][q][3][lane])));
             const float rmul = mul_of(gr);
             const uint64_t rm2 = f32x2(rmul, rmul);
-            const bool rnan = isnan(rmul);
             uint32_t x[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                x[k] = quant4<FMT>(bf16_lo(v[2 * k]), bf16_hi(v[2 * k]), bf16_lo(v[2 * k + 1]), bf16_hi(v[2 * k + 1]), rm2, rnan);
+            for (int k = 0; k < 8; ++k) x[k] = cvt_f32x4<FMT>(mul_f32x2(widen2(v[2 * k]), rm2), mul_f32x2(widen2(v[2 * k + 1]), rm2));
+            if (__any_sync(0xFFFFFFFFu, isnan(rmul))) {  // (a branch for each four codes would end their overlap)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = isnan(rmul) ? nan_codes4(v[2 * k], v[2 * k + 1]) : x[k];
+            }
             if (ok) {
                 uint8_t *to = p.q + static_cast<int64_t>(row0 + lane) * F + col0;
                 if ((reinterpret_cast<uintptr_t>(p.q) & 31u) == 0) {
@@ -912,34 +938,36 @@ PURO_DEV void gated_quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem,
 
         // ---- transposed copy: a column's group is the four warps' 128 rows
         named_bar_sync(bar_col, 128);
-        bool any_nan;
-        {  // lane l: the multiplier of the warp's column l
-            const uint32_t(*cm)[16] = qe.colmax[par][j];
-            const uint32_t m2c = __vmaxu2(__vmaxu2(cm[0][lane >> 1], cm[1][lane >> 1]), __vmaxu2(cm[2][lane >> 1], cm[3][lane >> 1]));
-            const uint32_t gc = e8m0_exponent<FMT>((lane & 1) ? (m2c >> 16) : (m2c & 0xFFFFu));
-            const float cmul = mul_of(gc);
-            colmul[lane] = cmul;
-            if (q == 0 && ok) store_scale_vec(p.qt_scale, col0 + lane, m0 / 128, p.M / 128, static_cast<uint8_t>(gc));
-            any_nan = __any_sync(0xFFFFFFFFu, isnan(cmul));  // (and the warp's multipliers are written)
-            __syncwarp();
-        }
-        uint8_t *qt_base = p.qt + static_cast<int64_t>(col0 + (lane & 3)) * p.M + row0 + 4 * (lane >> 2);
+        // lane l: the multiplier of the warp's column l
+        const uint32_t(*cmax)[16] = qe.colmax[par][j];
+        const uint32_t m2c = __vmaxu2(__vmaxu2(cmax[0][lane >> 1], cmax[1][lane >> 1]), __vmaxu2(cmax[2][lane >> 1], cmax[3][lane >> 1]));
+        const uint32_t gc = e8m0_exponent<FMT>((lane & 1) ? (m2c >> 16) : (m2c & 0xFFFFu));
+        const float cmul = mul_of(gc);
+        colmul[lane] = cmul;
+        if (q == 0 && ok) store_scale_vec(p.qt_scale, col0 + lane, m0 / 128, p.M / 128, static_cast<uint8_t>(gc));
+        const uint32_t nan_cols = __ballot_sync(0xFFFFFFFFu, isnan(cmul));  // (and the warp's multipliers are written)
+        __syncwarp();
+        uint32_t x[8];  // columns 4w .. 4w + 3 of the lane's row, then of four rows' one column
 #pragma unroll
-        for (int w = 0; w < 8; ++w) {  // columns 4w .. 4w+3 of the warp's 32
+        for (int w = 0; w < 8; ++w) {
             const float4 cm = *reinterpret_cast<const float4 *>(&colmul[4 * w]);
-            const uint32_t a = v[2 * w], b = v[2 * w + 1];
-            uint32_t lo, hi;
-            if (any_nan) {
-                lo = quant2_cols<FMT>(bf16_lo(a), bf16_hi(a), cm.x, cm.y);
-                hi = quant2_cols<FMT>(bf16_lo(b), bf16_hi(b), cm.z, cm.w);
-            } else {
-                lo = cvt_f32x2<FMT>(mul_f32x2(f32x2(bf16_lo(a), bf16_hi(a)), f32x2(cm.x, cm.y)));
-                hi = cvt_f32x2<FMT>(mul_f32x2(f32x2(bf16_lo(b), bf16_hi(b)), f32x2(cm.z, cm.w)));
+            x[w] = cvt_f32x4<FMT>(mul_f32x2(widen2(v[2 * w]), f32x2(cm.x, cm.y)), mul_f32x2(widen2(v[2 * w + 1]), f32x2(cm.z, cm.w)));
+        }
+        if (nan_cols) {
+#pragma unroll
+            for (int w = 0; w < 8; ++w) {
+                const uint32_t n4 = (nan_cols >> (4 * w)) & 15u, mask = ((n4 * 0x204081u) & 0x01010101u) * 0xFFu;  // a byte a column
+                x[w] = (x[w] & ~mask) | (nan_codes4(v[2 * w], v[2 * w + 1]) & mask);
             }
-            uint32_t x = lo | (hi << 16);
-            x = __byte_perm(x, __shfl_xor_sync(0xFFFFFFFFu, x, 1), sel1);
-            x = __byte_perm(x, __shfl_xor_sync(0xFFFFFFFFu, x, 2), sel2);
-            if (ok) *reinterpret_cast<uint32_t *>(qt_base + static_cast<int64_t>(4 * w) * p.M) = x;
+        }
+#pragma unroll
+        for (int w = 0; w < 8; ++w) x[w] = __byte_perm(x[w], __shfl_xor_sync(0xFFFFFFFFu, x[w], 1), sel1);
+#pragma unroll
+        for (int w = 0; w < 8; ++w) x[w] = __byte_perm(x[w], __shfl_xor_sync(0xFFFFFFFFu, x[w], 2), sel2);
+        if (ok) {
+            uint8_t *to = p.qt + static_cast<int64_t>(col0 + (lane & 3)) * p.M + row0 + 4 * (lane >> 2);
+#pragma unroll
+            for (int w = 0; w < 8; ++w) *reinterpret_cast<uint32_t *>(to + static_cast<int64_t>(4 * w) * p.M) = x[w];
         }
     }
 }
