@@ -17,6 +17,13 @@ enough that a full capture ends in seconds).  Not part of the library.
     python -m paper_2608_27370_gb300.microbench.kernels weights  # one grouped launch: the four weights of eight C5 layers
     python -m paper_2608_27370_gb300.microbench.kernels splitk   # qkv Wgrad at M = 32768: split reduction, BF16 and FP32 main-grad
     python -m paper_2608_27370_gb300.microbench.kernels unfused  # the unfused producers: RMSNorm [32768, 1536], SwiGLU [8192, 6144]
+    python -m paper_2608_27370_gb300.microbench.kernels linear_residual  # down Fprop [8192, 2048] x 6144 with a residual
+    python -m paper_2608_27370_gb300.microbench.kernels gated    # gate/up, SwiGLU and its copies, [8192, 8960] x 1536, gate/up kept
+    python -m paper_2608_27370_gb300.microbench.kernels act_backward    # tanh GELU's backward, [8192, 8960], both copies and dbias
+    python -m paper_2608_27370_gb300.microbench.kernels gated_backward  # SwiGLU's backward, [8192, 6144], both copies
+    python -m paper_2608_27370_gb300.microbench.kernels qk       # norms and rotation, 32768 tokens of 12 + 2 heads of 128
+    python -m paper_2608_27370_gb300.microbench.kernels qk_backward  # their backward with the gains' gradients
+    python -m paper_2608_27370_gb300.microbench.kernels skinny   # one token through gate/up [17920, 1536] in BF16
 
 Most inputs are larger than L2 (ncu flushes the caches before each pass in
 any case).  Every call is made twice: the second is the one to capture
@@ -144,9 +151,65 @@ def main(which: str) -> None:
         for _ in range(2):
             P.puro_rmsnorm_bf16(h, g, 1e-6, rstd, y)
             P.puro_swiglu_bf16(gu[:, :6144], gu[:, 6144:], hs)
+    elif which == "linear_residual":
+        M, N, K = 8192, 2048, 6144
+        x = P.quantize(W.normal_bf16((M, K), 1.0, dev, 16), transpose=False).rowwise
+        w = P.quantize(W.normal_bf16((N, K), 0.02, dev, 17), P.E4M3, P.SCALE_BLOCK, P.ROLE_WEIGHT, transpose=False).rowwise
+        res, y = W.normal_bf16((M, N), 1.0, dev, 18), torch.empty((M, N), dtype=torch.bfloat16, device=dev)
+        for _ in range(2):
+            P.puro_fp8_linear_fprop_epilogue(x, w, y, residual=res)
+    elif which == "gated":
+        M, F, K = 8192, 8960, 1536
+        x = P.quantize(W.normal_bf16((M, K), 1.0, dev, 19), transpose=False).rowwise
+        w = P.quantize(W.normal_bf16((2 * F, K), 0.02, dev, 20), P.E4M3, P.SCALE_BLOCK, P.ROLE_WEIGHT, transpose=False).rowwise
+        gate_up = torch.empty((M, 2 * F), dtype=torch.bfloat16, device=dev)
+        q = P.quantize(torch.empty((M, F), dtype=torch.bfloat16, device=dev))
+        for _ in range(2):
+            P.puro_fp8_gated_fprop(x, w, P.ACT_SILU, P.E4M3, gate_up, None, q.rowwise.data, q.rowwise.scale, q.colwise.data,
+                                   q.colwise.scale)
+    elif which == "act_backward":
+        M, N = 8192, 8960
+        z, dy = W.normal_bf16((M, N), 1.0, dev, 21), W.normal_bf16((M, N), 1e-3, dev, 22)
+        q = P.quantize(dy)
+        dbias = torch.empty(N, dtype=torch.float32, device=dev)
+        ws = torch.empty(P.puro_act_backward_workspace_size(M, N), dtype=torch.uint8, device=dev)
+        for _ in range(2):
+            P.puro_fp8_quantize_act_backward(dy, z, P.ACT_GELU_TANH, P.E4M3, None, dbias, ws, q.rowwise.data, q.rowwise.scale,
+                                             q.colwise.data, q.colwise.scale)
+    elif which == "gated_backward":
+        M, F = 8192, 6144
+        gu, dh = W.normal_bf16((M, 2 * F), 1.0, dev, 23), W.normal_bf16((M, F), 1e-3, dev, 24)
+        q = P.quantize(gu)
+        for _ in range(2):
+            P.puro_fp8_quantize_gated_backward(dh, gu[:, :F], gu[:, F:], P.ACT_SILU, P.E4M3, None, q.rowwise.data,
+                                               q.rowwise.scale, q.colwise.data, q.colwise.scale)
+    elif which in ("qk", "qk_backward"):
+        T, HQ, HK, D = 32768, 12, 2, 128
+        qkv, dqkv = W.normal_bf16((T, HQ + 2 * HK, D), 1.0, dev, 25), W.normal_bf16((T, HQ + HK, D), 1e-3, dev, 26)
+        q, k = qkv[:, :HQ], qkv[:, HQ:HQ + HK]
+        gq, gk = (W.normal_bf16((D,), 0.1, dev, 27 + i).add_(1.0) for i in range(2))
+        angle = torch.outer(torch.arange(T, device=dev), 1e4 ** (-torch.arange(0, D, 2, device=dev) / D))
+        cos, sin = angle.cos().float().contiguous(), angle.sin().float().contiguous()
+        out, rstd = torch.empty_like(dqkv), torch.empty((T, HQ + HK), dtype=torch.float32, device=dev)
+        dgq, dgk = (torch.empty(D, dtype=torch.float32, device=dev) for _ in range(2))
+        ws = torch.empty(P.puro_qk_norm_rope_workspace_size(T, HQ, HK, D), dtype=torch.uint8, device=dev)
+        for _ in range(2):
+            if which == "qk":
+                P.puro_qk_norm_rope(q, k, gq, gk, 1e-6, cos, sin, None, False, out[:, :HQ], out[:, HQ:], rstd)
+            else:
+                rstd.fill_(1.0)
+                P.puro_qk_norm_rope_backward(dqkv[:, :HQ], dqkv[:, HQ:], q, k, rstd, gq, gk, cos, sin, None, False,
+                                             out[:, :HQ], out[:, HQ:], dgq, dgk, ws)
+    elif which == "skinny":
+        F, K = 8960, 1536
+        x, w = W.normal_bf16((1, K), 1.0, dev, 29), W.normal_bf16((2 * F, K), 0.02, dev, 30)
+        gate_up, h = (torch.empty((1, n), dtype=torch.bfloat16, device=dev) for n in (2 * F, F))
+        for _ in range(2):
+            P.puro_bf16_gated_fprop(x, w, P.ACT_SILU, gate_up, h)
     else:
         raise SystemExit(f"unknown kernel {which!r}: swiglu, rmsnorm, muonh, gemm, gemm_k1536, gemm_oproj, "
-                         "dgrad_quant, quant, quant_small, tensor, bf16, weight, weights, splitk or unfused")
+                         "dgrad_quant, quant, quant_small, tensor, bf16, weight, weights, splitk, unfused, linear_residual, "
+                         "gated, act_backward, gated_backward, qk, qk_backward or skinny")
     torch.cuda.synchronize()
     print("ok", which)
 
