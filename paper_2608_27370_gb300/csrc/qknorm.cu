@@ -383,11 +383,16 @@ __global__ void __launch_bounds__(1024) qk_gain_kernel(const float *__restrict__
     const int from = blockIdx.y ? q_blocks : 0, n = blockIdx.y ? blocks - q_blocks : q_blocks;
     float *out = blockIdx.y ? dk_gain : dq_gain;
     const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = 32 * blockIdx.x + tx;
-    float a = 0.0f;
-    if (c < D) {
-#pragma unroll 4
-        for (int b = ty; b < n; b += 32) a += partial[static_cast<int64_t>(from + b) * D + c];
+    constexpr int kMost = (kQkBwdBlocks + 31) / 32;
+    float v[kMost];  // (all of a share's loads at once: one latency)
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        const int b = ty + 32 * i;
+        v[i] = c < D && b < n ? partial[static_cast<int64_t>(from + b) * D + c] : 0.0f;
     }
+    float a = v[0];
+#pragma unroll
+    for (int i = 1; i < kMost; ++i) a += v[i];
     part[ty][tx] = a;
     __syncthreads();
     if (ty != 0 || c >= D || !out) return;
