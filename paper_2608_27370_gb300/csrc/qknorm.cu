@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(kQkFwdThreads, 5) qk_norm_rope_kernel(const Qk
 // Blocks [0, p.q_blocks) take the query heads, the others the key heads, each a
 // strided share of (token, batch of heads); so a thread sums one gain's
 // gradient, in a fixed order, and a block leaves one partial sum [D].  8192 tokens
-// of 16 + 8 heads of 128 31.5 us with the gains' sum (4.9 TB/s), 32768 of 12 + 2 heads
+// of 16 + 8 heads of 128 30.8 us with the gains' sum (5.0 TB/s), 32768 of 12 + 2 heads
 // 65.8 (5.4 TB/s); one, three, four heads a batch 37, 33, 33 us on the first.
 template <int G, bool INTER>
 __global__ void __launch_bounds__(kQkThreads, 2) qk_norm_rope_backward_kernel(const QkArgs p) {
