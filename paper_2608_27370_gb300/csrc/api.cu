@@ -342,6 +342,11 @@ puro_status_t check_epilogue(const void *bias, int32_t act, const void *residual
     return PURO_OK;
 }
 
+// The map of y for the epilogue's stores of 16 rows of 32 columns.
+bool epilogue_map(const GemmEpilogue &e, int64_t M, int64_t N, GemmMaps *m) {
+    return make_map(&m->d, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, e.y, N, M, N * 2, 32, 16, CU_TENSOR_MAP_SWIZZLE_64B);
+}
+
 puro_status_t fp8_gemm_epilogue(const puro_fp8_tensor_t *x, const puro_fp8_tensor_t *w, const void *bias, int32_t act,
                                 const void *residual, int64_t ld_residual, void *z, void *y, void *workspace,
                                 size_t workspace_bytes, int32_t *dev_status, void *stream) {
@@ -362,6 +367,7 @@ puro_status_t fp8_gemm_epilogue(const puro_fp8_tensor_t *x, const puro_fp8_tenso
         return sms > 0 ? cuda_status(launch_epilogue(nullptr, 0, 0, g.M, g.N, epi, sms, s)) : PURO_ERR_CUDA;
     }
     g.epi = epi;
+    if (action == kGemmLaunch && !epilogue_map(epi, g.M, g.N, &m)) return PURO_ERR_CUDA;
     return run_fp8_gemm(action, g, m, s);
 }
 
@@ -390,6 +396,7 @@ puro_status_t bf16_gemm_epilogue(const void *x, const void *w, int64_t M, int64_
     if (st != PURO_OK) return st;
     g.cluster = cluster;
     g.epi = epi;
+    if (!epilogue_map(epi, M, N, &m)) return PURO_ERR_CUDA;
     return cuda_status(launch_gemm(g, m, s));
 }
 

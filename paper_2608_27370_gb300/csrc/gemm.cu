@@ -564,8 +564,9 @@ PURO_DEV void store_v8(void *p, const uint32_t *v) {
                  : "memory");
 }
 
+// (past L1: what it would keep may be overwritten by bulk stores)
 PURO_DEV void load_v8(const void *p, uint4 &a, uint4 &b) {
-    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+    asm volatile("ld.relaxed.gpu.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w)
                  : "l"(p)
                  : "memory");
@@ -581,6 +582,9 @@ PURO_DEV void load_v8(const void *p, uint4 &a, uint4 &b) {
 // through the warp's kilobyte of staging (64-byte rows, 16-byte chunk c of row r at
 // c ^ (r / 2) % 4), so that a store writes eight 64-byte pieces.
 constexpr int kRowStage = 1024;
+PURO_DEV bool rows_direct(const uint16_t *rows, int64_t ld, int col0, int cols) {
+    return ((reinterpret_cast<uintptr_t>(rows) | static_cast<uintptr_t>(2 * ld)) & 31u) == 0 && col0 + 32 <= cols;
+}
 PURO_DEV void round32(const float (&f)[32], uint32_t (&x)[16]) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -591,7 +595,7 @@ PURO_DEV void round32(const float (&f)[32], uint32_t (&x)[16]) {
 template <bool PAIRS = false>
 PURO_DEV void store_rows32(const uint32_t (&x)[16], uint8_t *stage, uint16_t *out, int64_t ld, int row0, int col0,
                            int rows, int cols, int lane) {
-    if (((reinterpret_cast<uintptr_t>(out) | static_cast<uintptr_t>(2 * ld)) & 31u) == 0 && col0 + 32 <= cols) {
+    if (rows_direct(out, ld, col0, cols)) {
         if constexpr (PAIRS) {  // the pair of lanes exchanges halves: 64 bytes of the even row, then of the odd one
             const bool odd = lane & 1;
             uint32_t even_row[8], odd_row[8];
@@ -666,14 +670,54 @@ PURO_DEV void act32(float (&f)[32], int act) {
     });
 }
 
+// 32 values of each lane's row, rounded to BF16, as two bulk stores of sixteen rows
+// through the warp's ring of kilobytes.  The map (box {32, 16}, 64-byte swizzle) leaves
+// out what lies past the last row or column.  With 32-byte stores of the lanes the next
+// tile's residual waits behind them in the load-store unit: us so and by bulk stores
+// [32768, 1536] x 1536 with a residual 81 and 72, [16384, 2048] x 2048 61 and 58, [8192,
+// 2048] x 512 with gelu, z and a residual 36.7 and 33.2, without a residual the same.  z
+// is stored by the lanes all the same: through this ring too 118, so 108 ([8192, 8960] x
+// 1536 with gelu), and a longer ring takes a stage of the operands' (qkv 80 -> 84).
+struct RowRing {
+    uint8_t *base;
+    int slot;
+};
+template <int SLOTS>
+PURO_DEV uint8_t *free_slot(const RowRing &ring, int lane) {
+    if (lane == 0) bulk_wait_group_read<SLOTS - 1>();
+    __syncwarp();
+    return ring.base + kRowStage * ring.slot;
+}
+template <int SLOTS>
+PURO_DEV void bulk_store_rows32(const float (&f)[32], RowRing &ring, const CUtensorMap *map, int row0, int col0, int rows, int lane) {
+    uint32_t x[16];
+    round32(f, x);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        uint8_t *slot = free_slot<SLOTS>(ring, lane);
+        if ((lane >> 4) == half) {  // 16-byte chunk c of row r at c ^ (r / 2) % 4
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                *reinterpret_cast<uint4 *>(slot + 64 * (lane & 15) + 16 * (c ^ ((lane >> 1) & 3))) =
+                    make_uint4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+            if (row0 + 16 * half < rows) tma_store_2d(map, slot, col0, row0 + 16 * half);
+            bulk_commit_group();
+        }
+        ring.slot = ring.slot + 1 == SLOTS ? 0 : ring.slot + 1;
+    }
+}
+
 // 32 columns of the lane's row of the residual (direct: where 32-byte loads are
 // aligned), or of the warp's rows as store_rows32 stores them; zeros past the last
 // row or column.  (The output may be the residual itself: pieces of less than a sector are
 // loaded past L1, where the part that another SM overwrites would stay as it was, for a
 // kernel that is already waiting there to read it.)
 PURO_DEV bool residual_direct(const GemmEpilogue &epi, int col0, int cols) {
-    return ((reinterpret_cast<uintptr_t>(epi.residual) | static_cast<uintptr_t>(2 * epi.ld_residual)) & 31u) == 0 &&
-           col0 + 32 <= cols;
+    return rows_direct(epi.residual, epi.ld_residual, col0, cols);
 }
 PURO_DEV void load_residual32(uint4 (&v)[4], const GemmEpilogue &epi, int row0, int col0, int rows, int cols, int lane) {
     if (residual_direct(epi, col0, cols)) {
@@ -739,11 +783,13 @@ PURO_DEV void gate32(float (&g)[32], const float (&up)[32], int act) {
 
 // kGemmOutEpilogue and kGemmOutGated.
 template <int KIND, int OUT, int BN, bool SHIFTED, class Smem>
-PURO_DEV void wide_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int warp, int lane, int pair, int num_pairs,
-                            int rank) {
+PURO_DEV void wide_epilogue(Smem &sm, const GemmParams &p, const CUtensorMap *tm_y, uint32_t tmem, int warp, int lane, int pair,
+                            int num_pairs, int rank) {
     constexpr int kAccBufs = SHIFTED ? 1 : 2, kAccShift = SHIFTED ? 128 : 256;
     const int j = (warp - 4) >> 2, q = warp & 3;
-    uint8_t *stage = sm.epi[0] + kRowStage * (warp - 4);
+    constexpr int kSlots = BN == 128 ? 2 : 1;  // of the sixteen kilobytes, for each of the form's warps
+    uint8_t *stage = sm.epi[0] + kRowStage * kSlots * (warp - 4);
+    RowRing ring{stage, 0};
     const uint32_t tempty0 = mapa_shared(smem_u32(&sm.tempty[0]), 0);  // the even CTA's
     float sab = 1.0f;
     if constexpr (KIND == kGemmFP8Tensor) sab = __fmul_rn(*p.sia, *p.sib);
@@ -812,16 +858,21 @@ PURO_DEV void wide_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int wa
                 const int col0 = nq + 32 * c;
                 if (col0 >= p.N) break;
                 if (p.epi.bias) add_bias32(f[c], reinterpret_cast<const uint4 *>(sm.qe.bias[warp - 4]) + 4 * c);
-                if (p.epi.z) store_rows32(f[c], stage, p.epi.z, p.N, row0, col0, p.M, p.N, lane);
+                if (p.epi.z) {
+                    uint8_t *slot = rows_direct(p.epi.z, p.N, col0, p.N) ? stage : free_slot<kSlots>(ring, lane);
+                    store_rows32(f[c], slot, p.epi.z, p.N, row0, col0, p.M, p.N, lane);
+                }
                 act32(f[c], p.epi.act);
                 if (p.epi.residual) {
-                    add_residual32(f[c], res, residual_direct(p.epi, col0, p.N), stage, lane);
+                    const bool direct = residual_direct(p.epi, col0, p.N);
+                    add_residual32(f[c], res, direct, direct ? stage : free_slot<kSlots>(ring, lane), lane);
                     if (c == 0) load_residual32(res, p.epi, row0, nq + 32, p.M, p.N, lane);
                 }
-                store_rows32(f[c], stage, p.epi.y, p.N, row0, col0, p.M, p.N, lane);
+                bulk_store_rows32<kSlots>(f[c], ring, tm_y, row0, col0, p.M, lane);
             }
         }
     }
+    if (OUT == kGemmOutEpilogue && lane == 0) bulk_wait_group0();
 }
 
 // NaN codes with the signs of four BF16 values.
@@ -1175,7 +1226,7 @@ __global__ void __cluster_dims__(2 * S, 1, 1) __launch_bounds__(gemm_threads<OUT
             else
                 gated_quant_epilogue<1>(sm, p, tmem, warp, lane, pair, num_pairs, static_cast<int>(rank));
         } else if constexpr (kWide) {
-            wide_epilogue<KIND, OUT, BN, kShifted>(sm, p, tmem, warp, lane, pair, num_pairs, static_cast<int>(rank));
+            wide_epilogue<KIND, OUT, BN, kShifted>(sm, p, &tm_d, tmem, warp, lane, pair, num_pairs, static_cast<int>(rank));
         }
     } else {
     if constexpr (kRegSplit) reg_dec<kFewRegs>();
