@@ -48,18 +48,6 @@ PURO_DEV Normal normal_both(float z) {
 constexpr float kGeluC = 1.5957691216f;              // 2 sqrt(2 / pi)
 constexpr float kGeluK = 0.044715f * 1.5957691216f;  // gelu_tanh(z) = z sigmoid(z (kGeluC + kGeluK z^2))
 
-// The activation of z (puro_act_t).
-template <int ACT>
-PURO_DEV float act_f32(float z) {
-    if constexpr (ACT == PURO_ACT_RELU) return z < 0.0f ? 0.0f : z;  // (NaN stays)
-    // (e^-u may overflow: the reciprocal is then zero, and the activation below 1e-36)
-    if constexpr (ACT == PURO_ACT_SILU) return z * rcp_approx(1.0f + ex2_approx(z * -1.44269504f));
-    if constexpr (ACT == PURO_ACT_GELU) return z * normal_both(z).cdf;
-    if constexpr (ACT == PURO_ACT_GELU_TANH)
-        return z * rcp_approx(1.0f + ex2_approx(z * fmaf(-1.44269504f * kGeluK, z * z, -1.44269504f * kGeluC)));
-    return z;
-}
-
 PURO_DEV uint64_t splat(float x) { return f32x2(x, x); }
 PURO_DEV uint64_t widen2(uint32_t w) { return f32x2(bf16_lo(w), bf16_hi(w)); }
 // Both BF16 values kept within 128 of zero (NaN stays).
@@ -81,6 +69,43 @@ PURO_DEV uint64_t tanh_gelu_exponent2(uint64_t z) {  // -u log2 e, u = z (kGeluC
     return mul_f32x2(z, fma_f32x2(mul_f32x2(z, z), splat(-1.44269504f * kGeluK), splat(-1.44269504f * kGeluC)));
 }
 
+// -|x| but at least -64, and max(x, 0); NaN stays.
+PURO_DEV float neg_abs_bounded(float x) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(-fabsf(x)), "f"(-64.0f));
+    return r;
+}
+PURO_DEV float relu_nan(float x) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(0.0f));
+    return r;
+}
+
+// The activations of two FP32 values, two an instruction.  GELU as max(z, 0) - |z| q, q =
+// Phi(-|z|) as in normal_both (beyond 64 q is zero, so infinities have their limits).
+template <int ACT>
+PURO_DEV uint64_t act_pair(uint64_t z) {
+    if constexpr (ACT == PURO_ACT_SILU) return mul_f32x2(z, sigmoid2(mul_f32x2(z, splat(-1.44269504f))));
+    if constexpr (ACT == PURO_ACT_GELU_TANH) return mul_f32x2(z, sigmoid2(tanh_gelu_exponent2(z)));
+    if constexpr (ACT == PURO_ACT_RELU || ACT == PURO_ACT_GELU) {
+        float a, b, lo, hi;
+        split_f32x2(z, a, b);
+        const uint64_t pos = f32x2(relu_nan(a), relu_nan(b));
+        if constexpr (ACT == PURO_ACT_RELU) return pos;
+        const uint64_t n = f32x2(neg_abs_bounded(a), neg_abs_bounded(b));
+        split_f32x2(fma_f32x2(n, splat(-0.3275911f * 0.70710678f), splat(1.0f)), lo, hi);
+        const uint64_t t = f32x2(rcp_approx(lo), rcp_approx(hi));
+        split_f32x2(mul_f32x2(mul_f32x2(n, n), splat(-0.72134752f)), lo, hi);
+        const uint64_t e = f32x2(ex2_approx(lo), ex2_approx(hi));
+        uint64_t q = fma_f32x2(t, splat(0.5f * 1.061405429f), splat(0.5f * -1.453152027f));
+        q = fma_f32x2(t, q, splat(0.5f * 1.421413741f));
+        q = fma_f32x2(t, q, splat(0.5f * -0.284496736f));
+        q = fma_f32x2(t, q, splat(0.5f * 0.254829592f));
+        return fma_f32x2(mul_f32x2(n, t), mul_f32x2(q, e), pos);
+    }
+    return z;
+}
+
 // Activations of a BF16 pair, and their slopes, in packed arithmetic.  With s =
 // sigmoid(u), Phi the normal distribution function:
 //   SiLU (u = z):  a = z s,    d = s + z s (1 - s)
@@ -91,11 +116,7 @@ PURO_DEV uint64_t tanh_gelu_exponent2(uint64_t z) {  // -u log2 e, u = z (kGeluC
 // where s is near 1, where d is too.
 template <int ACT>
 PURO_DEV uint64_t act2(uint32_t w) {
-    const uint64_t z = widen2(w);
-    if constexpr (ACT == PURO_ACT_SILU) return mul_f32x2(z, sigmoid2(mul_f32x2(z, splat(-1.44269504f))));
-    if constexpr (ACT == PURO_ACT_GELU_TANH) return mul_f32x2(z, sigmoid2(tanh_gelu_exponent2(z)));
-    if constexpr (ACT != PURO_ACT_NONE) return f32x2(act_f32<ACT>(bf16_lo(w)), act_f32<ACT>(bf16_hi(w)));
-    return z;
+    return act_pair<ACT>(widen2(w));
 }
 template <int ACT>
 PURO_DEV uint64_t slope2(uint32_t w) {
@@ -122,6 +143,14 @@ PURO_DEV uint32_t pack_bf16x2(uint64_t v) {
     split_f32x2(v, lo, hi);
     const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&b);
+}
+
+// The activation of z (puro_act_t).
+template <int ACT>
+PURO_DEV float act_f32(float z) {
+    float lo, hi;
+    split_f32x2(act_pair<ACT>(f32x2(z, 0.0f)), lo, hi);
+    return lo;
 }
 
 // dz = dy * act'(z) of two BF16 pairs; the unrounded values are added to s0, s1.

@@ -666,7 +666,7 @@ PURO_DEV void act32(float (&f)[32], int act) {
     if (act == PURO_ACT_NONE) return;
     act_dispatch(act, [&](auto a) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) f[i] = act_f32<decltype(a)::value>(f[i]);
+        for (int i = 0; i < 16; ++i) split_f32x2(act_pair<decltype(a)::value>(f32x2(f[2 * i], f[2 * i + 1])), f[2 * i], f[2 * i + 1]);
     });
 }
 
@@ -759,24 +759,13 @@ PURO_DEV void add_residual32(float (&f)[32], const uint4 (&v)[4], bool direct, u
     }
 }
 
-// g = act(g) * up.  SwiGLU's products and sums go in pairs.
+// g = act(g) * up, two an instruction.
 PURO_DEV void gate32(float (&g)[32], const float (&up)[32], int act) {
     act_dispatch(act, [&](auto a) {
-        constexpr int ACT = decltype(a)::value;
-        if constexpr (ACT == PURO_ACT_SILU) {
-            const uint64_t m = f32x2(-1.44269504f, -1.44269504f), one = f32x2(1.0f, 1.0f);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const uint64_t z = f32x2(g[2 * i], g[2 * i + 1]);
-                float lo, hi;
-                split_f32x2(mul_f32x2(z, m), lo, hi);
-                split_f32x2(add_f32x2(f32x2(ex2_approx(lo), ex2_approx(hi)), one), lo, hi);
-                const uint64_t s = mul_f32x2(z, f32x2(rcp_approx(lo), rcp_approx(hi)));
-                split_f32x2(mul_f32x2(s, f32x2(up[2 * i], up[2 * i + 1])), g[2 * i], g[2 * i + 1]);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) g[i] = act_f32<ACT>(g[i]) * up[i];
+        for (int i = 0; i < 16; ++i) {
+            const uint64_t h = act_pair<decltype(a)::value>(f32x2(g[2 * i], g[2 * i + 1]));
+            split_f32x2(mul_f32x2(h, f32x2(up[2 * i], up[2 * i + 1])), g[2 * i], g[2 * i + 1]);
         }
     });
 }
@@ -1788,7 +1777,7 @@ __global__ void __launch_bounds__(256) epilogue_kernel(const float *__restrict__
         if (epi.z) out(epi.z);
         act_dispatch(epi.act, [&](auto act) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] = act_f32<decltype(act)::value>(f[k]);
+            for (int k = 0; k < 4; ++k) split_f32x2(act_pair<decltype(act)::value>(f32x2(f[2 * k], f[2 * k + 1])), f[2 * k], f[2 * k + 1]);
         });
         if (epi.residual) add8(f, __ldcg(reinterpret_cast<const uint4 *>(epi.residual + row * epi.ld_residual + col)));
         out(epi.y);
