@@ -547,11 +547,11 @@ PURO_DEV void quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int w
 // tensor-memory lane quarter q, one per lane.  Four warps a scheduler keep the
 // special-function chains of the activations overlapped.  Everything they read
 // (bias, residual) comes straight from global memory, what they write in BF16
-// leaves by plain stores (store_rows32), so rows and columns may end anywhere
-// (columns at a multiple of eight).  us, rotating operands, [8192, 2048] x 6144
-// block-scaled: the plain GEMM 61.7, this epilogue alone 63.5, with bias 64.0, SiLU
-// 64.6, GELU 68.2, a residual (33 MB more) 67.1; [32768, 2048] x 1536 77-79, 80, 82, 81,
-// 96, 103.
+// leaves by plain stores (store_rows32) or bulk stores of few rows, so rows and
+// columns may end anywhere (columns at a multiple of eight).  us, rotating operands,
+// [8192, 2048] x 6144 block-scaled: the plain GEMM 62.3, this epilogue alone 63.7,
+// with bias 64.3, SiLU 64.5, GELU 66.5, a residual (33 MB more) 67.7; [32768, 2048] x
+// 1536 65.2, 70.0, 70.7, 69.9, 75.6, 80.8.
 template <int OUT, int BN, int S>
 constexpr bool wide_epilogue_form() {
     return S == 1 && (OUT == kGemmOutEpilogue || OUT == kGemmOutGated || OUT == kGemmOutGatedQuant);
@@ -879,8 +879,8 @@ PURO_DEV uint32_t nan_codes4(uint32_t a, uint32_t b) { return 0x7F7F7F7Fu | (__b
 // shape, 7250 of them the epilogue's, and 7430 without stores: they compete with the
 // operands' loads for L2, by requests more than by bytes (confined to 1 MB they cost
 // the same), so gate and up leave in 64-byte pieces (in 32-byte ones 775, 166).
-// Codes gathered in shared memory and stored as 128-byte rows: 740, 162, for the
-// barriers.  The stores of gate and up come first: behind the maxima, to fill the
+// By bulk stores, as a linear's y: 756, so 690.  Codes gathered in shared memory and
+// stored as 128-byte rows: 740, so 712, for the barriers.  The stores of gate and up come first: behind the maxima, to fill the
 // barriers' waits, 895 and 183.  The codes of a tile's copies are computed without a
 // branch for each four, which would end their overlap (826 -> 738 on the first).
 template <int FMT, class Smem>
