@@ -576,10 +576,9 @@ PURO_DEV void load_v8(const void *p, uint4 &a, uint4 &b) {
 // (rows ld elements apart), rows below `rows` and columns below `cols` only.  Two
 // 32-byte stores a lane, whole sectors, where the rows are aligned for them ([8192,
 // 8960] x 1536 with gelu and z 125 -> 99 us).  PAIRS: as 64-byte pieces of two lanes,
-// fewer requests for more instructions (worth it behind the gated form, but 77 -> 89
-// us on [8192, 2048] x 6144 with a residual, whose warps store before they release the
-// accumulator).  Otherwise sixteen rows at a time go
-// through the warp's kilobyte of staging (64-byte rows, 16-byte chunk c of row r at
+// fewer requests for more instructions and registers (worth it behind the gated form,
+// but with a linear's residual 77 -> 89 us on [8192, 2048] x 6144).  Otherwise sixteen
+// rows at a time go through the warp's kilobyte of staging (64-byte rows, 16-byte chunk c of row r at
 // c ^ (r / 2) % 4), so that a store writes eight 64-byte pieces.
 constexpr int kRowStage = 1024;
 PURO_DEV bool rows_direct(const uint16_t *rows, int64_t ld, int col0, int cols) {

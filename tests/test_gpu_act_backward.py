@@ -100,6 +100,23 @@ def test_fp8_form(rows, cols, fmt, act):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("act", L.ACTS)
+def test_every_finite_value_through_the_slope(act):
+    """dz of dy = 1, and [dgate, dup] of dh = up = 1: the slope, and the activation."""
+    _need_gpu()
+    z = torch.arange(65536, dtype=torch.int32, device=DEV).to(torch.int16).view(BF)
+    z = z[torch.isfinite(z)].view(-1, 8)
+    one, dz = torch.ones_like(z), torch.empty_like(z)
+    P.puro_act_backward_bf16(one, None if act == "none" else z, CODE[act], dz, None)
+    zd = z.double().cpu()
+    _close(dz, L.slope(zd, act), torch.ones_like(zd))
+    out = torch.empty(z.shape[0], 16, dtype=BF, device=DEV)
+    P.puro_gated_backward_bf16(one, z, one, CODE[act], out)
+    _close(out[:, :8], L.slope(zd, act), torch.ones_like(zd))
+    _close(out[:, 8:], L.act(zd, act), zd.abs().clamp(min=1))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("act", L.ACTS[1:])
 def test_far_and_not_finite_values(act):
     """Slopes at the ends: 0 and 1, NaN for NaN alone."""

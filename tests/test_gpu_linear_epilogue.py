@@ -162,6 +162,25 @@ def test_not_finite_values_stay_in_their_rows():
     assert bad.nonzero().flatten().tolist() == [7, 20]
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("m", [8160, 16])
+@pytest.mark.parametrize("act", L.ACTS)
+def test_every_finite_value_through_the_activation(act, m):
+    """x times the identity is x, exactly, so y is the activation of every finite BF16 value."""
+    _need_gpu()
+    x = torch.arange(65536, dtype=torch.int32, device=DEV).to(torch.int16).view(BF)
+    x = x[torch.isfinite(x)].view(m, -1)
+    eye = torch.eye(x.shape[1], dtype=BF, device=DEV)
+    y, h = torch.empty_like(x), torch.empty_like(x)
+    P.puro_bf16_linear_fprop_epilogue(x, eye, y, None, CODE[act])
+    ref, err = L.act(x.double(), act), 0 if act in ("none", "relu") else _act_error(x.double(), 0)
+    _within(y, ref, err + torch.zeros_like(ref))
+    P.puro_bf16_gated_fprop(x, torch.cat([eye, eye]), CODE[act], None, h)
+    small = x.double().abs() < 1e15  # (the product is finite)
+    # (below 2^-126 half a BF16 step is 2^-134, whatever the value, and FP32's 2^-150)
+    _within(h[small], (ref * x.double())[small], ((err + 2.0 ** -23 * ref.abs()) * x.double().abs())[small] + 2.0 ** -133)
+
+
 def _quantized(rows, cols):
     op = lambda r, c: P.FP8Operand(torch.full((r, c), 0x55, dtype=u8, device=DEV),  # noqa: E731
                                    P.empty_scales(r, c, P.SCALE_BLOCK, P.ROLE_ACT, DEV).fill_(0x55))
