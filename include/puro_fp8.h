@@ -22,6 +22,8 @@
  *     puro_fp8_get_status, which says so) and keeps no state between calls.
  *   - Overlap: an output may not overlap an input or another output, unless
  *     the call says which may be the same.
+ *   - Scratch: a workspace belongs to its call until that call's work is done;
+ *     calls that may run at the same time, graphs among them, need one each.
  *   - Ordering: all work is enqueued on `stream` (a cudaStream_t passed as
  *     void*; NULL is the legacy default stream) in call order.
  *   - Pointers: device pointers unless marked "host".  Every tensor pointer
