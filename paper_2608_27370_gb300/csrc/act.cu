@@ -21,6 +21,7 @@ constexpr int kActCols = 256;                // columns of a block: 32 threads o
 constexpr int kActRows = 8;                  // rows of threads
 constexpr int kActBatch = 2;                 // rows of a thread loaded at once
 constexpr int64_t kActBlocks = 152 * 4;      // blocks at most: four an SM are resident
+constexpr int kGateBlocks = 4;               // of the gate's kernel an SM
 
 ActBackwardPlan plan_act_backward(int64_t rows, int64_t cols) {
     const int64_t strips = (cols + kActCols - 1) / kActCols;
@@ -121,15 +122,10 @@ cudaError_t launch_column_sums(const float *partial, int64_t n, int64_t cols, fl
 
 // [dgate, dup] of eight columns of a row a thread and step.  Blocks an SM, and us at
 // four / five / six: SiLU [8192, 6144] 74.9 / 81.0 / 75.1, [777, 6144] 9.2 / 9.0 / 9.4, tanh
-// GELU 74.7 / 78.9 / 80.2 and 9.2 / 10.1 / 10.2, but GELU, which computes longer, 81.6 / 88.5 /
-// 79.5 and 10.3 / 10.8 / 9.9 (floors 74.2 and 7.0; eight blocks with a division a step: SiLU
-// 91.6 and 10.6).
+// GELU 74.7 / 78.9 / 80.2 and 9.2 / 10.1 / 10.2; GELU at four / six 77.0 / 81.2 and 9.6 / 9.8
+// (floors 74.2 and 7.0; eight with a division a step and SiLU 91.6 and 10.6).
 template <int ACT>
-constexpr int gate_blocks() {
-    return ACT == PURO_ACT_GELU ? 6 : 4;
-}
-template <int ACT>
-__global__ void __launch_bounds__(256, gate_blocks<ACT>()) gated_backward_kernel(const uint16_t *__restrict__ dh,
+__global__ void __launch_bounds__(256, kGateBlocks) gated_backward_kernel(const uint16_t *__restrict__ dh,
                                                                        const uint16_t *__restrict__ gate,
                                                                        const uint16_t *__restrict__ up, int64_t rows, int64_t cols,
                                                                        int64_t ld, uint16_t *__restrict__ dgate_up) {
@@ -157,20 +153,14 @@ __global__ void __launch_bounds__(256, gate_blocks<ACT>()) gated_backward_kernel
 
 cudaError_t launch_gated_backward(const uint16_t *dh, const uint16_t *gate, const uint16_t *up, int64_t rows, int64_t cols,
                                   int64_t ld, int act, uint16_t *dgate_up, cudaStream_t s) {
-    const int64_t want = (rows * (cols / 8) + 255) / 256;
-    auto launch = [&](auto a) {
-        constexpr int ACT = decltype(a)::value;
-        const int64_t cap = 152 * gate_blocks<ACT>();
-        return launch_pdl(gated_backward_kernel<ACT>, dim3(static_cast<unsigned>(want < cap ? want : cap)), dim3(256), 0, s, dh, gate,
-                          up, rows, cols, ld, dgate_up);
-    };
-    switch (act) {
-        case PURO_ACT_RELU: return launch(std::integral_constant<int, PURO_ACT_RELU>{});
-        case PURO_ACT_SILU: return launch(std::integral_constant<int, PURO_ACT_SILU>{});
-        case PURO_ACT_GELU: return launch(std::integral_constant<int, PURO_ACT_GELU>{});
-        case PURO_ACT_GELU_TANH: return launch(std::integral_constant<int, PURO_ACT_GELU_TANH>{});
-        default: return launch(std::integral_constant<int, PURO_ACT_NONE>{});
-    }
+    auto kern = act == PURO_ACT_RELU        ? gated_backward_kernel<PURO_ACT_RELU>
+                : act == PURO_ACT_SILU      ? gated_backward_kernel<PURO_ACT_SILU>
+                : act == PURO_ACT_GELU      ? gated_backward_kernel<PURO_ACT_GELU>
+                : act == PURO_ACT_GELU_TANH ? gated_backward_kernel<PURO_ACT_GELU_TANH>
+                                            : gated_backward_kernel<PURO_ACT_NONE>;
+    const int64_t want = (rows * (cols / 8) + 255) / 256, cap = 152 * kGateBlocks;
+    return launch_pdl(kern, dim3(static_cast<unsigned>(want < cap ? want : cap)), dim3(256), 0, s, dh, gate, up, rows, cols, ld,
+                      dgate_up);
 }
 
 }  // namespace puro
