@@ -58,16 +58,25 @@ PURO_DEV uint32_t bounded2(uint32_t w) {
     return r;
 }
 
-// sigmoid(u) from v = -u log2 e, two at a time.  (e^-u may overflow: the reciprocal
-// is then zero.)
-PURO_DEV uint64_t sigmoid2(uint64_t v) {
+// sigmoid(u) = 1 / (1 + 2^v), v = -u log2 e, two at a time, from v - 15: 2^15 sigmoid =
+// 1 / (2^-15 + 2^(v - 15)), so that neither the power nor the reciprocal leaves the normal
+// range before v = 141, where |z| sigmoid is below half of BF16's last subnormal (unscaled
+// they do from v = 126 on: SiLU of -88 came out as 0 for -5.3e-37).  The exact scaling by
+// 2^-15 gives subnormals too; beyond, the sigmoid is zero.  The rounding of v - 15 costs at
+// most 2^-21.5 of the sigmoid above z = -4.8.
+constexpr float kSigmoidShift = 15.0f, kSigmoidScale = 0x1p-15f;
+PURO_DEV uint64_t sigmoid2(uint64_t v_less_shift) {
     float lo, hi;
-    split_f32x2(v, lo, hi);
-    split_f32x2(add_f32x2(f32x2(ex2_approx(lo), ex2_approx(hi)), splat(1.0f)), lo, hi);
-    return f32x2(rcp_approx(lo), rcp_approx(hi));
+    split_f32x2(v_less_shift, lo, hi);
+    split_f32x2(add_f32x2(f32x2(ex2_approx(lo), ex2_approx(hi)), splat(kSigmoidScale)), lo, hi);
+    return mul_f32x2(f32x2(rcp_approx(lo), rcp_approx(hi)), splat(kSigmoidScale));
 }
-PURO_DEV uint64_t tanh_gelu_exponent2(uint64_t z) {  // -u log2 e, u = z (kGeluC + kGeluK z^2)
-    return mul_f32x2(z, fma_f32x2(mul_f32x2(z, z), splat(-1.44269504f * kGeluK), splat(-1.44269504f * kGeluC)));
+PURO_DEV uint64_t silu_exponent2(uint64_t z) {  // v - 15, u = z
+    return fma_f32x2(z, splat(-1.44269504f), splat(-kSigmoidShift));
+}
+PURO_DEV uint64_t tanh_gelu_exponent2(uint64_t z) {  // v - 15, u = z (kGeluC + kGeluK z^2)
+    const uint64_t f = fma_f32x2(mul_f32x2(z, z), splat(-1.44269504f * kGeluK), splat(-1.44269504f * kGeluC));
+    return fma_f32x2(z, f, splat(-kSigmoidShift));
 }
 
 // -|x| but at least -64, and max(x, 0); NaN stays.
@@ -86,7 +95,7 @@ PURO_DEV float relu_nan(float x) {
 // Phi(-|z|) as in normal_both (beyond 64 q is zero, so infinities have their limits).
 template <int ACT>
 PURO_DEV uint64_t act_pair(uint64_t z) {
-    if constexpr (ACT == PURO_ACT_SILU) return mul_f32x2(z, sigmoid2(mul_f32x2(z, splat(-1.44269504f))));
+    if constexpr (ACT == PURO_ACT_SILU) return mul_f32x2(z, sigmoid2(silu_exponent2(z)));
     if constexpr (ACT == PURO_ACT_GELU_TANH) return mul_f32x2(z, sigmoid2(tanh_gelu_exponent2(z)));
     if constexpr (ACT == PURO_ACT_RELU || ACT == PURO_ACT_GELU) {
         float a, b, lo, hi;
@@ -133,7 +142,7 @@ PURO_DEV uint64_t slope2(uint32_t w) {
         return fma_f32x2(mul_f32x2(z, splat(0.39894228f)), f32x2(n0.bell, n1.bell), f32x2(n0.cdf, n1.cdf));
     }
     constexpr bool kTanh = ACT == PURO_ACT_GELU_TANH;
-    const uint64_t s = sigmoid2(kTanh ? tanh_gelu_exponent2(z) : mul_f32x2(z, splat(-1.44269504f)));
+    const uint64_t s = sigmoid2(kTanh ? tanh_gelu_exponent2(z) : silu_exponent2(z));
     uint64_t bell = mul_f32x2(mul_f32x2(z, s), fma_f32x2(s, splat(-1.0f), splat(1.0f)));
     if constexpr (kTanh) bell = mul_f32x2(bell, fma_f32x2(mul_f32x2(z, z), splat(3.0f * kGeluK), splat(kGeluC)));
     return add_f32x2(bell, s);
