@@ -27,22 +27,33 @@ PURO_DEV float rcp_approx(float x) {
     return y;
 }
 
-// The normal distribution function Phi(z) and e^(-z^2/2), by formula 7.1.26 of
-// Abramowitz and Stegun, Handbook of Mathematical Functions (erf to 1.5e-7 by a
-// polynomial in 1 / (1 + p x) times e^(-x^2), x = |z| / sqrt(2)); with the FP32
-// roundings Phi is within 2^-21.  Behind the GEMM's epilogue CUDA's normcdff
-// made it the bound: [8192, 2048] x 6144 84.9 us.  Slopes take it one value at a time:
-// two an instruction, as act_pair does, 76.6 us for 74.0 on [8192, 8960] with dbias.
+// The normal distribution function Phi(z) and its bell.  Phi(-x) e^(x^2/2), x >= 0 (Mills'
+// ratio over sqrt(2 pi)), falls off as 1 / x, so it is t P(t), t = 1 / (1 + p x), P a polynomial
+// of degree 6.  p and P have the least maximum over 0 <= x <= 14 of the error of Phi(-x) over
+// min(7.5e-8, 2^-16 Phi(-x)), found by linear programming on a grid: 2.0e-8 and, in the tail,
+// 2^-17.9 of its value; with the FP32 roundings 2.2e-7 and 2^-17.  The bell is taken 16 times as
+// large, which costs no rounding near zero and keeps every normal GELU and slope (it is zero below
+// z = -13.4).  Formula 7.1.26 of Abramowitz and Stegun's Handbook, two terms shorter, bounds the
+// absolute error alone (1.5e-7 of erf): 0.16% off at -5, 2% at -10.  CUDA's normcdff, which holds
+// the tail too, made the GEMM's epilogue its bound: [8192, 2048] x 6144 84.9 us.  Slopes take it
+// one value at a time (two an instruction, of the shorter formula: 76.6 us for 74.0 on [8192, 8960]).
+constexpr float kBell = 16.0f, kBellLog2 = 4.0f;
+constexpr float kMillsP = 0.255f;
+constexpr float kMills0 = 0.1013295054f / kBell, kMills1 = 0.1078548532f / kBell, kMills2 = 0.0569961062f / kBell, kMills3 = 0.2068689727f / kBell,
+                kMills4 = -0.1678357881f / kBell, kMills5 = 0.2753503274f / kBell, kMills6 = -0.0805639588f / kBell;
 struct Normal {
-    float cdf, bell;
+    float cdf, bell;  // Phi(z), kBell e^(-z^2/2)
 };
 PURO_DEV Normal normal_both(float z) {
-    const float t = rcp_approx(fmaf(fabsf(z), 0.3275911f * 0.70710678f, 1.0f));
-    const float e = ex2_approx(z * z * -0.72134752f);
-    float q = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
-    q = fmaf(t, q, 0.5f * 1.421413741f);
-    q = fmaf(t, q, 0.5f * -0.284496736f);
-    q = fmaf(t, q, 0.5f * 0.254829592f) * (t * e);
+    const float t = rcp_approx(fmaf(fabsf(z), kMillsP, 1.0f));
+    const float e = ex2_approx(fmaf(z * z, -0.72134752f, kBellLog2));
+    float q = fmaf(t, kMills6, kMills5);
+    q = fmaf(t, q, kMills4);
+    q = fmaf(t, q, kMills3);
+    q = fmaf(t, q, kMills2);
+    q = fmaf(t, q, kMills1);
+    q = fmaf(t, q, kMills0);
+    q = t * q * e;
     return Normal{z >= 0.0f ? 1.0f - q : q, e};
 }
 
@@ -103,15 +114,17 @@ PURO_DEV uint64_t act_pair(uint64_t z) {
         const uint64_t pos = f32x2(relu_nan(a), relu_nan(b));
         if constexpr (ACT == PURO_ACT_RELU) return pos;
         const uint64_t n = f32x2(neg_abs_bounded(a), neg_abs_bounded(b));
-        split_f32x2(fma_f32x2(n, splat(-0.3275911f * 0.70710678f), splat(1.0f)), lo, hi);
+        split_f32x2(fma_f32x2(n, splat(-kMillsP), splat(1.0f)), lo, hi);
         const uint64_t t = f32x2(rcp_approx(lo), rcp_approx(hi));
-        split_f32x2(mul_f32x2(mul_f32x2(n, n), splat(-0.72134752f)), lo, hi);
+        split_f32x2(fma_f32x2(mul_f32x2(n, n), splat(-0.72134752f), splat(kBellLog2)), lo, hi);
         const uint64_t e = f32x2(ex2_approx(lo), ex2_approx(hi));
-        uint64_t q = fma_f32x2(t, splat(0.5f * 1.061405429f), splat(0.5f * -1.453152027f));
-        q = fma_f32x2(t, q, splat(0.5f * 1.421413741f));
-        q = fma_f32x2(t, q, splat(0.5f * -0.284496736f));
-        q = fma_f32x2(t, q, splat(0.5f * 0.254829592f));
-        return fma_f32x2(mul_f32x2(n, t), mul_f32x2(q, e), pos);
+        uint64_t q = fma_f32x2(t, splat(kMills6), splat(kMills5));
+        q = fma_f32x2(t, q, splat(kMills4));
+        q = fma_f32x2(t, q, splat(kMills3));
+        q = fma_f32x2(t, q, splat(kMills2));
+        q = fma_f32x2(t, q, splat(kMills1));
+        q = fma_f32x2(t, q, splat(kMills0));
+        return fma_f32x2(mul_f32x2(n, mul_f32x2(t, q)), e, pos);
     }
     return z;
 }
@@ -139,7 +152,7 @@ PURO_DEV uint64_t slope2(uint32_t w) {
     const uint64_t z = widen2(wb);
     if constexpr (ACT == PURO_ACT_GELU) {
         const Normal n0 = normal_both(bf16_lo(wb)), n1 = normal_both(bf16_hi(wb));
-        return fma_f32x2(mul_f32x2(z, splat(0.39894228f)), f32x2(n0.bell, n1.bell), f32x2(n0.cdf, n1.cdf));
+        return fma_f32x2(mul_f32x2(z, splat(0.39894228f / kBell)), f32x2(n0.bell, n1.bell), f32x2(n0.cdf, n1.cdf));
     }
     constexpr bool kTanh = ACT == PURO_ACT_GELU_TANH;
     const uint64_t s = sigmoid2(kTanh ? tanh_gelu_exponent2(z) : silu_exponent2(z));

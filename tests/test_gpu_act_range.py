@@ -8,20 +8,24 @@ import paper_2608_27370_gb300 as P
 
 DEV, BF = "cuda", torch.bfloat16
 CODE = dict(zip(L.ACTS, (P.ACT_NONE, P.ACT_RELU, P.ACT_SILU, P.ACT_GELU, P.ACT_GELU_TANH)))
-KINDS = ("silu", "gelu_tanh")
+KINDS = ("silu", "gelu_tanh", "gelu")
 
 # Before the rounding to BF16, relative to the value (for a slope: to the magnitudes of its two terms).  The exponent v of
 # e^-u = 2^v is at most 141 where a result is not zero in BF16, and it is off by at most
 # SiLU: 2^-18 (the rounding of v - 15, below 128) and 141 * 2^-25 (log2 e): e^-u by 0.69 * 8.0e-6, with ex2 and rcp (2^-22
 #       each) and two roundings below 6.2e-6 < 2^-17;
 # tanh GELU: 141 * (3 roundings of 2^-24, constants of 2^-24) and 2^-18: 0.69 * 3.8e-5 and those, below 2^-15.
+# GELU: Phi's tail by 2^-17.9; e^(-z^2/2) = 2^v by 0.69 * (130 * (2^-24 of z^2 + 2^-25 of the constant) + 2^-18), the
+#       polynomial and products 16 * 2^-24: below 2^-15.
 # A slope has one product more of each, and tanh GELU's u' its roundings: twice as much.
-REL = {"silu": 2.0 ** -17, "gelu_tanh": 2.0 ** -15}
+REL = {"silu": 2.0 ** -17, "gelu_tanh": 2.0 ** -15, "gelu": 2.0 ** -15}
 # Absolutely: half a step of a BF16 subnormal, 2^-134, and FP32's subnormals (2^-150, times a factor of at most 128).  A
 # sigmoid below 2^-141 is zero: less than half such a step of SiLU (|z| < 2^6.7), of its slope and of tanh GELU (|z| <
-# 2^3.4), but not of tanh GELU's slope (|z u'| < 2^8.1).
-TINY = 2.0 ** -134 + 2.0 ** -142
-TINY_SLOPE = {"silu": TINY, "gelu_tanh": 2.0 ** -132.9 + 2.0 ** -142}
+# 2^3.4), but not of tanh GELU's slope (|z u'| < 2^8.1).  GELU's bell below 2^-130 is zero, from z = -13.43 on: GELU is
+# below 2^-131.3 there and its slope below 2^-127.5, so both may be zero for a subnormal.
+SUB = 2.0 ** -142
+TINY = {"silu": 2.0 ** -134 + SUB, "gelu_tanh": 2.0 ** -134 + SUB, "gelu": 2.0 ** -131.3 + SUB}
+TINY_SLOPE = {"silu": 2.0 ** -134 + SUB, "gelu_tanh": 2.0 ** -132.9 + SUB, "gelu": 2.0 ** -127.5 + SUB}
 
 
 def _need_gpu():
@@ -34,7 +38,7 @@ def _every_finite_value():
     return z[torch.isfinite(z)].view(-1, 16)
 
 
-def _check(got, ref, size, rel, tiny=TINY):
+def _check(got, ref, size, rel, tiny):
     """Half a BF16 step (2^-8 of the value) and the error before the rounding."""
     err = rel * size
     bad = (got.double() - ref).abs() > 2.0 ** -8 * (ref.abs() + err) + err + tiny
@@ -61,9 +65,9 @@ def test_activation_relative_to_its_value(kind, m):
     eye = torch.eye(z.shape[1], dtype=BF, device=DEV)
     ref, y, h = L.act(z.double(), kind), torch.empty_like(z), torch.empty_like(z)
     P.puro_bf16_linear_fprop_epilogue(z, eye, y, None, CODE[kind])
-    _check(y, ref, ref.abs(), REL[kind])
+    _check(y, ref, ref.abs(), REL[kind], TINY[kind])
     P.puro_bf16_gated_fprop(*_gate_by_one(z), CODE[kind], None, h)
-    _check(h, ref, ref.abs(), REL[kind])
+    _check(h, ref, ref.abs(), REL[kind], TINY[kind])
 
 
 @pytest.mark.gpu
@@ -81,7 +85,7 @@ def test_slope_relative_to_its_terms(kind):
     _check(dz, d, size, 2 * REL[kind], TINY_SLOPE[kind])
     P.puro_gated_backward_bf16(one, z, one, CODE[kind], out)
     _check(out[:, :16], d, size, 2 * REL[kind], TINY_SLOPE[kind])
-    _check(out[:, 16:], a, a.abs(), REL[kind])
+    _check(out[:, 16:], a, a.abs(), REL[kind], TINY[kind])
 
 
 @pytest.mark.gpu
