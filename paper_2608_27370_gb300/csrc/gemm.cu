@@ -64,6 +64,7 @@
 #include "internal.h"
 #include "ptx.cuh"
 #include "quant_math.cuh"
+#include "register_check.h"
 
 namespace puro {
 
@@ -2009,11 +2010,17 @@ static cudaError_t launch_params(const GemmParams &p, const GemmArgs &g, const G
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
     if constexpr (register_split<OUT, BN>()) {
-        static const bool enough = [&] {
+        static RegisterCheck check;
+        int dev = 0;
+        e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        e = check.enough(dev, gemm_threads<OUT, BN>() / 32, 4 * kFewRegs + 16 * kManyRegs, [&](int *regs) {
             cudaFuncAttributes at{};
-            return cudaFuncGetAttributes(&at, kern) == cudaSuccess && at.numRegs * 20 >= 4 * kFewRegs + 16 * kManyRegs;
-        }();
-        if (!enough) return cudaErrorLaunchOutOfResources;
+            const cudaError_t q = cudaFuncGetAttributes(&at, kern);
+            *regs = at.numRegs;
+            return q;
+        });
+        if (e != cudaSuccess) return e;
     }
     const int pairs_max = max_resident_pairs<KIND, OUT, BN>(g.num_sms, smem);
     const int pairs = p.num_units < pairs_max ? p.num_units : pairs_max;
