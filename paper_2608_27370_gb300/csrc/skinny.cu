@@ -12,11 +12,13 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "act_math.cuh"
 #include "internal.h"
 #include "ptx.cuh"
 #include "quant_math.cuh"
+#include "skinny_plan.h"
 
 namespace puro {
 
@@ -36,12 +38,14 @@ PURO_DEV void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, ui
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+constexpr int skinny_unroll(bool gated) { return gated ? 2 : 3; }  // steps of 32 k that a warp loads at once
+
 // One block: columns 8 blockIdx.x .. + 7 of the output (GATED: of h, from those
 // rows of the gate and of up).  Up to 8 ROWS tokens.
 template <int WARPS, bool GATED, int ROWS>
 __global__ void __launch_bounds__(WARPS * 32) skinny_linear_kernel(const uint16_t *__restrict__ x, const uint16_t *__restrict__ w,
                                                                   int M, int N, int K, const GemmEpilogue epi) {
-    constexpr int kTiles = GATED ? 2 : 1, kUnroll = GATED ? 2 : 3;
+    constexpr int kTiles = GATED ? 2 : 1, kUnroll = skinny_unroll(GATED);
     constexpr int kMmas = (ROWS + 1) / 2;  // of sixteen tokens
     __shared__ float part[WARPS][kTiles][8 * ROWS][8];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
@@ -133,31 +137,58 @@ __global__ void __launch_bounds__(WARPS * 32) skinny_linear_kernel(const uint16_
     }
 }
 
-template <int WARPS, bool GATED>
-static cudaError_t launch_warps(const uint16_t *x, const uint16_t *w, int64_t M, int64_t N, int64_t K, const GemmEpilogue &epi,
-                                cudaStream_t s) {
-    auto kern = M > 16  ? skinny_linear_kernel<WARPS, GATED, 4>
-                : M > 8 ? skinny_linear_kernel<WARPS, GATED, 2>
-                        : skinny_linear_kernel<WARPS, GATED, 1>;
-    return launch_pdl(kern, dim3(static_cast<unsigned>(N / 8)), dim3(WARPS * 32), 0, s, x, w, static_cast<int>(M),
-                      static_cast<int>(N), static_cast<int>(K), epi);
+// (Linears of 17 to 32 tokens: as many blocks of 6 warps as of 8 are resident, of 12 as of 16.)
+template <int WARPS, bool GATED, int ROWS>
+constexpr bool skinny_built() { return GATED || ROWS < 4 || (WARPS != 6 && WARPS != 12); }
+
+// Blocks of a kernel that are resident at once, cached per device (0: not built, or the query failed, and is asked again).
+template <int WARPS, bool GATED, int ROWS>
+static int64_t resident_blocks(int dev) {
+    if constexpr (!skinny_built<WARPS, GATED, ROWS>()) return 0;
+    else {
+        static std::atomic<int> cache[64] = {};
+        const bool keep = dev >= 0 && dev < 64;
+        int n = keep ? cache[dev].load(std::memory_order_relaxed) : 0;
+        if (n > 0) return n;
+        int per_sm = 0, sms = 0;
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, skinny_linear_kernel<WARPS, GATED, ROWS>, WARPS * 32, 0) != cudaSuccess ||
+            cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return 0;
+        }
+        n = per_sm * sms;
+        if (keep) cache[dev].store(n, std::memory_order_relaxed);
+        return n;
+    }
 }
 
-// Warps a block, which share the reduction: as many as keep the launch within a
-// number of warps that are resident at once, since more blocks already spread the
-// loads.  One token, us, weights out of L2 in a graph, at 4 / 8 / 16 warps: linear
-// [1536] x 8960 (192 blocks) 14.9 / 9.0 / 6.9, [8960] x 1536 (1120 blocks) 7.3 /
-// 7.9 / 9.5 (6 warps: 6.2); gated [1024] x 1024 3.2 / 2.5 / 1.9, [8960] x 1536 10.8 /
-// 10.7 / 12.5.  Without the prefetch the first takes 10.6 and the last 10.8.
-template <bool GATED>
-static cudaError_t launch_skinny(const uint16_t *x, const uint16_t *w, int64_t M, int64_t N, int64_t K, const GemmEpilogue &epi,
-                                 cudaStream_t s) {
-    const int64_t blocks = N / 8, most = GATED ? 9300 : 6800;
-    if (blocks * 16 <= most) return launch_warps<16, GATED>(x, w, M, N, K, epi, s);
-    if (blocks * 12 <= most) return launch_warps<12, GATED>(x, w, M, N, K, epi, s);
-    if (blocks * 8 <= most) return launch_warps<8, GATED>(x, w, M, N, K, epi, s);
-    if (blocks * 6 <= most) return launch_warps<6, GATED>(x, w, M, N, K, epi, s);
-    return launch_warps<4, GATED>(x, w, M, N, K, epi, s);
+// Warps a block, which share the reduction: by skinny_form.  One token, us, in a graph,
+// at least 400 MB of weights in turn, at 4 / 6 / 8 / 12 / 16 warps: linear [1536] x 8960 (192
+// blocks) 33.9 / 23.7 / 14.1 / 14.8 / 7.7, [4096] x 2048 10.2 / 7.5 / 5.3 / 4.9 / 5.5, [8960] x
+// 1536 9.1 / 10.2 / 7.2 / 8.2 / 9.3, [9216] x 1536 9.5 / 10.3 / 7.4 / 8.3 / 9.4, [17920] x 1536 16.6 /
+// 16.2 / 11.6 / 16.0 / 16.9; gated [1024] x 1024 4.4 / 3.1 / 3.1 / 3.6 / 2.1, [6144] x 2048 14.5 / 12.8
+// / 14.4 / 14.2 / 16.0, [8960] x 1536 13.7 / 15.1 / 13.8 / 15.6 / 18.7.  Over 211 widths, reductions
+// and numbers of tokens (1 to 32) the rule's choice is 2.1% slower than the fastest of the
+// five in the geometric mean and 20% at most ([8192] x 512 on 32 tokens).
+template <bool GATED, int ROWS>
+static cudaError_t launch_rows(const uint16_t *x, const uint16_t *w, int64_t M, int64_t N, int64_t K, const GemmEpilogue &epi,
+                               cudaStream_t s) {
+    int dev = 0;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const int64_t resident[kSkinnyForms] = {resident_blocks<16, GATED, ROWS>(dev), resident_blocks<8, GATED, ROWS>(dev),
+                                            resident_blocks<6, GATED, ROWS>(dev), resident_blocks<12, GATED, ROWS>(dev),
+                                            resident_blocks<4, GATED, ROWS>(dev)};
+    const int warps = kSkinnyWarps[skinny_form(N / 8, (K + 31) / 32, skinny_unroll(GATED), resident)];
+    auto kern = warps == 16  ? skinny_linear_kernel<16, GATED, ROWS>
+                : warps == 8 ? skinny_linear_kernel<8, GATED, ROWS>
+                             : skinny_linear_kernel<4, GATED, ROWS>;
+    if constexpr (skinny_built<6, GATED, ROWS>())
+        if (warps == 6) kern = skinny_linear_kernel<6, GATED, ROWS>;
+    if constexpr (skinny_built<12, GATED, ROWS>())
+        if (warps == 12) kern = skinny_linear_kernel<12, GATED, ROWS>;
+    return launch_pdl(kern, dim3(static_cast<unsigned>(N / 8)), dim3(warps * 32), 0, s, x, w, static_cast<int>(M),
+                      static_cast<int>(N), static_cast<int>(K), epi);
 }
 
 // Up to 16 tokens, and up to 32 where the weight is small: every block reads all
@@ -174,7 +205,10 @@ bool is_skinny_linear(int64_t M, int64_t N, int64_t K, bool gated) {
 
 cudaError_t launch_skinny_linear(const uint16_t *x, const uint16_t *w, int64_t M, int64_t N, int64_t K, bool gated,
                                  const GemmEpilogue &epi, cudaStream_t s) {
-    return gated ? launch_skinny<true>(x, w, M, N, K, epi, s) : launch_skinny<false>(x, w, M, N, K, epi, s);
+    auto launch = M > 16  ? (gated ? launch_rows<true, 4> : launch_rows<false, 4>)
+                  : M > 8 ? (gated ? launch_rows<true, 2> : launch_rows<false, 2>)
+                          : (gated ? launch_rows<true, 1> : launch_rows<false, 1>);
+    return launch(x, w, M, N, K, epi, s);
 }
 
 }  // namespace puro
