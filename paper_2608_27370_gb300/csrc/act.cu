@@ -20,7 +20,7 @@ namespace puro {
 constexpr int kActCols = 256;                // columns of a block: 32 threads of eight
 constexpr int kActRows = 8;                  // rows of threads
 constexpr int kActBatch = 2;                 // rows of a thread loaded at once
-constexpr int64_t kActBlocks = 152 * 4;      // blocks at most: four an SM are resident
+constexpr int64_t kActBlocks = 152 * 4;      // blocks at most: four an SM are resident (a constant: it fixes the sums' order)
 constexpr int kGateBlocks = 4;               // of the gate's kernel an SM
 
 ActBackwardPlan plan_act_backward(int64_t rows, int64_t cols) {
@@ -158,7 +158,7 @@ cudaError_t launch_gated_backward(const uint16_t *dh, const uint16_t *gate, cons
                 : act == PURO_ACT_GELU      ? gated_backward_kernel<PURO_ACT_GELU>
                 : act == PURO_ACT_GELU_TANH ? gated_backward_kernel<PURO_ACT_GELU_TANH>
                                             : gated_backward_kernel<PURO_ACT_NONE>;
-    const int64_t want = (rows * (cols / 8) + 255) / 256, cap = 152 * kGateBlocks;
+    const int64_t want = (rows * (cols / 8) + 255) / 256, cap = static_cast<int64_t>(sm_count_here()) * kGateBlocks;
     return launch_pdl(kern, dim3(static_cast<unsigned>(want < cap ? want : cap)), dim3(256), 0, s, dh, gate, up, rows, cols, ld,
                       dgate_up);
 }

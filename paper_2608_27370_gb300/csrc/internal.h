@@ -30,6 +30,14 @@ inline cudaError_t launch_pdl(void (*kern)(KArgs...), dim3 grid, dim3 block, siz
 }
 
 
+// SMs of the current device.
+inline int sm_count_here() {
+    int dev = 0, sms = 148;
+    cudaGetDevice(&dev);
+    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    return sms;
+}
+
 // How a quantiser groups values (section "FP8 Mixed-Precision Training").
 enum QuantKind : int {
     kQuantBlockAct = 0,     // 1x128 groups along cols (q) and along rows (q_t)

@@ -30,7 +30,8 @@ namespace puro {
 
 constexpr int kQkFwdThreads = 128, kQkThreads = 256;  // (the backward's)
 constexpr int kQkFwdBatch = 4, kQkBwdBatch = 2;       // heads of a token a group loads at once
-constexpr int kQkBwdBlocks = 152 * 2;  // at most: two an SM are resident, each leaves a partial sum of a gain's gradient
+// At most: two an SM are resident, each leaves a partial sum of a gain's gradient (a constant: it fixes the sums' order).
+constexpr int kQkBwdBlocks = 152 * 2;
 constexpr int32_t kQkStatusInvalid = 1;  // PURO_ERR_INVALID_ARG
 
 // The lane's channels: two chunks of eight, at o0 and o1 of the head, and the

@@ -25,13 +25,6 @@
 
 namespace puro {
 
-static int sm_count_here() {
-    int dev = 0, sms = 148;
-    cudaGetDevice(&dev);
-    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    return sms;
-}
-
 // --------------------------------------------------------------- amax
 // Integer max of (bits & 0x7FFF) over bf16 values: exact for finite values,
 // +inf sorts above them and NaN above +inf.  A read-only stream: every
