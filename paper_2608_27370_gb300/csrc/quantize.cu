@@ -1153,7 +1153,9 @@ __global__ void __launch_bounds__(kQAThreads, 2)
 // computing both outputs from one activation, waited for their loads: [8192, 6144] 108
 // us, so 102 (4.9 TB/s, bound by its instructions: 64% of the issue slots).  Both
 // outputs from one evaluation here too, handed to the teams through the buffers,
-// took 109, for the barrier.
+// took 109, for the barrier.  A kernel for each activation: with all five in one, at the
+// 64 registers of 1024 threads, each took the longer the more another one needed (ReLU / SiLU
+// / tanh GELU / GELU 97.7 / 104.9 / 109.8 / 130.7 us, so 90.5 / 100.6 / 105.6 / 128.5).
 struct GatedBackwardSmem {
     struct Stage {
         alignas(1024) uint16_t h[kQT * kQT], z[2][kQT * kQT];  // dh; gate and up, then the codes of dgate and dup
@@ -1162,7 +1164,7 @@ struct GatedBackwardSmem {
     uint64_t full[2];
 };
 
-template <int FMT, bool HAS_T>
+template <int FMT, bool HAS_T, int ACT>
 __global__ void __launch_bounds__(2 * kQAThreads, 1)
     quant_gated_backward_kernel(const __grid_constant__ BackwardQuantMaps m, const BackwardQuantArgs a) {
     extern __shared__ uint8_t smem_raw[];
@@ -1212,20 +1214,17 @@ __global__ void __launch_bounds__(2 * kQAThreads, 1)
         const int64_t oc0 = team * a.cols + c0;
         const bool landed = tile_landed(&sm.full[s], static_cast<uint32_t>(it >> 1) & 1u, a.wait_ns);
         uint2 v[8];
-        act_dispatch(a.act, [&](auto act) {
-            constexpr int ACT = decltype(act)::value;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int at = (8 * br + i) * kQT + 4 * bc;
-                const uint2 h = *reinterpret_cast<const uint2 *>(sm.in[s].h + at), g = *reinterpret_cast<const uint2 *>(sm.in[s].z[0] + at);
-                if (team == 0) {
-                    const uint2 u = *reinterpret_cast<const uint2 *>(sm.in[s].z[1] + at);
-                    v[i] = make_uint2(gate_backward2<ACT>(h.x, g.x, u.x), gate_backward2<ACT>(h.y, g.y, u.y));
-                } else {
-                    v[i] = make_uint2(up_backward2<ACT>(h.x, g.x), up_backward2<ACT>(h.y, g.y));
-                }
+        for (int i = 0; i < 8; ++i) {
+            const int at = (8 * br + i) * kQT + 4 * bc;
+            const uint2 h = *reinterpret_cast<const uint2 *>(sm.in[s].h + at), g = *reinterpret_cast<const uint2 *>(sm.in[s].z[0] + at);
+            if (team == 0) {
+                const uint2 u = *reinterpret_cast<const uint2 *>(sm.in[s].z[1] + at);
+                v[i] = make_uint2(gate_backward2<ACT>(h.x, g.x, u.x), gate_backward2<ACT>(h.y, g.y, u.y));
+            } else {
+                v[i] = make_uint2(up_backward2<ACT>(h.x, g.x), up_backward2<ACT>(h.y, g.y));
             }
-        });
+        }
         const float mul = tile_maxima<FMT, HAS_T>(sm.out[team], v, br, bc);
         if (__syncthreads_or(!landed)) {  // (S2) partials written, every input in registers
             if (threadIdx.x == 0) {
@@ -1468,7 +1467,12 @@ static cudaError_t launch_swiglu_f(const QuantArgs &a, const CUtensorMap &tm_x, 
 
 template <int FMT, bool HAS_T>
 static cudaError_t launch_backward_f(const BackwardQuantArgs &a, const BackwardQuantMaps &m, bool gated, cudaStream_t s) {
-    auto kern = gated ? quant_gated_backward_kernel<FMT, HAS_T> : quant_act_backward_kernel<FMT, HAS_T>;
+    auto kern = !gated                        ? quant_act_backward_kernel<FMT, HAS_T>
+                : a.act == PURO_ACT_RELU      ? quant_gated_backward_kernel<FMT, HAS_T, PURO_ACT_RELU>
+                : a.act == PURO_ACT_SILU      ? quant_gated_backward_kernel<FMT, HAS_T, PURO_ACT_SILU>
+                : a.act == PURO_ACT_GELU      ? quant_gated_backward_kernel<FMT, HAS_T, PURO_ACT_GELU>
+                : a.act == PURO_ACT_GELU_TANH ? quant_gated_backward_kernel<FMT, HAS_T, PURO_ACT_GELU_TANH>
+                                              : quant_gated_backward_kernel<FMT, HAS_T, PURO_ACT_NONE>;
     const size_t smem = (gated ? sizeof(GatedBackwardSmem) : sizeof(ActBackwardSmem)) + 1024;
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
