@@ -85,7 +85,10 @@ typedef enum { PURO_E4M3 = 0, PURO_E5M2 = 1 } puro_fp8_format_t;
 typedef enum { PURO_SCALE_TENSOR = 0, PURO_SCALE_BLOCK = 1 } puro_scaling_t;
 typedef enum { PURO_ROLE_ACT = 0, PURO_ROLE_WEIGHT = 1 } puro_role_t;
 /* Activations: max(z, 0); z / (1 + e^-z); z Phi(z), Phi the normal
- * distribution function; z / (1 + e^-2u), u = sqrt(2/pi) (z + 0.044715 z^3). */
+ * distribution function; z / (1 + e^-2u), u = sqrt(2/pi) (z + 0.044715 z^3).
+ * In FP32 ahead of a rounding to BF16, and for every finite z within 2^-15 of the
+ * value (their slopes within 2^-14 of the larger of their terms), so that the
+ * far tails keep their digits; what is below 2^-126 may be zero. */
 typedef enum {
     PURO_ACT_NONE = 0,
     PURO_ACT_RELU = 1,

@@ -34,7 +34,8 @@ ActBackwardPlan plan_act_backward(int64_t rows, int64_t cols) {
 // Two rows of a thread at once, four blocks an SM.  With dbias, us at one / two / three /
 // four rows: SiLU [8192, 8960] 72.1 / 70.9 / 69.7 / 80.6, none 57.6 / 48.8 / 51.2 / 50.8, GELU
 // [1001, 1544] 6.4 / 6.1 / 7.2 / 7.0 (floors 65.0, 43.3, 1.4); five and six blocks no better;
-// with a row's loads behind the stores of the one before 147, 56, 7.0.
+// with a row's loads behind the stores of the one before 147, 56, 7.0.  (Of narrower sigmoids
+// and a shorter GELU; two rows now 69.0, 49.2, 6.3.)
 template <int ACT>
 __global__ void __launch_bounds__(256, 4) act_backward_kernel(const uint16_t *dy, const uint16_t *__restrict__ z,
                                                            int64_t rows, int64_t cols, int64_t slab_rows, uint16_t *dz,
@@ -123,7 +124,8 @@ cudaError_t launch_column_sums(const float *partial, int64_t n, int64_t cols, fl
 // [dgate, dup] of eight columns of a row a thread and step.  Blocks an SM, and us at
 // four / five / six: SiLU [8192, 6144] 74.9 / 81.0 / 75.1, [777, 6144] 9.2 / 9.0 / 9.4, tanh
 // GELU 74.7 / 78.9 / 80.2 and 9.2 / 10.1 / 10.2; GELU at four / six 77.0 / 81.2 and 9.6 / 9.8
-// (floors 74.2 and 7.0; eight with a division a step and SiLU 91.6 and 10.6).
+// (floors 74.2 and 7.0; eight with a division a step and SiLU 91.6 and 10.6).  (Of narrower
+// sigmoids and a shorter GELU; four now 75.0 and 9.2, 75.4 and 9.4, 79.1 and 10.0.)
 template <int ACT>
 __global__ void __launch_bounds__(256, kGateBlocks) gated_backward_kernel(const uint16_t *__restrict__ dh,
                                                                        const uint16_t *__restrict__ gate,

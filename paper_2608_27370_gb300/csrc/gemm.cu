@@ -549,10 +549,11 @@ PURO_DEV void quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int w
 // special-function chains of the activations overlapped.  Everything they read
 // (bias, residual) comes straight from global memory, what they write in BF16
 // leaves by plain stores (store_rows32) or bulk stores of few rows, so rows and
-// columns may end anywhere (columns at a multiple of eight).  us, rotating operands,
-// [8192, 2048] x 6144 block-scaled: the plain GEMM 62.3, this epilogue alone 63.7,
-// with bias 64.3, SiLU 64.5, GELU 66.5, a residual (33 MB more) 67.7; [32768, 2048] x
-// 1536 65.2, 70.0, 70.7, 69.9, 75.6, 80.8.
+// columns may end anywhere (columns at a multiple of eight).  us, rotating operands, ten
+// calls at a time: [8192, 2048] x 6144 block-scaled the plain GEMM 61.9, this epilogue
+// alone 63.4, with bias 64.0, SiLU too 65.1, GELU 67.4, a residual alone (33 MB more)
+// 67.5; [32768, 2048] x 1536 64.1, 69.2, 70.8, 72.5, 82.0, 79.8.  Back to back for 0.4 s, at
+// the power cap, 67.8, 69.0, 70.0, 71.0, 73.2, 73.2 and 73.4, 76.4, 78.0, 82.6, 90.2, 89.3.
 template <int OUT, int BN, int S>
 constexpr bool wide_epilogue_form() {
     return S == 1 && (OUT == kGemmOutEpilogue || OUT == kGemmOutGated || OUT == kGemmOutGatedQuant);
@@ -873,15 +874,16 @@ PURO_DEV uint32_t nan_codes4(uint32_t a, uint32_t b) { return 0x7F7F7F7Fu | (__b
 // exchange row maxima (named barrier 1 + q), the four of one j column maxima
 // (9 + j).  A warp whose wait runs out goes on through the barriers of its tiles,
 // where the others still meet it, and stores nothing more.
-// With gate and up kept, rotating operands, us: [32768, 8960] x 1536 725, [8192,
-// 6144] x 2048 154, [1024, 6144] x 2048 25.3 (the plain GEMM of [32768, 17920] 555-590,
-// the second kernel it would take 360-410).  A tile takes 9030 cycles on the first
+// With gate and up kept, rotating operands, back to back for 0.4 s, us: [32768, 8960] x
+// 1536 718-727 (ten calls at a time 635-647), [8192, 6144] x 2048 154, [1024, 6144] x 2048
+// 25.0 (the plain GEMM of [32768, 17920] 594, or 533, the second kernel it would take 334).
+// The figures below are older ones, to be compared with 725.  A tile takes 9030 cycles on the first
 // shape, 7250 of them the epilogue's, and 7430 without stores: they compete with the
 // operands' loads for L2, by requests more than by bytes (confined to 1 MB they cost
 // the same), so gate and up leave in 64-byte pieces (in 32-byte ones 775, 166).
 // By bulk stores, as a linear's y: 756, so 690.  Codes gathered in shared memory and
-// stored as 128-byte rows: 740, so 712, for the barriers.  The stores of gate and up come first: behind the maxima, to fill the
-// barriers' waits, 895 and 183.  The codes of a tile's copies are computed without a
+// stored as 128-byte rows: 740, so 712, for the barriers.  The stores of gate and up come
+// first: behind the maxima, to fill the barriers' waits, 895 and 183.  The codes of a tile's copies are computed without a
 // branch for each four, which would end their overlap (826 -> 738 on the first).
 template <int FMT, class Smem>
 PURO_DEV void gated_quant_epilogue(Smem &sm, const GemmParams &p, uint32_t tmem, int warp, int lane, int pair,
@@ -1030,7 +1032,8 @@ constexpr int gemm_threads() {
     return OUT == kGemmOutQuant ? kThreads + 384 : wide_epilogue_form<OUT, BN, S>() ? 128 + BN / 64 * 128 : kThreads;
 }
 // Registers: sixteen epilogue warps of a 640-thread block get 96 each at launch,
-// some short of what they hold (64 accumulators, the residual, addresses).  The
+// some short of what they hold (64 accumulators, the residual, addresses): a linear's
+// epilogue spills 60 to 68 bytes a thread, the gated ones none.  The
 // four warps ahead of them need few and give theirs up: 4 * 56 + 16 * 104 = 1888
 // a lane, of the 20 * 96 = 1920 that the block was launched with (launch_params
 // looks that it was: an increase beyond them would wait for ever).

@@ -1050,7 +1050,7 @@ PURO_DEV void tile_codes(const OutTile &t, const uint2 (&v)[8], float mul, uint8
 // ---- dz: two CTAs of one team an SM.  The buffers of dy and z are free for the next
 // tile once the outputs are in registers, so its loads run under the casting.  As a
 // producer of quant_act_kernel, with z loaded into registers, [8192, 8960] gelu_tanh
-// with dbias took 115 us, so 85 (5.2 TB/s).
+// with dbias took 115 us, so 86 (5.1 TB/s).
 struct ActBackwardSmem {
     alignas(1024) uint16_t y[kQT * kQT], z[kQT * kQT];
     alignas(1024) uint8_t stage[2 * kQT * kQT];
@@ -1151,7 +1151,7 @@ __global__ void __launch_bounds__(kQAThreads, 2)
 // one's 96 KB are on their way, and a tile's own gate and up buffers, once read,
 // hold the codes until they have left.  Two CTAs an SM with single buffers, each
 // computing both outputs from one activation, waited for their loads: [8192, 6144] 108
-// us, so 102 (4.9 TB/s, bound by its instructions: 64% of the issue slots).  Both
+// us, so 101 (5.0 TB/s, bound by its instructions: 65% of the issue slots).  Both
 // outputs from one evaluation here too, handed to the teams through the buffers,
 // took 109, for the barrier.  A kernel for each activation: with all five in one, at the
 // 64 registers of 1024 threads, each took the longer the more another one needed (ReLU / SiLU

@@ -193,11 +193,11 @@ static cudaError_t launch_rows(const uint16_t *x, const uint16_t *w, int64_t M, 
 
 // Up to 16 tokens, and up to 32 where the weight is small: every block reads all
 // the tokens, from L2, which costs more than the tiles' idle tensor cores where
-// there are many blocks.  us here / in the GEMM kernel at 17 and 32 tokens: linear
-// [2048] x 1536 3.9 / 7.7 and 4.2 / 7.7, [512] x 4096 5.4 / 7.2 and 5.9 / 7.2, but [4096] x
-// 2048 9.4 / 8.7 and 10.0 / 8.7, [1536] x 8960 14.2 / 13.8 and 15.9 / 13.9; gated [1024] x
-// 1024 2.7 / 8.3 and 2.9 / 8.3, [8960] x 1536 21.7 / 15.9 and 22.9 / 15.7 (at 16 tokens
-// 15.2 / 15.9).
+// there are many blocks.  us here at 17 and 32 tokens / in the GEMM kernel at 33, weights
+// out of L2: linear [2048] x 1536 3.9 and 4.2 / 7.8, [2048] x 2048 5.2 and 5.5 / 7.8, [4096] x 1024
+// 5.0 and 5.5 / 7.4, gated [1024] x 2048 5.1 and 5.3 / 12.4.  At 16 tokens here / at 33 there:
+// [4096] x 2048 7.0 / 8.7, [1536] x 8960 10.1 / 13.0, [8960] x 1536 10.4 / 13.0, but gated [6144] x
+// 2048 16.5 / 14.1 and [8960] x 1536 17.0 / 16.3.
 bool is_skinny_linear(int64_t M, int64_t N, int64_t K, bool gated) {
     if (K > (1 << 30)) return false;  // (k is an int there)
     return M <= 16 || (M <= 32 && N * K * (gated ? 2 : 1) <= (4 << 20));
