@@ -701,6 +701,71 @@ puro_status_t puro_qk_norm_rope_backward(const puro_heads_t *dq_out, const puro_
 /* Bytes of scratch for the gains' gradients.  Host-only, no CUDA call. */
 size_t puro_qk_norm_rope_workspace_size(int64_t tokens, int32_t q_heads, int32_t k_heads, int32_t head_dim);
 
+/*
+ * The position rotation without a norm, its backward, and its tables: layers of
+ * the Qwen2 architecture rotate queries and keys as the qkv projection leaves
+ * them.  (The paper has no counterpart of the frequencies' scalings; they are
+ * those of the published methods that stretch a trained context.)
+ *
+ * Pair i of the first rot_dim channels (i and i + rot_dim/2, or interleaved 2i and
+ * 2i + 1) turns by the angle p w_i at position p:
+ *     (a, b) -> scale (a cos - b sin, b cos + a sin),
+ * backward (a, b) -> scale (a cos + b sin, b cos - a sin); the other channels pass
+ * unturned and unscaled.  The arithmetic is FP32, y rounded to BF16 once; cosines
+ * and sines are within 2^-19 of those of p w_i, in the tables within 2^-22 (times
+ * scale), w_i as the integers below hold it.
+ *
+ * puro_rope_frequencies (host only, no CUDA call) writes the w_i as the integers
+ * w_i / (2 pi) 2^64 to the host array frequencies[rot_dim/2], which the caller
+ * copies to the device once.  With v_i = base^(-2i/rot_dim):
+ *   PURO_ROPE_NONE    w_i = v_i
+ *   PURO_ROPE_LINEAR  w_i = v_i / factor
+ *   PURO_ROPE_BASE    the same as NONE with base factor^(rot_dim/(rot_dim - 2))
+ *                     times as large
+ *   PURO_ROPE_TURNS   w_i = v_i (keep_i + (1 - keep_i) / factor), where keep_i goes
+ *                     from 0 for pairs that make at most slow_turns turns over
+ *                     trained_positions positions to 1 for those that make
+ *                     fast_turns or more, evenly in the number of turns
+ *   PURO_ROPE_INDEX   the same, keep_i evenly in i between the pairs at which the
+ *                     number of turns is fast_turns (rounded down, at least 0) and
+ *                     slow_turns (rounded up, at most the last pair)
+ * The last two go with scale = 0.1 ln(factor) + 1 or 1 as the model was trained;
+ * scale is the caller's.  rot_dim: a multiple of 16 up to 256; base > 1; factor >=
+ * 1 (not read for NONE); trained_positions > 0 and fast_turns > slow_turns > 0
+ * (read for the last two).
+ *
+ * puro_rope_tables writes cos, sin fp32 [count, rot_dim/2] of positions first, first
+ * + 1, ... (first + count <= 2^31), as puro_qk_norm_rope reads them.
+ *
+ * puro_rope, puro_rope_backward: q, k, ... and positions as for puro_qk_norm_rope
+ * (views of heads; NULL positions: token t is at position t; a negative position
+ * marks a padding row, whose output is zero), with no bound on the positions.
+ * rot_dim: a multiple of 16 from 16 to head_dim.  q_out, k_out may be q and k, and
+ * dq, dk may be dq_out and dk_out (same strides).  frequencies: device, 16-byte
+ * aligned.  One kernel each.
+ */
+typedef enum {
+    PURO_ROPE_NONE = 0,
+    PURO_ROPE_LINEAR = 1,
+    PURO_ROPE_BASE = 2,
+    PURO_ROPE_TURNS = 3,
+    PURO_ROPE_INDEX = 4
+} puro_rope_scaling_t;
+
+puro_status_t puro_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor,
+                                    int64_t trained_positions, double fast_turns, double slow_turns,
+                                    uint64_t *frequencies);
+puro_status_t puro_rope_tables(const uint64_t *frequencies, int32_t rot_dim, float scale, int64_t first,
+                               int64_t count, float *cos, float *sin, void *stream);
+puro_status_t puro_rope(const puro_heads_t *q, const puro_heads_t *k, int64_t tokens, int32_t head_dim,
+                        const uint64_t *frequencies, int32_t rot_dim, float scale, int32_t interleaved,
+                        const int32_t *positions, const puro_heads_t *q_out, const puro_heads_t *k_out,
+                        void *stream);
+puro_status_t puro_rope_backward(const puro_heads_t *dq_out, const puro_heads_t *dk_out, int64_t tokens,
+                                 int32_t head_dim, const uint64_t *frequencies, int32_t rot_dim, float scale,
+                                 int32_t interleaved, const int32_t *positions, const puro_heads_t *dq,
+                                 const puro_heads_t *dk, void *stream);
+
 /* Human-readable name of a status code (static string). */
 const char *puro_status_string(puro_status_t s);
 

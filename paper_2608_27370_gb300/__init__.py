@@ -36,6 +36,7 @@ E4M3, E5M2 = 0, 1
 SCALE_TENSOR, SCALE_BLOCK = 0, 1
 ROLE_ACT, ROLE_WEIGHT = 0, 1
 ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = range(5)
+ROPE_NONE, ROPE_LINEAR, ROPE_BASE, ROPE_TURNS, ROPE_INDEX = range(5)
 
 PURO_OK = 0
 PURO_ERR_INVALID_ARG = 1
@@ -114,6 +115,10 @@ _SIGNATURES = {
     "puro_qk_norm_rope_backward": (_I32, [_P, _P, _P, _P, _P, _I64, _I32, _P, _P, _P, _P, _I64, _I32, _I32, _P, _P, _P, _P,
                                           _P, _P, ctypes.c_size_t, _P, _P]),
     "puro_qk_norm_rope_workspace_size": (ctypes.c_size_t, [_I64, _I32, _I32, _I32]),
+    "puro_rope_frequencies": (_I32, [_I32, ctypes.c_double, _I32, ctypes.c_double, _I64, ctypes.c_double, ctypes.c_double, _P]),
+    "puro_rope_tables": (_I32, [_P, _I32, ctypes.c_float, _I64, _I64, _P, _P, _P]),
+    "puro_rope": (_I32, [_P, _P, _I64, _I32, _P, _I32, ctypes.c_float, _I32, _P, _P, _P, _P]),
+    "puro_rope_backward": (_I32, [_P, _P, _I64, _I32, _P, _I32, ctypes.c_float, _I32, _P, _P, _P, _P]),
     "puro_set_wait_timeout_ns": (None, [ctypes.c_uint64]),
     "puro_set_gemm_tile_n": (ctypes.c_int, [ctypes.c_int32]),
     "puro_status_string": (ctypes.c_char_p, [_I32]),
@@ -902,6 +907,82 @@ def puro_qk_norm_rope_workspace_size(tokens: int, q_heads: int, k_heads: int, he
     return int(load_library().puro_qk_norm_rope_workspace_size(tokens, q_heads, k_heads, head_dim))
 
 
+# --------------------------------------------------------------------------
+# The position rotation without a norm
+# --------------------------------------------------------------------------
+def puro_rope_frequencies(rot_dim: int, base: float, scaling: int, factor: float, trained_positions: int, fast_turns: float,
+                          slow_turns: float, frequencies: torch.Tensor) -> None:
+    """The angle of each pair of channels per position, as 2^64ths of a turn: into
+    frequencies, int64 [rot_dim / 2] on the CPU."""
+    if frequencies.is_cuda or frequencies.dtype != torch.int64 or not frequencies.is_contiguous() or \
+            frequencies.numel() != rot_dim // 2:
+        raise ValueError(f"frequencies must be an int64 CPU tensor [{rot_dim // 2}]")
+    st = load_library().puro_rope_frequencies(rot_dim, float(base), scaling, float(factor), trained_positions, float(fast_turns),
+                                              float(slow_turns), frequencies.data_ptr())
+    _check("puro_rope_frequencies", st)
+
+
+def rope_frequencies(rot_dim: int, base: float, scaling: int = ROPE_NONE, factor: float = 1.0, trained_positions: int = 0,
+                     fast_turns: float = 32.0, slow_turns: float = 1.0, device="cuda") -> torch.Tensor:
+    """The frequencies that puro_rope and puro_rope_tables read (int64 [rot_dim / 2]), scaled for
+    a context factor times the trained one where scaling is not ROPE_NONE."""
+    f = torch.empty(max(0, rot_dim) // 2, dtype=torch.int64)
+    puro_rope_frequencies(rot_dim, base, scaling, factor, trained_positions, fast_turns, slow_turns, f)
+    return f.to(device)
+
+
+def puro_rope_tables(frequencies: torch.Tensor, first: int, cos: torch.Tensor, sin: torch.Tensor, scale: float = 1.0,
+                     stream=None) -> None:
+    """cos and sin (fp32 [positions, rot_dim / 2], written) of positions first, first + 1, ..., times
+    scale: the tables of puro_qk_norm_rope."""
+    _on_current_device(frequencies)
+    st = (_native or _load_native()).puro_rope_tables(frequencies, first, cos, sin, scale, stream)
+    if st is not None:
+        return _check("puro_rope_tables", st)
+    _on_current_device(frequencies, cos, sin)
+    cp, sp, count, rot = _tables(cos, sin)
+    st = load_library().puro_rope_tables(_sized(frequencies, torch.int64, rot // 2, "frequencies"), rot, float(scale), first,
+                                         count, cp, sp, _stream(stream))
+    _check("puro_rope_tables", st)
+
+
+def _rope(name, x, x2, frequencies, positions, interleaved, y, y2, scale, stream, names):
+    _on_current_device(x if x is not None else x2)
+    st = getattr(_native or _load_native(), name)(x, x2, frequencies, positions, interleaved, y, y2, scale, stream)
+    if st is not None:
+        return _check(name, st)
+    _on_current_device(x, x2, frequencies, positions, y, y2)
+    some = x if x is not None else x2
+    if some is None or some.dim() != 3:
+        raise ValueError(f"{names[0]} or {names[1]} must be a bf16 CUDA tensor [tokens, heads, head_dim]")
+    tokens, _, d = some.shape
+    h = [_heads(t, n, tokens, d) for t, n in zip((x, x2, y, y2), names)]
+    st = getattr(load_library(), name)(
+        ctypes.byref(h[0]), ctypes.byref(h[1]), tokens, d, _ptr(frequencies, torch.int64, "frequencies"),
+        2 * frequencies.numel(), float(scale), int(bool(interleaved)), _sized(positions, torch.int32, tokens, "positions"),
+        ctypes.byref(h[2]), ctypes.byref(h[3]), _stream(stream))
+    _check(name, st)
+
+
+def puro_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], frequencies: torch.Tensor,
+              positions: Optional[torch.Tensor], interleaved: bool, q_out: Optional[torch.Tensor],
+              k_out: Optional[torch.Tensor], scale: float = 1.0, stream=None) -> None:
+    """Rotate each query and key head (bf16 [tokens, heads, head_dim] views, for
+    instance of one qkv output) by the tokens' positions, without a norm: q_out,
+    k_out, which may be q and k.  frequencies: rope_frequencies(rot_dim, ...) on the
+    device; scale multiplies the rotated channels.  positions: int32 [tokens], None
+    for 0, 1, ...; a negative one marks a padding row, whose output is zero."""
+    _rope("puro_rope", q, k, frequencies, positions, interleaved, q_out, k_out, scale, stream, ("q", "k", "q_out", "k_out"))
+
+
+def puro_rope_backward(dq_out: Optional[torch.Tensor], dk_out: Optional[torch.Tensor], frequencies: torch.Tensor,
+                       positions: Optional[torch.Tensor], interleaved: bool, dq: Optional[torch.Tensor],
+                       dk: Optional[torch.Tensor], scale: float = 1.0, stream=None) -> None:
+    """Backward of puro_rope: dq, dk (bf16 views, which may be dq_out and dk_out) from the gradients of its outputs."""
+    _rope("puro_rope_backward", dq_out, dk_out, frequencies, positions, interleaved, dq, dk, scale, stream,
+          ("dq_out", "dk_out", "dq", "dk"))
+
+
 def puro_set_wait_timeout_ns(ns: int) -> None:
     load_library().puro_set_wait_timeout_ns(int(ns))
 
@@ -965,6 +1046,6 @@ def quantize(x: torch.Tensor, fmt: int = E4M3, scaling: int = SCALE_BLOCK, role:
 
 __all__ = [n for n in dir() if n.startswith("puro_")] + [
     "E4M3", "E5M2", "SCALE_TENSOR", "SCALE_BLOCK", "ROLE_ACT", "ROLE_WEIGHT", "ACT_NONE", "ACT_RELU", "ACT_SILU",
-    "ACT_GELU", "ACT_GELU_TANH", "PuroError", "FP8Operand",
+    "ACT_GELU", "ACT_GELU_TANH", "ROPE_NONE", "ROPE_LINEAR", "ROPE_BASE", "ROPE_TURNS", "ROPE_INDEX", "rope_frequencies", "PuroError", "FP8Operand",
     "Quantized", "quantize", "load_library", "empty_scales", "scale_vec_shape", "LIB_PATH", "HEADER_PATH",
 ]

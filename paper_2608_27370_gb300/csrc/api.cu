@@ -4,6 +4,7 @@
 // entry point.
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <mutex>
 
 #include "internal.h"
@@ -503,6 +504,20 @@ puro_status_t fp8_gemm_quant(const puro_fp8_tensor_t *a, const puro_fp8_tensor_t
 }
 
 }  // namespace
+
+bool make_batched_map(CUtensorMap *m, CUtensorMapDataType dt, const void *base, uint64_t inner, uint64_t rows, uint64_t batch,
+                      uint64_t row_bytes, uint64_t batch_bytes, uint32_t box_inner, uint32_t box_rows, CUtensorMapSwizzle sw) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {inner, rows, batch};
+    const cuuint64_t strides[2] = {row_bytes, batch_bytes};
+    const cuuint32_t box[3] = {box_inner, box_rows, 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(m, dt, 3, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, sw,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+uint64_t wait_timeout_ns() { return g_wait_timeout_ns.load(); }
 
 puro_status_t fp8_gemm_entry(const puro_fp8_tensor_t *a, const puro_fp8_tensor_t *b, void *d, void *workspace,
                              size_t workspace_bytes, int32_t *dev_status, void *stream) {
@@ -1122,6 +1137,89 @@ PURO_API puro_status_t puro_qk_norm_rope_backward(const puro_heads_t *dq_out, co
         if (!dq_gain && !dk_gain) return PURO_OK;
     }
     return cuda_status(launch_qk_norm_rope_backward(p, dq_gain, dk_gain, static_cast<cudaStream_t>(stream)));
+}
+
+// ------------------------------------------------- the rotation alone
+PURO_API puro_status_t puro_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor,
+                                             int64_t trained_positions, double fast_turns, double slow_turns,
+                                             uint64_t *frequencies) {
+    constexpr double kTurn = 6.283185307179586476925;  // 2 pi
+    if (rot_dim < 16 || rot_dim > 256 || rot_dim % 16 || !frequencies) return PURO_ERR_INVALID_ARG;
+    if (!(base > 1.0) || !std::isfinite(base)) return PURO_ERR_INVALID_ARG;
+    if (scaling < PURO_ROPE_NONE || scaling > PURO_ROPE_INDEX) return PURO_ERR_INVALID_ARG;
+    if (scaling != PURO_ROPE_NONE && !(factor >= 1.0 && std::isfinite(factor))) return PURO_ERR_INVALID_ARG;
+    const bool ramp = scaling == PURO_ROPE_TURNS || scaling == PURO_ROPE_INDEX;
+    const double trained = static_cast<double>(trained_positions), pairs = rot_dim / 2;
+    if (ramp && !(trained_positions > 0 && slow_turns > 0.0 && fast_turns > slow_turns && std::isfinite(fast_turns)))
+        return PURO_ERR_INVALID_ARG;
+    if (scaling == PURO_ROPE_BASE) base *= std::pow(factor, rot_dim / (rot_dim - 2.0));
+    if (!std::isfinite(base)) return PURO_ERR_INVALID_ARG;
+    // PURO_ROPE_INDEX: the pairs at which the turns over the trained context are fast_turns and slow_turns
+    auto pair_of = [&](double turns) { return rot_dim * std::log(trained / (turns * kTurn)) / (2.0 * std::log(base)); };
+    const double lo = ramp ? std::max(0.0, std::floor(pair_of(fast_turns))) : 0.0;
+    const double hi = ramp ? std::min(pairs - 1.0, std::ceil(pair_of(slow_turns))) : 0.0;
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        double w = std::pow(base, -2.0 * i / rot_dim), keep = 1.0;
+        if (scaling == PURO_ROPE_LINEAR) keep = 0.0;
+        if (scaling == PURO_ROPE_TURNS) keep = (trained * w / kTurn - slow_turns) / (fast_turns - slow_turns);
+        if (scaling == PURO_ROPE_INDEX) keep = 1.0 - (i - lo) / std::max(hi - lo, 0.001);
+        keep = std::min(1.0, std::max(0.0, keep));
+        if (keep < 1.0) w = (1.0 - keep) * w / factor + keep * w;
+        frequencies[i] = static_cast<uint64_t>(std::ldexp(w / kTurn, 64));
+    }
+    return PURO_OK;
+}
+
+PURO_API puro_status_t puro_rope_tables(const uint64_t *frequencies, int32_t rot_dim, float scale, int64_t first,
+                                        int64_t count, float *cos, float *sin, void *stream) {
+    if (rot_dim < 16 || rot_dim > 256 || rot_dim % 16 || first < 0 || count < 0) return PURO_ERR_INVALID_ARG;
+    if (first > (int64_t{1} << 31) || count > (int64_t{1} << 31) - first) return PURO_ERR_INVALID_ARG;
+    if (!aligned16(frequencies) || !aligned16(cos) || !aligned16(sin)) return PURO_ERR_INVALID_ARG;
+    if (count == 0) return PURO_OK;
+    if (!frequencies || !cos || !sin) return PURO_ERR_INVALID_ARG;
+    return cuda_status(launch_rope_tables(frequencies, rot_dim / 2, scale, first, count, cos, sin, static_cast<cudaStream_t>(stream)));
+}
+
+namespace puro {
+namespace {
+
+puro_status_t rope(const puro_heads_t *x, const puro_heads_t *x2, int64_t tokens, int32_t D, const uint64_t *freq, int32_t rot,
+                   float scale, float sin_scale, int32_t interleaved, const int32_t *positions, const puro_heads_t *y,
+                   const puro_heads_t *y2, void *stream) {
+    RopeArgs p{};
+    if (tokens < 0 || D < 16 || D > 256 || D % 16 || rot < 16 || rot > D || rot % 16) return PURO_ERR_INVALID_ARG;
+    if (!take_heads(x, tokens, D, false, &p.q) || !take_heads(x2, tokens, D, false, &p.k) || !take_heads(y, tokens, D, true, &p.q_out) ||
+        !take_heads(y2, tokens, D, true, &p.k_out))
+        return PURO_ERR_INVALID_ARG;
+    if (!freq || !aligned16(freq) || (reinterpret_cast<uintptr_t>(positions) & 3u)) return PURO_ERR_INVALID_ARG;
+    if (p.q.heads != p.q_out.heads || p.k.heads != p.k_out.heads) return PURO_ERR_INVALID_ARG;
+    if (tokens > INT32_MAX || p.q.heads > 65535 || p.k.heads > 65535) return PURO_ERR_UNSUPPORTED;
+    if (tokens == 0 || p.q.heads + p.k.heads == 0) return PURO_OK;
+    p.tokens = tokens;
+    p.D = D;
+    p.rot = rot;
+    p.inter = interleaved != 0;
+    p.freq = freq;
+    p.scale = scale;
+    p.sin_scale = sin_scale;
+    p.positions = positions;
+    return cuda_status(launch_rope(p, static_cast<cudaStream_t>(stream)));
+}
+
+}  // namespace
+}  // namespace puro
+
+PURO_API puro_status_t puro_rope(const puro_heads_t *q, const puro_heads_t *k, int64_t tokens, int32_t head_dim,
+                                 const uint64_t *frequencies, int32_t rot_dim, float scale, int32_t interleaved,
+                                 const int32_t *positions, const puro_heads_t *q_out, const puro_heads_t *k_out, void *stream) {
+    return rope(q, k, tokens, head_dim, frequencies, rot_dim, scale, scale, interleaved, positions, q_out, k_out, stream);
+}
+
+PURO_API puro_status_t puro_rope_backward(const puro_heads_t *dq_out, const puro_heads_t *dk_out, int64_t tokens,
+                                          int32_t head_dim, const uint64_t *frequencies, int32_t rot_dim, float scale,
+                                          int32_t interleaved, const int32_t *positions, const puro_heads_t *dq,
+                                          const puro_heads_t *dk, void *stream) {
+    return rope(dq_out, dk_out, tokens, head_dim, frequencies, rot_dim, scale, -scale, interleaved, positions, dq, dk, stream);
 }
 
 PURO_API void puro_set_wait_timeout_ns(uint64_t ns) { g_wait_timeout_ns.store(ns); }

@@ -51,7 +51,10 @@ PyObject *operand_type = nullptr;  // the binding's FP8Operand class
     X(puro_fp8_quantize_gated_backward) \
     X(puro_gated_backward_bf16)        \
     X(puro_qk_norm_rope)               \
-    X(puro_qk_norm_rope_backward)
+    X(puro_qk_norm_rope_backward)      \
+    X(puro_rope)                       \
+    X(puro_rope_backward)              \
+    X(puro_rope_tables)
 struct Library {
 #define PURO_FIELD(name) decltype(&::name) name;
     PURO_ENTRIES(PURO_FIELD)
@@ -645,6 +648,52 @@ PyObject *qk_norm_rope_backward_call(Args &a) {
 }
 PURO_NATIVE(qk_norm_rope_backward, 18)
 
+// (q, k, frequencies, positions, interleaved, q_out, k_out, scale, stream)
+template <class Entry>
+PyObject *rope_of(Args &a, Entry Library::*entry) {
+    puro_heads_t q, k, qo, ko;
+    int64_t t[4], d[4];
+    a.heads(0, &q, &t[0], &d[0]);
+    a.heads(1, &k, &t[1], &d[1]);
+    const uint64_t *freq = static_cast<const uint64_t *>(a.ptr(2, at::kLong));
+    const int64_t pairs = a.ok ? THPVariable_Unpack(a.v[2]).numel() : 0;
+    const int32_t *pos = static_cast<const int32_t *>(a.opt(3, at::kInt));
+    const bool inter = a.flag(4);
+    a.heads(5, &qo, &t[2], &d[2]);
+    a.heads(6, &ko, &t[3], &d[3]);
+    const float scale = a.f32(7);
+    void *s = a.stream(8);
+    for (int i = 1; i < 4; ++i)
+        if (t[i] != t[0] || d[i] != d[0]) a.ok = false;
+    a.numel(3, t[0]);
+    if (d[0] > 1024 || pairs > 1024) a.ok = false;
+    a.one_device();
+    return finish(a, [&] {
+        return (lib.*entry)(&q, &k, t[0], static_cast<int32_t>(d[0]), freq, static_cast<int32_t>(2 * pairs), scale, inter, pos, &qo,
+                            &ko, s);
+    });
+}
+PyObject *rope_call(Args &a) { return rope_of(a, &Library::puro_rope); }
+PURO_NATIVE(rope, 9)
+PyObject *rope_backward_call(Args &a) { return rope_of(a, &Library::puro_rope_backward); }
+PURO_NATIVE(rope_backward, 9)
+
+// (frequencies, first, cos, sin, scale, stream)
+PyObject *rope_tables_call(Args &a) {
+    const uint64_t *freq = static_cast<const uint64_t *>(a.ptr(0, at::kLong));
+    const int64_t pairs = a.ok ? THPVariable_Unpack(a.v[0]).numel() : 0, first = a.i64(1);
+    float *co = static_cast<float *>(a.ptr(2, kF32)), *si = static_cast<float *>(a.ptr(3, kF32));
+    int64_t rows[2], cols[2];
+    a.shape(2, &rows[0], &cols[0]);
+    a.shape(3, &rows[1], &cols[1]);
+    const float scale = a.f32(4);
+    void *s = a.stream(5);
+    if (cols[0] != pairs || cols[1] != pairs || rows[0] != rows[1] || pairs > 1024) a.ok = false;
+    a.one_device();
+    return finish(a, [&] { return lib.puro_rope_tables(freq, static_cast<int32_t>(2 * pairs), scale, first, rows[0], co, si, s); });
+}
+PURO_NATIVE(rope_tables, 6)
+
 // (the FP8Operand class)
 PyObject *set_operand_type(PyObject *, PyObject *const *argv, Py_ssize_t n) {
     if (n != 1) {
@@ -708,6 +757,9 @@ PyMethodDef methods[] = {PURO_METHOD("set_operand_type", set_operand_type),
                          PURO_METHOD("puro_gated_backward_bf16", gated_backward_bf16),
                          PURO_METHOD("puro_qk_norm_rope", qk_norm_rope),
                          PURO_METHOD("puro_qk_norm_rope_backward", qk_norm_rope_backward),
+                         PURO_METHOD("puro_rope", rope),
+                         PURO_METHOD("puro_rope_backward", rope_backward),
+                         PURO_METHOD("puro_rope_tables", rope_tables),
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Native argument marshalling of the Python binding.", -1, methods};

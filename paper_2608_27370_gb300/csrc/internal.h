@@ -312,6 +312,28 @@ cudaError_t launch_qk_norm_rope_backward(QkArgs p, float *dq_gain, float *dk_gai
 // first.  Host-only, shape-only.
 void qk_backward_blocks(int64_t tokens, int q_heads, int k_heads, int D, int *q_blocks, int *blocks);
 
+// The position rotation alone (see rope.cu): y = scale R x, or with sin_scale =
+// -scale its transpose.
+struct RopeArgs {
+    QkHeads q, k;          // x
+    QkHeads q_out, k_out;  // y
+    int64_t tokens;
+    int D, rot, inter;
+    const uint64_t *freq;      // [rot / 2]
+    float scale, sin_scale;
+    const int32_t *positions;  // [tokens], or null: token t is at position t
+};
+cudaError_t launch_rope(const RopeArgs &p, cudaStream_t s);
+// Tables [count, pairs] of positions first ...; pairs a multiple of 4.
+cudaError_t launch_rope_tables(const uint64_t *freq, int pairs, float scale, int64_t first, int64_t count, float *cos, float *sin,
+                               cudaStream_t s);
+
+// 3-D tensor map over `batch` row-major [rows, inner] matrices.
+bool make_batched_map(CUtensorMap *m, CUtensorMapDataType dt, const void *base, uint64_t inner, uint64_t rows, uint64_t batch,
+                      uint64_t row_bytes, uint64_t batch_bytes, uint32_t box_inner, uint32_t box_rows, CUtensorMapSwizzle sw);
+// The bound on device-side waits that puro_set_wait_timeout_ns set.
+uint64_t wait_timeout_ns();
+
 // Tile shape of the GEMM kernel: rows of A per CTA (a CTA pair computes
 // 2 * kGemmBM rows), columns of a tile (rows of B per pair), and the bytes
 // of K per pipeline stage (one 128-byte swizzle row).

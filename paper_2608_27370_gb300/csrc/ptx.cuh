@@ -258,6 +258,26 @@ PURO_DEV void tma_load_2d_pair_e(uint32_t e, void *dst, const CUtensorMap *map, 
         : "memory");
 }
 
+// The same of a 3-D tensor (z: the matrix of a batch).
+PURO_DEV void tma_load_3d_pair_e(uint32_t e, void *dst, const CUtensorMap *map, uint32_t bar_cluster, int32_t x, int32_t y,
+                                 int32_t z) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+        "@q cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes.cta_group::2"
+        " [%0], [%1, {%2, %3, %4}], [%5];\n\t}" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar_cluster), "r"(e)
+        : "memory");
+}
+// 3-D tiled store with its commit.
+PURO_DEV void tma_store_3d_e(uint32_t e, const CUtensorMap *map, const void *src, int32_t x, int32_t y, int32_t z) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+        "@q cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];\n\t"
+        "@q cp.async.bulk.commit_group;\n\t}" ::"l"(reinterpret_cast<uint64_t>(map)),
+        "r"(smem_u32(src)), "r"(x), "r"(y), "r"(z), "r"(e)
+        : "memory");
+}
+
 // The 128-byte line at p into L2 (a hint: nothing waits for it).
 PURO_DEV void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
@@ -365,6 +385,19 @@ PURO_DEV uint64_t smem_desc_k_sw128(uint32_t saddr) {
     uint64_t d = 0;
     d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
     d |= static_cast<uint64_t>(1) << 16;
+    d |= static_cast<uint64_t>(1024 >> 4) << 32;
+    d |= static_cast<uint64_t>(1) << 46;
+    d |= static_cast<uint64_t>(2) << 61;
+    return d;
+}
+
+// MN-major operand tile of 16-bit values: boxes of 64 values of MN (128-byte rows,
+// the 128-byte swizzle) by K rows, `box` bytes apart.  Eight rows of K are 1024
+// bytes (SBO), the next 64 values of MN are the next box (LBO).
+PURO_DEV uint64_t smem_desc_mn_sw128(uint32_t saddr, uint32_t box) {
+    uint64_t d = 0;
+    d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+    d |= static_cast<uint64_t>(box >> 4) << 16;
     d |= static_cast<uint64_t>(1024 >> 4) << 32;
     d |= static_cast<uint64_t>(1) << 46;
     d |= static_cast<uint64_t>(2) << 61;

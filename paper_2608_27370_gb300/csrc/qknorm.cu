@@ -25,6 +25,7 @@
 #include "internal.h"
 #include "ptx.cuh"
 #include "quant_math.cuh"
+#include "rotation.cuh"
 
 namespace puro {
 
@@ -34,82 +35,6 @@ constexpr int kQkFwdBatch = 4, kQkBwdBatch = 2;       // heads of a token a grou
 constexpr int kQkBwdBlocks = 152 * 2;
 constexpr int32_t kQkStatusInvalid = 1;  // PURO_ERR_INVALID_ARG
 
-// The lane's channels: two chunks of eight, at o0 and o1 of the head, and the
-// first of the eight pairs (so of the table's columns) they make up.
-struct QkLane {
-    int o0, o1, pair;
-    bool in, turned;
-};
-PURO_DEV QkLane qk_lane(int c, int D, int rot, int inter) {
-    QkLane l;
-    l.in = 16 * c < D;
-    l.turned = 16 * c < rot;
-    l.pair = 8 * c;
-    l.o0 = l.turned && !inter ? 8 * c : 16 * c;
-    l.o1 = l.turned && !inter ? rot / 2 + 8 * c : 16 * c + 8;
-    return l;
-}
-
-// The lane's sixteen channels as eight pairs (a, b), two pairs to a packed value:
-// a[j] holds the first channels of pairs 2j and 2j + 1, b[j] the second.
-struct Pairs {
-    uint64_t a[4], b[4];
-};
-template <bool INTER>
-PURO_DEV Pairs unpack16(const uint4 &w0, const uint4 &w1) {
-    const uint32_t x[4] = {w0.x, w0.y, w0.z, w0.w}, y[4] = {w1.x, w1.y, w1.z, w1.w};
-    Pairs p;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if constexpr (INTER) {  // neighbours: pairs 0 .. 3 in w0, 4 .. 7 in w1
-            const uint32_t u = j < 2 ? x[2 * j] : y[2 * j - 4], v = j < 2 ? x[2 * j + 1] : y[2 * j - 3];
-            p.a[j] = f32x2(bf16_lo(u), bf16_lo(v));
-            p.b[j] = f32x2(bf16_hi(u), bf16_hi(v));
-        } else {
-            p.a[j] = f32x2(bf16_lo(x[j]), bf16_hi(x[j]));
-            p.b[j] = f32x2(bf16_lo(y[j]), bf16_hi(y[j]));
-        }
-    }
-    return p;
-}
-
-PURO_DEV uint32_t round2(float lo, float hi) {
-    __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<uint32_t *>(&b);
-}
-template <bool INTER>
-PURO_DEV void pack16(const Pairs &p, uint4 &w0, uint4 &w1) {
-    uint32_t x[4], y[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        float a0, a1, b0, b1;
-        split_f32x2(p.a[j], a0, a1);
-        split_f32x2(p.b[j], b0, b1);
-        if constexpr (INTER) {
-            (j < 2 ? x : y)[2 * j & 3] = round2(a0, b0);
-            (j < 2 ? x : y)[(2 * j & 3) + 1] = round2(a1, b1);
-        } else {
-            x[j] = round2(a0, a1);
-            y[j] = round2(b0, b1);
-        }
-    }
-    w0 = make_uint4(x[0], x[1], x[2], x[3]);
-    w1 = make_uint4(y[0], y[1], y[2], y[3]);
-}
-
-// The angles of the lane's pairs: cosines, sines and negative sines.
-struct Angles {
-    uint64_t c[4], s[4], n[4];
-};
-// R p, or with s and n exchanged R^T p.
-PURO_DEV void turn(Pairs &p, const uint64_t (&c)[4], const uint64_t (&s)[4], const uint64_t (&n)[4]) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint64_t a = p.a[j], b = p.b[j];
-        p.a[j] = fma_f32x2(b, n[j], mul_f32x2(a, c[j]));
-        p.b[j] = fma_f32x2(a, s[j], mul_f32x2(b, c[j]));
-    }
-}
 PURO_DEV void scale(Pairs &p, uint64_t f) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -146,7 +71,6 @@ PURO_DEV float group_sum(float x) {
 
 // The token's position and angles.  A negative position marks a padding row
 // (kRowPad); one past the tables cannot be rotated (kRowOut).
-enum QkRow : int { kRowLive, kRowPad, kRowOut };
 PURO_DEV QkRow qk_angles(const QkArgs &p, int64_t t, const QkLane &l, Angles &g) {
     const int64_t pos = p.positions ? __ldg(p.positions + t) : t;
     if (pos < 0) return kRowPad;
@@ -173,13 +97,6 @@ PURO_DEV float rsqrt_f32(float x) {
     float y;
     asm("rsqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
-}
-
-// What a row that is not live counts as: zeros for padding, whatever it holds,
-// and NaN past the tables.
-PURO_DEV void replace_row(QkRow row, uint4 (&w)[2]) {
-    const uint32_t v = row == kRowPad ? 0u : 0x7FC07FC0u;
-    w[0] = w[1] = make_uint4(v, v, v, v);
 }
 
 // A block: some tokens' batch of heads of one kind, the batches of the same tokens
@@ -402,8 +319,6 @@ __global__ void __launch_bounds__(1024) qk_gain_kernel(const float *__restrict__
     out[c] = a;
 }
 
-static int group_lanes(int D) { return D <= 64 ? 4 : D <= 128 ? 8 : 16; }
-
 // Blocks for the query and key heads of the backward pass; host-only, by shape
 // alone (the partial sums' order is fixed by it).
 void qk_backward_blocks(int64_t tokens, int q_heads, int k_heads, int D, int *q_blocks, int *blocks) {
@@ -419,12 +334,6 @@ void qk_backward_blocks(int64_t tokens, int q_heads, int k_heads, int D, int *q_
     *q_blocks = static_cast<int>(nk == 0 ? most : nq == 0 ? 0 : std::max<int64_t>(1, std::min<int64_t>(most - 1, q)));
     *blocks = static_cast<int>(most);
 }
-
-// kern<G, INTER> for the group's lanes and the kind of pairs
-#define PURO_QK_KERNEL(kern, p)                                                                      \
-    (group_lanes((p).D) == 4   ? ((p).inter ? kern<4, true> : kern<4, false>)                         \
-     : group_lanes((p).D) == 8 ? ((p).inter ? kern<8, true> : kern<8, false>)                         \
-                               : ((p).inter ? kern<16, true> : kern<16, false>))
 
 cudaError_t launch_qk_norm_rope(const QkArgs &p, cudaStream_t s) {
     const int64_t per = kQkFwdThreads / group_lanes(p.D);
