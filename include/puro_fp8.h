@@ -635,6 +635,61 @@ puro_status_t puro_muonh_step_grouped(const puro_muonh_matrix_t *mats, int32_t c
                                       void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * The Muon directions u of many matrices, as puro_muonh_step takes them: the
+ * momentum's update and its orthogonalisation by Newton-Schulz products.  (The paper
+ * takes u as given and does not specify the orthogonalisation; this is the
+ * published one.)  For each matrix, with the gradient g and the momentum buffer M:
+ *     M <- momentum M + g,   V = nesterov ? g + momentum M : M   (no buffer: V = g)
+ *     X = V / ||V||_F
+ *     for each step (a, b, c):  A = X X^T,  X <- a X + (b A + c A^2) X
+ *     u = X
+ * (A = X^T X and X <- a X + X (b A + c A^2) where there are more rows than columns:
+ * the same X.)  A buffer that averages, M <- momentum M + (1 - momentum) g, has the
+ * same directions, for X does not depend on V's size.
+ *
+ * V is FP32 and its norm FP64.  The products are FP16 with FP32 accumulation, X and
+ * their other results scaled by powers of two; X is kept in two FP16 numbers (22
+ * digits) ahead of each pair of steps.  u is within about 2^-9 of itself in the
+ * 2-norm (5 of Muon's steps, momenta of low rank with noise a third as large; what
+ * is in V's directions of small singular values is less exact, and BF16 products
+ * would be off eight times as much), whichever type it is stored in.
+ * The sums' order is fixed by the shapes, so results are deterministic; where a
+ * matrix's tiles are split depends on what it is grouped with, its sums do not.
+ *   mats: host array of `count` descriptors (read during the call only).  grad and u
+ *     are views with rows grad_stride and u_stride elements apart (u_stride >= cols);
+ *     aligned to their elements, faster at 16 bytes with strides and cols of multiples
+ *     of 8.  momentum: fp32 [rows, cols], 4-byte aligned, updated in place, or NULL.  A
+ *     matrix without rows or columns is skipped.  rows, cols <= 2^20.
+ *   momentum: from 0 to 1.
+ *   coefficients: host array of `steps` (1 to 64) triples a, b, c.  They are refused
+ *     (INVALID_ARG) where singular values of at most 1 could reach 1024, or |a + b t +
+ *     c t^2| could, t a squared singular value.  Muon's are five times 3.4445, -4.7750,
+ *     2.0315.
+ *   workspace: 256-byte aligned, puro_muon_direction_workspace_size(mats, count)
+ *     bytes (0 for a table with a malformed descriptor): about 8 (m n + m^2) bytes for
+ *     each matrix of m x n, m <= n.
+ * V = 0 gives u = 0; a V whose norm is not finite gives NaN in all of u.  Matrices are
+ * taken 128 at a time, of up to 8 shapes: three kernels and then seven for each pair
+ * of steps (three for a last odd one).  Every descriptor is checked before anything is
+ * enqueued.
+ */
+typedef enum { PURO_BF16 = 0, PURO_F32 = 1 } puro_float_t;
+typedef struct {
+    const void *grad;      /* [rows, cols], of grad_type                        */
+    float *momentum;       /* fp32 [rows, cols], updated in place, or NULL      */
+    void *u;               /* [rows, cols], of u_type, written                  */
+    int64_t rows, cols;
+    int64_t grad_stride, u_stride;
+    int32_t grad_type, u_type; /* puro_float_t                                  */
+    int64_t reserved;      /* must be 0                                         */
+} puro_muon_matrix_t;
+
+size_t puro_muon_direction_workspace_size(const puro_muon_matrix_t *mats, int32_t count);
+puro_status_t puro_muon_direction_grouped(const puro_muon_matrix_t *mats, int32_t count, double momentum,
+                                          int32_t nesterov, const double *coefficients, int32_t steps,
+                                          void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream);
+
+/*
  * RMSNorm of each query and key head with the position rotation in the same
  * pass, and its backward.
  *

@@ -84,6 +84,8 @@ _SIGNATURES = {
     "puro_muonh_step": (_I32, [_P, _P, _I64, ctypes.c_double, ctypes.c_double, _P, _P, ctypes.c_size_t, _P, _P]),
     "puro_muonh_grouped_workspace_size": (ctypes.c_size_t, [_P, _I32]),
     "puro_muonh_step_grouped": (_I32, [_P, _I32, ctypes.c_double, _P, _P, ctypes.c_size_t, _P]),
+    "puro_muon_direction_workspace_size": (ctypes.c_size_t, [_P, _I32]),
+    "puro_muon_direction_grouped": (_I32, [_P, _I32, ctypes.c_double, _I32, _P, _I32, _P, ctypes.c_size_t, _P, _P]),
     "puro_swiglu_bf16": (_I32, [_P, _P, _I64, _I64, _I64, _P, _P]),
     "puro_fp8_linear_fprop": (_I32, [_P, _P, _P, _P, ctypes.c_size_t, _P, _P]),
     "puro_fp8_linear_dgrad": (_I32, [_P, _P, _P, _P, ctypes.c_size_t, _P, _P]),
@@ -458,6 +460,74 @@ def puro_muonh_step_grouped(mats, eta: float, sums: torch.Tensor, workspace: tor
                                                 _ptr(workspace, None, "workspace"),
                                                 workspace.numel() * workspace.element_size(), _stream(stream))
     _check("puro_muonh_step_grouped", st)
+
+
+MUON_STEPS = ((3.4445, -4.7750, 2.0315),) * 5  # Muon's Newton-Schulz coefficients
+
+
+class puro_muon_matrix_t(ctypes.Structure):
+    """Mirror of the C struct puro_muon_matrix_t."""
+    _fields_ = [("grad", ctypes.c_void_p), ("momentum", ctypes.c_void_p), ("u", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("grad_stride", ctypes.c_int64),
+                ("u_stride", ctypes.c_int64), ("grad_type", ctypes.c_int32), ("u_type", ctypes.c_int32),
+                ("reserved", ctypes.c_int64)]
+
+
+def muon_table(mats):
+    """The host table of puro_muon_direction_grouped for a fixed list of (grad,
+    momentum or None, u): grad and u are bf16 or fp32 [rows, cols] with unit column
+    stride, momentum is fp32 [rows, cols].  Build it once and pass it to every call
+    (the tensors must stay alive and in place)."""
+    table = (puro_muon_matrix_t * max(1, len(mats)))()
+    types = {torch.bfloat16: 0, torch.float32: 1}
+    table.tensors = []
+    for i, (g, m, u) in enumerate(mats):
+        for t, name in ((g, "grad"), (u, "u")):
+            if not t.is_cuda or t.dtype not in types or t.dim() != 2 or t.shape != g.shape:
+                raise ValueError(f"matrix {i}: {name} must be a bf16 or fp32 CUDA tensor {tuple(g.shape)}")
+            if t.numel() and t.shape[1] > 1 and t.stride(1) != 1:
+                raise ValueError(f"matrix {i}: {name} must have unit column stride")
+        if m is not None and m.shape != g.shape:
+            raise ValueError(f"matrix {i}: momentum is {tuple(m.shape)}, expected {tuple(g.shape)}")
+        rows, cols = g.shape
+        table[i] = puro_muon_matrix_t(g.data_ptr() or None, _ptr(m, torch.float32, "momentum"), u.data_ptr() or None, rows, cols,
+                                      g.stride(0) if rows > 1 else cols, u.stride(0) if rows > 1 else cols, types[g.dtype],
+                                      types[u.dtype], 0)
+        table.tensors += [t for t in (g, m, u) if t is not None]
+    table.count = len(mats)
+    devices = {t.get_device() for t in table.tensors if t.numel()}
+    if len(devices) > 1:
+        raise ValueError(f"the matrices are on several devices: {sorted(devices)}")
+    table.device = devices.pop() if devices else None
+    return table
+
+
+def _muon_table(mats):
+    return mats if isinstance(mats, ctypes.Array) else muon_table(mats)
+
+
+def puro_muon_direction_workspace_size(mats) -> int:
+    table = _muon_table(mats)
+    return int(load_library().puro_muon_direction_workspace_size(table, table.count))
+
+
+def puro_muon_direction_grouped(mats, workspace: torch.Tensor, momentum: float = 0.95, nesterov: bool = True,
+                                coefficients=MUON_STEPS, dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The Muon direction u of every matrix: the momentum buffer takes the gradient,
+    and its update, divided by its Frobenius norm, is orthogonalised by a
+    Newton-Schulz step for each (a, b, c) of coefficients.  mats: a list of (grad,
+    momentum or None, u) or a table from muon_table()."""
+    table = _muon_table(mats)
+    if table.device not in (None, _current_device()):
+        raise ValueError(f"the matrices are on cuda:{table.device}, the current device is cuda:{_current_device()}")
+    _on_current_device(workspace, dev_status)
+    flat = [float(x) for step in coefficients for x in step]
+    if any(len(step) != 3 for step in coefficients):
+        raise ValueError("coefficients are triples (a, b, c)")
+    st = load_library().puro_muon_direction_grouped(table, table.count, float(momentum), int(bool(nesterov)),
+                                                    (ctypes.c_double * max(1, len(flat)))(*flat), len(coefficients),
+                                                    *_ws(workspace), _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
+    _check("puro_muon_direction_grouped", st)
 
 
 def muonh_radius(w0: torch.Tensor) -> float:
@@ -1046,6 +1116,6 @@ def quantize(x: torch.Tensor, fmt: int = E4M3, scaling: int = SCALE_BLOCK, role:
 
 __all__ = [n for n in dir() if n.startswith("puro_")] + [
     "E4M3", "E5M2", "SCALE_TENSOR", "SCALE_BLOCK", "ROLE_ACT", "ROLE_WEIGHT", "ACT_NONE", "ACT_RELU", "ACT_SILU",
-    "ACT_GELU", "ACT_GELU_TANH", "ROPE_NONE", "ROPE_LINEAR", "ROPE_BASE", "ROPE_TURNS", "ROPE_INDEX", "rope_frequencies", "PuroError", "FP8Operand",
+    "ACT_GELU", "ACT_GELU_TANH", "ROPE_NONE", "ROPE_LINEAR", "ROPE_BASE", "ROPE_TURNS", "ROPE_INDEX", "rope_frequencies", "MUON_STEPS", "muon_table", "PuroError", "FP8Operand",
     "Quantized", "quantize", "load_library", "empty_scales", "scale_vec_shape", "LIB_PATH", "HEADER_PATH",
 ]

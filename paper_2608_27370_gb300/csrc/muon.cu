@@ -1,0 +1,1083 @@
+// muon.cu -- the Muon directions u of many matrices: the momentum's update, and its
+// orthogonalisation by Newton-Schulz products (Puro-2B, section "Hyperball
+// Optimization", takes the Muon update direction u as given and does not specify
+// the orthogonalisation; this is the published one: odd polynomials of the update's
+// singular values, a few products each).
+//
+// For a matrix of m x n, m <= n (a taller one is transposed on its way in and out):
+//     V = the momentum's update,  X = V / ||V||_F,
+//     per step (a, b, c):  A = X X^T,  X <- (a I + b A + c A^2) X.
+//
+// How it is computed here.  The products run on the tensor cores in FP16 with FP32
+// accumulation (FP16 for its 11 digits: the singular values are at most about one,
+// so that a power of two per step puts every matrix in range).  Two steps at a time,
+// with A0 = X X^T, B0 = a I + b A0 + c A0^2:
+//     A1 = B0 A0 B0 (the next step's A, for B0 and A0 commute),
+//     B1 = a' I + b' A1 + c' A1^2,  X <- (B1 B0) X,
+// where products of m x m take the place of the second step's two of m x n: for n =
+// 6 m a pair costs 24 m^3 products instead of 38.  All m x m results are symmetric, so
+// only tiles on and above the diagonal are computed and each is stored twice.
+//
+// Where digits are lost.  A rounding of X adds noise of full rank, and the steps
+// blow small singular values up (3.4 times each, by Muon's coefficients), the noise
+// with them; a rounding of B only turns X's rows a little into one another.  So X is
+// kept as two FP16 numbers, x = hi + lo, 22 digits, where a pair of steps follows:
+// B1 B0 multiplies both (lo after hi, into the same accumulator), and A0 takes hi
+// alone.  Of random and of low-rank matrices with noise u is then within 1 to 4
+// 2^-10 of itself (2-norm), against 5 times that without lo, and 30 in BF16.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <cmath>
+#include <mutex>
+
+#include "internal.h"
+#include "ptx.cuh"
+
+namespace puro {
+namespace {
+
+constexpr int kMaxClasses = 8;   // shapes of one launch (their tensor maps are kernel parameters)
+constexpr int kMaxMats = 128;    // matrices of one launch
+constexpr int kMaxSteps = 64;
+constexpr int32_t kStatusTimeout = 4;  // PURO_ERR_TIMEOUT
+constexpr uint64_t kDrainNs = 2000000000ull, kSettleNs = 200000ull;
+
+// ------------------------------------------------ the update and its norm
+constexpr int kInRows = 64, kInCols = 128, kInThreads = 256;  // tile of the two passes over V
+constexpr int kInPasses = kInRows * kInCols / 8 / kInThreads;
+
+enum MatFlags : uint8_t {
+    kGradBf16 = 1,
+    kTall = 2,      // more rows than columns: X is its transpose
+    kVectors = 4,   // eight columns of a row are 16- or 32-byte aligned in grad and momentum
+    kOutF32 = 8,
+    kOutVectors = 16,  // eight columns of a row of u can be stored in 16-byte pieces
+};
+struct MuonIn {
+    int count;
+    int tile0[kMaxMats + 1];  // first tile of each matrix
+    const void *grad[kMaxMats];
+    float *momentum[kMaxMats];
+    int64_t stride[kMaxMats];
+    int rows[kMaxMats], cols[kMaxMats], ldx[kMaxMats];
+    uint16_t *hi[kMaxMats], *lo[kMaxMats];
+    uint8_t flags[kMaxMats];
+    float mu;
+    int nesterov;
+    bool store_lo;
+    double *partial;  // [tiles]: sum of V^2 over each tile
+    float2 *scale;    // [count]: X = (V * x) * y
+};
+
+PURO_DEV int mat_of(const int *start, int count, int t) {
+    int lo = 0, hi = count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (start[mid] <= t) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+// Eight values of V at (r, c0 ...), zero outside the matrix.  UPDATE: the momentum
+// takes the gradient first and is stored; else it has.
+template <bool UPDATE>
+PURO_DEV void update8(const MuonIn &p, int m, int r, int c0, float (&v)[8]) {
+    const int cols = p.cols[m];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = 0.0f;
+    if (r >= p.rows[m] || c0 >= cols) return;
+    const uint8_t f = p.flags[m];
+    float *mom = p.momentum[m] ? p.momentum[m] + static_cast<int64_t>(r) * cols + c0 : nullptr;
+    const int64_t at = r * p.stride[m] + c0;
+    float w[8];
+    if (f & kVectors) {
+        if (f & kGradBf16) {
+            const uint4 x = __ldg(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.grad[m]) + at));
+            const uint32_t s[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                v[2 * k] = __uint_as_float(s[k] << 16);
+                v[2 * k + 1] = __uint_as_float(s[k] & 0xFFFF0000u);
+            }
+        } else {
+            const float4 *g = reinterpret_cast<const float4 *>(static_cast<const float *>(p.grad[m]) + at);
+            *reinterpret_cast<float4 *>(&v[0]) = __ldg(g);
+            *reinterpret_cast<float4 *>(&v[4]) = __ldg(g + 1);
+        }
+        if (!mom) return;
+        *reinterpret_cast<float4 *>(&w[0]) = *reinterpret_cast<const float4 *>(mom);
+        *reinterpret_cast<float4 *>(&w[4]) = *reinterpret_cast<const float4 *>(mom + 4);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            w[k] = 0.0f;
+            if (c0 + k >= cols) continue;
+            v[k] = f & kGradBf16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t *>(p.grad[m])[at + k]) << 16)
+                                 : static_cast<const float *>(p.grad[m])[at + k];
+            if (mom) w[k] = mom[k];
+        }
+        if (!mom) return;
+    }
+    if constexpr (UPDATE) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = fmaf(p.mu, w[k], v[k]);
+        if (f & kVectors) {
+            *reinterpret_cast<float4 *>(mom) = *reinterpret_cast<const float4 *>(&w[0]);
+            *reinterpret_cast<float4 *>(mom + 4) = *reinterpret_cast<const float4 *>(&w[4]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (c0 + k < cols) mom[k] = w[k];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = p.nesterov ? fmaf(p.mu, w[k], v[k]) : w[k];
+}
+
+struct InTile {
+    int m, r0, c0;
+};
+PURO_DEV InTile in_tile(const MuonIn &p) {
+    InTile t;
+    t.m = mat_of(p.tile0, p.count, blockIdx.x);
+    const int i = static_cast<int>(blockIdx.x) - p.tile0[t.m], across = (p.cols[t.m] + kInCols - 1) / kInCols;
+    t.r0 = i / across * kInRows;
+    t.c0 = i % across * kInCols;
+    return t;
+}
+
+// The momentum takes the gradient; each tile's sum of V^2.  A thread's 32 squares
+// are summed in FP32, in FP64 where that left its range (or all are zero), the
+// threads' sums in FP64 in a fixed order.  Bound by memory.
+__global__ void __launch_bounds__(kInThreads) muon_update_kernel(const __grid_constant__ MuonIn p) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const InTile t = in_tile(p);
+    const int r = t.r0 + threadIdx.x / 16, c = t.c0 + threadIdx.x % 16 * 8;
+    float v[kInPasses][8], s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kInPasses; ++i) update8<true>(p, t.m, r + 16 * i, c, v[i]);
+#pragma unroll
+    for (int i = 0; i < kInPasses; ++i)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s = fmaf(v[i][k], v[i][k], s);
+    double d = s;
+    if (!(s > 1e-24f && s < 1e36f)) {
+        d = 0.0;
+#pragma unroll
+        for (int i = 0; i < kInPasses; ++i)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) d += static_cast<double>(v[i][k]) * v[i][k];
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xFFFFFFFFu, d, o);
+    __shared__ double part[kInThreads / 32];
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x / 32] = d;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double sum = 0.0;
+#pragma unroll
+        for (int w = 0; w < kInThreads / 32; ++w) sum += part[w];
+        p.partial[blockIdx.x] = sum;
+    }
+}
+
+// X's power of two: entries are at most 1.
+constexpr int kX0Exp = 14;
+
+// Each matrix's factor 2^14 / ||V||_F in two parts, neither of which leaves FP32's
+// range; NaN where the norm is not finite (all of u is then NaN), 0 for V = 0.
+__global__ void __launch_bounds__(256) muon_norm_kernel(const __grid_constant__ MuonIn p) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int m = blockIdx.x;
+    double d = 0.0;
+    for (int i = p.tile0[m] + threadIdx.x; i < p.tile0[m + 1]; i += 256) d += p.partial[i];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xFFFFFFFFu, d, o);
+    __shared__ double part[8];
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x / 32] = d;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    double sum = 0.0;
+    for (int w = 0; w < 8; ++w) sum += part[w];
+    float2 f = make_float2(0.0f, 0.0f);
+    if (!(sum < INFINITY)) {
+        f.x = f.y = NAN;
+    } else if (sum > 0.0) {
+        const double scale = static_cast<double>(1 << kX0Exp) / sqrt(sum);
+        const int e = ilogb(scale) / 2;
+        f = make_float2(static_cast<float>(ldexp(1.0, e)), static_cast<float>(ldexp(scale, -e)));
+    }
+    p.scale[m] = f;
+}
+
+// X = V / ||V||_F as FP16 pairs, a tall matrix transposed.
+__global__ void __launch_bounds__(kInThreads) muon_normalise_kernel(const __grid_constant__ MuonIn p) {
+    __shared__ uint32_t turn[kInCols][kInRows + 1];  // (hi, lo) of the transposed tile
+    pdl_wait();
+    pdl_launch_dependents();
+    const InTile t = in_tile(p);
+    const float2 f = p.scale[t.m];
+    const bool tall = p.flags[t.m] & kTall;
+    const int lr = threadIdx.x / 16, lc = threadIdx.x % 16 * 8, ldx = p.ldx[t.m];
+    float v[kInPasses][8];
+#pragma unroll
+    for (int i = 0; i < kInPasses; ++i) update8<false>(p, t.m, t.r0 + lr + 16 * i, t.c0 + lc, v[i]);
+#pragma unroll
+    for (int i = 0; i < kInPasses; ++i) {
+        uint16_t hi[8], lo[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float x = (v[i][k] * f.x) * f.y;
+            const __half h = __float2half_rn(x);
+            hi[k] = __half_as_ushort(h);
+            lo[k] = __half_as_ushort(__float2half_rn(x - __half2float(h)));
+        }
+        const int r = t.r0 + lr + 16 * i, c = t.c0 + lc;
+        if (tall) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) turn[lc + k][lr + 16 * i] = hi[k] | static_cast<uint32_t>(lo[k]) << 16;
+        } else if (r < p.rows[t.m] && c < ldx) {
+            const int64_t at = static_cast<int64_t>(r) * ldx + c;
+            auto pack = [](const uint16_t *h) {
+                return make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+            };
+            *reinterpret_cast<uint4 *>(p.hi[t.m] + at) = pack(hi);
+            if (p.store_lo) *reinterpret_cast<uint4 *>(p.lo[t.m] + at) = pack(lo);
+        }
+    }
+    if (!tall) return;
+    __syncthreads();
+    // a row of X: a column of V, 64 values, eight to a thread
+    const int r8 = threadIdx.x % 8 * 8;
+#pragma unroll
+    for (int i = 0; i < kInCols / 32; ++i) {
+        const int c = threadIdx.x / 8 + 32 * i;
+        if (t.c0 + c >= p.cols[t.m] || t.r0 + r8 >= ldx) continue;
+        uint32_t x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = turn[c][r8 + k];
+        const int64_t at = static_cast<int64_t>(t.c0 + c) * ldx + t.r0 + r8;
+        uint32_t h[4], l[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            h[k] = __byte_perm(x[2 * k], x[2 * k + 1], 0x5410);
+            l[k] = __byte_perm(x[2 * k], x[2 * k + 1], 0x7632);
+        }
+        *reinterpret_cast<uint4 *>(p.hi[t.m] + at) = make_uint4(h[0], h[1], h[2], h[3]);
+        if (p.store_lo) *reinterpret_cast<uint4 *>(p.lo[t.m] + at) = make_uint4(l[0], l[1], l[2], l[3]);
+    }
+}
+
+// ------------------------------------------------------------ the products
+// D = A B^T in FP16 (kind::f16), FP32 accumulators, as CTA pairs compute the linears'
+// products (see gemm.cu): pair MMAs of 256 x BN, a ring of k-blocks of 64 that the
+// TMA fills, two accumulators, so that a tile's epilogue runs beside the next one's
+// MMAs.
+//   warp 0       TMA producer (both CTAs)
+//   warp 1       MMA issuer (even CTA); tensor memory
+//   warps 4..11  epilogue (both CTAs): warp 4 + 4h + q has rows 32q .. of the CTA's
+//                128 and the h-th half of the columns
+// B is [N, K] with K contiguous, or X_MAJOR [K, N] with N contiguous (X as the right
+// factor of B X), which the tensor cores read as it lies (MN-major).  The matrices
+// of one shape are a class: one tensor map each for A, B and D with the matrix as
+// the third coordinate.
+constexpr int kBM = 128, kBK = 64;
+constexpr int kThreads = 384;
+constexpr int kEpiWarps = 8;
+constexpr int kTmemCols = 512;
+
+enum Epilogue : int {
+    kStore = 0,  // alpha D, symmetric
+    kPoly = 1,   // alpha D + beta G + gamma I, symmetric
+    kNext = 2,   // alpha D as hi (and lo)
+    kOut = 3,    // alpha D to u
+};
+
+struct MuonMaps {
+    CUtensorMap a, b, b_lo, d, d_lo;  // a: box 64 x 128; b: 64 x BN / 2, X_MAJOR 64 x 64; d: 32 x 32 (64-byte swizzle)
+};
+struct MuonPhase {
+    MuonMaps maps[kMaxClasses];
+    int classes, units;
+    int unit0[kMaxClasses + 1];  // first tile of each class
+    int per[kMaxClasses];        // tiles of a matrix
+    int tiles_n[kMaxClasses], tiles_m[kMaxClasses];
+    int rows[kMaxClasses], cols[kMaxClasses];  // of D
+    int kb[kMaxClasses];         // k-blocks of B (of lo as many more)
+    int first[kMaxClasses];      // kOut: the class's first matrix in MuonOut
+    const uint16_t *g[kMaxClasses];  // kPoly: G of the first matrix
+    int64_t g_batch[kMaxClasses];
+    int ldg[kMaxClasses];
+    float alpha, beta, gamma;
+    int passes;                  // 2: B's lo after its hi
+    bool store_lo;               // kNext
+    uint32_t idesc;
+    int32_t *status;
+    uint64_t wait_ns;
+};
+struct MuonOut {
+    void *u[kMaxMats];
+    int64_t stride[kMaxMats];
+    uint8_t flags[kMaxMats];
+};
+
+template <int BN>
+struct ProductSmem {
+    static constexpr int kStages = 192 * 1024 / (kBM * 128 + BN / 2 * 128);  // 6 (256), 8 (128)
+    alignas(1024) uint8_t a[kStages][kBM * 128];
+    alignas(1024) uint8_t b[kStages][BN / 2 * 128];
+    alignas(1024) uint8_t stage[kEpiWarps][4096];
+    uint64_t full[kStages], empty[kStages];
+    uint64_t tfull[2], tempty[2];
+    uint64_t drain;
+    uint32_t tmem_base;
+    volatile int abort_flag;
+};
+
+struct Unit {
+    int cls, z, m0, n0, kb;
+    bool mirror;  // off the diagonal of a symmetric D: stored transposed as well
+};
+
+template <int BN, bool SYM>
+PURO_DEV Unit unit_of(const MuonPhase &p, int u) {
+    Unit w;
+    w.cls = 0;
+    while (w.cls + 1 < p.classes && u >= p.unit0[w.cls + 1]) ++w.cls;
+    int i = u - p.unit0[w.cls];
+    w.z = i / p.per[w.cls];
+    i -= w.z * p.per[w.cls];
+    w.kb = p.kb[w.cls];
+    if constexpr (SYM) {
+        constexpr int kAcross = 256 / BN;
+        const int n = p.tiles_n[w.cls];
+        int row = 0;
+        while (i >= n - kAcross * row) {
+            i -= n - kAcross * row;
+            ++row;
+        }
+        w.m0 = 256 * row;
+        w.n0 = BN * (kAcross * row + i);
+        w.mirror = w.n0 >= w.m0 + 256;
+    } else {  // the rows of B fastest: a wave shares columns of X
+        const int tm = p.tiles_m[w.cls];
+        w.m0 = 256 * (i % tm);
+        w.n0 = BN * (i / tm);
+        w.mirror = false;
+    }
+    return w;
+}
+
+template <class Smem>
+PURO_DEV bool wait_or_abort(Smem &sm, uint64_t *bar, uint32_t parity, uint64_t ns, int32_t *status, int lane) {
+    if (__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity)) ||
+        __all_sync(0xFFFFFFFFu, sm.abort_flag == 0 && mbar_wait_bounded(bar, parity, ns)))
+        return true;
+    if (lane == 0) {
+        sm.abort_flag = 1;
+        if (status) atomicExch(status, kStatusTimeout);
+    }
+    return false;
+}
+
+PURO_DEV uint32_t half2_bits(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+PURO_DEV uint32_t bf162_bits(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// A 32 x 32 block of 16-bit values in the staging tile, rows of 64 bytes with the
+// 64-byte swizzle; w holds the lane's row in pairs of columns.
+PURO_DEV void stage_rows(uint8_t *to, const uint32_t (&w)[16], int lane) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<uint4 *>(to + 64 * lane + 16 * (i ^ ((lane >> 1) & 3))) =
+            make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+}
+// Its transpose: the lane's row becomes a column.  Neighbouring lanes exchange
+// halves, so that each stores two rows' values of one column in 32 bits.
+PURO_DEV void stage_columns(uint8_t *to, const uint32_t (&w)[16], int lane) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {  // columns 2i (even lanes) and 2i + 1 (odd lanes)
+        const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, w[i], 1);
+        const uint32_t x = lane & 1 ? __byte_perm(other, w[i], 0x7632) : __byte_perm(w[i], other, 0x5410);
+        const int row = 2 * i + (lane & 1), word = lane >> 1;
+        *reinterpret_cast<uint32_t *>(to + 64 * row + 16 * ((word >> 2) ^ ((row >> 1) & 3)) + 4 * (word & 3)) = x;
+    }
+}
+
+// A staged block to rows r0 .. and columns c0 .. of u.
+PURO_DEV void block_to_u(const uint8_t *from, bool f32, bool vectors, void *u, int64_t stride, int r0, int c0, int rows, int cols,
+                         int lane) {
+    if (vectors) {
+        const int per = f32 ? 8 : 4;  // 16-byte pieces of a row
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int row = (32 / per) * i + lane / per, piece = lane % per;
+            if (row >= 32) break;
+            const int c = c0 + piece * (32 / per);
+            if (r0 + row >= rows || c >= cols) continue;
+            const int s = f32 ? piece ^ (row & 7) : piece ^ ((row >> 1) & 3);
+            const uint4 x = *reinterpret_cast<const uint4 *>(from + (f32 ? 128 : 64) * row + 16 * s);
+            const int64_t at = (r0 + row) * stride + c;
+            *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(u) + at * (f32 ? 4 : 2)) = x;
+        }
+        return;
+    }
+    if (c0 + lane >= cols) return;
+    for (int row = 0; row < 32 && r0 + row < rows; ++row) {
+        const int64_t at = (r0 + row) * stride + c0 + lane;
+        if (f32)
+            static_cast<float *>(u)[at] = *reinterpret_cast<const float *>(from + 128 * row + 16 * ((lane >> 2) ^ (row & 7)) + 4 * (lane & 3));
+        else
+            static_cast<uint16_t *>(u)[at] =
+                *reinterpret_cast<const uint16_t *>(from + 64 * row + 16 * ((lane >> 3) ^ ((row >> 1) & 3)) + 2 * (lane & 7));
+    }
+}
+
+template <int BN, bool X_MAJOR, int EPI>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    muon_product_kernel(const __grid_constant__ MuonPhase p, const __grid_constant__ MuonOut out) {
+    using Smem = ProductSmem<BN>;
+    constexpr int kStages = Smem::kStages;
+    constexpr bool kSym = EPI == kStore || EPI == kPoly;
+    constexpr uint32_t kStageBytes = kBM * 128 + BN / 2 * 128;  // of one CTA
+    extern __shared__ uint8_t smem_raw[];
+    Smem &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    const int warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0);
+    const int lane = threadIdx.x & 31;
+    const int rank = __shfl_sync(0xFFFFFFFFu, static_cast<int>(cluster_ctarank()), 0);
+    const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(&sm.full[s], 1);
+            mbar_init(&sm.empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&sm.tfull[b], 1);
+            mbar_init(&sm.tempty[b], 2 * kEpiWarps);
+        }
+        mbar_init(&sm.drain, 1);
+        sm.abort_flag = 0;
+        fence_mbarrier_init();
+    }
+    __syncthreads();
+    if (warp == 1) {
+        tmem_alloc_pair(&sm.tmem_base, kTmemCols);
+        tmem_relinquish_alloc_permit_pair();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    cluster_arrive();
+    cluster_wait();  // both CTAs' barriers exist
+    pdl_wait();
+    pdl_launch_dependents();
+    const uint32_t tmem = sm.tmem_base;
+
+    if (warp == 0) {
+        // ------------------------------------------------ TMA producer
+        const uint32_t e = elect_one();
+        const uint32_t full0 = mapa_shared(smem_u32(&sm.full[0]), 0);
+        uint32_t stage = 0, phase = 0, issued = 0;
+        bool ok = true;
+        for (int u = pair; u < p.units && ok; u += pairs) {
+            const Unit w = unit_of<BN, kSym>(p, u);
+            const MuonMaps &maps = p.maps[w.cls];
+            const int a_row = w.m0 + kBM * rank, b_row = w.n0 + BN / 2 * rank;
+            for (int pass = 0; pass < p.passes && ok; ++pass) {
+                const CUtensorMap *mb = pass ? &maps.b_lo : &maps.b;
+                for (int kb = 0; kb < w.kb; ++kb) {
+                    ok = wait_or_abort(sm, &sm.empty[stage], phase ^ 1u, p.wait_ns, p.status, lane);
+                    if (!ok) break;
+                    const uint32_t bar = full0 + 8u * stage;
+                    if (rank == 0 && e) mbar_arrive_expect_tx(&sm.full[stage], 2u * kStageBytes);
+                    tma_load_3d_pair_e(e, sm.a[stage], &maps.a, bar, kb * kBK, a_row, w.z);
+                    if constexpr (X_MAJOR) {
+#pragma unroll
+                        for (int i = 0; i < BN / 128; ++i)
+                            tma_load_3d_pair_e(e, sm.b[stage] + 8192 * i, mb, bar, b_row + 64 * i, kb * kBK, w.z);
+                    } else {
+                        tma_load_3d_pair_e(e, sm.b[stage], mb, bar, kb * kBK, b_row, w.z);
+                    }
+                    ++issued;
+                    if (++stage == kStages) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
+                }
+            }
+        }
+        if (rank == 0) {  // every fill of the ring (both CTAs' copies) lands before the pair exits
+            for (uint32_t s = 0; s < kStages; ++s) {
+                const uint32_t fills = issued / kStages + (s < issued % kStages ? 1u : 0u);
+                if (fills > 0) mbar_wait_bounded(&sm.full[s], (fills - 1u) & 1u, kDrainNs);
+            }
+        }
+        if (!ok) {  // this CTA's copies count on the even CTA's barriers: give those in flight time to land
+            const uint64_t t0 = global_timer_ns();
+            while (global_timer_ns() - t0 < kSettleNs) {
+            }
+        }
+    } else if (warp == 1 && rank == 0) {
+        // ------------------------------------------------ MMA issuer
+        const uint32_t e = elect_one();
+        uint32_t stage = 0, phase = 0;
+        int local = 0;
+        bool ok = true;
+        for (int u = pair; u < p.units && ok; u += pairs, ++local) {
+            const Unit w = unit_of<BN, kSym>(p, u);
+            const int buf = local & 1;
+            ok = wait_or_abort(sm, &sm.tempty[buf], ((local >> 1) & 1u) ^ 1u, p.wait_ns, p.status, lane);
+            const uint32_t d = tmem + 256u * buf;
+            const int kbs = w.kb * p.passes;
+            for (int kb = 0; kb < kbs && ok; ++kb) {
+                ok = wait_or_abort(sm, &sm.full[stage], phase, p.wait_ns, p.status, lane);
+                if (!ok) break;
+                tc_fence_after_sync();
+                const uint32_t a = smem_u32(sm.a[stage]), b = smem_u32(sm.b[stage]);
+#pragma unroll
+                for (int k = 0; k < kBK / 16; ++k) {
+                    const uint64_t bd = X_MAJOR ? smem_desc_mn_sw128(b + 2048 * k, 8192) : smem_desc_k_sw128(b + 32 * k);
+                    mma_pair_f16_e(e, d, smem_desc_k_sw128(a + 32 * k), bd, p.idesc, kb > 0 || k > 0 ? 1u : 0u);
+                }
+                tc_commit_pair_multicast_e(e, &sm.empty[stage], 3);
+                if (++stage == kStages) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
+            }
+            if (ok) tc_commit_pair_multicast_e(e, &sm.tfull[buf], 3);
+        }
+        if (e) {  // all MMAs issued are complete before teardown
+            tc_commit_pair(&sm.drain);
+            mbar_wait_bounded(&sm.drain, 0, kDrainNs);
+        }
+        __syncwarp();
+    } else if (warp >= 4) {
+        // ------------------------------------------------ epilogue
+        const int q = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t e = elect_one();
+        uint8_t *stage_buf = sm.stage[warp - 4];
+        const uint32_t tempty0 = mapa_shared(smem_u32(&sm.tempty[0]), 0);
+        uint32_t pieces = 0;
+        // one 32 x 32 block by way of the next half of the staging tile
+        auto store = [&](const CUtensorMap *map, const uint32_t(&w)[16], bool transposed, int x, int y, int z) {
+            uint8_t *to = stage_buf + 2048 * (pieces & 1u);
+            if (e) bulk_wait_group_read<1>();
+            __syncwarp();
+            if (transposed)
+                stage_columns(to, w, lane);
+            else
+                stage_rows(to, w, lane);
+            fence_proxy_async_smem();
+            __syncwarp();
+            tma_store_3d_e(e, map, to, x, y, z);
+            ++pieces;
+        };
+        int local = 0;
+        for (int u = pair; u < p.units; u += pairs, ++local) {
+            const Unit w = unit_of<BN, kSym>(p, u);
+            const int buf = local & 1;
+            if (!wait_or_abort(sm, &sm.tfull[buf], (local >> 1) & 1u, p.wait_ns, p.status, lane)) break;
+            tc_fence_after_sync();
+            const MuonMaps &maps = p.maps[w.cls];
+            const int row0 = w.m0 + kBM * rank + 32 * q, rows = p.rows[w.cls], cols = p.cols[w.cls];
+            const uint32_t acc = tmem + (static_cast<uint32_t>(32 * q) << 16) + 256u * buf + BN / 2 * half;
+#pragma unroll 1
+            for (int i = 0; i < BN / 64; ++i) {
+                uint32_t r[32];
+                tmem_ld_32x32b_x32(acc + 32 * i, r);
+                tmem_ld_wait();
+                if (i == BN / 64 - 1) {
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster_cta_scope(tempty0 + 8u * buf);
+                }
+                const int col = w.n0 + BN / 2 * half + 32 * i;
+                if (row0 >= rows || col >= cols) continue;
+                float v[32];
+#pragma unroll
+                for (int k = 0; k < 32; ++k) v[k] = p.alpha * __uint_as_float(r[k]);
+                if constexpr (EPI == kPoly) {
+                    const int row = row0 + lane;
+                    const uint16_t *g = p.g[w.cls] + w.z * p.g_batch[w.cls] + static_cast<int64_t>(row) * p.ldg[w.cls] + col;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+                        if (row < rows && col + 8 * k < p.ldg[w.cls]) x = __ldg(reinterpret_cast<const uint4 *>(g) + k);
+                        const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&xs[j]));
+                            v[8 * k + 2 * j] = fmaf(p.beta, f.x, v[8 * k + 2 * j]);
+                            v[8 * k + 2 * j + 1] = fmaf(p.beta, f.y, v[8 * k + 2 * j + 1]);
+                        }
+                    }
+                    if (col <= row0 + 31 && row0 <= col + 31) {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            if (row0 + lane == col + k) v[k] += p.gamma;
+                    }
+                }
+                if constexpr (EPI == kOut) {
+                    const int m = p.first[w.cls] + w.z;
+                    const uint8_t f = out.flags[m];
+                    const bool tall = f & kTall, f32 = f & kOutF32;
+                    __syncwarp();  // the block before has left the staging tile
+                    if (f32) {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) {
+                            const int sr = tall ? k : lane, sc = tall ? lane : k;
+                            *reinterpret_cast<float *>(stage_buf + 128 * sr + 16 * ((sc >> 2) ^ (sr & 7)) + 4 * (sc & 3)) = v[k];
+                        }
+                    } else {
+                        uint32_t h[16];
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) h[k] = bf162_bits(v[2 * k], v[2 * k + 1]);
+                        if (tall)
+                            stage_columns(stage_buf, h, lane);
+                        else
+                            stage_rows(stage_buf, h, lane);
+                    }
+                    __syncwarp();
+                    block_to_u(stage_buf, f32, f & kOutVectors, out.u[m], out.stride[m], tall ? col : row0, tall ? row0 : col,
+                               tall ? cols : rows, tall ? rows : cols, lane);
+                } else {
+                    uint32_t h[16];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) h[k] = half2_bits(v[2 * k], v[2 * k + 1]);
+                    store(&maps.d, h, false, col, row0, w.z);
+                    if constexpr (kSym) {
+                        if (w.mirror) store(&maps.d, h, true, row0, col, w.z);
+                    } else if (p.store_lo) {
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h[k]));
+                            h[k] = half2_bits(v[2 * k] - f.x, v[2 * k + 1] - f.y);
+                        }
+                        store(&maps.d_lo, h, false, col, row0, w.z);
+                    }
+                }
+            }
+        }
+        if (e) bulk_wait_group0();
+        __syncwarp();
+    }
+    // the pair's MMAs are complete and read, and no arrival targets a CTA that has left
+    tc_fence_before_sync();
+    __syncthreads();
+    cluster_arrive();
+    cluster_wait();
+    tc_fence_after_sync();
+    if (warp == 1) tmem_dealloc_pair(tmem, kTmemCols);
+}
+
+// ------------------------------------------------------------------- host
+int64_t align_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
+
+struct Shape {
+    int64_t m, n;
+    bool operator==(const Shape &o) const { return m == o.m && n == o.n; }
+};
+Shape shape_of(const puro_muon_matrix_t &a) { return {std::min(a.rows, a.cols), std::max(a.rows, a.cols)}; }
+bool empty(const puro_muon_matrix_t &a) { return a.rows == 0 || a.cols == 0; }
+
+// The matrices of one series of launches: some in a row of the table, by shape.
+struct Chunk {
+    int count = 0, classes = 0;
+    int mats[kMaxMats];  // their places in the table, class by class
+    Shape shape[kMaxClasses];
+    int first[kMaxClasses + 1];
+};
+// Takes matrices from `at` on while they fit one chunk, and returns where it ended.
+int take_chunk(const puro_muon_matrix_t *mats, int at, int count, Chunk *c) {
+    *c = Chunk{};
+    int cls[kMaxMats];
+    int n[kMaxClasses] = {};
+    for (; at < count && c->count < kMaxMats; ++at) {
+        if (empty(mats[at])) continue;
+        const Shape s = shape_of(mats[at]);
+        int k = 0;
+        while (k < c->classes && !(c->shape[k] == s)) ++k;
+        if (k == kMaxClasses) break;
+        if (k == c->classes) c->shape[c->classes++] = s;
+        cls[c->count] = k;
+        c->mats[c->count++] = at;
+        ++n[k];
+    }
+    // classes of the longest rows first: their tiles are the long ones
+    int order[kMaxClasses], place[kMaxClasses];
+    for (int k = 0; k < c->classes; ++k) order[k] = k;
+    std::sort(order, order + c->classes, [&](int a, int b) {
+        return c->shape[a].n != c->shape[b].n ? c->shape[a].n > c->shape[b].n
+                                              : c->shape[a].m != c->shape[b].m ? c->shape[a].m > c->shape[b].m : a < b;
+    });
+    Shape sorted[kMaxClasses];
+    int next[kMaxClasses];
+    c->first[0] = 0;
+    for (int k = 0; k < c->classes; ++k) {
+        place[order[k]] = k;
+        sorted[k] = c->shape[order[k]];
+        next[k] = c->first[k];
+        c->first[k + 1] = c->first[k] + n[order[k]];
+    }
+    int by[kMaxMats];
+    for (int i = 0; i < c->count; ++i) by[next[place[cls[i]]]++] = c->mats[i];
+    std::copy(by, by + c->count, c->mats);
+    std::copy(sorted, sorted + c->classes, c->shape);
+    return at;
+}
+
+constexpr int64_t kAlign = 256;
+
+// Scratch of a chunk.
+struct Scratch {
+    int64_t bytes = 0;
+    int64_t x[4][kMaxClasses];  // offsets: X hi, lo and the next X's
+    int64_t g[4][kMaxClasses];  // G, B0, T (then B1 B0), B1
+    int64_t partial = 0, scale = 0;
+};
+int64_t tiles_in(int64_t rows, int64_t cols) {
+    return (rows + kInRows - 1) / kInRows * ((cols + kInCols - 1) / kInCols);
+}
+Scratch scratch_of(const puro_muon_matrix_t *mats, const Chunk &c) {
+    Scratch s;
+    auto take = [&](int64_t bytes) {
+        const int64_t at = s.bytes;
+        s.bytes += align_up(bytes, kAlign);
+        return at;
+    };
+    int64_t tiles = 0;
+    for (int i = 0; i < c.count; ++i) tiles += tiles_in(mats[c.mats[i]].rows, mats[c.mats[i]].cols);
+    s.partial = take(tiles * 8);
+    s.scale = take(c.count * 8);
+    for (int k = 0; k < c.classes; ++k) {
+        const int64_t n = c.first[k + 1] - c.first[k];
+        for (int b = 0; b < 4; ++b) s.x[b][k] = take(n * c.shape[k].m * align_up(c.shape[k].n, 8) * 2);
+        for (int b = 0; b < 4; ++b) s.g[b][k] = take(n * c.shape[k].m * align_up(c.shape[k].m, 8) * 2);
+    }
+    return s;
+}
+
+// One step's polynomial p(t) = a + b t + c t^2 of the squared singular values, and
+// what it does to singular values up to `most`: the bound of |p| and of sigma |p|.
+struct Step {
+    double a, b, c, most_p, most_out;
+};
+bool plan_step(const double *abc, double most, Step *s) {
+    s->a = abc[0];
+    s->b = abc[1];
+    s->c = abc[2];
+    if (!std::isfinite(s->a) || !std::isfinite(s->b) || !std::isfinite(s->c)) return false;
+    const double t1 = most * most;
+    auto p = [&](double t) { return s->a + t * (s->b + t * s->c); };
+    auto f = [&](double t) { return std::sqrt(t) * std::fabs(p(t)); };
+    s->most_p = std::max(std::fabs(s->a), std::fabs(p(t1)));
+    s->most_out = f(t1);
+    const double v = -s->b / (2 * s->c);  // (c = 0: not finite, no vertex)
+    if (v > 0 && v < t1) s->most_p = std::max(s->most_p, std::fabs(p(v)));
+    // extremes of sigma p(sigma^2): a + 3 b t + 5 c t^2 = 0
+    const double disc = 9 * s->b * s->b - 20 * s->a * s->c;
+    auto at = [&](double t) {
+        if (t > 0 && t < t1) s->most_out = std::max(s->most_out, f(t));
+    };
+    if (s->c != 0) {
+        if (disc >= 0) {
+            at((-3 * s->b + std::sqrt(disc)) / (10 * s->c));
+            at((-3 * s->b - std::sqrt(disc)) / (10 * s->c));
+        }
+    } else if (s->b != 0) {
+        at(-s->a / (3 * s->b));
+    }
+    return s->most_p < 1024 && s->most_out < 1024;
+}
+constexpr double kMargin = 1.0 + 1.0 / 64;  // of a bound, for what roundings add
+// The power of two that puts values up to `most` within FP16, with half of it to spare.
+double pow2_for(double most) { return std::ldexp(1.0, most > 0 ? std::min(14, std::ilogb(32768.0 / (most * kMargin))) : 14); }
+
+template <class Kernel>
+int resident_pairs(Kernel kern, size_t smem, int sms) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(sms / 2 * 2), 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 2;
+    attr.val.clusterDim.y = 1;
+    attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n <= 0) {
+        (void)cudaGetLastError();
+        n = sms / 2;
+    }
+    return n;
+}
+
+template <int BN, bool X_MAJOR, int EPI>
+cudaError_t launch_product(const MuonPhase &p, const MuonOut &out, cudaStream_t s) {
+    auto kern = muon_product_kernel<BN, X_MAJOR, EPI>;
+    const size_t smem = sizeof(ProductSmem<BN>) + 1024;
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e != cudaSuccess) return e;
+    static int cache[64] = {0};
+    int dev = 0, most = 0;
+    if (cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < 64) most = cache[dev];
+    if (most == 0) {
+        most = resident_pairs(kern, smem, sm_count_here());
+        if (dev >= 0 && dev < 64) cache[dev] = most;
+    }
+    return launch_pdl(kern, dim3(2 * std::min(p.units, most)), dim3(kThreads), smem, s, p, out);
+}
+
+// The products of a chunk, phase after phase.
+struct Products {
+    const Chunk &c;
+    const Scratch &at;
+    uint8_t *ws;
+    int32_t *status;
+    cudaStream_t s;
+    MuonOut out;
+
+    int64_t ld(int k, bool square) const { return align_up(square ? c.shape[k].m : c.shape[k].n, 8); }
+    uint16_t *x(int b, int k) const { return reinterpret_cast<uint16_t *>(ws + at.x[b][k]); }
+    uint16_t *g(int b, int k) const { return reinterpret_cast<uint16_t *>(ws + at.g[b][k]); }
+    bool map(CUtensorMap *m, uint16_t *base, int k, bool square, int bx, int by, CUtensorMapSwizzle sw) const {
+        const int64_t cols = square ? c.shape[k].m : c.shape[k].n, row = 2 * ld(k, square);
+        return make_batched_map(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, base, cols, c.shape[k].m, c.first[k + 1] - c.first[k], row,
+                                row * c.shape[k].m, bx, by, sw);
+    }
+
+    // Tiles of 256 x bn, and what the slowest pair has to do, in k-blocks of 256 x 256.
+    double plan(MuonPhase *p, int bn, bool sym, int passes, bool k_is_n) const {
+        p->units = 0;
+        double work = 0, longest = 0;
+        const double cost = bn == 256 ? 1.0 : 0.55;
+        for (int k = 0; k < c.classes; ++k) {
+            const int64_t m = c.shape[k].m, cols = sym ? m : c.shape[k].n;
+            const int64_t tm = (m + 255) / 256, tn = (cols + bn - 1) / bn;
+            int64_t per = tm * tn;
+            if (sym) {
+                per = 0;
+                for (int64_t i = 0; i < tm; ++i) per += tn - 256 / bn * i;
+            }
+            p->unit0[k] = p->units;
+            p->per[k] = static_cast<int>(per);
+            p->tiles_m[k] = static_cast<int>(tm);
+            p->tiles_n[k] = static_cast<int>(tn);
+            p->rows[k] = static_cast<int>(m);
+            p->cols[k] = static_cast<int>(cols);
+            p->kb[k] = static_cast<int>(((k_is_n ? c.shape[k].n : m) + kBK - 1) / kBK);
+            p->first[k] = c.first[k];
+            const int64_t units = per * (c.first[k + 1] - c.first[k]);
+            p->units += static_cast<int>(units);
+            work += cost * static_cast<double>(units) * p->kb[k] * passes;
+            longest = std::max(longest, cost * p->kb[k] * passes);
+        }
+        p->classes = c.classes;
+        p->unit0[c.classes] = p->units;
+        const double pairs = 76, waves = std::ceil(p->units / pairs);
+        return std::max(longest, work / p->units * waves);
+    }
+
+    // EPI kStore / kPoly: square D (buffer d) of square A and B (buffers a, b), or with a < 0 of X X^T;
+    // kNext / kOut: the next X (or u) = square A times X.
+    template <int EPI>
+    cudaError_t run(int a, int b, int d, int x0, int passes, bool lo, double alpha, double beta, double gamma, int poly_g) const {
+        constexpr bool kSym = EPI == kStore || EPI == kPoly;
+        const bool gram = a < 0;
+        MuonPhase wide{}, narrow{};
+        const double tw = plan(&wide, 256, kSym, passes, gram), tn = plan(&narrow, 128, kSym, passes, gram);
+        const int bn = tw <= tn ? 256 : 128;
+        MuonPhase &p = bn == 256 ? wide : narrow;
+        const auto kSw = CU_TENSOR_MAP_SWIZZLE_128B;
+        for (int k = 0; k < c.classes; ++k) {
+            MuonMaps &m = p.maps[k];
+            bool ok = gram ? map(&m.a, x(x0, k), k, false, 64, 128, kSw) : map(&m.a, g(a, k), k, true, 64, 128, kSw);
+            if (kSym) {
+                ok = ok && (gram ? map(&m.b, x(x0, k), k, false, 64, bn / 2, kSw) : map(&m.b, g(b, k), k, true, 64, bn / 2, kSw));
+                ok = ok && map(&m.d, g(d, k), k, true, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+            } else {
+                ok = ok && map(&m.b, x(x0, k), k, false, 64, 64, kSw);
+                if (passes > 1) ok = ok && map(&m.b_lo, x(x0 + 1, k), k, false, 64, 64, kSw);
+                if (EPI == kNext) ok = ok && map(&m.d, x(x0 ^ 2, k), k, false, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+                if (lo) ok = ok && map(&m.d_lo, x((x0 ^ 2) + 1, k), k, false, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+            }
+            if (!ok) return cudaErrorInvalidValue;
+            if (EPI == kPoly) {
+                p.g[k] = g(poly_g, k);
+                p.ldg[k] = static_cast<int>(ld(k, true));
+                p.g_batch[k] = c.shape[k].m * ld(k, true);
+            }
+        }
+        p.alpha = static_cast<float>(alpha);
+        p.beta = static_cast<float>(beta);
+        p.gamma = static_cast<float>(gamma);
+        p.passes = passes;
+        p.store_lo = lo;
+        p.status = status;
+        p.wait_ns = wait_timeout_ns();
+        // kind::f16, FP32 accumulators, FP16 operands; B N-major for X; N, M = 256 (a pair MMA)
+        p.idesc = (1u << 4) | (kSym ? 0u : 1u << 16) | (static_cast<uint32_t>(bn >> 3) << 17) | ((256u >> 4) << 24);
+        return bn == 256 ? launch_product<256, !kSym, EPI>(p, out, s) : launch_product<128, !kSym, EPI>(p, out, s);
+    }
+};
+
+bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+puro_status_t check_matrix(const puro_muon_matrix_t &a) {
+    if (a.rows < 0 || a.cols < 0 || a.reserved != 0) return PURO_ERR_INVALID_ARG;
+    if ((a.grad_type != PURO_BF16 && a.grad_type != PURO_F32) || (a.u_type != PURO_BF16 && a.u_type != PURO_F32))
+        return PURO_ERR_INVALID_ARG;
+    if (empty(a)) return PURO_OK;
+    if (!a.grad || !a.u || !aligned(a.grad, a.grad_type == PURO_F32 ? 4 : 2) || !aligned(a.u, a.u_type == PURO_F32 ? 4 : 2) ||
+        !aligned(a.momentum, 4))
+        return PURO_ERR_INVALID_ARG;
+    if (a.grad_stride < 0 || (a.rows > 1 && a.u_stride < a.cols)) return PURO_ERR_INVALID_ARG;
+    if (a.rows > (1 << 20) || a.cols > (1 << 20)) return PURO_ERR_UNSUPPORTED;
+    return PURO_OK;
+}
+
+cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu, int nesterov, const Step *steps, int n_steps,
+                      uint8_t *ws, int32_t *status, cudaStream_t s) {
+    const Scratch at = scratch_of(mats, c);
+    Products run{c, at, ws, status, s, MuonOut{}};
+    // the update, its norm, X
+    MuonIn in{};
+    in.count = c.count;
+    in.mu = static_cast<float>(mu);
+    in.nesterov = nesterov;
+    in.store_lo = n_steps > 1;
+    in.partial = reinterpret_cast<double *>(ws + at.partial);
+    in.scale = reinterpret_cast<float2 *>(ws + at.scale);
+    for (int k = 0; k < c.classes; ++k)
+        for (int i = c.first[k]; i < c.first[k + 1]; ++i) {
+            const puro_muon_matrix_t &a = mats[c.mats[i]];
+            const int64_t z = (i - c.first[k]) * c.shape[k].m * run.ld(k, false);
+            in.grad[i] = a.grad;
+            in.momentum[i] = a.momentum;
+            in.stride[i] = a.rows > 1 ? a.grad_stride : a.cols;
+            in.rows[i] = static_cast<int>(a.rows);
+            in.cols[i] = static_cast<int>(a.cols);
+            in.ldx[i] = static_cast<int>(run.ld(k, false));
+            in.hi[i] = run.x(0, k) + z;
+            in.lo[i] = run.x(1, k) + z;
+            const bool tall = a.rows > a.cols, bf16 = a.grad_type == PURO_BF16, f32 = a.u_type == PURO_F32;
+            const int64_t us = a.rows > 1 ? a.u_stride : a.cols;
+            in.flags[i] = (bf16 ? kGradBf16 : 0) | (tall ? kTall : 0);
+            if (a.cols % 8 == 0 && aligned(a.grad, 16) && in.stride[i] % (bf16 ? 8 : 4) == 0 && aligned(a.momentum, 16))
+                in.flags[i] |= kVectors;
+            run.out.u[i] = a.u;
+            run.out.stride[i] = us;
+            run.out.flags[i] = (tall ? kTall : 0) | (f32 ? kOutF32 : 0);
+            if (a.cols % (f32 ? 4 : 8) == 0 && us % (f32 ? 4 : 8) == 0 && aligned(a.u, 16)) run.out.flags[i] |= kOutVectors;
+            in.tile0[i + 1] = in.tile0[i] + static_cast<int>(tiles_in(a.rows, a.cols));
+        }
+    const dim3 tiles(in.tile0[c.count]);
+    cudaError_t e = launch_pdl(muon_update_kernel, tiles, dim3(kInThreads), 0, s, in);
+    if (e == cudaSuccess) e = launch_pdl(muon_norm_kernel, dim3(c.count), dim3(256), 0, s, in);
+    if (e == cudaSuccess) e = launch_pdl(muon_normalise_kernel, tiles, dim3(kInThreads), 0, s, in);
+    // the steps, two at a time
+    enum { G = 0, B0 = 1, T = 2, B1 = 3 };
+    double most = 1.0, sx = 1 << kX0Exp;
+    int x = 0;  // X's buffers: x, x + 1
+    for (int i = 0; i < n_steps && e == cudaSuccess;) {
+        const bool pair = i + 1 < n_steps;
+        const int taken = pair ? 2 : 1;
+        const Step &s0 = steps[i];
+        const double before = most;
+        const double sg = pow2_for(most * most), sb = pow2_for(s0.most_p);
+        e = run.run<kStore>(-1, -1, G, x, 1, false, sg / (sx * sx), 0, 0, 0);
+        if (e == cudaSuccess) e = run.run<kPoly>(G, G, B0, 0, 1, false, s0.c * sb / (sg * sg), s0.b * sb / sg, s0.a * sb, G);
+        double sp = sb;
+        int product = B0;
+        most = s0.most_out * kMargin;
+        if (pair) {
+            const Step &s1 = steps[i + 1];
+            const double st = pow2_for(before * before * s0.most_p), sg1 = pow2_for(most * most), sb1 = pow2_for(s1.most_p);
+            if (e == cudaSuccess) e = run.run<kStore>(G, B0, T, 0, 1, false, st / (sg * sb), 0, 0, 0);
+            if (e == cudaSuccess) e = run.run<kStore>(T, B0, G, 0, 1, false, sg1 / (st * sb), 0, 0, 0);
+            if (e == cudaSuccess) e = run.run<kPoly>(G, G, B1, 0, 1, false, s1.c * sb1 / (sg1 * sg1), s1.b * sb1 / sg1, s1.a * sb1, G);
+            sp = pow2_for(s0.most_p * s1.most_p);
+            if (e == cudaSuccess) e = run.run<kStore>(B1, B0, T, 0, 1, false, sp / (sb1 * sb), 0, 0, 0);
+            product = T;
+            most = s1.most_out * kMargin;
+        }
+        const int passes = pair ? 2 : 1;  // hi and lo, or hi alone
+        if (i + taken == n_steps) {
+            if (e == cudaSuccess) e = run.run<kOut>(product, -1, -1, x, passes, false, 1.0 / (sp * sx), 0, 0, 0);
+        } else {
+            const double next = pow2_for(most);
+            const bool lo = i + 3 < n_steps;  // a pair follows
+            if (e == cudaSuccess) e = run.run<kNext>(product, -1, -1, x, passes, lo, next / (sp * sx), 0, 0, 0);
+            sx = next;
+            x ^= 2;
+        }
+        i += taken;
+    }
+    return e;
+}
+
+}  // namespace
+}  // namespace puro
+
+using namespace puro;
+
+#define PURO_MUON_API extern "C" __attribute__((visibility("default")))
+
+PURO_MUON_API size_t puro_muon_direction_workspace_size(const puro_muon_matrix_t *mats, int32_t count) {
+    if (!mats || count <= 0) return 0;
+    for (int32_t i = 0; i < count; ++i)
+        if (check_matrix(mats[i]) != PURO_OK) return 0;
+    int64_t most = 0;
+    for (int at = 0; at < count;) {  // the chunks use the scratch one after the other
+        Chunk c;
+        at = take_chunk(mats, at, count, &c);
+        most = std::max(most, scratch_of(mats, c).bytes);
+    }
+    return static_cast<size_t>(most);
+}
+
+PURO_MUON_API puro_status_t puro_muon_direction_grouped(const puro_muon_matrix_t *mats, int32_t count, double momentum,
+                                                        int32_t nesterov, const double *coefficients, int32_t steps,
+                                                        void *workspace, size_t workspace_bytes, int32_t *dev_status,
+                                                        void *stream) {
+    if (count < 0 || (count > 0 && !mats)) return PURO_ERR_INVALID_ARG;
+    if (!(momentum >= 0.0 && momentum <= 1.0)) return PURO_ERR_INVALID_ARG;
+    if (steps < 1 || steps > kMaxSteps || !coefficients || !aligned(dev_status, 4)) return PURO_ERR_INVALID_ARG;
+    Step plan[kMaxSteps];
+    double most = 1.0;
+    for (int i = 0; i < steps; ++i) {
+        if (!plan_step(coefficients + 3 * i, most, &plan[i])) return PURO_ERR_INVALID_ARG;
+        most = plan[i].most_out * kMargin;
+    }
+    bool any = false;
+    for (int32_t i = 0; i < count; ++i) {
+        const puro_status_t st = check_matrix(mats[i]);
+        if (st != PURO_OK) return st;
+        any = any || !empty(mats[i]);
+    }
+    if (!any) return PURO_OK;
+    const size_t need = puro_muon_direction_workspace_size(mats, count);
+    if (!workspace || !aligned(workspace, kAlign) || workspace_bytes < need) return PURO_ERR_INVALID_ARG;
+    for (int at = 0; at < count;) {
+        Chunk c;
+        at = take_chunk(mats, at, count, &c);
+        if (c.count == 0) break;
+        if (run_chunk(mats, c, momentum, nesterov != 0, plan, steps, static_cast<uint8_t *>(workspace), dev_status,
+                      static_cast<cudaStream_t>(stream)) != cudaSuccess)
+            return PURO_ERR_CUDA;
+    }
+    return PURO_OK;
+}
