@@ -11,20 +11,26 @@
 // How it is computed here.  The products run on the tensor cores in FP16 with FP32
 // accumulation (FP16 for its 11 digits: the singular values are at most about one,
 // so that a power of two per step puts every matrix in range).  Two steps at a time,
-// with A0 = X X^T, B0 = a I + b A0 + c A0^2:
-//     A1 = B0 A0 B0 (the next step's A, for B0 and A0 commute),
-//     B1 = a' I + b' A1 + c' A1^2,  X <- (B1 B0) X,
-// where products of m x m take the place of the second step's two of m x n: for n =
-// 6 m a pair costs 24 m^3 products instead of 38.  All m x m results are symmetric, so
-// only tiles on and above the diagonal are computed and each is stored twice.
+// with G = X X^T, B0 = a I + b G + c G^2:
+//     G1 = B0 G B0 (the next step's G, for B0 and G commute),
+//     B1 = a' I + b' G1 + c' G1^2,  X <- (B1 B0) X,
+// so that products of m x m take the place of the second step's two of m x n: for n =
+// 6 m a pair takes 19 of m x m x m for 33 without lo, 38 with it in both steps.  Results
+// that are symmetric (G, B0, G1, B1) are computed on and above the diagonal and
+// stored twice.
 //
 // Where digits are lost.  A rounding of X adds noise of full rank, and the steps
 // blow small singular values up (3.4 times each, by Muon's coefficients), the noise
 // with them; a rounding of B only turns X's rows a little into one another.  So X is
 // kept as two FP16 numbers, x = hi + lo, 22 digits, where a pair of steps follows:
-// B1 B0 multiplies both (lo after hi, into the same accumulator), and A0 takes hi
-// alone.  Of random and of low-rank matrices with noise u is then within 1 to 4
-// 2^-10 of itself (2-norm), against 5 times that without lo, and 30 in BF16.
+// B1 B0 multiplies both (lo after hi, into the same accumulator), and G takes hi
+// alone.  A rounding of G is harmless in B0 but blown up in G1, so behind the first
+// pair G, too, is hi + lo for G1.  And G1 is B0 (B0 G)^T, symmetric whatever B0's
+// roundings: (B0 G) B0 with a mirrored or transposed factor doubles the error, for
+// rounded B0 and G no longer commute.  The model of all roundings in tests/_muon.py
+// gives for momenta of low rank with noise half as large, of 48 x 80 to 1000 x 4000,
+// errors of 1.1 to 1.4 10^-3 of u's 2-norm; without X's lo 3 to 4, without G's up to
+// 2, with BF16 operands 30.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -291,7 +297,7 @@ constexpr int kEpiWarps = 8;
 constexpr int kTmemCols = 512;
 
 enum Epilogue : int {
-    kStore = 0,  // alpha D, symmetric
+    kStore = 0,  // alpha D as hi (and lo), symmetric
     kPoly = 1,   // alpha D + beta G + gamma I, symmetric
     kNext = 2,   // alpha D as hi (and lo)
     kOut = 3,    // alpha D to u
@@ -314,7 +320,7 @@ struct MuonPhase {
     int ldg[kMaxClasses];
     float alpha, beta, gamma;
     int passes;                  // 2: B's lo after its hi
-    bool store_lo;               // kNext
+    bool store_lo;
     uint32_t idesc;
     int32_t *status;
     uint64_t wait_ns;
@@ -656,15 +662,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int k = 0; k < 16; ++k) h[k] = half2_bits(v[2 * k], v[2 * k + 1]);
                     store(&maps.d, h, false, col, row0, w.z);
-                    if constexpr (kSym) {
-                        if (w.mirror) store(&maps.d, h, true, row0, col, w.z);
-                    } else if (p.store_lo) {
+                    if (w.mirror) store(&maps.d, h, true, row0, col, w.z);
+                    if (p.store_lo) {
 #pragma unroll
                         for (int k = 0; k < 16; ++k) {
                             const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h[k]));
                             h[k] = half2_bits(v[2 * k] - f.x, v[2 * k + 1] - f.y);
                         }
                         store(&maps.d_lo, h, false, col, row0, w.z);
+                        if (w.mirror) store(&maps.d_lo, h, true, row0, col, w.z);
                     }
                 }
             }
@@ -743,7 +749,7 @@ constexpr int64_t kAlign = 256;
 struct Scratch {
     int64_t bytes = 0;
     int64_t x[4][kMaxClasses];  // offsets: X hi, lo and the next X's
-    int64_t g[4][kMaxClasses];  // G, B0, T (then B1 B0), B1
+    int64_t g[4][kMaxClasses];  // G, B0, T (then B1 B0), G's lo (then B1)
     int64_t partial = 0, scale = 0;
 };
 int64_t tiles_in(int64_t rows, int64_t cols) {
@@ -860,12 +866,12 @@ struct Products {
     }
 
     // Tiles of 256 x bn, and what the slowest pair has to do, in k-blocks of 256 x 256.
-    double plan(MuonPhase *p, int bn, bool sym, int passes, bool k_is_n) const {
+    double plan(MuonPhase *p, int bn, bool sym, bool square, int passes, bool k_is_n) const {
         p->units = 0;
         double work = 0, longest = 0;
         const double cost = bn == 256 ? 1.0 : 0.55;
         for (int k = 0; k < c.classes; ++k) {
-            const int64_t m = c.shape[k].m, cols = sym ? m : c.shape[k].n;
+            const int64_t m = c.shape[k].m, cols = square ? m : c.shape[k].n;
             const int64_t tm = (m + 255) / 256, tn = (cols + bn - 1) / bn;
             int64_t per = tm * tn;
             if (sym) {
@@ -891,46 +897,62 @@ struct Products {
         return std::max(longest, work / p->units * waves);
     }
 
-    // EPI kStore / kPoly: square D (buffer d) of square A and B (buffers a, b), or with a < 0 of X X^T;
-    // kNext / kOut: the next X (or u) = square A times X.
-    template <int EPI>
-    cudaError_t run(int a, int b, int d, int x0, int passes, bool lo, double alpha, double beta, double gamma, int poly_g) const {
-        constexpr bool kSym = EPI == kStore || EPI == kPoly;
-        const bool gram = a < 0;
+    // D = A B^T (BOTH_SQUARE, or of X alone: the Gram matrix) or A X.  Operands and
+    // results by their buffers: g(0 .. 3), x(0 .. 3); -1: none.
+    struct Product {
+        int a = -1;             // square A; -1: A and B are X's hi
+        int b = -1, b_lo = -1;  // square B, and what is added to it (a second pass over A)
+        int x = 0;              // X: x (hi), x + 1 (lo)
+        bool x_lo = false;      // A X: X's lo as well
+        int d = -1, d_lo = -1;  // square results; -1: the next X, x ^ 2
+        bool next_lo = false;   // of the next X its lo too
+        int poly = -1;          // kPoly: G
+        double alpha = 0, beta = 0, gamma = 0;
+    };
+    template <int EPI, bool X_MAJOR>
+    cudaError_t run(const Product &q) const {
+        constexpr bool kSym = EPI == kStore || EPI == kPoly, kSquare = kSym || !X_MAJOR;
+        const bool gram = q.a < 0;
+        const int passes = (X_MAJOR ? q.x_lo : q.b_lo >= 0) ? 2 : 1;
         MuonPhase wide{}, narrow{};
-        const double tw = plan(&wide, 256, kSym, passes, gram), tn = plan(&narrow, 128, kSym, passes, gram);
+        const double tw = plan(&wide, 256, kSym, kSquare, passes, gram), tn = plan(&narrow, 128, kSym, kSquare, passes, gram);
         const int bn = tw <= tn ? 256 : 128;
         MuonPhase &p = bn == 256 ? wide : narrow;
-        const auto kSw = CU_TENSOR_MAP_SWIZZLE_128B;
+        const auto kSw = CU_TENSOR_MAP_SWIZZLE_128B, kSwD = CU_TENSOR_MAP_SWIZZLE_64B;
         for (int k = 0; k < c.classes; ++k) {
             MuonMaps &m = p.maps[k];
-            bool ok = gram ? map(&m.a, x(x0, k), k, false, 64, 128, kSw) : map(&m.a, g(a, k), k, true, 64, 128, kSw);
-            if (kSym) {
-                ok = ok && (gram ? map(&m.b, x(x0, k), k, false, 64, bn / 2, kSw) : map(&m.b, g(b, k), k, true, 64, bn / 2, kSw));
-                ok = ok && map(&m.d, g(d, k), k, true, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+            bool ok = gram ? map(&m.a, x(q.x, k), k, false, 64, 128, kSw) : map(&m.a, g(q.a, k), k, true, 64, 128, kSw);
+            if (X_MAJOR) {
+                ok = ok && map(&m.b, x(q.x, k), k, false, 64, 64, kSw);
+                if (q.x_lo) ok = ok && map(&m.b_lo, x(q.x + 1, k), k, false, 64, 64, kSw);
             } else {
-                ok = ok && map(&m.b, x(x0, k), k, false, 64, 64, kSw);
-                if (passes > 1) ok = ok && map(&m.b_lo, x(x0 + 1, k), k, false, 64, 64, kSw);
-                if (EPI == kNext) ok = ok && map(&m.d, x(x0 ^ 2, k), k, false, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
-                if (lo) ok = ok && map(&m.d_lo, x((x0 ^ 2) + 1, k), k, false, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+                ok = ok && (gram ? map(&m.b, x(q.x, k), k, false, 64, bn / 2, kSw) : map(&m.b, g(q.b, k), k, true, 64, bn / 2, kSw));
+                if (q.b_lo >= 0) ok = ok && map(&m.b_lo, g(q.b_lo, k), k, true, 64, bn / 2, kSw);
+            }
+            if (kSquare) {
+                ok = ok && map(&m.d, g(q.d, k), k, true, 32, 32, kSwD);
+                if (q.d_lo >= 0) ok = ok && map(&m.d_lo, g(q.d_lo, k), k, true, 32, 32, kSwD);
+            } else if (EPI == kNext) {
+                ok = ok && map(&m.d, x(q.x ^ 2, k), k, false, 32, 32, kSwD);
+                if (q.next_lo) ok = ok && map(&m.d_lo, x((q.x ^ 2) + 1, k), k, false, 32, 32, kSwD);
             }
             if (!ok) return cudaErrorInvalidValue;
             if (EPI == kPoly) {
-                p.g[k] = g(poly_g, k);
+                p.g[k] = g(q.poly, k);
                 p.ldg[k] = static_cast<int>(ld(k, true));
                 p.g_batch[k] = c.shape[k].m * ld(k, true);
             }
         }
-        p.alpha = static_cast<float>(alpha);
-        p.beta = static_cast<float>(beta);
-        p.gamma = static_cast<float>(gamma);
+        p.alpha = static_cast<float>(q.alpha);
+        p.beta = static_cast<float>(q.beta);
+        p.gamma = static_cast<float>(q.gamma);
         p.passes = passes;
-        p.store_lo = lo;
+        p.store_lo = kSquare ? q.d_lo >= 0 : q.next_lo;
         p.status = status;
         p.wait_ns = wait_timeout_ns();
         // kind::f16, FP32 accumulators, FP16 operands; B N-major for X; N, M = 256 (a pair MMA)
-        p.idesc = (1u << 4) | (kSym ? 0u : 1u << 16) | (static_cast<uint32_t>(bn >> 3) << 17) | ((256u >> 4) << 24);
-        return bn == 256 ? launch_product<256, !kSym, EPI>(p, out, s) : launch_product<128, !kSym, EPI>(p, out, s);
+        p.idesc = (1u << 4) | (X_MAJOR ? 1u << 16 : 0u) | (static_cast<uint32_t>(bn >> 3) << 17) | ((256u >> 4) << 24);
+        return bn == 256 ? launch_product<256, X_MAJOR, EPI>(p, out, s) : launch_product<128, X_MAJOR, EPI>(p, out, s);
     }
 };
 
@@ -989,42 +1011,74 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
     if (e == cudaSuccess) e = launch_pdl(muon_norm_kernel, dim3(c.count), dim3(256), 0, s, in);
     if (e == cudaSuccess) e = launch_pdl(muon_normalise_kernel, tiles, dim3(kInThreads), 0, s, in);
     // the steps, two at a time
-    enum { G = 0, B0 = 1, T = 2, B1 = 3 };
+    using Product = Products::Product;
+    enum { G = 0, B0 = 1, T = 2, B1 = 3, Glo = B1 };  // (G's lo is read before B1 is written)
     double most = 1.0, sx = 1 << kX0Exp;
+    Product q;
+    auto scaled = [&](double alpha, double beta = 0, double gamma = 0) {
+        q.alpha = alpha;
+        q.beta = beta;
+        q.gamma = gamma;
+        return q;
+    };
     int x = 0;  // X's buffers: x, x + 1
     for (int i = 0; i < n_steps && e == cudaSuccess;) {
-        const bool pair = i + 1 < n_steps;
-        const int taken = pair ? 2 : 1;
+        const bool pair = i + 1 < n_steps, glo = pair && i > 0;
         const Step &s0 = steps[i];
-        const double before = most;
         const double sg = pow2_for(most * most), sb = pow2_for(s0.most_p);
-        e = run.run<kStore>(-1, -1, G, x, 1, false, sg / (sx * sx), 0, 0, 0);
-        if (e == cudaSuccess) e = run.run<kPoly>(G, G, B0, 0, 1, false, s0.c * sb / (sg * sg), s0.b * sb / sg, s0.a * sb, G);
-        double sp = sb;
+        q = Product{};  // G = X X^T
+        q.x = x;
+        q.d = G;
+        q.d_lo = glo ? Glo : -1;
+        e = run.run<kStore, false>(scaled(sg / (sx * sx)));
+        q = Product{};  // B0 = a I + b G + c G^2
+        q.a = q.b = q.poly = G;
+        q.d = B0;
+        if (e == cudaSuccess) e = run.run<kPoly, false>(scaled(s0.c * sb / (sg * sg), s0.b * sb / sg, s0.a * sb));
+        double sp = sb, out = s0.most_out * kMargin;
         int product = B0;
-        most = s0.most_out * kMargin;
         if (pair) {
             const Step &s1 = steps[i + 1];
-            const double st = pow2_for(before * before * s0.most_p), sg1 = pow2_for(most * most), sb1 = pow2_for(s1.most_p);
-            if (e == cudaSuccess) e = run.run<kStore>(G, B0, T, 0, 1, false, st / (sg * sb), 0, 0, 0);
-            if (e == cudaSuccess) e = run.run<kStore>(T, B0, G, 0, 1, false, sg1 / (st * sb), 0, 0, 0);
-            if (e == cudaSuccess) e = run.run<kPoly>(G, G, B1, 0, 1, false, s1.c * sb1 / (sg1 * sg1), s1.b * sb1 / sg1, s1.a * sb1, G);
+            const double st = pow2_for(most * most * s0.most_p), sg1 = pow2_for(out * out), sb1 = pow2_for(s1.most_p);
+            q = Product{};  // T^T = B0 G
+            q.a = B0;
+            q.b = G;
+            q.b_lo = glo ? Glo : -1;
+            q.d = T;
+            if (e == cudaSuccess) e = run.run<kNext, false>(scaled(st / (sg * sb)));
+            q = Product{};  // G = B0 T
+            q.a = B0;
+            q.b = T;
+            q.d = G;
+            if (e == cudaSuccess) e = run.run<kStore, false>(scaled(sg1 / (st * sb)));
+            q = Product{};  // B1
+            q.a = q.b = q.poly = G;
+            q.d = B1;
+            if (e == cudaSuccess) e = run.run<kPoly, false>(scaled(s1.c * sb1 / (sg1 * sg1), s1.b * sb1 / sg1, s1.a * sb1));
             sp = pow2_for(s0.most_p * s1.most_p);
-            if (e == cudaSuccess) e = run.run<kStore>(B1, B0, T, 0, 1, false, sp / (sb1 * sb), 0, 0, 0);
+            q = Product{};  // B1 B0
+            q.a = B1;
+            q.b = B0;
+            q.d = T;
+            if (e == cudaSuccess) e = run.run<kNext, false>(scaled(sp / (sb1 * sb)));
             product = T;
-            most = s1.most_out * kMargin;
+            out = s1.most_out * kMargin;
         }
-        const int passes = pair ? 2 : 1;  // hi and lo, or hi alone
-        if (i + taken == n_steps) {
-            if (e == cudaSuccess) e = run.run<kOut>(product, -1, -1, x, passes, false, 1.0 / (sp * sx), 0, 0, 0);
+        i += pair ? 2 : 1;
+        q = Product{};
+        q.a = product;
+        q.x = x;
+        q.x_lo = pair;
+        if (i == n_steps) {
+            if (e == cudaSuccess) e = run.run<kOut, true>(scaled(1.0 / (sp * sx)));
         } else {
-            const double next = pow2_for(most);
-            const bool lo = i + 3 < n_steps;  // a pair follows
-            if (e == cudaSuccess) e = run.run<kNext>(product, -1, -1, x, passes, lo, next / (sp * sx), 0, 0, 0);
+            const double next = pow2_for(out);
+            q.next_lo = i + 1 < n_steps;  // a pair follows
+            if (e == cudaSuccess) e = run.run<kNext, true>(scaled(next / (sp * sx)));
             sx = next;
             x ^= 2;
         }
-        i += taken;
+        most = out;
     }
     return e;
 }

@@ -67,8 +67,10 @@ def model(v, steps=STEPS):
         if pair:
             a, b, c = steps[i + 1]
             mp1, out1 = bounds(steps[i + 1], out)
-            t = _half(g @ b0, _scale(most ** 2 * mp))
-            g = _half(t @ b0, _scale(out ** 2))
+            g_lo = _half(hi @ hi.T - g, _scale(most ** 2)) if i else 0 * g
+            t = _half(b0 @ (g + g_lo), _scale(most ** 2 * mp))
+            g = _half(b0 @ t.T, _scale(out ** 2))
+            g = torch.triu(g) + torch.triu(g, 1).T
             b1 = _half(a * eye + b * g + c * (g @ g), _scale(mp1))
             b0, out = _half(b1 @ b0, _scale(mp * mp1)), out1
         x = b0 @ hi + b0 @ lo
