@@ -36,7 +36,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <mutex>
 
 #include "internal.h"
 #include "ptx.cuh"
@@ -52,18 +51,21 @@ constexpr uint64_t kDrainNs = 2000000000ull, kSettleNs = 200000ull;
 
 // ------------------------------------------------ the update and its norm
 constexpr int kInRows = 64, kInCols = 128, kInThreads = 256;  // tile of the two passes over V
-constexpr int kInPasses = kInRows * kInCols / 8 / kInThreads;
+constexpr int kInWarps = kInThreads / 32, kInPasses = 4;  // a warp a row, four rows of a warp at a time
+constexpr int kMaxSlabs = kInThreads;
 
 enum MatFlags : uint8_t {
     kGradBf16 = 1,
     kTall = 2,      // more rows than columns: X is its transpose
-    kVectors = 4,   // eight columns of a row are 16- or 32-byte aligned in grad and momentum
+    kVectors = 4,   // four columns of a row can be read at once in grad and momentum
     kOutF32 = 8,
     kOutVectors = 16,  // eight columns of a row of u can be stored in 16-byte pieces
 };
 struct MuonIn {
     int count;
     int tile0[kMaxMats + 1];  // first tile of each matrix
+    int slab0[kMaxMats + 1];  // first slab: a run of slab_tiles tiles whose sum of V^2 one block takes
+    int slab_tiles[kMaxMats];
     const void *grad[kMaxMats];
     float *momentum[kMaxMats];
     int64_t stride[kMaxMats];
@@ -73,8 +75,7 @@ struct MuonIn {
     float mu;
     int nesterov;
     bool store_lo;
-    double *partial;  // [tiles]: sum of V^2 over each tile
-    float2 *scale;    // [count]: X = (V * x) * y
+    double *partial;  // [slabs]: sum of V^2 over each
 };
 
 PURO_DEV int mat_of(const int *start, int count, int t) {
@@ -86,173 +87,218 @@ PURO_DEV int mat_of(const int *start, int count, int t) {
     return lo;
 }
 
-// Eight values of V at (r, c0 ...), zero outside the matrix.  UPDATE: the momentum
-// takes the gradient first and is stored; else it has.
-template <bool UPDATE>
-PURO_DEV void update8(const MuonIn &p, int m, int r, int c0, float (&v)[8]) {
-    const int cols = p.cols[m];
+// A lane's four columns of a tile's row: neighbours where grad and momentum can be
+// read in vectors, else 32 apart, so that a warp's accesses are dense either way.
+PURO_DEV int in_col(uint8_t flags, int lane, int k) { return flags & kVectors ? 4 * lane + k : lane + 32 * k; }
+
+// The values of V of a lane's columns c0 ... in rows r0 + warp, r0 + warp + kInWarps, ...,
+// zero outside the matrix.  UPDATE: the momentum takes the gradient first and is
+// stored; else it has.  All loads are issued ahead of the first use (with each row's
+// behind the row before's stores a layer's update took 114 us instead of XX).
+template <bool UPDATE, bool VEC, bool BF16>
+PURO_DEV void tile_of(const MuonIn &p, int m, int r0, int c0, float (&v)[kInPasses][4]) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rows = p.rows[m], cols = p.cols[m];
+    float *const mom = p.momentum[m];
+    const bool read_g = UPDATE || !mom || p.nesterov;
+    const int64_t stride = p.stride[m];
+    float w[kInPasses][4];
+    auto in = [&](int i, int k) { return r0 + warp + kInWarps * i < rows && c0 + (VEC ? 4 * lane : lane + 32 * k) < cols; };
+    auto at = [&](int i, int k, int64_t pitch) { return (r0 + warp + kInWarps * i) * pitch + c0 + (VEC ? 4 * lane : lane + 32 * k); };
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = 0.0f;
-    if (r >= p.rows[m] || c0 >= cols) return;
-    const uint8_t f = p.flags[m];
-    float *mom = p.momentum[m] ? p.momentum[m] + static_cast<int64_t>(r) * cols + c0 : nullptr;
-    const int64_t at = r * p.stride[m] + c0;
-    float w[8];
-    if (f & kVectors) {
-        if (f & kGradBf16) {
-            const uint4 x = __ldg(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.grad[m]) + at));
-            const uint32_t s[4] = {x.x, x.y, x.z, x.w};
+    for (int i = 0; i < kInPasses; ++i) {
+        if constexpr (VEC) {
+            uint4 x = make_uint4(0u, 0u, 0u, 0u);
+            float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (in(i, 0)) {
+                if (read_g) {
+                    if constexpr (BF16) {
+                        const uint2 z = __ldg(reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p.grad[m]) + at(i, 0, stride)));
+                        x.x = z.x;
+                        x.y = z.y;
+                    } else {
+                        x = __ldg(reinterpret_cast<const uint4 *>(static_cast<const float *>(p.grad[m]) + at(i, 0, stride)));
+                    }
+                }
+                if (mom) y = *reinterpret_cast<const float4 *>(mom + at(i, 0, cols));
+            }
+            v[i][0] = __uint_as_float(BF16 ? x.x << 16 : x.x);
+            v[i][1] = __uint_as_float(BF16 ? x.x & 0xFFFF0000u : x.y);
+            v[i][2] = __uint_as_float(BF16 ? x.y << 16 : x.z);
+            v[i][3] = __uint_as_float(BF16 ? x.y & 0xFFFF0000u : x.w);
+            w[i][0] = y.x;
+            w[i][1] = y.y;
+            w[i][2] = y.z;
+            w[i][3] = y.w;
+        } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                v[2 * k] = __uint_as_float(s[k] << 16);
-                v[2 * k + 1] = __uint_as_float(s[k] & 0xFFFF0000u);
+                v[i][k] = w[i][k] = 0.0f;
+                if (!in(i, k)) continue;
+                if (read_g)
+                    v[i][k] = BF16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t *>(p.grad[m])[at(i, k, stride)]) << 16)
+                                   : static_cast<const float *>(p.grad[m])[at(i, k, stride)];
+                if (mom) w[i][k] = mom[at(i, k, cols)];
             }
-        } else {
-            const float4 *g = reinterpret_cast<const float4 *>(static_cast<const float *>(p.grad[m]) + at);
-            *reinterpret_cast<float4 *>(&v[0]) = __ldg(g);
-            *reinterpret_cast<float4 *>(&v[4]) = __ldg(g + 1);
         }
-        if (!mom) return;
-        *reinterpret_cast<float4 *>(&w[0]) = *reinterpret_cast<const float4 *>(mom);
-        *reinterpret_cast<float4 *>(&w[4]) = *reinterpret_cast<const float4 *>(mom + 4);
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            w[k] = 0.0f;
-            if (c0 + k >= cols) continue;
-            v[k] = f & kGradBf16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t *>(p.grad[m])[at + k]) << 16)
-                                 : static_cast<const float *>(p.grad[m])[at + k];
-            if (mom) w[k] = mom[k];
-        }
-        if (!mom) return;
     }
+    if (!mom) return;
     if constexpr (UPDATE) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = fmaf(p.mu, w[k], v[k]);
-        if (f & kVectors) {
-            *reinterpret_cast<float4 *>(mom) = *reinterpret_cast<const float4 *>(&w[0]);
-            *reinterpret_cast<float4 *>(mom + 4) = *reinterpret_cast<const float4 *>(&w[4]);
-        } else {
+        for (int i = 0; i < kInPasses; ++i) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (c0 + k < cols) mom[k] = w[k];
+            for (int k = 0; k < 4; ++k) w[i][k] = fmaf(p.mu, w[i][k], v[i][k]);
+            if constexpr (VEC) {
+                if (in(i, 0)) *reinterpret_cast<float4 *>(mom + at(i, 0, cols)) = make_float4(w[i][0], w[i][1], w[i][2], w[i][3]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (in(i, k)) mom[at(i, k, cols)] = w[i][k];
+            }
         }
     }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = p.nesterov ? fmaf(p.mu, w[k], v[k]) : w[k];
-}
-
-struct InTile {
-    int m, r0, c0;
-};
-PURO_DEV InTile in_tile(const MuonIn &p) {
-    InTile t;
-    t.m = mat_of(p.tile0, p.count, blockIdx.x);
-    const int i = static_cast<int>(blockIdx.x) - p.tile0[t.m], across = (p.cols[t.m] + kInCols - 1) / kInCols;
-    t.r0 = i / across * kInRows;
-    t.c0 = i % across * kInCols;
-    return t;
-}
-
-// The momentum takes the gradient; each tile's sum of V^2.  A thread's 32 squares
-// are summed in FP32, in FP64 where that left its range (or all are zero), the
-// threads' sums in FP64 in a fixed order.  Bound by memory.
-__global__ void __launch_bounds__(kInThreads) muon_update_kernel(const __grid_constant__ MuonIn p) {
-    pdl_wait();
-    pdl_launch_dependents();
-    const InTile t = in_tile(p);
-    const int r = t.r0 + threadIdx.x / 16, c = t.c0 + threadIdx.x % 16 * 8;
-    float v[kInPasses][8], s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kInPasses; ++i) update8<true>(p, t.m, r + 16 * i, c, v[i]);
 #pragma unroll
     for (int i = 0; i < kInPasses; ++i)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) s = fmaf(v[i][k], v[i][k], s);
-    double d = s;
-    if (!(s > 1e-24f && s < 1e36f)) {
-        d = 0.0;
-#pragma unroll
-        for (int i = 0; i < kInPasses; ++i)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) d += static_cast<double>(v[i][k]) * v[i][k];
+        for (int k = 0; k < 4; ++k) v[i][k] = p.nesterov ? fmaf(p.mu, w[i][k], v[i][k]) : w[i][k];
+}
+template <bool UPDATE>
+PURO_DEV void read_tile(const MuonIn &p, int m, int r0, int c0, float (&v)[kInPasses][4]) {
+    const uint8_t f = p.flags[m];
+    if (f & kVectors) {
+        if (f & kGradBf16)
+            tile_of<UPDATE, true, true>(p, m, r0, c0, v);
+        else
+            tile_of<UPDATE, true, false>(p, m, r0, c0, v);
+    } else {
+        if (f & kGradBf16)
+            tile_of<UPDATE, false, true>(p, m, r0, c0, v);
+        else
+            tile_of<UPDATE, false, false>(p, m, r0, c0, v);
     }
+}
+
+struct InTile {
+    int r0, c0;
+};
+PURO_DEV InTile in_tile(int i, int cols) {
+    const int across = (cols + kInCols - 1) / kInCols;
+    return {i / across * kInRows, i % across * kInCols};
+}
+
+PURO_DEV double warp_sum(double d) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xFFFFFFFFu, d, o);
-    __shared__ double part[kInThreads / 32];
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x / 32] = d;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        double sum = 0.0;
+    return d;
+}
+
+// The momentum takes the gradient; each slab's sum of V^2.  A thread's 16 squares of
+// half a tile are summed in FP32, in FP64 where that left its range (or all are zero), the
+// rest in FP64 in a fixed order.  Bound by memory.
+__global__ void __launch_bounds__(kInThreads, 4) muon_update_kernel(const __grid_constant__ MuonIn p) {
+    __shared__ double part[kInWarps];
+    pdl_wait();
+    pdl_launch_dependents();
+    const int m = mat_of(p.slab0, p.count, blockIdx.x), tiles = p.tile0[m + 1] - p.tile0[m];
+    const int first = (static_cast<int>(blockIdx.x) - p.slab0[m]) * p.slab_tiles[m];
+    double sum = 0.0;
+    constexpr int kParts = kInRows / (kInWarps * kInPasses);
+    for (int i = kParts * first; i < kParts * min(tiles, first + p.slab_tiles[m]); ++i) {
+        const InTile t = in_tile(i / kParts, p.cols[m]);
+        float v[kInPasses][4], s = 0.0f;
+        read_tile<true>(p, m, t.r0 + i % kParts * kInWarps * kInPasses, t.c0, v);
 #pragma unroll
-        for (int w = 0; w < kInThreads / 32; ++w) sum += part[w];
-        p.partial[blockIdx.x] = sum;
+        for (int j = 0; j < kInPasses; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s = fmaf(v[j][k], v[j][k], s);
+        if (s > 1e-24f && s < 1e36f) {
+            sum += s;
+        } else {
+#pragma unroll
+            for (int j = 0; j < kInPasses; ++j)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum += static_cast<double>(v[j][k]) * v[j][k];
+        }
     }
+    sum = warp_sum(sum);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < kInWarps; ++w) sum += part[w];
+    p.partial[blockIdx.x] = sum;
 }
 
 // X's power of two: entries are at most 1.
 constexpr int kX0Exp = 14;
 
-// Each matrix's factor 2^14 / ||V||_F in two parts, neither of which leaves FP32's
-// range; NaN where the norm is not finite (all of u is then NaN), 0 for V = 0.
-__global__ void __launch_bounds__(256) muon_norm_kernel(const __grid_constant__ MuonIn p) {
-    pdl_wait();
-    pdl_launch_dependents();
-    const int m = blockIdx.x;
-    double d = 0.0;
-    for (int i = p.tile0[m] + threadIdx.x; i < p.tile0[m + 1]; i += 256) d += p.partial[i];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xFFFFFFFFu, d, o);
-    __shared__ double part[8];
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x / 32] = d;
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    double sum = 0.0;
-    for (int w = 0; w < 8; ++w) sum += part[w];
-    float2 f = make_float2(0.0f, 0.0f);
-    if (!(sum < INFINITY)) {
-        f.x = f.y = NAN;
-    } else if (sum > 0.0) {
-        const double scale = static_cast<double>(1 << kX0Exp) / sqrt(sum);
-        const int e = ilogb(scale) / 2;
-        f = make_float2(static_cast<float>(ldexp(1.0, e)), static_cast<float>(ldexp(scale, -e)));
-    }
-    p.scale[m] = f;
-}
-
-// X = V / ||V||_F as FP16 pairs, a tall matrix transposed.
-__global__ void __launch_bounds__(kInThreads) muon_normalise_kernel(const __grid_constant__ MuonIn p) {
+// X = V / ||V||_F as FP16 pairs, a tall matrix transposed.  Each block adds up its
+// matrix's sums (at most kMaxSlabs) for the factor 2^14 / ||V||_F,
+// taken in two parts, neither of which leaves FP32's range; NaN where the norm is not
+// finite (all of u is then NaN), 0 for V = 0.
+__global__ void __launch_bounds__(kInThreads, 4) muon_normalise_kernel(const __grid_constant__ MuonIn p) {
     __shared__ uint32_t turn[kInCols][kInRows + 1];  // (hi, lo) of the transposed tile
+    __shared__ float2 factor;
     pdl_wait();
     pdl_launch_dependents();
-    const InTile t = in_tile(p);
-    const float2 f = p.scale[t.m];
-    const bool tall = p.flags[t.m] & kTall;
-    const int lr = threadIdx.x / 16, lc = threadIdx.x % 16 * 8, ldx = p.ldx[t.m];
-    float v[kInPasses][8];
-#pragma unroll
-    for (int i = 0; i < kInPasses; ++i) update8<false>(p, t.m, t.r0 + lr + 16 * i, t.c0 + lc, v[i]);
-#pragma unroll
-    for (int i = 0; i < kInPasses; ++i) {
-        uint16_t hi[8], lo[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float x = (v[i][k] * f.x) * f.y;
-            const __half h = __float2half_rn(x);
-            hi[k] = __half_as_ushort(h);
-            lo[k] = __half_as_ushort(__float2half_rn(x - __half2float(h)));
+    const int m = mat_of(p.tile0, p.count, blockIdx.x);
+    const InTile t = in_tile(static_cast<int>(blockIdx.x) - p.tile0[m], p.cols[m]);
+    const uint8_t flags = p.flags[m];
+    const bool tall = flags & kTall;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ldx = p.ldx[m];
+    float v[kInPasses][4];
+    read_tile<false>(p, m, t.r0, t.c0, v);
+    if (warp == 0) {  // (one warp: FP64 is slow)
+        double sum = 0.0;
+        for (int i = p.slab0[m] + lane; i < p.slab0[m + 1]; i += 32) sum += p.partial[i];
+        sum = warp_sum(sum);
+        if (lane == 0) {
+            float2 f = make_float2(0.0f, 0.0f);
+            if (!(sum < INFINITY)) {
+                f.x = f.y = NAN;
+            } else if (sum > 0.0) {
+                const double scale = static_cast<double>(1 << kX0Exp) / sqrt(sum);
+                const int e = ilogb(scale) / 2;
+                f = make_float2(static_cast<float>(ldexp(1.0, e)), static_cast<float>(ldexp(scale, -e)));
+            }
+            factor = f;
         }
-        const int r = t.r0 + lr + 16 * i, c = t.c0 + lc;
-        if (tall) {
+    }
+    __syncthreads();
+    const float2 f = factor;
+#pragma unroll 1
+    for (int half = 0; half < kInRows; half += kInWarps * kInPasses) {
+        if (half > 0) read_tile<false>(p, m, t.r0 + half, t.c0, v);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) turn[lc + k][lr + 16 * i] = hi[k] | static_cast<uint32_t>(lo[k]) << 16;
-        } else if (r < p.rows[t.m] && c < ldx) {
-            const int64_t at = static_cast<int64_t>(r) * ldx + c;
-            auto pack = [](const uint16_t *h) {
-                return make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
-            };
-            *reinterpret_cast<uint4 *>(p.hi[t.m] + at) = pack(hi);
-            if (p.store_lo) *reinterpret_cast<uint4 *>(p.lo[t.m] + at) = pack(lo);
+        for (int i = 0; i < kInPasses; ++i) {
+            const int lr = half + warp + kInWarps * i, r = t.r0 + lr;
+            uint32_t x[4];  // hi, lo
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float y = (v[i][k] * f.x) * f.y;
+                const __half h = __float2half_rn(y), l = __float2half_rn(y - __half2float(h));
+                x[k] = __half_as_ushort(h) | static_cast<uint32_t>(__half_as_ushort(l)) << 16;
+            }
+            if (tall) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) turn[in_col(flags, lane, k)][lr] = x[k];
+            } else if (r < p.rows[m]) {
+                const int64_t at = static_cast<int64_t>(r) * ldx + t.c0;
+                if (flags & kVectors) {
+                    if (t.c0 + 4 * lane >= ldx) continue;
+                    *reinterpret_cast<uint2 *>(p.hi[m] + at + 4 * lane) = make_uint2(__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[2], x[3], 0x5410));
+                    if (p.store_lo)
+                        *reinterpret_cast<uint2 *>(p.lo[m] + at + 4 * lane) = make_uint2(__byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632));
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int c = lane + 32 * k;
+                        if (t.c0 + c >= ldx) continue;
+                        p.hi[m][at + c] = static_cast<uint16_t>(x[k]);
+                        if (p.store_lo) p.lo[m][at + c] = static_cast<uint16_t>(x[k] >> 16);
+                    }
+                }
+            }
         }
     }
     if (!tall) return;
@@ -262,7 +308,7 @@ __global__ void __launch_bounds__(kInThreads) muon_normalise_kernel(const __grid
 #pragma unroll
     for (int i = 0; i < kInCols / 32; ++i) {
         const int c = threadIdx.x / 8 + 32 * i;
-        if (t.c0 + c >= p.cols[t.m] || t.r0 + r8 >= ldx) continue;
+        if (t.c0 + c >= p.cols[m] || t.r0 + r8 >= ldx) continue;
         uint32_t x[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[k] = turn[c][r8 + k];
@@ -273,8 +319,8 @@ __global__ void __launch_bounds__(kInThreads) muon_normalise_kernel(const __grid
             h[k] = __byte_perm(x[2 * k], x[2 * k + 1], 0x5410);
             l[k] = __byte_perm(x[2 * k], x[2 * k + 1], 0x7632);
         }
-        *reinterpret_cast<uint4 *>(p.hi[t.m] + at) = make_uint4(h[0], h[1], h[2], h[3]);
-        if (p.store_lo) *reinterpret_cast<uint4 *>(p.lo[t.m] + at) = make_uint4(l[0], l[1], l[2], l[3]);
+        *reinterpret_cast<uint4 *>(p.hi[m] + at) = make_uint4(h[0], h[1], h[2], h[3]);
+        if (p.store_lo) *reinterpret_cast<uint4 *>(p.lo[m] + at) = make_uint4(l[0], l[1], l[2], l[3]);
     }
 }
 
@@ -295,6 +341,7 @@ constexpr int kBM = 128, kBK = 64;
 constexpr int kThreads = 384;
 constexpr int kEpiWarps = 8;
 constexpr int kTmemCols = 512;
+constexpr int kMaxSegments = 16;
 
 enum Epilogue : int {
     kStore = 0,  // alpha D as hi (and lo), symmetric
@@ -311,6 +358,9 @@ struct MuonPhase {
     int classes, units;
     int unit0[kMaxClasses + 1];  // first tile of each class
     int per[kMaxClasses];        // tiles of a matrix
+    int segments;                // of tiles, each dealt to a range of the pairs in turn
+    int from[kMaxSegments], to[kMaxSegments];
+    int16_t pair0[kMaxSegments], pairs[kMaxSegments];
     int tiles_n[kMaxClasses], tiles_m[kMaxClasses];
     int rows[kMaxClasses], cols[kMaxClasses];  // of D
     int kb[kMaxClasses];         // k-blocks of B (of lo as many more)
@@ -344,6 +394,23 @@ struct ProductSmem {
     volatile int abort_flag;
 };
 
+// A pair's units, in order.
+struct Walk {
+    int segment = 0, u = -1;
+    PURO_DEV int next(const MuonPhase &p, int pair) {
+        for (; segment < p.segments; ++segment, u = -1) {
+            if (u < 0) {
+                const int i = pair - p.pair0[segment];
+                if (i < 0 || i >= p.pairs[segment]) continue;
+                u = p.from[segment] + i;
+            } else {
+                u += p.pairs[segment];
+            }
+            if (u < p.to[segment]) return u;
+        }
+        return -1;
+    }
+};
 struct Unit {
     int cls, z, m0, n0, kb;
     bool mirror;  // off the diagonal of a symmetric D: stored transposed as well
@@ -460,7 +527,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     const int warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0);
     const int lane = threadIdx.x & 31;
     const int rank = __shfl_sync(0xFFFFFFFFu, static_cast<int>(cluster_ctarank()), 0);
-    const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+    const int pair = blockIdx.x / 2;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
@@ -495,7 +562,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const uint32_t full0 = mapa_shared(smem_u32(&sm.full[0]), 0);
         uint32_t stage = 0, phase = 0, issued = 0;
         bool ok = true;
-        for (int u = pair; u < p.units && ok; u += pairs) {
+        Walk walk;
+        for (int u = walk.next(p, pair); u >= 0 && ok; u = walk.next(p, pair)) {
             const Unit w = unit_of<BN, kSym>(p, u);
             const MuonMaps &maps = p.maps[w.cls];
             const int a_row = w.m0 + kBM * rank, b_row = w.n0 + BN / 2 * rank;
@@ -539,7 +607,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         uint32_t stage = 0, phase = 0;
         int local = 0;
         bool ok = true;
-        for (int u = pair; u < p.units && ok; u += pairs, ++local) {
+        Walk walk;
+        for (int u = walk.next(p, pair); u >= 0 && ok; u = walk.next(p, pair), ++local) {
             const Unit w = unit_of<BN, kSym>(p, u);
             const int buf = local & 1;
             ok = wait_or_abort(sm, &sm.tempty[buf], ((local >> 1) & 1u) ^ 1u, p.wait_ns, p.status, lane);
@@ -590,13 +659,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             ++pieces;
         };
         int local = 0;
-        for (int u = pair; u < p.units; u += pairs, ++local) {
+        Walk walk;
+        for (int u = walk.next(p, pair); u >= 0; u = walk.next(p, pair), ++local) {
             const Unit w = unit_of<BN, kSym>(p, u);
             const int buf = local & 1;
-            if (!wait_or_abort(sm, &sm.tfull[buf], (local >> 1) & 1u, p.wait_ns, p.status, lane)) break;
-            tc_fence_after_sync();
             const MuonMaps &maps = p.maps[w.cls];
             const int row0 = w.m0 + kBM * rank + 32 * q, rows = p.rows[w.cls], cols = p.cols[w.cls];
+            uint4 g[4];
+            auto load_g = [&](int col) {  // the lane's row of G (kPoly), ahead of its use
+                const int row = row0 + lane, ldg = p.ldg[w.cls];
+                const uint4 *from = reinterpret_cast<const uint4 *>(p.g[w.cls] + w.z * p.g_batch[w.cls] + static_cast<int64_t>(row) * ldg + col);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    g[k] = make_uint4(0u, 0u, 0u, 0u);
+                    if (row < rows && col + 8 * k < ldg) g[k] = __ldg(from + k);
+                }
+            };
+            if constexpr (EPI == kPoly) load_g(w.n0 + BN / 2 * half);
+            if (!wait_or_abort(sm, &sm.tfull[buf], (local >> 1) & 1u, p.wait_ns, p.status, lane)) break;
+            tc_fence_after_sync();
             const uint32_t acc = tmem + (static_cast<uint32_t>(32 * q) << 16) + 256u * buf + BN / 2 * half;
 #pragma unroll 1
             for (int i = 0; i < BN / 64; ++i) {
@@ -614,13 +695,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int k = 0; k < 32; ++k) v[k] = p.alpha * __uint_as_float(r[k]);
                 if constexpr (EPI == kPoly) {
-                    const int row = row0 + lane;
-                    const uint16_t *g = p.g[w.cls] + w.z * p.g_batch[w.cls] + static_cast<int64_t>(row) * p.ldg[w.cls] + col;
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                        if (row < rows && col + 8 * k < p.ldg[w.cls]) x = __ldg(reinterpret_cast<const uint4 *>(g) + k);
-                        const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+                        const uint32_t xs[4] = {g[k].x, g[k].y, g[k].z, g[k].w};
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&xs[j]));
@@ -628,6 +705,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                             v[8 * k + 2 * j + 1] = fmaf(p.beta, f.y, v[8 * k + 2 * j + 1]);
                         }
                     }
+                    if (i + 1 < BN / 64) load_g(col + 32);
                     if (col <= row0 + 31 && row0 <= col + 31) {
 #pragma unroll
                         for (int k = 0; k < 32; ++k)
@@ -697,6 +775,12 @@ struct Shape {
 Shape shape_of(const puro_muon_matrix_t &a) { return {std::min(a.rows, a.cols), std::max(a.rows, a.cols)}; }
 bool empty(const puro_muon_matrix_t &a) { return a.rows == 0 || a.cols == 0; }
 
+template <class Less>
+void sort_few(int *v, int n, Less less) {
+    for (int i = 1; i < n; ++i)
+        for (int j = i; j > 0 && less(v[j], v[j - 1]); --j) std::swap(v[j], v[j - 1]);
+}
+
 // The matrices of one series of launches: some in a row of the table, by shape.
 struct Chunk {
     int count = 0, classes = 0;
@@ -723,7 +807,7 @@ int take_chunk(const puro_muon_matrix_t *mats, int at, int count, Chunk *c) {
     // classes of the longest rows first: their tiles are the long ones
     int order[kMaxClasses], place[kMaxClasses];
     for (int k = 0; k < c->classes; ++k) order[k] = k;
-    std::sort(order, order + c->classes, [&](int a, int b) {
+    sort_few(order, c->classes, [&](int a, int b) {
         return c->shape[a].n != c->shape[b].n ? c->shape[a].n > c->shape[b].n
                                               : c->shape[a].m != c->shape[b].m ? c->shape[a].m > c->shape[b].m : a < b;
     });
@@ -748,9 +832,9 @@ constexpr int64_t kAlign = 256;
 // Scratch of a chunk.
 struct Scratch {
     int64_t bytes = 0;
-    int64_t x[4][kMaxClasses];  // offsets: X hi, lo and the next X's
+    int64_t x[3][kMaxClasses];  // offsets: X, the first X's lo, the next X
     int64_t g[4][kMaxClasses];  // G, B0, T (then B1 B0), G's lo (then B1)
-    int64_t partial = 0, scale = 0;
+    int64_t partial = 0;
 };
 int64_t tiles_in(int64_t rows, int64_t cols) {
     return (rows + kInRows - 1) / kInRows * ((cols + kInCols - 1) / kInCols);
@@ -762,13 +846,10 @@ Scratch scratch_of(const puro_muon_matrix_t *mats, const Chunk &c) {
         s.bytes += align_up(bytes, kAlign);
         return at;
     };
-    int64_t tiles = 0;
-    for (int i = 0; i < c.count; ++i) tiles += tiles_in(mats[c.mats[i]].rows, mats[c.mats[i]].cols);
-    s.partial = take(tiles * 8);
-    s.scale = take(c.count * 8);
+    s.partial = take(8 * c.count * kMaxSlabs);
     for (int k = 0; k < c.classes; ++k) {
         const int64_t n = c.first[k + 1] - c.first[k];
-        for (int b = 0; b < 4; ++b) s.x[b][k] = take(n * c.shape[k].m * align_up(c.shape[k].n, 8) * 2);
+        for (int b = 0; b < 3; ++b) s.x[b][k] = take(n * c.shape[k].m * align_up(c.shape[k].n, 8) * 2);
         for (int b = 0; b < 4; ++b) s.g[b][k] = take(n * c.shape[k].m * align_up(c.shape[k].m, 8) * 2);
     }
     return s;
@@ -806,16 +887,103 @@ bool plan_step(const double *abc, double most, Step *s) {
     }
     return s->most_p < 1024 && s->most_out < 1024;
 }
+// What a k-block of a 256 x 128 tile takes next to one of 256 x 256, and a tile's
+// epilogue that no product hides, in k-blocks.
+constexpr double kNarrowBlock = 0.65, kTileBlocks = 4.0;
 constexpr double kMargin = 1.0 + 1.0 / 64;  // of a bound, for what roundings add
 // The power of two that puts values up to `most` within FP16, with half of it to spare.
 double pow2_for(double most) { return std::ldexp(1.0, most > 0 ? std::min(14, std::ilogb(32768.0 / (most * kMargin))) : 14); }
 
-template <class Kernel>
-int resident_pairs(Kernel kern, size_t smem, int sms) {
+// Deals n units of a cost to the pairs, least loaded first: windows of neighbouring
+// pairs with the same load.
+struct Dealer {
+    struct Window {
+        int from, len;
+        double load;
+    };
+    Window w[2 * kMaxSegments];
+    int windows = 1;
+    double most = 0;
+    Dealer(int pairs) { w[0] = {0, pairs, 0}; }
+
+    void deal(MuonPhase *p, int first, int n, double cost) {
+        int u = first;
+        const int end = first + n;
+        while (u < end) {
+            if (p->segments >= kMaxSegments - 1 || windows >= 2 * kMaxSegments - 1) {  // the rest in turn
+                int all = 0;
+                for (int i = 0; i < windows; ++i) all += w[i].len;
+                segment(p, u, end, 0, all);
+                most += cost * ((end - u + all - 1) / all);
+                return;
+            }
+            int low = 0;
+            double next = INFINITY;
+            for (int i = 1; i < windows; ++i)
+                if (w[i].load < w[low].load) low = i;
+            for (int i = 0; i < windows; ++i)
+                if (i != low) next = std::min(next, w[i].load);
+            Window &x = w[low];
+            const double rounds_most = std::isfinite(next) ? std::max(1.0, std::ceil((next - x.load) / cost - 1e-9)) : 1e9;
+            const int rounds = static_cast<int>(std::min<double>(rounds_most, (end - u) / x.len));
+            if (rounds > 0) {
+                segment(p, u, u + rounds * x.len, x.from, x.len);
+                u += rounds * x.len;
+                x.load += rounds * cost;
+                most = std::max(most, x.load);
+            } else {  // fewer than a round: the window splits
+                const int rem = end - u;
+                segment(p, u, end, x.from, rem);
+                for (int i = windows; i > low + 1; --i) w[i] = w[i - 1];
+                ++windows;
+                w[low + 1] = {x.from + rem, x.len - rem, x.load};
+                w[low].len = rem;
+                w[low].load += cost;
+                most = std::max(most, w[low].load);
+                u = end;
+            }
+            for (int i = 0; i + 1 < windows;) {  // neighbours that are level become one
+                if (std::fabs(w[i].load - w[i + 1].load) < 1e-9 * cost) {
+                    w[i].len += w[i + 1].len;
+                    for (int j = i + 1; j + 1 < windows; ++j) w[j] = w[j + 1];
+                    --windows;
+                } else {
+                    ++i;
+                }
+            }
+        }
+    }
+    static void segment(MuonPhase *p, int from, int to, int pair0, int pairs) {
+        const int s = p->segments++;
+        p->from[s] = from;
+        p->to[s] = to;
+        p->pair0[s] = static_cast<int16_t>(pair0);
+        p->pairs[s] = static_cast<int16_t>(pairs);
+    }
+};
+
+template <int BN, bool X_MAJOR, int EPI>
+cudaError_t product_attribute() {
+    return cudaFuncSetAttribute(muon_product_kernel<BN, X_MAJOR, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                static_cast<int>(sizeof(ProductSmem<BN>) + 1024));
+}
+// CTA pairs that are resident at one time (one CTA an SM, whatever the kernel).
+cudaError_t resident_pairs(int *pairs) {
+    static int cache[64] = {0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64 && cache[dev] > 0) {
+        *pairs = cache[dev];
+        return cudaSuccess;
+    }
+    e = product_attribute<256, false, kStore>();
+    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
+    const int sms = sm_count_here();
     cfg.gridDim = dim3(static_cast<unsigned>(sms / 2 * 2), 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = sizeof(ProductSmem<256>) + 1024;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = 2;
@@ -824,27 +992,21 @@ int resident_pairs(Kernel kern, size_t smem, int sms) {
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n <= 0) {
+    if (cudaOccupancyMaxActiveClusters(&n, muon_product_kernel<256, false, kStore>, &cfg) != cudaSuccess || n <= 0) {
         (void)cudaGetLastError();
         n = sms / 2;
     }
-    return n;
+    if (dev >= 0 && dev < 64) cache[dev] = n;
+    *pairs = n;
+    return cudaSuccess;
 }
 
 template <int BN, bool X_MAJOR, int EPI>
-cudaError_t launch_product(const MuonPhase &p, const MuonOut &out, cudaStream_t s) {
-    auto kern = muon_product_kernel<BN, X_MAJOR, EPI>;
-    const size_t smem = sizeof(ProductSmem<BN>) + 1024;
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+cudaError_t launch_product(const MuonPhase &p, const MuonOut &out, int pairs, cudaStream_t s) {
+    const cudaError_t e = product_attribute<BN, X_MAJOR, EPI>();
     if (e != cudaSuccess) return e;
-    static int cache[64] = {0};
-    int dev = 0, most = 0;
-    if (cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < 64) most = cache[dev];
-    if (most == 0) {
-        most = resident_pairs(kern, smem, sm_count_here());
-        if (dev >= 0 && dev < 64) cache[dev] = most;
-    }
-    return launch_pdl(kern, dim3(2 * std::min(p.units, most)), dim3(kThreads), smem, s, p, out);
+    return launch_pdl(muon_product_kernel<BN, X_MAJOR, EPI>, dim3(2 * std::min(p.units, pairs)), dim3(kThreads),
+                      sizeof(ProductSmem<BN>) + 1024, s, p, out);
 }
 
 // The products of a chunk, phase after phase.
@@ -854,6 +1016,7 @@ struct Products {
     uint8_t *ws;
     int32_t *status;
     cudaStream_t s;
+    int pairs;  // that are resident at one time
     MuonOut out;
 
     int64_t ld(int k, bool square) const { return align_up(square ? c.shape[k].m : c.shape[k].n, 8); }
@@ -865,11 +1028,11 @@ struct Products {
                                 row * c.shape[k].m, bx, by, sw);
     }
 
-    // Tiles of 256 x bn, and what the slowest pair has to do, in k-blocks of 256 x 256.
+    // Tiles of 256 x bn, dealt to the pairs; returns what the longest-working pair has
+    // to do, in k-blocks of 256 x 256.
     double plan(MuonPhase *p, int bn, bool sym, bool square, int passes, bool k_is_n) const {
-        p->units = 0;
-        double work = 0, longest = 0;
-        const double cost = bn == 256 ? 1.0 : 0.55;
+        Dealer dealer(pairs);
+        int order[kMaxClasses], n[kMaxClasses];
         for (int k = 0; k < c.classes; ++k) {
             const int64_t m = c.shape[k].m, cols = square ? m : c.shape[k].n;
             const int64_t tm = (m + 255) / 256, tn = (cols + bn - 1) / bn;
@@ -878,7 +1041,10 @@ struct Products {
                 per = 0;
                 for (int64_t i = 0; i < tm; ++i) per += tn - 256 / bn * i;
             }
+            order[k] = k;
+            n[k] = static_cast<int>(per) * (c.first[k + 1] - c.first[k]);
             p->unit0[k] = p->units;
+            p->units += n[k];
             p->per[k] = static_cast<int>(per);
             p->tiles_m[k] = static_cast<int>(tm);
             p->tiles_n[k] = static_cast<int>(tn);
@@ -886,26 +1052,24 @@ struct Products {
             p->cols[k] = static_cast<int>(cols);
             p->kb[k] = static_cast<int>(((k_is_n ? c.shape[k].n : m) + kBK - 1) / kBK);
             p->first[k] = c.first[k];
-            const int64_t units = per * (c.first[k + 1] - c.first[k]);
-            p->units += static_cast<int>(units);
-            work += cost * static_cast<double>(units) * p->kb[k] * passes;
-            longest = std::max(longest, cost * p->kb[k] * passes);
         }
         p->classes = c.classes;
         p->unit0[c.classes] = p->units;
-        const double pairs = 76, waves = std::ceil(p->units / pairs);
-        return std::max(longest, work / p->units * waves);
+        sort_few(order, c.classes, [&](int a, int b) { return p->kb[a] != p->kb[b] ? p->kb[a] > p->kb[b] : a < b; });
+        const double block = bn == 256 ? 1.0 : kNarrowBlock;
+        for (int i = 0; i < c.classes; ++i)
+            dealer.deal(p, p->unit0[order[i]], n[order[i]], block * (p->kb[order[i]] * passes + kTileBlocks));
+        return dealer.most;
     }
 
     // D = A B^T (BOTH_SQUARE, or of X alone: the Gram matrix) or A X.  Operands and
-    // results by their buffers: g(0 .. 3), x(0 .. 3); -1: none.
+    // results by their buffers: g(0 .. 3), x(0 .. 2); -1: none.
     struct Product {
         int a = -1;             // square A; -1: A and B are X's hi
         int b = -1, b_lo = -1;  // square B, and what is added to it (a second pass over A)
-        int x = 0;              // X: x (hi), x + 1 (lo)
-        bool x_lo = false;      // A X: X's lo as well
-        int d = -1, d_lo = -1;  // square results; -1: the next X, x ^ 2
-        bool next_lo = false;   // of the next X its lo too
+        int x = 0;              // X
+        bool x_lo = false;      // A X: the first X's lo (buffer 1) as well
+        int d = -1, d_lo = -1;  // square results; -1: the next X, 2 - x
         int poly = -1;          // kPoly: G
         double alpha = 0, beta = 0, gamma = 0;
     };
@@ -924,7 +1088,7 @@ struct Products {
             bool ok = gram ? map(&m.a, x(q.x, k), k, false, 64, 128, kSw) : map(&m.a, g(q.a, k), k, true, 64, 128, kSw);
             if (X_MAJOR) {
                 ok = ok && map(&m.b, x(q.x, k), k, false, 64, 64, kSw);
-                if (q.x_lo) ok = ok && map(&m.b_lo, x(q.x + 1, k), k, false, 64, 64, kSw);
+                if (q.x_lo) ok = ok && map(&m.b_lo, x(1, k), k, false, 64, 64, kSw);
             } else {
                 ok = ok && (gram ? map(&m.b, x(q.x, k), k, false, 64, bn / 2, kSw) : map(&m.b, g(q.b, k), k, true, 64, bn / 2, kSw));
                 if (q.b_lo >= 0) ok = ok && map(&m.b_lo, g(q.b_lo, k), k, true, 64, bn / 2, kSw);
@@ -933,8 +1097,7 @@ struct Products {
                 ok = ok && map(&m.d, g(q.d, k), k, true, 32, 32, kSwD);
                 if (q.d_lo >= 0) ok = ok && map(&m.d_lo, g(q.d_lo, k), k, true, 32, 32, kSwD);
             } else if (EPI == kNext) {
-                ok = ok && map(&m.d, x(q.x ^ 2, k), k, false, 32, 32, kSwD);
-                if (q.next_lo) ok = ok && map(&m.d_lo, x((q.x ^ 2) + 1, k), k, false, 32, 32, kSwD);
+                ok = ok && map(&m.d, x(2 - q.x, k), k, false, 32, 32, kSwD);
             }
             if (!ok) return cudaErrorInvalidValue;
             if (EPI == kPoly) {
@@ -947,12 +1110,12 @@ struct Products {
         p.beta = static_cast<float>(q.beta);
         p.gamma = static_cast<float>(q.gamma);
         p.passes = passes;
-        p.store_lo = kSquare ? q.d_lo >= 0 : q.next_lo;
+        p.store_lo = q.d_lo >= 0;
         p.status = status;
         p.wait_ns = wait_timeout_ns();
         // kind::f16, FP32 accumulators, FP16 operands; B N-major for X; N, M = 256 (a pair MMA)
         p.idesc = (1u << 4) | (X_MAJOR ? 1u << 16 : 0u) | (static_cast<uint32_t>(bn >> 3) << 17) | ((256u >> 4) << 24);
-        return bn == 256 ? launch_product<256, X_MAJOR, EPI>(p, out, s) : launch_product<128, X_MAJOR, EPI>(p, out, s);
+        return bn == 256 ? launch_product<256, X_MAJOR, EPI>(p, out, pairs, s) : launch_product<128, X_MAJOR, EPI>(p, out, pairs, s);
     }
 };
 
@@ -974,7 +1137,10 @@ puro_status_t check_matrix(const puro_muon_matrix_t &a) {
 cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu, int nesterov, const Step *steps, int n_steps,
                       uint8_t *ws, int32_t *status, cudaStream_t s) {
     const Scratch at = scratch_of(mats, c);
-    Products run{c, at, ws, status, s, MuonOut{}};
+    int pairs = 0;
+    cudaError_t e = resident_pairs(&pairs);
+    if (e != cudaSuccess) return e;
+    Products run{c, at, ws, status, s, pairs, MuonOut{}};
     // the update, its norm, X
     MuonIn in{};
     in.count = c.count;
@@ -982,7 +1148,6 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
     in.nesterov = nesterov;
     in.store_lo = n_steps > 1;
     in.partial = reinterpret_cast<double *>(ws + at.partial);
-    in.scale = reinterpret_cast<float2 *>(ws + at.scale);
     for (int k = 0; k < c.classes; ++k)
         for (int i = c.first[k]; i < c.first[k + 1]; ++i) {
             const puro_muon_matrix_t &a = mats[c.mats[i]];
@@ -998,18 +1163,19 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
             const bool tall = a.rows > a.cols, bf16 = a.grad_type == PURO_BF16, f32 = a.u_type == PURO_F32;
             const int64_t us = a.rows > 1 ? a.u_stride : a.cols;
             in.flags[i] = (bf16 ? kGradBf16 : 0) | (tall ? kTall : 0);
-            if (a.cols % 8 == 0 && aligned(a.grad, 16) && in.stride[i] % (bf16 ? 8 : 4) == 0 && aligned(a.momentum, 16))
+            if (a.cols % 4 == 0 && aligned(a.grad, bf16 ? 8 : 16) && in.stride[i] % 4 == 0 && aligned(a.momentum, 16))
                 in.flags[i] |= kVectors;
             run.out.u[i] = a.u;
             run.out.stride[i] = us;
             run.out.flags[i] = (tall ? kTall : 0) | (f32 ? kOutF32 : 0);
             if (a.cols % (f32 ? 4 : 8) == 0 && us % (f32 ? 4 : 8) == 0 && aligned(a.u, 16)) run.out.flags[i] |= kOutVectors;
-            in.tile0[i + 1] = in.tile0[i] + static_cast<int>(tiles_in(a.rows, a.cols));
+            const int tiles = static_cast<int>(tiles_in(a.rows, a.cols)), each = (tiles + kMaxSlabs - 1) / kMaxSlabs;
+            in.tile0[i + 1] = in.tile0[i] + tiles;
+            in.slab_tiles[i] = each;
+            in.slab0[i + 1] = in.slab0[i] + (tiles + each - 1) / each;
         }
-    const dim3 tiles(in.tile0[c.count]);
-    cudaError_t e = launch_pdl(muon_update_kernel, tiles, dim3(kInThreads), 0, s, in);
-    if (e == cudaSuccess) e = launch_pdl(muon_norm_kernel, dim3(c.count), dim3(256), 0, s, in);
-    if (e == cudaSuccess) e = launch_pdl(muon_normalise_kernel, tiles, dim3(kInThreads), 0, s, in);
+    e = launch_pdl(muon_update_kernel, dim3(in.slab0[c.count]), dim3(kInThreads), 0, s, in);
+    if (e == cudaSuccess) e = launch_pdl(muon_normalise_kernel, dim3(in.tile0[c.count]), dim3(kInThreads), 0, s, in);
     // the steps, two at a time
     using Product = Products::Product;
     enum { G = 0, B0 = 1, T = 2, B1 = 3, Glo = B1 };  // (G's lo is read before B1 is written)
@@ -1021,7 +1187,8 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
         q.gamma = gamma;
         return q;
     };
-    int x = 0;  // X's buffers: x, x + 1
+    int x = 0;  // X's buffer
+    bool first = true;
     for (int i = 0; i < n_steps && e == cudaSuccess;) {
         const bool pair = i + 1 < n_steps, glo = pair && i > 0;
         const Step &s0 = steps[i];
@@ -1068,15 +1235,15 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
         q = Product{};
         q.a = product;
         q.x = x;
-        q.x_lo = pair;
+        q.x_lo = in.store_lo && first;
+        first = false;
         if (i == n_steps) {
             if (e == cudaSuccess) e = run.run<kOut, true>(scaled(1.0 / (sp * sx)));
         } else {
             const double next = pow2_for(out);
-            q.next_lo = i + 1 < n_steps;  // a pair follows
             if (e == cudaSuccess) e = run.run<kNext, true>(scaled(next / (sp * sx)));
             sx = next;
-            x ^= 2;
+            x = 2 - x;
         }
         most = out;
     }

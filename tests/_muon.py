@@ -59,7 +59,7 @@ def model(v, steps=STEPS):
     while i < len(steps):
         hi = _half(x, sx)
         pair = i + 1 < len(steps)
-        lo = _half(x - hi, sx) if pair else 0 * x
+        lo = _half(x - hi, sx) if pair and i == 0 else 0 * x
         a, b, c = steps[i]
         mp, out = bounds(steps[i], most)
         g = _half(hi @ hi.T, _scale(most ** 2))
