@@ -52,7 +52,7 @@ constexpr uint64_t kDrainNs = 2000000000ull, kSettleNs = 200000ull;
 // ------------------------------------------------ the update and its norm
 constexpr int kInRows = 64, kInCols = 128, kInThreads = 256;  // tile of the two passes over V
 constexpr int kInWarps = kInThreads / 32, kInPasses = 4;  // a warp a row, four rows of a warp at a time
-constexpr int kMaxSlabs = kInThreads;
+constexpr int kMaxSlabs = 512;
 
 enum MatFlags : uint8_t {
     kGradBf16 = 1,
@@ -236,7 +236,7 @@ constexpr int kX0Exp = 14;
 // matrix's sums (at most kMaxSlabs) for the factor 2^14 / ||V||_F,
 // taken in two parts, neither of which leaves FP32's range; NaN where the norm is not
 // finite (all of u is then NaN), 0 for V = 0.
-__global__ void __launch_bounds__(kInThreads, 4) muon_normalise_kernel(const __grid_constant__ MuonIn p) {
+__global__ void __launch_bounds__(kInThreads + 32, 3) muon_normalise_kernel(const __grid_constant__ MuonIn p) {
     __shared__ uint32_t turn[kInCols][kInRows + 1];  // (hi, lo) of the transposed tile
     __shared__ float2 factor;
     pdl_wait();
@@ -247,10 +247,13 @@ __global__ void __launch_bounds__(kInThreads, 4) muon_normalise_kernel(const __g
     const bool tall = flags & kTall;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ldx = p.ldx[m];
     float v[kInPasses][4];
-    read_tile<false>(p, m, t.r0, t.c0, v);
-    if (warp == 0) {  // (one warp: FP64 is slow)
+    if (warp == kInWarps) {  // a warp of its own: FP64 is slow
         double sum = 0.0;
-        for (int i = p.slab0[m] + lane; i < p.slab0[m + 1]; i += 32) sum += p.partial[i];
+#pragma unroll
+        for (int i = 0; i < kMaxSlabs / 32; ++i) {
+            const int at = p.slab0[m] + lane + 32 * i;
+            sum += at < p.slab0[m + 1] ? p.partial[at] : 0.0;
+        }
         sum = warp_sum(sum);
         if (lane == 0) {
             float2 f = make_float2(0.0f, 0.0f);
@@ -263,9 +266,15 @@ __global__ void __launch_bounds__(kInThreads, 4) muon_normalise_kernel(const __g
             }
             factor = f;
         }
+    } else {
+        read_tile<false>(p, m, t.r0, t.c0, v);
     }
     __syncthreads();
     const float2 f = factor;
+    if (warp == kInWarps) {
+        if (tall) __syncthreads();
+        return;
+    }
 #pragma unroll 1
     for (int half = 0; half < kInRows; half += kInWarps * kInPasses) {
         if (half > 0) read_tile<false>(p, m, t.r0 + half, t.c0, v);
@@ -393,7 +402,6 @@ struct ProductSmem {
     uint32_t tmem_base;
     volatile int abort_flag;
 };
-
 // A pair's units, in order.
 struct Walk {
     int segment = 0, u = -1;
@@ -521,9 +529,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     using Smem = ProductSmem<BN>;
     constexpr int kStages = Smem::kStages;
     constexpr bool kSym = EPI == kStore || EPI == kPoly;
+    constexpr int kWarpCols = BN / 2;                           // columns of an epilogue warp
     constexpr uint32_t kStageBytes = kBM * 128 + BN / 2 * 128;  // of one CTA
-    extern __shared__ uint8_t smem_raw[];
-    Smem &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    Smem &sm = *reinterpret_cast<Smem *>(smem_raw);
     const int warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0);
     const int lane = threadIdx.x & 31;
     const int rank = __shfl_sync(0xFFFFFFFFu, static_cast<int>(cluster_ctarank()), 0);
@@ -612,7 +621,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const Unit w = unit_of<BN, kSym>(p, u);
             const int buf = local & 1;
             ok = wait_or_abort(sm, &sm.tempty[buf], ((local >> 1) & 1u) ^ 1u, p.wait_ns, p.status, lane);
-            const uint32_t d = tmem + 256u * buf;
+            const uint32_t d = tmem + static_cast<uint32_t>(BN) * buf;
             const int kbs = w.kb * p.passes;
             for (int kb = 0; kb < kbs && ok; ++kb) {
                 ok = wait_or_abort(sm, &sm.full[stage], phase, p.wait_ns, p.status, lane);
@@ -675,21 +684,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     if (row < rows && col + 8 * k < ldg) g[k] = __ldg(from + k);
                 }
             };
-            if constexpr (EPI == kPoly) load_g(w.n0 + BN / 2 * half);
+            if constexpr (EPI == kPoly) load_g(w.n0 + kWarpCols * half);
             if (!wait_or_abort(sm, &sm.tfull[buf], (local >> 1) & 1u, p.wait_ns, p.status, lane)) break;
             tc_fence_after_sync();
-            const uint32_t acc = tmem + (static_cast<uint32_t>(32 * q) << 16) + 256u * buf + BN / 2 * half;
+            const uint32_t acc = tmem + (static_cast<uint32_t>(32 * q) << 16) + static_cast<uint32_t>(BN * buf + kWarpCols * half);
 #pragma unroll 1
-            for (int i = 0; i < BN / 64; ++i) {
+            for (int i = 0; i < kWarpCols / 32; ++i) {
                 uint32_t r[32];
                 tmem_ld_32x32b_x32(acc + 32 * i, r);
                 tmem_ld_wait();
-                if (i == BN / 64 - 1) {
+                if (i == kWarpCols / 32 - 1) {
                     tc_fence_before_sync();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_cluster_cta_scope(tempty0 + 8u * buf);
                 }
-                const int col = w.n0 + BN / 2 * half + 32 * i;
+                const int col = w.n0 + kWarpCols * half + 32 * i;
                 if (row0 >= rows || col >= cols) continue;
                 float v[32];
 #pragma unroll
@@ -705,7 +714,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                             v[8 * k + 2 * j + 1] = fmaf(p.beta, f.y, v[8 * k + 2 * j + 1]);
                         }
                     }
-                    if (i + 1 < BN / 64) load_g(col + 32);
+                    if (i + 1 < kWarpCols / 32) load_g(col + 32);
                     if (col <= row0 + 31 && row0 <= col + 31) {
 #pragma unroll
                         for (int k = 0; k < 32; ++k)
@@ -965,9 +974,9 @@ struct Dealer {
 template <int BN, bool X_MAJOR, int EPI>
 cudaError_t product_attribute() {
     return cudaFuncSetAttribute(muon_product_kernel<BN, X_MAJOR, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                static_cast<int>(sizeof(ProductSmem<BN>) + 1024));
+                                static_cast<int>(sizeof(ProductSmem<BN>)));
 }
-// CTA pairs that are resident at one time (one CTA an SM, whatever the kernel).
+// Pairs of SMs that run pairs of CTAs.
 cudaError_t resident_pairs(int *pairs) {
     static int cache[64] = {0};
     int dev = 0;
@@ -983,7 +992,7 @@ cudaError_t resident_pairs(int *pairs) {
     const int sms = sm_count_here();
     cfg.gridDim = dim3(static_cast<unsigned>(sms / 2 * 2), 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = sizeof(ProductSmem<256>) + 1024;
+    cfg.dynamicSmemBytes = sizeof(ProductSmem<256>);
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = 2;
@@ -1006,7 +1015,7 @@ cudaError_t launch_product(const MuonPhase &p, const MuonOut &out, int pairs, cu
     const cudaError_t e = product_attribute<BN, X_MAJOR, EPI>();
     if (e != cudaSuccess) return e;
     return launch_pdl(muon_product_kernel<BN, X_MAJOR, EPI>, dim3(2 * std::min(p.units, pairs)), dim3(kThreads),
-                      sizeof(ProductSmem<BN>) + 1024, s, p, out);
+                      sizeof(ProductSmem<BN>), s, p, out);
 }
 
 // The products of a chunk, phase after phase.
@@ -1016,7 +1025,7 @@ struct Products {
     uint8_t *ws;
     int32_t *status;
     cudaStream_t s;
-    int pairs;  // that are resident at one time
+    int pairs;  // of SMs
     MuonOut out;
 
     int64_t ld(int k, bool square) const { return align_up(square ? c.shape[k].m : c.shape[k].n, 8); }
@@ -1175,7 +1184,7 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
             in.slab0[i + 1] = in.slab0[i] + (tiles + each - 1) / each;
         }
     e = launch_pdl(muon_update_kernel, dim3(in.slab0[c.count]), dim3(kInThreads), 0, s, in);
-    if (e == cudaSuccess) e = launch_pdl(muon_normalise_kernel, dim3(in.tile0[c.count]), dim3(kInThreads), 0, s, in);
+    if (e == cudaSuccess) e = launch_pdl(muon_normalise_kernel, dim3(in.tile0[c.count]), dim3(kInThreads + 32), 0, s, in);
     // the steps, two at a time
     using Product = Products::Product;
     enum { G = 0, B0 = 1, T = 2, B1 = 3, Glo = B1 };  // (G's lo is read before B1 is written)
