@@ -61,6 +61,13 @@ enum MatFlags : uint8_t {
     kOutF32 = 8,
     kOutVectors = 16,  // eight columns of a row of u can be stored in 16-byte pieces
 };
+// How X is held ahead of the first step: hi + lo is guess V (a power of two that a
+// sample of the gradient gave), and r of it is X; or, where that would have left
+// FP16's range, hi + lo is V x y = 2^14 X.
+struct MuonScale {
+    float guess, r, x, y;
+    int redo;
+};
 struct MuonIn {
     int count;
     int tile0[kMaxMats + 1];  // first tile of each matrix
@@ -76,6 +83,7 @@ struct MuonIn {
     int nesterov;
     bool store_lo;
     double *partial;  // [slabs]: sum of V^2 over each
+    MuonScale *scale;  // [count]
 };
 
 PURO_DEV int mat_of(const int *start, int count, int t) {
@@ -191,145 +199,207 @@ PURO_DEV double warp_sum(double d) {
     return d;
 }
 
-// The momentum takes the gradient; each slab's sum of V^2.  A thread's 16 squares of
-// half a tile are summed in FP32, in FP64 where that left its range (or all are zero), the
-// rest in FP64 in a fixed order.  Bound by memory.
-__global__ void __launch_bounds__(kInThreads, 4) muon_update_kernel(const __grid_constant__ MuonIn p) {
+// hi + lo of v scaled, four values of a row of the tile at (r0, c0): to X, or for a tall
+// matrix to `turn`, which store_turned() writes.  turn[c][r ^ (c / 4) % 32]: without
+// bank conflicts for lanes that hold four neighbouring columns.
+struct Turn {
+    uint32_t at[kInCols][kInRows];
+};
+PURO_DEV void store_x(const MuonIn &p, int m, Turn &turn, int r0, int lr, int c0, const float (&v)[4], float f0, float f1) {
+    const uint8_t flags = p.flags[m];
+    const int lane = threadIdx.x & 31, ldx = p.ldx[m], r = r0 + lr;
+    uint32_t x[4];  // hi, lo
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float y = (v[k] * f0) * f1;
+        const __half h = __float2half_rn(y), l = __float2half_rn(y - __half2float(h));
+        x[k] = __half_as_ushort(h) | static_cast<uint32_t>(__half_as_ushort(l)) << 16;
+    }
+    if (flags & kTall) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int c = in_col(flags, lane, k);
+            turn.at[c][lr ^ ((flags & kVectors ? c >> 2 : c) & 31)] = x[k];
+        }
+    } else if (r < p.rows[m]) {
+        const int64_t at = static_cast<int64_t>(r) * ldx + c0;
+        if (flags & kVectors) {
+            if (c0 + 4 * lane >= ldx) return;
+            *reinterpret_cast<uint2 *>(p.hi[m] + at + 4 * lane) = make_uint2(__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[2], x[3], 0x5410));
+            if (p.store_lo)
+                *reinterpret_cast<uint2 *>(p.lo[m] + at + 4 * lane) = make_uint2(__byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632));
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int c = lane + 32 * k;
+                if (c0 + c >= ldx) continue;
+                p.hi[m][at + c] = static_cast<uint16_t>(x[k]);
+                if (p.store_lo) p.lo[m][at + c] = static_cast<uint16_t>(x[k] >> 16);
+            }
+        }
+    }
+}
+// A row of X is a column of V: 64 values, two to a lane.
+PURO_DEV void store_turned(const MuonIn &p, int m, const Turn &turn, int r0, int c0) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ldx = p.ldx[m], r = r0 + 2 * lane;
+    const bool vec = p.flags[m] & kVectors;
+    if (r >= ldx) return;
+#pragma unroll 4
+    for (int c = warp; c < kInCols; c += kInWarps) {
+        if (c0 + c >= p.cols[m]) break;
+        const int turned = (vec ? c >> 2 : c) & 31;
+        const uint32_t a = turn.at[c][(2 * lane) ^ turned], b = turn.at[c][(2 * lane + 1) ^ turned];
+        const int64_t at = static_cast<int64_t>(c0 + c) * ldx + r;
+        *reinterpret_cast<uint32_t *>(p.hi[m] + at) = __byte_perm(a, b, 0x5410);
+        if (p.store_lo) *reinterpret_cast<uint32_t *>(p.lo[m] + at) = __byte_perm(a, b, 0x7632);
+    }
+}
+
+constexpr int kSampled = 1024;      // values of the gradient that the guess goes by
+constexpr int kGuessExp = 9;        // it puts their norm's estimate at 2^9: V's may be 2^7 times that, or 2^-3
+constexpr float kLeastNorm = 64.0f, kMostNorm = 65024.0f;  // what guess ||V|| has to lie in: FP16's largest value is 65504
+
+// The momentum takes the gradient; each slab's sum of V^2; hi + lo of V times a power
+// of two.  V is not read again for that (12 bytes a value of 28), so the factor has to
+// be known before the norm: each block takes it from the same sample of the gradient,
+// and muon_norm_kernel finds whether it holds.  A thread's 16 squares of half a tile
+// are summed in FP32, in FP64 where that left its range (or all are zero), the rest in
+// FP64 in a fixed order.  Bound by memory.
+__global__ void __launch_bounds__(kInThreads, 3) muon_update_kernel(const __grid_constant__ MuonIn p) {
+    __shared__ Turn turn;
     __shared__ double part[kInWarps];
+    __shared__ float sampled[kInWarps];
     pdl_wait();
     pdl_launch_dependents();
     const int m = mat_of(p.slab0, p.count, blockIdx.x), tiles = p.tile0[m + 1] - p.tile0[m];
-    const int first = (static_cast<int>(blockIdx.x) - p.slab0[m]) * p.slab_tiles[m];
+    const int slab = static_cast<int>(blockIdx.x) - p.slab0[m], first = slab * p.slab_tiles[m];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const bool tall = p.flags[m] & kTall;
+    const int64_t total = static_cast<int64_t>(p.rows[m]) * p.cols[m];
+    float guess;
+    {
+        const int64_t step = total > kSampled ? (total / kSampled) | 1 : 1;
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kSampled / kInThreads; ++i) {
+            const int64_t e = (threadIdx.x + kInThreads * i) * step;
+            if (e >= total) break;
+            const int64_t r = e / p.cols[m], at = r * p.stride[m] + (e - r * p.cols[m]);
+            s += fabsf(p.flags[m] & kGradBf16 ? __uint_as_float(static_cast<uint32_t>(__ldg(static_cast<const uint16_t *>(p.grad[m]) + at)) << 16)
+                                              : __ldg(static_cast<const float *>(p.grad[m]) + at));
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+        if (lane == 0) sampled[warp] = s;
+        __syncthreads();
+        s = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kInWarps; ++w) s += sampled[w];
+        // ||g|| is about the mean of |g| times sqrt(total)
+        const float norm = s * (1.0f / static_cast<float>(total < kSampled ? total : kSampled)) * sqrtf(static_cast<float>(total));
+        const int k = norm > 0.0f && norm < INFINITY ? min(max(kGuessExp - ilogbf(norm), -126), 127) : 0;
+        guess = __uint_as_float(static_cast<uint32_t>(k + 127) << 23);
+    }
     double sum = 0.0;
-    constexpr int kParts = kInRows / (kInWarps * kInPasses);
-    for (int i = kParts * first; i < kParts * min(tiles, first + p.slab_tiles[m]); ++i) {
-        const InTile t = in_tile(i / kParts, p.cols[m]);
-        float v[kInPasses][4], s = 0.0f;
-        read_tile<true>(p, m, t.r0 + i % kParts * kInWarps * kInPasses, t.c0, v);
+    for (int i = first; i < min(tiles, first + p.slab_tiles[m]); ++i) {
+        const InTile t = in_tile(i, p.cols[m]);
+#pragma unroll 1
+        for (int half = 0; half < kInRows; half += kInWarps * kInPasses) {
+            float v[kInPasses][4], s = 0.0f;
+            read_tile<true>(p, m, t.r0 + half, t.c0, v);
 #pragma unroll
-        for (int j = 0; j < kInPasses; ++j)
+            for (int j = 0; j < kInPasses; ++j) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) s = fmaf(v[j][k], v[j][k], s);
-        if (s > 1e-24f && s < 1e36f) {
-            sum += s;
-        } else {
+                for (int k = 0; k < 4; ++k) s = fmaf(v[j][k], v[j][k], s);
+                store_x(p, m, turn, t.r0, half + warp + kInWarps * j, t.c0, v[j], guess, 1.0f);
+            }
+            if (s > 1e-24f && s < 1e36f) {
+                sum += s;
+            } else {
 #pragma unroll
-            for (int j = 0; j < kInPasses; ++j)
+                for (int j = 0; j < kInPasses; ++j)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) sum += static_cast<double>(v[j][k]) * v[j][k];
+                    for (int k = 0; k < 4; ++k) sum += static_cast<double>(v[j][k]) * v[j][k];
+            }
+        }
+        if (tall) {
+            __syncthreads();
+            store_turned(p, m, turn, t.r0, t.c0);
+            __syncthreads();
         }
     }
     sum = warp_sum(sum);
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sum;
+    if (lane == 0) part[warp] = sum;
     __syncthreads();
     if (threadIdx.x != 0) return;
     sum = 0.0;
 #pragma unroll
     for (int w = 0; w < kInWarps; ++w) sum += part[w];
     p.partial[blockIdx.x] = sum;
+    if (slab == 0) p.scale[m].guess = guess;
 }
 
-// X's power of two: entries are at most 1.
+// The first X's power of two where the guess did not hold: entries are at most 1.
 constexpr int kX0Exp = 14;
 
-// X = V / ||V||_F as FP16 pairs, a tall matrix transposed.  Each block adds up its
-// matrix's sums (at most kMaxSlabs) for the factor 2^14 / ||V||_F,
-// taken in two parts, neither of which leaves FP32's range; NaN where the norm is not
-// finite (all of u is then NaN), 0 for V = 0.
-__global__ void __launch_bounds__(kInThreads + 32, 3) muon_normalise_kernel(const __grid_constant__ MuonIn p) {
-    __shared__ uint32_t turn[kInCols][kInRows + 1];  // (hi, lo) of the transposed tile
-    __shared__ float2 factor;
+// Each matrix's norm, and by it what the first step multiplies with: NaN where it is
+// not finite (all of u is then NaN), 0 for V = 0.
+__global__ void __launch_bounds__(kMaxSlabs) muon_norm_kernel(const __grid_constant__ MuonIn p) {
+    __shared__ double part[kMaxSlabs / 32];
     pdl_wait();
     pdl_launch_dependents();
-    const int m = mat_of(p.tile0, p.count, blockIdx.x);
-    const InTile t = in_tile(static_cast<int>(blockIdx.x) - p.tile0[m], p.cols[m]);
-    const uint8_t flags = p.flags[m];
-    const bool tall = flags & kTall;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ldx = p.ldx[m];
-    float v[kInPasses][4];
-    if (warp == kInWarps) {  // a warp of its own: FP64 is slow
-        double sum = 0.0;
-#pragma unroll
-        for (int i = 0; i < kMaxSlabs / 32; ++i) {
-            const int at = p.slab0[m] + lane + 32 * i;
-            sum += at < p.slab0[m + 1] ? p.partial[at] : 0.0;
-        }
-        sum = warp_sum(sum);
-        if (lane == 0) {
-            float2 f = make_float2(0.0f, 0.0f);
-            if (!(sum < INFINITY)) {
-                f.x = f.y = NAN;
-            } else if (sum > 0.0) {
-                const double scale = static_cast<double>(1 << kX0Exp) / sqrt(sum);
-                const int e = ilogb(scale) / 2;
-                f = make_float2(static_cast<float>(ldexp(1.0, e)), static_cast<float>(ldexp(scale, -e)));
-            }
-            factor = f;
-        }
-    } else {
-        read_tile<false>(p, m, t.r0, t.c0, v);
-    }
+    const int m = blockIdx.x, i = p.slab0[m] + static_cast<int>(threadIdx.x);
+    double d = i < p.slab0[m + 1] ? p.partial[i] : 0.0;
+    d = warp_sum(d);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = d;
     __syncthreads();
-    const float2 f = factor;
-    if (warp == kInWarps) {
-        if (tall) __syncthreads();
-        return;
+    if (threadIdx.x >= 32) return;
+    d = threadIdx.x < kMaxSlabs / 32 ? part[threadIdx.x] : 0.0;
+    d = warp_sum(d);
+    if (threadIdx.x != 0) return;
+    MuonScale s{p.scale[m].guess, 0.0f, 0.0f, 0.0f, 0};
+    if (!(d < INFINITY)) {
+        s.r = NAN;
+    } else if (d > 0.0) {
+        const double norm = sqrt(d), held = norm * s.guess;
+        s.r = static_cast<float>(1.0 / held);
+        if (!(held >= kLeastNorm && held <= kMostNorm)) {
+            // the factor in two parts, neither of which leaves FP32's range
+            const double scale = static_cast<double>(1 << kX0Exp) / norm;
+            const int e = ilogb(scale) / 2;
+            s.x = static_cast<float>(ldexp(1.0, e));
+            s.y = static_cast<float>(ldexp(scale, -e));
+            s.r = 1.0f / static_cast<float>(1 << kX0Exp);
+            s.redo = 1;
+        }
     }
+    p.scale[m] = s;
+}
+
+// X once more, by the norm, of the matrices whose guess did not hold.
+__global__ void __launch_bounds__(kInThreads, 3) muon_redo_kernel(const __grid_constant__ MuonIn p) {
+    __shared__ Turn turn;
+    pdl_wait();
+    pdl_launch_dependents();
+    if (!__syncthreads_or(static_cast<int>(threadIdx.x) < p.count && p.scale[threadIdx.x].redo)) return;
+    for (int i = blockIdx.x; i < p.tile0[p.count]; i += gridDim.x) {
+        const int m = mat_of(p.tile0, p.count, i);
+        const MuonScale s = p.scale[m];
+        if (!s.redo) continue;
+        const InTile t = in_tile(i - p.tile0[m], p.cols[m]);
 #pragma unroll 1
-    for (int half = 0; half < kInRows; half += kInWarps * kInPasses) {
-        if (half > 0) read_tile<false>(p, m, t.r0 + half, t.c0, v);
+        for (int half = 0; half < kInRows; half += kInWarps * kInPasses) {
+            float v[kInPasses][4];
+            read_tile<false>(p, m, t.r0 + half, t.c0, v);
 #pragma unroll
-        for (int i = 0; i < kInPasses; ++i) {
-            const int lr = half + warp + kInWarps * i, r = t.r0 + lr;
-            uint32_t x[4];  // hi, lo
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float y = (v[i][k] * f.x) * f.y;
-                const __half h = __float2half_rn(y), l = __float2half_rn(y - __half2float(h));
-                x[k] = __half_as_ushort(h) | static_cast<uint32_t>(__half_as_ushort(l)) << 16;
-            }
-            if (tall) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) turn[in_col(flags, lane, k)][lr] = x[k];
-            } else if (r < p.rows[m]) {
-                const int64_t at = static_cast<int64_t>(r) * ldx + t.c0;
-                if (flags & kVectors) {
-                    if (t.c0 + 4 * lane >= ldx) continue;
-                    *reinterpret_cast<uint2 *>(p.hi[m] + at + 4 * lane) = make_uint2(__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[2], x[3], 0x5410));
-                    if (p.store_lo)
-                        *reinterpret_cast<uint2 *>(p.lo[m] + at + 4 * lane) = make_uint2(__byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632));
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int c = lane + 32 * k;
-                        if (t.c0 + c >= ldx) continue;
-                        p.hi[m][at + c] = static_cast<uint16_t>(x[k]);
-                        if (p.store_lo) p.lo[m][at + c] = static_cast<uint16_t>(x[k] >> 16);
-                    }
-                }
-            }
+            for (int j = 0; j < kInPasses; ++j)
+                store_x(p, m, turn, t.r0, half + static_cast<int>(threadIdx.x >> 5) + kInWarps * j, t.c0, v[j], s.x, s.y);
         }
-    }
-    if (!tall) return;
-    __syncthreads();
-    // a row of X: a column of V, 64 values, eight to a thread
-    const int r8 = threadIdx.x % 8 * 8;
-#pragma unroll
-    for (int i = 0; i < kInCols / 32; ++i) {
-        const int c = threadIdx.x / 8 + 32 * i;
-        if (t.c0 + c >= p.cols[m] || t.r0 + r8 >= ldx) continue;
-        uint32_t x[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = turn[c][r8 + k];
-        const int64_t at = static_cast<int64_t>(t.c0 + c) * ldx + t.r0 + r8;
-        uint32_t h[4], l[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            h[k] = __byte_perm(x[2 * k], x[2 * k + 1], 0x5410);
-            l[k] = __byte_perm(x[2 * k], x[2 * k + 1], 0x7632);
+        if (p.flags[m] & kTall) {
+            __syncthreads();
+            store_turned(p, m, turn, t.r0, t.c0);
+            __syncthreads();
         }
-        *reinterpret_cast<uint4 *>(p.hi[m] + at) = make_uint4(h[0], h[1], h[2], h[3]);
-        if (p.store_lo) *reinterpret_cast<uint4 *>(p.lo[m] + at) = make_uint4(l[0], l[1], l[2], l[3]);
     }
 }
 
@@ -378,6 +448,8 @@ struct MuonPhase {
     int64_t g_batch[kMaxClasses];
     int ldg[kMaxClasses];
     float alpha, beta, gamma;
+    const MuonScale *scale;      // of the first X, or null: alpha times r, of X X^T r^2
+    bool squared;
     int passes;                  // 2: B's lo after its hi
     bool store_lo;
     uint32_t idesc;
@@ -674,6 +746,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const int buf = local & 1;
             const MuonMaps &maps = p.maps[w.cls];
             const int row0 = w.m0 + kBM * rank + 32 * q, rows = p.rows[w.cls], cols = p.cols[w.cls];
+            float alpha = p.alpha;
+            if (p.scale) {
+                const float x = __ldg(&p.scale[p.first[w.cls] + w.z].r);
+                alpha *= p.squared ? x * x : x;
+            }
             uint4 g[4];
             auto load_g = [&](int col) {  // the lane's row of G (kPoly), ahead of its use
                 const int row = row0 + lane, ldg = p.ldg[w.cls];
@@ -702,7 +779,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 if (row0 >= rows || col >= cols) continue;
                 float v[32];
 #pragma unroll
-                for (int k = 0; k < 32; ++k) v[k] = p.alpha * __uint_as_float(r[k]);
+                for (int k = 0; k < 32; ++k) v[k] = alpha * __uint_as_float(r[k]);
                 if constexpr (EPI == kPoly) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
@@ -843,7 +920,7 @@ struct Scratch {
     int64_t bytes = 0;
     int64_t x[3][kMaxClasses];  // offsets: X, the first X's lo, the next X
     int64_t g[4][kMaxClasses];  // G, B0, T (then B1 B0), G's lo (then B1)
-    int64_t partial = 0;
+    int64_t partial = 0, scale = 0;
 };
 int64_t tiles_in(int64_t rows, int64_t cols) {
     return (rows + kInRows - 1) / kInRows * ((cols + kInCols - 1) / kInCols);
@@ -856,6 +933,7 @@ Scratch scratch_of(const puro_muon_matrix_t *mats, const Chunk &c) {
         return at;
     };
     s.partial = take(8 * c.count * kMaxSlabs);
+    s.scale = take(static_cast<int64_t>(sizeof(MuonScale)) * c.count);
     for (int k = 0; k < c.classes; ++k) {
         const int64_t n = c.first[k + 1] - c.first[k];
         for (int b = 0; b < 3; ++b) s.x[b][k] = take(n * c.shape[k].m * align_up(c.shape[k].n, 8) * 2);
@@ -1080,6 +1158,7 @@ struct Products {
         bool x_lo = false;      // A X: the first X's lo (buffer 1) as well
         int d = -1, d_lo = -1;  // square results; -1: the next X, 2 - x
         int poly = -1;          // kPoly: G
+        const MuonScale *scale = nullptr;  // of the first X
         double alpha = 0, beta = 0, gamma = 0;
     };
     template <int EPI, bool X_MAJOR>
@@ -1120,6 +1199,8 @@ struct Products {
         p.gamma = static_cast<float>(q.gamma);
         p.passes = passes;
         p.store_lo = q.d_lo >= 0;
+        p.scale = q.scale;
+        p.squared = gram;
         p.status = status;
         p.wait_ns = wait_timeout_ns();
         // kind::f16, FP32 accumulators, FP16 operands; B N-major for X; N, M = 256 (a pair MMA)
@@ -1157,6 +1238,7 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
     in.nesterov = nesterov;
     in.store_lo = n_steps > 1;
     in.partial = reinterpret_cast<double *>(ws + at.partial);
+    in.scale = reinterpret_cast<MuonScale *>(ws + at.scale);
     for (int k = 0; k < c.classes; ++k)
         for (int i = c.first[k]; i < c.first[k + 1]; ++i) {
             const puro_muon_matrix_t &a = mats[c.mats[i]];
@@ -1184,11 +1266,12 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
             in.slab0[i + 1] = in.slab0[i] + (tiles + each - 1) / each;
         }
     e = launch_pdl(muon_update_kernel, dim3(in.slab0[c.count]), dim3(kInThreads), 0, s, in);
-    if (e == cudaSuccess) e = launch_pdl(muon_normalise_kernel, dim3(in.tile0[c.count]), dim3(kInThreads + 32), 0, s, in);
+    if (e == cudaSuccess) e = launch_pdl(muon_norm_kernel, dim3(c.count), dim3(kMaxSlabs), 0, s, in);
+    if (e == cudaSuccess) e = launch_pdl(muon_redo_kernel, dim3(std::min(in.tile0[c.count], 6 * pairs)), dim3(kInThreads), 0, s, in);
     // the steps, two at a time
     using Product = Products::Product;
     enum { G = 0, B0 = 1, T = 2, B1 = 3, Glo = B1 };  // (G's lo is read before B1 is written)
-    double most = 1.0, sx = 1 << kX0Exp;
+    double most = 1.0, sx = 1.0;  // (the first X's power of two is in its MuonScale)
     Product q;
     auto scaled = [&](double alpha, double beta = 0, double gamma = 0) {
         q.alpha = alpha;
@@ -1206,6 +1289,7 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
         q.x = x;
         q.d = G;
         q.d_lo = glo ? Glo : -1;
+        q.scale = first ? in.scale : nullptr;
         e = run.run<kStore, false>(scaled(sg / (sx * sx)));
         q = Product{};  // B0 = a I + b G + c G^2
         q.a = q.b = q.poly = G;
@@ -1245,6 +1329,7 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
         q.a = product;
         q.x = x;
         q.x_lo = in.store_lo && first;
+        q.scale = first ? in.scale : nullptr;
         first = false;
         if (i == n_steps) {
             if (e == cudaSuccess) e = run.run<kOut, true>(scaled(1.0 / (sp * sx)));

@@ -146,6 +146,27 @@ def test_the_size_of_v_does_not_count(factor):
         assert (a - b).norm() <= 2.0 ** -8 * a.norm()
 
 
+@pytest.mark.parametrize("r,c", [(60, 200), (200, 60), (33, 71)])
+@pytest.mark.parametrize("g_size,m_size", [(0.0, 1.0), (1.0, 1e5), (1e-30, 1.0), (1.0, 0.0), (1e30, 1e36), (1e-38, 1e-38)])
+def test_a_gradient_that_says_nothing_of_the_momentum(r, c, g_size, m_size):
+    """X is scaled by a sample of the gradient, or by the norm where that does not hold for V."""
+    g, m = 1024 * M.gradient(r, c, 1) * g_size, 1024 * M.gradient(r, c, 2) * m_size
+    buf, u = m.to(DEV), torch.empty(r, c, device=DEV)
+    directions([(g.to(DEV), buf, u)], mu=0.5, nesterov=False)
+    want, v = M.update(g.double(), m.double(), 0.5, False)
+    assert ((buf.cpu().double() - want).abs() <= 2.0 ** -24 * want.abs() + 2.0 ** -149).all()
+    check(u, buf.cpu(), F32)
+
+
+@pytest.mark.parametrize("r,c", [(64, 90), (90, 64)])
+def test_few_values_are_not_zero(r, c):
+    g = torch.zeros(r, c)
+    g[5, 7], g[40, 60], g[40, 7] = 3.0, -2.0, 1e-3
+    u = torch.empty(r, c, device=DEV)
+    directions([(g.to(DEV), None, u)])
+    check(u, g, F32)
+
+
 def test_denormal_values():
     g = M.gradient(20, 30, 9, "noise") * 2.0 ** -130
     u = torch.empty(20, 30, device=DEV)
