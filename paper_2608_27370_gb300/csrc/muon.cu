@@ -36,6 +36,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "internal.h"
 #include "ptx.cuh"
@@ -57,8 +58,9 @@ constexpr int kMaxSlabs = 512;
 enum MatFlags : uint8_t {
     kGradBf16 = 1,
     kTall = 2,      // more rows than columns: X is its transpose
-    kVectors = 4,   // four columns of a row can be read at once in grad and momentum
+    kVectors = 4,   // four columns of a row can be read at once in momentum (and stored in X)
     kOutF32 = 8,
+    kGradVectors = 32,  // and in grad
     kOutVectors = 16,  // eight columns of a row of u can be stored in 16-byte pieces
 };
 // How X is held ahead of the first step: hi + lo is guess V (a power of two that a
@@ -68,22 +70,27 @@ struct MuonScale {
     float guess, r, x, y;
     int redo;
 };
+// One matrix's part of the update (together: a block's first use of a parameter is a
+// cache miss).
+struct alignas(16) MatIn {
+    const void *grad;
+    float *momentum;
+    int64_t stride;
+    uint16_t *hi, *lo;
+    int rows, cols, ldx;
+    int slab_tiles;  // tiles of a slab
+    uint8_t flags;
+};
 struct MuonIn {
     int count;
-    int tile0[kMaxMats + 1];  // first tile of each matrix
-    int slab0[kMaxMats + 1];  // first slab: a run of slab_tiles tiles whose sum of V^2 one block takes
-    int slab_tiles[kMaxMats];
-    const void *grad[kMaxMats];
-    float *momentum[kMaxMats];
-    int64_t stride[kMaxMats];
-    int rows[kMaxMats], cols[kMaxMats], ldx[kMaxMats];
-    uint16_t *hi[kMaxMats], *lo[kMaxMats];
-    uint8_t flags[kMaxMats];
     float mu;
     int nesterov;
     bool store_lo;
     double *partial;  // [slabs]: sum of V^2 over each
     MuonScale *scale;  // [count]
+    int tile0[kMaxMats + 1];  // first tile of each matrix
+    int slab0[kMaxMats + 1];  // first slab: a run of tiles whose sum of V^2 one block takes
+    MatIn mat[kMaxMats];
 };
 
 PURO_DEV int mat_of(const int *start, int count, int t) {
@@ -103,12 +110,12 @@ PURO_DEV int in_col(uint8_t flags, int lane, int k) { return flags & kVectors ? 
 // zero outside the matrix.  UPDATE: the momentum takes the gradient first and is
 // stored; else it has.  All loads are issued ahead of the first use (with each row's
 // behind the row before's stores a layer's update took 114 us instead of XX).
-template <bool UPDATE, bool VEC, bool BF16>
+template <bool UPDATE, bool VEC, bool GRAD_VEC, bool BF16>
 PURO_DEV void tile_of(const MuonIn &p, int m, int r0, int c0, float (&v)[kInPasses][4]) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rows = p.rows[m], cols = p.cols[m];
-    float *const mom = p.momentum[m];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rows = p.mat[m].rows, cols = p.mat[m].cols;
+    float *const mom = p.mat[m].momentum;
     const bool read_g = UPDATE || !mom || p.nesterov;
-    const int64_t stride = p.stride[m];
+    const int64_t stride = p.mat[m].stride;
     float w[kInPasses][4];
     auto in = [&](int i, int k) { return r0 + warp + kInWarps * i < rows && c0 + (VEC ? 4 * lane : lane + 32 * k) < cols; };
     auto at = [&](int i, int k, int64_t pitch) { return (r0 + warp + kInWarps * i) * pitch + c0 + (VEC ? 4 * lane : lane + 32 * k); };
@@ -119,12 +126,23 @@ PURO_DEV void tile_of(const MuonIn &p, int m, int r0, int c0, float (&v)[kInPass
             float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             if (in(i, 0)) {
                 if (read_g) {
-                    if constexpr (BF16) {
-                        const uint2 z = __ldg(reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p.grad[m]) + at(i, 0, stride)));
+                    if constexpr (!GRAD_VEC) {  // (a warp's loads of one k are 8 or 16 bytes apart: the next find them in L1)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int64_t from = at(i, 0, stride) + k;
+                            const uint32_t z = BF16 ? __ldg(static_cast<const uint16_t *>(p.mat[m].grad) + from)
+                                                    : __float_as_uint(__ldg(static_cast<const float *>(p.mat[m].grad) + from));
+                            if (BF16)
+                                (k < 2 ? x.x : x.y) |= z << (16 * (k & 1));
+                            else
+                                (k == 0 ? x.x : k == 1 ? x.y : k == 2 ? x.z : x.w) = z;
+                        }
+                    } else if constexpr (BF16) {
+                        const uint2 z = __ldg(reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p.mat[m].grad) + at(i, 0, stride)));
                         x.x = z.x;
                         x.y = z.y;
                     } else {
-                        x = __ldg(reinterpret_cast<const uint4 *>(static_cast<const float *>(p.grad[m]) + at(i, 0, stride)));
+                        x = __ldg(reinterpret_cast<const uint4 *>(static_cast<const float *>(p.mat[m].grad) + at(i, 0, stride)));
                     }
                 }
                 if (mom) y = *reinterpret_cast<const float4 *>(mom + at(i, 0, cols));
@@ -143,8 +161,8 @@ PURO_DEV void tile_of(const MuonIn &p, int m, int r0, int c0, float (&v)[kInPass
                 v[i][k] = w[i][k] = 0.0f;
                 if (!in(i, k)) continue;
                 if (read_g)
-                    v[i][k] = BF16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t *>(p.grad[m])[at(i, k, stride)]) << 16)
-                                   : static_cast<const float *>(p.grad[m])[at(i, k, stride)];
+                    v[i][k] = BF16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t *>(p.mat[m].grad)[at(i, k, stride)]) << 16)
+                                   : static_cast<const float *>(p.mat[m].grad)[at(i, k, stride)];
                 if (mom) w[i][k] = mom[at(i, k, cols)];
             }
         }
@@ -171,18 +189,20 @@ PURO_DEV void tile_of(const MuonIn &p, int m, int r0, int c0, float (&v)[kInPass
 }
 template <bool UPDATE>
 PURO_DEV void read_tile(const MuonIn &p, int m, int r0, int c0, float (&v)[kInPasses][4]) {
-    const uint8_t f = p.flags[m];
-    if (f & kVectors) {
-        if (f & kGradBf16)
-            tile_of<UPDATE, true, true>(p, m, r0, c0, v);
+    const uint8_t f = p.mat[m].flags;
+    auto read = [&](auto bf16) {
+        constexpr bool kBf16 = decltype(bf16)::value;
+        if (!(f & kVectors))
+            tile_of<UPDATE, false, false, kBf16>(p, m, r0, c0, v);
+        else if (f & kGradVectors)
+            tile_of<UPDATE, true, true, kBf16>(p, m, r0, c0, v);
         else
-            tile_of<UPDATE, true, false>(p, m, r0, c0, v);
-    } else {
-        if (f & kGradBf16)
-            tile_of<UPDATE, false, true>(p, m, r0, c0, v);
-        else
-            tile_of<UPDATE, false, false>(p, m, r0, c0, v);
-    }
+            tile_of<UPDATE, true, false, kBf16>(p, m, r0, c0, v);
+    };
+    if (f & kGradBf16)
+        read(std::true_type{});
+    else
+        read(std::false_type{});
 }
 
 struct InTile {
@@ -206,8 +226,8 @@ struct Turn {
     uint32_t at[kInCols][kInRows];
 };
 PURO_DEV void store_x(const MuonIn &p, int m, Turn &turn, int r0, int lr, int c0, const float (&v)[4], float f0, float f1) {
-    const uint8_t flags = p.flags[m];
-    const int lane = threadIdx.x & 31, ldx = p.ldx[m], r = r0 + lr;
+    const uint8_t flags = p.mat[m].flags;
+    const int lane = threadIdx.x & 31, ldx = p.mat[m].ldx, r = r0 + lr;
     uint32_t x[4];  // hi, lo
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -221,37 +241,37 @@ PURO_DEV void store_x(const MuonIn &p, int m, Turn &turn, int r0, int lr, int c0
             const int c = in_col(flags, lane, k);
             turn.at[c][lr ^ ((flags & kVectors ? c >> 2 : c) & 31)] = x[k];
         }
-    } else if (r < p.rows[m]) {
+    } else if (r < p.mat[m].rows) {
         const int64_t at = static_cast<int64_t>(r) * ldx + c0;
         if (flags & kVectors) {
             if (c0 + 4 * lane >= ldx) return;
-            *reinterpret_cast<uint2 *>(p.hi[m] + at + 4 * lane) = make_uint2(__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[2], x[3], 0x5410));
+            *reinterpret_cast<uint2 *>(p.mat[m].hi + at + 4 * lane) = make_uint2(__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[2], x[3], 0x5410));
             if (p.store_lo)
-                *reinterpret_cast<uint2 *>(p.lo[m] + at + 4 * lane) = make_uint2(__byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632));
+                *reinterpret_cast<uint2 *>(p.mat[m].lo + at + 4 * lane) = make_uint2(__byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632));
         } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int c = lane + 32 * k;
                 if (c0 + c >= ldx) continue;
-                p.hi[m][at + c] = static_cast<uint16_t>(x[k]);
-                if (p.store_lo) p.lo[m][at + c] = static_cast<uint16_t>(x[k] >> 16);
+                p.mat[m].hi[at + c] = static_cast<uint16_t>(x[k]);
+                if (p.store_lo) p.mat[m].lo[at + c] = static_cast<uint16_t>(x[k] >> 16);
             }
         }
     }
 }
 // A row of X is a column of V: 64 values, two to a lane.
 PURO_DEV void store_turned(const MuonIn &p, int m, const Turn &turn, int r0, int c0) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ldx = p.ldx[m], r = r0 + 2 * lane;
-    const bool vec = p.flags[m] & kVectors;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ldx = p.mat[m].ldx, r = r0 + 2 * lane;
+    const bool vec = p.mat[m].flags & kVectors;
     if (r >= ldx) return;
 #pragma unroll 4
     for (int c = warp; c < kInCols; c += kInWarps) {
-        if (c0 + c >= p.cols[m]) break;
+        if (c0 + c >= p.mat[m].cols) break;
         const int turned = (vec ? c >> 2 : c) & 31;
         const uint32_t a = turn.at[c][(2 * lane) ^ turned], b = turn.at[c][(2 * lane + 1) ^ turned];
         const int64_t at = static_cast<int64_t>(c0 + c) * ldx + r;
-        *reinterpret_cast<uint32_t *>(p.hi[m] + at) = __byte_perm(a, b, 0x5410);
-        if (p.store_lo) *reinterpret_cast<uint32_t *>(p.lo[m] + at) = __byte_perm(a, b, 0x7632);
+        *reinterpret_cast<uint32_t *>(p.mat[m].hi + at) = __byte_perm(a, b, 0x5410);
+        if (p.store_lo) *reinterpret_cast<uint32_t *>(p.mat[m].lo + at) = __byte_perm(a, b, 0x7632);
     }
 }
 
@@ -263,59 +283,61 @@ constexpr float kLeastNorm = 64.0f, kMostNorm = 65024.0f;  // what guess ||V|| h
 // of two.  V is not read again for that (12 bytes a value of 28), so the factor has to
 // be known before the norm: each block takes it from the same sample of the gradient,
 // and muon_norm_kernel finds whether it holds.  A thread's 16 squares of half a tile
-// are summed in FP32, in FP64 where that left its range (or all are zero), the rest in
-// FP64 in a fixed order.  Bound by memory.
-__global__ void __launch_bounds__(kInThreads, 3) muon_update_kernel(const __grid_constant__ MuonIn p) {
+// are summed in FP32, in FP64 where that left its range, the rest in FP64 in a fixed
+// order.  Bound by memory.
+__global__ void __launch_bounds__(kInThreads, 4) muon_update_kernel(const __grid_constant__ MuonIn p) {
     __shared__ Turn turn;
     __shared__ double part[kInWarps];
     __shared__ float sampled[kInWarps];
     pdl_wait();
     pdl_launch_dependents();
     const int m = mat_of(p.slab0, p.count, blockIdx.x), tiles = p.tile0[m + 1] - p.tile0[m];
-    const int slab = static_cast<int>(blockIdx.x) - p.slab0[m], first = slab * p.slab_tiles[m];
+    const int slab = static_cast<int>(blockIdx.x) - p.slab0[m], first = slab * p.mat[m].slab_tiles;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const bool tall = p.flags[m] & kTall;
-    const int64_t total = static_cast<int64_t>(p.rows[m]) * p.cols[m];
-    float guess;
-    {
-        const int64_t step = total > kSampled ? (total / kSampled) | 1 : 1;
-        float s = 0.0f;
+    const bool tall = p.mat[m].flags & kTall;
+    float sample = 0.0f;  // rows evenly, columns by a hash
 #pragma unroll
-        for (int i = 0; i < kSampled / kInThreads; ++i) {
-            const int64_t e = (threadIdx.x + kInThreads * i) * step;
-            if (e >= total) break;
-            const int64_t r = e / p.cols[m], at = r * p.stride[m] + (e - r * p.cols[m]);
-            s += fabsf(p.flags[m] & kGradBf16 ? __uint_as_float(static_cast<uint32_t>(__ldg(static_cast<const uint16_t *>(p.grad[m]) + at)) << 16)
-                                              : __ldg(static_cast<const float *>(p.grad[m]) + at));
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-        if (lane == 0) sampled[warp] = s;
-        __syncthreads();
-        s = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kInWarps; ++w) s += sampled[w];
-        // ||g|| is about the mean of |g| times sqrt(total)
-        const float norm = s * (1.0f / static_cast<float>(total < kSampled ? total : kSampled)) * sqrtf(static_cast<float>(total));
-        const int k = norm > 0.0f && norm < INFINITY ? min(max(kGuessExp - ilogbf(norm), -126), 127) : 0;
-        guess = __uint_as_float(static_cast<uint32_t>(k + 127) << 23);
+    for (int i = 0; i < kSampled / kInThreads; ++i) {
+        const uint32_t e = threadIdx.x + kInThreads * i;
+        const int64_t at = (e * static_cast<uint32_t>(p.mat[m].rows) / kSampled) * p.mat[m].stride +
+                           __umulhi(e * 2654435761u, static_cast<uint32_t>(p.mat[m].cols));
+        sample += fabsf(p.mat[m].flags & kGradBf16
+                            ? __uint_as_float(static_cast<uint32_t>(__ldg(static_cast<const uint16_t *>(p.mat[m].grad) + at)) << 16)
+                            : __ldg(static_cast<const float *>(p.mat[m].grad) + at));
     }
+    float guess = 0.0f;
     double sum = 0.0;
-    for (int i = first; i < min(tiles, first + p.slab_tiles[m]); ++i) {
-        const InTile t = in_tile(i, p.cols[m]);
+    for (int i = first; i < min(tiles, first + p.mat[m].slab_tiles); ++i) {
+        const InTile t = in_tile(i, p.mat[m].cols);
 #pragma unroll 1
         for (int half = 0; half < kInRows; half += kInWarps * kInPasses) {
-            float v[kInPasses][4], s = 0.0f;
+            float v[kInPasses][4], s = 0.0f, most = 0.0f;
             read_tile<true>(p, m, t.r0 + half, t.c0, v);
+            if (guess == 0.0f) {  // once, beside the first reads
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) sample += __shfl_xor_sync(0xFFFFFFFFu, sample, o);
+                if (lane == 0) sampled[warp] = sample;
+                __syncthreads();
+                float n = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kInWarps; ++w) n += sampled[w];
+                // ||g|| is about the mean of |g| times sqrt(total)
+                n *= (1.0f / kSampled) * sqrtf(static_cast<float>(p.mat[m].rows) * static_cast<float>(p.mat[m].cols));
+                const int k = n > 0.0f && n < INFINITY ? min(max(kGuessExp - ilogbf(n), -126), 127) : 0;
+                guess = __uint_as_float(static_cast<uint32_t>(k + 127) << 23);
+            }
 #pragma unroll
             for (int j = 0; j < kInPasses; ++j) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) s = fmaf(v[j][k], v[j][k], s);
+                for (int k = 0; k < 4; ++k) {
+                    s = fmaf(v[j][k], v[j][k], s);
+                    most = fmaxf(most, fabsf(v[j][k]));
+                }
                 store_x(p, m, turn, t.r0, half + warp + kInWarps * j, t.c0, v[j], guess, 1.0f);
             }
             if (s > 1e-24f && s < 1e36f) {
                 sum += s;
-            } else {
+            } else if (!(s == 0.0f && most == 0.0f)) {  // (FP64 is 64 times slower: not for what lies outside the matrix)
 #pragma unroll
                 for (int j = 0; j < kInPasses; ++j)
 #pragma unroll
@@ -386,7 +408,7 @@ __global__ void __launch_bounds__(kInThreads, 3) muon_redo_kernel(const __grid_c
         const int m = mat_of(p.tile0, p.count, i);
         const MuonScale s = p.scale[m];
         if (!s.redo) continue;
-        const InTile t = in_tile(i - p.tile0[m], p.cols[m]);
+        const InTile t = in_tile(i - p.tile0[m], p.mat[m].cols);
 #pragma unroll 1
         for (int half = 0; half < kInRows; half += kInWarps * kInPasses) {
             float v[kInPasses][4];
@@ -395,7 +417,7 @@ __global__ void __launch_bounds__(kInThreads, 3) muon_redo_kernel(const __grid_c
             for (int j = 0; j < kInPasses; ++j)
                 store_x(p, m, turn, t.r0, half + static_cast<int>(threadIdx.x >> 5) + kInWarps * j, t.c0, v[j], s.x, s.y);
         }
-        if (p.flags[m] & kTall) {
+        if (p.mat[m].flags & kTall) {
             __syncthreads();
             store_turned(p, m, turn, t.r0, t.c0);
             __syncthreads();
@@ -922,6 +944,10 @@ struct Scratch {
     int64_t g[4][kMaxClasses];  // G, B0, T (then B1 B0), G's lo (then B1)
     int64_t partial = 0, scale = 0;
 };
+// Tiles of a slab: one where that leaves each SM a block or so, else as many as make
+// 128 to 256 slabs (a block's sample takes 1.5 us).  By the matrix's size alone: the
+// sums' order follows from it.
+int slab_tiles_of(int tiles) { return tiles <= 512 ? 1 : (tiles + 255) / 256; }
 int64_t tiles_in(int64_t rows, int64_t cols) {
     return (rows + kInRows - 1) / kInRows * ((cols + kInCols - 1) / kInCols);
 }
@@ -1243,26 +1269,29 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
         for (int i = c.first[k]; i < c.first[k + 1]; ++i) {
             const puro_muon_matrix_t &a = mats[c.mats[i]];
             const int64_t z = (i - c.first[k]) * c.shape[k].m * run.ld(k, false);
-            in.grad[i] = a.grad;
-            in.momentum[i] = a.momentum;
-            in.stride[i] = a.rows > 1 ? a.grad_stride : a.cols;
-            in.rows[i] = static_cast<int>(a.rows);
-            in.cols[i] = static_cast<int>(a.cols);
-            in.ldx[i] = static_cast<int>(run.ld(k, false));
-            in.hi[i] = run.x(0, k) + z;
-            in.lo[i] = run.x(1, k) + z;
+            MatIn &to = in.mat[i];
+            to.grad = a.grad;
+            to.momentum = a.momentum;
+            to.stride = a.rows > 1 ? a.grad_stride : a.cols;
+            to.rows = static_cast<int>(a.rows);
+            to.cols = static_cast<int>(a.cols);
+            to.ldx = static_cast<int>(run.ld(k, false));
+            to.hi = run.x(0, k) + z;
+            to.lo = run.x(1, k) + z;
             const bool tall = a.rows > a.cols, bf16 = a.grad_type == PURO_BF16, f32 = a.u_type == PURO_F32;
             const int64_t us = a.rows > 1 ? a.u_stride : a.cols;
-            in.flags[i] = (bf16 ? kGradBf16 : 0) | (tall ? kTall : 0);
-            if (a.cols % 4 == 0 && aligned(a.grad, bf16 ? 8 : 16) && in.stride[i] % 4 == 0 && aligned(a.momentum, 16))
-                in.flags[i] |= kVectors;
+            to.flags = (bf16 ? kGradBf16 : 0) | (tall ? kTall : 0);
+            if (a.cols % 4 == 0 && aligned(a.momentum, 16)) {
+                to.flags |= kVectors;
+                if (aligned(a.grad, bf16 ? 8 : 16) && to.stride % 4 == 0) to.flags |= kGradVectors;
+            }
             run.out.u[i] = a.u;
             run.out.stride[i] = us;
             run.out.flags[i] = (tall ? kTall : 0) | (f32 ? kOutF32 : 0);
             if (a.cols % (f32 ? 4 : 8) == 0 && us % (f32 ? 4 : 8) == 0 && aligned(a.u, 16)) run.out.flags[i] |= kOutVectors;
-            const int tiles = static_cast<int>(tiles_in(a.rows, a.cols)), each = (tiles + kMaxSlabs - 1) / kMaxSlabs;
+            const int tiles = static_cast<int>(tiles_in(a.rows, a.cols)), each = slab_tiles_of(tiles);
             in.tile0[i + 1] = in.tile0[i] + tiles;
-            in.slab_tiles[i] = each;
+            to.slab_tiles = each;
             in.slab0[i + 1] = in.slab0[i] + (tiles + each - 1) / each;
         }
     e = launch_pdl(muon_update_kernel, dim3(in.slab0[c.count]), dim3(kInThreads), 0, s, in);
