@@ -1,5 +1,7 @@
 """The Muon direction's 64-bit reference against singular values, and what the entry point refuses (no GPU)."""
 import ctypes
+import os
+import subprocess
 
 import pytest
 import torch
@@ -92,6 +94,13 @@ def test_tables_are_checked():
         P.muon_table([(x, None, x)])  # not on CUDA
 
 
-def test_struct_layout():
+def test_struct_layout(tmp_path):
+    """The Python mirror of puro_muon_matrix_t against the C compiler."""
     t = P.puro_muon_matrix_t
-    assert ctypes.sizeof(t) == 72 and t.rows.offset == 24 and t.grad_type.offset == 56 and t.reserved.offset == 64
+    fields = [f for f, _ in t._fields_]
+    src, exe = tmp_path / "probe.c", tmp_path / "probe"
+    src.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "puro_fp8.h"\nint main(void) { printf("%zu", sizeof(puro_muon_matrix_t));\n' +
+                   "".join('printf(" %%zu", offsetof(puro_muon_matrix_t, %s));\n' % f for f in fields) + "return 0; }\n")
+    subprocess.run(["gcc", "-std=c11", "-I", os.path.dirname(P.HEADER_PATH), str(src), "-o", str(exe)], check=True)
+    got = [int(v) for v in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.split()]
+    assert got == [ctypes.sizeof(t)] + [getattr(t, f).offset for f in fields]
