@@ -655,9 +655,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     tc_fence_after_sync();
     cluster_arrive();
     cluster_wait();  // both CTAs' barriers exist
-    pdl_wait();
-    pdl_launch_dependents();
     const uint32_t tmem = sm.tmem_base;
+    // The first unit is worked out, and its maps fetched, before the wait for the kernel
+    // before (the empty asm keeps it there).
+    Walk walk;
+    int u = walk.next(p, pair);
+    Unit w{};
+    if (u >= 0) w = unit_of<BN, kSym>(p, u);
+    asm volatile("" : "+r"(w.cls), "+r"(w.z), "+r"(w.m0), "+r"(w.n0), "+r"(w.kb));
+    auto next = [&] {
+        u = walk.next(p, pair);
+        if (u >= 0) w = unit_of<BN, kSym>(p, u);
+    };
 
     if (warp == 0) {
         // ------------------------------------------------ TMA producer
@@ -665,9 +674,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const uint32_t full0 = mapa_shared(smem_u32(&sm.full[0]), 0);
         uint32_t stage = 0, phase = 0, issued = 0;
         bool ok = true;
-        Walk walk;
-        for (int u = walk.next(p, pair); u >= 0 && ok; u = walk.next(p, pair)) {
-            const Unit w = unit_of<BN, kSym>(p, u);
+        if (lane < 3 + (EPI == kOut ? 0 : 1)) {
+            const MuonMaps &m = p.maps[w.cls];
+            tma_prefetch_desc(lane == 0 ? &m.a : lane == 1 ? &m.b : lane == 2 && p.passes > 1 ? &m.b_lo : lane == 3 ? &m.d : &m.a);
+        }
+        __syncwarp();
+        pdl_wait();
+        pdl_launch_dependents();
+        for (; u >= 0 && ok; next()) {
             const MuonMaps &maps = p.maps[w.cls];
             const int a_row = w.m0 + kBM * rank, b_row = w.n0 + BN / 2 * rank;
             for (int pass = 0; pass < p.passes && ok; ++pass) {
@@ -710,9 +724,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         uint32_t stage = 0, phase = 0;
         int local = 0;
         bool ok = true;
-        Walk walk;
-        for (int u = walk.next(p, pair); u >= 0 && ok; u = walk.next(p, pair), ++local) {
-            const Unit w = unit_of<BN, kSym>(p, u);
+        for (; u >= 0 && ok; next(), ++local) {
             const int buf = local & 1;
             ok = wait_or_abort(sm, &sm.tempty[buf], ((local >> 1) & 1u) ^ 1u, p.wait_ns, p.status, lane);
             const uint32_t d = tmem + static_cast<uint32_t>(BN) * buf;
@@ -762,9 +774,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             ++pieces;
         };
         int local = 0;
-        Walk walk;
-        for (int u = walk.next(p, pair); u >= 0; u = walk.next(p, pair), ++local) {
-            const Unit w = unit_of<BN, kSym>(p, u);
+        pdl_wait();  // (before G is read and anything stored)
+        for (; u >= 0; next(), ++local) {
             const int buf = local & 1;
             const MuonMaps &maps = p.maps[w.cls];
             const int row0 = w.m0 + kBM * rank + 32 * q, rows = p.rows[w.cls], cols = p.cols[w.cls];

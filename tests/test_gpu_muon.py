@@ -134,6 +134,16 @@ def test_groups_are_their_matrices():
         assert mats[i][1] is None or torch.equal(mats[i][1], alone[i][1])
 
 
+def test_narrow_and_wide_tiles_agree():
+    """Alone its products are few tiles of 128 columns, in a group many of 256: the same sums."""
+    g = [M.gradient(1100, c, c).to(DEV) for c in (1100, 2000, 1500, 1300, 1100)]
+    u, alone = ([torch.empty_like(x) for x in g] for _ in range(2))
+    directions([(x, None, y) for x, y in zip(g, u)])
+    for x, y in zip(g, alone):
+        directions([(x, None, y)])
+    assert all(torch.equal(a, b) for a, b in zip(u, alone))
+
+
 @pytest.mark.parametrize("factor", [2.0 ** -120, 2.0 ** -60, 2.0 ** 60, 2.0 ** 110])
 def test_the_size_of_v_does_not_count(factor):
     g = M.gradient(50, 90, 2) * 1024
