@@ -35,6 +35,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <type_traits>
 
@@ -454,18 +455,22 @@ enum Epilogue : int {
 struct MuonMaps {
     CUtensorMap a, b, b_lo, d, d_lo;  // a: box 64 x 128; b: 64 x BN / 2, X_MAJOR 64 x 64; d: 32 x 32 (64-byte swizzle)
 };
-struct MuonPhase {
-    MuonMaps maps[kMaxClasses];
+// The tiles of a product, and who takes them.
+struct Tiles {
+    int bn;
     int classes, units;
     int unit0[kMaxClasses + 1];  // first tile of each class
     int per[kMaxClasses];        // tiles of a matrix
-    int segments;                // of tiles, each dealt to a range of the pairs in turn
-    int from[kMaxSegments], to[kMaxSegments];
-    int16_t pair0[kMaxSegments], pairs[kMaxSegments];
     int tiles_n[kMaxClasses], tiles_m[kMaxClasses];
     int rows[kMaxClasses], cols[kMaxClasses];  // of D
     int kb[kMaxClasses];         // k-blocks of B (of lo as many more)
-    int first[kMaxClasses];      // kOut: the class's first matrix in MuonOut
+    int first[kMaxClasses];      // the class's first matrix
+    int segments;                // of tiles, each dealt to a range of the pairs in turn
+    int from[kMaxSegments], to[kMaxSegments];
+    int16_t pair0[kMaxSegments], pairs[kMaxSegments];
+};
+struct MuonPhase : Tiles {
+    MuonMaps maps[kMaxClasses];
     const uint16_t *g[kMaxClasses];  // kPoly: G of the first matrix
     int64_t g_batch[kMaxClasses];
     int ldg[kMaxClasses];
@@ -483,6 +488,9 @@ struct MuonOut {
     int64_t stride[kMaxMats];
     uint8_t flags[kMaxMats];
 };
+struct NoOut {};
+template <int EPI>
+using OutOf = std::conditional_t<EPI == kOut, MuonOut, NoOut>;  // (launches copy their parameters)
 
 template <int BN>
 struct ProductSmem {
@@ -619,7 +627,7 @@ PURO_DEV void block_to_u(const uint8_t *from, bool f32, bool vectors, void *u, i
 
 template <int BN, bool X_MAJOR, int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-    muon_product_kernel(const __grid_constant__ MuonPhase p, const __grid_constant__ MuonOut out) {
+    muon_product_kernel(const __grid_constant__ MuonPhase p, const __grid_constant__ OutOf<EPI> out) {
     using Smem = ProductSmem<BN>;
     constexpr int kStages = Smem::kStages;
     constexpr bool kSym = EPI == kStore || EPI == kPoly;
@@ -1030,7 +1038,7 @@ struct Dealer {
     double most = 0;
     Dealer(int pairs) { w[0] = {0, pairs, 0}; }
 
-    void deal(MuonPhase *p, int first, int n, double cost) {
+    void deal(Tiles *p, int first, int n, double cost) {
         int u = first;
         const int end = first + n;
         while (u < end) {
@@ -1077,7 +1085,7 @@ struct Dealer {
             }
         }
     }
-    static void segment(MuonPhase *p, int from, int to, int pair0, int pairs) {
+    static void segment(Tiles *p, int from, int to, int pair0, int pairs) {
         const int s = p->segments++;
         p->from[s] = from;
         p->to[s] = to;
@@ -1086,10 +1094,17 @@ struct Dealer {
     }
 };
 
+// (once per device: it costs as much of the host's time as an eighth of a launch)
 template <int BN, bool X_MAJOR, int EPI>
 cudaError_t product_attribute() {
-    return cudaFuncSetAttribute(muon_product_kernel<BN, X_MAJOR, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                static_cast<int>(sizeof(ProductSmem<BN>)));
+    static std::atomic<bool> done[64] = {};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || (dev >= 0 && dev < 64 && done[dev].load(std::memory_order_relaxed))) return e;
+    e = cudaFuncSetAttribute(muon_product_kernel<BN, X_MAJOR, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             static_cast<int>(sizeof(ProductSmem<BN>)));
+    if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev].store(true, std::memory_order_relaxed);
+    return e;
 }
 // Pairs of SMs that run pairs of CTAs.
 cudaError_t resident_pairs(int *pairs) {
@@ -1126,7 +1141,7 @@ cudaError_t resident_pairs(int *pairs) {
 }
 
 template <int BN, bool X_MAJOR, int EPI>
-cudaError_t launch_product(const MuonPhase &p, const MuonOut &out, int pairs, cudaStream_t s) {
+cudaError_t launch_product(const MuonPhase &p, const OutOf<EPI> &out, int pairs, cudaStream_t s) {
     const cudaError_t e = product_attribute<BN, X_MAJOR, EPI>();
     if (e != cudaSuccess) return e;
     return launch_pdl(muon_product_kernel<BN, X_MAJOR, EPI>, dim3(2 * std::min(p.units, pairs)), dim3(kThreads),
@@ -1134,6 +1149,8 @@ cudaError_t launch_product(const MuonPhase &p, const MuonOut &out, int pairs, cu
 }
 
 // The products of a chunk, phase after phase.
+enum Form { kGram, kSquareSym, kSquare, kTimesX, kForms };  // X X^T; m x m, symmetric or not; m x m times X
+enum Buffer { kG, kB0, kT, kB1, kX, kXlo, kXnext, kBuffers, kNone = -1 };  // square ones; X, the first X's lo, the next X
 struct Products {
     const Chunk &c;
     const Scratch &at;
@@ -1142,26 +1159,25 @@ struct Products {
     cudaStream_t s;
     int pairs;  // of SMs
     MuonOut out;
+    Tiles tiles[kForms];
+    // of each buffer: 64 x 128 (A; B of 256 columns), 64 x 64 (B of 128; X), 32 x 32 (D)
+    CUtensorMap rows128[kMaxClasses][kBuffers], rows64[kMaxClasses][kBuffers], block[kMaxClasses][kBuffers];
 
     int64_t ld(int k, bool square) const { return align_up(square ? c.shape[k].m : c.shape[k].n, 8); }
-    uint16_t *x(int b, int k) const { return reinterpret_cast<uint16_t *>(ws + at.x[b][k]); }
-    uint16_t *g(int b, int k) const { return reinterpret_cast<uint16_t *>(ws + at.g[b][k]); }
-    bool map(CUtensorMap *m, uint16_t *base, int k, bool square, int bx, int by, CUtensorMapSwizzle sw) const {
-        const int64_t cols = square ? c.shape[k].m : c.shape[k].n, row = 2 * ld(k, square);
-        return make_batched_map(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, base, cols, c.shape[k].m, c.first[k + 1] - c.first[k], row,
-                                row * c.shape[k].m, bx, by, sw);
-    }
+    uint16_t *buffer(int b, int k) const { return reinterpret_cast<uint16_t *>(ws + (b < kX ? at.g[b][k] : at.x[b - kX][k])); }
 
     // Tiles of 256 x bn, dealt to the pairs; returns what the longest-working pair has
     // to do, in k-blocks of 256 x 256.
-    double plan(MuonPhase *p, int bn, bool sym, bool square, int passes, bool k_is_n) const {
+    double deal(Tiles *p, int form, int bn) const {
+        *p = Tiles{};
+        p->bn = bn;
         Dealer dealer(pairs);
         int order[kMaxClasses], n[kMaxClasses];
         for (int k = 0; k < c.classes; ++k) {
-            const int64_t m = c.shape[k].m, cols = square ? m : c.shape[k].n;
+            const int64_t m = c.shape[k].m, cols = form == kTimesX ? c.shape[k].n : m;
             const int64_t tm = (m + 255) / 256, tn = (cols + bn - 1) / bn;
             int64_t per = tm * tn;
-            if (sym) {
+            if (form == kGram || form == kSquareSym) {
                 per = 0;
                 for (int64_t i = 0; i < tm; ++i) per += tn - 256 / bn * i;
             }
@@ -1174,75 +1190,75 @@ struct Products {
             p->tiles_n[k] = static_cast<int>(tn);
             p->rows[k] = static_cast<int>(m);
             p->cols[k] = static_cast<int>(cols);
-            p->kb[k] = static_cast<int>(((k_is_n ? c.shape[k].n : m) + kBK - 1) / kBK);
+            p->kb[k] = static_cast<int>(((form == kGram ? c.shape[k].n : m) + kBK - 1) / kBK);
             p->first[k] = c.first[k];
         }
         p->classes = c.classes;
         p->unit0[c.classes] = p->units;
         sort_few(order, c.classes, [&](int a, int b) { return p->kb[a] != p->kb[b] ? p->kb[a] > p->kb[b] : a < b; });
-        const double block = bn == 256 ? 1.0 : kNarrowBlock;
+        const double block_cost = bn == 256 ? 1.0 : kNarrowBlock;
         for (int i = 0; i < c.classes; ++i)
-            dealer.deal(p, p->unit0[order[i]], n[order[i]], block * (p->kb[order[i]] * passes + kTileBlocks));
+            dealer.deal(p, p->unit0[order[i]], n[order[i]], block_cost * (p->kb[order[i]] + kTileBlocks));
         return dealer.most;
     }
 
-    // D = A B^T (BOTH_SQUARE, or of X alone: the Gram matrix) or A X.  Operands and
-    // results by their buffers: g(0 .. 3), x(0 .. 2); -1: none.
+    cudaError_t prepare() {
+        for (int form = 0; form < kForms; ++form) {
+            Tiles narrow;
+            if (deal(&narrow, form, 128) < deal(&tiles[form], form, 256)) tiles[form] = narrow;
+        }
+        for (int k = 0; k < c.classes; ++k)
+            for (int b = 0; b < kBuffers; ++b) {
+                const bool square = b < kX;
+                const int64_t cols = square ? c.shape[k].m : c.shape[k].n, row = 2 * ld(k, square);
+                auto map = [&](CUtensorMap *m, int bx, int by, CUtensorMapSwizzle sw) {
+                    return make_batched_map(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, buffer(b, k), cols, c.shape[k].m,
+                                            c.first[k + 1] - c.first[k], row, row * c.shape[k].m, bx, by, sw);
+                };
+                if (!map(&rows128[k][b], 64, 128, CU_TENSOR_MAP_SWIZZLE_128B) || !map(&rows64[k][b], 64, 64, CU_TENSOR_MAP_SWIZZLE_128B) ||
+                    !map(&block[k][b], 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
+                    return cudaErrorInvalidValue;
+            }
+        return cudaSuccess;
+    }
+
+    // D = A B^T or (kTimesX) A X, of buffers.
     struct Product {
-        int a = -1;             // square A; -1: A and B are X's hi
-        int b = -1, b_lo = -1;  // square B, and what is added to it (a second pass over A)
-        int x = 0;              // X
-        bool x_lo = false;      // A X: the first X's lo (buffer 1) as well
-        int d = -1, d_lo = -1;  // square results; -1: the next X, 2 - x
-        int poly = -1;          // kPoly: G
+        Form form;
+        int a, b, b_lo;  // b_lo: what is added to B (a second pass over A)
+        int d, d_lo;     // d_lo: the digits that d loses
         const MuonScale *scale = nullptr;  // of the first X
         double alpha = 0, beta = 0, gamma = 0;
     };
     template <int EPI, bool X_MAJOR>
     cudaError_t run(const Product &q) const {
-        constexpr bool kSym = EPI == kStore || EPI == kPoly, kSquare = kSym || !X_MAJOR;
-        const bool gram = q.a < 0;
-        const int passes = (X_MAJOR ? q.x_lo : q.b_lo >= 0) ? 2 : 1;
-        MuonPhase wide{}, narrow{};
-        const double tw = plan(&wide, 256, kSym, kSquare, passes, gram), tn = plan(&narrow, 128, kSym, kSquare, passes, gram);
-        const int bn = tw <= tn ? 256 : 128;
-        MuonPhase &p = bn == 256 ? wide : narrow;
-        const auto kSw = CU_TENSOR_MAP_SWIZZLE_128B, kSwD = CU_TENSOR_MAP_SWIZZLE_64B;
+        MuonPhase p;
+        static_cast<Tiles &>(p) = tiles[q.form];
         for (int k = 0; k < c.classes; ++k) {
-            MuonMaps &m = p.maps[k];
-            bool ok = gram ? map(&m.a, x(q.x, k), k, false, 64, 128, kSw) : map(&m.a, g(q.a, k), k, true, 64, 128, kSw);
-            if (X_MAJOR) {
-                ok = ok && map(&m.b, x(q.x, k), k, false, 64, 64, kSw);
-                if (q.x_lo) ok = ok && map(&m.b_lo, x(1, k), k, false, 64, 64, kSw);
-            } else {
-                ok = ok && (gram ? map(&m.b, x(q.x, k), k, false, 64, bn / 2, kSw) : map(&m.b, g(q.b, k), k, true, 64, bn / 2, kSw));
-                if (q.b_lo >= 0) ok = ok && map(&m.b_lo, g(q.b_lo, k), k, true, 64, bn / 2, kSw);
-            }
-            if (kSquare) {
-                ok = ok && map(&m.d, g(q.d, k), k, true, 32, 32, kSwD);
-                if (q.d_lo >= 0) ok = ok && map(&m.d_lo, g(q.d_lo, k), k, true, 32, 32, kSwD);
-            } else if (EPI == kNext) {
-                ok = ok && map(&m.d, x(2 - q.x, k), k, false, 32, 32, kSwD);
-            }
-            if (!ok) return cudaErrorInvalidValue;
-            if (EPI == kPoly) {
-                p.g[k] = g(q.poly, k);
-                p.ldg[k] = static_cast<int>(ld(k, true));
-                p.g_batch[k] = c.shape[k].m * ld(k, true);
-            }
+            const CUtensorMap *b = X_MAJOR || p.bn == 128 ? rows64[k] : rows128[k];
+            p.maps[k].a = rows128[k][q.a];
+            p.maps[k].b = b[q.b];
+            if (q.b_lo != kNone) p.maps[k].b_lo = b[q.b_lo];
+            if (q.d != kNone) p.maps[k].d = block[k][q.d];
+            if (q.d_lo != kNone) p.maps[k].d_lo = block[k][q.d_lo];
+            p.g[k] = buffer(kG, k);
+            p.ldg[k] = static_cast<int>(ld(k, true));
+            p.g_batch[k] = c.shape[k].m * ld(k, true);
         }
         p.alpha = static_cast<float>(q.alpha);
         p.beta = static_cast<float>(q.beta);
         p.gamma = static_cast<float>(q.gamma);
-        p.passes = passes;
-        p.store_lo = q.d_lo >= 0;
+        p.passes = q.b_lo != kNone ? 2 : 1;
+        p.store_lo = q.d_lo != kNone;
         p.scale = q.scale;
-        p.squared = gram;
+        p.squared = q.form == kGram;
         p.status = status;
         p.wait_ns = wait_timeout_ns();
         // kind::f16, FP32 accumulators, FP16 operands; B N-major for X; N, M = 256 (a pair MMA)
-        p.idesc = (1u << 4) | (X_MAJOR ? 1u << 16 : 0u) | (static_cast<uint32_t>(bn >> 3) << 17) | ((256u >> 4) << 24);
-        return bn == 256 ? launch_product<256, X_MAJOR, EPI>(p, out, pairs, s) : launch_product<128, X_MAJOR, EPI>(p, out, pairs, s);
+        p.idesc = (1u << 4) | (X_MAJOR ? 1u << 16 : 0u) | (static_cast<uint32_t>(p.bn >> 3) << 17) | ((256u >> 4) << 24);
+        OutOf<EPI> to{};
+        if constexpr (EPI == kOut) to = out;
+        return p.bn == 256 ? launch_product<256, X_MAJOR, EPI>(p, to, pairs, s) : launch_product<128, X_MAJOR, EPI>(p, to, pairs, s);
     }
 };
 
@@ -1267,7 +1283,9 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
     int pairs = 0;
     cudaError_t e = resident_pairs(&pairs);
     if (e != cudaSuccess) return e;
-    Products run{c, at, ws, status, s, pairs, MuonOut{}};
+    Products run{c, at, ws, status, s, pairs};
+    e = run.prepare();
+    if (e != cudaSuccess) return e;
     // the update, its norm, X
     MuonIn in{};
     in.count = c.count;
@@ -1287,8 +1305,8 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
             to.rows = static_cast<int>(a.rows);
             to.cols = static_cast<int>(a.cols);
             to.ldx = static_cast<int>(run.ld(k, false));
-            to.hi = run.x(0, k) + z;
-            to.lo = run.x(1, k) + z;
+            to.hi = run.buffer(kX, k) + z;
+            to.lo = run.buffer(kXlo, k) + z;
             const bool tall = a.rows > a.cols, bf16 = a.grad_type == PURO_BF16, f32 = a.u_type == PURO_F32;
             const int64_t us = a.rows > 1 ? a.u_stride : a.cols;
             to.flags = (bf16 ? kGradBf16 : 0) | (tall ? kTall : 0);
@@ -1309,75 +1327,43 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
     if (e == cudaSuccess) e = launch_pdl(muon_norm_kernel, dim3(c.count), dim3(kMaxSlabs), 0, s, in);
     if (e == cudaSuccess) e = launch_pdl(muon_redo_kernel, dim3(std::min(in.tile0[c.count], 6 * pairs)), dim3(kInThreads), 0, s, in);
     // the steps, two at a time
-    using Product = Products::Product;
-    enum { G = 0, B0 = 1, T = 2, B1 = 3, Glo = B1 };  // (G's lo is read before B1 is written)
+    constexpr int kGlo = kB1;  // (G's lo is read before B1 is written)
     double most = 1.0, sx = 1.0;  // (the first X's power of two is in its MuonScale)
-    Product q;
-    auto scaled = [&](double alpha, double beta = 0, double gamma = 0) {
-        q.alpha = alpha;
-        q.beta = beta;
-        q.gamma = gamma;
-        return q;
-    };
-    int x = 0;  // X's buffer
-    bool first = true;
+    int x = kX;
     for (int i = 0; i < n_steps && e == cudaSuccess;) {
-        const bool pair = i + 1 < n_steps, glo = pair && i > 0;
+        const bool pair = i + 1 < n_steps, first = i == 0, glo = pair && !first;
+        const MuonScale *scale = first ? in.scale : nullptr;
         const Step &s0 = steps[i];
         const double sg = pow2_for(most * most), sb = pow2_for(s0.most_p);
-        q = Product{};  // G = X X^T
-        q.x = x;
-        q.d = G;
-        q.d_lo = glo ? Glo : -1;
-        q.scale = first ? in.scale : nullptr;
-        e = run.run<kStore, false>(scaled(sg / (sx * sx)));
-        q = Product{};  // B0 = a I + b G + c G^2
-        q.a = q.b = q.poly = G;
-        q.d = B0;
-        if (e == cudaSuccess) e = run.run<kPoly, false>(scaled(s0.c * sb / (sg * sg), s0.b * sb / sg, s0.a * sb));
+        // G = X X^T;  B0 = a I + b G + c G^2
+        e = run.run<kStore, false>({kGram, x, x, kNone, kG, glo ? kGlo : kNone, scale, sg / (sx * sx)});
+        if (e == cudaSuccess)
+            e = run.run<kPoly, false>({kSquareSym, kG, kG, kNone, kB0, kNone, nullptr, s0.c * sb / (sg * sg), s0.b * sb / sg, s0.a * sb});
         double sp = sb, out = s0.most_out * kMargin;
-        int product = B0;
+        int product = kB0;
         if (pair) {
             const Step &s1 = steps[i + 1];
             const double st = pow2_for(most * most * s0.most_p), sg1 = pow2_for(out * out), sb1 = pow2_for(s1.most_p);
-            q = Product{};  // T^T = B0 G
-            q.a = B0;
-            q.b = G;
-            q.b_lo = glo ? Glo : -1;
-            q.d = T;
-            if (e == cudaSuccess) e = run.run<kNext, false>(scaled(st / (sg * sb)));
-            q = Product{};  // G = B0 T
-            q.a = B0;
-            q.b = T;
-            q.d = G;
-            if (e == cudaSuccess) e = run.run<kStore, false>(scaled(sg1 / (st * sb)));
-            q = Product{};  // B1
-            q.a = q.b = q.poly = G;
-            q.d = B1;
-            if (e == cudaSuccess) e = run.run<kPoly, false>(scaled(s1.c * sb1 / (sg1 * sg1), s1.b * sb1 / sg1, s1.a * sb1));
+            // T^T = B0 G;  G = B0 T;  B1;  T = B1 B0
+            if (e == cudaSuccess) e = run.run<kNext, false>({kSquare, kB0, kG, glo ? kGlo : kNone, kT, kNone, nullptr, st / (sg * sb)});
+            if (e == cudaSuccess) e = run.run<kStore, false>({kSquareSym, kB0, kT, kNone, kG, kNone, nullptr, sg1 / (st * sb)});
+            if (e == cudaSuccess)
+                e = run.run<kPoly, false>({kSquareSym, kG, kG, kNone, kB1, kNone, nullptr, s1.c * sb1 / (sg1 * sg1), s1.b * sb1 / sg1, s1.a * sb1});
             sp = pow2_for(s0.most_p * s1.most_p);
-            q = Product{};  // B1 B0
-            q.a = B1;
-            q.b = B0;
-            q.d = T;
-            if (e == cudaSuccess) e = run.run<kNext, false>(scaled(sp / (sb1 * sb)));
-            product = T;
+            if (e == cudaSuccess) e = run.run<kNext, false>({kSquare, kB1, kB0, kNone, kT, kNone, nullptr, sp / (sb1 * sb)});
+            product = kT;
             out = s1.most_out * kMargin;
         }
         i += pair ? 2 : 1;
-        q = Product{};
-        q.a = product;
-        q.x = x;
-        q.x_lo = in.store_lo && first;
-        q.scale = first ? in.scale : nullptr;
-        first = false;
+        const int lo = first && in.store_lo ? kXlo : kNone;
         if (i == n_steps) {
-            if (e == cudaSuccess) e = run.run<kOut, true>(scaled(1.0 / (sp * sx)));
+            if (e == cudaSuccess) e = run.run<kOut, true>({kTimesX, product, x, lo, kNone, kNone, scale, 1.0 / (sp * sx)});
         } else {
             const double next = pow2_for(out);
-            if (e == cudaSuccess) e = run.run<kNext, true>(scaled(next / (sp * sx)));
+            const int y = x == kX ? kXnext : kX;
+            if (e == cudaSuccess) e = run.run<kNext, true>({kTimesX, product, x, lo, y, kNone, scale, next / (sp * sx)});
             sx = next;
-            x = 2 - x;
+            x = y;
         }
         most = out;
     }
