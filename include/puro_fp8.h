@@ -648,13 +648,13 @@ puro_status_t puro_muonh_step_grouped(const puro_muonh_matrix_t *mats, int32_t c
  * same directions, for X does not depend on V's size.
  *
  * V is FP32 and its norm FP64.  The products are FP16 with FP32 accumulation, X and
- * their other results scaled by powers of two; X is kept in two FP16 numbers (22
- * digits) ahead of each pair of steps.  u is within about 2^-9 of itself in the
- * 2-norm (5 of Muon's steps, momenta of low rank with noise a third as large; what
- * is in V's directions of small singular values is less exact, and BF16 products
- * would be off eight times as much), whichever type it is stored in.
- * The sums' order is fixed by the shapes, so results are deterministic; where a
- * matrix's tiles are split depends on what it is grouped with, its sums do not.
+ * their other results scaled by powers of two, the first X in two FP16 numbers (22
+ * digits).  u is off by 1.0 to 1.6 10^-3 of its 2-norm, whichever type it is stored in
+ * (five of Muon's steps on momenta of rank 16 with noise half as large; what lies in
+ * V's directions of small singular values is less exact: 7 10^-3 where the noise is
+ * 1/130 of the signal; products in BF16 would be off eight times as much).
+ * Results are deterministic, and a matrix's u does not depend on what it is grouped
+ * with.
  *   mats: host array of `count` descriptors (read during the call only).  grad and u
  *     are views with rows grad_stride and u_stride elements apart (u_stride >= cols);
  *     aligned to their elements, faster at 16 bytes with strides and cols of multiples
@@ -666,12 +666,12 @@ puro_status_t puro_muonh_step_grouped(const puro_muonh_matrix_t *mats, int32_t c
  *     c t^2| could, t a squared singular value.  Muon's are five times 3.4445, -4.7750,
  *     2.0315.
  *   workspace: 256-byte aligned, puro_muon_direction_workspace_size(mats, count)
- *     bytes (0 for a table with a malformed descriptor): about 8 (m n + m^2) bytes for
- *     each matrix of m x n, m <= n.
+ *     bytes (0 for a table with a malformed descriptor): about 6 m n + 8 m^2 bytes for
+ *     each matrix of m x n, m <= n, of the largest 128 in a row.
  * V = 0 gives u = 0; a V whose norm is not finite gives NaN in all of u.  Matrices are
- * taken 128 at a time, of up to 8 shapes: three kernels and then seven for each pair
- * of steps (three for a last odd one).  Every descriptor is checked before anything is
- * enqueued.
+ * taken in order, up to 128 of up to 8 shapes at a time: three kernels, and then seven
+ * for each pair of steps (three for a last odd one).  Every descriptor is checked
+ * before anything is enqueued.
  */
 typedef enum { PURO_BF16 = 0, PURO_F32 = 1 } puro_float_t;
 typedef struct {

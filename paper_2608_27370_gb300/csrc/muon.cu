@@ -15,22 +15,27 @@
 //     G1 = B0 G B0 (the next step's G, for B0 and G commute),
 //     B1 = a' I + b' G1 + c' G1^2,  X <- (B1 B0) X,
 // so that products of m x m take the place of the second step's two of m x n: for n =
-// 6 m a pair takes 19 of m x m x m for 33 without lo, 38 with it in both steps.  Results
-// that are symmetric (G, B0, G1, B1) are computed on and above the diagonal and
-// stored twice.
+// 6 m a pair of steps takes 12.5 m^3 products and sums for 19.  G, B0, G1 and B1 are
+// symmetric: computed on and above the diagonal and stored twice.
 //
 // Where digits are lost.  A rounding of X adds noise of full rank, and the steps
 // blow small singular values up (3.4 times each, by Muon's coefficients), the noise
-// with them; a rounding of B only turns X's rows a little into one another.  So X is
-// kept as two FP16 numbers, x = hi + lo, 22 digits, where a pair of steps follows:
-// B1 B0 multiplies both (lo after hi, into the same accumulator), and G takes hi
-// alone.  A rounding of G is harmless in B0 but blown up in G1, so behind the first
-// pair G, too, is hi + lo for G1.  And G1 is B0 (B0 G)^T, symmetric whatever B0's
-// roundings: (B0 G) B0 with a mirrored or transposed factor doubles the error, for
-// rounded B0 and G no longer commute.  The model of all roundings in tests/_muon.py
-// gives for momenta of low rank with noise half as large, of 48 x 80 to 1000 x 4000,
-// errors of 1.1 to 1.4 10^-3 of u's 2-norm; without X's lo 3 to 4, without G's up to
-// 2, with BF16 operands 30.
+// with them, the first rounding the most; a rounding of B only turns X's rows a little
+// into one another.  So the first X is two FP16 numbers, x = hi + lo, 22 digits: B1 B0
+// multiplies both (lo after hi, into the same accumulator), and G takes hi alone.  A
+// rounding of G is harmless in B0 but blown up in G1, so behind the first pair G, too, is
+// hi + lo for G1.  And G1 is B0 (B0 G)^T, symmetric whatever B0's roundings: as (B0 G) B0
+// with a mirrored or transposed factor it doubles the error, for rounded B0 and G no
+// longer commute.  u is then off by 1.0 to 1.6 10^-3 of its 2-norm for momenta of rank 16
+// and noise half as large, 48 x 80 to 2048 x 6144 (G without lo: up to 2.0; every BF16
+// operand: eight times as much).  Where the noise is 1/130 of a signal of rank 16, by
+// 7 10^-3 (X without lo: 20; lo of the second pair's X, too: 2, for a fifth of the time
+// more).
+//
+// Measured and not kept: all products in one cooperative launch with a barrier of all
+// blocks between them (one [1536, 1536] 205 us for 178, a layer of Qwen2-1.5B 1162 for
+// 1142), and as tickets that pairs draw, each tile waiting for its matrix's product before
+// (207 for 177, 965 for 990); two CTAs of narrow tiles an SM (191 for 177).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -110,7 +115,7 @@ PURO_DEV int in_col(uint8_t flags, int lane, int k) { return flags & kVectors ? 
 // The values of V of a lane's columns c0 ... in rows r0 + warp, r0 + warp + kInWarps, ...,
 // zero outside the matrix.  UPDATE: the momentum takes the gradient first and is
 // stored; else it has.  All loads are issued ahead of the first use (with each row's
-// behind the row before's stores a layer's update took 114 us instead of XX).
+// behind the row before's stores 114 us for 82 over a layer's matrices).
 template <bool UPDATE, bool VEC, bool GRAD_VEC, bool BF16>
 PURO_DEV void tile_of(const MuonIn &p, int m, int r0, int c0, float (&v)[kInPasses][4]) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rows = p.mat[m].rows, cols = p.mat[m].cols;
@@ -1024,7 +1029,7 @@ bool plan_step(const double *abc, double most, Step *s) {
 constexpr double kNarrowBlock = 0.65, kTileBlocks = 4.0;
 constexpr double kMargin = 1.0 + 1.0 / 64;  // of a bound, for what roundings add
 // The power of two that puts values up to `most` within FP16, with half of it to spare.
-double pow2_for(double most) { return std::ldexp(1.0, most > 0 ? std::min(14, std::ilogb(32768.0 / (most * kMargin))) : 14); }
+double pow2_for(double most) { return std::ldexp(1.0, most > 0 ? std::min(100, std::ilogb(32768.0 / (most * kMargin))) : 14); }
 
 // Deals n units of a cost to the pairs, least loaded first: windows of neighbouring
 // pairs with the same load.

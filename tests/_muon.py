@@ -37,7 +37,7 @@ def _half(x, scale):
 
 
 def _scale(most):
-    return 2.0 ** 14 if most <= 0 else 2.0 ** min(14, math.floor(math.log2(32768 / (most * (1 + 1 / 64)))))
+    return 2.0 ** 14 if most <= 0 else 2.0 ** min(100, math.floor(math.log2(32768 / (most * (1 + 1 / 64)))))
 
 
 def model(v, steps=STEPS):

@@ -69,7 +69,7 @@ def test_numbers_of_steps(n):
     check(u, g, F32, steps)
 
 
-@pytest.mark.parametrize("steps", [((1.5, -0.5, 0.0),) * 8, ((4.0, -6.0, 2.7), (3.0, -4.0, 1.8), (1.875, -1.25, 0.375)), ((0.0, 0.0, 0.0),), ((2.0, 0.0, 0.0),),
+@pytest.mark.parametrize("steps", [((1.5, -0.5, 0.0),) * 8, ((4.0, -6.0, 2.7), (3.0, -4.0, 1.8), (1.875, -1.25, 0.375)), ((0.0, 0.0, 0.0),), ((2.0, 0.0, 0.0),), ((0.25, 0.0, 0.0),) * 20,
                                    ((15 / 8, -10 / 8, 3 / 8),) * 5])
 def test_other_coefficients(steps):
     g = M.gradient(70, 110, 5, "noise")
