@@ -26,7 +26,7 @@
 // rounding of G is harmless in B0 but blown up in G1, so behind the first pair G, too, is
 // hi + lo for G1.  And G1 is B0 (B0 G)^T, symmetric whatever B0's roundings: as (B0 G) B0
 // with a mirrored or transposed factor it doubles the error, for rounded B0 and G no
-// longer commute.  u is then off by 1.0 to 1.6 10^-3 of its 2-norm for momenta of rank 16
+// longer commute.  u is then off by 1.0 to 1.9 10^-3 of its 2-norm for momenta of rank 16
 // and noise half as large, 48 x 80 to 2048 x 6144 (G without lo: up to 2.0; every BF16
 // operand: eight times as much).  Where the noise is 1/130 of a signal of rank 16, by
 // 7 10^-3 (X without lo: 20; lo of the second pair's X, too: 2, for a fifth of the time
@@ -458,7 +458,7 @@ enum Epilogue : int {
 };
 
 struct MuonMaps {
-    CUtensorMap a, b, b_lo, d, d_lo;  // a: box 64 x 128; b: 64 x BN / 2, X_MAJOR 64 x 64; d: 32 x 32 (64-byte swizzle)
+    CUtensorMap a, a_lo, b, b_lo, d, d_lo;  // a: box 64 x 128; b: 64 x BN / 2, X_MAJOR 64 x 64; d: 32 x 32 (64-byte swizzle)
 };
 // The tiles of a product, and who takes them.
 struct Tiles {
@@ -476,14 +476,14 @@ struct Tiles {
 };
 struct MuonPhase : Tiles {
     MuonMaps maps[kMaxClasses];
-    const uint16_t *g[kMaxClasses];  // kPoly: G of the first matrix
+    int passes[kMaxClasses];     // over A and B: 2, B's lo after its hi; 3, then A's lo with B's hi
+    bool store_lo[kMaxClasses];
+    const uint16_t *g[kMaxClasses], *g_lo[kMaxClasses];  // kPoly: G of the first matrix, and its lo or null
     int64_t g_batch[kMaxClasses];
     int ldg[kMaxClasses];
     float alpha, beta, gamma;
     const MuonScale *scale;      // of the first X, or null: alpha times r, of X X^T r^2
     bool squared;
-    int passes;                  // 2: B's lo after its hi
-    bool store_lo;
     uint32_t idesc;
     int32_t *status;
     uint64_t wait_ns;
@@ -689,7 +689,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         bool ok = true;
         if (lane < 3 + (EPI == kOut ? 0 : 1)) {
             const MuonMaps &m = p.maps[w.cls];
-            tma_prefetch_desc(lane == 0 ? &m.a : lane == 1 ? &m.b : lane == 2 && p.passes > 1 ? &m.b_lo : lane == 3 ? &m.d : &m.a);
+            tma_prefetch_desc(lane == 0 ? &m.a : lane == 1 ? &m.b : lane == 2 && p.passes[w.cls] > 1 ? &m.b_lo : lane == 3 ? &m.d : &m.a);
         }
         __syncwarp();
         pdl_wait();
@@ -697,14 +697,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         for (; u >= 0 && ok; next()) {
             const MuonMaps &maps = p.maps[w.cls];
             const int a_row = w.m0 + kBM * rank, b_row = w.n0 + BN / 2 * rank;
-            for (int pass = 0; pass < p.passes && ok; ++pass) {
-                const CUtensorMap *mb = pass ? &maps.b_lo : &maps.b;
+            for (int pass = 0; pass < p.passes[w.cls] && ok; ++pass) {
+                const CUtensorMap *ma = pass == 2 ? &maps.a_lo : &maps.a, *mb = pass == 1 ? &maps.b_lo : &maps.b;
                 for (int kb = 0; kb < w.kb; ++kb) {
                     ok = wait_or_abort(sm, &sm.empty[stage], phase ^ 1u, p.wait_ns, p.status, lane);
                     if (!ok) break;
                     const uint32_t bar = full0 + 8u * stage;
                     if (rank == 0 && e) mbar_arrive_expect_tx(&sm.full[stage], 2u * kStageBytes);
-                    tma_load_3d_pair_e(e, sm.a[stage], &maps.a, bar, kb * kBK, a_row, w.z);
+                    tma_load_3d_pair_e(e, sm.a[stage], ma, bar, kb * kBK, a_row, w.z);
                     if constexpr (X_MAJOR) {
 #pragma unroll
                         for (int i = 0; i < BN / 128; ++i)
@@ -741,7 +741,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const int buf = local & 1;
             ok = wait_or_abort(sm, &sm.tempty[buf], ((local >> 1) & 1u) ^ 1u, p.wait_ns, p.status, lane);
             const uint32_t d = tmem + static_cast<uint32_t>(BN) * buf;
-            const int kbs = w.kb * p.passes;
+            const int kbs = w.kb * p.passes[w.cls];
             for (int kb = 0; kb < kbs && ok; ++kb) {
                 ok = wait_or_abort(sm, &sm.full[stage], phase, p.wait_ns, p.status, lane);
                 if (!ok) break;
@@ -798,16 +798,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 alpha *= p.squared ? x * x : x;
             }
             uint4 g[4];
-            auto load_g = [&](int col) {  // the lane's row of G (kPoly), ahead of its use
+            auto load_g = [&](const uint16_t *of, int col) {  // the lane's row of G (kPoly), ahead of its use
                 const int row = row0 + lane, ldg = p.ldg[w.cls];
-                const uint4 *from = reinterpret_cast<const uint4 *>(p.g[w.cls] + w.z * p.g_batch[w.cls] + static_cast<int64_t>(row) * ldg + col);
+                const uint4 *from = reinterpret_cast<const uint4 *>(of + w.z * p.g_batch[w.cls] + static_cast<int64_t>(row) * ldg + col);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     g[k] = make_uint4(0u, 0u, 0u, 0u);
                     if (row < rows && col + 8 * k < ldg) g[k] = __ldg(from + k);
                 }
             };
-            if constexpr (EPI == kPoly) load_g(w.n0 + kWarpCols * half);
+            if constexpr (EPI == kPoly) load_g(p.g[w.cls], w.n0 + kWarpCols * half);
             if (!wait_or_abort(sm, &sm.tfull[buf], (local >> 1) & 1u, p.wait_ns, p.status, lane)) break;
             tc_fence_after_sync();
             const uint32_t acc = tmem + (static_cast<uint32_t>(32 * q) << 16) + static_cast<uint32_t>(BN * buf + kWarpCols * half);
@@ -827,17 +827,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int k = 0; k < 32; ++k) v[k] = alpha * __uint_as_float(r[k]);
                 if constexpr (EPI == kPoly) {
+                    auto add_g = [&] {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const uint32_t xs[4] = {g[k].x, g[k].y, g[k].z, g[k].w};
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t xs[4] = {g[k].x, g[k].y, g[k].z, g[k].w};
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&xs[j]));
-                            v[8 * k + 2 * j] = fmaf(p.beta, f.x, v[8 * k + 2 * j]);
-                            v[8 * k + 2 * j + 1] = fmaf(p.beta, f.y, v[8 * k + 2 * j + 1]);
+                            for (int j = 0; j < 4; ++j) {
+                                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&xs[j]));
+                                v[8 * k + 2 * j] = fmaf(p.beta, f.x, v[8 * k + 2 * j]);
+                                v[8 * k + 2 * j + 1] = fmaf(p.beta, f.y, v[8 * k + 2 * j + 1]);
+                            }
                         }
+                    };
+                    add_g();
+                    if (p.g_lo[w.cls]) {
+                        load_g(p.g_lo[w.cls], col);
+                        add_g();
                     }
-                    if (i + 1 < kWarpCols / 32) load_g(col + 32);
+                    if (i + 1 < kWarpCols / 32) load_g(p.g[w.cls], col + 32);
                     if (col <= row0 + 31 && row0 <= col + 31) {
 #pragma unroll
                         for (int k = 0; k < 32; ++k)
@@ -873,7 +880,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     for (int k = 0; k < 16; ++k) h[k] = half2_bits(v[2 * k], v[2 * k + 1]);
                     store(&maps.d, h, false, col, row0, w.z);
                     if (w.mirror) store(&maps.d, h, true, row0, col, w.z);
-                    if (p.store_lo) {
+                    if (p.store_lo[w.cls]) {
 #pragma unroll
                         for (int k = 0; k < 16; ++k) {
                             const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h[k]));
@@ -961,11 +968,24 @@ int take_chunk(const puro_muon_matrix_t *mats, int at, int count, Chunk *c) {
 
 constexpr int64_t kAlign = 256;
 
+enum Form { kGram, kSquareSym, kSquare, kTimesX, kForms };  // X X^T; m x m, symmetric or not; m x m times X
+// Square ones; X, its lo, the next X; the others' lo where a class keeps all (is_precise).
+enum Buffer { kG, kB0, kT, kB1, kX, kXlo, kXnext, kXnextLo, kGlo, kB0lo, kTlo, kB1lo, kBuffers, kNone = -1 };
+bool is_square(int b) { return b < kX || b >= kGlo; }
+int lo_of(int b) { return b == kX ? kXlo : b == kXnext ? kXnextLo : b + kGlo; }
+// Matrices of few rows keep all digits: every result of a product is hi + lo, every
+// product of two has three passes (hi hi, hi lo, lo hi).  A few rows do not average
+// roundings out: u of 4 to 16 was off by up to 6.5 10^-3 of itself, of 17 to 32 by 2.9,
+// of more by at most 1.9; with them it is 0.4.  They are no gift (48 x 80: 85.7 us a call
+// with passes and lo's, 70.5 without), hence 32.  The Gram matrix of longer rows takes
+// one pass: it averages over them.
+constexpr int64_t kPrecise = 32, kPreciseGram = 512;
+bool is_precise(int64_t m) { return m <= kPrecise; }
+
 // Scratch of a chunk.
 struct Scratch {
     int64_t bytes = 0;
-    int64_t x[3][kMaxClasses];  // offsets: X, the first X's lo, the next X
-    int64_t g[4][kMaxClasses];  // G, B0, T (then B1 B0), G's lo (then B1)
+    int64_t buffer[kBuffers][kMaxClasses];  // offsets; -1: none
     int64_t partial = 0, scale = 0;
 };
 // Tiles of a slab: one where that leaves each SM a block or so, else as many as make
@@ -986,8 +1006,10 @@ Scratch scratch_of(const puro_muon_matrix_t *mats, const Chunk &c) {
     s.scale = take(static_cast<int64_t>(sizeof(MuonScale)) * c.count);
     for (int k = 0; k < c.classes; ++k) {
         const int64_t n = c.first[k + 1] - c.first[k];
-        for (int b = 0; b < 3; ++b) s.x[b][k] = take(n * c.shape[k].m * align_up(c.shape[k].n, 8) * 2);
-        for (int b = 0; b < 4; ++b) s.g[b][k] = take(n * c.shape[k].m * align_up(c.shape[k].m, 8) * 2);
+        for (int b = 0; b < kBuffers; ++b) {
+            const bool there = b <= kXnext || is_precise(c.shape[k].m);
+            s.buffer[b][k] = there ? take(n * c.shape[k].m * align_up(is_square(b) ? c.shape[k].m : c.shape[k].n, 8) * 2) : -1;
+        }
     }
     return s;
 }
@@ -1154,8 +1176,6 @@ cudaError_t launch_product(const MuonPhase &p, const OutOf<EPI> &out, int pairs,
 }
 
 // The products of a chunk, phase after phase.
-enum Form { kGram, kSquareSym, kSquare, kTimesX, kForms };  // X X^T; m x m, symmetric or not; m x m times X
-enum Buffer { kG, kB0, kT, kB1, kX, kXlo, kXnext, kBuffers, kNone = -1 };  // square ones; X, the first X's lo, the next X
 struct Products {
     const Chunk &c;
     const Scratch &at;
@@ -1169,7 +1189,8 @@ struct Products {
     CUtensorMap rows128[kMaxClasses][kBuffers], rows64[kMaxClasses][kBuffers], block[kMaxClasses][kBuffers];
 
     int64_t ld(int k, bool square) const { return align_up(square ? c.shape[k].m : c.shape[k].n, 8); }
-    uint16_t *buffer(int b, int k) const { return reinterpret_cast<uint16_t *>(ws + (b < kX ? at.g[b][k] : at.x[b - kX][k])); }
+    uint16_t *buffer(int b, int k) const { return reinterpret_cast<uint16_t *>(ws + at.buffer[b][k]); }
+    bool precise(int k) const { return is_precise(c.shape[k].m); }
 
     // Tiles of 256 x bn, dealt to the pairs; returns what the longest-working pair has
     // to do, in k-blocks of 256 x 256.
@@ -1203,7 +1224,8 @@ struct Products {
         sort_few(order, c.classes, [&](int a, int b) { return p->kb[a] != p->kb[b] ? p->kb[a] > p->kb[b] : a < b; });
         const double block_cost = bn == 256 ? 1.0 : kNarrowBlock;
         for (int i = 0; i < c.classes; ++i)
-            dealer.deal(p, p->unit0[order[i]], n[order[i]], block_cost * (p->kb[order[i]] + kTileBlocks));
+            dealer.deal(p, p->unit0[order[i]], n[order[i]],
+                        block_cost * (p->kb[order[i]] * (precise(order[i]) ? 3 : 1) + kTileBlocks));
         return dealer.most;
     }
 
@@ -1214,7 +1236,8 @@ struct Products {
         }
         for (int k = 0; k < c.classes; ++k)
             for (int b = 0; b < kBuffers; ++b) {
-                const bool square = b < kX;
+                if (at.buffer[b][k] < 0) continue;
+                const bool square = is_square(b);
                 const int64_t cols = square ? c.shape[k].m : c.shape[k].n, row = 2 * ld(k, square);
                 auto map = [&](CUtensorMap *m, int bx, int by, CUtensorMapSwizzle sw) {
                     return make_batched_map(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, buffer(b, k), cols, c.shape[k].m,
@@ -1230,8 +1253,10 @@ struct Products {
     // D = A B^T or (kTimesX) A X, of buffers.
     struct Product {
         Form form;
-        int a, b, b_lo;  // b_lo: what is added to B (a second pass over A)
-        int d, d_lo;     // d_lo: the digits that d loses
+        int a, b;
+        bool b_lo;  // B's lo is added (a second pass over A); a precise class has all products of hi and lo but lo's with lo
+        int d;
+        bool d_lo;  // the digits that D loses are kept as well; in a precise class they all are
         const MuonScale *scale = nullptr;  // of the first X
         double alpha = 0, beta = 0, gamma = 0;
     };
@@ -1241,20 +1266,25 @@ struct Products {
         static_cast<Tiles &>(p) = tiles[q.form];
         for (int k = 0; k < c.classes; ++k) {
             const CUtensorMap *b = X_MAJOR || p.bn == 128 ? rows64[k] : rows128[k];
+            const bool all = precise(k);
+            // elsewhere G's lo is in B1's place, and read before that is written
+            auto lo = [&](int buf) { return !all && buf == kG ? static_cast<int>(kB1) : lo_of(buf); };
+            p.passes[k] = all ? (q.form == kGram && c.shape[k].n > kPreciseGram ? 1 : 3) : q.b_lo ? 2 : 1;
+            p.store_lo[k] = (all || q.d_lo) && q.d != kNone;
             p.maps[k].a = rows128[k][q.a];
             p.maps[k].b = b[q.b];
-            if (q.b_lo != kNone) p.maps[k].b_lo = b[q.b_lo];
+            if (p.passes[k] > 1) p.maps[k].b_lo = b[lo(q.b)];
+            if (p.passes[k] > 2) p.maps[k].a_lo = rows128[k][lo(q.a)];
             if (q.d != kNone) p.maps[k].d = block[k][q.d];
-            if (q.d_lo != kNone) p.maps[k].d_lo = block[k][q.d_lo];
+            if (p.store_lo[k]) p.maps[k].d_lo = block[k][lo(q.d)];
             p.g[k] = buffer(kG, k);
+            p.g_lo[k] = all ? buffer(kGlo, k) : nullptr;
             p.ldg[k] = static_cast<int>(ld(k, true));
             p.g_batch[k] = c.shape[k].m * ld(k, true);
         }
         p.alpha = static_cast<float>(q.alpha);
         p.beta = static_cast<float>(q.beta);
         p.gamma = static_cast<float>(q.gamma);
-        p.passes = q.b_lo != kNone ? 2 : 1;
-        p.store_lo = q.d_lo != kNone;
         p.scale = q.scale;
         p.squared = q.form == kGram;
         p.status = status;
@@ -1297,6 +1327,7 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
     in.mu = static_cast<float>(mu);
     in.nesterov = nesterov;
     in.store_lo = n_steps > 1;
+    for (int k = 0; k < c.classes; ++k) in.store_lo = in.store_lo || is_precise(c.shape[k].m);
     in.partial = reinterpret_cast<double *>(ws + at.partial);
     in.scale = reinterpret_cast<MuonScale *>(ws + at.scale);
     for (int k = 0; k < c.classes; ++k)
@@ -1332,7 +1363,6 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
     if (e == cudaSuccess) e = launch_pdl(muon_norm_kernel, dim3(c.count), dim3(kMaxSlabs), 0, s, in);
     if (e == cudaSuccess) e = launch_pdl(muon_redo_kernel, dim3(std::min(in.tile0[c.count], 6 * pairs)), dim3(kInThreads), 0, s, in);
     // the steps, two at a time
-    constexpr int kGlo = kB1;  // (G's lo is read before B1 is written)
     double most = 1.0, sx = 1.0;  // (the first X's power of two is in its MuonScale)
     int x = kX;
     for (int i = 0; i < n_steps && e == cudaSuccess;) {
@@ -1341,32 +1371,32 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
         const Step &s0 = steps[i];
         const double sg = pow2_for(most * most), sb = pow2_for(s0.most_p);
         // G = X X^T;  B0 = a I + b G + c G^2
-        e = run.run<kStore, false>({kGram, x, x, kNone, kG, glo ? kGlo : kNone, scale, sg / (sx * sx)});
+        e = run.run<kStore, false>({kGram, x, x, false, kG, glo, scale, sg / (sx * sx)});
         if (e == cudaSuccess)
-            e = run.run<kPoly, false>({kSquareSym, kG, kG, kNone, kB0, kNone, nullptr, s0.c * sb / (sg * sg), s0.b * sb / sg, s0.a * sb});
+            e = run.run<kPoly, false>({kSquareSym, kG, kG, false, kB0, false, nullptr, s0.c * sb / (sg * sg), s0.b * sb / sg, s0.a * sb});
         double sp = sb, out = s0.most_out * kMargin;
         int product = kB0;
         if (pair) {
             const Step &s1 = steps[i + 1];
             const double st = pow2_for(most * most * s0.most_p), sg1 = pow2_for(out * out), sb1 = pow2_for(s1.most_p);
             // T^T = B0 G;  G = B0 T;  B1;  T = B1 B0
-            if (e == cudaSuccess) e = run.run<kNext, false>({kSquare, kB0, kG, glo ? kGlo : kNone, kT, kNone, nullptr, st / (sg * sb)});
-            if (e == cudaSuccess) e = run.run<kStore, false>({kSquareSym, kB0, kT, kNone, kG, kNone, nullptr, sg1 / (st * sb)});
+            if (e == cudaSuccess) e = run.run<kNext, false>({kSquare, kB0, kG, glo, kT, false, nullptr, st / (sg * sb)});
+            if (e == cudaSuccess) e = run.run<kStore, false>({kSquareSym, kB0, kT, false, kG, false, nullptr, sg1 / (st * sb)});
             if (e == cudaSuccess)
-                e = run.run<kPoly, false>({kSquareSym, kG, kG, kNone, kB1, kNone, nullptr, s1.c * sb1 / (sg1 * sg1), s1.b * sb1 / sg1, s1.a * sb1});
+                e = run.run<kPoly, false>({kSquareSym, kG, kG, false, kB1, false, nullptr, s1.c * sb1 / (sg1 * sg1), s1.b * sb1 / sg1, s1.a * sb1});
             sp = pow2_for(s0.most_p * s1.most_p);
-            if (e == cudaSuccess) e = run.run<kNext, false>({kSquare, kB1, kB0, kNone, kT, kNone, nullptr, sp / (sb1 * sb)});
+            if (e == cudaSuccess) e = run.run<kNext, false>({kSquare, kB1, kB0, false, kT, false, nullptr, sp / (sb1 * sb)});
             product = kT;
             out = s1.most_out * kMargin;
         }
         i += pair ? 2 : 1;
-        const int lo = first && in.store_lo ? kXlo : kNone;
+        const bool lo = first && n_steps > 1;
         if (i == n_steps) {
-            if (e == cudaSuccess) e = run.run<kOut, true>({kTimesX, product, x, lo, kNone, kNone, scale, 1.0 / (sp * sx)});
+            if (e == cudaSuccess) e = run.run<kOut, true>({kTimesX, product, x, lo, kNone, false, scale, 1.0 / (sp * sx)});
         } else {
             const double next = pow2_for(out);
             const int y = x == kX ? kXnext : kX;
-            if (e == cudaSuccess) e = run.run<kNext, true>({kTimesX, product, x, lo, y, kNone, scale, next / (sp * sx)});
+            if (e == cudaSuccess) e = run.run<kNext, true>({kTimesX, product, x, lo, y, false, scale, next / (sp * sx)});
             sx = next;
             x = y;
         }

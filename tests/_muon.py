@@ -40,6 +40,9 @@ def _scale(most):
     return 2.0 ** 14 if most <= 0 else 2.0 ** min(100, math.floor(math.log2(32768 / (most * (1 + 1 / 64)))))
 
 
+PRECISE, LONG = 32, 512  # up to so many rows every number is kept as two FP16 ones; the Gram matrix of longer rows is of their upper halves
+
+
 def model(v, steps=STEPS):
     v = v.double()
     tall = v.shape[0] > v.shape[1]
@@ -47,6 +50,7 @@ def model(v, steps=STEPS):
     norm = x.norm()
     x = x / norm if norm > 0 else x
     eye = torch.eye(len(x), dtype=torch.float64)
+    every = len(x) <= PRECISE
     most, i = 1.0, 0
 
     def bounds(step, most):
@@ -55,36 +59,51 @@ def model(v, steps=STEPS):
         p = (a + b * s ** 2 + c * s ** 4).abs()
         return float(p.max()), float((s * p).max()) * (1 + 1 / 64)
 
+    def keep(x, scale, lo=False):
+        """hi and lo of a result."""
+        hi = _half(x, scale)
+        return hi, _half(x - hi, scale) if lo or every else 0 * x
+
+    def times(x, y):
+        return x[0] @ y[0] + x[0] @ y[1] + (x[1] @ y[0] if every else 0)
+
+    def turn(x):
+        return x[0].T, x[1].T
+
+    def mirror(x):
+        return tuple(torch.triu(h) + torch.triu(h, 1).T for h in x)
+
     sx = 2.0 ** 14
     while i < len(steps):
-        hi = _half(x, sx)
         pair = i + 1 < len(steps)
-        lo = _half(x - hi, sx) if pair and i == 0 else 0 * x
+        x = keep(x, sx, pair and i == 0)
         a, b, c = steps[i]
         mp, out = bounds(steps[i], most)
-        g = _half(hi @ hi.T, _scale(most ** 2))
-        b0 = _half(a * eye + b * g + c * (g @ g), _scale(mp))
+        gram = times(x, turn(x)) if every and x[0].shape[1] <= LONG else x[0] @ x[0].T
+        g = keep(gram, _scale(most ** 2), pair and i > 0)
+        low = g if every else (g[0], 0 * g[0])  # elsewhere G's lo is for T alone
+        b0 = keep(a * eye + b * (low[0] + low[1]) + c * times(low, low), _scale(mp))
         if pair:
             a, b, c = steps[i + 1]
             mp1, out1 = bounds(steps[i + 1], out)
-            g_lo = _half(hi @ hi.T - g, _scale(most ** 2)) if i else 0 * g
-            t = _half(b0 @ (g + g_lo), _scale(most ** 2 * mp))
-            g = _half(b0 @ t.T, _scale(out ** 2))
-            g = torch.triu(g) + torch.triu(g, 1).T
-            b1 = _half(a * eye + b * g + c * (g @ g), _scale(mp1))
-            b0, out = _half(b1 @ b0, _scale(mp * mp1)), out1
-        x = b0 @ hi + b0 @ lo
+            t = keep(times(b0, g), _scale(most ** 2 * mp))
+            g = mirror(keep(times(b0, turn(t)), _scale(out ** 2)))
+            b1 = keep(a * eye + b * (g[0] + g[1]) + c * times(g, g), _scale(mp1))
+            b0, out = keep(times(b1, b0), _scale(mp * mp1)), out1
+        x = times(b0, x)
         most, sx = out, _scale(out)
         i += 2 if pair else 1
     return x.T if tall else x
 
 
 def bound(v, u_type, steps=STEPS):
-    """What u may be off by in the 2-norm: twice the model's error, which is one draw of the same roundings; 2^-9 for matrices of
-    few values, whose draws differ (the last product's two FP16 operands are each within 2^-11 and of norm at most 2 to u's 1); and
-    half a step of u's type."""
+    """What u may be off by in the 2-norm: twice the model's error, which is one draw of the same roundings; what the model lacks or draws of
+    few values may differ by; and half a step of u's type.  The second is 2^-9 (the last product's two FP16 operands are each within 2^-11
+    and of norm at most 2 to u's 1), or where every number has 22 digits what FP32's sums add: 2^-22 each, of which the first steps' are
+    blown up 3.4445^5 = 485 times, so 2^-13."""
     e = exact(v, steps)
-    return e, 2 * float((model(v, steps) - e).norm()) + (2.0 ** -9 + (2.0 ** -8 if u_type == torch.bfloat16 else 2.0 ** -24)) * float(e.norm())
+    more = 2.0 ** -13 if min(v.shape) <= PRECISE else 2.0 ** -9
+    return e, 2 * float((model(v, steps) - e).norm()) + (more + (2.0 ** -8 if u_type == torch.bfloat16 else 2.0 ** -24)) * float(e.norm())
 
 
 def gradient(r, c, seed, kind="mixed"):

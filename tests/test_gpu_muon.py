@@ -33,7 +33,8 @@ def check(u, v, u_type, steps=M.STEPS):
 
 
 SHAPES = [(1, 1), (1, 5), (5, 1), (1, 300), (3, 7), (8, 8), (48, 80), (64, 64), (127, 129), (129, 127), (128, 256), (256, 128), (257, 130),
-          (130, 259), (300, 1000), (1000, 300), (512, 512), (515, 384), (96, 2048), (2050, 70)]
+          (130, 259), (300, 1000), (1000, 300), (512, 512), (515, 384), (96, 2048), (2050, 70), (255, 400), (256, 2100), (8, 32), (3000, 9),
+          (32, 600), (600, 33), (20, 512), (513, 24), (320, 3000)]
 
 
 @pytest.mark.parametrize("r,c", SHAPES)

@@ -29,8 +29,9 @@ def test_the_definition_maps_singular_values(r, c):
 
 
 def test_the_model_differs_by_roundings_only():
-    v = M.gradient(40, 70, 3, "noise")
-    assert 1e-5 < (M.model(v) - M.exact(v)).norm() / M.exact(v).norm() < 2e-2
+    for r, c, low, high in ((40, 70, 1e-5, 2e-2), (20, 70, 1e-8, 1e-4), (70, 20, 1e-8, 1e-4)):  # FP16's, and with all digits
+        v = M.gradient(r, c, 3, "noise")
+        assert low < (M.model(v) - M.exact(v)).norm() / M.exact(v).norm() < high
 
 
 def entry(grad=A, momentum=A, u=A, rows=64, cols=96, gs=96, us=96, gt=0, ut=1, reserved=0):
