@@ -59,7 +59,7 @@ constexpr uint64_t kDrainNs = 2000000000ull, kSettleNs = 200000ull;
 // ------------------------------------------------ the update and its norm
 constexpr int kInRows = 64, kInCols = 128, kInThreads = 256;  // tile of the two passes over V
 constexpr int kInWarps = kInThreads / 32, kInPasses = 4;  // a warp a row, four rows of a warp at a time
-constexpr int kMaxSlabs = 512;
+constexpr int kNormThreads = 256;
 
 enum MatFlags : uint8_t {
     kGradBf16 = 1,
@@ -84,7 +84,6 @@ struct alignas(16) MatIn {
     int64_t stride;
     uint16_t *hi, *lo;
     int rows, cols, ldx;
-    int slab_tiles;  // tiles of a slab
     uint8_t flags;
 };
 struct MuonIn {
@@ -92,10 +91,9 @@ struct MuonIn {
     float mu;
     int nesterov;
     bool store_lo;
-    double *partial;  // [slabs]: sum of V^2 over each
+    double *partial;  // [tiles]: sum of V^2 over each
     MuonScale *scale;  // [count]
     int tile0[kMaxMats + 1];  // first tile of each matrix
-    int slab0[kMaxMats + 1];  // first slab: a run of tiles whose sum of V^2 one block takes
     MatIn mat[kMaxMats];
 };
 
@@ -115,7 +113,8 @@ PURO_DEV int in_col(uint8_t flags, int lane, int k) { return flags & kVectors ? 
 // The values of V of a lane's columns c0 ... in rows r0 + warp, r0 + warp + kInWarps, ...,
 // zero outside the matrix.  UPDATE: the momentum takes the gradient first and is
 // stored; else it has.  All loads are issued ahead of the first use (with each row's
-// behind the row before's stores 114 us for 82 over a layer's matrices).
+// behind the row before's stores 114 us for 82 over a layer's matrices); what is read
+// once makes room in L2 for X first.
 template <bool UPDATE, bool VEC, bool GRAD_VEC, bool BF16>
 PURO_DEV void tile_of(const MuonIn &p, int m, int r0, int c0, float (&v)[kInPasses][4]) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rows = p.mat[m].rows, cols = p.mat[m].cols;
@@ -144,14 +143,14 @@ PURO_DEV void tile_of(const MuonIn &p, int m, int r0, int c0, float (&v)[kInPass
                                 (k == 0 ? x.x : k == 1 ? x.y : k == 2 ? x.z : x.w) = z;
                         }
                     } else if constexpr (BF16) {
-                        const uint2 z = __ldg(reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p.mat[m].grad) + at(i, 0, stride)));
+                        const uint2 z = __ldcs(reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p.mat[m].grad) + at(i, 0, stride)));
                         x.x = z.x;
                         x.y = z.y;
                     } else {
-                        x = __ldg(reinterpret_cast<const uint4 *>(static_cast<const float *>(p.mat[m].grad) + at(i, 0, stride)));
+                        x = __ldcs(reinterpret_cast<const uint4 *>(static_cast<const float *>(p.mat[m].grad) + at(i, 0, stride)));
                     }
                 }
-                if (mom) y = *reinterpret_cast<const float4 *>(mom + at(i, 0, cols));
+                if (mom) y = __ldcs(reinterpret_cast<const float4 *>(mom + at(i, 0, cols)));
             }
             v[i][0] = __uint_as_float(BF16 ? x.x << 16 : x.x);
             v[i][1] = __uint_as_float(BF16 ? x.x & 0xFFFF0000u : x.y);
@@ -180,7 +179,7 @@ PURO_DEV void tile_of(const MuonIn &p, int m, int r0, int c0, float (&v)[kInPass
 #pragma unroll
             for (int k = 0; k < 4; ++k) w[i][k] = fmaf(p.mu, w[i][k], v[i][k]);
             if constexpr (VEC) {
-                if (in(i, 0)) *reinterpret_cast<float4 *>(mom + at(i, 0, cols)) = make_float4(w[i][0], w[i][1], w[i][2], w[i][3]);
+                if (in(i, 0)) __stcs(reinterpret_cast<float4 *>(mom + at(i, 0, cols)), make_float4(w[i][0], w[i][1], w[i][2], w[i][3]));
             } else {
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
@@ -209,6 +208,22 @@ PURO_DEV void read_tile(const MuonIn &p, int m, int r0, int c0, float (&v)[kInPa
         read(std::true_type{});
     else
         read(std::false_type{});
+}
+
+// The lines that a warp reads of half a tile at (r0, c0), to L2: one to a lane.
+PURO_DEV void prefetch_half(const MuonIn &p, int m, int r0, int c0) {
+    const int lane = threadIdx.x & 31, i = (lane >> 2) & 3, c = c0 + 32 * (lane & 3);
+    const int r = r0 + (threadIdx.x >> 5) + kInWarps * i;
+    if (r >= p.mat[m].rows || c >= p.mat[m].cols) return;
+    const void *at;
+    if (lane < 16)
+        at = p.mat[m].flags & kGradBf16 ? static_cast<const void *>(static_cast<const uint16_t *>(p.mat[m].grad) + r * p.mat[m].stride + c)
+                                        : static_cast<const float *>(p.mat[m].grad) + r * p.mat[m].stride + c;
+    else if (p.mat[m].momentum)
+        at = p.mat[m].momentum + static_cast<int64_t>(r) * p.mat[m].cols + c;
+    else
+        return;
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
 }
 
 struct InTile {
@@ -285,86 +300,104 @@ constexpr int kSampled = 1024;      // values of the gradient that the guess goe
 constexpr int kGuessExp = 9;        // it puts their norm's estimate at 2^9: V's may be 2^7 times that, or 2^-3
 constexpr float kLeastNorm = 64.0f, kMostNorm = 65024.0f;  // what guess ||V|| has to lie in: FP16's largest value is 65504
 
-// The momentum takes the gradient; each slab's sum of V^2; hi + lo of V times a power
+// The momentum takes the gradient; each tile's sum of V^2; hi + lo of V times a power
 // of two.  V is not read again for that (12 bytes a value of 28), so the factor has to
 // be known before the norm: each block takes it from the same sample of the gradient,
 // and muon_norm_kernel finds whether it holds.  A thread's 16 squares of half a tile
-// are summed in FP32, in FP64 where that left its range, the rest in FP64 in a fixed
-// order.  Bound by memory.
+// and its warp's are summed in FP32, in FP64 where that left its range; the warps' and
+// tiles' in FP64 in a fixed order.  Bound by memory: a block has a run of tiles, all
+// blocks equally many, across the matrices, and asks L2 for half a tile ahead (a sum for
+// each of at most 256 runs of a matrix's tiles had left the large ones 1.6 blocks an SM;
+// a call for Qwen2-1.5B's layer 996 us then, 965 now;
+// 24 matrices of [128, 1536] and 11 small ones 157 and 145).
 __global__ void __launch_bounds__(kInThreads, 4) muon_update_kernel(const __grid_constant__ MuonIn p) {
     __shared__ Turn turn;
-    __shared__ double part[kInWarps];
+    __shared__ double part[2][kInWarps];
     __shared__ float sampled[kInWarps];
     pdl_wait();
     pdl_launch_dependents();
-    const int m = mat_of(p.slab0, p.count, blockIdx.x), tiles = p.tile0[m + 1] - p.tile0[m];
-    const int slab = static_cast<int>(blockIdx.x) - p.slab0[m], first = slab * p.mat[m].slab_tiles;
+    const int64_t all = p.tile0[p.count];
+    const int end = static_cast<int>(all * (blockIdx.x + 1) / gridDim.x);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const bool tall = p.mat[m].flags & kTall;
-    float sample = 0.0f;  // rows evenly, columns by a hash
+    int i = static_cast<int>(all * blockIdx.x / gridDim.x);
+    for (int m = mat_of(p.tile0, p.count, i); i < end; ++m) {
+        const bool tall = p.mat[m].flags & kTall;
+        float sample = 0.0f;  // rows evenly, columns by a hash
 #pragma unroll
-    for (int i = 0; i < kSampled / kInThreads; ++i) {
-        const uint32_t e = threadIdx.x + kInThreads * i;
-        const int64_t at = (e * static_cast<uint32_t>(p.mat[m].rows) / kSampled) * p.mat[m].stride +
-                           __umulhi(e * 2654435761u, static_cast<uint32_t>(p.mat[m].cols));
-        sample += fabsf(p.mat[m].flags & kGradBf16
-                            ? __uint_as_float(static_cast<uint32_t>(__ldg(static_cast<const uint16_t *>(p.mat[m].grad) + at)) << 16)
-                            : __ldg(static_cast<const float *>(p.mat[m].grad) + at));
-    }
-    float guess = 0.0f;
-    double sum = 0.0;
-    for (int i = first; i < min(tiles, first + p.mat[m].slab_tiles); ++i) {
-        const InTile t = in_tile(i, p.mat[m].cols);
+        for (int j = 0; j < kSampled / kInThreads; ++j) {
+            const uint32_t e = threadIdx.x + kInThreads * j;
+            const int64_t at = (e * static_cast<uint32_t>(p.mat[m].rows) / kSampled) * p.mat[m].stride +
+                               __umulhi(e * 2654435761u, static_cast<uint32_t>(p.mat[m].cols));
+            sample += fabsf(p.mat[m].flags & kGradBf16
+                                ? __uint_as_float(static_cast<uint32_t>(__ldg(static_cast<const uint16_t *>(p.mat[m].grad) + at)) << 16)
+                                : __ldg(static_cast<const float *>(p.mat[m].grad) + at));
+        }
+        float guess = 0.0f;
+        for (const int last = min(end, p.tile0[m + 1]); i < last; ++i) {
+            const InTile t = in_tile(i - p.tile0[m], p.mat[m].cols);
+            float sum = 0.0f;
+            double far = 0.0;  // what FP32 does not hold
 #pragma unroll 1
-        for (int half = 0; half < kInRows; half += kInWarps * kInPasses) {
-            float v[kInPasses][4], s = 0.0f, most = 0.0f;
-            read_tile<true>(p, m, t.r0 + half, t.c0, v);
-            if (guess == 0.0f) {  // once, beside the first reads
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) sample += __shfl_xor_sync(0xFFFFFFFFu, sample, o);
-                if (lane == 0) sampled[warp] = sample;
-                __syncthreads();
-                float n = 0.0f;
-#pragma unroll
-                for (int w = 0; w < kInWarps; ++w) n += sampled[w];
-                // ||g|| is about the mean of |g| times sqrt(total)
-                n *= (1.0f / kSampled) * sqrtf(static_cast<float>(p.mat[m].rows) * static_cast<float>(p.mat[m].cols));
-                const int k = n > 0.0f && n < INFINITY ? min(max(kGuessExp - ilogbf(n), -126), 127) : 0;
-                guess = __uint_as_float(static_cast<uint32_t>(k + 127) << 23);
-            }
-#pragma unroll
-            for (int j = 0; j < kInPasses; ++j) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    s = fmaf(v[j][k], v[j][k], s);
-                    most = fmaxf(most, fabsf(v[j][k]));
+            for (int half = 0; half < kInRows; half += kInWarps * kInPasses) {
+                float v[kInPasses][4], s = 0.0f, most = 0.0f;
+                read_tile<true>(p, m, t.r0 + half, t.c0, v);
+                if (half == 0) {
+                    prefetch_half(p, m, t.r0 + kInWarps * kInPasses, t.c0);
+                } else if (i + 1 < last) {
+                    const InTile next = in_tile(i + 1 - p.tile0[m], p.mat[m].cols);
+                    prefetch_half(p, m, next.r0, next.c0);
                 }
-                store_x(p, m, turn, t.r0, half + warp + kInWarps * j, t.c0, v[j], guess, 1.0f);
-            }
-            if (s > 1e-24f && s < 1e36f) {
-                sum += s;
-            } else if (!(s == 0.0f && most == 0.0f)) {  // (FP64 is 64 times slower: not for what lies outside the matrix)
+                if (guess == 0.0f) {  // once a matrix, beside the first reads
 #pragma unroll
-                for (int j = 0; j < kInPasses; ++j)
+                    for (int o = 16; o > 0; o >>= 1) sample += __shfl_xor_sync(0xFFFFFFFFu, sample, o);
+                    if (lane == 0) sampled[warp] = sample;
+                    __syncthreads();
+                    float n = 0.0f;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) sum += static_cast<double>(v[j][k]) * v[j][k];
+                    for (int w = 0; w < kInWarps; ++w) n += sampled[w];
+                    // ||g|| is about the mean of |g| times sqrt(total)
+                    n *= (1.0f / kSampled) * sqrtf(static_cast<float>(p.mat[m].rows) * static_cast<float>(p.mat[m].cols));
+                    const int k = n > 0.0f && n < INFINITY ? min(max(kGuessExp - ilogbf(n), -126), 127) : 0;
+                    guess = __uint_as_float(static_cast<uint32_t>(k + 127) << 23);
+                    if (i == p.tile0[m] && threadIdx.x == 0) p.scale[m].guess = guess;
+                }
+#pragma unroll
+                for (int j = 0; j < kInPasses; ++j) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        s = fmaf(v[j][k], v[j][k], s);
+                        most = fmaxf(most, fabsf(v[j][k]));
+                    }
+                    store_x(p, m, turn, t.r0, half + warp + kInWarps * j, t.c0, v[j], guess, 1.0f);
+                }
+                if (s > 1e-24f && s < 1e36f) {
+                    sum += s;
+                } else if (!(s == 0.0f && most == 0.0f)) {  // (FP64 is 64 times slower: not for what lies outside the matrix)
+#pragma unroll
+                    for (int j = 0; j < kInPasses; ++j)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) far += static_cast<double>(v[j][k]) * v[j][k];
+                }
             }
-        }
-        if (tall) {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+            double *const parts = part[i & 1];  // the tile before's are still read
+            const bool any = __any_sync(0xFFFFFFFFu, far != 0.0);
+            if (any) far = warp_sum(far);
+            if (lane == 0) parts[warp] = any ? sum + far : sum;
             __syncthreads();
-            store_turned(p, m, turn, t.r0, t.c0);
-            __syncthreads();
+            if (threadIdx.x == 0) {
+                double d = 0.0;
+#pragma unroll
+                for (int w = 0; w < kInWarps; ++w) d += parts[w];
+                p.partial[i] = d;
+            }
+            if (tall) {
+                store_turned(p, m, turn, t.r0, t.c0);
+                __syncthreads();
+            }
         }
     }
-    sum = warp_sum(sum);
-    if (lane == 0) part[warp] = sum;
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    sum = 0.0;
-#pragma unroll
-    for (int w = 0; w < kInWarps; ++w) sum += part[w];
-    p.partial[blockIdx.x] = sum;
-    if (slab == 0) p.scale[m].guess = guess;
 }
 
 // The first X's power of two where the guess did not hold: entries are at most 1.
@@ -372,19 +405,28 @@ constexpr int kX0Exp = 14;
 
 // Each matrix's norm, and by it what the first step multiplies with: NaN where it is
 // not finite (all of u is then NaN), 0 for V = 0.
-__global__ void __launch_bounds__(kMaxSlabs) muon_norm_kernel(const __grid_constant__ MuonIn p) {
-    __shared__ double part[kMaxSlabs / 32];
+__global__ void __launch_bounds__(kNormThreads) muon_norm_kernel(const __grid_constant__ MuonIn p) {
+    __shared__ double part[kNormThreads / 32];
+    constexpr int kAtOnce = 16;
     pdl_wait();
     pdl_launch_dependents();
-    const int m = blockIdx.x, i = p.slab0[m] + static_cast<int>(threadIdx.x);
-    double d = i < p.slab0[m + 1] ? p.partial[i] : 0.0;
-    d = warp_sum(d);
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = d;
+    const int m = blockIdx.x, end = p.tile0[m + 1], warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    double d = 0.0;
+    for (int i = p.tile0[m] + 32 * warp; i < end; i += kAtOnce * kNormThreads) {  // (few additions: FP64 is 64 times slower)
+        double v[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) v[j] = j * kNormThreads + lane < end - i ? p.partial[i + j * kNormThreads + lane] : 0.0;
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j)
+            if (j * kNormThreads < end - i) d += v[j];
+    }
+    if (p.tile0[m] + 32 * warp < end) d = warp_sum(d);
+    if (lane == 0) part[warp] = d;
     __syncthreads();
-    if (threadIdx.x >= 32) return;
-    d = threadIdx.x < kMaxSlabs / 32 ? part[threadIdx.x] : 0.0;
-    d = warp_sum(d);
     if (threadIdx.x != 0) return;
+    d = 0.0;
+#pragma unroll
+    for (int w = 0; w < kNormThreads / 32; ++w) d += part[w];
     MuonScale s{p.scale[m].guess, 0.0f, 0.0f, 0.0f, 0};
     if (!(d < INFINITY)) {
         s.r = NAN;
@@ -988,10 +1030,6 @@ struct Scratch {
     int64_t buffer[kBuffers][kMaxClasses];  // offsets; -1: none
     int64_t partial = 0, scale = 0;
 };
-// Tiles of a slab: one where that leaves each SM a block or so, else as many as make
-// 128 to 256 slabs (a block's sample takes 1.5 us).  By the matrix's size alone: the
-// sums' order follows from it.
-int slab_tiles_of(int tiles) { return tiles <= 512 ? 1 : (tiles + 255) / 256; }
 int64_t tiles_in(int64_t rows, int64_t cols) {
     return (rows + kInRows - 1) / kInRows * ((cols + kInCols - 1) / kInCols);
 }
@@ -1002,7 +1040,9 @@ Scratch scratch_of(const puro_muon_matrix_t *mats, const Chunk &c) {
         s.bytes += align_up(bytes, kAlign);
         return at;
     };
-    s.partial = take(8 * c.count * kMaxSlabs);
+    int64_t tiles = 0;
+    for (int i = 0; i < c.count; ++i) tiles += tiles_in(mats[c.mats[i]].rows, mats[c.mats[i]].cols);
+    s.partial = take(8 * tiles);
     s.scale = take(static_cast<int64_t>(sizeof(MuonScale)) * c.count);
     for (int k = 0; k < c.classes; ++k) {
         const int64_t n = c.first[k + 1] - c.first[k];
@@ -1354,13 +1394,10 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
             run.out.stride[i] = us;
             run.out.flags[i] = (tall ? kTall : 0) | (f32 ? kOutF32 : 0);
             if (a.cols % (f32 ? 4 : 8) == 0 && us % (f32 ? 4 : 8) == 0 && aligned(a.u, 16)) run.out.flags[i] |= kOutVectors;
-            const int tiles = static_cast<int>(tiles_in(a.rows, a.cols)), each = slab_tiles_of(tiles);
-            in.tile0[i + 1] = in.tile0[i] + tiles;
-            to.slab_tiles = each;
-            in.slab0[i + 1] = in.slab0[i] + (tiles + each - 1) / each;
+            in.tile0[i + 1] = in.tile0[i] + static_cast<int>(tiles_in(a.rows, a.cols));
         }
-    e = launch_pdl(muon_update_kernel, dim3(in.slab0[c.count]), dim3(kInThreads), 0, s, in);
-    if (e == cudaSuccess) e = launch_pdl(muon_norm_kernel, dim3(c.count), dim3(kMaxSlabs), 0, s, in);
+    e = launch_pdl(muon_update_kernel, dim3(std::min(in.tile0[c.count], 8 * pairs)), dim3(kInThreads), 0, s, in);
+    if (e == cudaSuccess) e = launch_pdl(muon_norm_kernel, dim3(c.count), dim3(kNormThreads), 0, s, in);
     if (e == cudaSuccess) e = launch_pdl(muon_redo_kernel, dim3(std::min(in.tile0[c.count], 6 * pairs)), dim3(kInThreads), 0, s, in);
     // the steps, two at a time
     double most = 1.0, sx = 1.0;  // (the first X's power of two is in its MuonScale)

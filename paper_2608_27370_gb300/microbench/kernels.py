@@ -24,6 +24,9 @@ enough that a full capture ends in seconds).  Not part of the library.
     python -m paper_2608_27370_gb300.microbench.kernels qk       # norms and rotation, 32768 tokens of 12 + 2 heads of 128
     python -m paper_2608_27370_gb300.microbench.kernels qk_backward  # their backward with the gains' gradients
     python -m paper_2608_27370_gb300.microbench.kernels skinny   # one token through gate/up [17920, 1536] in BF16
+    python -m paper_2608_27370_gb300.microbench.kernels rope     # rotation without norms, 32768 tokens of 12 + 2 heads of 128
+    python -m paper_2608_27370_gb300.microbench.kernels rope_tables     # cosines and sines of 131072 positions, 64 pairs
+    python -m paper_2608_27370_gb300.microbench.kernels muon     # Muon directions of one layer: qkv, o_proj, gate_up, down
 
 Most inputs are larger than L2 (ncu flushes the caches before each pass in
 any case).  Every call is made twice: the second is the one to capture
@@ -206,10 +209,30 @@ def main(which: str) -> None:
         gate_up, h = (torch.empty((1, n), dtype=torch.bfloat16, device=dev) for n in (2 * F, F))
         for _ in range(2):
             P.puro_bf16_gated_fprop(x, w, P.ACT_SILU, gate_up, h)
+    elif which in ("rope", "rope_tables"):
+        T, HQ, HK, D = 32768, 12, 2, 128
+        freq = P.rope_frequencies(D, 1e6, device=dev)
+        qkv, out = W.normal_bf16((T, HQ + 2 * HK, D), 1.0, dev, 31), torch.empty((T, HQ + HK, D), dtype=torch.bfloat16, device=dev)
+        positions = torch.arange(T, dtype=torch.int32, device=dev)
+        cos, sin = (torch.empty((131072, D // 2), dtype=torch.float32, device=dev) for _ in range(2))
+        for _ in range(2):
+            if which == "rope":
+                P.puro_rope(qkv[:, :HQ], qkv[:, HQ:HQ + HK], freq, positions, False, out[:, :HQ], out[:, HQ:])
+            else:
+                P.puro_rope_tables(freq, 0, cos, sin)
+    elif which == "muon":
+        mats = []
+        for j, (_, N, K) in enumerate(W.QWEN2_1P5B_LINEARS):
+            g, v = W.normal_f32((N, K), 1e-3, dev, 110 + j), W.normal_f32((N, K), 1e-2, dev, 120 + j)
+            mats.append((g, v, torch.empty((N, K), dtype=torch.bfloat16, device=dev)))
+        table = P.muon_table(mats)
+        ws = torch.empty(P.puro_muon_direction_workspace_size(table), dtype=torch.uint8, device=dev)
+        for _ in range(2):
+            P.puro_muon_direction_grouped(table, ws)
     else:
         raise SystemExit(f"unknown kernel {which!r}: swiglu, rmsnorm, muonh, gemm, gemm_k1536, gemm_oproj, "
                          "dgrad_quant, quant, quant_small, tensor, bf16, weight, weights, splitk, unfused, linear_residual, "
-                         "gated, act_backward, gated_backward, qk, qk_backward or skinny")
+                         "gated, act_backward, gated_backward, qk, qk_backward, skinny, rope, rope_tables or muon")
     torch.cuda.synchronize()
     print("ok", which)
 
