@@ -672,7 +672,8 @@ puro_status_t puro_muonh_step_grouped(const puro_muonh_matrix_t *mats, int32_t c
  *     a row.
  * V = 0 gives u = 0; a V whose norm is not finite gives NaN in all of u.  Matrices are
  * taken in order, up to 128 of up to 8 shapes at a time: three kernels, and then seven
- * for each pair of steps (three for a last odd one).  Every descriptor is checked
+ * for each pair of steps (three for a last odd one), or one for all steps where all have
+ * few rows (or columns).  Every descriptor is checked
  * before anything is enqueued.
  */
 typedef enum { PURO_BF16 = 0, PURO_F32 = 1 } puro_float_t;

@@ -223,7 +223,7 @@ PURO_DEV void prefetch_half(const MuonIn &p, int m, int r0, int c0) {
         at = p.mat[m].momentum + static_cast<int64_t>(r) * p.mat[m].cols + c;
     else
         return;
-    asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
+    prefetch_l2(at);
 }
 
 struct InTile {
@@ -672,6 +672,32 @@ PURO_DEV void block_to_u(const uint8_t *from, bool f32, bool vectors, void *u, i
     }
 }
 
+// A lane's row of 32 x 32 values at (row0, col) of X, of rows x cols, to u.
+PURO_DEV void values_to_u(uint8_t *stage, const MuonOut &out, int m, const float (&v)[32], int row0, int col, int rows, int cols,
+                          int lane) {
+    const uint8_t f = out.flags[m];
+    const bool tall = f & kTall, f32 = f & kOutF32;
+    __syncwarp();  // the block before has left the staging tile
+    if (f32) {
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+            const int sr = tall ? k : lane, sc = tall ? lane : k;
+            *reinterpret_cast<float *>(stage + 128 * sr + 16 * ((sc >> 2) ^ (sr & 7)) + 4 * (sc & 3)) = v[k];
+        }
+    } else {
+        uint32_t h[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) h[k] = bf162_bits(v[2 * k], v[2 * k + 1]);
+        if (tall)
+            stage_columns(stage, h, lane);
+        else
+            stage_rows(stage, h, lane);
+    }
+    __syncwarp();
+    block_to_u(stage, f32, f & kOutVectors, out.u[m], out.stride[m], tall ? col : row0, tall ? row0 : col, tall ? cols : rows,
+               tall ? rows : cols, lane);
+}
+
 template <int BN, bool X_MAJOR, int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     muon_product_kernel(const __grid_constant__ MuonPhase p, const __grid_constant__ OutOf<EPI> out) {
@@ -894,28 +920,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     }
                 }
                 if constexpr (EPI == kOut) {
-                    const int m = p.first[w.cls] + w.z;
-                    const uint8_t f = out.flags[m];
-                    const bool tall = f & kTall, f32 = f & kOutF32;
-                    __syncwarp();  // the block before has left the staging tile
-                    if (f32) {
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) {
-                            const int sr = tall ? k : lane, sc = tall ? lane : k;
-                            *reinterpret_cast<float *>(stage_buf + 128 * sr + 16 * ((sc >> 2) ^ (sr & 7)) + 4 * (sc & 3)) = v[k];
-                        }
-                    } else {
-                        uint32_t h[16];
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) h[k] = bf162_bits(v[2 * k], v[2 * k + 1]);
-                        if (tall)
-                            stage_columns(stage_buf, h, lane);
-                        else
-                            stage_rows(stage_buf, h, lane);
-                    }
-                    __syncwarp();
-                    block_to_u(stage_buf, f32, f & kOutVectors, out.u[m], out.stride[m], tall ? col : row0, tall ? row0 : col,
-                               tall ? cols : rows, tall ? rows : cols, lane);
+                    values_to_u(stage_buf, out, p.first[w.cls] + w.z, v, row0, col, rows, cols, lane);
                 } else {
                     uint32_t h[16];
 #pragma unroll
@@ -932,6 +937,416 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                         if (w.mirror) store(&maps.d_lo, h, true, row0, col, w.z);
                     }
                 }
+            }
+        }
+        if (e) bulk_wait_group0();
+        __syncwarp();
+    }
+    // the pair's MMAs are complete and read, and no arrival targets a CTA that has left
+    tc_fence_before_sync();
+    __syncthreads();
+    cluster_arrive();
+    cluster_wait();
+    tc_fence_after_sync();
+    if (warp == 1) tmem_dealloc_pair(tmem, kTmemCols);
+}
+
+// ------------------------------------- all products of a matrix of few rows
+// A pair of CTAs takes a matrix of m <= 256 through all steps: the results of m x m
+// stay in shared memory, each CTA with h = m / 2 rows (up to a multiple of 32) of all of
+// them, and X goes through L2.  CTA r has rows h r .. of A and, the first h of its 128,
+// of B, so that a pair MMA of 256 x 2h gives row h r + i in lane i of CTA r; rows h .. 127
+// of A are whatever lies there, and so are the accumulators' lanes, which nothing reads.
+// G and its powers have zeros in columns m .. 2h.  Every sum is that of the launches, bit
+// for bit.  Bound by latency: seven products in a row, each waiting for the one before,
+// 1.8 us each (the cluster-wide release and acquire of a square 0.2 of it) where a launch
+// takes 2.9: one [48, 80] 70 -> 43 us a call, 24 matrices of [128, 1536] and 11 smaller
+// ones 145 -> 111.
+//   warp 0       TMA producer (both CTAs): X's rows for G, its columns for B X
+//   warp 1       MMA issuer (even CTA); tensor memory
+//   warps 4..11  epilogue (both CTAs): warp 4 + 4h + q has rows 32q .. and every second
+//                32 columns
+struct SmallClass {
+    CUtensorMap rows[2], cols[2], lo, block[2];  // X and the next X: 64 x 128, 64 x 64 (and its lo), 32 x 32
+    int m, n, first;                             // first: of the class's matrices
+};
+struct StepPair {
+    bool pair, glo, last;  // glo: G's lost digits are kept for T
+    float g, c0, b0, a0, t, g1, c1, b1, a1, p, x;
+};
+struct MuonSmall {
+    int classes, units, steps;
+    bool lo;  // the first X has digits in its lo
+    int unit0[kMaxClasses + 1];
+    SmallClass cls[kMaxClasses];
+    StepPair step[kMaxSteps / 2 + 1];
+    const MuonScale *scale;
+    int32_t *status;
+    uint64_t wait_ns;
+};
+constexpr int kSmallMost = 256, kSmallStages = 8, kSquareBytes = 4 * kBM * 128;
+struct SmallSmem {
+    // 0: G, G1, B1 B0 (or the last B0).  1: G's lo, T', B1.  2: B0.  Chunks of 64 columns,
+    // [128][64] with the 128-byte swizzle.  1 and 2 are the ring of X's k-blocks meanwhile.
+    alignas(1024) uint8_t square[3][kSquareBytes];
+    alignas(1024) uint8_t stage[kEpiWarps][4096];
+    uint64_t full[kSmallStages], empty[kSmallStages];
+    uint64_t tfull[2], tempty[2];
+    uint64_t stored;  // (even CTA's) a result of m x m lies in both CTAs' shared memory
+    uint64_t ring;    // 1 and 2 have been read
+    uint64_t next;    // this CTA's rows of the next X are in memory
+    uint64_t drain;
+    uint32_t tmem_base;
+    volatile int abort_flag;
+};
+static_assert(2 * kSquareBytes == kSmallStages * kBM * 128, "the ring is two squares");
+struct SmallUnit {
+    int cls, z, h, kb_m, kb_n, tiles;
+};
+PURO_DEV SmallUnit small_unit(const MuonSmall &p, int u) {
+    SmallUnit w;
+    w.cls = 0;
+    while (w.cls + 1 < p.classes && u >= p.unit0[w.cls + 1]) ++w.cls;
+    const int m = p.cls[w.cls].m, n = p.cls[w.cls].n;
+    w.z = u - p.unit0[w.cls];
+    w.h = (m + 63) / 64 * 32;
+    w.kb_m = (m + kBK - 1) / kBK;
+    w.kb_n = (n + kBK - 1) / kBK;
+    w.tiles = (n + 255) / 256;
+    return w;
+}
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    muon_small_kernel(const __grid_constant__ MuonSmall p, const __grid_constant__ MuonOut out) {
+    constexpr uint32_t kBlockBytes = kBM * 128;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    SmallSmem &sm = *reinterpret_cast<SmallSmem *>(smem_raw);
+    const int warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0);
+    const int lane = threadIdx.x & 31;
+    const int rank = __shfl_sync(0xFFFFFFFFu, static_cast<int>(cluster_ctarank()), 0);
+    const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kSmallStages; ++s) {
+            mbar_init(&sm.full[s], 1);
+            mbar_init(&sm.empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&sm.tfull[b], 1);
+            mbar_init(&sm.tempty[b], 2 * kEpiWarps);
+        }
+        mbar_init(&sm.stored, 2 * kEpiWarps);
+        mbar_init(&sm.ring, kEpiWarps);
+        mbar_init(&sm.next, kEpiWarps);
+        mbar_init(&sm.drain, 1);
+        sm.abort_flag = 0;
+        fence_mbarrier_init();
+    }
+    __syncthreads();
+    if (warp == 1) {
+        tmem_alloc_pair(&sm.tmem_base, kTmemCols);
+        tmem_relinquish_alloc_permit_pair();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    cluster_arrive();
+    cluster_wait();  // both CTAs' barriers exist
+    const uint32_t tmem = sm.tmem_base;
+    uint8_t *const ring = sm.square[1];
+
+    if (warp == 0) {
+        // ------------------------------------------------ TMA producer
+        const uint32_t e = elect_one();
+        const uint32_t full0 = mapa_shared(smem_u32(&sm.full[0]), 0);
+        uint32_t stage = 0, phase = 0, issued = 0, ring_phase = 0, next_phase = 0;
+        bool ok = true;
+        pdl_wait();
+        pdl_launch_dependents();
+        auto slot = [&] {  // a free place, or null
+            ok = wait_or_abort(sm, &sm.empty[stage], phase ^ 1u, p.wait_ns, p.status, lane);
+            if (ok && rank == 0 && e) mbar_arrive_expect_tx(&sm.full[stage], 2u * kBlockBytes);
+            return ring + kBlockBytes * stage;
+        };
+        auto filled = [&] {
+            ++issued;
+            if (++stage == kSmallStages) {
+                stage = 0;
+                phase ^= 1u;
+            }
+        };
+        for (int u = pair; u < p.units && ok; u += pairs) {
+            const SmallUnit w = small_unit(p, u);
+            const SmallClass &c = p.cls[w.cls];
+            for (int s = 0; s < p.steps && ok; ++s) {
+                if (s > 0) {
+                    ok = wait_or_abort(sm, &sm.next, next_phase, p.wait_ns, p.status, lane);
+                    next_phase ^= 1u;
+                    fence_proxy_async_global();
+                }
+                for (int kb = 0; kb < w.kb_n && ok; ++kb) {
+                    uint8_t *to = slot();
+                    if (!ok) break;
+                    tma_load_3d_pair_e(e, to, &c.rows[s & 1], full0 + 8u * stage, kb * kBK, w.h * rank, w.z);
+                    filled();
+                }
+                if (!ok) break;
+                ok = wait_or_abort(sm, &sm.ring, ring_phase, p.wait_ns, p.status, lane);
+                ring_phase ^= 1u;
+                fence_proxy_async_global();
+                for (int t = 0; t < w.tiles && ok; ++t)
+                    for (int kb = 0; kb < w.kb_m * (s == 0 && p.lo ? 2 : 1); ++kb) {
+                        const CUtensorMap *map = kb < w.kb_m ? &c.cols[s & 1] : &c.lo;
+                        uint8_t *to = slot();
+                        if (!ok) break;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            tma_load_3d_pair_e(e, to + 8192 * i, map, full0 + 8u * stage, 256 * t + 128 * rank + 64 * i,
+                                               kb % w.kb_m * kBK, w.z);
+                        filled();
+                    }
+            }
+        }
+        if (rank == 0) {  // every fill of the ring (both CTAs' copies) lands before the pair exits
+            for (uint32_t s = 0; s < kSmallStages; ++s) {
+                const uint32_t fills = issued / kSmallStages + (s < issued % kSmallStages ? 1u : 0u);
+                if (fills > 0) mbar_wait_bounded(&sm.full[s], (fills - 1u) & 1u, kDrainNs);
+            }
+        }
+        if (!ok) {  // this CTA's copies count on the even CTA's barriers: give those in flight time to land
+            const uint64_t t0 = global_timer_ns();
+            while (global_timer_ns() - t0 < kSettleNs) {
+            }
+        }
+    } else if (warp == 1 && rank == 0) {
+        // ------------------------------------------------ MMA issuer
+        const uint32_t e = elect_one();
+        uint32_t stage = 0, phase = 0, stored_phase = 0;
+        int local = 0;
+        bool ok = true;
+        // kind::f16, FP32 accumulators, FP16 operands, M = 256
+        constexpr uint32_t kIdesc = (1u << 4) | ((256u >> 4) << 24), kXIdesc = kIdesc | (1u << 16) | ((256u >> 3) << 17);
+        auto free_buffer = [&] { ok = ok && wait_or_abort(sm, &sm.tempty[local & 1], ((local >> 1) & 1u) ^ 1u, p.wait_ns, p.status, lane); };
+        auto done = [&] {
+            if (ok) tc_commit_pair_multicast_e(e, &sm.tfull[local & 1], 3);
+            ++local;
+        };
+        auto ring_block = [&](auto &&mmas) {
+            ok = ok && wait_or_abort(sm, &sm.full[stage], phase, p.wait_ns, p.status, lane);
+            if (!ok) return;
+            tc_fence_after_sync();
+            mmas(smem_u32(ring + kBlockBytes * stage));
+            tc_commit_pair_multicast_e(e, &sm.empty[stage], 3);
+            if (++stage == kSmallStages) {
+                stage = 0;
+                phase ^= 1u;
+            }
+        };
+        auto wait_stored = [&] {
+            ok = ok && wait_or_abort(sm, &sm.stored, stored_phase, p.wait_ns, p.status, lane);
+            if (ok) mbar_test_wait_cluster(&sm.stored, stored_phase);  // (complete: acquires what the other CTA's warps released)
+            stored_phase ^= 1u;
+            tc_fence_after_sync();
+        };
+        for (int u = pair; u < p.units && ok; u += pairs) {
+            const SmallUnit w = small_unit(p, u);
+            const uint32_t idesc = kIdesc | (static_cast<uint32_t>(2 * w.h >> 3) << 17);
+            auto square = [&](int a, int b, bool more) {  // d (+)= a b^T
+                const uint32_t d = tmem + 256u * (local & 1);
+                const uint32_t from = smem_u32(sm.square[a]), to = smem_u32(sm.square[b]);
+                for (int kb = 0; kb < w.kb_m && ok; ++kb)
+#pragma unroll
+                    for (int k = 0; k < kBK / 16; ++k)
+                        mma_pair_f16_e(e, d, smem_desc_k_sw128(from + kBlockBytes * kb + 32 * k), smem_desc_k_sw128(to + kBlockBytes * kb + 32 * k),
+                                       idesc, more || kb > 0 || k > 0 ? 1u : 0u);
+            };
+            auto product = [&](int a, int b) {
+                wait_stored();
+                free_buffer();
+                square(a, b, false);
+                done();
+            };
+            for (int s = 0; s < p.steps && ok; ++s) {
+                const StepPair &q = p.step[s];
+                free_buffer();
+                const uint32_t d = tmem + 256u * (local & 1);
+                for (int kb = 0; kb < w.kb_n && ok; ++kb)
+                    ring_block([&](uint32_t x) {
+#pragma unroll
+                        for (int k = 0; k < kBK / 16; ++k)
+                            mma_pair_f16_e(e, d, smem_desc_k_sw128(x + 32 * k), smem_desc_k_sw128(x + 32 * k), idesc, kb > 0 || k > 0 ? 1u : 0u);
+                    });
+                done();
+                product(0, 0);  // B0
+                if (q.pair) {
+                    wait_stored();  // T' = B0 G
+                    free_buffer();
+                    square(2, 0, false);
+                    if (q.glo) square(2, 1, true);
+                    done();
+                    product(2, 1);  // G1 = B0 T
+                    product(0, 0);  // B1
+                    product(1, 2);  // B1 B0
+                }
+                wait_stored();
+                for (int t = 0; t < w.tiles && ok; ++t) {
+                    free_buffer();
+                    const uint32_t dx = tmem + 256u * (local & 1), a = smem_u32(sm.square[0]);
+                    for (int kb = 0; kb < w.kb_m * (s == 0 && p.lo ? 2 : 1) && ok; ++kb)
+                        ring_block([&](uint32_t x) {
+#pragma unroll
+                            for (int k = 0; k < kBK / 16; ++k)
+                                mma_pair_f16_e(e, dx, smem_desc_k_sw128(a + kBlockBytes * (kb % w.kb_m) + 32 * k),
+                                               smem_desc_mn_sw128(x + 2048 * k, 8192), kXIdesc, kb > 0 || k > 0 ? 1u : 0u);
+                        });
+                    done();
+                }
+            }
+        }
+        if (e) {  // all MMAs issued are complete before teardown
+            tc_commit_pair(&sm.drain);
+            mbar_wait_bounded(&sm.drain, 0, kDrainNs);
+        }
+        __syncwarp();
+    } else if (warp >= 4) {
+        // ------------------------------------------------ epilogue
+        const int q = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t e = elect_one();
+        uint8_t *stage_buf = sm.stage[warp - 4];
+        const uint32_t tempty0 = mapa_shared(smem_u32(&sm.tempty[0]), 0), stored0 = mapa_shared(smem_u32(&sm.stored), 0);
+        const uint32_t own_ring = mapa_shared(smem_u32(&sm.ring), rank), own_next = mapa_shared(smem_u32(&sm.next), rank);
+        uint32_t pieces = 0;
+        int local = 0;
+        bool ok = true;
+        pdl_wait();
+        for (int u = pair; u < p.units && ok; u += pairs) {
+            const SmallUnit w = small_unit(p, u);
+            const SmallClass &c = p.cls[w.cls];
+            const int row0 = w.h * rank + 32 * q, row = 32 * q + lane;  // of X, of the CTA's
+            const bool some = 32 * q < w.h;
+            auto wait_acc = [&] {
+                ok = wait_or_abort(sm, &sm.tfull[local & 1], (local >> 1) & 1u, p.wait_ns, p.status, lane);
+                tc_fence_after_sync();
+                return tmem + (static_cast<uint32_t>(32 * q) << 16) + 256u * (local & 1);
+            };
+            auto read_acc = [&] {  // the accumulator is free
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster_cta_scope(tempty0 + 8u * (local & 1));
+                ++local;
+            };
+            auto arrive_own = [&](uint32_t bar) {
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster_cta_scope(bar);
+            };
+            // pieces of 8 values of 32 columns from col on
+            auto piece = [&](int at, int col, int k) {
+                return reinterpret_cast<uint4 *>(sm.square[at] + kBlockBytes * (col >> 6) + 128 * row + 16 * ((((col & 63) >> 3) + k) ^ (row & 7)));
+            };
+            // alpha D, or alpha D + beta G + gamma I, of m x m, to square `to`; the digits that it loses to `lo`
+            auto square = [&](int to, int lo, float alpha, bool poly, float beta, float gamma) {
+                const uint32_t acc = wait_acc();
+                if (!ok) return;
+                for (int col = 32 * half; some && col < 2 * w.h; col += 64) {
+                    uint32_t r[32];
+                    tmem_ld_32x32b_x32(acc + col, r);
+                    tmem_ld_wait();
+                    float v[32];
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) v[k] = alpha * __uint_as_float(r[k]);
+                    if (poly) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint4 g = *piece(0, col, k);
+                            const uint32_t xs[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&xs[j]));
+                                v[8 * k + 2 * j] = fmaf(beta, f.x, v[8 * k + 2 * j]);
+                                v[8 * k + 2 * j + 1] = fmaf(beta, f.y, v[8 * k + 2 * j + 1]);
+                            }
+                        }
+                        if (col == row0) {
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                if (lane == k) v[k] += gamma;
+                        }
+                    }
+                    if (col + 32 > c.m) {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            if (col + k >= c.m) v[k] = 0.0f;
+                    }
+                    uint32_t x[16];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) x[k] = half2_bits(v[2 * k], v[2 * k + 1]);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) *piece(to, col, k) = make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+                    if (lo >= 0) {
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&x[k]));
+                            x[k] = half2_bits(v[2 * k] - f.x, v[2 * k + 1] - f.y);
+                        }
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) *piece(lo, col, k) = make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+                    }
+                }
+                read_acc();
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(stored0);
+            };
+            const float r = __ldg(&p.scale[c.first + w.z].r);  // of the first X
+            for (int s = 0; s < p.steps && ok; ++s) {
+                const StepPair &f = p.step[s];
+                square(0, f.glo ? 1 : -1, s == 0 ? f.g * (r * r) : f.g, false, 0.0f, 0.0f);
+                if (f.pair) {
+                    if (ok) square(2, -1, f.c0, true, f.b0, f.a0);
+                    if (ok) square(1, -1, f.t, false, 0.0f, 0.0f);
+                    if (ok) square(0, -1, f.g1, false, 0.0f, 0.0f);
+                    if (ok) square(1, -1, f.c1, true, f.b1, f.a1);
+                    if (ok) square(0, -1, f.p, false, 0.0f, 0.0f);
+                } else if (ok) {
+                    square(0, -1, f.c0, true, f.b0, f.a0);
+                }
+                if (!ok) break;
+                arrive_own(own_ring);  // the last product of squares was complete
+                const float alpha = s == 0 ? f.x * r : f.x;
+                for (int t = 0; t < w.tiles; ++t) {
+                    const uint32_t acc = wait_acc();
+                    if (!ok) break;
+                    for (int i = half; some && row0 < c.m && i < 8; i += 2) {
+                        const int col = 256 * t + 32 * i;
+                        if (col >= c.n) break;
+                        uint32_t d[32];
+                        tmem_ld_32x32b_x32(acc + 32 * i, d);
+                        tmem_ld_wait();
+                        float v[32];
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) v[k] = alpha * __uint_as_float(d[k]);
+                        if (f.last) {
+                            values_to_u(stage_buf, out, c.first + w.z, v, row0, col, c.m, c.n, lane);
+                        } else {
+                            uint32_t x[16];
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) x[k] = half2_bits(v[2 * k], v[2 * k + 1]);
+                            uint8_t *to = stage_buf + 2048 * (pieces & 1u);
+                            if (e) bulk_wait_group_read<1>();
+                            __syncwarp();
+                            stage_rows(to, x, lane);
+                            fence_proxy_async_smem();
+                            __syncwarp();
+                            tma_store_3d_e(e, &c.block[(s + 1) & 1], to, col, row0, w.z);
+                            ++pieces;
+                        }
+                    }
+                    read_acc();
+                }
+                if (!ok || f.last) break;
+                if (e) bulk_wait_group0();
+                fence_proxy_async_global();
+                arrive_own(own_next);
             }
         }
         if (e) bulk_wait_group0();
@@ -1173,6 +1588,15 @@ cudaError_t product_attribute() {
     if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev].store(true, std::memory_order_relaxed);
     return e;
 }
+cudaError_t small_attribute() {
+    static std::atomic<bool> done[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || (dev >= 0 && dev < 64 && done[dev].load(std::memory_order_relaxed))) return e;
+    e = cudaFuncSetAttribute(muon_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(SmallSmem)));
+    if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev].store(true, std::memory_order_relaxed);
+    return e;
+}
 // Pairs of SMs that run pairs of CTAs.
 cudaError_t resident_pairs(int *pairs) {
     static int cache[64] = {0};
@@ -1223,6 +1647,7 @@ struct Products {
     int32_t *status;
     cudaStream_t s;
     int pairs;  // of SMs
+    bool small;  // muon_small_kernel takes all of them
     MuonOut out;
     Tiles tiles[kForms];
     // of each buffer: 64 x 128 (A; B of 256 columns), 64 x 64 (B of 128; X), 32 x 32 (D)
@@ -1269,8 +1694,30 @@ struct Products {
         return dealer.most;
     }
 
+    // Whether a pair of CTAs for each matrix is faster than a launch for each product, by
+    // what both were measured to take (us): a launch 2.75, and 0.25 for each 64 rows; the
+    // long rows of the Gram matrix; where there are many, a good part of what a pair would
+    // have taken by itself.  Five steps on one [128, 128] 47 and 68, on [256, 256] 69 and 75,
+    // on [128, 1536] 84 and 79, on 64 of them 134 and 170, on [256, 1536] 117 and 85, on 64 of
+    // them 210 and 260.
+    bool small_pays(int n_steps) const {
+        const int products = 7 * (n_steps / 2) + 3 * (n_steps % 2), turns = (n_steps + 1) / 2;
+        double launches = 0, all = 0, longest = 0;
+        for (int k = 0, at = 0; k < c.classes; ++k) {
+            const int64_t m = c.shape[k].m, units = c.first[k + 1] - c.first[k];
+            if (is_precise(m) || m > kSmallMost) return false;
+            const double kb_m = static_cast<double>((m + kBK - 1) / kBK), kb_n = static_cast<double>((c.shape[k].n + kBK - 1) / kBK);
+            const double one = products * (1.24 + 0.476 * kb_m) + turns * (0.5 + 0.065 * kb_m) * kb_n;
+            launches = std::max(launches, products * (2.75 + 0.25 * kb_m) + turns * 0.17 * kb_n);
+            all += one * static_cast<double>(units);
+            for (int64_t i = 0; i < units; ++i, ++at)  // (dealt in turn, the longest first)
+                if (at % pairs == 0) longest += one;
+        }
+        return longest < launches + 0.8 * all / pairs;
+    }
+
     cudaError_t prepare() {
-        for (int form = 0; form < kForms; ++form) {
+        for (int form = 0; form < kForms && !small; ++form) {
             Tiles narrow;
             if (deal(&narrow, form, 128) < deal(&tiles[form], form, 256)) tiles[form] = narrow;
         }
@@ -1290,6 +1737,35 @@ struct Products {
         return cudaSuccess;
     }
 
+    // All products, where small.
+    cudaError_t run_small(const StepPair *step, int n, bool lo, const MuonScale *scale) const {
+        MuonSmall p{};
+        for (int k = 0; k < c.classes; ++k) {
+            SmallClass &to = p.cls[p.classes++];
+            for (int i = 0; i < 2; ++i) {
+                const int x = i == 0 ? kX : kXnext;
+                to.rows[i] = rows128[k][x];
+                to.cols[i] = rows64[k][x];
+                to.block[i] = block[k][x];
+            }
+            to.lo = rows64[k][kXlo];
+            to.m = static_cast<int>(c.shape[k].m);
+            to.n = static_cast<int>(c.shape[k].n);
+            to.first = c.first[k];
+            p.units += c.first[k + 1] - c.first[k];
+            p.unit0[p.classes] = p.units;
+        }
+        const cudaError_t e = small_attribute();
+        if (e != cudaSuccess) return e;
+        std::copy(step, step + n, p.step);
+        p.steps = n;
+        p.lo = lo;
+        p.scale = scale;
+        p.status = status;
+        p.wait_ns = wait_timeout_ns();
+        return launch_pdl(muon_small_kernel, dim3(2 * std::min(p.units, pairs)), dim3(kThreads), sizeof(SmallSmem), s, p, out);
+    }
+
     // D = A B^T or (kTimesX) A X, of buffers.
     struct Product {
         Form form;
@@ -1298,7 +1774,7 @@ struct Products {
         int d;
         bool d_lo;  // the digits that D loses are kept as well; in a precise class they all are
         const MuonScale *scale = nullptr;  // of the first X
-        double alpha = 0, beta = 0, gamma = 0;
+        float alpha = 0, beta = 0, gamma = 0;
     };
     template <int EPI, bool X_MAJOR>
     cudaError_t run(const Product &q) const {
@@ -1322,9 +1798,9 @@ struct Products {
             p.ldg[k] = static_cast<int>(ld(k, true));
             p.g_batch[k] = c.shape[k].m * ld(k, true);
         }
-        p.alpha = static_cast<float>(q.alpha);
-        p.beta = static_cast<float>(q.beta);
-        p.gamma = static_cast<float>(q.gamma);
+        p.alpha = q.alpha;
+        p.beta = q.beta;
+        p.gamma = q.gamma;
         p.scale = q.scale;
         p.squared = q.form == kGram;
         p.status = status;
@@ -1359,6 +1835,7 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
     cudaError_t e = resident_pairs(&pairs);
     if (e != cudaSuccess) return e;
     Products run{c, at, ws, status, s, pairs};
+    run.small = run.small_pays(n_steps);
     e = run.prepare();
     if (e != cudaSuccess) return e;
     // the update, its norm, X
@@ -1399,45 +1876,64 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
     e = launch_pdl(muon_update_kernel, dim3(std::min(in.tile0[c.count], 8 * pairs)), dim3(kInThreads), 0, s, in);
     if (e == cudaSuccess) e = launch_pdl(muon_norm_kernel, dim3(c.count), dim3(kNormThreads), 0, s, in);
     if (e == cudaSuccess) e = launch_pdl(muon_redo_kernel, dim3(std::min(in.tile0[c.count], 6 * pairs)), dim3(kInThreads), 0, s, in);
-    // the steps, two at a time
+    // the steps, two at a time: what each product's results are scaled with
+    StepPair plan[kMaxSteps / 2 + 1];
+    int n_plan = 0;
     double most = 1.0, sx = 1.0;  // (the first X's power of two is in its MuonScale)
-    int x = kX;
-    for (int i = 0; i < n_steps && e == cudaSuccess;) {
-        const bool pair = i + 1 < n_steps, first = i == 0, glo = pair && !first;
-        const MuonScale *scale = first ? in.scale : nullptr;
+    for (int i = 0; i < n_steps;) {
+        const bool pair = i + 1 < n_steps;
         const Step &s0 = steps[i];
+        StepPair &f = plan[n_plan++];
         const double sg = pow2_for(most * most), sb = pow2_for(s0.most_p);
-        // G = X X^T;  B0 = a I + b G + c G^2
-        e = run.run<kStore, false>({kGram, x, x, false, kG, glo, scale, sg / (sx * sx)});
-        if (e == cudaSuccess)
-            e = run.run<kPoly, false>({kSquareSym, kG, kG, false, kB0, false, nullptr, s0.c * sb / (sg * sg), s0.b * sb / sg, s0.a * sb});
-        double sp = sb, out = s0.most_out * kMargin;
-        int product = kB0;
+        f.pair = pair;
+        f.glo = pair && i > 0;
+        f.g = static_cast<float>(sg / (sx * sx));
+        f.c0 = static_cast<float>(s0.c * sb / (sg * sg));
+        f.b0 = static_cast<float>(s0.b * sb / sg);
+        f.a0 = static_cast<float>(s0.a * sb);
+        double sp = sb, bound = s0.most_out * kMargin;
         if (pair) {
             const Step &s1 = steps[i + 1];
-            const double st = pow2_for(most * most * s0.most_p), sg1 = pow2_for(out * out), sb1 = pow2_for(s1.most_p);
-            // T^T = B0 G;  G = B0 T;  B1;  T = B1 B0
-            if (e == cudaSuccess) e = run.run<kNext, false>({kSquare, kB0, kG, glo, kT, false, nullptr, st / (sg * sb)});
-            if (e == cudaSuccess) e = run.run<kStore, false>({kSquareSym, kB0, kT, false, kG, false, nullptr, sg1 / (st * sb)});
-            if (e == cudaSuccess)
-                e = run.run<kPoly, false>({kSquareSym, kG, kG, false, kB1, false, nullptr, s1.c * sb1 / (sg1 * sg1), s1.b * sb1 / sg1, s1.a * sb1});
+            const double st = pow2_for(most * most * s0.most_p), sg1 = pow2_for(bound * bound), sb1 = pow2_for(s1.most_p);
+            f.t = static_cast<float>(st / (sg * sb));
+            f.g1 = static_cast<float>(sg1 / (st * sb));
+            f.c1 = static_cast<float>(s1.c * sb1 / (sg1 * sg1));
+            f.b1 = static_cast<float>(s1.b * sb1 / sg1);
+            f.a1 = static_cast<float>(s1.a * sb1);
             sp = pow2_for(s0.most_p * s1.most_p);
-            if (e == cudaSuccess) e = run.run<kNext, false>({kSquare, kB1, kB0, false, kT, false, nullptr, sp / (sb1 * sb)});
-            product = kT;
-            out = s1.most_out * kMargin;
+            f.p = static_cast<float>(sp / (sb1 * sb));
+            bound = s1.most_out * kMargin;
         }
         i += pair ? 2 : 1;
-        const bool lo = first && n_steps > 1;
-        if (i == n_steps) {
-            if (e == cudaSuccess) e = run.run<kOut, true>({kTimesX, product, x, lo, kNone, false, scale, 1.0 / (sp * sx)});
-        } else {
-            const double next = pow2_for(out);
-            const int y = x == kX ? kXnext : kX;
-            if (e == cudaSuccess) e = run.run<kNext, true>({kTimesX, product, x, lo, y, false, scale, next / (sp * sx)});
-            sx = next;
-            x = y;
+        f.last = i == n_steps;
+        const double next = f.last ? 1.0 : pow2_for(bound);
+        f.x = static_cast<float>(next / (sp * sx));
+        sx = next;
+        most = bound;
+    }
+    if (run.small) return e == cudaSuccess ? run.run_small(plan, n_plan, n_steps > 1, in.scale) : e;
+    for (int i = 0; i < n_plan && e == cudaSuccess; ++i) {
+        const StepPair &f = plan[i];
+        const MuonScale *scale = i == 0 ? in.scale : nullptr;
+        const int x = i & 1 ? kXnext : kX, y = i & 1 ? kX : kXnext;
+        const bool lo = i == 0 && n_steps > 1;
+        // G = X X^T;  B0 = a I + b G + c G^2
+        e = run.run<kStore, false>({kGram, x, x, false, kG, f.glo, scale, f.g});
+        if (e == cudaSuccess) e = run.run<kPoly, false>({kSquareSym, kG, kG, false, kB0, false, nullptr, f.c0, f.b0, f.a0});
+        int product = kB0;
+        if (f.pair) {
+            // T^T = B0 G;  G = B0 T;  B1;  T = B1 B0
+            if (e == cudaSuccess) e = run.run<kNext, false>({kSquare, kB0, kG, f.glo, kT, false, nullptr, f.t});
+            if (e == cudaSuccess) e = run.run<kStore, false>({kSquareSym, kB0, kT, false, kG, false, nullptr, f.g1});
+            if (e == cudaSuccess) e = run.run<kPoly, false>({kSquareSym, kG, kG, false, kB1, false, nullptr, f.c1, f.b1, f.a1});
+            if (e == cudaSuccess) e = run.run<kNext, false>({kSquare, kB1, kB0, false, kT, false, nullptr, f.p});
+            product = kT;
         }
-        most = out;
+        if (e != cudaSuccess) break;
+        if (f.last)
+            e = run.run<kOut, true>({kTimesX, product, x, lo, kNone, false, scale, f.x});
+        else
+            e = run.run<kNext, true>({kTimesX, product, x, lo, y, false, scale, f.x});
     }
     return e;
 }

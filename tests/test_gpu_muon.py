@@ -145,6 +145,34 @@ def test_narrow_and_wide_tiles_agree():
     assert all(torch.equal(a, b) for a, b in zip(u, alone))
 
 
+@pytest.mark.parametrize("steps", [1, 2, 3, 5, 6])
+def test_a_pair_for_each_matrix_and_launches_agree(steps):
+    """Few rows, whose products one kernel takes; beside a larger matrix each product is a launch: the same sums."""
+    shapes = [(48, 80), (33, 40), (700, 64), (127, 129), (256, 256), (130, 512), (65, 300)]
+    mats = [(M.gradient(r, c, r + c).to(DEV), M.gradient(r, c, 9).to(DEV)) for r, c in shapes]
+    together, beside = ([(g, m.clone(), torch.empty_like(g)) for g, m in mats] for _ in range(2))
+    coefficients = (M.STEPS * 2)[:steps]
+    directions(together, steps=coefficients)
+    big = M.gradient(300, 320, 1).to(DEV)
+    for x in beside:
+        directions([x, (big, None, torch.empty_like(big))], steps=coefficients)
+    for a, b, (g, m) in zip(together, beside, mats):
+        assert torch.equal(a[2], b[2]), g.shape
+        v = 0.95 * m.cpu() + g.cpu()
+        check(a[2], g.cpu() + 0.95 * v, F32, coefficients)
+
+
+@pytest.mark.parametrize("count", [77, 128])
+def test_more_matrices_than_pairs(count):
+    g = [M.gradient(40 + i % 2, 60, i).to(DEV) for i in range(count)]
+    u = [torch.empty_like(x) for x in g]
+    directions([(x, None, y) for x, y in zip(g, u)])
+    for i in list(range(3)) + list(range(72, count)):
+        alone = torch.empty_like(g[i])
+        directions([(g[i], None, alone)])
+        assert torch.equal(alone, u[i]), i
+
+
 @pytest.mark.parametrize("factor", [2.0 ** -120, 2.0 ** -60, 2.0 ** 60, 2.0 ** 110])
 def test_the_size_of_v_does_not_count(factor):
     g = M.gradient(50, 90, 2) * 1024
@@ -271,7 +299,7 @@ def test_refusals():
         P.puro_muon_direction_grouped([(g, None, torch.empty_like(g))], ws, coefficients=())
 
 
-@pytest.mark.parametrize("r,c", [(1536, 2048), (96, 8000)])
+@pytest.mark.parametrize("r,c", [(1536, 2048), (96, 8000), (96, 120)])
 def test_a_wait_that_runs_out_sets_the_status(r, c):
     """With no time to wait a product gives up, says so and ends; the same call then gives what it gave before."""
     g, u, want = M.gradient(r, c, 1).to(DEV), torch.empty(r, c, device=DEV), torch.empty(r, c, device=DEV)
