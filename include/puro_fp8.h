@@ -671,7 +671,7 @@ puro_status_t puro_muonh_step_grouped(const puro_muonh_matrix_t *mats, int32_t c
  *     each matrix of m x n, m <= n (8 m n + 16 m^2 up to m = 32), of the largest 128 in
  *     a row.
  * V = 0 gives u = 0; a V whose norm is not finite gives NaN in all of u.  Matrices are
- * taken in order, up to 128 of up to 8 shapes at a time: three kernels, and then seven
+ * taken in order, up to 128 of up to 8 shapes at a time: two kernels, and then seven
  * for each pair of steps (three for a last odd one), or one for all steps where all have
  * few rows (or columns).  Every descriptor is checked
  * before anything is enqueued.

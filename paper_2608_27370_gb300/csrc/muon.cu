@@ -59,7 +59,6 @@ constexpr uint64_t kDrainNs = 2000000000ull, kSettleNs = 200000ull;
 // ------------------------------------------------ the update and its norm
 constexpr int kInRows = 64, kInCols = 128, kInThreads = 256;  // tile of the two passes over V
 constexpr int kInWarps = kInThreads / 32, kInPasses = 4;  // a warp a row, four rows of a warp at a time
-constexpr int kNormThreads = 256;
 
 enum MatFlags : uint8_t {
     kGradBf16 = 1,
@@ -73,8 +72,7 @@ enum MatFlags : uint8_t {
 // sample of the gradient gave), and r of it is X; or, where that would have left
 // FP16's range, hi + lo is V x y = 2^14 X.
 struct MuonScale {
-    float guess, r, x, y;
-    int redo;
+    float r, x, y;
 };
 // One matrix's part of the update (together: a block's first use of a parameter is a
 // cache miss).
@@ -92,6 +90,7 @@ struct MuonIn {
     int nesterov;
     bool store_lo;
     double *partial;  // [tiles]: sum of V^2 over each
+    float *guess;      // [count]
     MuonScale *scale;  // [count]
     int tile0[kMaxMats + 1];  // first tile of each matrix
     MatIn mat[kMaxMats];
@@ -298,7 +297,7 @@ PURO_DEV void store_turned(const MuonIn &p, int m, const Turn &turn, int r0, int
 
 constexpr int kSampled = 1024;      // values of the gradient that the guess goes by
 constexpr int kGuessExp = 9;        // it puts their norm's estimate at 2^9: V's may be 2^7 times that, or 2^-3
-constexpr float kLeastNorm = 64.0f, kMostNorm = 65024.0f;  // what guess ||V|| has to lie in: FP16's largest value is 65504
+constexpr double kLeastNorm = 64.0, kMostNorm = 65024.0;  // what guess ||V|| has to lie in: FP16's largest value is 65504
 
 // The momentum takes the gradient; each tile's sum of V^2; hi + lo of V times a power
 // of two.  V is not read again for that (12 bytes a value of 28), so the factor has to
@@ -359,7 +358,7 @@ __global__ void __launch_bounds__(kInThreads, 4) muon_update_kernel(const __grid
                     n *= (1.0f / kSampled) * sqrtf(static_cast<float>(p.mat[m].rows) * static_cast<float>(p.mat[m].cols));
                     const int k = n > 0.0f && n < INFINITY ? min(max(kGuessExp - ilogbf(n), -126), 127) : 0;
                     guess = __uint_as_float(static_cast<uint32_t>(k + 127) << 23);
-                    if (i == p.tile0[m] && threadIdx.x == 0) p.scale[m].guess = guess;
+                    if (i == p.tile0[m] && threadIdx.x == 0) p.guess[m] = guess;
                 }
 #pragma unroll
                 for (int j = 0; j < kInPasses; ++j) {
@@ -404,66 +403,69 @@ __global__ void __launch_bounds__(kInThreads, 4) muon_update_kernel(const __grid
 constexpr int kX0Exp = 14;
 
 // Each matrix's norm, and by it what the first step multiplies with: NaN where it is
-// not finite (all of u is then NaN), 0 for V = 0.
-__global__ void __launch_bounds__(kNormThreads) muon_norm_kernel(const __grid_constant__ MuonIn p) {
-    __shared__ double part[kNormThreads / 32];
+// not finite (all of u is then NaN), 0 for V = 0.  And X once more where the guess did not
+// hold.  Block (b, m) of gridDim.x for matrix m; each adds the norm up for itself, which
+// is a launch less than to be told (one [48, 80] 42.6 -> 40.1 us, [1536, 1536] 171.9 -> 169.3).
+__global__ void __launch_bounds__(kInThreads, 3) muon_norm_kernel(const __grid_constant__ MuonIn p) {
+    __shared__ Turn turn;
+    __shared__ double part[kInWarps];
+    __shared__ MuonScale again;  // what X is written with once more, or 0
     constexpr int kAtOnce = 16;
     pdl_wait();
     pdl_launch_dependents();
-    const int m = blockIdx.x, end = p.tile0[m + 1], warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int m = blockIdx.y, first = p.tile0[m], end = p.tile0[m + 1], warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (8 * static_cast<int>(blockIdx.x) >= end - first) return;
     double d = 0.0;
-    for (int i = p.tile0[m] + 32 * warp; i < end; i += kAtOnce * kNormThreads) {  // (few additions: FP64 is 64 times slower)
+    for (int i = first + 32 * warp; i < end; i += kAtOnce * kInThreads) {  // (few additions: FP64 is 64 times slower)
         double v[kAtOnce];
 #pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) v[j] = j * kNormThreads + lane < end - i ? p.partial[i + j * kNormThreads + lane] : 0.0;
+        for (int j = 0; j < kAtOnce; ++j) v[j] = j * kInThreads + lane < end - i ? p.partial[i + j * kInThreads + lane] : 0.0;
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j)
-            if (j * kNormThreads < end - i) d += v[j];
+            if (j * kInThreads < end - i) d += v[j];
     }
-    if (p.tile0[m] + 32 * warp < end) d = warp_sum(d);
+    if (first + 32 * warp < end) d = warp_sum(d);
     if (lane == 0) part[warp] = d;
     __syncthreads();
-    if (threadIdx.x != 0) return;
-    d = 0.0;
+    if (warp == 0) {
+        d = part[0];
 #pragma unroll
-    for (int w = 0; w < kNormThreads / 32; ++w) d += part[w];
-    MuonScale s{p.scale[m].guess, 0.0f, 0.0f, 0.0f, 0};
-    if (!(d < INFINITY)) {
-        s.r = NAN;
-    } else if (d > 0.0) {
-        const double norm = sqrt(d), held = norm * s.guess;
-        s.r = static_cast<float>(1.0 / held);
-        if (!(held >= kLeastNorm && held <= kMostNorm)) {
-            // the factor in two parts, neither of which leaves FP32's range
-            const double scale = static_cast<double>(1 << kX0Exp) / norm;
-            const int e = ilogb(scale) / 2;
-            s.x = static_cast<float>(ldexp(1.0, e));
-            s.y = static_cast<float>(ldexp(scale, -e));
-            s.r = 1.0f / static_cast<float>(1 << kX0Exp);
-            s.redo = 1;
+        for (int w = 1; w < kInWarps; ++w)
+            if (first + 32 * w < end) d += part[w];
+        const float guess = p.guess[m];
+        MuonScale s{0.0f, 0.0f, 0.0f};
+        bool redo = false;
+        if (!(d < INFINITY)) {
+            s.r = NAN;
+        } else if (d > 0.0) {
+            const double held2 = d * guess * guess;
+            redo = !(held2 >= kLeastNorm * kLeastNorm && held2 <= kMostNorm * kMostNorm);
+            if (!redo) {
+                if (blockIdx.x == 0) s.r = static_cast<float>(1.0 / (sqrt(d) * guess));
+            } else {
+                // the factor in two parts, neither of which leaves FP32's range
+                const double scale = static_cast<double>(1 << kX0Exp) / sqrt(d);
+                const int e = ilogb(scale) / 2;
+                s.x = static_cast<float>(ldexp(1.0, e));
+                s.y = static_cast<float>(ldexp(scale, -e));
+                s.r = 1.0f / static_cast<float>(1 << kX0Exp);
+            }
         }
+        if (blockIdx.x == 0 && lane == 0) p.scale[m] = s;
+        if (lane == 0) again = redo ? s : MuonScale{0.0f, 0.0f, 0.0f};
     }
-    p.scale[m] = s;
-}
-
-// X once more, by the norm, of the matrices whose guess did not hold.
-__global__ void __launch_bounds__(kInThreads, 3) muon_redo_kernel(const __grid_constant__ MuonIn p) {
-    __shared__ Turn turn;
-    pdl_wait();
-    pdl_launch_dependents();
-    if (!__syncthreads_or(static_cast<int>(threadIdx.x) < p.count && p.scale[threadIdx.x].redo)) return;
-    for (int i = blockIdx.x; i < p.tile0[p.count]; i += gridDim.x) {
-        const int m = mat_of(p.tile0, p.count, i);
-        const MuonScale s = p.scale[m];
-        if (!s.redo) continue;
-        const InTile t = in_tile(i - p.tile0[m], p.mat[m].cols);
+    __syncthreads();
+    const MuonScale s = again;
+    if (s.x == 0.0f) return;
+    const int blocks = min(static_cast<int>(gridDim.x), (end - first + 7) / 8);
+    for (int i = blockIdx.x; i < end - first; i += blocks) {
+        const InTile t = in_tile(i, p.mat[m].cols);
 #pragma unroll 1
         for (int half = 0; half < kInRows; half += kInWarps * kInPasses) {
             float v[kInPasses][4];
             read_tile<false>(p, m, t.r0 + half, t.c0, v);
 #pragma unroll
-            for (int j = 0; j < kInPasses; ++j)
-                store_x(p, m, turn, t.r0, half + static_cast<int>(threadIdx.x >> 5) + kInWarps * j, t.c0, v[j], s.x, s.y);
+            for (int j = 0; j < kInPasses; ++j) store_x(p, m, turn, t.r0, half + warp + kInWarps * j, t.c0, v[j], s.x, s.y);
         }
         if (p.mat[m].flags & kTall) {
             __syncthreads();
@@ -1443,7 +1445,7 @@ bool is_precise(int64_t m) { return m <= kPrecise; }
 struct Scratch {
     int64_t bytes = 0;
     int64_t buffer[kBuffers][kMaxClasses];  // offsets; -1: none
-    int64_t partial = 0, scale = 0;
+    int64_t partial = 0, guess = 0, scale = 0;
 };
 int64_t tiles_in(int64_t rows, int64_t cols) {
     return (rows + kInRows - 1) / kInRows * ((cols + kInCols - 1) / kInCols);
@@ -1458,6 +1460,7 @@ Scratch scratch_of(const puro_muon_matrix_t *mats, const Chunk &c) {
     int64_t tiles = 0;
     for (int i = 0; i < c.count; ++i) tiles += tiles_in(mats[c.mats[i]].rows, mats[c.mats[i]].cols);
     s.partial = take(8 * tiles);
+    s.guess = take(4 * c.count);
     s.scale = take(static_cast<int64_t>(sizeof(MuonScale)) * c.count);
     for (int k = 0; k < c.classes; ++k) {
         const int64_t n = c.first[k + 1] - c.first[k];
@@ -1846,6 +1849,7 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
     in.store_lo = n_steps > 1;
     for (int k = 0; k < c.classes; ++k) in.store_lo = in.store_lo || is_precise(c.shape[k].m);
     in.partial = reinterpret_cast<double *>(ws + at.partial);
+    in.guess = reinterpret_cast<float *>(ws + at.guess);
     in.scale = reinterpret_cast<MuonScale *>(ws + at.scale);
     for (int k = 0; k < c.classes; ++k)
         for (int i = c.first[k]; i < c.first[k + 1]; ++i) {
@@ -1874,8 +1878,11 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
             in.tile0[i + 1] = in.tile0[i] + static_cast<int>(tiles_in(a.rows, a.cols));
         }
     e = launch_pdl(muon_update_kernel, dim3(std::min(in.tile0[c.count], 8 * pairs)), dim3(kInThreads), 0, s, in);
-    if (e == cudaSuccess) e = launch_pdl(muon_norm_kernel, dim3(c.count), dim3(kNormThreads), 0, s, in);
-    if (e == cudaSuccess) e = launch_pdl(muon_redo_kernel, dim3(std::min(in.tile0[c.count], 6 * pairs)), dim3(kInThreads), 0, s, in);
+    int widest = 0;  // tiles of a matrix
+    for (int i = 0; i < c.count; ++i) widest = std::max(widest, in.tile0[i + 1] - in.tile0[i]);
+    // (a block holds an SM from the product behind, whose shared memory does not fit beside)
+    const dim3 blocks(std::min((widest + 7) / 8, std::max(1, 2 * pairs / c.count)), c.count);
+    if (e == cudaSuccess) e = launch_pdl(muon_norm_kernel, blocks, dim3(kInThreads), 0, s, in);
     // the steps, two at a time: what each product's results are scaled with
     StepPair plan[kMaxSteps / 2 + 1];
     int n_plan = 0;

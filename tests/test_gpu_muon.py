@@ -299,18 +299,20 @@ def test_refusals():
         P.puro_muon_direction_grouped([(g, None, torch.empty_like(g))], ws, coefficients=())
 
 
-@pytest.mark.parametrize("r,c", [(1536, 2048), (96, 8000), (96, 120)])
-def test_a_wait_that_runs_out_sets_the_status(r, c):
-    """With no time to wait a product gives up, says so and ends; the same call then gives what it gave before."""
+@pytest.mark.parametrize("r,c,count", [(1536, 2048, 1), (96, 8000, 1), (256, 1536, 70)])
+def test_a_wait_that_runs_out_sets_the_status(r, c, count):
+    """With no time to wait a product gives up, says so and ends; the same call then gives what it gave before.  (The waits are long: a short
+    one may end before the first look at the clock.)"""
     g, u, want = M.gradient(r, c, 1).to(DEV), torch.empty(r, c, device=DEV), torch.empty(r, c, device=DEV)
-    directions([(g, None, want)])
+    more = [(g, None, torch.empty_like(u)) for _ in range(count - 1)]
+    directions([(g, None, want)] + more)
     torch.cuda.synchronize()
     P.puro_set_wait_timeout_ns(0)
     try:
-        status = directions([(g, None, u)])
+        status = directions([(g, None, u)] + more)
         torch.cuda.synchronize()
     finally:
         P.puro_set_wait_timeout_ns(2_000_000_000)
     assert P.puro_fp8_get_status(status) == P.PURO_ERR_TIMEOUT
-    assert P.puro_fp8_get_status(directions([(g, None, u)])) == P.PURO_OK
+    assert P.puro_fp8_get_status(directions([(g, None, u)] + more)) == P.PURO_OK
     assert torch.equal(u, want)
