@@ -1162,12 +1162,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                         mma_pair_f16_e(e, d, smem_desc_k_sw128(from + kBlockBytes * kb + 32 * k), smem_desc_k_sw128(to + kBlockBytes * kb + 32 * k),
                                        idesc, more || kb > 0 || k > 0 ? 1u : 0u);
             };
-            auto product = [&](int a, int b) {
-                wait_stored();
-                free_buffer();
-                square(a, b, false);
-                done();
-            };
             for (int s = 0; s < p.steps && ok; ++s) {
                 const StepPair &q = p.step[s];
                 free_buffer();
@@ -1179,16 +1173,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                             mma_pair_f16_e(e, d, smem_desc_k_sw128(x + 32 * k), smem_desc_k_sw128(x + 32 * k), idesc, kb > 0 || k > 0 ? 1u : 0u);
                     });
                 done();
-                product(0, 0);  // B0
-                if (q.pair) {
-                    wait_stored();  // T' = B0 G
+                // B0; T' = B0 G; G1 = B0 T; B1; B1 B0
+#pragma unroll 1
+                for (int i = 1; i < (q.pair ? 6 : 2); ++i) {
+                    wait_stored();
                     free_buffer();
-                    square(2, 0, false);
-                    if (q.glo) square(2, 1, true);
+                    for (int pass = 0; pass < (i == 2 && q.glo ? 2 : 1); ++pass)
+                        square(i == 2 || i == 3 ? 2 : i == 5 ? 1 : 0, i == 3 ? 1 : i == 5 ? 2 : pass, pass > 0);
                     done();
-                    product(2, 1);  // G1 = B0 T
-                    product(0, 0);  // B1
-                    product(1, 2);  // B1 B0
                 }
                 wait_stored();
                 for (int t = 0; t < w.tiles && ok; ++t) {
@@ -1302,15 +1294,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const float r = __ldg(&p.scale[c.first + w.z].r);  // of the first X
             for (int s = 0; s < p.steps && ok; ++s) {
                 const StepPair &f = p.step[s];
-                square(0, f.glo ? 1 : -1, s == 0 ? f.g * (r * r) : f.g, false, 0.0f, 0.0f);
-                if (f.pair) {
-                    if (ok) square(2, -1, f.c0, true, f.b0, f.a0);
-                    if (ok) square(1, -1, f.t, false, 0.0f, 0.0f);
-                    if (ok) square(0, -1, f.g1, false, 0.0f, 0.0f);
-                    if (ok) square(1, -1, f.c1, true, f.b1, f.a1);
-                    if (ok) square(0, -1, f.p, false, 0.0f, 0.0f);
-                } else if (ok) {
-                    square(0, -1, f.c0, true, f.b0, f.a0);
+                // (one piece of code for them all: a call is over before six were fetched)
+#pragma unroll 1
+                for (int i = 0; i < (f.pair ? 6 : 2) && ok; ++i) {
+                    const bool poly = i == 1 || i == 4;
+                    const float alpha = i == 0 ? (s == 0 ? f.g * (r * r) : f.g) : i == 1 ? f.c0 : i == 2 ? f.t : i == 3 ? f.g1 : i == 4 ? f.c1 : f.p;
+                    square(i == 1 && f.pair ? 2 : i == 2 || i == 4 ? 1 : 0, i == 0 && f.glo ? 1 : -1, alpha, poly, i == 1 ? f.b0 : f.b1,
+                           i == 1 ? f.a0 : f.a1);
                 }
                 if (!ok) break;
                 arrive_own(own_ring);  // the last product of squares was complete
