@@ -1690,8 +1690,8 @@ struct Products {
     // Whether a pair of CTAs for each matrix is faster than a launch for each product, by
     // what both were measured to take (us): a launch 2.75, and 0.25 for each 64 rows; the
     // long rows of the Gram matrix; where there are many, a good part of what a pair would
-    // have taken by itself.  Five steps on one [128, 128] 47 and 68, on [256, 256] 69 and 75,
-    // on [128, 1536] 84 and 79, on 64 of them 134 and 170, on [256, 1536] 117 and 85, on 64 of
+    // have taken by itself.  Five steps on one [128, 128] 43 and 68, on [256, 256] 68 and 75,
+    // on [128, 1536] 82 and 79, on 64 of them 134 and 170, on [256, 1536] 117 and 85, on 64 of
     // them 210 and 260.
     bool small_pays(int n_steps) const {
         const int products = 7 * (n_steps / 2) + 3 * (n_steps % 2), turns = (n_steps + 1) / 2;
@@ -1716,7 +1716,7 @@ struct Products {
         }
         for (int k = 0; k < c.classes; ++k)
             for (int b = 0; b < kBuffers; ++b) {
-                if (at.buffer[b][k] < 0) continue;
+                if (at.buffer[b][k] < 0 || (small && is_square(b))) continue;
                 const bool square = is_square(b);
                 const int64_t cols = square ? c.shape[k].m : c.shape[k].n, row = 2 * ld(k, square);
                 auto map = [&](CUtensorMap *m, int bx, int by, CUtensorMapSwizzle sw) {

@@ -27,6 +27,7 @@ enough that a full capture ends in seconds).  Not part of the library.
     python -m paper_2608_27370_gb300.microbench.kernels rope     # rotation without norms, 32768 tokens of 12 + 2 heads of 128
     python -m paper_2608_27370_gb300.microbench.kernels rope_tables     # cosines and sines of 131072 positions, 64 pairs
     python -m paper_2608_27370_gb300.microbench.kernels muon     # Muon directions of one layer: qkv, o_proj, gate_up, down
+    python -m paper_2608_27370_gb300.microbench.kernels muon_small     # the same of 24 matrices of [128, 1536]
 
 Most inputs are larger than L2 (ncu flushes the caches before each pass in
 any case).  Every call is made twice: the second is the one to capture
@@ -220,9 +221,9 @@ def main(which: str) -> None:
                 P.puro_rope(qkv[:, :HQ], qkv[:, HQ:HQ + HK], freq, positions, False, out[:, :HQ], out[:, HQ:])
             else:
                 P.puro_rope_tables(freq, 0, cos, sin)
-    elif which == "muon":
+    elif which in ("muon", "muon_small"):
         mats = []
-        for j, (_, N, K) in enumerate(W.QWEN2_1P5B_LINEARS):
+        for j, (N, K) in enumerate([(128, 1536)] * 24 if which == "muon_small" else [(N, K) for _, N, K in W.QWEN2_1P5B_LINEARS]):
             g, v = W.normal_f32((N, K), 1e-3, dev, 110 + j), W.normal_f32((N, K), 1e-2, dev, 120 + j)
             mats.append((g, v, torch.empty((N, K), dtype=torch.bfloat16, device=dev)))
         table = P.muon_table(mats)
@@ -232,7 +233,7 @@ def main(which: str) -> None:
     else:
         raise SystemExit(f"unknown kernel {which!r}: swiglu, rmsnorm, muonh, gemm, gemm_k1536, gemm_oproj, "
                          "dgrad_quant, quant, quant_small, tensor, bf16, weight, weights, splitk, unfused, linear_residual, "
-                         "gated, act_backward, gated_backward, qk, qk_backward, skinny, rope, rope_tables or muon")
+                         "gated, act_backward, gated_backward, qk, qk_backward, skinny, rope, rope_tables, muon or muon_small")
     torch.cuda.synchronize()
     print("ok", which)
 
