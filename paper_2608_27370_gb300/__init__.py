@@ -495,6 +495,9 @@ def muon_table(mats):
                                       types[u.dtype], 0)
         table.tensors += [t for t in (g, m, u) if t is not None]
     table.count = len(mats)
+    written = [t.data_ptr() for _, m, u in mats for t in (m, u) if t is not None and t.numel()]
+    if len(set(written)) < len(written):
+        raise ValueError("a momentum or u is there twice")
     devices = {t.get_device() for t in table.tensors if t.numel()}
     if len(devices) > 1:
         raise ValueError(f"the matrices are on several devices: {sorted(devices)}")

@@ -297,6 +297,10 @@ def test_refusals():
         P.puro_muon_direction_grouped([(g, None, torch.empty_like(g))], ws, coefficients=((1.0, 2.0),))
     with pytest.raises(P.PuroError):
         P.puro_muon_direction_grouped([(g, None, torch.empty_like(g))], ws, coefficients=())
+    u, m = torch.empty_like(g), torch.zeros_like(g, dtype=F32)
+    for twice in ([(g, None, u), (g, None, u)], [(g, m, u), (g, m, torch.empty_like(g))]):
+        with pytest.raises(ValueError):
+            P.muon_table(twice)
 
 
 @pytest.mark.parametrize("r,c,count", [(1536, 2048, 1), (96, 8000, 1), (256, 1536, 70)])
