@@ -970,17 +970,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 //                32 columns
 struct SmallClass {
     CUtensorMap rows[2], cols[2], lo, block[2];  // X and the next X: 64 x 128, 64 x 64 (and its lo), 32 x 32
-    int m, n, first;                             // first: of the class's matrices
+    int m, n, first;    // first: of the class's matrices
+    int passes;         // of X X^T: 3 with hi and lo, 1
+    bool precise;       // all results are hi and lo: lo is the second block of a square
 };
 struct StepPair {
     bool pair, glo, last;  // glo: G's lost digits are kept for T
     float g, c0, b0, a0, t, g1, c1, b1, a1, p, x;
 };
+struct SmallLo {  // the same of all lo's
+    CUtensorMap rows[2], next_cols, block[2];
+};
+struct NoLo {};
+template <bool PRECISE>  // some classes are (launches copy their parameters)
 struct MuonSmall {
     int classes, units, steps;
     bool lo;  // the first X has digits in its lo
     int unit0[kMaxClasses + 1];
     SmallClass cls[kMaxClasses];
+    std::conditional_t<PRECISE, SmallLo, NoLo> lo_of[kMaxClasses];
     StepPair step[kMaxSteps / 2 + 1];
     const MuonScale *scale;
     int32_t *status;
@@ -990,6 +998,7 @@ constexpr int kSmallMost = 256, kSmallStages = 8, kSquareBytes = 4 * kBM * 128;
 struct SmallSmem {
     // 0: G, G1, B1 B0 (or the last B0).  1: G's lo, T', B1.  2: B0.  Chunks of 64 columns,
     // [128][64] with the 128-byte swizzle.  1 and 2 are the ring of X's k-blocks meanwhile.
+    // Up to 32 rows lo lies where the second chunk would.
     alignas(1024) uint8_t square[3][kSquareBytes];
     alignas(1024) uint8_t stage[kEpiWarps][4096];
     uint64_t full[kSmallStages], empty[kSmallStages];
@@ -1005,7 +1014,10 @@ static_assert(2 * kSquareBytes == kSmallStages * kBM * 128, "the ring is two squ
 struct SmallUnit {
     int cls, z, h, kb_m, kb_n, tiles;
 };
-PURO_DEV SmallUnit small_unit(const MuonSmall &p, int u) {
+// Over P and X: 2, X's lo after its hi; 3, then P's lo with X's hi.
+PURO_DEV int x_passes(bool lo, bool precise, int s) { return precise ? 3 : s == 0 && lo ? 2 : 1; }
+template <bool PRECISE>
+PURO_DEV SmallUnit small_unit(const MuonSmall<PRECISE> &p, int u) {
     SmallUnit w;
     w.cls = 0;
     while (w.cls + 1 < p.classes && u >= p.unit0[w.cls + 1]) ++w.cls;
@@ -1018,8 +1030,9 @@ PURO_DEV SmallUnit small_unit(const MuonSmall &p, int u) {
     return w;
 }
 
+template <bool PRECISE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-    muon_small_kernel(const __grid_constant__ MuonSmall p, const __grid_constant__ MuonOut out) {
+    muon_small_kernel(const __grid_constant__ MuonSmall<PRECISE> p, const __grid_constant__ MuonOut out) {
     constexpr uint32_t kBlockBytes = kBM * 128;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     SmallSmem &sm = *reinterpret_cast<SmallSmem *>(smem_raw);
@@ -1080,25 +1093,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         for (int u = pair; u < p.units && ok; u += pairs) {
             const SmallUnit w = small_unit(p, u);
             const SmallClass &c = p.cls[w.cls];
+            const bool precise = PRECISE && c.precise;
             for (int s = 0; s < p.steps && ok; ++s) {
                 if (s > 0) {
                     ok = wait_or_abort(sm, &sm.next, next_phase, p.wait_ns, p.status, lane);
                     next_phase ^= 1u;
                     fence_proxy_async_global();
                 }
-                for (int kb = 0; kb < w.kb_n && ok; ++kb) {
-                    uint8_t *to = slot();
-                    if (!ok) break;
-                    tma_load_3d_pair_e(e, to, &c.rows[s & 1], full0 + 8u * stage, kb * kBK, w.h * rank, w.z);
-                    filled();
-                }
+                for (int pass = 0; pass < (precise ? c.passes : 1); ++pass)  // hi; hi, lo; lo, hi
+                    for (int kb = 0; kb < w.kb_n && ok; ++kb)
+                        for (int i = 0; i < (pass == 0 ? 1 : 2); ++i) {
+                            uint8_t *to = slot();
+                            if (!ok) break;
+                            const CUtensorMap *map = &c.rows[s & 1];
+                            if constexpr (PRECISE)
+                                if (pass + i == 2) map = &p.lo_of[w.cls].rows[s & 1];
+                            tma_load_3d_pair_e(e, to, map, full0 + 8u * stage, kb * kBK, w.h * rank, w.z);
+                            filled();
+                        }
                 if (!ok) break;
                 ok = wait_or_abort(sm, &sm.ring, ring_phase, p.wait_ns, p.status, lane);
                 ring_phase ^= 1u;
                 fence_proxy_async_global();
                 for (int t = 0; t < w.tiles && ok; ++t)
-                    for (int kb = 0; kb < w.kb_m * (s == 0 && p.lo ? 2 : 1); ++kb) {
-                        const CUtensorMap *map = kb < w.kb_m ? &c.cols[s & 1] : &c.lo;
+                    for (int kb = 0; kb < w.kb_m * x_passes(p.lo, precise, s); ++kb) {
+                        const CUtensorMap *map = kb / w.kb_m == 1 ? &c.lo : &c.cols[s & 1];
+                        if constexpr (PRECISE)
+                            if (kb / w.kb_m == 1 && (s & 1)) map = &p.lo_of[w.cls].next_cols;
                         uint8_t *to = slot();
                         if (!ok) break;
 #pragma unroll
@@ -1133,16 +1154,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             if (ok) tc_commit_pair_multicast_e(e, &sm.tfull[local & 1], 3);
             ++local;
         };
-        auto ring_block = [&](auto &&mmas) {
+        auto next_block = [&] {  // of the ring
             ok = ok && wait_or_abort(sm, &sm.full[stage], phase, p.wait_ns, p.status, lane);
-            if (!ok) return;
             tc_fence_after_sync();
-            mmas(smem_u32(ring + kBlockBytes * stage));
-            tc_commit_pair_multicast_e(e, &sm.empty[stage], 3);
+            const uint32_t at = smem_u32(ring + kBlockBytes * stage);
             if (++stage == kSmallStages) {
                 stage = 0;
                 phase ^= 1u;
             }
+            return at;
+        };
+        auto release = [&](uint32_t at) {
+            if (ok) tc_commit_pair_multicast_e(e, &sm.empty[(at - smem_u32(ring)) / kBlockBytes], 3);
         };
         auto wait_stored = [&] {
             ok = ok && wait_or_abort(sm, &sm.stored, stored_phase, p.wait_ns, p.status, lane);
@@ -1152,10 +1175,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         };
         for (int u = pair; u < p.units && ok; u += pairs) {
             const SmallUnit w = small_unit(p, u);
+            const SmallClass &c = p.cls[w.cls];
+            const bool precise = PRECISE && c.precise;
             const uint32_t idesc = kIdesc | (static_cast<uint32_t>(2 * w.h >> 3) << 17);
-            auto square = [&](int a, int b, bool more) {  // d (+)= a b^T
+            auto square = [&](uint32_t from, uint32_t to, bool more) {  // d (+)= a b^T
                 const uint32_t d = tmem + 256u * (local & 1);
-                const uint32_t from = smem_u32(sm.square[a]), to = smem_u32(sm.square[b]);
                 for (int kb = 0; kb < w.kb_m && ok; ++kb)
 #pragma unroll
                     for (int k = 0; k < kBK / 16; ++k)
@@ -1166,33 +1190,43 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 const StepPair &q = p.step[s];
                 free_buffer();
                 const uint32_t d = tmem + 256u * (local & 1);
-                for (int kb = 0; kb < w.kb_n && ok; ++kb)
-                    ring_block([&](uint32_t x) {
+                for (int pass = 0; pass < (precise ? c.passes : 1); ++pass)
+                    for (int kb = 0; kb < w.kb_n && ok; ++kb) {
+                        const uint32_t x = next_block(), y = pass == 0 ? x : next_block();
+                        if (!ok) break;
 #pragma unroll
                         for (int k = 0; k < kBK / 16; ++k)
-                            mma_pair_f16_e(e, d, smem_desc_k_sw128(x + 32 * k), smem_desc_k_sw128(x + 32 * k), idesc, kb > 0 || k > 0 ? 1u : 0u);
-                    });
+                            mma_pair_f16_e(e, d, smem_desc_k_sw128(x + 32 * k), smem_desc_k_sw128(y + 32 * k), idesc,
+                                           pass > 0 || kb > 0 || k > 0 ? 1u : 0u);
+                        release(x);
+                        if (pass > 0) release(y);
+                    }
                 done();
                 // B0; T' = B0 G; G1 = B0 T; B1; B1 B0
 #pragma unroll 1
                 for (int i = 1; i < (q.pair ? 6 : 2); ++i) {
                     wait_stored();
                     free_buffer();
-                    for (int pass = 0; pass < (i == 2 && q.glo ? 2 : 1); ++pass)
-                        square(i == 2 || i == 3 ? 2 : i == 5 ? 1 : 0, i == 3 ? 1 : i == 5 ? 2 : pass, pass > 0);
+                    const uint32_t a = smem_u32(sm.square[i == 2 || i == 3 ? 2 : i == 5 ? 1 : 0]);
+                    const uint32_t b = smem_u32(sm.square[i == 3 ? 1 : i == 5 ? 2 : 0]), g_lo = smem_u32(sm.square[1]);
+                    for (int pass = 0; pass < (precise ? 3 : i == 2 && q.glo ? 2 : 1); ++pass)
+                        square(pass == 2 ? a + kBlockBytes : a, pass != 1 ? b : precise ? b + kBlockBytes : g_lo, pass > 0);
                     done();
                 }
                 wait_stored();
                 for (int t = 0; t < w.tiles && ok; ++t) {
                     free_buffer();
                     const uint32_t dx = tmem + 256u * (local & 1), a = smem_u32(sm.square[0]);
-                    for (int kb = 0; kb < w.kb_m * (s == 0 && p.lo ? 2 : 1) && ok; ++kb)
-                        ring_block([&](uint32_t x) {
+                    for (int kb = 0; kb < w.kb_m * x_passes(p.lo, precise, s); ++kb) {
+                        const uint32_t x = next_block();
+                        if (!ok) break;
+                        const uint32_t from = kb / w.kb_m == 2 ? a + kBlockBytes : a + kBlockBytes * (kb % w.kb_m);
 #pragma unroll
-                            for (int k = 0; k < kBK / 16; ++k)
-                                mma_pair_f16_e(e, dx, smem_desc_k_sw128(a + kBlockBytes * (kb % w.kb_m) + 32 * k),
-                                               smem_desc_mn_sw128(x + 2048 * k, 8192), kXIdesc, kb > 0 || k > 0 ? 1u : 0u);
-                        });
+                        for (int k = 0; k < kBK / 16; ++k)
+                            mma_pair_f16_e(e, dx, smem_desc_k_sw128(from + 32 * k), smem_desc_mn_sw128(x + 2048 * k, 8192), kXIdesc,
+                                           kb > 0 || k > 0 ? 1u : 0u);
+                        release(x);
+                    }
                     done();
                 }
             }
@@ -1212,10 +1246,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         uint32_t pieces = 0;
         int local = 0;
         bool ok = true;
+        // one 32 x 32 block by way of the next half of the staging tile
+        auto store = [&](const CUtensorMap *map, const uint32_t(&x)[16], int col, int row, int z) {
+            uint8_t *to = stage_buf + 2048 * (pieces & 1u);
+            if (e) bulk_wait_group_read<1>();
+            __syncwarp();
+            stage_rows(to, x, lane);
+            fence_proxy_async_smem();
+            __syncwarp();
+            tma_store_3d_e(e, map, to, col, row, z);
+            ++pieces;
+        };
         pdl_wait();
         for (int u = pair; u < p.units && ok; u += pairs) {
             const SmallUnit w = small_unit(p, u);
             const SmallClass &c = p.cls[w.cls];
+            const bool precise = PRECISE && c.precise;
             const int row0 = w.h * rank + 32 * q, row = 32 * q + lane;  // of X, of the CTA's
             const bool some = 32 * q < w.h;
             auto wait_acc = [&] {
@@ -1234,8 +1280,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 if (lane == 0) mbar_arrive_cluster_cta_scope(bar);
             };
             // pieces of 8 values of 32 columns from col on
-            auto piece = [&](int at, int col, int k) {
-                return reinterpret_cast<uint4 *>(sm.square[at] + kBlockBytes * (col >> 6) + 128 * row + 16 * ((((col & 63) >> 3) + k) ^ (row & 7)));
+            auto piece = [&](int at, int block, int col, int k) {
+                return reinterpret_cast<uint4 *>(sm.square[at] + kBlockBytes * (block + (col >> 6)) + 128 * row +
+                                                 16 * ((((col & 63) >> 3) + k) ^ (row & 7)));
             };
             // alpha D, or alpha D + beta G + gamma I, of m x m, to square `to`; the digits that it loses to `lo`
             auto square = [&](int to, int lo, float alpha, bool poly, float beta, float gamma) {
@@ -1249,17 +1296,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int k = 0; k < 32; ++k) v[k] = alpha * __uint_as_float(r[k]);
                     if (poly) {
+#pragma unroll 1
+                        for (int block = 0; block < (precise ? 2 : 1); ++block)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const uint4 g = *piece(0, col, k);
-                            const uint32_t xs[4] = {g.x, g.y, g.z, g.w};
+                            for (int k = 0; k < 4; ++k) {
+                                const uint4 g = *piece(0, block, col, k);
+                                const uint32_t xs[4] = {g.x, g.y, g.z, g.w};
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&xs[j]));
-                                v[8 * k + 2 * j] = fmaf(beta, f.x, v[8 * k + 2 * j]);
-                                v[8 * k + 2 * j + 1] = fmaf(beta, f.y, v[8 * k + 2 * j + 1]);
+                                for (int j = 0; j < 4; ++j) {
+                                    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&xs[j]));
+                                    v[8 * k + 2 * j] = fmaf(beta, f.x, v[8 * k + 2 * j]);
+                                    v[8 * k + 2 * j + 1] = fmaf(beta, f.y, v[8 * k + 2 * j + 1]);
+                                }
                             }
-                        }
                         if (col == row0) {
 #pragma unroll
                             for (int k = 0; k < 32; ++k)
@@ -1275,7 +1324,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int k = 0; k < 16; ++k) x[k] = half2_bits(v[2 * k], v[2 * k + 1]);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) *piece(to, col, k) = make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+                    for (int k = 0; k < 4; ++k) *piece(to, 0, col, k) = make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
                     if (lo >= 0) {
 #pragma unroll
                         for (int k = 0; k < 16; ++k) {
@@ -1283,7 +1332,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                             x[k] = half2_bits(v[2 * k] - f.x, v[2 * k + 1] - f.y);
                         }
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) *piece(lo, col, k) = make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+                        for (int k = 0; k < 4; ++k) *piece(lo, precise ? 1 : 0, col, k) = make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
                     }
                 }
                 read_acc();
@@ -1299,8 +1348,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 for (int i = 0; i < (f.pair ? 6 : 2) && ok; ++i) {
                     const bool poly = i == 1 || i == 4;
                     const float alpha = i == 0 ? (s == 0 ? f.g * (r * r) : f.g) : i == 1 ? f.c0 : i == 2 ? f.t : i == 3 ? f.g1 : i == 4 ? f.c1 : f.p;
-                    square(i == 1 && f.pair ? 2 : i == 2 || i == 4 ? 1 : 0, i == 0 && f.glo ? 1 : -1, alpha, poly, i == 1 ? f.b0 : f.b1,
-                           i == 1 ? f.a0 : f.a1);
+                    const int to = i == 1 && f.pair ? 2 : i == 2 || i == 4 ? 1 : 0;
+                    square(to, precise ? to : i == 0 && f.glo ? 1 : -1, alpha, poly, i == 1 ? f.b0 : f.b1, i == 1 ? f.a0 : f.a1);
                 }
                 if (!ok) break;
                 arrive_own(own_ring);  // the last product of squares was complete
@@ -1323,14 +1372,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                             uint32_t x[16];
 #pragma unroll
                             for (int k = 0; k < 16; ++k) x[k] = half2_bits(v[2 * k], v[2 * k + 1]);
-                            uint8_t *to = stage_buf + 2048 * (pieces & 1u);
-                            if (e) bulk_wait_group_read<1>();
-                            __syncwarp();
-                            stage_rows(to, x, lane);
-                            fence_proxy_async_smem();
-                            __syncwarp();
-                            tma_store_3d_e(e, &c.block[(s + 1) & 1], to, col, row0, w.z);
-                            ++pieces;
+                            store(&c.block[(s + 1) & 1], x, col, row0, w.z);
+                            if constexpr (PRECISE) {
+                                if (precise) {
+#pragma unroll
+                                    for (int k = 0; k < 16; ++k) {
+                                        const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&x[k]));
+                                        x[k] = half2_bits(v[2 * k] - y.x, v[2 * k + 1] - y.y);
+                                    }
+                                    store(&p.lo_of[w.cls].block[(s + 1) & 1], x, col, row0, w.z);
+                                }
+                            }
                         }
                     }
                     read_acc();
@@ -1425,8 +1477,8 @@ int lo_of(int b) { return b == kX ? kXlo : b == kXnext ? kXnextLo : b + kGlo; }
 // Matrices of few rows keep all digits: every result of a product is hi + lo, every
 // product of two has three passes (hi hi, hi lo, lo hi).  A few rows do not average
 // roundings out: u of 4 to 16 was off by up to 6.5 10^-3 of itself, of 17 to 32 by 2.9,
-// of more by at most 1.9; with them it is 0.4.  They are no gift (48 x 80: 85.7 us a call
-// with passes and lo's, 70.5 without), hence 32.  The Gram matrix of longer rows takes
+// of more by at most 1.9; with them it is 0.4.  They are no gift (48 x 80, a launch for
+// each product: 85.7 us a call with passes and lo's, 70.5 without), hence 32.  The Gram matrix of longer rows takes
 // one pass: it averages over them.
 constexpr int64_t kPrecise = 32, kPreciseGram = 512;
 bool is_precise(int64_t m) { return m <= kPrecise; }
@@ -1581,12 +1633,13 @@ cudaError_t product_attribute() {
     if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev].store(true, std::memory_order_relaxed);
     return e;
 }
+template <bool PRECISE>
 cudaError_t small_attribute() {
     static std::atomic<bool> done[64];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess || (dev >= 0 && dev < 64 && done[dev].load(std::memory_order_relaxed))) return e;
-    e = cudaFuncSetAttribute(muon_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(SmallSmem)));
+    e = cudaFuncSetAttribute(muon_small_kernel<PRECISE>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(SmallSmem)));
     if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev].store(true, std::memory_order_relaxed);
     return e;
 }
@@ -1698,10 +1751,11 @@ struct Products {
         double launches = 0, all = 0, longest = 0;
         for (int k = 0, at = 0; k < c.classes; ++k) {
             const int64_t m = c.shape[k].m, units = c.first[k + 1] - c.first[k];
-            if (is_precise(m) || m > kSmallMost) return false;
+            if (m > kSmallMost) return false;
             const double kb_m = static_cast<double>((m + kBK - 1) / kBK), kb_n = static_cast<double>((c.shape[k].n + kBK - 1) / kBK);
-            const double one = products * (1.24 + 0.476 * kb_m) + turns * (0.5 + 0.065 * kb_m) * kb_n;
-            launches = std::max(launches, products * (2.75 + 0.25 * kb_m) + turns * 0.17 * kb_n);
+            const double passes = is_precise(m) ? 1.2 : 1.0;
+            const double one = passes * (products * (1.24 + 0.476 * kb_m) + turns * (0.5 + 0.065 * kb_m) * kb_n);
+            launches = std::max(launches, passes * (products * (2.75 + 0.25 * kb_m) + turns * 0.17 * kb_n));
             all += one * static_cast<double>(units);
             for (int64_t i = 0; i < units; ++i, ++at)  // (dealt in turn, the longest first)
                 if (at % pairs == 0) longest += one;
@@ -1731,32 +1785,42 @@ struct Products {
     }
 
     // All products, where small.
+    template <bool PRECISE>
     cudaError_t run_small(const StepPair *step, int n, bool lo, const MuonScale *scale) const {
-        MuonSmall p{};
+        const cudaError_t e = small_attribute<PRECISE>();
+        if (e != cudaSuccess) return e;
+        MuonSmall<PRECISE> p{};
         for (int k = 0; k < c.classes; ++k) {
-            SmallClass &to = p.cls[p.classes++];
+            SmallClass &to = p.cls[p.classes];
             for (int i = 0; i < 2; ++i) {
                 const int x = i == 0 ? kX : kXnext;
                 to.rows[i] = rows128[k][x];
                 to.cols[i] = rows64[k][x];
                 to.block[i] = block[k][x];
+                if constexpr (PRECISE) {
+                    if (!precise(k)) continue;
+                    SmallLo &more = p.lo_of[p.classes];
+                    more.rows[i] = rows128[k][lo_of(x)];
+                    more.block[i] = block[k][lo_of(x)];
+                    if (i == 1) more.next_cols = rows64[k][lo_of(x)];
+                }
             }
             to.lo = rows64[k][kXlo];
+            to.precise = precise(k);
+            to.passes = to.precise && c.shape[k].n <= kPreciseGram ? 3 : 1;
             to.m = static_cast<int>(c.shape[k].m);
             to.n = static_cast<int>(c.shape[k].n);
             to.first = c.first[k];
             p.units += c.first[k + 1] - c.first[k];
-            p.unit0[p.classes] = p.units;
+            p.unit0[++p.classes] = p.units;
         }
-        const cudaError_t e = small_attribute();
-        if (e != cudaSuccess) return e;
         std::copy(step, step + n, p.step);
         p.steps = n;
         p.lo = lo;
         p.scale = scale;
         p.status = status;
         p.wait_ns = wait_timeout_ns();
-        return launch_pdl(muon_small_kernel, dim3(2 * std::min(p.units, pairs)), dim3(kThreads), sizeof(SmallSmem), s, p, out);
+        return launch_pdl(muon_small_kernel<PRECISE>, dim3(2 * std::min(p.units, pairs)), dim3(kThreads), sizeof(SmallSmem), s, p, out);
     }
 
     // D = A B^T or (kTimesX) A X, of buffers.
@@ -1908,7 +1972,11 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
         sx = next;
         most = bound;
     }
-    if (run.small) return e == cudaSuccess ? run.run_small(plan, n_plan, n_steps > 1, in.scale) : e;
+    if (run.small && e == cudaSuccess) {
+        bool any = false;
+        for (int k = 0; k < c.classes; ++k) any = any || is_precise(c.shape[k].m);
+        return any ? run.run_small<true>(plan, n_plan, n_steps > 1, in.scale) : run.run_small<false>(plan, n_plan, n_steps > 1, in.scale);
+    }
     for (int i = 0; i < n_plan && e == cudaSuccess; ++i) {
         const StepPair &f = plan[i];
         const MuonScale *scale = i == 0 ? in.scale : nullptr;

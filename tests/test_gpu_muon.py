@@ -146,9 +146,10 @@ def test_narrow_and_wide_tiles_agree():
 
 
 @pytest.mark.parametrize("steps", [1, 2, 3, 5, 6])
-def test_a_pair_for_each_matrix_and_launches_agree(steps):
+@pytest.mark.parametrize("shapes", [[(48, 80), (33, 40), (700, 64), (127, 129), (256, 256), (130, 512), (65, 300)],
+                                    [(20, 40), (32, 600), (5, 5), (1, 7), (400, 31), (32, 513), (16, 512), (64, 64)]])
+def test_a_pair_for_each_matrix_and_launches_agree(shapes, steps):
     """Few rows, whose products one kernel takes; beside a larger matrix each product is a launch: the same sums."""
-    shapes = [(48, 80), (33, 40), (700, 64), (127, 129), (256, 256), (130, 512), (65, 300)]
     mats = [(M.gradient(r, c, r + c).to(DEV), M.gradient(r, c, 9).to(DEV)) for r, c in shapes]
     together, beside = ([(g, m.clone(), torch.empty_like(g)) for g, m in mats] for _ in range(2))
     coefficients = (M.STEPS * 2)[:steps]
