@@ -20,14 +20,15 @@ def update(g, m, mu, nesterov):
     return m, g + mu * m if nesterov else m
 
 
-def exact(v, steps=STEPS):
+def exact(v, steps=STEPS, kept=1.0):
+    """kept: what sums over X's rows leave of themselves."""
     v = v.double()
     tall = v.shape[0] > v.shape[1]
     x = v.T if tall else v
     norm = x.norm()
     x = x / norm if norm > 0 else x
     for a, b, c in steps:
-        g = x @ x.T
+        g = kept * (x @ x.T)
         x = a * x + (b * g + c * (g @ g)) @ x
     return x.T if tall else x
 
@@ -100,10 +101,13 @@ def bound(v, u_type, steps=STEPS):
     """What u may be off by in the 2-norm: twice the model's error, which is one draw of the same roundings; what the model lacks or draws of
     few values may differ by; and half a step of u's type.  The second is 2^-9 (the last product's two FP16 operands are each within 2^-11
     and of norm at most 2 to u's 1), or where every number has 22 digits what FP32's sums add: 2^-22 each, of which the first steps' are
-    blown up 3.4445^5 = 485 times, so 2^-13."""
+    blown up 3.4445^5 = 485 times, so 2^-13.  Long rows add what their sums in FP32 lose: an entry of G = X X^T is a sum of n products, each
+    addition of which may cut off a step, 2^-23 of the sum, all in the same direction; so what u changes by where each G is 1 - n 2^-23 of
+    itself."""
     e = exact(v, steps)
     more = 2.0 ** -13 if min(v.shape) <= PRECISE else 2.0 ** -9
-    return e, 2 * float((model(v, steps) - e).norm()) + (more + (2.0 ** -8 if u_type == torch.bfloat16 else 2.0 ** -24)) * float(e.norm())
+    return e, (2 * float((model(v, steps) - e).norm()) + float((exact(v, steps, 1 - max(v.shape) * 2.0 ** -23) - e).norm()) +
+               (more + (2.0 ** -8 if u_type == torch.bfloat16 else 2.0 ** -24)) * float(e.norm()))
 
 
 def gradient(r, c, seed, kind="mixed"):

@@ -34,7 +34,7 @@ def check(u, v, u_type, steps=M.STEPS):
 
 SHAPES = [(1, 1), (1, 5), (5, 1), (1, 300), (3, 7), (8, 8), (48, 80), (64, 64), (127, 129), (129, 127), (128, 256), (256, 128), (257, 130),
           (130, 259), (300, 1000), (1000, 300), (512, 512), (515, 384), (96, 2048), (2050, 70), (255, 400), (256, 2100), (8, 32), (3000, 9),
-          (32, 600), (600, 33), (20, 512), (513, 24), (320, 3000)]
+          (32, 600), (600, 33), (20, 512), (513, 24), (320, 3000), (3, 70001), (70001, 2)]
 
 
 @pytest.mark.parametrize("r,c", SHAPES)
@@ -251,10 +251,11 @@ def test_twice_the_same_and_on_another_stream():
     assert torch.equal(u[0], u[1]) and torch.equal(u[0], u[2])
 
 
-def test_two_calls_at_once():
+@pytest.mark.parametrize("r,c", [(300, 600), (60, 100), (20, 30)])
+def test_two_calls_at_once(r, c):
     """On two streams, each with its own scratch."""
-    gs = [M.gradient(300, 600, i).to(DEV) for i in range(2)]
-    want, got = ([torch.empty(300, 600, device=DEV) for _ in range(2)] for _ in range(2))
+    gs = [M.gradient(r, c, i).to(DEV) for i in range(2)]
+    want, got = ([torch.empty(r, c, device=DEV) for _ in range(2)] for _ in range(2))
     for g, u in zip(gs, want):
         directions([(g, None, u)])
     streams = [torch.cuda.Stream() for _ in range(2)]
@@ -269,10 +270,11 @@ def test_two_calls_at_once():
         assert torch.equal(a, b)
 
 
-def test_in_a_graph():
-    g, m = M.gradient(130, 260, 1).to(DEV), M.gradient(130, 260, 2).to(DEV)
+@pytest.mark.parametrize("r,c", [(130, 260), (300, 520), (24, 40)])
+def test_in_a_graph(r, c):
+    g, m = M.gradient(r, c, 1).to(DEV), M.gradient(r, c, 2).to(DEV)
     eager = m.clone()
-    u, want = torch.empty(130, 260, dtype=BF, device=DEV), torch.empty(130, 260, dtype=BF, device=DEV)
+    u, want = torch.empty(r, c, dtype=BF, device=DEV), torch.empty(r, c, dtype=BF, device=DEV)
     table = P.muon_table([(g, m, u)])
     ws = torch.empty(P.puro_muon_direction_workspace_size(table), dtype=torch.uint8, device=DEV)
     graph = torch.cuda.CUDAGraph()
