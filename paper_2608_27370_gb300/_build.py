@@ -25,7 +25,7 @@ NATIVE = os.path.join(PKG, "_native.so")
 BINDING = os.path.join(CSRC, "binding.cpp")
 NATIVE_FOR = os.path.join(BUILD, "native_for.txt")  # what _native.so was compiled for
 SOURCES = ["api.cu", "quantize.cu", "gemm.cu", "noalloc.cu", "muonh.cu", "qknorm.cu", "rope.cu", "muon.cu", "act.cu", "skinny.cu"]
-HEADERS = ["ptx.cuh", "internal.h", "quant_math.cuh", "act_math.cuh", "rotation.cuh", "register_check.h", "skinny_plan.h"]
+HEADERS = ["ptx.cuh", "internal.h", "quant_math.cuh", "act_math.cuh", "rotation.cuh", "register_check.h", "skinny_plan.h", "muon_plan.h"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
               "-Xcompiler", "-Wall", "--expt-relaxed-constexpr", "-I", INCLUDE, "-I", CSRC]

@@ -45,13 +45,12 @@
 #include <type_traits>
 
 #include "internal.h"
+#include "muon_plan.h"
 #include "ptx.cuh"
 
 namespace puro {
 namespace {
 
-constexpr int kMaxClasses = 8;   // shapes of one launch (their tensor maps are kernel parameters)
-constexpr int kMaxMats = 128;    // matrices of one launch
 constexpr int kMaxSteps = 64;
 constexpr int32_t kStatusTimeout = 4;  // PURO_ERR_TIMEOUT
 constexpr uint64_t kDrainNs = 2000000000ull, kSettleNs = 200000ull;
@@ -488,11 +487,10 @@ __global__ void __launch_bounds__(kInThreads, 3) muon_norm_kernel(const __grid_c
 // factor of B X), which the tensor cores read as it lies (MN-major).  The matrices
 // of one shape are a class: one tensor map each for A, B and D with the matrix as
 // the third coordinate.
-constexpr int kBM = 128, kBK = 64;
+constexpr int kBM = 128;
 constexpr int kThreads = 384;
 constexpr int kEpiWarps = 8;
 constexpr int kTmemCols = 512;
-constexpr int kMaxSegments = 16;
 
 enum Epilogue : int {
     kStore = 0,  // alpha D as hi (and lo), symmetric
@@ -503,20 +501,6 @@ enum Epilogue : int {
 
 struct MuonMaps {
     CUtensorMap a, a_lo, b, b_lo, d, d_lo;  // a: box 64 x 128; b: 64 x BN / 2, X_MAJOR 64 x 64; d: 32 x 32 (64-byte swizzle)
-};
-// The tiles of a product, and who takes them.
-struct Tiles {
-    int bn;
-    int classes, units;
-    int unit0[kMaxClasses + 1];  // first tile of each class
-    int per[kMaxClasses];        // tiles of a matrix
-    int tiles_n[kMaxClasses], tiles_m[kMaxClasses];
-    int rows[kMaxClasses], cols[kMaxClasses];  // of D
-    int kb[kMaxClasses];         // k-blocks of B (of lo as many more)
-    int first[kMaxClasses];      // the class's first matrix
-    int segments;                // of tiles, each dealt to a range of the pairs in turn
-    int from[kMaxSegments], to[kMaxSegments];
-    int16_t pair0[kMaxSegments], pairs[kMaxSegments];
 };
 struct MuonPhase : Tiles {
     MuonMaps maps[kMaxClasses];
@@ -553,57 +537,6 @@ struct ProductSmem {
     uint32_t tmem_base;
     volatile int abort_flag;
 };
-// A pair's units, in order.
-struct Walk {
-    int segment = 0, u = -1;
-    PURO_DEV int next(const MuonPhase &p, int pair) {
-        for (; segment < p.segments; ++segment, u = -1) {
-            if (u < 0) {
-                const int i = pair - p.pair0[segment];
-                if (i < 0 || i >= p.pairs[segment]) continue;
-                u = p.from[segment] + i;
-            } else {
-                u += p.pairs[segment];
-            }
-            if (u < p.to[segment]) return u;
-        }
-        return -1;
-    }
-};
-struct Unit {
-    int cls, z, m0, n0, kb;
-    bool mirror;  // off the diagonal of a symmetric D: stored transposed as well
-};
-
-template <int BN, bool SYM>
-PURO_DEV Unit unit_of(const MuonPhase &p, int u) {
-    Unit w;
-    w.cls = 0;
-    while (w.cls + 1 < p.classes && u >= p.unit0[w.cls + 1]) ++w.cls;
-    int i = u - p.unit0[w.cls];
-    w.z = i / p.per[w.cls];
-    i -= w.z * p.per[w.cls];
-    w.kb = p.kb[w.cls];
-    if constexpr (SYM) {
-        constexpr int kAcross = 256 / BN;
-        const int n = p.tiles_n[w.cls];
-        int row = 0;
-        while (i >= n - kAcross * row) {
-            i -= n - kAcross * row;
-            ++row;
-        }
-        w.m0 = 256 * row;
-        w.n0 = BN * (kAcross * row + i);
-        w.mirror = w.n0 >= w.m0 + 256;
-    } else {  // the rows of B fastest: a wave shares columns of X
-        const int tm = p.tiles_m[w.cls];
-        w.m0 = 256 * (i % tm);
-        w.n0 = BN * (i / tm);
-        w.mirror = false;
-    }
-    return w;
-}
-
 template <class Smem>
 PURO_DEV bool wait_or_abort(Smem &sm, uint64_t *bar, uint32_t parity, uint64_t ns, int32_t *status, int lane) {
     if (__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity)) ||
@@ -994,7 +927,7 @@ struct MuonSmall {
     int32_t *status;
     uint64_t wait_ns;
 };
-constexpr int kSmallMost = 256, kSmallStages = 8, kSquareBytes = 4 * kBM * 128;
+constexpr int kSmallStages = 8, kSquareBytes = 4 * kBM * 128;
 struct SmallSmem {
     // 0: G, G1, B1 B0 (or the last B0).  1: G's lo, T', B1.  2: B0.  Chunks of 64 columns,
     // [128][64] with the 128-byte swizzle.  1 and 2 are the ring of X's k-blocks meanwhile.
@@ -1406,82 +1339,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 }
 
 // ------------------------------------------------------------------- host
-int64_t align_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
-
-struct Shape {
-    int64_t m, n;
-    bool operator==(const Shape &o) const { return m == o.m && n == o.n; }
-};
-Shape shape_of(const puro_muon_matrix_t &a) { return {std::min(a.rows, a.cols), std::max(a.rows, a.cols)}; }
-bool empty(const puro_muon_matrix_t &a) { return a.rows == 0 || a.cols == 0; }
-
-template <class Less>
-void sort_few(int *v, int n, Less less) {
-    for (int i = 1; i < n; ++i)
-        for (int j = i; j > 0 && less(v[j], v[j - 1]); --j) std::swap(v[j], v[j - 1]);
-}
-
-// The matrices of one series of launches: some in a row of the table, by shape.
-struct Chunk {
-    int count = 0, classes = 0;
-    int mats[kMaxMats];  // their places in the table, class by class
-    Shape shape[kMaxClasses];
-    int first[kMaxClasses + 1];
-};
-// Takes matrices from `at` on while they fit one chunk, and returns where it ended.
-int take_chunk(const puro_muon_matrix_t *mats, int at, int count, Chunk *c) {
-    *c = Chunk{};
-    int cls[kMaxMats];
-    int n[kMaxClasses] = {};
-    for (; at < count && c->count < kMaxMats; ++at) {
-        if (empty(mats[at])) continue;
-        const Shape s = shape_of(mats[at]);
-        int k = 0;
-        while (k < c->classes && !(c->shape[k] == s)) ++k;
-        if (k == kMaxClasses) break;
-        if (k == c->classes) c->shape[c->classes++] = s;
-        cls[c->count] = k;
-        c->mats[c->count++] = at;
-        ++n[k];
-    }
-    // classes of the longest rows first: their tiles are the long ones
-    int order[kMaxClasses], place[kMaxClasses];
-    for (int k = 0; k < c->classes; ++k) order[k] = k;
-    sort_few(order, c->classes, [&](int a, int b) {
-        return c->shape[a].n != c->shape[b].n ? c->shape[a].n > c->shape[b].n
-                                              : c->shape[a].m != c->shape[b].m ? c->shape[a].m > c->shape[b].m : a < b;
-    });
-    Shape sorted[kMaxClasses];
-    int next[kMaxClasses];
-    c->first[0] = 0;
-    for (int k = 0; k < c->classes; ++k) {
-        place[order[k]] = k;
-        sorted[k] = c->shape[order[k]];
-        next[k] = c->first[k];
-        c->first[k + 1] = c->first[k] + n[order[k]];
-    }
-    int by[kMaxMats];
-    for (int i = 0; i < c->count; ++i) by[next[place[cls[i]]]++] = c->mats[i];
-    std::copy(by, by + c->count, c->mats);
-    std::copy(sorted, sorted + c->classes, c->shape);
-    return at;
-}
-
 constexpr int64_t kAlign = 256;
 
-enum Form { kGram, kSquareSym, kSquare, kTimesX, kForms };  // X X^T; m x m, symmetric or not; m x m times X
 // Square ones; X, its lo, the next X; the others' lo where a class keeps all (is_precise).
 enum Buffer { kG, kB0, kT, kB1, kX, kXlo, kXnext, kXnextLo, kGlo, kB0lo, kTlo, kB1lo, kBuffers, kNone = -1 };
 bool is_square(int b) { return b < kX || b >= kGlo; }
 int lo_of(int b) { return b == kX ? kXlo : b == kXnext ? kXnextLo : b + kGlo; }
-// Matrices of few rows keep all digits: every result of a product is hi + lo, every
-// product of two has three passes (hi hi, hi lo, lo hi).  A few rows do not average
-// roundings out: u of 4 to 16 was off by up to 6.5 10^-3 of itself, of 17 to 32 by 2.9,
-// of more by at most 1.9; with them it is 0.4.  They are no gift (48 x 80, a launch for
-// each product: 85.7 us a call with passes and lo's, 70.5 without), hence 32.  The Gram matrix of longer rows takes
-// one pass: it averages over them.
-constexpr int64_t kPrecise = 32, kPreciseGram = 512;
-bool is_precise(int64_t m) { return m <= kPrecise; }
 
 // Scratch of a chunk.
 struct Scratch {
@@ -1546,80 +1409,9 @@ bool plan_step(const double *abc, double most, Step *s) {
     }
     return s->most_p < 1024 && s->most_out < 1024;
 }
-// What a k-block of a 256 x 128 tile takes next to one of 256 x 256, and a tile's
-// epilogue that no product hides, in k-blocks.
-constexpr double kNarrowBlock = 0.65, kTileBlocks = 4.0;
 constexpr double kMargin = 1.0 + 1.0 / 64;  // of a bound, for what roundings add
 // The power of two that puts values up to `most` within FP16, with half of it to spare.
 double pow2_for(double most) { return std::ldexp(1.0, most > 0 ? std::min(100, std::ilogb(32768.0 / (most * kMargin))) : 14); }
-
-// Deals n units of a cost to the pairs, least loaded first: windows of neighbouring
-// pairs with the same load.
-struct Dealer {
-    struct Window {
-        int from, len;
-        double load;
-    };
-    Window w[2 * kMaxSegments];
-    int windows = 1;
-    double most = 0;
-    Dealer(int pairs) { w[0] = {0, pairs, 0}; }
-
-    void deal(Tiles *p, int first, int n, double cost) {
-        int u = first;
-        const int end = first + n;
-        while (u < end) {
-            if (p->segments >= kMaxSegments - 1 || windows >= 2 * kMaxSegments - 1) {  // the rest in turn
-                int all = 0;
-                for (int i = 0; i < windows; ++i) all += w[i].len;
-                segment(p, u, end, 0, all);
-                most += cost * ((end - u + all - 1) / all);
-                return;
-            }
-            int low = 0;
-            double next = INFINITY;
-            for (int i = 1; i < windows; ++i)
-                if (w[i].load < w[low].load) low = i;
-            for (int i = 0; i < windows; ++i)
-                if (i != low) next = std::min(next, w[i].load);
-            Window &x = w[low];
-            const double rounds_most = std::isfinite(next) ? std::max(1.0, std::ceil((next - x.load) / cost - 1e-9)) : 1e9;
-            const int rounds = static_cast<int>(std::min<double>(rounds_most, (end - u) / x.len));
-            if (rounds > 0) {
-                segment(p, u, u + rounds * x.len, x.from, x.len);
-                u += rounds * x.len;
-                x.load += rounds * cost;
-                most = std::max(most, x.load);
-            } else {  // fewer than a round: the window splits
-                const int rem = end - u;
-                segment(p, u, end, x.from, rem);
-                for (int i = windows; i > low + 1; --i) w[i] = w[i - 1];
-                ++windows;
-                w[low + 1] = {x.from + rem, x.len - rem, x.load};
-                w[low].len = rem;
-                w[low].load += cost;
-                most = std::max(most, w[low].load);
-                u = end;
-            }
-            for (int i = 0; i + 1 < windows;) {  // neighbours that are level become one
-                if (std::fabs(w[i].load - w[i + 1].load) < 1e-9 * cost) {
-                    w[i].len += w[i + 1].len;
-                    for (int j = i + 1; j + 1 < windows; ++j) w[j] = w[j + 1];
-                    --windows;
-                } else {
-                    ++i;
-                }
-            }
-        }
-    }
-    static void segment(Tiles *p, int from, int to, int pair0, int pairs) {
-        const int s = p->segments++;
-        p->from[s] = from;
-        p->to[s] = to;
-        p->pair0[s] = static_cast<int16_t>(pair0);
-        p->pairs[s] = static_cast<int16_t>(pairs);
-    }
-};
 
 // (once per device: it costs as much of the host's time as an eighth of a launch)
 template <int BN, bool X_MAJOR, int EPI>
@@ -1703,70 +1495,12 @@ struct Products {
     uint16_t *buffer(int b, int k) const { return reinterpret_cast<uint16_t *>(ws + at.buffer[b][k]); }
     bool precise(int k) const { return is_precise(c.shape[k].m); }
 
-    // Tiles of 256 x bn, dealt to the pairs; returns what the longest-working pair has
-    // to do, in k-blocks of 256 x 256.
-    double deal(Tiles *p, int form, int bn) const {
-        *p = Tiles{};
-        p->bn = bn;
-        Dealer dealer(pairs);
-        int order[kMaxClasses], n[kMaxClasses];
-        for (int k = 0; k < c.classes; ++k) {
-            const int64_t m = c.shape[k].m, cols = form == kTimesX ? c.shape[k].n : m;
-            const int64_t tm = (m + 255) / 256, tn = (cols + bn - 1) / bn;
-            int64_t per = tm * tn;
-            if (form == kGram || form == kSquareSym) {
-                per = 0;
-                for (int64_t i = 0; i < tm; ++i) per += tn - 256 / bn * i;
-            }
-            order[k] = k;
-            n[k] = static_cast<int>(per) * (c.first[k + 1] - c.first[k]);
-            p->unit0[k] = p->units;
-            p->units += n[k];
-            p->per[k] = static_cast<int>(per);
-            p->tiles_m[k] = static_cast<int>(tm);
-            p->tiles_n[k] = static_cast<int>(tn);
-            p->rows[k] = static_cast<int>(m);
-            p->cols[k] = static_cast<int>(cols);
-            p->kb[k] = static_cast<int>(((form == kGram ? c.shape[k].n : m) + kBK - 1) / kBK);
-            p->first[k] = c.first[k];
-        }
-        p->classes = c.classes;
-        p->unit0[c.classes] = p->units;
-        sort_few(order, c.classes, [&](int a, int b) { return p->kb[a] != p->kb[b] ? p->kb[a] > p->kb[b] : a < b; });
-        const double block_cost = bn == 256 ? 1.0 : kNarrowBlock;
-        for (int i = 0; i < c.classes; ++i)
-            dealer.deal(p, p->unit0[order[i]], n[order[i]],
-                        block_cost * (p->kb[order[i]] * (precise(order[i]) ? 3 : 1) + kTileBlocks));
-        return dealer.most;
-    }
-
-    // Whether a pair of CTAs for each matrix is faster than a launch for each product, by
-    // what both were measured to take (us): a launch 2.75, and 0.25 for each 64 rows; the
-    // long rows of the Gram matrix; where there are many, a good part of what a pair would
-    // have taken by itself.  Five steps on one [128, 128] 43 and 68, on [256, 256] 68 and 75,
-    // on [128, 1536] 82 and 79, on 64 of them 134 and 170, on [256, 1536] 117 and 85, on 64 of
-    // them 210 and 260.
-    bool small_pays(int n_steps) const {
-        const int products = 7 * (n_steps / 2) + 3 * (n_steps % 2), turns = (n_steps + 1) / 2;
-        double launches = 0, all = 0, longest = 0;
-        for (int k = 0, at = 0; k < c.classes; ++k) {
-            const int64_t m = c.shape[k].m, units = c.first[k + 1] - c.first[k];
-            if (m > kSmallMost) return false;
-            const double kb_m = static_cast<double>((m + kBK - 1) / kBK), kb_n = static_cast<double>((c.shape[k].n + kBK - 1) / kBK);
-            const double passes = is_precise(m) ? 1.2 : 1.0;
-            const double one = passes * (products * (1.24 + 0.476 * kb_m) + turns * (0.5 + 0.065 * kb_m) * kb_n);
-            launches = std::max(launches, passes * (products * (2.75 + 0.25 * kb_m) + turns * 0.17 * kb_n));
-            all += one * static_cast<double>(units);
-            for (int64_t i = 0; i < units; ++i, ++at)  // (dealt in turn, the longest first)
-                if (at % pairs == 0) longest += one;
-        }
-        return longest < launches + 0.8 * all / pairs;
-    }
-
     cudaError_t prepare() {
         for (int form = 0; form < kForms && !small; ++form) {
             Tiles narrow;
-            if (deal(&narrow, form, 128) < deal(&tiles[form], form, 256)) tiles[form] = narrow;
+            const double narrow_most = deal(c, pairs, &narrow, form, 128), wide_most = deal(c, pairs, &tiles[form], form, 256);
+            if (narrow_most < wide_most) tiles[form] = narrow;
+            if (!std::isfinite(std::min(narrow_most, wide_most))) return cudaErrorInvalidConfiguration;
         }
         for (int k = 0; k < c.classes; ++k)
             for (int b = 0; b < kBuffers; ++b) {
@@ -1892,7 +1626,7 @@ cudaError_t run_chunk(const puro_muon_matrix_t *mats, const Chunk &c, double mu,
     cudaError_t e = resident_pairs(&pairs);
     if (e != cudaSuccess) return e;
     Products run{c, at, ws, status, s, pairs};
-    run.small = run.small_pays(n_steps);
+    run.small = small_pays(c, pairs, n_steps);
     e = run.prepare();
     if (e != cudaSuccess) return e;
     // the update, its norm, X
