@@ -787,7 +787,8 @@ size_t puro_qk_norm_rope_workspace_size(int64_t tokens, int32_t q_heads, int32_t
  *                     fast_turns or more, evenly in the number of turns
  *   PURO_ROPE_INDEX   the same, keep_i evenly in i between the pairs at which the
  *                     number of turns is fast_turns (rounded down, at least 0) and
- *                     slow_turns (rounded up, at most the last pair)
+ *                     slow_turns (rounded up, at most rot_dim - 1: where that is past
+ *                     the last pair, the last pairs are partly kept)
  * The last two go with scale = 0.1 ln(factor) + 1 or 1 as the model was trained;
  * scale is the caller's.  rot_dim: a multiple of 16 up to 256; base > 1; factor >=
  * 1 (not read for NONE); trained_positions > 0 and fast_turns > slow_turns > 0

@@ -1149,15 +1149,16 @@ PURO_API puro_status_t puro_rope_frequencies(int32_t rot_dim, double base, int32
     if (scaling < PURO_ROPE_NONE || scaling > PURO_ROPE_INDEX) return PURO_ERR_INVALID_ARG;
     if (scaling != PURO_ROPE_NONE && !(factor >= 1.0 && std::isfinite(factor))) return PURO_ERR_INVALID_ARG;
     const bool ramp = scaling == PURO_ROPE_TURNS || scaling == PURO_ROPE_INDEX;
-    const double trained = static_cast<double>(trained_positions), pairs = rot_dim / 2;
+    const double trained = static_cast<double>(trained_positions);
     if (ramp && !(trained_positions > 0 && slow_turns > 0.0 && fast_turns > slow_turns && std::isfinite(fast_turns)))
         return PURO_ERR_INVALID_ARG;
     if (scaling == PURO_ROPE_BASE) base *= std::pow(factor, rot_dim / (rot_dim - 2.0));
     if (!std::isfinite(base)) return PURO_ERR_INVALID_ARG;
-    // PURO_ROPE_INDEX: the pairs at which the turns over the trained context are fast_turns and slow_turns
+    // PURO_ROPE_INDEX: the pairs at which the turns over the trained context are fast_turns and slow_turns; the
+    // published rule ends the ramp at channel rot_dim - 1, which is past the last pair
     auto pair_of = [&](double turns) { return rot_dim * std::log(trained / (turns * kTurn)) / (2.0 * std::log(base)); };
     const double lo = ramp ? std::max(0.0, std::floor(pair_of(fast_turns))) : 0.0;
-    const double hi = ramp ? std::min(pairs - 1.0, std::ceil(pair_of(slow_turns))) : 0.0;
+    const double hi = ramp ? std::min(rot_dim - 1.0, std::ceil(pair_of(slow_turns))) : 0.0;
     for (int i = 0; i < rot_dim / 2; ++i) {
         double w = std::pow(base, -2.0 * i / rot_dim), keep = 1.0;
         if (scaling == PURO_ROPE_LINEAR) keep = 0.0;
