@@ -743,6 +743,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         for (; u >= 0 && ok; next(), ++local) {
             const int buf = local & 1;
             ok = wait_or_abort(sm, &sm.tempty[buf], ((local >> 1) & 1u) ^ 1u, p.wait_ns, p.status, lane);
+            if (local == 0) pdl_wait();  // (the kernel before is not what a bounded wait is for)
             const uint32_t d = tmem + static_cast<uint32_t>(BN) * buf;
             const int kbs = w.kb * p.passes[w.cls];
             for (int kb = 0; kb < kbs && ok; ++kb) {
@@ -1122,6 +1123,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             for (int s = 0; s < p.steps && ok; ++s) {
                 const StepPair &q = p.step[s];
                 free_buffer();
+                if (local == 0) pdl_wait();  // (the kernel before is not what a bounded wait is for)
                 const uint32_t d = tmem + 256u * (local & 1);
                 for (int pass = 0; pass < (precise ? c.passes : 1); ++pass)
                     for (int kb = 0; kb < w.kb_n && ok; ++kb) {
