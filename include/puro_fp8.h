@@ -662,6 +662,8 @@ puro_status_t puro_muonh_step_grouped(const puro_muonh_matrix_t *mats, int32_t c
  *     aligned to their elements, faster at 16 bytes with strides and cols of multiples
  *     of 8.  momentum: fp32 [rows, cols], 4-byte aligned, updated in place, or NULL.  A
  *     matrix without rows or columns is skipped.  rows, cols <= 2^20.
+ *     No momentum and no u may share bytes with anything else of the table
+ *     (INVALID_ARG), but u may lie in its own matrix's grad.  Gradients may share theirs.
  *   momentum: from 0 to 1.
  *   coefficients: host array of `steps` (1 to 64) triples a, b, c.  They are refused
  *     (INVALID_ARG) where singular values of at most 1 could reach 1024, or |a + b t +

@@ -42,6 +42,8 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <memory>
+#include <new>
 #include <type_traits>
 
 #include "internal.h"
@@ -1779,6 +1781,11 @@ PURO_MUON_API puro_status_t puro_muon_direction_grouped(const puro_muon_matrix_t
         any = any || !empty(mats[i]);
     }
     if (!any) return PURO_OK;
+    {
+        const std::unique_ptr<Place[]> places(new (std::nothrow) Place[3 * static_cast<size_t>(count)]);
+        if (!places) return PURO_ERR_UNSUPPORTED;
+        if (writes_overlap(mats, count, places.get())) return PURO_ERR_INVALID_ARG;
+    }
     const size_t need = puro_muon_direction_workspace_size(mats, count);
     if (!workspace || !aligned(workspace, kAlign) || workspace_bytes < need) return PURO_ERR_INVALID_ARG;
     for (int at = 0; at < count;) {

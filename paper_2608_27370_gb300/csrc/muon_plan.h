@@ -98,6 +98,60 @@ struct Shape {
 inline Shape shape_of(const puro_muon_matrix_t &a) { return {std::min(a.rows, a.cols), std::max(a.rows, a.cols)}; }
 inline bool empty(const puro_muon_matrix_t &a) { return a.rows == 0 || a.cols == 0; }
 
+// The bytes of a matrix: rows that are `pitch` apart.
+struct Bytes {
+    uintptr_t from;
+    int64_t rows, row, pitch;
+    uintptr_t end() const { return from + static_cast<uintptr_t>((rows - 1) * pitch + row); }
+};
+inline Bytes bytes_of(const void *p, int64_t rows, int64_t cols, int64_t stride, int64_t size) {
+    const bool one = rows == 1 || stride == 0;  // (a stride of 0: one row, read again)
+    stride = std::min(stride, int64_t{1} << 40);  // (more than any memory has)
+    return {reinterpret_cast<uintptr_t>(p), one ? 1 : rows, cols * size, one ? cols * size : stride * size};
+}
+inline bool share(const Bytes &a, const Bytes &b) {
+    if (a.from >= b.end() || b.from >= a.end()) return false;
+    if (a.pitch == b.pitch && a.row <= a.pitch && b.row <= b.pitch) {  // columns of one wider matrix, say
+        const Bytes &x = a.from <= b.from ? a : b, &y = a.from <= b.from ? b : a;
+        const int64_t d = static_cast<int64_t>(y.from - x.from), row = d / x.pitch, at = d % x.pitch;
+        return (at < x.row && row < x.rows) || (at + y.row > x.pitch && row + 1 < x.rows);
+    }
+    const Bytes &few = a.rows <= b.rows ? a : b, &many = a.rows <= b.rows ? b : a;
+    for (int64_t i = 0; i < few.rows; ++i) {  // the first of `many` that ends behind the row's start
+        const uintptr_t start = few.from + static_cast<uintptr_t>(i * few.pitch);
+        const int64_t before = start < many.from + static_cast<uintptr_t>(many.row)
+                                   ? 0 : static_cast<int64_t>(start - many.from - static_cast<uintptr_t>(many.row)) / many.pitch + 1;
+        if (before < many.rows && many.from + static_cast<uintptr_t>(before * many.pitch) < start + static_cast<uintptr_t>(few.row)) return true;
+    }
+    return false;
+}
+// Whether something that a call writes lies where something else of it does.  Only a
+// matrix's u may lie in its own gradient, which has been read by then.  `at`: 3 count places.
+struct Place {
+    Bytes bytes;
+    int32_t mat;
+    enum : int32_t { kGrad, kMomentum, kU } what;
+};
+inline bool writes_overlap(const puro_muon_matrix_t *mats, int count, Place *at) {
+    int n = 0;
+    for (int i = 0; i < count; ++i) {
+        const puro_muon_matrix_t &a = mats[i];
+        if (empty(a)) continue;
+        at[n++] = {bytes_of(a.grad, a.rows, a.cols, a.grad_stride, a.grad_type == PURO_F32 ? 4 : 2), i, Place::kGrad};
+        if (a.momentum) at[n++] = {bytes_of(a.momentum, a.rows, a.cols, a.cols, 4), i, Place::kMomentum};
+        at[n++] = {bytes_of(a.u, a.rows, a.cols, a.u_stride, a.u_type == PURO_F32 ? 4 : 2), i, Place::kU};
+    }
+    std::sort(at, at + n, [](const Place &x, const Place &y) { return x.bytes.from < y.bytes.from; });
+    for (int i = 0; i < n; ++i)
+        for (int j = i + 1; j < n && at[j].bytes.from < at[i].bytes.end(); ++j) {
+            const Place &x = at[i], &y = at[j];
+            if (x.what == Place::kGrad && y.what == Place::kGrad) continue;
+            if (x.mat == y.mat && x.what != Place::kMomentum && y.what != Place::kMomentum) continue;
+            if (share(x.bytes, y.bytes)) return true;
+        }
+    return false;
+}
+
 template <class Less>
 void sort_few(int *v, int n, Less less) {
     for (int i = 1; i < n; ++i)

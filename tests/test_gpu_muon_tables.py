@@ -60,3 +60,28 @@ def test_whole_models(linears, layers):
     assert all(bool(torch.isfinite(u).all()) for _, _, u in mats)
     g, _, u = mats[per * (layers - 2) + 1]  # (the smallest linear: 64 bits on the host)
     check(u, g.cpu(), BF)
+
+
+@pytest.mark.parametrize("r,c", [(60, 200), (200, 60), (300, 520)])
+def test_u_in_its_own_gradient_and_columns_of_one_matrix(r, c):
+    """What may lie in the same place, or beside it in the same rows, gives what it gives apart."""
+    g = [gradient(r, c, i) for i in range(3)]
+    want = [torch.empty_like(x) for x in g]
+    directions([(x, None, u) for x, u in zip(g, want)])
+    wide = torch.cat(g, 1)
+    grads, out = [wide[:, i * c:(i + 1) * c] for i in range(3)], torch.empty(r, 3 * c, device=DEV)
+    directions([(x, None, out[:, i * c:(i + 1) * c]) for i, x in enumerate(grads)])
+    assert all(torch.equal(out[:, i * c:(i + 1) * c], u) for i, u in enumerate(want))
+    directions([(x, None, x) for x in grads])
+    assert all(torch.equal(x, u) for x, u in zip(grads, want))
+
+
+def test_overlaps_are_refused():
+    x, u = torch.zeros(9, 40, device=DEV), torch.empty(9, 40, device=DEV)
+    buf = torch.zeros(20, 40, device=DEV)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
+    for bad in ([(x, x, u)], [(x, buf[:9], u), (x, buf[8:17], u.clone())], [(x, buf[:9], buf[5:14])], [(x, None, u), (x[:7], None, u[1:8])],
+                [(x, None, u), (u, None, x.clone())]):
+        with pytest.raises(P.PuroError):
+            P.puro_muon_direction_grouped(bad, ws)
+    assert (x == 0).all() and (buf == 0).all()
