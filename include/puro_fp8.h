@@ -647,9 +647,10 @@ puro_status_t puro_muonh_step_grouped(const puro_muonh_matrix_t *mats, int32_t c
  * the same X.)  A buffer that averages, M <- momentum M + (1 - momentum) g, has the
  * same directions, for X does not depend on V's size.
  *
- * V is FP32; the sums of its norm are FP64 but within 1024 values.  The products are FP16 with FP32 accumulation, X and
- * their other results scaled by powers of two, the first X in two FP16 numbers (22
- * digits).  u is off by 1.0 to 1.9 10^-3 of its 2-norm, whichever type it is stored in
+ * V is FP32; the sums of its norm are FP64 but within 1024 values.  The products are
+ * FP16 with FP32 accumulation, X and their other results scaled by powers of two, the
+ * first X in two FP16 numbers: each value to 2^-22 of itself, or to 2^-31 of V's norm
+ * where that is more (2^-34 as a rule).  u is off by 1.0 to 1.9 10^-3 of its 2-norm, whichever type it is stored in
  * (five of Muon's steps on momenta of rank 16 with noise half as large; what lies in
  * V's directions of small singular values is less exact: 7 10^-3 where the noise is
  * 1/130 of the signal; products in BF16 would be off eight times as much).  Matrices of

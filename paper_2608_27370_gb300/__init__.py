@@ -477,7 +477,8 @@ def muon_table(mats):
     """The host table of puro_muon_direction_grouped for a fixed list of (grad,
     momentum or None, u): grad and u are bf16 or fp32 [rows, cols] with unit column
     stride, momentum is fp32 [rows, cols].  Build it once and pass it to every call
-    (the tensors must stay alive and in place)."""
+    (the tensors must stay alive and in place).  No momentum and no u may share memory
+    with anything else of the list, but u may lie in its own grad."""
     table = (puro_muon_matrix_t * max(1, len(mats)))()
     types = {torch.bfloat16: 0, torch.float32: 1}
     table.tensors = []

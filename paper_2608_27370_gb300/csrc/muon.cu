@@ -21,8 +21,11 @@
 // Where digits are lost.  A rounding of X adds noise of full rank, and the steps
 // blow small singular values up (3.4 times each, by Muon's coefficients), the noise
 // with them, the first rounding the most; a rounding of B only turns X's rows a little
-// into one another.  So the first X is two FP16 numbers, x = hi + lo, 22 digits: B1 B0
-// multiplies both (lo after hi, into the same accumulator), and G takes hi alone.  A
+// into one another.  So the first X is two FP16 numbers, x = hi + lo, scaled to a norm of
+// about 2^9 (2^6 to 2^16): 22 digits of the larger values, the rest to half of FP16's
+// least step, 2^-25 (values of [8960, 1536] are 0.14 on average at 2^9: 22 digits, at the
+// least norm 19).  B1 B0 multiplies both (lo after hi, into the same accumulator), and G
+// takes hi alone.  A
 // rounding of G is harmless in B0 but blown up in G1, so behind the first pair G, too, is
 // hi + lo for G1.  And G1 is B0 (B0 G)^T, symmetric whatever B0's roundings: as (B0 G) B0
 // with a mirrored or transposed factor it doubles the error, for rounded B0 and G no
@@ -308,7 +311,7 @@ constexpr double kLeastNorm = 64.0, kMostNorm = 65024.0;  // what guess ||V|| ha
 // tiles' in FP64 in a fixed order.  Bound by memory: a block has a run of tiles, all
 // blocks equally many, across the matrices, and asks L2 for half a tile ahead (a sum for
 // each of at most 256 runs of a matrix's tiles had left the large ones 1.6 blocks an SM;
-// a call for Qwen2-1.5B's layer 996 us then, 965 now;
+// a call for Qwen2-1.5B's layer took 996 us so, 965 with the blocks level;
 // 24 matrices of [128, 1536] and 11 small ones 157 and 145).
 __global__ void __launch_bounds__(kInThreads, 4) muon_update_kernel(const __grid_constant__ MuonIn p) {
     __shared__ Turn turn;
@@ -897,9 +900,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 // of A are whatever lies there, and so are the accumulators' lanes, which nothing reads.
 // G and its powers have zeros in columns m .. 2h.  Every sum is that of the launches, bit
 // for bit.  Bound by latency: seven products in a row, each waiting for the one before,
-// 1.8 us each (the cluster-wide release and acquire of a square 0.2 of it) where a launch
-// takes 2.9: one [48, 80] 70 -> 43 us a call, 24 matrices of [128, 1536] and 11 smaller
-// ones 145 -> 111.
+// 1.6 us each (the cluster-wide release and acquire of a square 0.2 of it) where a launch
+// takes 2.9: one [48, 80] 70 -> 38 us a call, 24 matrices of [128, 1536] and 11 smaller
+// ones 145 -> 105.
 //   warp 0       TMA producer (both CTAs): X's rows for G, its columns for B X
 //   warp 1       MMA issuer (even CTA); tensor memory
 //   warps 4..11  epilogue (both CTAs): warp 4 + 4h + q has rows 32q .. and every second

@@ -12,9 +12,10 @@
 // So a frequency is kept as the 64-bit integer F_i = w_i / (2 pi) 2^64, and p F_i
 // modulo 2^64 is the fraction of a turn in units of 2^-64: an integer product,
 // which wraps round where the angle does, loses nothing at far positions, and
-// needs neither 64-bit floating point nor tables in memory.  F_i is off by 2^-54 of
-// itself (a double's rounding), so the angle by 2 pi p 2^-54 w_i / (2 pi): 2^-23 at
-// position 2^31.
+// needs neither 64-bit floating point nor tables in memory.  F_i is made in doubles: the
+// power's argument, of which w_i is off by |ln w_i| 2^-53, at most four roundings of 2^-53
+// more, and the fraction cut off, one unit.  w |ln w| is at most 0.37, so the angle at
+// position 2^31 is within 2^-20 (2^-21.6 the worst of 750 tables of all scalings).
 #include <cuda_bf16.h>
 
 #include "internal.h"
